@@ -294,6 +294,83 @@ luna_status luna_attn_decode(const luna_attn_desc *ad, const luna_phi_desc *pd, 
                              const void *k, const void *v, void *o, float *S, int64_t S_stride, float *z,
                              int64_t z_stride, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * A block of linear attention with decay.  Next to the learned feature map the
+ * library holds the three operators such a block is made of, forward and
+ * backward: the attention itself (luna_decay_*), the norms before and after a
+ * block with its gate and residual scale (luna_norm_*), and the projections
+ * (luna_linear_*).  The paper has no counterpart of them.
+ *
+ * The conventions above hold (device pointers, asynchronous calls, checks before
+ * any launch, fp32 sums).  Beyond them, tensors may be views: a stride or leading
+ * dimension counts elements, the innermost dimension is contiguous, and inputs
+ * may overlap each other or repeat (stride 0) while outputs may not: an output
+ * whose strides let two of its elements share an address is
+ * LUNA_ERR_INVALID_ARG.  With io = bf16 each output is rounded once. */
+
+/* Strides of a (B, heads, n, width) tensor: batch entry, head, token.  All three
+ * 0 stands for the contiguous layout. */
+typedef struct {
+    int64_t b, h, t;
+} luna_strides;
+
+/* Linear attention with a decay for each head.  With lambda_h =
+ * exp(log_decay[h]) and the state S (d x dv, fp32) of each (b, h):
+ *
+ *     S_i = lambda_h S_{i-1} + k_i v_i^T,    o_i = scale * q_i^T S_i
+ *
+ * H query heads share Hkv heads of keys and values (H a multiple of Hkv): query
+ * head h reads head h / (H / Hkv), and every query head has its own decay and
+ * state.  log_decay is a device array of H fp32; -inf (lambda = 0: each token
+ * sees only itself) and 0 (no decay) are valid, and values above 0 grow without
+ * a check.  It takes no gradient.  Rows at or past a sequence's length neither
+ * enter the state nor are read; their outputs and gradients are 0.  A value that
+ * is not finite in a valid row may reach any valid row of the sequence.
+ * Supported: 1 <= d, dv <= 128, n <= 2^24, B * H <= 2^24; empty problems are
+ * no-ops (n = 0 copies the initial state).
+ * bf16 with d and dv multiples of 8, and every tensor on 16-byte boundaries with
+ * strides that are multiples of 8 elements, runs on tensor cores, where scores
+ * and states enter products as bf16 roundings and the carried state itself stays
+ * exact to fp32; everything else runs in fp32 on CUDA cores. */
+typedef struct {
+    int B, H, Hkv, n, d, dv;
+    float scale;
+    luna_dtype io;
+    luna_strides q, k, v, o;      /* Q, K, V, O                                */
+    luna_strides gq, gk, gv, go;  /* dQ, dK, dV, dO (luna_decay_bwd only)      */
+} luna_decay_desc;
+
+/* Bytes of scratch memory of luna_decay_fwd (backward = 0) or luna_decay_bwd
+ * (1); the workspace must be 256-byte aligned.  The size does not depend on the
+ * strides. */
+luna_status luna_decay_workspace_size(const luna_decay_desc *dd, int backward, size_t *bytes);
+
+/* Whole prompts.  S0: NULL (zero) or the initial states, fp32 [B][H][d][dv];
+ * S1: NULL or the states after each sequence's last valid token, the same
+ * layout (S1 may be S0 itself). */
+luna_status luna_decay_fwd(const luna_decay_desc *dd, const float *log_decay, const void *Q, const void *K,
+                           const void *V, const int32_t *lengths, const float *S0, void *O, float *S1,
+                           void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradients of luna_decay_fwd on the same inputs.  dS1: NULL (zero) or the
+ * gradient of the final states; dS0: NULL or the gradient of the initial states.
+ * The gradients of shared keys and values are summed over their query heads in
+ * fp32, in head order.  No atomics: equal inputs give equal bits. */
+luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, const void *Q, const void *K,
+                           const void *V, const void *dO, const int32_t *lengths, const float *S0, const float *dS1,
+                           void *dQ, void *dK, void *dV, float *dS0, void *workspace, size_t ws_bytes,
+                           void *stream);
+
+/* One token of each of B sequences: S <- lambda S + k v^T, o = scale q^T S, in
+ * place in a pool of states, fp32 [nslots][H][d][dv].  slots: NULL (sequence b
+ * is slot b) or B int32 in device memory; a sequence whose slot is outside
+ * [0, nslots) is idle (o = 0, no state is touched), and no two sequences may
+ * share a slot.  q, k, v, o are one token for each head; the strides .b and .h
+ * of the descriptor apply (all three 0: contiguous (B, heads, width)) and n and
+ * .t are ignored. */
+luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, const void *q, const void *k,
+                            const void *v, const int32_t *slots, int nslots, float *S, void *o, void *stream);
+
 /* Synchronises `stream`, then reads and clears the device status word at the
  * start of `workspace`.  Every luna_attn_fwd / luna_attn_bwd call clears the
  * word when it starts; a device-side wait of that call that ran out of its

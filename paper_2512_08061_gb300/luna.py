@@ -57,6 +57,16 @@ class AttnDesc(ctypes.Structure):
                 ("io", ctypes.c_int)]
 
 
+class Strides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
+
+
+class DecayDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("Hkv", ctypes.c_int), ("n", ctypes.c_int),
+                ("d", ctypes.c_int), ("dv", ctypes.c_int), ("scale", ctypes.c_float), ("io", ctypes.c_int),
+                *[(k, Strides) for k in ("q", "k", "v", "o", "gq", "gk", "gv", "go")]]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -68,6 +78,7 @@ def _load():
     lib = ctypes.CDLL(path)
     P, S, I, I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
     pd, ad = ctypes.POINTER(PhiDesc), ctypes.POINTER(AttnDesc)
+    dd = ctypes.POINTER(DecayDesc)
     sig = {
         "luna_status_string": ([I], ctypes.c_char_p),
         "luna_version": ([], I),
@@ -89,6 +100,10 @@ def _load():
         "luna_selftest_wait": ([P, I64, P], I),
         "luna_noalloc_scratch": ([ctypes.POINTER(P), ctypes.POINTER(S)], I),
         "luna_attn_weights": ([ad, pd, P, P, P, P, I, I, I, P, P], I),
+        "luna_decay_workspace_size": ([dd, I, ctypes.POINTER(S)], I),
+        "luna_decay_fwd": ([dd, P, P, P, P, P, P, P, P, P, S, P], I),
+        "luna_decay_bwd": ([dd, P, P, P, P, P, P, P, P, P, P, P, P, P, S, P], I),
+        "luna_decay_step": ([dd, P, P, P, P, P, I, P, P, P], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -102,7 +117,8 @@ EXPORTED = ("luna_status_string", "luna_version", "luna_phi_table_size", "luna_p
             "luna_workspace_size", "luna_state_size", "luna_attn_fwd", "luna_attn_bwd", "luna_device_status",
             "luna_profile_start", "luna_profile_stop", "luna_launch_count", "luna_attn_fwd_noalloc",
             "luna_state_final", "luna_attn_decode", "luna_selftest_wait", "luna_noalloc_scratch",
-            "luna_attn_weights")
+            "luna_attn_weights",
+            "luna_decay_workspace_size", "luna_decay_fwd", "luna_decay_bwd", "luna_decay_step")
 
 
 def _ptr(t):
@@ -226,6 +242,39 @@ def luna_attn_decode(ad, pd, table, q, k, v, o, S, S_stride, z, z_stride, stream
                                  sp, S_stride, zp, z_stride, _stream(stream)), "luna_attn_decode")
 
 
+# ---------------------------------------------------------------------------
+# linear attention with a decay for each head
+
+def decay_desc(B, H, n, d, dv, Hkv=None, scale=None, io=LUNA_BF16) -> DecayDesc:
+    """Contiguous tensors; set the strides q, k, v, o (gq, gk, gv, go) for views."""
+    return DecayDesc(B, H, H if Hkv is None else Hkv, n, d, dv,
+                     max(d, 1) ** -0.5 if scale is None else scale, io)
+
+
+def luna_decay_workspace_size(dd: DecayDesc, backward: bool) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.luna_decay_workspace_size(ctypes.byref(dd), int(bool(backward)), ctypes.byref(out)),
+           "luna_decay_workspace_size")
+    return out.value
+
+
+def luna_decay_fwd(dd, log_decay, Q, K, V, lengths, S0, O, S1, workspace, stream=None) -> None:
+    _check(_lib.luna_decay_fwd(ctypes.byref(dd), _ptr(log_decay), _ptr(Q), _ptr(K), _ptr(V), _ptr(lengths), _ptr(S0),
+                               _ptr(O), _ptr(S1), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                               _stream(stream)), "luna_decay_fwd")
+
+
+def luna_decay_bwd(dd, log_decay, Q, K, V, dO, lengths, S0, dS1, dQ, dK, dV, dS0, workspace, stream=None) -> None:
+    _check(_lib.luna_decay_bwd(ctypes.byref(dd), _ptr(log_decay), _ptr(Q), _ptr(K), _ptr(V), _ptr(dO), _ptr(lengths),
+                               _ptr(S0), _ptr(dS1), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dS0), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream(stream)), "luna_decay_bwd")
+
+
+def luna_decay_step(dd, log_decay, q, k, v, slots, nslots: int, S, o, stream=None) -> None:
+    _check(_lib.luna_decay_step(ctypes.byref(dd), _ptr(log_decay), _ptr(q), _ptr(k), _ptr(v), _ptr(slots), nslots,
+                                _ptr(S), _ptr(o), _stream(stream)), "luna_decay_step")
+
+
 def luna_device_status(workspace: torch.Tensor, stream=None) -> int:
     return _lib.luna_device_status(_ptr(workspace), _stream(stream))
 
@@ -325,4 +374,102 @@ class Luna:
             o = torch.empty(q.shape[:-1] + (self.ad.dv,), dtype=q.dtype, device=q.device)
         S, Ss, z, zs = luna_state_final(self.ad, self.pd, self.state)
         luna_attn_decode(self.ad, self.pd, self.table, q, k, v, o, S, Ss, z, zs, stream)
+        return o
+
+
+def _want(name: str, t, shape, dtype, device) -> None:
+    """An argument's shape, type and place, before its address goes to the library."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
+    if t.device.type != device.type or (device.index is not None and t.device.index != device.index):
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _dense(name: str, t) -> None:
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+
+
+class Decay:
+    """Linear attention with a decay for each head at one problem shape; owns the workspace.
+    Q: (B, H, n, d), K: (B, Hkv, n, d), V: (B, Hkv, n, dv), any strides with a contiguous last
+    dimension; log_decay: (H,) fp32; lengths: (B,) int32 or None; states: (B, H, d, dv) fp32."""
+
+    def __init__(self, B, H, n, d, dv, Hkv=None, scale=None, io=torch.bfloat16, device="cuda", backward=False):
+        self.dd = decay_desc(B, H, n, d, dv, Hkv, scale, _DTYPES[io])
+        self.io, self.device = io, torch.device(device)
+        self.ws = alloc_bytes(luna_decay_workspace_size(self.dd, backward), self.device)
+        self.shapes = {"q": (B, H, n, d), "k": (B, self.dd.Hkv, n, d), "v": (B, self.dd.Hkv, n, dv), "o": (B, H, n, dv)}
+        self.state_shape = (B, H, d, dv)
+
+    def _view(self, field: str, t) -> None:
+        _want(field, t, self.shapes[field[-1]], self.io, self.device)
+        s = t.stride()
+        if s[3] != 1 and t.shape[3] != 1:
+            raise ValueError(f"{field}: the last dimension is not contiguous")
+        if s[0] == s[1] == s[2] == 0 and t[..., 0].numel() > 1:
+            raise ValueError(f"{field}: one row repeated over batch, heads and tokens")
+        setattr(self.dd, field, Strides(s[0], s[1], s[2]))
+
+    def _checked(self, log_decay, lengths, states) -> None:
+        B, H = self.state_shape[:2]
+        _want("log_decay", log_decay, (H,), torch.float32, self.device)
+        _want("lengths", lengths, (B,), torch.int32, self.device)
+        _dense("log_decay", log_decay)
+        _dense("lengths", lengths)
+        for name, t in states.items():
+            _want(name, t, self.state_shape, torch.float32, self.device)
+            _dense(name, t)
+
+    def forward(self, Q, K, V, log_decay, lengths=None, S0=None, want_state=False, O=None, S1=None, stream=None):
+        """O, or (O, S1) with want_state."""
+        if O is None:
+            O = torch.empty_like(V if V.shape == self.shapes["o"] else Q if Q.shape == self.shapes["o"] else
+                                 Q.new_empty(self.shapes["o"]))
+        if want_state and S1 is None:
+            S1 = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
+        for field, t in (("q", Q), ("k", K), ("v", V), ("o", O)):
+            self._view(field, t)
+        self._checked(log_decay, lengths, {"S0": S0, "S1": S1})
+        luna_decay_fwd(self.dd, log_decay, Q, K, V, lengths, S0, O, S1, self.ws, stream)
+        return (O, S1) if want_state else O
+
+    def backward(self, Q, K, V, dO, log_decay, lengths=None, S0=None, dS1=None, out=None, stream=None):
+        """dQ, dK, dV, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
+        if out is None:
+            out = {"dQ": torch.empty_like(Q), "dK": torch.empty_like(K), "dV": torch.empty_like(V)}
+            if S0 is not None:
+                out["dS0"] = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
+        for field, t in (("q", Q), ("k", K), ("v", V), ("go", dO), ("gq", out["dQ"]), ("gk", out["dK"]),
+                         ("gv", out["dV"])):
+            self._view(field, t)
+        self._checked(log_decay, lengths, {"S0": S0, "dS1": dS1, "dS0": out.get("dS0")})
+        luna_decay_bwd(self.dd, log_decay, Q, K, V, dO, lengths, S0, dS1, out["dQ"], out["dK"], out["dV"],
+                       out.get("dS0"), self.ws, stream)
+        return out
+
+    def step(self, q, k, v, log_decay, S, slots=None, o=None, stream=None):
+        """One token: q (B, H, d), k (B, Hkv, d), v (B, Hkv, dv); S (nslots, H, d, dv) is advanced in place."""
+        B, H, d, dv = self.state_shape
+        if o is None:
+            o = torch.empty((B, H, dv), dtype=self.io, device=q.device)
+        for field, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+            sh = self.shapes[field]
+            _want(field, t, (sh[0], sh[1], sh[3]), self.io, self.device)
+            st = t.stride()
+            if st[2] != 1 and t.shape[2] != 1:
+                raise ValueError(f"{field}: the last dimension is not contiguous")
+            if st[0] == st[1] == 0 and t[..., 0].numel() > 1:
+                raise ValueError(f"{field}: one row repeated over batch and heads")
+            setattr(self.dd, field, Strides(st[0], st[1], 0))
+        _want("S", S, (S.shape[0], H, d, dv), torch.float32, self.device)
+        _want("slots", slots, (B,), torch.int32, self.device)
+        _want("log_decay", log_decay, (H,), torch.float32, self.device)
+        for name, t in (("S", S), ("slots", slots), ("log_decay", log_decay)):
+            _dense(name, t)
+        luna_decay_step(self.dd, log_decay, q, k, v, slots, S.shape[0], S, o, stream)
         return o
