@@ -371,6 +371,98 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
 luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, const void *q, const void *k,
                             const void *v, const int32_t *slots, int nslots, float *S, void *o, void *stream);
 
+/* The norms after and before a block, fused with its gate and its residual
+ * scale, over `rows` rows of `cols` values:
+ *
+ *     u  = norm(y) w_post + b_post    over each of `groups` equal groups of a row
+ *     x' = x + alpha * u * act(gate)
+ *     h  = norm(x') w_pre + b_pre     over the row
+ *
+ * norm(z) = z / sqrt(mean(z^2) + eps); the layer kind takes the mean of z out
+ * first.  Parts are chosen by their pointers: x NULL (no residual: x' = alpha u
+ * act(gate)), y NULL (x' = x, the norm before a first block), w_post NULL (u =
+ * y), w_pre NULL (no h), each b NULL (0), and the gate by `gate`.  One call is
+ * then a plain norm, the gated norm of an attention's heads (groups = H), or the
+ * step from one block's output to the next block's input.
+ * x, y, gate and their gradients, x' and h have the type io and a row stride
+ * (ld*, in elements; 0 = cols) of at least cols; weights and biases are fp32
+ * arrays of cols.  Statistics and sums are fp32; h is computed from x' before
+ * its rounding.
+ * Supported: cols <= 16384, rows < 2^31; rows = 0 is a no-op. */
+typedef enum { LUNA_NORM_RMS = 0, LUNA_NORM_LAYER = 1 } luna_norm_kind;
+typedef enum { LUNA_GATE_NONE = 0, LUNA_GATE_SIGMOID = 1, LUNA_GATE_SILU = 2 } luna_gate;
+
+typedef struct {
+    int64_t rows;
+    int cols, groups;
+    luna_norm_kind kind;
+    luna_gate gate;
+    float alpha, eps;
+    luna_dtype io;
+    int64_t ldx, ldy, ldgate, ldX, ldH;           /* x, y, gate, x', h            */
+    int64_t lddX, lddH, lddx, lddy, lddgate;      /* their gradients (backward)   */
+} luna_norm_desc;
+
+/* Bytes of the workspace of luna_norm_bwd (256-byte aligned; the weight
+ * gradients' partial sums). */
+luna_status luna_norm_workspace_size(const luna_norm_desc *nd, size_t *bytes);
+
+/* X (x') may be NULL where w_pre is given; H is required with w_pre and ignored
+ * without.  X and H may be x and y themselves (same strides). */
+luna_status luna_norm_fwd(const luna_norm_desc *nd, const void *x, const void *y, const void *gate,
+                          const float *w_post, const float *b_post, const float *w_pre, const float *b_pre, void *X,
+                          void *H, void *stream);
+
+/* Gradients from dX = dLoss/dx' (NULL: zero; required without w_pre) and dH =
+ * dLoss/dh (required with w_pre).  dx, dy, dgate are required where x, y, gate
+ * are given; the weight gradients dw_post, db_post, dw_pre, db_pre (fp32, cols,
+ * overwritten, summed over the rows in a fixed order) are written where not NULL
+ * (db_* also where that bias is absent).  The workspace is not needed without
+ * weight gradients. */
+luna_status luna_norm_bwd(const luna_norm_desc *nd, const void *x, const void *y, const void *gate,
+                          const float *w_post, const float *b_post, const float *w_pre, const void *dX, const void *dH,
+                          void *dx, void *dy, void *dgate, float *dw_post, float *db_post, float *dw_pre,
+                          float *db_pre, void *workspace, size_t ws_bytes, void *stream);
+
+/* Linear layers with their epilogue in the product:
+ *
+ *     z = X W^T + bias,   Y = act(z) + R
+ *
+ * X: m x k, W: n x k, bias: n values, R, Y, Z: m x n, all of type io, rows a
+ * leading dimension apart (ld*, in elements; 0 = the row's width, else at least
+ * that).  bias and R may be NULL; R may be Y.  Z, where not NULL, receives the
+ * pre-activation, which luna_linear_bwd needs with an activation.  GELU is the
+ * erf form.  Sums are fp32.
+ * bf16 with 16-byte aligned matrices and leading dimensions that are multiples
+ * of 8 runs on tensor cores; everything else in fp32 on CUDA cores.
+ * Supported: m <= 2^23, n, k <= 2^20; k = 0 sums nothing. */
+typedef enum {
+    LUNA_LINEAR_NONE = 0, LUNA_LINEAR_RELU = 1, LUNA_LINEAR_GELU = 2, LUNA_LINEAR_SILU = 3
+} luna_linear_act;
+
+typedef struct {
+    int64_t m;
+    int n, k;
+    luna_linear_act act;
+    luna_dtype io;
+    int64_t ldx, ldw, ldy, ldr, ldz;  /* X, W, Y, R, Z        */
+    int64_t lddy, lddx;               /* dY, dX (backward)    */
+} luna_linear_desc;
+
+/* Bytes of the workspace of luna_linear_fwd (backward = 0) or luna_linear_bwd
+ * (1): partial sums and, with an activation, dLoss/dz.  256-byte aligned. */
+luna_status luna_linear_workspace_size(const luna_linear_desc *ld, int backward, size_t *bytes);
+
+luna_status luna_linear_fwd(const luna_linear_desc *ld, const void *X, const void *W, const void *bias, const void *R,
+                            void *Y, void *Z, void *workspace, size_t ws_bytes, void *stream);
+
+/* dX = dz W, dW = dz^T X (contiguous n x k), db = the column sums of dz (n), with
+ * dz = dY act'(z); each is written where not NULL (the gradient of R is dY).
+ * The bias gradient sums dz before dz is rounded to io for the products.  No
+ * atomics: equal inputs give equal bits. */
+luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const void *W, const void *Z, const void *dY,
+                            void *dX, void *dW, void *db, void *workspace, size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, then reads and clears the device status word at the
  * start of `workspace`.  Every luna_attn_fwd / luna_attn_bwd call clears the
  * word when it starts; a device-side wait of that call that ran out of its

@@ -1,0 +1,75 @@
+// Matrix products with a fused epilogue: argument blocks and launchers.
+//
+//     out = act(A B^T + bias) + R,   A: M x K, B: N x K,   z = A B^T + bias kept where asked
+//
+// The three products of a linear layer are this one with other operands:
+//     forward  Y  (m x n): A = X (m x k),    B = W (n x k)
+//     backward dX (m x k): A = dZ (m x n),   B = W^T (k x n)
+//     backward dW (n x k): A = dZ^T (n x m), B = X^T (k x m)
+#pragma once
+
+#include "luna_common.cuh"
+
+namespace luna {
+
+struct MatView {           // element (row, k) at p[row * ld + k], or with kt at p[k * ld + row]
+    const void *p;
+    int64_t ld;
+    bool kt;
+};
+
+struct Product {
+    MatView A, B;
+    int64_t M, N, K;
+    const void *bias;      // N values, or NULL
+    int act;               // luna_linear_act
+    const void *R;         // residual M x N, or NULL
+    void *Z, *out;         // Z: pre-activation M x N, or NULL
+    int64_t ldr, ldz, ldo;
+    float *part;           // fp32 partial products [split][M][N]
+    size_t part_bytes;
+    int *status;           // device status word
+};
+
+__device__ __forceinline__ float linear_act(float z, int act) {
+    switch (act) {
+        case LUNA_LINEAR_RELU: return z > 0.0f ? z : (z == z ? 0.0f : z);
+        case LUNA_LINEAR_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+        case LUNA_LINEAR_SILU: return __fdividef(z, 1.0f + __expf(-z));
+    }
+    return z;
+}
+
+// d act / d z
+__device__ __forceinline__ float linear_slope(float z, int act) {
+    switch (act) {
+        case LUNA_LINEAR_RELU: return z > 0.0f ? 1.0f : 0.0f;
+        case LUNA_LINEAR_GELU:
+            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+        case LUNA_LINEAR_SILU: {
+            const float s = __fdividef(1.0f, 1.0f + __expf(-z));
+            return s * (1.0f + z * (1.0f - s));
+        }
+    }
+    return 1.0f;
+}
+
+// One output value from its sum: z = sum + bias (kept), act, residual.
+template <typename IO>
+__device__ __forceinline__ void linear_finish(const Product &p, int64_t row, int64_t col, float sum) {
+    if (p.bias) sum += io_load(static_cast<const IO *>(p.bias) + col);
+    if (p.Z) io_store(static_cast<IO *>(p.Z) + row * p.ldz + col, sum);
+    float y = linear_act(sum, p.act);
+    if (p.R) y += io_load(static_cast<const IO *>(p.R) + row * p.ldr + col);
+    io_store(static_cast<IO *>(p.out) + row * p.ldo + col, y);
+}
+
+// Pieces of K that a product of M x N x K is cut into on a launch of `tiles` blocks: enough to give
+// every SM a block, none under `least` of K, and no more than the partial buffer holds.
+int linear_splits(const Product &p, int64_t tiles, int64_t least);
+
+cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);          // picks a kernel
+cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
+cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);
+
+}  // namespace luna

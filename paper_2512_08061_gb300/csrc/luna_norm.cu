@@ -1,0 +1,781 @@
+// The norms after and before a block, fused with the block's gate and residual scale:
+//
+//     u = norm_g(y) w_post + b_post        (norm over each of the row's groups; or u = y)
+//     x' = x + alpha u act(gate)           (act: none, sigmoid or silu)
+//     h = norm(x') w_pre + b_pre           (norm over the row)
+//
+// norm(z) = z / sqrt(mean(z^2) + eps), with the mean of z taken out first for the layer kind.
+// Gradients of one row, from dX = dL/dx' and dH = dL/dh, with zhat = norm(z), r = 1 / root:
+//
+//     norm's input gradient from d (its output's):  r (d - zhat mean(d zhat) - [layer] mean(d))
+//     g = dX + that of dH w_pre;   dx = g;   dgate = alpha g u act'(gate);   du = alpha g act(gate)
+//     dy = that of du w_post;      dw_post = sum_rows du yhat;   dw_pre = sum_rows dH xhat
+//
+// The bytes bound both directions: every row is read once and written once, held in registers
+// between the reductions (the statistics are recomputed by the backward pass, which has to read
+// the same rows anyway), and the weight gradients are summed in registers over the rows of a
+// block and joined by a second small kernel in a fixed order.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "luna_common.cuh"
+#include "luna_prof.cuh"
+
+namespace luna {
+namespace {
+
+constexpr int kMaxCols = 16384;
+
+// Threads of a row at most: with one or two vectors a thread, small blocks (several an SM) forward and
+// blocks of 128 registers a thread backward; beyond that, what kMaxCols columns need.
+template <int VEC, int NV>
+constexpr int max_threads(bool backward) {
+    return VEC == 1 ? 1024 : NV < 4 ? (backward ? 512 : 256) : kMaxCols / VEC / NV;
+}
+
+struct NormArgs {
+    const void *x, *y, *gate, *dX, *dH;
+    void *X, *H, *dx, *dy, *dgate;
+    const float *w_post, *b_post, *w_pre, *b_pre;
+    float *part;       // [slot][array][cols]: weight-gradient partials (dw_post, db_post, dw_pre, db_pre)
+    int64_t rows;
+    int cols, groups, layer, act;
+    float alpha, eps;
+    int64_t ldx, ldy, ldgate, ldX, ldH, lddX, lddH, lddx, lddy, lddgate;
+    int gvec;          // vectors of a group
+    int gmode;         // how a group is summed: 0 whole row, 1 lanes of a warp, 2 through shared memory
+};
+
+template <typename IO, int VEC> struct Vec;
+template <> struct Vec<float, 4> {
+    static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
+        const float4 w = *reinterpret_cast<const float4 *>(p);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) {
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+};
+template <> struct Vec<__nv_bfloat16, 8> {
+    static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&v)[8]) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t b[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(b[i] << 16);
+            v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&v)[8]) {
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 w = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            memcpy(&b[i], &w, 4);
+        }
+        *reinterpret_cast<uint4 *>(p) = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+};
+template <typename IO> struct Vec<IO, 1> {
+    static __device__ __forceinline__ void load(const IO *p, float (&v)[1]) { v[0] = io_load(p); }
+    static __device__ __forceinline__ void store(IO *p, const float (&v)[1]) { io_store(p, v[0]); }
+};
+
+template <int VEC>
+__device__ __forceinline__ void load_w(const float *p, int c, float (&v)[VEC]) {
+    if (VEC == 1) {
+        v[0] = p[c];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) {
+            const float4 w = *reinterpret_cast<const float4 *>(p + c + i);
+            v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
+        }
+    }
+}
+
+// The threads of one row: a warp (eight rows a block) or the whole block.  Vector i of thread t is
+// number t + i * threads of the row.
+template <int NV>
+struct RowTeam {
+    int t, threads;     // this thread's number in the row, threads of the row
+    bool warp_row;
+    float *red;         // block rows: [2][32][2] sums of the warps
+    float *gsm;         // group sums through shared memory: [vectors][2] then [groups][2]
+    int nvec, buf;
+
+    __device__ __forceinline__ void sync() const {
+        if (warp_row) __syncwarp();
+        else __syncthreads();
+    }
+
+    // Sum of (a, b) over the row, to every thread.
+    __device__ __forceinline__ float2 row_sum(float2 v) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+            v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+        }
+        if (warp_row) return v;
+        float2 *r = reinterpret_cast<float2 *>(red) + 32 * buf;
+        buf ^= 1;  // the buffer after next is free: every thread has passed the barrier in between
+        if ((t & 31) == 0) r[t >> 5] = v;
+        __syncthreads();
+        float2 s = make_float2(0.f, 0.f);
+        for (int w = 0; w < threads / 32; ++w) { s.x += r[w].x; s.y += r[w].y; }
+        return s;
+    }
+
+    // Sums over each group of the thread's vectors (v in, sums of the vector's group out).
+    __device__ __forceinline__ void group_sum(float2 (&v)[NV], const NormArgs &a, const int (&grp)[NV]) {
+        if (a.gmode == 0) {
+            float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) { s.x += v[i].x; s.y += v[i].y; }
+            s = row_sum(s);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] = s;
+        } else if (a.gmode == 1) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                for (int o = a.gvec >> 1; o > 0; o >>= 1) {
+                    v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, o);
+                    v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, o);
+                }
+        } else {
+            float2 *p = reinterpret_cast<float2 *>(gsm), *g = p + nvec;
+            sync();  // the last call's sums have been read
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (t + i * threads < nvec) p[t + i * threads] = v[i];
+            sync();
+            for (int q = t >> 5; q < a.groups; q += threads / 32) {  // a warp for each group
+                float2 s = make_float2(0.f, 0.f);
+                for (int j = t & 31; j < a.gvec; j += 32) { s.x += p[q * a.gvec + j].x; s.y += p[q * a.gvec + j].y; }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
+                    s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
+                }
+                if ((t & 31) == 0) g[q] = s;
+            }
+            sync();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (t + i * threads < nvec) v[i] = g[grp[i]];
+        }
+    }
+};
+
+__device__ __forceinline__ float sigmoidf(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+
+template <int NV>
+__device__ __forceinline__ RowTeam<NV> make_team(const NormArgs &a, int nvec, float *sm) {
+    RowTeam<NV> t;
+    t.warp_row = blockDim.y > 1;
+    t.t = threadIdx.x;
+    t.threads = blockDim.x;
+    t.red = sm;
+    t.nvec = nvec;
+    t.gsm = sm + 128 + threadIdx.y * 2 * (nvec + a.groups);
+    t.buf = 0;
+    return t;
+}
+
+// z -> norm(z) over each group (or the row), in place; r[i] the reciprocal root of vector i's group.
+template <int VEC, int NV>
+__device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], RowTeam<NV> &tm, const NormArgs &a,
+                                          bool grouped, const int (&grp)[NV], int active) {
+    const float inv = 1.0f / (float)(grouped ? a.cols / a.groups : a.cols);
+    float2 s[NV];
+    auto sum = [&]() {
+        if (grouped) {
+            tm.group_sum(s, a, grp);
+        } else {
+            float2 q = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) { q.x += s[i].x; q.y += s[i].y; }
+            q = tm.row_sum(q);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i] = q;
+        }
+    };
+    if (a.layer) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            s[i] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s[i].x += z[i][e];
+        }
+        sum();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < active)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) z[i][e] -= s[i].x * inv;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        s[i] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[i].x = fmaf(z[i][e], z[i][e], s[i].x);
+    }
+    sum();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        r[i] = rsqrtf(fmaf(s[i].x, inv, a.eps));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) z[i][e] *= r[i];
+    }
+}
+
+template <typename IO, int VEC, int NV>
+__device__ __forceinline__ void load_row(const void *p, int64_t off, float (&v)[NV][VEC], int t, int threads, int active) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < active) {
+            Vec<IO, VEC>::load(static_cast<const IO *>(p) + off + (int64_t)(t + i * threads) * VEC, v[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[i][e] = 0.0f;
+        }
+}
+
+template <typename IO, int VEC, int NV>
+__device__ __forceinline__ void store_row(void *p, int64_t off, const float (&v)[NV][VEC], int t, int threads, int active) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < active) Vec<IO, VEC>::store(static_cast<IO *>(p) + off + (int64_t)(t + i * threads) * VEC, v[i]);
+}
+
+// Vectors of this thread (0 .. NV) and their groups.
+template <int VEC, int NV>
+__device__ __forceinline__ int my_vectors(const NormArgs &a, int nvec, int (&grp)[NV]) {
+    int active = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int q = threadIdx.x + i * blockDim.x;
+        if (q < nvec) active = i + 1;
+        grp[i] = a.gmode == 2 ? min(q / a.gvec, a.groups - 1) : 0;
+    }
+    return active;
+}
+
+template <typename IO, int VEC, int NV>
+__global__ void __launch_bounds__(max_threads<VEC, NV>(false)) k_norm_fwd(NormArgs a) {
+    extern __shared__ float sm[];
+    const int nvec = a.cols / VEC;
+    RowTeam<NV> tm = make_team<NV>(a, nvec, sm);
+    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (row >= a.rows) return;  // whole warps: a block with one row never gets here
+    int grp[NV];
+    const int active = my_vectors<VEC, NV>(a, nvec, grp);
+    float z[NV][VEC], x[NV][VEC], g[NV][VEC], r[NV];
+    if (a.x) load_row<IO, VEC, NV>(a.x, row * a.ldx, x, tm.t, tm.threads, active);
+    if (a.y) load_row<IO, VEC, NV>(a.y, row * a.ldy, z, tm.t, tm.threads, active);
+    if (a.gate) load_row<IO, VEC, NV>(a.gate, row * a.ldgate, g, tm.t, tm.threads, active);
+    if (a.y) {
+        if (a.w_post) {
+            normalise<VEC, NV>(z, r, tm, a, true, grp, active);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < active) {
+                    const int c = (tm.t + i * tm.threads) * VEC;
+                    float w[VEC];
+                    load_w<VEC>(a.w_post, c, w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
+                    if (a.b_post) {
+                        load_w<VEC>(a.b_post, c, w);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
+                    }
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float v = z[i][e];
+                if (a.gate && i < active) {
+                    const float sg = sigmoidf(g[i][e]);
+                    v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
+                }
+                z[i][e] = a.x ? fmaf(a.alpha, v, x[i][e]) : a.alpha * v;
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) z[i][e] = x[i][e];
+    }
+    if (a.X) store_row<IO, VEC, NV>(a.X, row * a.ldX, z, tm.t, tm.threads, active);
+    if (a.w_pre) {
+        normalise<VEC, NV>(z, r, tm, a, false, grp, active);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < active) {
+                const int c = (tm.t + i * tm.threads) * VEC;
+                float w[VEC];
+                load_w<VEC>(a.w_pre, c, w);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
+                if (a.b_pre) {
+                    load_w<VEC>(a.b_pre, c, w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
+                }
+            }
+        store_row<IO, VEC, NV>(a.H, row * a.ldH, z, tm.t, tm.threads, active);
+    }
+}
+
+// d -> the gradient of norm's input: r (d - zhat mean(d zhat) - [layer] mean(d)).
+template <int VEC, int NV>
+__device__ __forceinline__ void normalise_grad(float (&d)[NV][VEC], const float (&zhat)[NV][VEC], const float (&r)[NV],
+                                               RowTeam<NV> &tm, const NormArgs &a, bool grouped, const int (&grp)[NV],
+                                               int active) {
+    const int count = grouped ? a.cols / a.groups : a.cols;
+    if (count == 1) {  // the difference below cancels to r d (1 - zhat^2) = r d eps r^2, or to 0 without the mean
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[i][e] = a.layer ? 0.0f : d[i][e] * r[i] * (a.eps * r[i] * r[i]);
+        return;
+    }
+    const float inv = 1.0f / (float)count;
+    float2 s[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        s[i] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            s[i].x = fmaf(d[i][e], zhat[i][e], s[i].x);
+            s[i].y += d[i][e];
+        }
+    }
+    if (grouped) {
+        tm.group_sum(s, a, grp);
+    } else {
+        float2 q = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { q.x += s[i].x; q.y += s[i].y; }
+        q = tm.row_sum(q);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s[i] = q;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const float mz = s[i].x * inv, md = a.layer ? s[i].y * inv : 0.0f;
+        if (i < active)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[i][e] = r[i] * (d[i][e] - md - zhat[i][e] * mz);
+    }
+}
+
+// BIAS: the biases' gradients are summed too.
+template <typename IO, int VEC, int NV, bool BIAS>
+__global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArgs a) {
+    extern __shared__ float sm[];
+    const int nvec = a.cols / VEC;
+    RowTeam<NV> tm = make_team<NV>(a, nvec, sm);
+    int grp[NV];
+    const int active = my_vectors<VEC, NV>(a, nvec, grp);
+    const int t = tm.t, T = tm.threads;
+    float sw_post[NV][VEC], sw_pre[NV][VEC], sb_post[BIAS ? NV : 1][VEC], sb_pre[BIAS ? NV : 1][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            sw_post[i][e] = sw_pre[i][e] = 0.0f;
+            if (BIAS) sb_post[i][e] = sb_pre[i][e] = 0.0f;
+        }
+    const int64_t slots = (int64_t)gridDim.x * blockDim.y, slot = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    for (int64_t row = slot; row < a.rows; row += slots) {
+        float z[NV][VEC], g[NV][VEC], x[NV][VEC], d[NV][VEC], ry[NV], rx[NV];
+        if (a.y) load_row<IO, VEC, NV>(a.y, row * a.ldy, z, t, T, active);
+        if (a.gate) load_row<IO, VEC, NV>(a.gate, row * a.ldgate, g, t, T, active);
+        if (a.x) load_row<IO, VEC, NV>(a.x, row * a.ldx, x, t, T, active);
+        if (a.dX) {
+            load_row<IO, VEC, NV>(a.dX, row * a.lddX, d, t, T, active);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[i][e] = 0.0f;
+        }
+        float dh[NV][VEC];
+        if (a.w_pre) load_row<IO, VEC, NV>(a.dH, row * a.lddH, dh, t, T, active);
+        if (a.y && a.w_post) normalise<VEC, NV>(z, ry, tm, a, true, grp, active);
+        // u of vector i (post-norm output, before the gate)
+        auto u_of = [&](int i, float (&u)[VEC]) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) u[e] = z[i][e];
+            if (a.w_post) {
+                const int c = (t + i * T) * VEC;
+                float w[VEC];
+                load_w<VEC>(a.w_post, c, w);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) u[e] *= w[e];
+                if (a.b_post) {
+                    load_w<VEC>(a.b_post, c, w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) u[e] += w[e];
+                }
+            }
+        };
+        if (a.w_pre) {
+            if (!a.x) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) x[i][e] = 0.0f;
+            }
+            if (a.y) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (i < active) {
+                        float u[VEC];
+                        u_of(i, u);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            float v = u[e];
+                            if (a.gate) {
+                                const float sg = sigmoidf(g[i][e]);
+                                v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
+                            }
+                            x[i][e] = fmaf(a.alpha, v, x[i][e]);
+                        }
+                    }
+            }
+            normalise<VEC, NV>(x, rx, tm, a, false, grp, active);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < active) {
+                    float w[VEC];
+                    load_w<VEC>(a.w_pre, (t + i * T) * VEC, w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        sw_pre[i][e] = fmaf(dh[i][e], x[i][e], sw_pre[i][e]);
+                        if (BIAS) sb_pre[i][e] += dh[i][e];
+                        dh[i][e] *= w[e];
+                    }
+                }
+            normalise_grad<VEC, NV>(dh, x, rx, tm, a, false, grp, active);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[i][e] += dh[i][e];
+        }
+        if (a.dx) store_row<IO, VEC, NV>(a.dx, row * a.lddx, d, t, T, active);
+        if (!a.y) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < active) {
+                float dg[VEC];
+                if (a.gate) {
+                    float u[VEC];
+                    u_of(i, u);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float sg = sigmoidf(g[i][e]), dt = a.alpha * d[i][e];
+                        const float act = a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
+                        const float slope = a.act == LUNA_GATE_SILU ? sg * (1.0f + g[i][e] * (1.0f - sg)) : sg * (1.0f - sg);
+                        dg[e] = dt * u[e] * slope;
+                        d[i][e] = dt * act;
+                    }
+                    Vec<IO, VEC>::store(static_cast<IO *>(a.dgate) + row * a.lddgate + (int64_t)(t + i * T) * VEC, dg);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) d[i][e] *= a.alpha;
+                }
+                if (a.w_post) {
+                    float w[VEC];
+                    load_w<VEC>(a.w_post, (t + i * T) * VEC, w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        sw_post[i][e] = fmaf(d[i][e], z[i][e], sw_post[i][e]);
+                        if (BIAS) sb_post[i][e] += d[i][e];
+                        d[i][e] *= w[e];
+                    }
+                }
+            }
+        if (a.w_post) normalise_grad<VEC, NV>(d, z, ry, tm, a, true, grp, active);
+        store_row<IO, VEC, NV>(a.dy, row * a.lddy, d, t, T, active);
+    }
+    // this slot's sums: [dw_post | dw_pre | db_post | db_pre] of a row's columns
+    if (a.part) {
+        float *p = a.part + slot * (BIAS ? 4 : 2) * a.cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < active)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int c = (t + i * T) * VEC + e;
+                    p[c] = sw_post[i][e];
+                    p[a.cols + c] = sw_pre[i][e];
+                    if (BIAS) {
+                        p[2 * a.cols + c] = sb_post[i][e];
+                        p[3 * a.cols + c] = sb_pre[i][e];
+                    }
+                }
+    }
+}
+
+struct NormSum {
+    const float *part;
+    float *out[4];
+    int slots, arrays, cols;
+};
+
+// Sums the slots of 32 columns of one array: eight warps take slots w, w + 8, ..., joined in order.
+__global__ void __launch_bounds__(256) k_norm_sum(NormSum a) {
+    __shared__ float s[8][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, arr = blockIdx.y;
+    float *out = a.out[arr];
+    if (!out) return;
+    float acc = 0.0f;
+    if (c < a.cols) {
+        const float *p = a.part + (int64_t)arr * a.cols + c;
+#pragma unroll 4
+        for (int i = w; i < a.slots; i += 8) acc += p[(int64_t)i * a.arrays * a.cols];
+    }
+    s[w][lane] = acc;
+    __syncthreads();
+    if (w == 0 && c < a.cols) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) acc += s[i][lane];
+        out[c] = acc;
+    }
+}
+
+// ---------------------------------------------------------------------------
+
+struct Shape {
+    int vec, nv, threads, rows_per_block;
+    size_t smem;
+};
+
+// Vectors of a thread and threads of a row.  A row of at most 32 vectors is a warp's.
+Shape shape_of(int cols, bool vectors, int vec_io, bool backward) {
+    Shape s;
+    s.vec = vectors ? vec_io : 1;
+    const int nvec = cols / s.vec;
+    if (vectors) {
+        const int most = backward ? 512 : 256;
+        s.nv = nvec <= most ? 1 : nvec <= 2 * most ? 2 : 4;
+    } else {
+        s.nv = cols <= 4096 ? 4 : 16;
+    }
+    s.threads = ((nvec + s.nv - 1) / s.nv + 31) / 32 * 32;
+    s.rows_per_block = s.threads == 32 ? 8 : 1;
+    s.smem = sizeof(float) * 128;
+    return s;
+}
+
+void group_mode(NormArgs &a, Shape &s) {
+    a.gmode = 0;
+    a.gvec = a.cols / s.vec / a.groups;
+    if (a.w_post && a.groups > 1) {
+        a.gmode = a.gvec <= 32 && (a.gvec & (a.gvec - 1)) == 0 ? 1 : 2;
+        if (a.gmode == 2) s.smem += sizeof(float) * 2 * s.rows_per_block * (a.cols / s.vec + a.groups);
+    }
+}
+
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+bool vectors_ok(const NormArgs &a, int vec) {
+    if (a.cols % vec || (a.w_post && (a.cols / a.groups) % vec)) return false;
+    for (const void *p : {a.x, a.y, a.gate, a.dX, a.dH, (const void *)a.X, (const void *)a.H, (const void *)a.dx,
+                          (const void *)a.dy, (const void *)a.dgate, (const void *)a.w_post, (const void *)a.b_post,
+                          (const void *)a.w_pre, (const void *)a.b_pre})
+        if (!al16(p)) return false;
+    for (int64_t ld : {a.ldx, a.ldy, a.ldgate, a.ldX, a.ldH, a.lddX, a.lddH, a.lddx, a.lddy, a.lddgate})
+        if (ld % vec) return false;
+    return true;
+}
+
+template <typename K>
+cudaError_t big_smem(K kernel, size_t smem) {
+    if (smem <= 48 * 1024) return cudaSuccess;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
+template <typename IO, int VEC, int NV>
+cudaError_t fwd_launch(const NormArgs &a, const Shape &sh, cudaStream_t s) {
+    cudaError_t e = big_smem(k_norm_fwd<IO, VEC, NV>, sh.smem);
+    if (e != cudaSuccess) return e;
+    const unsigned grid = (unsigned)((a.rows + sh.rows_per_block - 1) / sh.rows_per_block);
+    LUNA_LAUNCH("norm_fwd", (k_norm_fwd<IO, VEC, NV>), grid, dim3(sh.threads, sh.rows_per_block), sh.smem, s, a);
+    return cudaGetLastError();
+}
+
+template <typename IO, int VECIO>
+cudaError_t fwd(NormArgs a, cudaStream_t s) {
+    const bool v = vectors_ok(a, VECIO);
+    Shape sh = shape_of(a.cols, v, VECIO, false);
+    group_mode(a, sh);
+    if (v) {
+        if (sh.nv == 1) return fwd_launch<IO, VECIO, 1>(a, sh, s);
+        if (sh.nv == 2) return fwd_launch<IO, VECIO, 2>(a, sh, s);
+        return fwd_launch<IO, VECIO, 4>(a, sh, s);
+    }
+    if (sh.nv == 4) return fwd_launch<IO, 1, 4>(a, sh, s);
+    return fwd_launch<IO, 1, 16>(a, sh, s);
+}
+
+// Blocks of the backward pass: each sums its rows' weight gradients in registers, so no more than
+// fill the device (512 threads an SM).
+int bwd_grid(int64_t rows, const Shape &sh) {
+    const int64_t blocks = (int64_t)152 * std::max(1, 512 / (sh.threads * sh.rows_per_block));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, (rows + sh.rows_per_block - 1) / sh.rows_per_block));
+}
+
+template <typename IO, int VEC, int NV, bool BIAS>
+cudaError_t bwd_launch(const NormArgs &a, const Shape &sh, int grid, cudaStream_t s) {
+    cudaError_t e = big_smem(k_norm_bwd<IO, VEC, NV, BIAS>, sh.smem);
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("norm_bwd", (k_norm_bwd<IO, VEC, NV, BIAS>), grid, dim3(sh.threads, sh.rows_per_block), sh.smem, s, a);
+    return cudaGetLastError();
+}
+
+template <typename IO, int VECIO, bool BIAS>
+cudaError_t bwd(NormArgs a, float *const (&out)[4], cudaStream_t s) {
+    const bool v = vectors_ok(a, VECIO);
+    Shape sh = shape_of(a.cols, v, VECIO, true);
+    group_mode(a, sh);
+    const int grid = bwd_grid(a.rows, sh);
+    cudaError_t e;
+    if (v) {
+        if (sh.nv == 1) e = bwd_launch<IO, VECIO, 1, BIAS>(a, sh, grid, s);
+        else if (sh.nv == 2) e = bwd_launch<IO, VECIO, 2, BIAS>(a, sh, grid, s);
+        else e = bwd_launch<IO, VECIO, 4, BIAS>(a, sh, grid, s);
+    } else {
+        if (sh.nv == 4) e = bwd_launch<IO, 1, 4, BIAS>(a, sh, grid, s);
+        else e = bwd_launch<IO, 1, 16, BIAS>(a, sh, grid, s);
+    }
+    if (e != cudaSuccess || !a.part) return e;
+    NormSum n{a.part, {out[0], out[1], out[2], out[3]}, grid * sh.rows_per_block, BIAS ? 4 : 2, a.cols};
+    LUNA_LAUNCH("norm_sum", k_norm_sum, dim3((a.cols + 31) / 32, BIAS ? 4 : 2), 256, 0, s, n);
+    return cudaGetLastError();
+}
+
+luna_status check(const luna_norm_desc *nd) {
+    if (!nd) return LUNA_ERR_INVALID_ARG;
+    if (nd->rows < 0 || nd->cols < 1 || nd->groups < 1 || nd->cols % nd->groups) return LUNA_ERR_INVALID_ARG;
+    if (nd->kind != LUNA_NORM_RMS && nd->kind != LUNA_NORM_LAYER) return LUNA_ERR_INVALID_ARG;
+    if (nd->gate < LUNA_GATE_NONE || nd->gate > LUNA_GATE_SILU) return LUNA_ERR_INVALID_ARG;
+    if (nd->io != LUNA_F32 && nd->io != LUNA_BF16) return LUNA_ERR_INVALID_ARG;
+    if (!(nd->eps >= 0.0f) || isinf(nd->eps) || !isfinite(nd->alpha)) return LUNA_ERR_INVALID_ARG;
+    for (int64_t ld : {nd->ldx, nd->ldy, nd->ldgate, nd->ldX, nd->ldH, nd->lddX, nd->lddH, nd->lddx, nd->lddy, nd->lddgate})
+        if (ld != 0 && ld < nd->cols) return LUNA_ERR_INVALID_ARG;
+    if (nd->cols > kMaxCols || nd->rows > (int64_t(1) << 31) - 1) return LUNA_ERR_UNSUPPORTED;
+    return LUNA_OK;
+}
+
+NormArgs args(const luna_norm_desc *nd, const void *x, const void *y, const void *gate, const float *w_post,
+              const float *b_post, const float *w_pre, const float *b_pre) {
+    NormArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = x; a.y = y;
+    a.gate = nd->gate == LUNA_GATE_NONE ? nullptr : gate;
+    a.w_post = w_post; a.b_post = b_post; a.w_pre = w_pre; a.b_pre = b_pre;
+    a.rows = nd->rows; a.cols = nd->cols; a.groups = nd->groups;
+    a.layer = nd->kind == LUNA_NORM_LAYER; a.act = nd->gate;
+    a.alpha = nd->alpha; a.eps = nd->eps;
+    auto ld = [&](int64_t v) { return v ? v : (int64_t)nd->cols; };
+    a.ldx = ld(nd->ldx); a.ldy = ld(nd->ldy); a.ldgate = ld(nd->ldgate); a.ldX = ld(nd->ldX); a.ldH = ld(nd->ldH);
+    a.lddX = ld(nd->lddX); a.lddH = ld(nd->lddH); a.lddx = ld(nd->lddx); a.lddy = ld(nd->lddy);
+    a.lddgate = ld(nd->lddgate);
+    return a;
+}
+
+// The combinations a call may ask for: something to norm or add, a gate and a post-norm only with y.
+bool combination_ok(const luna_norm_desc *nd, const void *x, const void *y, const void *gate, const float *w_post,
+                    const float *b_post, const float *w_pre, const float *b_pre) {
+    if (!x && !y) return false;
+    if (!y && (w_post || nd->gate != LUNA_GATE_NONE)) return false;
+    if (nd->gate != LUNA_GATE_NONE && !gate) return false;
+    if ((b_post && !w_post) || (b_pre && !w_pre)) return false;
+    return true;
+}
+
+// The partial sums of the launch shape with vectors or without, whichever has more.
+size_t partial_bytes(const luna_norm_desc *nd) {
+    size_t slots = 0;
+    for (bool v : {false, true}) {
+        const Shape sh = shape_of(nd->cols, v, nd->io == LUNA_F32 ? 4 : 8, true);
+        slots = std::max(slots, (size_t)bwd_grid(nd->rows, sh) * sh.rows_per_block);
+    }
+    return slots * 4 * nd->cols * sizeof(float);
+}
+
+luna_status cuda_status(cudaError_t e) { return e == cudaSuccess ? LUNA_OK : LUNA_ERR_CUDA; }
+
+}  // namespace
+}  // namespace luna
+
+using namespace luna;
+
+extern "C" {
+
+luna_status luna_norm_workspace_size(const luna_norm_desc *nd, size_t *bytes) {
+    if (!bytes) return LUNA_ERR_INVALID_ARG;
+    const luna_status st = check(nd);
+    if (st != LUNA_OK) return st;
+    *bytes = nd->rows ? (size_t)align256((int64_t)partial_bytes(nd)) : 256;
+    return LUNA_OK;
+}
+
+luna_status luna_norm_fwd(const luna_norm_desc *nd, const void *x, const void *y, const void *gate,
+                          const float *w_post, const float *b_post, const float *w_pre, const float *b_pre, void *X,
+                          void *H, void *stream) {
+    const luna_status st = check(nd);
+    if (st != LUNA_OK) return st;
+    if (nd->rows == 0) return LUNA_OK;
+    if (!combination_ok(nd, x, y, gate, w_post, b_post, w_pre, b_pre)) return LUNA_ERR_INVALID_ARG;
+    if ((w_pre && !H) || (!w_pre && !X)) return LUNA_ERR_INVALID_ARG;
+    NormArgs a = args(nd, x, y, gate, w_post, b_post, w_pre, b_pre);
+    a.X = X;
+    a.H = w_pre ? H : nullptr;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return cuda_status(nd->io == LUNA_F32 ? fwd<float, 4>(a, s) : fwd<__nv_bfloat16, 8>(a, s));
+}
+
+luna_status luna_norm_bwd(const luna_norm_desc *nd, const void *x, const void *y, const void *gate,
+                          const float *w_post, const float *b_post, const float *w_pre, const void *dX, const void *dH,
+                          void *dx, void *dy, void *dgate, float *dw_post, float *db_post, float *dw_pre,
+                          float *db_pre, void *workspace, size_t ws_bytes, void *stream) {
+    const luna_status st = check(nd);
+    if (st != LUNA_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    float *const out[4] = {dw_post, dw_pre, db_post, db_pre};
+    if (nd->rows == 0) {  // sums over no rows
+        for (float *p : out)
+            if (p && cudaMemsetAsync(p, 0, sizeof(float) * nd->cols, s) != cudaSuccess) return LUNA_ERR_CUDA;
+        return LUNA_OK;
+    }
+    if (!combination_ok(nd, x, y, gate, w_post, b_post, w_pre, nullptr)) return LUNA_ERR_INVALID_ARG;
+    if ((w_pre && !dH) || (!w_pre && !dX)) return LUNA_ERR_INVALID_ARG;
+    if ((x && !dx) || (y && !dy) || (nd->gate != LUNA_GATE_NONE && !dgate)) return LUNA_ERR_INVALID_ARG;
+    if (((dw_post || db_post) && !w_post) || ((dw_pre || db_pre) && !w_pre)) return LUNA_ERR_INVALID_ARG;
+    const bool sums = dw_post || db_post || dw_pre || db_pre;
+    if (sums && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))) return LUNA_ERR_INVALID_ARG;
+    if (sums && ws_bytes < partial_bytes(nd)) return LUNA_ERR_WORKSPACE;
+    NormArgs a = args(nd, x, y, gate, w_post, b_post, w_pre, nullptr);
+    a.dX = dX;
+    a.dH = w_pre ? dH : nullptr;
+    a.dx = x ? dx : nullptr; a.dy = y ? dy : nullptr; a.dgate = a.gate ? dgate : nullptr;
+    a.part = sums ? static_cast<float *>(workspace) : nullptr;
+    const bool bias = db_post || db_pre;
+    cudaError_t e;
+    if (nd->io == LUNA_F32)
+        e = bias ? bwd<float, 4, true>(a, out, s) : bwd<float, 4, false>(a, out, s);
+    else
+        e = bias ? bwd<__nv_bfloat16, 8, true>(a, out, s) : bwd<__nv_bfloat16, 8, false>(a, out, s);
+    return cuda_status(e);
+}
+
+}  // extern "C"

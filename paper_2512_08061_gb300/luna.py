@@ -67,6 +67,25 @@ class DecayDesc(ctypes.Structure):
                 *[(k, Strides) for k in ("q", "k", "v", "o", "gq", "gk", "gv", "go")]]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int), ("groups", ctypes.c_int), ("kind", ctypes.c_int),
+                ("gate", ctypes.c_int), ("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("io", ctypes.c_int),
+                *[(k, ctypes.c_int64) for k in ("ldx", "ldy", "ldgate", "ldX", "ldH", "lddX", "lddH", "lddx", "lddy",
+                                                "lddgate")]]
+
+
+NORM_KINDS = {"rms": 0, "layer": 1}  # luna_norm_kind
+GATES = {"none": 0, "sigmoid": 1, "silu": 2}  # luna_gate
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int), ("k", ctypes.c_int), ("act", ctypes.c_int),
+                ("io", ctypes.c_int), *[(k, ctypes.c_int64) for k in ("ldx", "ldw", "ldy", "ldr", "ldz", "lddy", "lddx")]]
+
+
+LINEAR_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}  # luna_linear_act
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -78,7 +97,7 @@ def _load():
     lib = ctypes.CDLL(path)
     P, S, I, I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
     pd, ad = ctypes.POINTER(PhiDesc), ctypes.POINTER(AttnDesc)
-    dd = ctypes.POINTER(DecayDesc)
+    dd, nd, ld = ctypes.POINTER(DecayDesc), ctypes.POINTER(NormDesc), ctypes.POINTER(LinearDesc)
     sig = {
         "luna_status_string": ([I], ctypes.c_char_p),
         "luna_version": ([], I),
@@ -104,6 +123,12 @@ def _load():
         "luna_decay_fwd": ([dd, P, P, P, P, P, P, P, P, P, S, P], I),
         "luna_decay_bwd": ([dd, P, P, P, P, P, P, P, P, P, P, P, P, P, S, P], I),
         "luna_decay_step": ([dd, P, P, P, P, P, I, P, P, P], I),
+        "luna_norm_workspace_size": ([nd, ctypes.POINTER(S)], I),
+        "luna_norm_fwd": ([nd] + [P] * 10, I),
+        "luna_norm_bwd": ([nd] + [P] * 16 + [S, P], I),
+        "luna_linear_workspace_size": ([ld, I, ctypes.POINTER(S)], I),
+        "luna_linear_fwd": ([ld] + [P] * 7 + [S, P], I),
+        "luna_linear_bwd": ([ld] + [P] * 8 + [S, P], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -118,7 +143,9 @@ EXPORTED = ("luna_status_string", "luna_version", "luna_phi_table_size", "luna_p
             "luna_profile_start", "luna_profile_stop", "luna_launch_count", "luna_attn_fwd_noalloc",
             "luna_state_final", "luna_attn_decode", "luna_selftest_wait", "luna_noalloc_scratch",
             "luna_attn_weights",
-            "luna_decay_workspace_size", "luna_decay_fwd", "luna_decay_bwd", "luna_decay_step")
+            "luna_decay_workspace_size", "luna_decay_fwd", "luna_decay_bwd", "luna_decay_step",
+            "luna_norm_workspace_size", "luna_norm_fwd", "luna_norm_bwd",
+            "luna_linear_workspace_size", "luna_linear_fwd", "luna_linear_bwd")
 
 
 def _ptr(t):
@@ -273,6 +300,58 @@ def luna_decay_bwd(dd, log_decay, Q, K, V, dO, lengths, S0, dS1, dQ, dK, dV, dS0
 def luna_decay_step(dd, log_decay, q, k, v, slots, nslots: int, S, o, stream=None) -> None:
     _check(_lib.luna_decay_step(ctypes.byref(dd), _ptr(log_decay), _ptr(q), _ptr(k), _ptr(v), _ptr(slots), nslots,
                                 _ptr(S), _ptr(o), _stream(stream)), "luna_decay_step")
+
+
+# ---------------------------------------------------------------------------
+# norms after and before a block, with its gate and residual scale
+
+def norm_desc(rows, cols, groups=1, kind="rms", gate="none", res_scale=1.0, eps=1e-6, io=LUNA_BF16) -> NormDesc:
+    return NormDesc(rows, cols, groups, NORM_KINDS[kind], GATES[gate], res_scale, eps, io)
+
+
+def luna_norm_workspace_size(nd: NormDesc) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.luna_norm_workspace_size(ctypes.byref(nd), ctypes.byref(out)), "luna_norm_workspace_size")
+    return out.value
+
+
+def luna_norm_fwd(nd, x, y, gate, w_post, b_post, w_pre, b_pre, X, H, stream=None) -> None:
+    _check(_lib.luna_norm_fwd(ctypes.byref(nd), _ptr(x), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre),
+                              _ptr(b_pre), _ptr(X), _ptr(H), _stream(stream)), "luna_norm_fwd")
+
+
+def luna_norm_bwd(nd, x, y, gate, w_post, b_post, w_pre, dX, dH, dx, dy, dgate, dw_post, db_post, dw_pre, db_pre,
+                  workspace, stream=None) -> None:
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.luna_norm_bwd(ctypes.byref(nd), _ptr(x), _ptr(y), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre),
+                              _ptr(dX), _ptr(dH), _ptr(dx), _ptr(dy), _ptr(dgate), _ptr(dw_post), _ptr(db_post),
+                              _ptr(dw_pre), _ptr(db_pre), _ptr(workspace), nbytes, _stream(stream)), "luna_norm_bwd")
+
+
+# ---------------------------------------------------------------------------
+# linear layers
+
+def linear_desc(m, n, k, act="none", io=LUNA_BF16) -> LinearDesc:
+    return LinearDesc(m, n, k, LINEAR_ACTS[act], io)
+
+
+def luna_linear_workspace_size(ld: LinearDesc, backward: bool) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.luna_linear_workspace_size(ctypes.byref(ld), int(bool(backward)), ctypes.byref(out)),
+           "luna_linear_workspace_size")
+    return out.value
+
+
+def luna_linear_fwd(ld, X, W, bias, R, Y, Z, workspace, stream=None) -> None:
+    _check(_lib.luna_linear_fwd(ctypes.byref(ld), _ptr(X), _ptr(W), _ptr(bias), _ptr(R), _ptr(Y), _ptr(Z),
+                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "luna_linear_fwd")
+
+
+def luna_linear_bwd(ld, X, W, Z, dY, dX, dW, db, workspace, stream=None) -> None:
+    _check(_lib.luna_linear_bwd(ctypes.byref(ld), _ptr(X), _ptr(W), _ptr(Z), _ptr(dY), _ptr(dX), _ptr(dW), _ptr(db),
+                                _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "luna_linear_bwd")
 
 
 def luna_device_status(workspace: torch.Tensor, stream=None) -> int:
@@ -473,3 +552,109 @@ class Decay:
             _dense(name, t)
         luna_decay_step(self.dd, log_decay, q, k, v, slots, S.shape[0], S, o, stream)
         return o
+
+
+class BlockNorm:
+    """The norms after and before a block with its gate and residual scale, over (rows, cols) matrices
+    whose rows may be strided; weights are (cols,) fp32.  Owns the workspace of the backward pass."""
+
+    def __init__(self, rows, cols, groups=1, kind="rms", gate="none", res_scale=1.0, eps=1e-6, io=torch.bfloat16,
+                 device="cuda", backward=False):
+        self.nd = norm_desc(rows, cols, groups, kind, gate, res_scale, eps, _DTYPES[io])
+        self.io, self.device, self.shape = io, torch.device(device), (rows, cols)
+        self.ws = alloc_bytes(luna_norm_workspace_size(self.nd), self.device) if backward else None
+
+    def _rows(self, name: str, t) -> None:
+        if t is None:
+            return
+        _want(name, t, self.shape, self.io, self.device)
+        if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name}: rows are not contiguous")
+        setattr(self.nd, "ld" + name, t.stride(0) if t.shape[0] > 1 else 0)
+
+    def _weights(self, **weights) -> None:
+        for name, t in weights.items():
+            _want(name, t, self.shape[1:], torch.float32, self.device)
+            _dense(name, t)
+
+    def forward(self, x, y, gate=None, w_post=None, w_pre=None, b_post=None, b_pre=None, X=None, H=None, stream=None):
+        """{"X": x'} where there is a residual or no second norm (or X is given), {"H": h} with w_pre."""
+        like = x if x is not None else y
+        if X is None and ((x is not None and y is not None) or w_pre is None):
+            X = torch.empty(self.shape, dtype=self.io, device=like.device)
+        if H is None and w_pre is not None:
+            H = torch.empty(self.shape, dtype=self.io, device=like.device)
+        for name, t in (("x", x), ("y", y), ("gate", gate), ("X", X), ("H", H)):
+            self._rows(name, t)
+        self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre)
+        luna_norm_fwd(self.nd, x, y, gate, w_post, b_post, w_pre, b_pre, X, H, stream)
+        return {k: t for k, t in (("X", X), ("H", H)) if t is not None}
+
+    def backward(self, x, y, gate, w_post, w_pre, dX, dH, b_post=None, b_pre=None, out=None, stream=None):
+        """dx, dy, dgate, dw_post, dw_pre of what forward was given, and db_post, db_pre of given biases."""
+        if out is None:
+            out = {k: torch.empty(self.shape, dtype=self.io, device=self.device)
+                   for k, t in (("dx", x), ("dy", y), ("dgate", gate)) if t is not None}
+            out.update({k: torch.empty(self.shape[1], dtype=torch.float32, device=self.device)
+                        for k, t in (("dw_post", w_post), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
+                        if t is not None})
+        for name, t in (("x", x), ("y", y), ("gate", gate), ("dX", dX), ("dH", dH), ("dx", out.get("dx")),
+                        ("dy", out.get("dy")), ("dgate", out.get("dgate"))):
+            self._rows(name, t)
+        sums = {k: out.get(k) for k in ("dw_post", "db_post", "dw_pre", "db_pre")}
+        self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre, **sums)
+        luna_norm_bwd(self.nd, x, y, gate, w_post, b_post, w_pre, dX, dH, out.get("dx"), out.get("dy"),
+                      out.get("dgate"), sums["dw_post"], sums["db_post"], sums["dw_pre"], sums["db_pre"], self.ws, stream)
+        return out
+
+
+class Linear:
+    """Y = act(X W^T + bias) + R for X (m, k), W (n, k), rows strided or not; owns the workspace."""
+
+    def __init__(self, m, n, k, act="none", io=torch.bfloat16, device="cuda", backward=False):
+        self.ld = linear_desc(m, n, k, act, _DTYPES[io])
+        self.io, self.device, self.m, self.n, self.k = io, torch.device(device), m, n, k
+        self.ws = alloc_bytes(max(luna_linear_workspace_size(self.ld, b) for b in ((False, True) if backward else (False,))),
+                              self.device)
+
+    def _rows(self, name: str, t, shape) -> None:
+        if t is None:
+            return
+        _want(name, t, shape, self.io, self.device)
+        if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name}: rows are not contiguous")
+        setattr(self.ld, "ld" + name, t.stride(0) if t.shape[0] > 1 else 0)
+
+    def _vector(self, name: str, t, shape) -> None:
+        _want(name, t, shape, self.io, self.device)
+        _dense(name, t)
+
+    def forward(self, x, W, bias=None, r=None, save_z=False, Y=None, Z=None, stream=None):
+        """Y, or (Y, z) with save_z."""
+        out = (self.m, self.n)
+        if Y is None:
+            Y = torch.empty(out, dtype=self.io, device=x.device)
+        if save_z and Z is None:
+            Z = torch.empty(out, dtype=self.io, device=x.device)
+        for name, t, shape in (("x", x, (self.m, self.k)), ("w", W, (self.n, self.k)), ("r", r, out), ("y", Y, out),
+                               ("z", Z, out)):
+            self._rows(name, t, shape)
+        self._vector("bias", bias, (self.n,))
+        luna_linear_fwd(self.ld, x, W, bias, r, Y, Z, self.ws, stream)
+        return (Y, Z) if save_z else Y
+
+    def backward(self, x, W, dY, Z=None, bias=False, out=None, stream=None):
+        """dX, dW and with `bias` db; Z is forward's z (needed with an activation)."""
+        if out is None:
+            new = dict(dtype=self.io, device=dY.device)
+            out = {"dX": torch.empty((self.m, self.k), **new), "dW": torch.empty((self.n, self.k), **new)}
+            if bias:
+                out["db"] = torch.empty(self.n, **new)
+        dX, dW, db = out.get("dX"), out.get("dW"), out.get("db")
+        for name, t, shape in (("x", x, (self.m, self.k)), ("w", W, (self.n, self.k)), ("z", Z, (self.m, self.n)),
+                               ("dy", dY, (self.m, self.n)), ("dx", dX, (self.m, self.k))):
+            self._rows(name, t, shape)
+        self._vector("dW", dW, (self.n, self.k))
+        self._vector("db", db, (self.n,))
+        luna_linear_bwd(self.ld, x, W, Z, dY, dX, dW, db, self.ws, stream)
+        return out
