@@ -228,7 +228,7 @@ cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, c
 }
 
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
-    return launch_product_simt(p, io, s);
+    return io == LUNA_BF16 && product_tc_ok(p) ? launch_product_tc(p, s) : launch_product_simt(p, io, s);
 }
 
 }  // namespace luna

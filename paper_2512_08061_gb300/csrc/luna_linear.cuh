@@ -70,6 +70,8 @@ int linear_splits(const Product &p, int64_t tiles, int64_t least);
 
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);          // picks a kernel
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
+bool product_tc_ok(const Product &p);                                                 // aligned operands
+cudaError_t launch_product_tc(const Product &p, cudaStream_t s);                      // bf16, tensor cores
 cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);
 
 }  // namespace luna

@@ -1,0 +1,378 @@
+// Matrix products with a fused epilogue on tensor cores (bf16, tcgen05 / TMEM / TMA).
+//
+// Persistent blocks walk the output tiles.  One thread loads 64-deep slices of A and B by TMA into a
+// ring of shared-memory stages, one thread issues the products of each full stage into one of two
+// TMEM accumulators, and eight warps carry the other accumulator through the epilogue (bias, kept
+// pre-activation, activation, residual, one rounding), so that the products of the next tile never
+// wait for it.  Either operand may be stored along the other dimension (k x rows, as the gradients'
+// operands are): its slices then are read as MN-major operands, without a transposed copy.
+//
+// CG = 2: two CTAs of a cluster share a 256 x BN tile.  Each holds its 128 rows of A and half of B
+// (a CTA alone has to read A and all of B from its shared memory for every product, which the
+// shared-memory bandwidth does not sustain at 128 x 256), and the leader's thread issues the products
+// of both.  TMA zero-fills past every edge, so ragged sizes only guard the stores.
+#include "luna_linear.cuh"
+
+#include <algorithm>
+
+#include "luna_prof.cuh"
+#include "luna_sm100.cuh"
+
+namespace luna {
+
+int tc_sm_count();
+bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
+                    const uint32_t *box);
+
+namespace {
+using namespace sm100;
+
+constexpr int kEpiWarps = 8, kWarpTma = 8, kWarpMma = 9, kTcThreads = 320;
+constexpr int kDepth = 64;  // K of a stage
+
+template <int CG, int BN> struct Tile {
+    static constexpr int BM = 128;                    // rows of a CTA
+    static constexpr int NB = BN / CG;                // B rows a CTA holds
+    static constexpr int NBL = NB < 64 ? 64 : NB;     // ... and loads (an MN-major slice is 64 wide)
+    static constexpr uint32_t A_BYTES = BM * 128, B_BYTES = NBL * 128, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = (int)((208 * 1024) / STAGE) > 8 ? 8 : (int)((208 * 1024) / STAGE);
+    static constexpr uint32_t COLS = 2 * BN;          // two accumulators
+    static constexpr uint32_t SMEM = STAGES * STAGE + 1024 + 256;
+};
+
+struct ProductTc {
+    Product p;
+    int tiles_m, tiles_n, splits, k_steps, steps_per_split;  // tiles of BM * CG rows, BN columns
+    bool swap;      // the product is computed transposed: A = the layer's B (few rows of X)
+    bool vec;       // outputs and residual on 16-byte boundaries
+};
+
+__device__ __forceinline__ uint8_t *align_1024(uint8_t *p) {
+    return p + ((1024u - (smem_u32(p) & 1023u)) & 1023u);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+
+// Work unit -> tile: runs of eight tile rows are walked column by column, so that the blocks at work
+// share slices of A and of B in L2.
+__device__ __forceinline__ void unit_tile(const ProductTc &a, int u, int &tm, int &tn, int &split) {
+    split = u % a.splits;
+    u /= a.splits;
+    constexpr int G = 8;
+    const int per = G * a.tiles_n, g = u / per, rows = min(G, a.tiles_m - g * G), r = u - g * per;
+    tm = g * G + r % rows;
+    tn = r / rows;
+}
+
+// Epilogue of 32 columns of one row, all inside the output, 16-byte accesses.
+template <int ACT>
+__device__ __forceinline__ void finish_vec(const Product &p, int64_t row, int64_t col, float (&v)[32]) {
+    using B = __nv_bfloat16;
+    if (p.bias) {
+        const uint4 *b = reinterpret_cast<const uint4 *>(static_cast<const B *>(p.bias) + col);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 w = __ldg(b + q);
+            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
+                v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
+            }
+        }
+    }
+    if (p.Z) {
+        uint4 *z = reinterpret_cast<uint4 *>(static_cast<B *>(p.Z) + row * p.ldz + col);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            z[q] = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
+                              pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+    }
+    if (ACT != LUNA_LINEAR_NONE) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = linear_act(v[i], ACT);
+    }
+    if (p.R) {
+        const uint4 *r = reinterpret_cast<const uint4 *>(static_cast<const B *>(p.R) + row * p.ldr + col);
+        uint4 w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = r[q];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t x[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
+                v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
+            }
+        }
+    }
+    uint4 *o = reinterpret_cast<uint4 *>(static_cast<B *>(p.out) + row * p.ldo + col);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        o[q] = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
+                          pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+}
+
+template <int CG, int BN>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    k_product_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+                 const __grid_constant__ ProductTc a) {
+    using T = Tile<CG, BN>;
+    constexpr int S = T::STAGES;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = align_1024(smem_raw);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + S * T::STAGE);
+    uint64_t *full = bars, *empty = bars + S, *tfull = bars + 2 * S, *tempty = tfull + 2;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(tempty + 2);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    if (tid == 0) {
+        for (int i = 0; i < S; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(tfull + i, 1); mbar_init(tempty + i, CG * kEpiWarps); }
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        if (CG == 2) { tmem_alloc_pair(tslot, T::COLS); tmem_relinquish_pair(); }
+        else { tmem_alloc(tslot, T::COLS); tmem_relinquish(); }
+    }
+    tc_fence_before();
+    if (CG == 2) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = *tslot;
+    const Product &p = a.p;
+    const int units = a.tiles_m * a.tiles_n * a.splits;
+    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+    bool failed = false;
+    auto wait = [&](uint64_t *bar, uint32_t parity) {
+        if (!failed && !mbar_wait(bar, parity)) {
+            failed = true;
+            atomicOr(p.status, 1);
+        }
+    };
+
+    if (warp == kWarpTma) {
+        if (lane == 0) {
+            int it = 0;
+            for (int u = first; u < units && !failed; u += stride) {
+                int tm, tn, sp;
+                unit_tile(a, u, tm, tn, sp);
+                const int s0 = sp * a.steps_per_split, s1 = min(a.k_steps, s0 + a.steps_per_split);
+                const int ra = (tm * CG + (int)rank) * T::BM, rb = tn * BN + (int)rank * T::NB;
+                for (int s = s0; s < s1 && !failed; ++s, ++it) {
+                    const int st = it % S;
+                    wait(empty + st, ((it / S) & 1) ^ 1);
+                    if (failed) break;
+                    uint8_t *sa = sm + st * T::STAGE, *sb = sa + T::A_BYTES;
+                    if (rank == 0) mbar_arrive_expect_tx(full + st, CG * T::STAGE);
+                    const uint32_t bar = CG == 2 ? leader_addr(full + st) : 0;
+                    auto load = [&](uint8_t *dst, const CUtensorMap *m, int x, int y) {
+                        if (CG == 2) tma_load_2d_pair(dst, m, x, y, bar);
+                        else tma_load_2d(dst, m, x, y, full + st);
+                    };
+                    if (p.A.kt) {
+                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, s * kDepth);
+                    } else {
+                        load(sa, &mapA, s * kDepth, ra);
+                    }
+                    if (p.B.kt) {
+                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, s * kDepth);
+                    } else {
+                        load(sb, &mapB, s * kDepth, rb);
+                    }
+                }
+            }
+        }
+    } else if (warp == kWarpMma) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t id = idesc_bf16(CG * T::BM, BN, p.A.kt, p.B.kt);
+            const uint32_t lboA = p.A.kt ? 8192 : 16, lboB = p.B.kt ? 8192 : 16;
+            const uint32_t stepA = p.A.kt ? 2048 : 32, stepB = p.B.kt ? 2048 : 32;  // bytes of 16 of K
+            int it = 0, n = 0;
+            for (int u = first; u < units && !failed; u += stride, ++n) {
+                int tm, tn, sp;
+                unit_tile(a, u, tm, tn, sp);
+                const int s0 = sp * a.steps_per_split, s1 = min(a.k_steps, s0 + a.steps_per_split);
+                const int acc = n & 1;
+                wait(tempty + acc, ((n >> 1) & 1) ^ 1);
+                tc_fence_after();
+                const uint32_t d = tbase + acc * BN;
+                for (int s = s0; s < s1 && !failed; ++s, ++it) {
+                    const int st = it % S;
+                    wait(full + st, (it / S) & 1);
+                    if (failed) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(sm + st * T::STAGE);
+                    const uint64_t da = sdesc(sa, lboA, 1024, kSwizzle128), db = sdesc(sa + T::A_BYTES, lboB, 1024, kSwizzle128);
+#pragma unroll
+                    for (int k = 0; k < kDepth / 16; ++k) {
+                        const uint64_t ka = da + ((k * stepA) >> 4), kb = db + ((k * stepB) >> 4);
+                        if (CG == 2) mma_bf16_ss_pair(d, ka, kb, id, s > s0 || k > 0);
+                        else mma_bf16_ss(d, ka, kb, id, s > s0 || k > 0);
+                    }
+                    if (CG == 2) mma_commit_pair(empty + st);
+                    else mma_commit(empty + st);
+                }
+                if (failed) break;
+                if (CG == 2) mma_commit_pair(tfull + acc);
+                else mma_commit(tfull + acc);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tempty_leader[2] = {CG == 2 ? leader_addr(tempty) : 0, CG == 2 ? leader_addr(tempty + 1) : 0};
+        int n = 0;
+        for (int u = first; u < units && !failed; u += stride, ++n) {
+            int tm, tn, sp;
+            unit_tile(a, u, tm, tn, sp);
+            const int acc = n & 1;
+            wait(tfull + acc, (n >> 1) & 1);
+            if (__any_sync(0xffffffffu, failed)) break;
+            tc_fence_after();
+            const int64_t row = (int64_t)(tm * CG + (int)rank) * T::BM + quarter * 32 + lane;
+            constexpr int CH = BN / 32;  // chunks of 32 columns, in halves
+            const bool last_split_empty = a.steps_per_split * sp >= a.k_steps;
+#pragma unroll 1
+            for (int c = half * ((CH + 1) / 2); c < (half ? CH : (CH + 1) / 2); ++c) {
+                const int64_t col = (int64_t)tn * BN + 32 * c;
+                uint32_t x[32];
+                tmem_ld32(tbase + lane_base + acc * BN + 32 * c, x);
+                tmem_wait_ld();
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = last_split_empty ? 0.0f : __uint_as_float(x[i]);
+                const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;  // of the computed product
+                const int w = row < M ? (int)max((int64_t)0, min((int64_t)32, N - col)) : 0;
+                if (w == 0) {
+                    // nothing of the row in this chunk
+                } else if (a.swap) {
+                    if (a.splits > 1) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i < w) p.part[((int64_t)sp * p.M + col + i) * p.N + row] = v[i];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i < w) linear_finish<__nv_bfloat16>(p, col + i, row, v[i]);
+                    }
+                } else if (a.splits > 1) {
+                    float *o = p.part + ((int64_t)sp * p.M + row) * p.N + col;
+                    if (w == 32 && p.N % 4 == 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4 *>(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (i < w) o[i] = v[i];
+                    }
+                } else if (a.vec && w == 32) {
+                    switch (p.act) {
+                        case LUNA_LINEAR_NONE: finish_vec<LUNA_LINEAR_NONE>(p, row, col, v); break;
+                        case LUNA_LINEAR_RELU: finish_vec<LUNA_LINEAR_RELU>(p, row, col, v); break;
+                        case LUNA_LINEAR_GELU: finish_vec<LUNA_LINEAR_GELU>(p, row, col, v); break;
+                        default: finish_vec<LUNA_LINEAR_SILU>(p, row, col, v);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (i < w) linear_finish<__nv_bfloat16>(p, row, col + i, v[i]);
+                }
+                __syncwarp();  // the TMEM load of the next chunk is the whole warp's
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) mbar_arrive_cluster(tempty_leader[acc]);
+                else mbar_arrive(tempty + acc);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    if (CG == 2) cluster_sync();  // the leader's products read this CTA's slices, its loads signal the leader
+    else __syncthreads();
+    if (warp == 0) {
+        if (CG == 2) tmem_dealloc_pair(tbase, T::COLS);
+        else tmem_dealloc(tbase, T::COLS);
+    }
+}
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Map of an operand whose slices are `rows` rows x 64 deep.
+bool operand_map(CUtensorMap *m, const MatView &v, int64_t rows, int64_t K, int slice_rows) {
+    const uint64_t dims[2] = {(uint64_t)(v.kt ? rows : K), (uint64_t)(v.kt ? K : rows)};
+    const uint64_t strides[1] = {(uint64_t)v.ld * 2};
+    const uint32_t box[2] = {64, (uint32_t)(v.kt ? kDepth : slice_rows)};
+    return tc_make_map_nd(m, v.p, 2, dims, strides, box);
+}
+
+template <int CG, int BN>
+cudaError_t launch(ProductTc a, cudaStream_t s) {
+    using T = Tile<CG, BN>;
+    Product &p = a.p;
+    const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;
+    if (a.swap) std::swap(p.A, p.B);
+    a.tiles_m = (int)cdiv(M, T::BM * CG);
+    a.tiles_n = (int)cdiv(N, BN);
+    a.k_steps = (int)cdiv(p.K, kDepth);
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
+    a.splits = linear_splits(p, tiles * CG, 256);
+    a.steps_per_split = (int)cdiv(a.k_steps, a.splits);
+    a.splits = (int)cdiv(a.k_steps, a.steps_per_split);
+    CUtensorMap mA, mB;
+    if (!operand_map(&mA, p.A, M, p.K, T::BM) || !operand_map(&mB, p.B, N, p.K, T::NBL)) return cudaErrorInvalidValue;
+    cudaError_t e = cudaFuncSetAttribute(k_product_tc<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
+    if (e != cudaSuccess) return e;
+    const int sms = tc_sm_count() / CG * CG;
+    const int grid = (int)std::min<int64_t>(tiles * a.splits * CG, sms);
+    const int splits = a.splits;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = T::SMEM;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = CG == 2 ? 1 : 0;
+    prof_before("product_tc", s);
+    e = cudaLaunchKernelEx(&cfg, k_product_tc<CG, BN>, mA, mB, a);
+    prof_after("product_tc", s);
+    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || splits == 1) return e;
+    return launch_product_finish(p, splits, LUNA_BF16, s);
+}
+
+}  // namespace
+
+bool product_tc_ok(const Product &p) {
+    for (const MatView *v : {&p.A, &p.B})
+        if (!al16(v->p) || v->ld % 8 != 0) return false;
+    return p.K >= 1;
+}
+
+cudaError_t launch_product_tc(const Product &p, cudaStream_t s) {
+    ProductTc a;
+    a.p = p;
+    a.swap = false;
+    a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % 8 == 0 && p.ldr % 8 == 0 && p.ldz % 8 == 0;
+    if (p.M <= 64) {  // few rows of X: the weight's rows fill the tile's 128 rows, X's are its columns
+        a.swap = true;
+        // (an MN-major slice is 64 wide)
+        return p.M <= 32 && !p.A.kt ? launch<1, 32>(a, s) : launch<1, 64>(a, s);
+    }
+    const int64_t sms = tc_sm_count();
+    if (cdiv(p.M, 128) * cdiv(p.N, 256) >= sms) return launch<1, 256>(a, s);
+    return launch<1, 128>(a, s);
+}
+
+}  // namespace luna
