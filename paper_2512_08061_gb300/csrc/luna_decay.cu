@@ -269,6 +269,7 @@ cudaError_t mix(const DecayMix &a, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_decay_mix(const DecayMix &a, luna_dtype io, luna_dtype out, cudaStream_t s) {
+    if (decay_tc_ok(a, io, out)) return launch_decay_mix_tc(a, out, s);
     if (io == LUNA_F32) return mix<float, float>(a, s);
     return out == LUNA_F32 ? mix<__nv_bfloat16, float>(a, s) : mix<__nv_bfloat16, __nv_bfloat16>(a, s);
 }

@@ -41,7 +41,7 @@ struct DecayMix {
     int x_pieces;         // nseg, or 1 (one piece)
     int x_trans;          // X is stored [dc][da]
     float *Xout;          // carry out of every piece, [bh][s][da][dc], or NULL
-    float *partial;       // tensor-core kernels: unused by the generic ones
+    int *status;          // device status word of the call
 };
 
 // Carries into the pieces from the pieces' own sums U (carry out of each from zero):
@@ -73,6 +73,8 @@ __device__ __forceinline__ float decay_log(const float *log_decay, int h) {
 }
 
 cudaError_t launch_decay_mix(const DecayMix &a, luna_dtype io, luna_dtype out, cudaStream_t s);
+bool decay_tc_ok(const DecayMix &a, luna_dtype io, luna_dtype out);  // shapes and alignments of the tensor-core form
+cudaError_t launch_decay_mix_tc(const DecayMix &a, luna_dtype out, cudaStream_t s);
 cudaError_t launch_decay_scan(const DecayScan &a, cudaStream_t s);
 cudaError_t launch_decay_step(const DecayStep &a, luna_dtype io, cudaStream_t s);
 // Sums groups of G consecutive heads of an fp32 (B, H, n, width) array into a tensor of H / G heads.

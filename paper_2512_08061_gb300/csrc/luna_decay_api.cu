@@ -80,9 +80,10 @@ bool empty(const luna_decay_desc *dd) { return (int64_t)dd->B * dd->H == 0; }
 RowView view(const void *p, const luna_strides &s, int heads) { return RowView{p, s.b, s.h, s.t, heads}; }
 
 // What all passes of a call share.
-DecayMix base(const luna_decay_desc *dd, const Plan &p, const float *log_decay, const int32_t *lengths) {
+DecayMix base(const luna_decay_desc *dd, const Plan &p, const float *log_decay, const int32_t *lengths, char *ws) {
     DecayMix a;
     memset(&a, 0, sizeof(a));
+    a.status = reinterpret_cast<int *>(ws);
     a.log_decay = log_decay;
     a.lengths = lengths;
     a.B = dd->B; a.H = dd->H; a.n = dd->n;
@@ -142,7 +143,7 @@ luna_status luna_decay_fwd(const luna_decay_desc *dd, const float *log_decay, co
 
     cudaError_t e = cudaMemsetAsync(ws, 0, sizeof(int), s);  // the status word of this call
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
-    DecayMix a = base(dd, p, log_decay, lengths);
+    DecayMix a = base(dd, p, log_decay, lengths, ws);
     a.a = view(Q, sq, dd->H); a.b = view(K, sk, dd->Hkv); a.c = view(V, sv, dd->Hkv);
     a.da = dd->d; a.dc = dd->dv;
     a.p = a.x = dd->scale;
@@ -189,7 +190,7 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
 
     // states before every piece, gradients of the states after every piece
-    DecayMix a = base(dd, p, log_decay, lengths);
+    DecayMix a = base(dd, p, log_decay, lengths, ws);
     a.a = k; a.b = k; a.c = v; a.da = d; a.dc = dv;
     if ((e = carries(a, p, dd->io, ws, S0, X, nullptr, s)) != cudaSuccess) return LUNA_ERR_CUDA;
     a.reverse = 1;
@@ -197,7 +198,7 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
     a.u = dd->scale;
     if ((e = carries(a, p, dd->io, ws, dS1, R, dS0, s)) != cudaSuccess) return LUNA_ERR_CUDA;
 
-    a = base(dd, p, log_decay, lengths);
+    a = base(dd, p, log_decay, lengths, ws);
     a.x_pieces = p.nseg;
     a.x_trans = 1;
     a.p = a.x = dd->scale;
