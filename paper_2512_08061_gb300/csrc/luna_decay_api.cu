@@ -55,14 +55,23 @@ struct Plan {
     size_t o_U = 256, o_X = 0, o_R = 0, o_part = 0, fwd = 0, bwd = 0;
 };
 
-// Pieces of the rows: as many as give every SM about two blocks, none under 256 rows (a piece
-// costs the write and the read of a state, a row's worth of d tokens).
+// Pieces of the rows.  More pieces fill more SMs, but with more than one the states before each have to
+// be summed first, a pass over two of the four tensors; the piece count with the least of (rounds of
+// blocks) x (chunks of a block, and about one for its start) x (passes) is taken.
 Plan make_plan(const luna_decay_desc *dd) {
     Plan p;
-    const int64_t BH = (int64_t)dd->B * dd->H;
-    const int64_t want = std::max<int64_t>(1, cdiv(304, std::max<int64_t>(1, BH)));
-    const int64_t ns = std::min<int64_t>(want, std::max<int64_t>(1, dd->n / 256));
-    p.seg_len = (int)(cdiv(cdiv(std::max(1, dd->n), ns), 128) * 128);
+    const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), 128);
+    const bool tc = dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0;
+    // blocks an SM holds: tensor-core form one (two up to width 64), else three, one for each 32 columns of a head
+    const double room = 152.0 * (tc ? (std::max(dd->d, dd->dv) <= 64 ? 2 : 1) : 3.0 / cdiv(std::max(dd->d, dd->dv), 32));
+    int64_t best = 1;
+    double least = 1e300;
+    for (int64_t ns = 1; ns <= std::min<int64_t>(64, std::max<int64_t>(1, chunks / 2)); ++ns) {
+        const double rounds = ceil((double)(BH * ns) / room);
+        const double cost = rounds * (double)(cdiv(chunks, ns) + 1) * (ns > 1 ? 1.45 : 1.0);
+        if (cost < least) { least = cost; best = ns; }
+    }
+    p.seg_len = (int)(cdiv(chunks, best) * 128);
     p.nseg = (int)cdiv(std::max(1, dd->n), p.seg_len);
     p.state = (size_t)align256((int64_t)BH * p.nseg * dd->d * dd->dv * 4);
     p.o_X = p.o_U + p.state;

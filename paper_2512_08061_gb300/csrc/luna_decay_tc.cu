@@ -1,7 +1,7 @@
 // Linear attention with a decay for each head on tensor cores (bf16, tcgen05 / TMEM / TMA).
 //
 // A block walks one piece of a head's rows in chunks of 128 (a, b, c as in luna_decay.cuh) and keeps the
-// state X (da x dc) in fp32 registers.  Per chunk of nv rows, m a row's number in processing order:
+// state X (da x dc, fp32) in TMEM.  Per chunk of nv rows, m a row's number in processing order:
 //     MMA    P = a b^T,  E = a X                       (X as a bf16 operand)
 //     warps  P masked and decayed, as bf16 back into TMEM;  E scaled by x lambda^{m+e} in place
 //            b scaled by lambda^{nv-m-e} into bf16 terms b1 + b2 (+ b3)
@@ -9,12 +9,13 @@
 //     warps  out = E;  X = lambda^{nv} X + u U, and its bf16 operand
 // The decay sits on b alone, so c enters U as it is; one bf16 rounding of the scaled b would cost the
 // state 1.7e-3, two terms leave 3e-6 and three 2^-24.  Passes whose state leaves the kernel use three,
-// the others two (their state only enters outputs as one more bf16 rounding).
+// the others two (their state only enters outputs as one more bf16 rounding).  X is not accumulated by
+// the products themselves: their additions onto a large X round toward zero, chunk after chunk.
 //
 // Bound: by its bytes the pass is (da + dc) * 4 bytes a row at HBM rate; the shared-memory traffic of
-// the products' operands and of the scaled terms comes next (about 4/5 of that at d = 128).  Two groups
-// of warps (P and out; X and the scaled b) work on their halves of a chunk side by side, and the
-// next tiles load while they do: a ring of four slots takes a, b, c in turn.
+// the products' operands and of the scaled terms comes next (about 2/3 of that at d = 128).  Three
+// groups of warps (the scaled b; X; P and out) work on their parts of neighbouring chunks side by side,
+// and the next tiles load while they do: a ring of four slots takes a, b, c in turn.
 #include <math.h>
 #include <string.h>
 
@@ -33,21 +34,20 @@ using namespace sm100;
 constexpr int kRows = 128;   // rows of a chunk
 constexpr int kSlots = 4;
 
+constexpr int kScaleWarps = 8, kStateWarps = 4, kScoreWarps = 8;  // the three groups (multiples of four warps)
+
 template <int D, int NT, bool STATE> struct Cfg {
-    static constexpr int NW = D / 16;               // warps of a group (8 or 4)
-    static constexpr int GT = NW * 32;              // threads of a group
-    static constexpr int GROUPS = STATE ? 1 : 2;
-    static constexpr int THREADS = GROUPS * GT + 64;
+    static constexpr int WARPS = kScaleWarps + kStateWarps + (STATE ? 0 : kScoreWarps);
+    static constexpr int THREADS = WARPS * 32 + 64;
     static constexpr int KB = D / 64;               // 64-column blocks of a row
     static constexpr uint32_t BLK = kRows * 128;    // one block of a tile
     static constexpr uint32_t TILE = KB * BLK;
     static constexpr uint32_t XBLK = D * 128, XOP = KB * XBLK;  // X operand: [64-column block][feature][64]
-    static constexpr uint32_t SMEM = kSlots * TILE + (NT - 1) * TILE + (STATE ? 0 : XOP) + 1024 + 1024;
+    static constexpr uint32_t SMEM = kSlots * TILE + (NT - 1) * TILE + (STATE ? 0 : XOP) + 2048 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory");
-    // TMEM columns: P (then its bf16 form in the first half) | E | U
-    static constexpr uint32_t cP = 0, cE = 128, cU = STATE ? 0 : 128 + D;
-    static constexpr uint32_t COLS = STATE ? D : D == 64 ? 256 : 512;
-    static constexpr int CPT = D == 64 ? 64 : D * D / GT;  // state columns of a thread (D = 64: 16 lanes of a warp)
+    // TMEM columns: U | X | E | P (then its bf16 form in the first half)
+    static constexpr uint32_t cU = 0, cX = D, cE = 2 * D, cP = 3 * D;
+    static constexpr uint32_t COLS = STATE ? 2 * D : 512;
 };
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -70,57 +70,105 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
         : "memory");
 }
 
-// 32 scores of row i, columns 32 jb ..: masked, decayed, times p.  Off the diagonal block the decay is a
-// factor of the row times one of the column (both at most 1 for lambda <= 1), on it a table lookup.
-__device__ __forceinline__ void decay_scores(float (&v)[32], int i, int jb, bool reverse, int nv, float p,
-                                             const float *pw) {
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t f2(uint32_t lo, uint32_t hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t f2(float lo, float hi) { return f2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpack2(uint64_t v, float &lo, float &hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack2(uint64_t v) {
+    float lo, hi;
+    unpack2(v, lo, hi);
+    return pack2(lo, hi);
+}
+__device__ __forceinline__ uint64_t widen2(uint32_t bf) { return f2(bf << 16, bf & 0xffff0000u); }
+
+// Decays of the diagonal block by x = column - row + 31: four copies, the m-th shifted by m, so that any
+// row's 32 are whole 16-byte loads, and 72 floats apart, so that a warp's fall into different banks.
+constexpr int kDiagCopy = 72;
+
+// 32 scores of row i, columns 32 jb .. (TMEM address `taddr`): masked, decayed, times p, as bf16 pairs.
+// Off the diagonal block the decay is a factor of the row times one of the column (both at most 1 for
+// lambda <= 1), on it it comes from the table of decays by distance, 0 where the distance is negative.
+__device__ __forceinline__ void decay_scores(uint32_t taddr, int i, int jb, bool reverse, int nv, float p,
+                                             const float *pw, const float *diag, uint32_t (&w)[16]) {
     const int ib = i >> 5, li = i & 31, j0 = 32 * jb;
+    if (reverse ? jb < ib : jb > ib) {  // the same for the whole warp
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = 0u;
+        return;
+    }
+    uint32_t x[32];
+    tmem_ld32(taddr, x);
     if (jb == ib) {
+        const int m = (31 - li) & 3;
+        const float4 *t = reinterpret_cast<const float4 *>(diag + m * kDiagCopy + 31 - li - m);
+        tmem_wait_ld();
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const int dist = reverse ? j - li : li - j;
-            const bool on = dist >= 0 && i < nv && j0 + j < nv;
-            v[j] = on ? v[j] * (p * pw[on ? dist : 0]) : 0.0f;
+        for (int q = 0; q < 8; ++q) {
+            const float4 c = t[q];
+            w[2 * q] = pack2(mul2(f2(x[4 * q], x[4 * q + 1]), f2(c.x, c.y)));
+            w[2 * q + 1] = pack2(mul2(f2(x[4 * q + 2], x[4 * q + 3]), f2(c.z, c.w)));
         }
-        return;
+    } else {
+        const float row = p * (reverse ? pw[j0 - i] : pw[i - j0 - 31]);
+        const uint64_t row2 = f2(row, row);
+        const float4 *t = reinterpret_cast<const float4 *>(pw);
+        tmem_wait_ld();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            // forward: column j of the block decays by 31 - j, reverse: by j
+            const float4 c = reverse ? t[q] : t[7 - q];
+            const uint64_t c0 = reverse ? f2(c.x, c.y) : f2(c.w, c.z), c1 = reverse ? f2(c.z, c.w) : f2(c.y, c.x);
+            w[2 * q] = pack2(mul2(f2(x[4 * q], x[4 * q + 1]), mul2(row2, c0)));
+            w[2 * q + 1] = pack2(mul2(f2(x[4 * q + 2], x[4 * q + 3]), mul2(row2, c1)));
+        }
     }
-    if (reverse ? jb < ib : jb > ib) {
+    if (nv < kRows) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-        return;
-    }
-    const float row = p * (reverse ? pw[j0 - i] : pw[i - j0 - 31]);
-    const float4 *t = reinterpret_cast<const float4 *>(pw);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        // forward: column j of the block decays by 31 - j, reverse: by j
-        const float4 w = reverse ? t[q] : t[7 - q];
-        const float c[4] = {reverse ? w.x : w.w, reverse ? w.y : w.z, reverse ? w.z : w.y, reverse ? w.w : w.x};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bool on = i < nv && j0 + 4 * q + k < nv;
-            v[4 * q + k] = on ? v[4 * q + k] * (row * c[k]) : 0.0f;
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t keep = i >= nv ? 0u : (j0 + 2 * j < nv ? 0xffffu : 0u) | (j0 + 2 * j + 1 < nv ? 0xffff0000u : 0u);
+            w[j] &= keep;
         }
     }
 }
 
 template <int D, int NT, bool STATE, typename OUT>
-__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
+__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     k_decay_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-               const __grid_constant__ CUtensorMap mapC, const __grid_constant__ DecayMix a) {
+               const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapO,
+               const __grid_constant__ DecayMix a) {
     using C = Cfg<D, NT, STATE>;
+    constexpr bool STAGED = !STATE && sizeof(OUT) == 2;  // bf16 outputs leave by TMA from the chunk's c slot
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = align_1024(smem_raw);
     uint8_t *terms = sm + kSlots * C::TILE;           // b2, b3 (b1 overwrites b in its slot)
     uint8_t *Xop = terms + (NT - 1) * C::TILE;
     float *pw = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));  // lambda^0 .. lambda^128
-    uint64_t *bars = reinterpret_cast<uint64_t *>(pw + 132);
+    float *diag = pw + 132;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(diag + 4 * kDiagCopy);
     uint64_t *full = bars, *freeb = bars + kSlots, *pready = bars + 2 * kSlots;
     uint64_t *eready = pready + 1, *scaled = pready + 2, *uready = pready + 3, *xready = pready + 4;
-    uint64_t *masked = pready + 5, *oready = pready + 6, *efree = pready + 7;
-    uint32_t *tslot = reinterpret_cast<uint32_t *>(pready + 8);
+    uint64_t *masked = pready + 5, *oready = pready + 6, *efree = pready + 7, *ufree = pready + 8;
+    uint64_t *stored = pready + 9;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(pready + 10);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    constexpr int kTma = C::GROUPS * C::NW, kMma = kTma + 1;
+    constexpr int kTma = C::WARPS, kMma = kTma + 1;
+    constexpr int kStateWarp0 = kScaleWarps, kScoreWarp0 = kScaleWarps + kStateWarps;
 
     const int seg = blockIdx.x % a.nseg;
     const int64_t bh = blockIdx.x / a.nseg;
@@ -135,11 +183,17 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
     if (tid == 0) {
         for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 1); mbar_init(freeb + i, 1); }
         mbar_init(pready, 1); mbar_init(eready, 1); mbar_init(uready, 1); mbar_init(oready, 1);
-        mbar_init(scaled, C::GT); mbar_init(xready, C::GT); mbar_init(masked, C::GT); mbar_init(efree, C::GT);
+        mbar_init(scaled, kScaleWarps); mbar_init(xready, kStateWarps); mbar_init(ufree, kStateWarps);
+        mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps * D / 128);
         fence_mbar_init();
     }
     if (warp == kMma) { tmem_alloc(tslot, C::COLS); tmem_relinquish(); }
     for (int i = tid; i <= kRows; i += C::THREADS) pw[i] = expf(g * (float)i);
+    if (!STATE)
+        for (int i = tid; i < 4 * kDiagCopy; i += C::THREADS) {
+            const int dist = (i % kDiagCopy + i / kDiagCopy - 31) * (a.reverse ? 1 : -1);
+            diag[i] = dist >= 0 && dist < 32 ? a.p * expf(g * (float)dist) : 0.0f;
+        }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -151,6 +205,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
             atomicOr(a.status, 1);
         }
     };
+    auto arrive = [&](uint64_t *bar) {  // once for the warp, after all its lanes
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
     // the slot and use of load number L: a (not for states), b, c of each chunk in turn
     constexpr int LOADS = STATE ? 2 : 3;
 
@@ -158,12 +216,18 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
         if (lane == 0) {
             const int ha = h / (a.H / a.a.heads), hb = h / (a.H / a.b.heads), hc = h / (a.H / a.c.heads);
             int L = 0;
+            uint32_t uses = 0;  // bit s: parity of the phases of freeb[s] waited for
             for (int c = 0; c < nch && !failed; ++c) {
                 const int row = chunk_row(c);
 #pragma unroll
                 for (int w = 3 - LOADS; w < 3; ++w, ++L) {
                     const int s = L % kSlots;
-                    if (L >= kSlots) wait(freeb + s, ((L / kSlots) - 1) & 1);
+                    if (STAGED && L >= kSlots && (L - kSlots) % LOADS == LOADS - 1) {
+                        wait(stored, ((L - kSlots) / LOADS) & 1);  // the slot held c and then the outputs
+                    } else if (L >= kSlots) {
+                        wait(freeb + s, (uses >> s) & 1);
+                        uses ^= 1u << s;
+                    }
                     if (failed) break;
                     const CUtensorMap *m = w == 0 ? &mapA : w == 1 ? &mapB : &mapC;
                     const int hh = w == 0 ? ha : w == 1 ? hb : hc;
@@ -189,7 +253,6 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
                 wait(full + Lb % kSlots, (Lb / kSlots) & 1);
                 if (!STATE) {
                     wait(full + La % kSlots, (La / kSlots) & 1);
-                    if (c > 0) wait(efree, (c - 1) & 1);
                     if (failed) break;
                     tc_fence_after();
                     const uint64_t dA = sdesc(ta, 16, 1024, kSwizzle128), dB = sdesc(tbb, 16, 1024, kSwizzle128);
@@ -200,6 +263,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
                     }
                     mma_commit(pready);
                     wait(xready, ph);
+                    if (c > 0) wait(efree, (c - 1) & 1);
                     if (failed) break;
                     tc_fence_after();
 #pragma unroll
@@ -212,6 +276,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
                 }
                 wait(scaled, ph);
                 wait(full + Lc % kSlots, (Lc / kSlots) & 1);
+                if (STATE && c > 0) wait(ufree, (c - 1) & 1);  // (otherwise before X was ready)
                 if (failed) break;
                 tc_fence_after();
                 const uint64_t dB1 = sdesc(tbb, C::BLK, 1024, kSwizzle128), dC = sdesc(tc, C::BLK, 1024, kSwizzle128);
@@ -233,163 +298,54 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
                     for (int k = 0; k < kRows / 16; ++k)
                         mma_bf16_ts(tb + C::cE, tb + C::cP + 8 * k, dadd(dC, 2048 * k), idE, 1);
                     mma_commit(oready);
-                    mma_commit(freeb + Lc % kSlots);
+                    if (!STAGED) mma_commit(freeb + Lc % kSlots);
                 }
             }
         }
-    } else if (!STATE && warp < C::NW) {
-        // scores and outputs: thread (row, column part); warps w and w + 4 share the rows of quarter w % 4
-        constexpr int PARTS = C::NW / 4, PC = kRows / PARTS, EC = D / PARTS;
-        const int quarter = warp & 3, part = warp >> 2, i = quarter * 32 + lane;
-        const uint32_t lb = (uint32_t)(quarter * 32) << 16;
-        OUT *O = static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh;
+    } else if (warp < kScaleWarps) {
+        // the scaled terms of b: thread (row, half of its 16-byte pieces)
+        const int fr = tid & (kRows - 1), fp = tid / kRows;
+        constexpr int PIECES = D / 8 / (kScaleWarps * 32 / kRows);
         for (int c = 0; c < nch; ++c) {
-            const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
-            const uint32_t ph = c & 1;
-            wait(pready, ph);
-            tc_fence_after();
-            {
-                uint32_t w[PC / 2];
-#pragma unroll
-                for (int q = 0; q < PC / 32; ++q) {
-                    uint32_t x[32];
-                    tmem_ld32(tb + lb + C::cP + part * PC + 32 * q, x);
-                    tmem_wait_ld();
-                    float v[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(x[k]);
-                    decay_scores(v, i, part * (PC / 32) + q, a.reverse != 0, nv, a.p, pw);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) w[16 * q + k] = pack2(v[2 * k], v[2 * k + 1]);
-                }
-                // the bf16 scores overwrite the first half of P: after both warps of the rows have read theirs
-                if (PARTS > 1) {
-                    tc_fence_before();
-                    asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter), "n"(PARTS * 32) : "memory");
-                    tc_fence_after();
-                }
-#pragma unroll
-                for (int q = 0; q < PC / 32; ++q) {
-                    uint32_t y[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) y[k] = w[16 * q + k];
-                    tmem_st16(tb + lb + C::cP + part * (PC / 2) + 16 * q, y);
-                }
-            }
-            wait(eready, ph);
-            tc_fence_after();
-            const int m = a.reverse ? nv - 1 - i : i;
-            const float xs = a.x * pw[max(0, m) + e];
-#pragma unroll
-            for (int q = 0; q < EC / 16; ++q) {
-                uint32_t x[16];
-                tmem_ld16(tb + lb + C::cE + part * EC + 16 * q, x);
-                tmem_wait_ld();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(xs * __uint_as_float(x[k]));
-                tmem_st16(tb + lb + C::cE + part * EC + 16 * q, x);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(masked);
-            wait(oready, ph);
-            tc_fence_after();
-            OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
-#pragma unroll
-            for (int q = 0; q < EC / 32; ++q) {
-                uint32_t x[32];
-                tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
-                tmem_wait_ld();
-                if (q == EC / 32 - 1) {
-                    tc_fence_before();
-                    mbar_arrive(efree);
-                }
-                if (i < nv) {
-#pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        if (part * EC + 32 * q + k < a.dc) {  // dc is a multiple of 8
-                            if (sizeof(OUT) == 4) {
-                                uint4 *dst = reinterpret_cast<uint4 *>(o + 32 * q + k);
-                                dst[0] = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-                                dst[1] = make_uint4(x[k + 4], x[k + 5], x[k + 6], x[k + 7]);
-                            } else {
-                                auto f = [&](int z) { return __uint_as_float(x[k + z]); };
-                                *reinterpret_cast<uint4 *>(o + 32 * q + k) =
-                                    make_uint4(pack2(f(0), f(1)), pack2(f(2), f(3)), pack2(f(4), f(5)), pack2(f(6), f(7)));
-                            }
-                        }
-                }
-                __syncwarp();
-            }
-        }
-        // rows at and past the length
-        OUT *z = O + (int64_t)r1 * a.ot;
-        for (int64_t k = tid; k < (int64_t)(rend - r1) * a.dc; k += C::GT) io_store(z + (k / a.dc) * a.ot + k % a.dc, 0.0f);
-    } else {
-        // state: thread (feature f, columns c0 ..); the accumulator's row f is lane f, or with 64 rows lane
-        // 32 (f / 16) + f % 16
-        const int gt = tid - (STATE ? 0 : C::GT), gw = gt >> 5, quarter = warp & 3;
-        const bool own = D == 128 || lane < 16;
-        const int f = D == 128 ? quarter * 32 + lane : quarter * 16 + (lane & 15);
-        const int c0 = D == 128 ? (gw >> 2) * C::CPT : 0;
-        const uint32_t lb = (uint32_t)(quarter * 32) << 16;
-        const int fr = gt & (kRows - 1), fp = gt / kRows;  // scaling: row of b, part of its 16-byte pieces
-        constexpr int FP = C::GT / kRows, PIECES = D / 8 / FP;
-        float X[C::CPT];
-        {
-            const float *x = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
-#pragma unroll
-            for (int k = 0; k < C::CPT; ++k)
-                X[k] = x && own && f < a.da && c0 + k < a.dc
-                           ? (a.x_trans ? x[(int64_t)(c0 + k) * a.da + f] : x[(int64_t)f * a.dc + c0 + k]) : 0.0f;
-        }
-        auto put_operand = [&]() {  // X as the bf16 operand
-            if (own) {
-#pragma unroll
-                for (int k = 0; k < C::CPT; k += 8) {
-                    const int cc = c0 + k;
-                    *reinterpret_cast<uint4 *>(Xop + (cc / 64) * C::XBLK + sw128_chunk(f, (cc % 64) / 8)) =
-                        make_uint4(pack2(X[k], X[k + 1]), pack2(X[k + 2], X[k + 3]), pack2(X[k + 4], X[k + 5]),
-                                   pack2(X[k + 6], X[k + 7]));
-                }
-            }
-            fence_proxy_async_smem();
-            mbar_arrive(xready);
-        };
-        if (!STATE) put_operand();
-        for (int c = 0; c < nch; ++c) {
-            const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
+            const int nv = min(kRows, r1 - chunk_row(c));
             const uint32_t ph = c & 1;
             const int Lb = c * LOADS + LOADS - 2, Lc = Lb + 1;
             uint8_t *tbb = sm + (Lb % kSlots) * C::TILE, *tcc = sm + (Lc % kSlots) * C::TILE;
             wait(full + Lb % kSlots, (Lb / kSlots) & 1);
-            if (!STATE) wait(pready, ph);  // P has read b
-            const float w = fr < nv ? pw[nv - (a.reverse ? nv - 1 - fr : fr) - e] : 0.0f;
+            if (!STATE) wait(pready, ph);             // P has read b
+            if (c > 0) wait(uready, (c - 1) & 1);     // the last chunk's terms have been read
+            const bool on = fr < nv;
+            const float w = on ? pw[nv - (a.reverse ? nv - 1 - fr : fr) - e] : 0.0f;
+            const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
+            uint4 in4[PIECES];
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q) {
+                const int piece = fp * PIECES + q;
+                in4[q] = *reinterpret_cast<const uint4 *>(tbb + (piece / 8) * C::BLK + sw128_chunk(fr, piece % 8));
+            }
 #pragma unroll
             for (int q = 0; q < PIECES; ++q) {
                 const int piece = fp * PIECES + q;
                 const uint32_t off = (piece / 8) * C::BLK + sw128_chunk(fr, piece % 8);
-                uint4 v = *reinterpret_cast<const uint4 *>(tbb + off);
+                uint4 v = in4[q];
+                if (!on) v = make_uint4(0, 0, 0, 0);  // rows past the length may hold anything
                 const uint32_t in[4] = {v.x, v.y, v.z, v.w};
                 uint32_t o1[4], o2[4], o3[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    float lo = __uint_as_float(in[k] << 16) * w, hi = __uint_as_float(in[k] & 0xffff0000u) * w;
-                    if (fr >= nv) lo = hi = 0.0f;
-                    o1[k] = pack2(lo, hi);
-                    lo -= __uint_as_float(o1[k] << 16);
-                    hi -= __uint_as_float(o1[k] & 0xffff0000u);
-                    o2[k] = pack2(lo, hi);
-                    if (NT == 3)
-                        o3[k] = pack2(lo - __uint_as_float(o2[k] << 16), hi - __uint_as_float(o2[k] & 0xffff0000u));
+                    uint64_t r = mul2(widen2(in[k]), w2);
+                    o1[k] = pack2(r);
+                    r = fma2(widen2(o1[k]), minus, r);
+                    o2[k] = pack2(r);
+                    if (NT == 3) o3[k] = pack2(fma2(widen2(o2[k]), minus, r));
                 }
                 *reinterpret_cast<uint4 *>(tbb + off) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
                 *reinterpret_cast<uint4 *>(terms + off) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
                 if (NT == 3) *reinterpret_cast<uint4 *>(terms + C::TILE + off) = make_uint4(o3[0], o3[1], o3[2], o3[3]);
             }
-            if (nv < kRows) {  // rows past the length may hold anything: c without them
+            if (nv < kRows) {  // c without the rows past the length
                 wait(full + Lc % kSlots, (Lc / kSlots) & 1);
-                if (fr >= nv) {
+                if (!on) {
 #pragma unroll
                     for (int q = 0; q < PIECES; ++q) {
                         const int piece = fp * PIECES + q;
@@ -399,30 +355,199 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
                 }
             }
             fence_proxy_async_smem();
-            mbar_arrive(scaled);
+            arrive(scaled);
+        }
+    } else if (warp < kScoreWarp0) {
+        // state: thread = feature f; an accumulator's row f is lane f, or with 64 rows lane 32 (f / 16) + f % 16
+        const int quarter = warp & 3;
+        const bool own = D == 128 || lane < 16;
+        const int f = D == 128 ? quarter * 32 + lane : quarter * 16 + (lane & 15);
+        const uint32_t lb = (uint32_t)(quarter * 32) << 16;
+        auto put_operand = [&](int cc, const float (&x)[16]) {  // columns cc .. of X as bf16
+            if (own) {
+#pragma unroll
+                for (int k = 0; k < 16; k += 8)
+                    *reinterpret_cast<uint4 *>(Xop + ((cc + k) / 64) * C::XBLK + sw128_chunk(f, ((cc + k) % 64) / 8)) =
+                        make_uint4(pack2(x[k], x[k + 1]), pack2(x[k + 2], x[k + 3]), pack2(x[k + 4], x[k + 5]),
+                                   pack2(x[k + 6], x[k + 7]));
+            }
+        };
+        const float *X0 = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
+#pragma unroll 1
+        for (int cc = 0; cc < D; cc += 16) {
+            float x[16];
+            uint32_t y[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                x[k] = X0 && own && f < a.da && cc + k < a.dc
+                           ? (a.x_trans ? X0[(int64_t)(cc + k) * a.da + f] : X0[(int64_t)f * a.dc + cc + k]) : 0.0f;
+                y[k] = __float_as_uint(x[k]);
+            }
+            tmem_st16(tb + lb + C::cX + cc, y);
+            if (!STATE) put_operand(cc, x);
+        }
+        tmem_wait_st();
+        if (!STATE) {
+            fence_proxy_async_smem();
+            arrive(xready);
+        }
+        for (int c = 0; c < nch; ++c) {
+            const int nv = min(kRows, r1 - chunk_row(c));
+            const uint32_t ph = c & 1;
             wait(uready, ph);
+            if (!STATE) wait(eready, ph);  // E has read the operand
             tc_fence_after();
             const float dec = pw[nv];
+            const uint64_t dec2 = f2(dec, dec), u2 = f2(a.u, a.u);
 #pragma unroll
-            for (int q = 0; q < C::CPT / 16; ++q) {
+            for (int cc = 0; cc < D; cc += 16) {
+                uint32_t xu[16], xx[16];
+                tmem_ld16(tb + lb + C::cU + cc, xu);
+                tmem_ld16(tb + lb + C::cX + cc, xx);
+                tmem_wait_ld();
+                float x[16];
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                    unpack2(fma2(dec2, f2(xx[k], xx[k + 1]), mul2(u2, f2(xu[k], xu[k + 1]))), x[k], x[k + 1]);
+                    xx[k] = __float_as_uint(x[k]);
+                    xx[k + 1] = __float_as_uint(x[k + 1]);
+                }
+                tmem_st16(tb + lb + C::cX + cc, xx);
+                if (!STATE && c + 1 < nch) put_operand(cc, x);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            if (STATE) {
+                arrive(ufree);
+            } else if (c + 1 < nch) {
+                fence_proxy_async_smem();
+                arrive(xready);
+            }
+        }
+        if (a.Xout) {
+            float *X = a.Xout + (bh * a.nseg + seg) * a.da * a.dc + (int64_t)f * a.dc;
+#pragma unroll 1
+            for (int cc = 0; cc < D; cc += 16) {
                 uint32_t x[16];
-                tmem_ld16(tb + lb + C::cU + c0 + 16 * q, x);
+                tmem_ld16(tb + lb + C::cX + cc, x);
+                tmem_wait_ld();
+                if (own && f < a.da) {
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        if (cc + k < a.dc) *reinterpret_cast<uint4 *>(X + cc + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                }
+                __syncwarp();
+            }
+        }
+    } else if (!STATE) {
+        // scores and outputs: thread (row, column half); the two warps of a quarter share its rows
+        constexpr int PC = kRows / 2, EC = D / 2;
+        const int gw = warp - kScoreWarp0, quarter = warp & 3, part = gw >> 2, i = quarter * 32 + lane;
+        const uint32_t lb = (uint32_t)(quarter * 32) << 16;
+        OUT *O = static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh;
+        for (int c = 0; c < nch; ++c) {
+            const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
+            const uint32_t ph = c & 1;
+            wait(pready, ph);
+            tc_fence_after();
+            {
+                uint32_t w[2][16];
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    decay_scores(tb + lb + C::cP + part * PC + 32 * q, i, part * 2 + q, a.reverse != 0, nv, a.p, pw, diag, w[q]);
+                // the bf16 scores overwrite the first half of P: after both warps of the rows have read theirs
+                tc_fence_before();
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+                tc_fence_after();
+#pragma unroll
+                for (int q = 0; q < 2; ++q) tmem_st16(tb + lb + C::cP + part * (PC / 2) + 16 * q, w[q]);
+            }
+            wait(eready, ph);
+            tc_fence_after();
+            const int m = a.reverse ? nv - 1 - i : i;
+            const float xs = a.x * pw[max(0, m) + e];
+            const uint64_t xs2 = f2(xs, xs);
+#pragma unroll
+            for (int q = 0; q < EC / 32; ++q) {
+                uint32_t x[32];
+                tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
                 tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) X[16 * q + k] = fmaf(dec, X[16 * q + k], a.u * __uint_as_float(x[k]));
-            }
-            tc_fence_before();
-            if (!STATE && c + 1 < nch) {
-                wait(eready, ph);  // E has read the operand
-                put_operand();
-            }
-        }
-        if (a.Xout && own && f < a.da) {
-            float *x = a.Xout + (bh * a.nseg + seg) * a.da * a.dc + (int64_t)f * a.dc;
+                for (int s = 0; s < 2; ++s) {
+                    uint32_t y[16];
 #pragma unroll
-            for (int k = 0; k < C::CPT; k += 4)
-                if (c0 + k < a.dc) *reinterpret_cast<float4 *>(x + c0 + k) = make_float4(X[k], X[k + 1], X[k + 2], X[k + 3]);
+                    for (int k = 0; k < 16; k += 2) {
+                        float lo, hi;
+                        unpack2(mul2(xs2, f2(x[16 * s + k], x[16 * s + k + 1])), lo, hi);
+                        y[k] = __float_as_uint(lo);
+                        y[k + 1] = __float_as_uint(hi);
+                    }
+                    tmem_st16(tb + lb + C::cE + part * EC + 32 * q + 16 * s, y);
+                }
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            arrive(masked);
+            wait(oready, ph);
+            tc_fence_after();
+            const int Lc = c * LOADS + LOADS - 1;
+            uint8_t *tcc = sm + (Lc % kSlots) * C::TILE;  // U and the scores' product have read c
+            OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
+#pragma unroll
+            for (int q = 0; q < EC / 32; ++q) {
+                uint32_t x[32];
+                tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
+                tmem_wait_ld();
+                if (q == EC / 32 - 1) {
+                    tc_fence_before();
+                    arrive(efree);
+                }
+                const int cc = part * EC + 32 * q;
+                if (STAGED) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (i < nv)
+                            v = make_uint4(pack2(f2(x[k], x[k + 1])), pack2(f2(x[k + 2], x[k + 3])),
+                                           pack2(f2(x[k + 4], x[k + 5])), pack2(f2(x[k + 6], x[k + 7])));
+                        *reinterpret_cast<uint4 *>(tcc + (cc / 64) * C::BLK + sw128_chunk(i, (cc % 64 + k) / 8)) = v;
+                    }
+                } else if (i < nv) {
+#pragma unroll
+                    for (int k = 0; k < 32; k += 8)
+                        if (cc + k < a.dc) {  // dc is a multiple of 8
+                            uint4 *dst = reinterpret_cast<uint4 *>(o + 32 * q + k);
+                            dst[0] = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                            dst[1] = make_uint4(x[k + 4], x[k + 5], x[k + 6], x[k + 7]);
+                        }
+                }
+                __syncwarp();
+            }
+            if (STAGED) {  // 32 rows of a 64-column block at a time: a warp's own, or with D = 64 its pair's
+                fence_proxy_async_smem();
+                if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+                else __syncwarp();
+                if (lane == 0 && (D == 128 || part == 0)) {
+                    const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
+                    if (row < a.n && 64 * blk < a.dc)
+                        tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, h, b);
+                    bulk_commit();
+                    bulk_wait_read();
+                    mbar_arrive(stored);
+                }
+                __syncwarp();
+            }
         }
+        if (STAGED && lane == 0) bulk_wait();
+        // rows at and past the length
+        constexpr int ZB = 16 / (int)sizeof(OUT), GT = kScoreWarps * 32;
+        const int gt = tid - kScoreWarp0 * 32, pieces = a.dc / ZB, step = GT / pieces;
+        const int z0 = min(rend, r0 + nch * kRows);  // staged chunks have written theirs
+        const int zr = STAGED ? z0 : r1;
+        OUT *z = O + (int64_t)zr * a.ot + (gt % pieces) * ZB;
+        if (gt < step * pieces)
+            for (int k = gt / pieces; k < rend - zr; k += step)
+                *reinterpret_cast<uint4 *>(z + (int64_t)k * a.ot) = make_uint4(0, 0, 0, 0);
     }
     __syncwarp();
     tc_fence_before();
@@ -432,12 +557,12 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, D == 64 ? 2 : 1)
 
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-bool row_map(CUtensorMap *m, const RowView &v, int B, int n, int width) {
+bool row_map(CUtensorMap *m, const RowView &v, int B, int n, int width, int rows = kRows) {
     const uint64_t dims[4] = {(uint64_t)width, (uint64_t)n, (uint64_t)v.heads, (uint64_t)B};
     // the stride of a dimension with one entry is never used, but has to be a valid one
     auto st = [&](int64_t s, int ext) { return ext > 1 ? (uint64_t)s * 2 : (uint64_t)256; };
     const uint64_t strides[3] = {st(v.st, n), st(v.sh, v.heads), st(v.sb, B)};
-    const uint32_t box[4] = {64, kRows, 1, 1};
+    const uint32_t box[4] = {64, (uint32_t)rows, 1, 1};
     return tc_make_map_nd(m, v.p, 4, dims, strides, box);
 }
 
@@ -449,15 +574,17 @@ bool view_ok(const RowView &v, int B, int n) {
 template <int D, int NT, bool STATE, typename OUT>
 cudaError_t launch(const DecayMix &a, cudaStream_t s) {
     using C = Cfg<D, NT, STATE>;
-    CUtensorMap mA, mB, mC;
+    CUtensorMap mA, mB, mC, mO;
     if (!row_map(&mB, a.b, a.B, a.n, a.da) || !row_map(&mC, a.c, a.B, a.n, a.dc)) return cudaErrorInvalidValue;
-    mA = mB;
+    mA = mO = mB;
     if (!STATE && !row_map(&mA, a.a, a.B, a.n, a.da)) return cudaErrorInvalidValue;
+    if (!STATE && sizeof(OUT) == 2 && !row_map(&mO, RowView{a.out, a.ob, a.oh, a.ot, a.H}, a.B, a.n, a.dc, 32))
+        return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(k_decay_tc<D, NT, STATE, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nseg);
     LUNA_LAUNCH(STATE ? "decay_state_tc" : "decay_mix_tc", (k_decay_tc<D, NT, STATE, OUT>), grid, C::THREADS, C::SMEM, s, mA,
-                mB, mC, a);
+                mB, mC, mO, a);
     return cudaGetLastError();
 }
 
