@@ -33,8 +33,9 @@ using namespace sm100;
 
 constexpr int kRows = 128;   // rows of a chunk
 constexpr int kSlots = 4;
+constexpr int kAhead = 2;
 
-constexpr int kScaleWarps = 8, kStateWarps = 4, kScoreWarps = 8;  // the three groups (multiples of four warps)
+constexpr int kScaleWarps = 8, kStateWarps = 8, kScoreWarps = 8;  // the three groups (multiples of four warps)
 
 template <int D, int NT, bool STATE> struct Cfg {
     static constexpr int WARPS = kScaleWarps + kStateWarps + (STATE ? 0 : kScoreWarps);
@@ -43,9 +44,13 @@ template <int D, int NT, bool STATE> struct Cfg {
     static constexpr uint32_t BLK = kRows * 128;    // one block of a tile
     static constexpr uint32_t TILE = KB * BLK;
     static constexpr uint32_t XBLK = D * 128, XOP = KB * XBLK;  // X operand: [64-column block][feature][64]
-    static constexpr uint32_t SMEM = kSlots * TILE + (NT - 1) * TILE + (STATE ? 0 : XOP) + 2048 + 1024;
+    // the terms of b, half a chunk at a time: b1 takes b's own place where there is no room beside it, and
+    // then waits for P to have read b
+    static constexpr bool INPLACE = D == 128 && NT == 3;
+    static constexpr int TERMS = INPLACE ? NT - 1 : NT;
+    static constexpr uint32_t SMEM = kSlots * TILE + TERMS * TILE + (STATE ? 0 : XOP) + 2048 + 1024;
     static_assert(SMEM <= 227 * 1024, "shared memory");
-    // TMEM columns: U | X | E | P (then its bf16 form in the first half)
+    // TMEM columns: U | X | E | P (the bf16 form of each 64 columns in their first 32)
     static constexpr uint32_t cU = 0, cX = D, cE = 2 * D, cP = 3 * D;
     static constexpr uint32_t COLS = STATE ? 2 * D : 512;
 };
@@ -156,16 +161,16 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     constexpr bool STAGED = !STATE && sizeof(OUT) == 2;  // bf16 outputs leave by TMA from the chunk's c slot
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = align_1024(smem_raw);
-    uint8_t *terms = sm + kSlots * C::TILE;           // b2, b3 (b1 overwrites b in its slot)
-    uint8_t *Xop = terms + (NT - 1) * C::TILE;
+    uint8_t *terms = sm + kSlots * C::TILE;
+    uint8_t *Xop = terms + C::TERMS * C::TILE;
     float *pw = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));  // lambda^0 .. lambda^128
     float *diag = pw + 132;
     uint64_t *bars = reinterpret_cast<uint64_t *>(diag + 4 * kDiagCopy);
     uint64_t *full = bars, *freeb = bars + kSlots, *pready = bars + 2 * kSlots;
-    uint64_t *eready = pready + 1, *scaled = pready + 2, *uready = pready + 3, *xready = pready + 4;
-    uint64_t *masked = pready + 5, *oready = pready + 6, *efree = pready + 7, *ufree = pready + 8;
-    uint64_t *stored = pready + 9;
-    uint32_t *tslot = reinterpret_cast<uint32_t *>(pready + 10);
+    uint64_t *eready = pready + 1, *scaled = pready + 2 /* of each half */, *uread = pready + 4 /* of each half */;
+    uint64_t *xready = pready + 6, *masked = pready + 7, *oready = pready + 8, *efree = pready + 9, *ufree = pready + 10;
+    uint64_t *stored = pready + 11;
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(pready + 12);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     constexpr int kTma = C::WARPS, kMma = kTma + 1;
     constexpr int kStateWarp0 = kScaleWarps, kScoreWarp0 = kScaleWarps + kStateWarps;
@@ -182,8 +187,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
 
     if (tid == 0) {
         for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 1); mbar_init(freeb + i, 1); }
-        mbar_init(pready, 1); mbar_init(eready, 1); mbar_init(uready, 1); mbar_init(oready, 1);
-        mbar_init(scaled, kScaleWarps); mbar_init(xready, kStateWarps); mbar_init(ufree, kStateWarps);
+        mbar_init(pready, 1); mbar_init(eready, 1); mbar_init(oready, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(scaled + i, kScaleWarps); mbar_init(uread + i, 1); }
+        mbar_init(xready, kStateWarps); mbar_init(ufree, kStateWarps);
         mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps * D / 128);
         fence_mbar_init();
     }
@@ -219,6 +225,13 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             uint32_t uses = 0;  // bit s: parity of the phases of freeb[s] waited for
             for (int c = 0; c < nch && !failed; ++c) {
                 const int row = chunk_row(c);
+                // the slots hold little more than a chunk, less than a load's way from DRAM: ask L2 for the tiles
+                // two chunks ahead
+                for (int cp = c == 0 ? 1 : c + kAhead; cp <= c + kAhead && cp < nch; ++cp)
+                    for (int w = 3 - LOADS; w < 3; ++w)
+                        for (int k = 0; k < C::KB; ++k)
+                            tma_prefetch_4d(w == 0 ? &mapA : w == 1 ? &mapB : &mapC, 64 * k, chunk_row(cp),
+                                            w == 0 ? ha : w == 1 ? hb : hc, b);
 #pragma unroll
                 for (int w = 3 - LOADS; w < 3; ++w, ++L) {
                     const int s = L % kSlots;
@@ -245,27 +258,31 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             constexpr uint32_t idP = idesc_bf16(128, 128, false, false);
             constexpr uint32_t idE = idesc_bf16(128, D, false, true);
             constexpr uint32_t idU = idesc_bf16(D, D, true, true);
+            auto slot_addr = [&](int L) { return base + (L % kSlots) * C::TILE; };
+            auto scores = [&](int c) {  // P = a b^T of chunk c
+                const int La = c * LOADS, Lb = La + 1;
+                wait(full + La % kSlots, (La / kSlots) & 1);
+                wait(full + Lb % kSlots, (Lb / kSlots) & 1);
+                if (failed) return;
+                tc_fence_after();
+                const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128), dB = sdesc(slot_addr(Lb), 16, 1024, kSwizzle128);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t o = (k / 4) * C::BLK + 32 * (k % 4);
+                    mma_bf16_ss(tb + C::cP, dadd(dA, o), dadd(dB, o), idP, k > 0);
+                }
+                mma_commit(pready);
+            };
+            if (!STATE && nch > 0) scores(0);
             for (int c = 0; c < nch && !failed; ++c) {
                 const int La = c * LOADS, Lb = La + LOADS - 2, Lc = Lb + 1;
                 const uint32_t ph = c & 1;
-                const uint32_t ta = base + (La % kSlots) * C::TILE, tbb = base + (Lb % kSlots) * C::TILE;
-                const uint32_t tc = base + (Lc % kSlots) * C::TILE;
-                wait(full + Lb % kSlots, (Lb / kSlots) & 1);
                 if (!STATE) {
-                    wait(full + La % kSlots, (La / kSlots) & 1);
-                    if (failed) break;
-                    tc_fence_after();
-                    const uint64_t dA = sdesc(ta, 16, 1024, kSwizzle128), dB = sdesc(tbb, 16, 1024, kSwizzle128);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t o = (k / 4) * C::BLK + 32 * (k % 4);
-                        mma_bf16_ss(tb + C::cP, dadd(dA, o), dadd(dB, o), idP, k > 0);
-                    }
-                    mma_commit(pready);
                     wait(xready, ph);
                     if (c > 0) wait(efree, (c - 1) & 1);
                     if (failed) break;
                     tc_fence_after();
+                    const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t o = (k / 4) * C::BLK + 32 * (k % 4);
@@ -274,19 +291,25 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                     mma_commit(eready);
                     mma_commit(freeb + La % kSlots);
                 }
-                wait(scaled, ph);
                 wait(full + Lc % kSlots, (Lc / kSlots) & 1);
                 if (STATE && c > 0) wait(ufree, (c - 1) & 1);  // (otherwise before X was ready)
+                const uint64_t dB1 = sdesc(C::INPLACE ? slot_addr(Lb) : smem_u32(terms), C::BLK, 1024, kSwizzle128);
+                const uint64_t dB2 = sdesc(smem_u32(terms) + (C::INPLACE ? 0 : C::TILE), C::BLK, 1024, kSwizzle128);
+                const uint64_t dC = sdesc(slot_addr(Lc), C::BLK, 1024, kSwizzle128);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    wait(scaled + half, ph);
+                    if (failed) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int q = 0; q < NT; ++q)
+#pragma unroll
+                        for (int k = 4 * half; k < 4 * half + 4; ++k)
+                            mma_bf16_ss(tb + C::cU, q == 0 ? dadd(dB1, 2048 * k) : dadd(dB2, (q - 1) * C::TILE + 2048 * k),
+                                        dadd(dC, 2048 * k), idU, (half | q | (k & 3)) != 0);
+                    mma_commit(uread + half);
+                }
                 if (failed) break;
-                tc_fence_after();
-                const uint64_t dB1 = sdesc(tbb, C::BLK, 1024, kSwizzle128), dC = sdesc(tc, C::BLK, 1024, kSwizzle128);
-#pragma unroll
-                for (int q = 0; q < NT; ++q)
-#pragma unroll
-                    for (int k = 0; k < kRows / 16; ++k)
-                        mma_bf16_ss(tb + C::cU, q == 0 ? dadd(dB1, 2048 * k) : dadd(dT, (q - 1) * C::TILE + 2048 * k),
-                                    dadd(dC, 2048 * k), idU, (q | k) != 0);
-                mma_commit(uready);
                 mma_commit(freeb + Lb % kSlots);
                 if (STATE) {
                     mma_commit(freeb + Lc % kSlots);
@@ -296,70 +319,73 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                     tc_fence_after();
 #pragma unroll
                     for (int k = 0; k < kRows / 16; ++k)
-                        mma_bf16_ts(tb + C::cE, tb + C::cP + 8 * k, dadd(dC, 2048 * k), idE, 1);
+                        mma_bf16_ts(tb + C::cE, tb + C::cP + 64 * (k / 4) + 8 * (k % 4), dadd(dC, 2048 * k), idE, 1);
                     mma_commit(oready);
                     if (!STAGED) mma_commit(freeb + Lc % kSlots);
+                    if (c + 1 < nch) scores(c + 1);
                 }
             }
         }
     } else if (warp < kScaleWarps) {
-        // the scaled terms of b: thread (row, half of its 16-byte pieces)
-        const int fr = tid & (kRows - 1), fp = tid / kRows;
-        constexpr int PIECES = D / 8 / (kScaleWarps * 32 / kRows);
+        // the scaled terms of b, rows of the first half and then of the second: thread (row, part of its pieces)
+        constexpr int PIECES = D / 8 / (kScaleWarps * 32 / 64);
+        const int hr = tid & 63, piece0 = (tid >> 6) * PIECES;
         for (int c = 0; c < nch; ++c) {
             const int nv = min(kRows, r1 - chunk_row(c));
             const uint32_t ph = c & 1;
             const int Lb = c * LOADS + LOADS - 2, Lc = Lb + 1;
             uint8_t *tbb = sm + (Lb % kSlots) * C::TILE, *tcc = sm + (Lc % kSlots) * C::TILE;
+            uint8_t *t1 = C::INPLACE ? tbb : terms, *t2 = terms + (C::INPLACE ? 0 : C::TILE);
             wait(full + Lb % kSlots, (Lb / kSlots) & 1);
-            if (!STATE) wait(pready, ph);             // P has read b
-            if (c > 0) wait(uready, (c - 1) & 1);     // the last chunk's terms have been read
-            const bool on = fr < nv;
-            const float w = on ? pw[nv - (a.reverse ? nv - 1 - fr : fr) - e] : 0.0f;
-            const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
-            uint4 in4[PIECES];
+            if (!STATE && C::INPLACE) wait(pready, ph);  // P has read b
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int r = half * 64 + hr;
+                const bool on = r < nv;
+                const float w = on ? a.u * pw[nv - (a.reverse ? nv - 1 - r : r) - e] : 0.0f;
+                const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
+                uint4 in4[PIECES];
 #pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int piece = fp * PIECES + q;
-                in4[q] = *reinterpret_cast<const uint4 *>(tbb + (piece / 8) * C::BLK + sw128_chunk(fr, piece % 8));
-            }
+                for (int q = 0; q < PIECES; ++q)
+                    in4[q] = *reinterpret_cast<const uint4 *>(tbb + ((piece0 + q) / 8) * C::BLK +
+                                                              sw128_chunk(r, (piece0 + q) % 8));
+                if (c > 0) wait(uread + half, (c - 1) & 1);  // the last chunk's terms have been read
 #pragma unroll
-            for (int q = 0; q < PIECES; ++q) {
-                const int piece = fp * PIECES + q;
-                const uint32_t off = (piece / 8) * C::BLK + sw128_chunk(fr, piece % 8);
-                uint4 v = in4[q];
-                if (!on) v = make_uint4(0, 0, 0, 0);  // rows past the length may hold anything
-                const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                uint32_t o1[4], o2[4], o3[4];
+                for (int q = 0; q < PIECES; ++q) {
+                    const uint32_t off = ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8);
+                    uint4 v = in4[q];
+                    if (!on) v = make_uint4(0, 0, 0, 0);  // rows past the length may hold anything
+                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                    uint32_t o1[4], o2[4], o3[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint64_t r = mul2(widen2(in[k]), w2);
-                    o1[k] = pack2(r);
-                    r = fma2(widen2(o1[k]), minus, r);
-                    o2[k] = pack2(r);
-                    if (NT == 3) o3[k] = pack2(fma2(widen2(o2[k]), minus, r));
+                    for (int k = 0; k < 4; ++k) {
+                        uint64_t x = mul2(widen2(in[k]), w2);
+                        o1[k] = pack2(x);
+                        x = fma2(widen2(o1[k]), minus, x);
+                        o2[k] = pack2(x);
+                        if (NT == 3) o3[k] = pack2(fma2(widen2(o2[k]), minus, x));
+                    }
+                    *reinterpret_cast<uint4 *>(t1 + off) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+                    *reinterpret_cast<uint4 *>(t2 + off) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
+                    if (NT == 3) *reinterpret_cast<uint4 *>(t2 + C::TILE + off) = make_uint4(o3[0], o3[1], o3[2], o3[3]);
                 }
-                *reinterpret_cast<uint4 *>(tbb + off) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
-                *reinterpret_cast<uint4 *>(terms + off) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
-                if (NT == 3) *reinterpret_cast<uint4 *>(terms + C::TILE + off) = make_uint4(o3[0], o3[1], o3[2], o3[3]);
-            }
-            if (nv < kRows) {  // c without the rows past the length
-                wait(full + Lc % kSlots, (Lc / kSlots) & 1);
-                if (!on) {
+                if (nv < kRows) {  // c without the rows past the length
+                    wait(full + Lc % kSlots, (Lc / kSlots) & 1);
+                    if (!on) {
 #pragma unroll
-                    for (int q = 0; q < PIECES; ++q) {
-                        const int piece = fp * PIECES + q;
-                        *reinterpret_cast<uint4 *>(tcc + (piece / 8) * C::BLK + sw128_chunk(fr, piece % 8)) =
-                            make_uint4(0, 0, 0, 0);
+                        for (int q = 0; q < PIECES; ++q)
+                            *reinterpret_cast<uint4 *>(tcc + ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8)) =
+                                make_uint4(0, 0, 0, 0);
                     }
                 }
+                fence_proxy_async_smem();
+                arrive(scaled + half);
             }
-            fence_proxy_async_smem();
-            arrive(scaled);
         }
     } else if (warp < kScoreWarp0) {
-        // state: thread = feature f; an accumulator's row f is lane f, or with 64 rows lane 32 (f / 16) + f % 16
-        const int quarter = warp & 3;
+        // state: thread (feature f, half of the columns); an accumulator's row f is lane f, or with 64 rows lane
+        // 32 (f / 16) + f % 16
+        const int quarter = warp & 3, cc0 = ((warp - kScaleWarps) >> 2) * (D / 2);
         const bool own = D == 128 || lane < 16;
         const int f = D == 128 ? quarter * 32 + lane : quarter * 16 + (lane & 15);
         const uint32_t lb = (uint32_t)(quarter * 32) << 16;
@@ -374,7 +400,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         };
         const float *X0 = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
 #pragma unroll 1
-        for (int cc = 0; cc < D; cc += 16) {
+        for (int cc = cc0; cc < cc0 + D / 2; cc += 16) {
             float x[16];
             uint32_t y[16];
 #pragma unroll
@@ -394,13 +420,14 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         for (int c = 0; c < nch; ++c) {
             const int nv = min(kRows, r1 - chunk_row(c));
             const uint32_t ph = c & 1;
-            wait(uready, ph);
+            wait(uread + 1, ph);
             if (!STATE) wait(eready, ph);  // E has read the operand
             tc_fence_after();
             const float dec = pw[nv];
-            const uint64_t dec2 = f2(dec, dec), u2 = f2(a.u, a.u);
+            const uint64_t dec2 = f2(dec, dec);
 #pragma unroll
-            for (int cc = 0; cc < D; cc += 16) {
+            for (int c1 = 0; c1 < D / 2; c1 += 16) {
+                const int cc = cc0 + c1;
                 uint32_t xu[16], xx[16];
                 tmem_ld16(tb + lb + C::cU + cc, xu);
                 tmem_ld16(tb + lb + C::cX + cc, xx);
@@ -408,7 +435,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                 float x[16];
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    unpack2(fma2(dec2, f2(xx[k], xx[k + 1]), mul2(u2, f2(xu[k], xu[k + 1]))), x[k], x[k + 1]);
+                    unpack2(fma2(dec2, f2(xx[k], xx[k + 1]), f2(xu[k], xu[k + 1])), x[k], x[k + 1]);
                     xx[k] = __float_as_uint(x[k]);
                     xx[k + 1] = __float_as_uint(x[k + 1]);
                 }
@@ -427,7 +454,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         if (a.Xout) {
             float *X = a.Xout + (bh * a.nseg + seg) * a.da * a.dc + (int64_t)f * a.dc;
 #pragma unroll 1
-            for (int cc = 0; cc < D; cc += 16) {
+            for (int cc = cc0; cc < cc0 + D / 2; cc += 16) {
                 uint32_t x[16];
                 tmem_ld16(tb + lb + C::cX + cc, x);
                 tmem_wait_ld();
@@ -445,23 +472,26 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         const int gw = warp - kScoreWarp0, quarter = warp & 3, part = gw >> 2, i = quarter * 32 + lane;
         const uint32_t lb = (uint32_t)(quarter * 32) << 16;
         OUT *O = static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh;
+        const bool stores = lane == 0 && (D == 128 || part == 0);
+        auto give_slot = [&]() {  // the last chunk's outputs have left their slot
+            if (stores) {
+                bulk_wait_read();
+                mbar_arrive(stored);
+            }
+            __syncwarp();
+        };
         for (int c = 0; c < nch; ++c) {
             const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
             const uint32_t ph = c & 1;
             wait(pready, ph);
             tc_fence_after();
-            {
-                uint32_t w[2][16];
 #pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    decay_scores(tb + lb + C::cP + part * PC + 32 * q, i, part * 2 + q, a.reverse != 0, nv, a.p, pw, diag, w[q]);
-                // the bf16 scores overwrite the first half of P: after both warps of the rows have read theirs
-                tc_fence_before();
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
-                tc_fence_after();
-#pragma unroll
-                for (int q = 0; q < 2; ++q) tmem_st16(tb + lb + C::cP + part * (PC / 2) + 16 * q, w[q]);
+            for (int q = 0; q < 2; ++q) {  // the bf16 scores take the place of columns that this warp has read
+                uint32_t w[16];
+                decay_scores(tb + lb + C::cP + part * PC + 32 * q, i, part * 2 + q, a.reverse != 0, nv, a.p, pw, diag, w);
+                tmem_st16(tb + lb + C::cP + part * PC + 16 * q, w);
             }
+            if (STAGED && c > 0) give_slot();
             wait(eready, ph);
             tc_fence_after();
             const int m = a.reverse ? nv - 1 - i : i;
@@ -527,18 +557,16 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                 fence_proxy_async_smem();
                 if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
                 else __syncwarp();
-                if (lane == 0 && (D == 128 || part == 0)) {
+                if (stores) {
                     const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
                     if (row < a.n && 64 * blk < a.dc)
                         tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, h, b);
                     bulk_commit();
-                    bulk_wait_read();
-                    mbar_arrive(stored);
                 }
                 __syncwarp();
             }
         }
-        if (STAGED && lane == 0) bulk_wait();
+        if (STAGED && stores) bulk_wait();
         // rows at and past the length
         constexpr int ZB = 16 / (int)sizeof(OUT), GT = kScoreWarps * 32;
         const int gt = tid - kScoreWarp0 * 32, pieces = a.dc / ZB, step = GT / pieces;
