@@ -25,6 +25,7 @@ __device__ __forceinline__ const T *row_base(const RowView &v, int b, int h, int
 template <typename IO, typename OUT>
 __global__ void __launch_bounds__(kMixThreads) k_decay_mix(DecayMix a) {
     extern __shared__ float sm[];
+    clear_status(a);
     const int da = a.da, lda = da + 1;
     float *sa = sm, *sb = sa + kCh * lda, *sc = sb + kCh * lda, *sP = sc + kCh * (kCols + 1);
     float *sX = sP + kCh * (kCh + 1), *pw = sX + da * kCols;

@@ -42,6 +42,7 @@ struct DecayMix {
     int x_trans;          // X is stored [dc][da]
     float *Xout;          // carry out of every piece, [bh][s][da][dc], or NULL
     int *status;          // device status word of the call
+    int clear;            // first launch of the call: clears it
 };
 
 // Carries into the pieces from the pieces' own sums U (carry out of each from zero):
@@ -65,6 +66,11 @@ struct DecayStep {
     int nslots, B, H, Hkv, d, dv;
     float scale;
 };
+
+// The first block of a call's first kernel clears the status word; the waits that set it run for a second.
+__device__ __forceinline__ void clear_status(const DecayMix &a) {
+    if (a.clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = 0;
+}
 
 // log lambda of a head, with -inf (lambda = 0) as a finite value so that 0 * log lambda is 0.
 __device__ __forceinline__ float decay_log(const float *log_decay, int h) {

@@ -150,17 +150,17 @@ luna_status luna_decay_fwd(const luna_decay_desc *dd, const float *log_decay, co
     if (ws_bytes < p.fwd) return LUNA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
 
-    cudaError_t e = cudaMemsetAsync(ws, 0, sizeof(int), s);  // the status word of this call
-    if (e != cudaSuccess) return LUNA_ERR_CUDA;
     DecayMix a = base(dd, p, log_decay, lengths, ws);
     a.a = view(Q, sq, dd->H); a.b = view(K, sk, dd->Hkv); a.c = view(V, sv, dd->Hkv);
     a.da = dd->d; a.dc = dd->dv;
     a.p = a.x = dd->scale;
     float *X = reinterpret_cast<float *>(ws + p.o_X);
-    e = carries(a, p, dd->io, ws, S0, X, S1, s);
+    a.clear = 1;
+    cudaError_t e = carries(a, p, dd->io, ws, S0, X, S1, s);
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
     a.out = O;
     a.ob = so.b; a.oh = so.h; a.ot = so.t;
+    a.clear = p.nseg == 1;
     a.X = p.nseg == 1 ? S0 : X;
     a.x_pieces = p.nseg;
     a.Xout = p.nseg == 1 ? S1 : nullptr;
@@ -195,13 +195,14 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
     const RowView q = view(Q, sq, H), k = view(K, sk, Hkv), v = view(V, sv, Hkv), g = view(dO, go, H);
     float *X = reinterpret_cast<float *>(ws + p.o_X), *R = reinterpret_cast<float *>(ws + p.o_R);
     float *part = reinterpret_cast<float *>(ws + p.o_part);
-    cudaError_t e = cudaMemsetAsync(ws, 0, sizeof(int), s);
-    if (e != cudaSuccess) return LUNA_ERR_CUDA;
+    cudaError_t e;
 
     // states before every piece, gradients of the states after every piece
     DecayMix a = base(dd, p, log_decay, lengths, ws);
     a.a = k; a.b = k; a.c = v; a.da = d; a.dc = dv;
+    a.clear = 1;
     if ((e = carries(a, p, dd->io, ws, S0, X, nullptr, s)) != cudaSuccess) return LUNA_ERR_CUDA;
+    a.clear = 0;
     a.reverse = 1;
     a.a = q; a.b = q; a.c = g;
     a.u = dd->scale;
@@ -214,7 +215,9 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
     a.a = g; a.b = v; a.c = k; a.da = dv; a.dc = d;
     a.X = p.nseg == 1 ? S0 : X;
     a.out = dQ; a.ob = gq.b; a.oh = gq.h; a.ot = gq.t;
+    a.clear = p.nseg == 1;
     if ((e = launch_decay_mix(a, dd->io, dd->io, s)) != cudaSuccess) return LUNA_ERR_CUDA;
+    a.clear = 0;
 
     a.reverse = 1;
     a.x = 1.0f;

@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     using C = Cfg<D, NT, STATE>;
     constexpr bool STAGED = !STATE && sizeof(OUT) == 2;  // bf16 outputs leave by TMA from the chunk's c slot
     extern __shared__ uint8_t smem_raw[];
+    clear_status(a);
     uint8_t *sm = align_1024(smem_raw);
     uint8_t *terms = sm + kSlots * C::TILE;
     uint8_t *Xop = terms + C::TERMS * C::TILE;

@@ -24,6 +24,44 @@ __device__ __forceinline__ float at(const MatView &v, int64_t row, int64_t rows,
     return io_load(static_cast<const IO *>(v.p) + (v.kt ? k * v.ld + row : row * v.ld + k));
 }
 
+// VEC values (16 bytes, or one) as fp32.
+template <typename IO, int VEC>
+__device__ __forceinline__ void load_vec(const IO *p, float (&v)[VEC]) {
+    if (VEC == 1) {
+        v[0] = io_load(p);
+    } else {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (sizeof(IO) == 4) {
+                v[i] = __uint_as_float(x[i]);
+            } else {
+                v[2 * i % VEC] = __uint_as_float(x[i] << 16);
+                v[(2 * i + 1) % VEC] = __uint_as_float(x[i] & 0xffff0000u);
+            }
+        }
+    }
+}
+template <typename IO, int VEC>
+__device__ __forceinline__ void store_vec(IO *p, const float (&v)[VEC]) {
+    if (VEC == 1) {
+        io_store(p, v[0]);
+    } else {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (sizeof(IO) == 4) {
+                x[i] = __float_as_uint(v[i]);
+            } else {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i % VEC], v[(2 * i + 1) % VEC]);
+                memcpy(&x[i], &b, 4);
+            }
+        }
+        *reinterpret_cast<uint4 *>(p) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+}
+
 // 128 x 128 tile of A B^T over one piece of K: operands staged in shared memory 16 deep, eight by
 // eight sums a thread in fp32, the next step's values loaded while this one's are multiplied.
 // Bound by the fp32 FMA rate.
@@ -31,6 +69,7 @@ template <typename IO>
 __global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, int splits) {
     __shared__ float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+    clear_status(p.clear, p.status);
     const int64_t row0 = (int64_t)blockIdx.x * kT, col0 = (int64_t)blockIdx.y * kT;
     const int64_t k0 = (int64_t)blockIdx.z * depth, k1 = min(p.K, k0 + depth);
     float acc[8][8];
@@ -104,31 +143,101 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, int splits) {
     linear_finish<IO>(p, i / p.N, i % p.N, acc);
 }
 
-// dZ = dY act'(Z) (not written where there is no activation) and the column sums of dZ over a
-// block's rows, one partial row a block.  32 columns x 8 rows of threads.
-template <typename IO>
-__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ, int64_t m,
-                                                   int n, int act, int64_t rows, float *part) {
-    __shared__ float s[8][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-    const int64_t r0 = (int64_t)blockIdx.y * rows, r1 = min(m, r0 + rows);
-    float acc = 0.0f;
-    if (c < n)
-        for (int64_t r = r0 + w; r < r1; r += 8) {
-            float d = io_load(dY + r * lddy + c);
-            if (act != LUNA_LINEAR_NONE) {
-                d *= linear_slope(io_load(Z + r * ldz + c), act);
-                io_store(dZ + r * n + c, d);
-            }
-            acc += d;
-        }
-    s[w][threadIdx.x & 31] = acc;
-    __syncthreads();
-    if (part && w == 0 && c < n) {
+// A few rows of X (at most eight) against rows of W, both along k: a warp owns RW rows of W and `split`
+// warps share them, each with its part of k; every lane has its sums for all rows of X, so W is read
+// once, 16 bytes a lane and RW loads in flight, and X comes from the first-level cache.  Bound by the
+// bytes of W.
+template <typename IO, int VEC, int MR>
+__global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
+    constexpr int RW = 4;
+    __shared__ float part[8][MR * RW];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    clear_status(p.clear, p.status);
+    const int64_t row0 = ((int64_t)blockIdx.x * (8 / split) + warp / split) * RW;
+    const int64_t units = p.K / VEC;  // (VEC = 1 otherwise)
+    const int64_t u0 = units * (warp % split) / split, u1 = units * (warp % split + 1) / split;
+    const IO *W = static_cast<const IO *>(p.B.p), *X = static_cast<const IO *>(p.A.p);
+    float acc[MR][RW];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) acc += s[i][threadIdx.x & 31];
-        part[(int64_t)blockIdx.y * n + c] = acc;
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+        for (int r = 0; r < RW; ++r) acc[i][r] = 0.0f;
+    const IO *w[RW];
+#pragma unroll
+    for (int r = 0; r < RW; ++r) w[r] = W + min(row0 + r, p.N - 1) * p.B.ld;
+#pragma unroll 2
+    for (int64_t u = u0 + lane; u < u1; u += 32) {
+        float wv[RW][VEC];
+#pragma unroll
+        for (int r = 0; r < RW; ++r) load_vec<IO, VEC>(w[r] + u * VEC, wv[r]);
+#pragma unroll
+        for (int i = 0; i < MR; ++i) {
+            float xv[VEC];
+            load_vec<IO, VEC>(X + min((int64_t)i, p.M - 1) * p.A.ld + u * VEC, xv);
+#pragma unroll
+            for (int r = 0; r < RW; ++r)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[i][r] = fmaf(xv[e], wv[r][e], acc[i][r]);
+        }
     }
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) acc[i][r] += __shfl_xor_sync(0xffffffffu, acc[i][r], o);
+            if (lane == 0) part[warp][i * RW + r] = acc[i][r];
+        }
+    __syncthreads();
+    // one thread an output: group of `split` warps, row of X, row of W
+    for (int t = threadIdx.x; t < (8 / split) * MR * RW; t += 256) {
+        const int g = t / (MR * RW), j = t % (MR * RW);
+        const int64_t row = j / RW, col = ((int64_t)blockIdx.x * (8 / split) + g) * RW + j % RW;
+        float sum = 0.0f;
+        for (int k = 0; k < split; ++k) sum += part[g * split + k][j];
+        if (row < p.M && col < p.N) linear_finish<IO>(p, row, col, sum);
+    }
+}
+
+// dZ = dY act'(Z) (not written where there is no activation) and the column sums of dZ over a
+// block's rows, one partial row a block.  32 column pieces x 8 rows of threads; bound by the bytes.
+template <typename IO, int VEC>
+__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ, int64_t m,
+                                                   int n, int act, int64_t rows, float *part, int *status) {
+    __shared__ float s[8][32 * VEC + 1];
+    clear_status(1, status);
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * VEC;
+    const int64_t r0 = (int64_t)blockIdx.y * rows, r1 = min(m, r0 + rows);
+    float acc[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+    if (c < n) {
+#pragma unroll 4
+        for (int64_t r = r0 + w; r < r1; r += 8) {
+            float d[VEC];
+            load_vec<IO, VEC>(dY + r * lddy + c, d);
+            if (act != LUNA_LINEAR_NONE) {
+                float z[VEC];
+                load_vec<IO, VEC>(Z + r * ldz + c, z);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[e] *= linear_slope<IO>(z[e], act);
+                store_vec<IO, VEC>(dZ + r * n + c, d);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] += d[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[w][lane * VEC + e] = acc[e];
+    __syncthreads();
+    if (part)
+        for (int t = threadIdx.x; t < 32 * VEC; t += 256) {
+            const int col = blockIdx.x * 32 * VEC + t;
+            float a = s[0][t];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) a += s[i][t];
+            if (col < n) part[(int64_t)blockIdx.y * n + col] = a;
+        }
 }
 
 template <typename IO>
@@ -158,15 +267,42 @@ cudaError_t simt(const Product &p, cudaStream_t s) {
 
 constexpr int64_t kDzRows = 256;  // rows of a block of the column sums
 
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename IO, int VEC>
+void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t m, int n, int act, float *part,
+               int parts, int *status, cudaStream_t s) {
+    LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC>), dim3((unsigned)cdiv(n, 32 * VEC), parts), 256, 0, s,
+                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), m, n, act, kDzRows,
+                part, status);
+}
+
 template <typename IO>
 cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t m, int n, int act, float *part,
-               void *db, cudaStream_t s) {
+               void *db, int *status, cudaStream_t s) {
+    constexpr int VEC = 16 / (int)sizeof(IO);
     const int parts = (int)cdiv(m, kDzRows);
-    LUNA_LAUNCH("linear_dz", k_linear_dz<IO>, dim3((unsigned)cdiv(n, 32), parts), 256, 0, s, static_cast<const IO *>(dY), lddy,
-                static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), m, n, act, kDzRows, db ? part : nullptr);
+    const bool a = act != LUNA_LINEAR_NONE;
+    if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
+        dz_launch<IO, VEC>(dY, lddy, Z, ldz, dZ, m, n, act, db ? part : nullptr, parts, status, s);
+    else
+        dz_launch<IO, 1>(dY, lddy, Z, ldz, dZ, m, n, act, db ? part : nullptr, parts, status, s);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !db) return e;
     LUNA_LAUNCH("linear_db", k_linear_db<IO>, (unsigned)cdiv(n, 256), 256, 0, s, part, parts, n, static_cast<IO *>(db));
+    return cudaGetLastError();
+}
+
+template <typename IO, int VEC>
+cudaError_t rows_launch(const Product &p, cudaStream_t s) {
+    // warps that share four rows of W: as many as keep some 2000 warps at work, with 16 loads each at least
+    int split = 1;
+    while (split < 8 && cdiv(p.N, 4) * split < 2000 && p.K / VEC / (split * 2) >= 128) split *= 2;
+    const unsigned grid = (unsigned)cdiv(cdiv(p.N, 4) * split, 8);
+    if (p.M == 1) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 1>), grid, 256, 0, s, p, split);
+    else if (p.M == 2) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 2>), grid, 256, 0, s, p, split);
+    else if (p.M <= 4) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 4>), grid, 256, 0, s, p, split);
+    else LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 8>), grid, 256, 0, s, p, split);
     return cudaGetLastError();
 }
 
@@ -227,7 +363,19 @@ cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, c
     return cudaGetLastError();
 }
 
+bool product_rows_ok(const Product &p) { return p.M <= 8 && p.K > 0 && !p.A.kt && !p.B.kt; }
+
+cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s) {
+    const int vec = io == LUNA_F32 ? 4 : 8;
+    const bool v = p.K % vec == 0 && al16(p.A.p) && al16(p.B.p) && p.A.ld % vec == 0 && p.B.ld % vec == 0;
+    if (io == LUNA_F32) return v ? rows_launch<float, 4>(p, s) : rows_launch<float, 1>(p, s);
+    return v ? rows_launch<__nv_bfloat16, 8>(p, s) : rows_launch<__nv_bfloat16, 1>(p, s);
+}
+
+// Up to eight rows of X the product is a read of W (at m = 8, n = 8192, k = 4096 the fp32 sums take about
+// as long as the bytes); tensor cores take what is aligned beyond that.
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
+    if (product_rows_ok(p)) return launch_product_rows(p, io, s);
     return io == LUNA_BF16 && product_tc_ok(p) ? launch_product_tc(p, s) : launch_product_simt(p, io, s);
 }
 
@@ -265,7 +413,7 @@ luna_status luna_linear_fwd(const luna_linear_desc *ld, const void *X, const voi
     p.ldr = ld->ldr ? ld->ldr : ld->n; p.ldz = ld->ldz ? ld->ldz : ld->n; p.ldo = ld->ldy ? ld->ldy : ld->n;
     p.part = reinterpret_cast<float *>(ws + pl.o_part); p.part_bytes = pl.part_fwd;
     p.status = reinterpret_cast<int *>(ws);
-    if (cudaMemsetAsync(ws, 0, sizeof(int), s) != cudaSuccess) return LUNA_ERR_CUDA;
+    p.clear = 1;
     return cuda_status(launch_product(p, ld->io, s));
 }
 
@@ -289,13 +437,13 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     if (ws_bytes < pl.bwd) return LUNA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     float *part = reinterpret_cast<float *>(ws + pl.o_part);
-    if (cudaMemsetAsync(ws, 0, sizeof(int), s) != cudaSuccess) return LUNA_ERR_CUDA;
+    int *status = reinterpret_cast<int *>(ws);
     const int64_t lddy = ld->lddy ? ld->lddy : n, ldz = ld->ldz ? ld->ldz : n;
     cudaError_t e = cudaSuccess;
     if (act || db) {
         void *dZ = ws + pl.o_dz;
-        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, s)
-                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, s);
+        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, status, s)
+                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, status, s);
         if (e != cudaSuccess) return LUNA_ERR_CUDA;
     }
     if (k == 0) return LUNA_OK;
@@ -305,13 +453,15 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     memset(&p, 0, sizeof(p));
     p.act = LUNA_LINEAR_NONE;
     p.part = part; p.part_bytes = pl.part_bwd;
-    p.status = reinterpret_cast<int *>(ws);
+    p.status = status;
+    p.clear = !(act || db);
     if (dX) {
         p.A = MatView{G, ldg, false};
         p.B = MatView{W, ldw, true};
         p.M = m; p.N = k; p.K = n;
         p.out = dX; p.ldo = ld->lddx ? ld->lddx : k;
         if ((e = launch_product(p, ld->io, s)) != cudaSuccess) return LUNA_ERR_CUDA;
+        p.clear = 0;
     }
     if (dW) {
         p.A = MatView{G, ldg, true};

@@ -29,23 +29,54 @@ struct Product {
     float *part;           // fp32 partial products [split][M][N]
     size_t part_bytes;
     int *status;           // device status word
+    int clear;             // first launch of the call: clears it
 };
 
+// The first block of a call's first kernel clears the status word; the waits that set it run for a second.
+__device__ __forceinline__ void clear_status(int clear, int *status) {
+    if (clear && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *status = 0;
+}
+
+// The standard normal distribution function and its density.  With fp32 outputs by erff; with bf16
+// outputs the upper tail from Abramowitz and Stegun 7.1.26 (erfc(x) = t (a1 + ... + a5 t^4) e^{-x^2},
+// t = 1 / (1 + p x)), which shares its exponential with the density and keeps Phi(z) below zero to
+// 2^-9 relative down to z = -5: 12 operations against about 40 an element, which the epilogue of a
+// product of depth 1024 has no time for.
+template <typename IO>
+__device__ __forceinline__ float normal_cdf(float z, float &density) {
+    const float e = __expf(-0.5f * z * z);
+    density = 0.39894228040143268f * e;
+    if (sizeof(IO) == 4) return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    const float tail = 0.5f * t * q * e;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+template <typename IO>
 __device__ __forceinline__ float linear_act(float z, int act) {
+    float d;
     switch (act) {
         case LUNA_LINEAR_RELU: return z > 0.0f ? z : (z == z ? 0.0f : z);
-        case LUNA_LINEAR_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+        case LUNA_LINEAR_GELU: return z * normal_cdf<IO>(z, d);
         case LUNA_LINEAR_SILU: return __fdividef(z, 1.0f + __expf(-z));
     }
     return z;
 }
 
 // d act / d z
+template <typename IO>
 __device__ __forceinline__ float linear_slope(float z, int act) {
     switch (act) {
         case LUNA_LINEAR_RELU: return z > 0.0f ? 1.0f : 0.0f;
-        case LUNA_LINEAR_GELU:
-            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * __expf(-0.5f * z * z);
+        case LUNA_LINEAR_GELU: {
+            float d;
+            const float c = normal_cdf<IO>(z, d);
+            return fmaf(z, d, c);
+        }
         case LUNA_LINEAR_SILU: {
             const float s = __fdividef(1.0f, 1.0f + __expf(-z));
             return s * (1.0f + z * (1.0f - s));
@@ -59,7 +90,7 @@ template <typename IO>
 __device__ __forceinline__ void linear_finish(const Product &p, int64_t row, int64_t col, float sum) {
     if (p.bias) sum += io_load(static_cast<const IO *>(p.bias) + col);
     if (p.Z) io_store(static_cast<IO *>(p.Z) + row * p.ldz + col, sum);
-    float y = linear_act(sum, p.act);
+    float y = linear_act<IO>(sum, p.act);
     if (p.R) y += io_load(static_cast<const IO *>(p.R) + row * p.ldr + col);
     io_store(static_cast<IO *>(p.out) + row * p.ldo + col, y);
 }
@@ -70,6 +101,8 @@ int linear_splits(const Product &p, int64_t tiles, int64_t least);
 
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);          // picks a kernel
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
+bool product_rows_ok(const Product &p);                                               // a few rows of X
+cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s);
 bool product_tc_ok(const Product &p);                                                 // aligned operands
 cudaError_t launch_product_tc(const Product &p, cudaStream_t s);                      // bf16, tensor cores
 cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);

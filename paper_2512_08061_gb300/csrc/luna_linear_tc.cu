@@ -93,7 +93,7 @@ __device__ __forceinline__ void finish_vec(const Product &p, int64_t row, int64_
     }
     if (ACT != LUNA_LINEAR_NONE) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = linear_act(v[i], ACT);
+        for (int i = 0; i < 32; ++i) v[i] = linear_act<B>(v[i], ACT);
     }
     if (p.R) {
         const uint4 *r = reinterpret_cast<const uint4 *>(static_cast<const B *>(p.R) + row * p.ldr + col);
@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     uint32_t *tslot = reinterpret_cast<uint32_t *>(tempty + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    clear_status(a.p.clear, a.p.status);
     if (tid == 0) {
         for (int i = 0; i < S; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(tfull + i, 1); mbar_init(tempty + i, CG * kEpiWarps); }

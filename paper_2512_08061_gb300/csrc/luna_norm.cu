@@ -48,19 +48,18 @@ struct NormArgs {
     int gmode;         // how a group is summed: 0 whole row, 1 lanes of a warp, 2 through shared memory
 };
 
+// VEC values as they are loaded (16 bytes, or one value), and as fp32.
 template <typename IO, int VEC> struct Vec;
 template <> struct Vec<float, 4> {
-    static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
-        const float4 w = *reinterpret_cast<const float4 *>(p);
-        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-    }
+    using Raw = float4;
+    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[4]) { v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w; }
     static __device__ __forceinline__ void store(float *p, const float (&v)[4]) {
         *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
     }
 };
 template <> struct Vec<__nv_bfloat16, 8> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&v)[8]) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    using Raw = uint4;
+    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[8]) {
         const uint32_t b[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -79,7 +78,8 @@ template <> struct Vec<__nv_bfloat16, 8> {
     }
 };
 template <typename IO> struct Vec<IO, 1> {
-    static __device__ __forceinline__ void load(const IO *p, float (&v)[1]) { v[0] = io_load(p); }
+    using Raw = IO;
+    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[1]) { v[0] = io_load(&w); }
     static __device__ __forceinline__ void store(IO *p, const float (&v)[1]) { io_store(p, v[0]); }
 };
 
@@ -231,17 +231,28 @@ __device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], R
     }
 }
 
-template <typename IO, int VEC, int NV>
-__device__ __forceinline__ void load_row(const void *p, int64_t off, float (&v)[NV][VEC], int t, int threads, int active) {
+// A thread's part of one row of a matrix, as loaded; nothing of an absent matrix.
+template <typename IO, int VEC, int NV> struct RowPart {
+    typename Vec<IO, VEC>::Raw raw[NV];
+    __device__ __forceinline__ void fetch(const void *p, int64_t off, int t, int threads, int active) {
+        if (!p) return;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (i < active) {
-            Vec<IO, VEC>::load(static_cast<const IO *>(p) + off + (int64_t)(t + i * threads) * VEC, v[i]);
-        } else {
+        for (int i = 0; i < NV; ++i)
+            if (i < active)
+                raw[i] = *reinterpret_cast<const typename Vec<IO, VEC>::Raw *>(static_cast<const IO *>(p) + off +
+                                                                              (int64_t)(t + i * threads) * VEC);
+    }
+    __device__ __forceinline__ void get(const void *p, float (&v)[NV][VEC], int active) const {  // zeros where there is nothing
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[i][e] = 0.0f;
-        }
-}
+        for (int i = 0; i < NV; ++i)
+            if (p && i < active) {
+                Vec<IO, VEC>::unpack(raw[i], v[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[i][e] = 0.0f;
+            }
+    }
+};
 
 template <typename IO, int VEC, int NV>
 __device__ __forceinline__ void store_row(void *p, int64_t off, const float (&v)[NV][VEC], int t, int threads, int active) {
@@ -268,67 +279,81 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(false)) k_norm_fwd(NormAr
     extern __shared__ float sm[];
     const int nvec = a.cols / VEC;
     RowTeam<NV> tm = make_team<NV>(a, nvec, sm);
-    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    if (row >= a.rows) return;  // whole warps: a block with one row never gets here
     int grp[NV];
     const int active = my_vectors<VEC, NV>(a, nvec, grp);
-    float z[NV][VEC], x[NV][VEC], g[NV][VEC], r[NV];
-    if (a.x) load_row<IO, VEC, NV>(a.x, row * a.ldx, x, tm.t, tm.threads, active);
-    if (a.y) load_row<IO, VEC, NV>(a.y, row * a.ldy, z, tm.t, tm.threads, active);
-    if (a.gate) load_row<IO, VEC, NV>(a.gate, row * a.ldgate, g, tm.t, tm.threads, active);
-    if (a.y) {
-        if (a.w_post) {
-            normalise<VEC, NV>(z, r, tm, a, true, grp, active);
+    const int t = tm.t, T = tm.threads;
+    // the next row is on its way while this one is worked on
+    constexpr bool AHEAD = VEC > 1 && NV <= 2;
+    RowPart<IO, VEC, NV> px, py, pg;
+    auto fetch = [&](int64_t row) {
+        px.fetch(a.x, row * a.ldx, t, T, active);
+        py.fetch(a.y, row * a.ldy, t, T, active);
+        pg.fetch(a.gate, row * a.ldgate, t, T, active);
+    };
+    const int64_t slots = (int64_t)gridDim.x * blockDim.y;
+    int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    if (AHEAD && row < a.rows) fetch(row);
+    for (; row < a.rows; row += slots) {
+        if (!AHEAD) fetch(row);
+        float z[NV][VEC], x[NV][VEC], g[NV][VEC], r[NV];
+        px.get(a.x, x, active);
+        py.get(a.y, z, active);
+        pg.get(a.gate, g, active);
+        if (AHEAD && row + slots < a.rows) fetch(row + slots);
+        if (a.y) {
+            if (a.w_post) {
+                normalise<VEC, NV>(z, r, tm, a, true, grp, active);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (i < active) {
+                        const int c = (tm.t + i * tm.threads) * VEC;
+                        float w[VEC];
+                        load_w<VEC>(a.w_post, c, w);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
+                        if (a.b_post) {
+                            load_w<VEC>(a.b_post, c, w);
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
+                        }
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    float v = z[i][e];
+                    if (a.gate && i < active) {
+                        const float sg = sigmoidf(g[i][e]);
+                        v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
+                    }
+                    z[i][e] = a.x ? fmaf(a.alpha, v, x[i][e]) : a.alpha * v;
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) z[i][e] = x[i][e];
+        }
+        if (a.X) store_row<IO, VEC, NV>(a.X, row * a.ldX, z, tm.t, tm.threads, active);
+        if (a.w_pre) {
+            normalise<VEC, NV>(z, r, tm, a, false, grp, active);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < active) {
                     const int c = (tm.t + i * tm.threads) * VEC;
                     float w[VEC];
-                    load_w<VEC>(a.w_post, c, w);
+                    load_w<VEC>(a.w_pre, c, w);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
-                    if (a.b_post) {
-                        load_w<VEC>(a.b_post, c, w);
+                    if (a.b_pre) {
+                        load_w<VEC>(a.b_pre, c, w);
 #pragma unroll
                         for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
                     }
                 }
+            store_row<IO, VEC, NV>(a.H, row * a.ldH, z, tm.t, tm.threads, active);
         }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                float v = z[i][e];
-                if (a.gate && i < active) {
-                    const float sg = sigmoidf(g[i][e]);
-                    v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
-                }
-                z[i][e] = a.x ? fmaf(a.alpha, v, x[i][e]) : a.alpha * v;
-            }
-    } else {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) z[i][e] = x[i][e];
-    }
-    if (a.X) store_row<IO, VEC, NV>(a.X, row * a.ldX, z, tm.t, tm.threads, active);
-    if (a.w_pre) {
-        normalise<VEC, NV>(z, r, tm, a, false, grp, active);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < active) {
-                const int c = (tm.t + i * tm.threads) * VEC;
-                float w[VEC];
-                load_w<VEC>(a.w_pre, c, w);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
-                if (a.b_pre) {
-                    load_w<VEC>(a.b_pre, c, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
-                }
-            }
-        store_row<IO, VEC, NV>(a.H, row * a.ldH, z, tm.t, tm.threads, active);
     }
 }
 
@@ -393,21 +418,25 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArg
             if (BIAS) sb_post[i][e] = sb_pre[i][e] = 0.0f;
         }
     const int64_t slots = (int64_t)gridDim.x * blockDim.y, slot = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    constexpr bool AHEAD = VEC > 1 && NV <= 2;  // as in the forward pass
+    RowPart<IO, VEC, NV> px, py, pg, pdX, pdH;
+    auto fetch = [&](int64_t row) {
+        py.fetch(a.y, row * a.ldy, t, T, active);
+        pg.fetch(a.gate, row * a.ldgate, t, T, active);
+        px.fetch(a.x, row * a.ldx, t, T, active);
+        pdX.fetch(a.dX, row * a.lddX, t, T, active);
+        pdH.fetch(a.dH, row * a.lddH, t, T, active);
+    };
+    if (AHEAD && slot < a.rows) fetch(slot);
     for (int64_t row = slot; row < a.rows; row += slots) {
-        float z[NV][VEC], g[NV][VEC], x[NV][VEC], d[NV][VEC], ry[NV], rx[NV];
-        if (a.y) load_row<IO, VEC, NV>(a.y, row * a.ldy, z, t, T, active);
-        if (a.gate) load_row<IO, VEC, NV>(a.gate, row * a.ldgate, g, t, T, active);
-        if (a.x) load_row<IO, VEC, NV>(a.x, row * a.ldx, x, t, T, active);
-        if (a.dX) {
-            load_row<IO, VEC, NV>(a.dX, row * a.lddX, d, t, T, active);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) d[i][e] = 0.0f;
-        }
-        float dh[NV][VEC];
-        if (a.w_pre) load_row<IO, VEC, NV>(a.dH, row * a.lddH, dh, t, T, active);
+        if (!AHEAD) fetch(row);
+        float z[NV][VEC], g[NV][VEC], x[NV][VEC], d[NV][VEC], dh[NV][VEC], ry[NV], rx[NV];
+        py.get(a.y, z, active);
+        pg.get(a.gate, g, active);
+        px.get(a.x, x, active);
+        pdX.get(a.dX, d, active);
+        pdH.get(a.dH, dh, active);
+        if (AHEAD && row + slots < a.rows) fetch(row + slots);
         if (a.y && a.w_post) normalise<VEC, NV>(z, ry, tm, a, true, grp, active);
         // u of vector i (post-norm output, before the gate)
         auto u_of = [&](int i, float (&u)[VEC]) {
@@ -427,12 +456,6 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArg
             }
         };
         if (a.w_pre) {
-            if (!a.x) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) x[i][e] = 0.0f;
-            }
             if (a.y) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
@@ -607,7 +630,9 @@ template <typename IO, int VEC, int NV>
 cudaError_t fwd_launch(const NormArgs &a, const Shape &sh, cudaStream_t s) {
     cudaError_t e = big_smem(k_norm_fwd<IO, VEC, NV>, sh.smem);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)((a.rows + sh.rows_per_block - 1) / sh.rows_per_block);
+    // as many blocks as the device holds at once, 1024 threads an SM
+    const int64_t most = (int64_t)152 * std::max(1, 1024 / (sh.threads * sh.rows_per_block));
+    const unsigned grid = (unsigned)std::min<int64_t>(most, (a.rows + sh.rows_per_block - 1) / sh.rows_per_block);
     LUNA_LAUNCH("norm_fwd", (k_norm_fwd<IO, VEC, NV>), grid, dim3(sh.threads, sh.rows_per_block), sh.smem, s, a);
     return cudaGetLastError();
 }

@@ -473,49 +473,116 @@ def _dense(name: str, t) -> None:
         raise ValueError(f"{name}: not contiguous")
 
 
-class Decay:
-    """Linear attention with a decay for each head at one problem shape; owns the workspace.
-    Q: (B, H, n, d), K: (B, Hkv, n, d), V: (B, Hkv, n, dv), any strides with a contiguous last
-    dimension; log_decay: (H,) fp32; lengths: (B,) int32 or None; states: (B, H, d, dv) fp32."""
+def _layout(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+# the current stream's handle without the stream object around it, where torch offers that (a single
+# token's kernels take less time than the object does)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _handle(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
+
+
+class _Checked:
+    """Calls of one problem shape.  The arguments' shapes, strides, types and devices are looked at in full
+    when they differ from those of the last call of the same kind, and their strides put into that
+    kind's descriptor."""
+
+    def __init__(self, desc):
+        self._desc = {kind: type(desc).from_buffer_copy(desc) for kind in ("forward", "backward", "step")}
+        self._ref = {kind: ctypes.byref(d) for kind, d in self._desc.items()}
+        self._seen = {}
+
+    def _looked_at(self, kind: str, *tensors) -> bool:
+        """Whether these layouts are the last call's; the caller checks and fills in the descriptor if not."""
+        layouts = [_layout(t) for t in tensors]
+        if self._seen.get(kind) == layouts:
+            return True
+        self._seen[kind] = None
+        self._pending = (kind, layouts)
+        return False
+
+    def _accept(self) -> None:
+        kind, layouts = self._pending
+        self._seen[kind] = layouts
+
+
+class Decay(_Checked):
+    """Linear attention with a decay for each head at one problem shape; owns the workspace, so its calls
+    belong on one stream at a time.  Q: (B, H, n, d), K: (B, Hkv, n, d), V: (B, Hkv, n, dv), any strides
+    with a contiguous last dimension; log_decay: (H,) fp32; lengths: (B,) int32 or None; states:
+    (B, H, d, dv) fp32."""
 
     def __init__(self, B, H, n, d, dv, Hkv=None, scale=None, io=torch.bfloat16, device="cuda", backward=False):
         self.dd = decay_desc(B, H, n, d, dv, Hkv, scale, _DTYPES[io])
+        super().__init__(self.dd)
         self.io, self.device = io, torch.device(device)
         self.ws = alloc_bytes(luna_decay_workspace_size(self.dd, backward), self.device)
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
         self.shapes = {"q": (B, H, n, d), "k": (B, self.dd.Hkv, n, d), "v": (B, self.dd.Hkv, n, dv), "o": (B, H, n, dv)}
         self.state_shape = (B, H, d, dv)
 
-    def _view(self, field: str, t) -> None:
-        _want(field, t, self.shapes[field[-1]], self.io, self.device)
+    def _view(self, kind: str, field: str, t) -> None:
+        """Checks a tensor of rows (of single rows for a step) and notes its strides."""
+        shape = self.shapes[field[-1]]
+        if kind == "step":
+            shape = shape[:2] + shape[3:]
+        _want(field, t, shape, self.io, self.device)
         s = t.stride()
-        if s[3] != 1 and t.shape[3] != 1:
+        if s[-1] != 1 and t.shape[-1] != 1:
             raise ValueError(f"{field}: the last dimension is not contiguous")
-        if s[0] == s[1] == s[2] == 0 and t[..., 0].numel() > 1:
-            raise ValueError(f"{field}: one row repeated over batch, heads and tokens")
-        setattr(self.dd, field, Strides(s[0], s[1], s[2]))
+        if not any(s[:-1]) and t[..., 0].numel() > 1:
+            raise ValueError(f"{field}: one row repeated")
+        setattr(self._desc[kind], field, Strides(s[0], s[1], s[2] if kind != "step" else 0))
 
-    def _checked(self, log_decay, lengths, states) -> None:
+    def _vectors(self, log_decay, lengths, name="lengths") -> None:
         B, H = self.state_shape[:2]
         _want("log_decay", log_decay, (H,), torch.float32, self.device)
-        _want("lengths", lengths, (B,), torch.int32, self.device)
+        _want(name, lengths, (B,), torch.int32, self.device)
         _dense("log_decay", log_decay)
-        _dense("lengths", lengths)
+        _dense(name, lengths)
+
+    def _states(self, **states) -> None:
         for name, t in states.items():
             _want(name, t, self.state_shape, torch.float32, self.device)
             _dense(name, t)
 
     def forward(self, Q, K, V, log_decay, lengths=None, S0=None, want_state=False, O=None, S1=None, stream=None):
         """O, or (O, S1) with want_state."""
+        if not self._looked_at("forward", Q, K, V, log_decay, lengths, S0, O, S1):
+            for field, t in (("q", Q), ("k", K), ("v", V)):
+                self._view("forward", field, t)
+            self._vectors(log_decay, lengths)
+            self._states(S0=S0, S1=S1)
+            # a new output lies as V does, or Q
+            self._like = next((tuple(torch.empty_like(t).stride()) for t in (V, Q) if t.shape == self.shapes["o"]), None)
+            self._view("forward", "o", self._new_output(Q) if O is None else O)
+            self._accept()
         if O is None:
-            O = torch.empty_like(V if V.shape == self.shapes["o"] else Q if Q.shape == self.shapes["o"] else
-                                 Q.new_empty(self.shapes["o"]))
+            O = self._new_output(Q)
         if want_state and S1 is None:
             S1 = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
-        for field, t in (("q", Q), ("k", K), ("v", V), ("o", O)):
-            self._view(field, t)
-        self._checked(log_decay, lengths, {"S0": S0, "S1": S1})
-        luna_decay_fwd(self.dd, log_decay, Q, K, V, lengths, S0, O, S1, self.ws, stream)
+        _check(_lib.luna_decay_fwd(self._ref["forward"], log_decay.data_ptr(), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+                                   _addr(lengths), _addr(S0), O.data_ptr(), _addr(S1), *self._ws, _handle(stream)),
+               "luna_decay_fwd")
         return (O, S1) if want_state else O
+
+    def _new_output(self, Q):
+        shape = self.shapes["o"]
+        if self._like is None:
+            return torch.empty(shape, dtype=self.io, device=Q.device)
+        return torch.empty_strided(shape, self._like, dtype=self.io, device=Q.device)
 
     def backward(self, Q, K, V, dO, log_decay, lengths=None, S0=None, dS1=None, out=None, stream=None):
         """dQ, dK, dV, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
@@ -523,54 +590,61 @@ class Decay:
             out = {"dQ": torch.empty_like(Q), "dK": torch.empty_like(K), "dV": torch.empty_like(V)}
             if S0 is not None:
                 out["dS0"] = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
-        for field, t in (("q", Q), ("k", K), ("v", V), ("go", dO), ("gq", out["dQ"]), ("gk", out["dK"]),
-                         ("gv", out["dV"])):
-            self._view(field, t)
-        self._checked(log_decay, lengths, {"S0": S0, "dS1": dS1, "dS0": out.get("dS0")})
-        luna_decay_bwd(self.dd, log_decay, Q, K, V, dO, lengths, S0, dS1, out["dQ"], out["dK"], out["dV"],
-                       out.get("dS0"), self.ws, stream)
+        dQ, dK, dV, dS0 = out["dQ"], out["dK"], out["dV"], out.get("dS0")
+        if not self._looked_at("backward", Q, K, V, dO, log_decay, lengths, S0, dS1, dQ, dK, dV, dS0):
+            for field, t in (("q", Q), ("k", K), ("v", V), ("go", dO), ("gq", dQ), ("gk", dK), ("gv", dV)):
+                self._view("backward", field, t)
+            self._vectors(log_decay, lengths)
+            self._states(S0=S0, dS1=dS1, dS0=dS0)
+            self._accept()
+        _check(_lib.luna_decay_bwd(self._ref["backward"], log_decay.data_ptr(), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+                                   dO.data_ptr(), _addr(lengths), _addr(S0), _addr(dS1), dQ.data_ptr(), dK.data_ptr(),
+                                   dV.data_ptr(), _addr(dS0), *self._ws, _handle(stream)), "luna_decay_bwd")
         return out
 
     def step(self, q, k, v, log_decay, S, slots=None, o=None, stream=None):
         """One token: q (B, H, d), k (B, Hkv, d), v (B, Hkv, dv); S (nslots, H, d, dv) is advanced in place."""
-        B, H, d, dv = self.state_shape
         if o is None:
-            o = torch.empty((B, H, dv), dtype=self.io, device=q.device)
-        for field, t in (("q", q), ("k", k), ("v", v), ("o", o)):
-            sh = self.shapes[field]
-            _want(field, t, (sh[0], sh[1], sh[3]), self.io, self.device)
-            st = t.stride()
-            if st[2] != 1 and t.shape[2] != 1:
-                raise ValueError(f"{field}: the last dimension is not contiguous")
-            if st[0] == st[1] == 0 and t[..., 0].numel() > 1:
-                raise ValueError(f"{field}: one row repeated over batch and heads")
-            setattr(self.dd, field, Strides(st[0], st[1], 0))
-        _want("S", S, (S.shape[0], H, d, dv), torch.float32, self.device)
-        _want("slots", slots, (B,), torch.int32, self.device)
-        _want("log_decay", log_decay, (H,), torch.float32, self.device)
-        for name, t in (("S", S), ("slots", slots), ("log_decay", log_decay)):
-            _dense(name, t)
-        luna_decay_step(self.dd, log_decay, q, k, v, slots, S.shape[0], S, o, stream)
+            o = torch.empty(self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=q.device)
+        if not self._looked_at("step", q, k, v, log_decay, S, slots, o):
+            for field, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+                self._view("step", field, t)
+            _want("S", S, (S.shape[0],) + self.state_shape[1:], torch.float32, self.device)
+            _dense("S", S)
+            self._vectors(log_decay, slots, "slots")
+            self._accept()
+        _check(_lib.luna_decay_step(self._ref["step"], log_decay.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                    _addr(slots), S.shape[0], S.data_ptr(), o.data_ptr(), _handle(stream)),
+               "luna_decay_step")
         return o
 
 
-class BlockNorm:
+def _set_rows(desc, field: str, name: str, t, shape, dtype, device) -> None:
+    """Checks a matrix of contiguous rows and puts the distance of its rows into a descriptor."""
+    if t is None:
+        return
+    _want(name, t, shape, dtype, device)
+    if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: rows are not contiguous")
+    setattr(desc, field, t.stride(0) if t.shape[0] > 1 else 0)
+
+
+class BlockNorm(_Checked):
     """The norms after and before a block with its gate and residual scale, over (rows, cols) matrices
-    whose rows may be strided; weights are (cols,) fp32.  Owns the workspace of the backward pass."""
+    whose rows may be strided; weights are (cols,) fp32.  Owns the workspace of the backward pass, whose
+    calls belong on one stream at a time."""
 
     def __init__(self, rows, cols, groups=1, kind="rms", gate="none", res_scale=1.0, eps=1e-6, io=torch.bfloat16,
                  device="cuda", backward=False):
         self.nd = norm_desc(rows, cols, groups, kind, gate, res_scale, eps, _DTYPES[io])
+        super().__init__(self.nd)
         self.io, self.device, self.shape = io, torch.device(device), (rows, cols)
         self.ws = alloc_bytes(luna_norm_workspace_size(self.nd), self.device) if backward else None
+        self._ws = (self.ws.data_ptr(), self.ws.numel()) if backward else (None, 0)
 
-    def _rows(self, name: str, t) -> None:
-        if t is None:
-            return
-        _want(name, t, self.shape, self.io, self.device)
-        if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise ValueError(f"{name}: rows are not contiguous")
-        setattr(self.nd, "ld" + name, t.stride(0) if t.shape[0] > 1 else 0)
+    def _rows(self, kind: str, **matrices) -> None:
+        for name, t in matrices.items():
+            _set_rows(self._desc[kind], "ld" + name, name, t, self.shape, self.io, self.device)
 
     def _weights(self, **weights) -> None:
         for name, t in weights.items():
@@ -579,51 +653,56 @@ class BlockNorm:
 
     def forward(self, x, y, gate=None, w_post=None, w_pre=None, b_post=None, b_pre=None, X=None, H=None, stream=None):
         """{"X": x'} where there is a residual or no second norm (or X is given), {"H": h} with w_pre."""
-        like = x if x is not None else y
         if X is None and ((x is not None and y is not None) or w_pre is None):
-            X = torch.empty(self.shape, dtype=self.io, device=like.device)
+            X = torch.empty(self.shape, dtype=self.io, device=(y if x is None else x).device)
         if H is None and w_pre is not None:
-            H = torch.empty(self.shape, dtype=self.io, device=like.device)
-        for name, t in (("x", x), ("y", y), ("gate", gate), ("X", X), ("H", H)):
-            self._rows(name, t)
-        self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre)
-        luna_norm_fwd(self.nd, x, y, gate, w_post, b_post, w_pre, b_pre, X, H, stream)
-        return {k: t for k, t in (("X", X), ("H", H)) if t is not None}
+            H = torch.empty(self.shape, dtype=self.io, device=(y if x is None else x).device)
+        if not self._looked_at("forward", x, y, gate, w_post, w_pre, b_post, b_pre, X, H):
+            self._rows("forward", x=x, y=y, gate=gate, X=X, H=H)
+            self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre)
+            self._accept()
+        _check(_lib.luna_norm_fwd(self._ref["forward"], _addr(x), _addr(y), _addr(gate), _addr(w_post), _addr(b_post),
+                                  _addr(w_pre), _addr(b_pre), _addr(X), _addr(H), _handle(stream)), "luna_norm_fwd")
+        if X is None:
+            return {"H": H}
+        return {"X": X} if H is None else {"X": X, "H": H}
 
     def backward(self, x, y, gate, w_post, w_pre, dX, dH, b_post=None, b_pre=None, out=None, stream=None):
         """dx, dy, dgate, dw_post, dw_pre of what forward was given, and db_post, db_pre of given biases."""
         if out is None:
-            out = {k: torch.empty(self.shape, dtype=self.io, device=self.device)
+            out = {k: torch.empty(self.shape, dtype=self.io, device=t.device)
                    for k, t in (("dx", x), ("dy", y), ("dgate", gate)) if t is not None}
-            out.update({k: torch.empty(self.shape[1], dtype=torch.float32, device=self.device)
+            out.update({k: torch.empty_like(t)
                         for k, t in (("dw_post", w_post), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
                         if t is not None})
-        for name, t in (("x", x), ("y", y), ("gate", gate), ("dX", dX), ("dH", dH), ("dx", out.get("dx")),
-                        ("dy", out.get("dy")), ("dgate", out.get("dgate"))):
-            self._rows(name, t)
-        sums = {k: out.get(k) for k in ("dw_post", "db_post", "dw_pre", "db_pre")}
-        self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre, **sums)
-        luna_norm_bwd(self.nd, x, y, gate, w_post, b_post, w_pre, dX, dH, out.get("dx"), out.get("dy"),
-                      out.get("dgate"), sums["dw_post"], sums["db_post"], sums["dw_pre"], sums["db_pre"], self.ws, stream)
+        g = [out.get(k) for k in ("dx", "dy", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")]
+        if not self._looked_at("backward", x, y, gate, w_post, w_pre, dX, dH, b_post, b_pre, *g):
+            self._rows("backward", x=x, y=y, gate=gate, dX=dX, dH=dH, dx=g[0], dy=g[1], dgate=g[2])
+            self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre, dw_post=g[3], db_post=g[4],
+                          dw_pre=g[5], db_pre=g[6])
+            self._accept()
+        _check(_lib.luna_norm_bwd(self._ref["backward"], _addr(x), _addr(y), _addr(gate), _addr(w_post), _addr(b_post),
+                                  _addr(w_pre), _addr(dX), _addr(dH), *[_addr(t) for t in g], *self._ws,
+                                  _handle(stream)), "luna_norm_bwd")
         return out
 
 
-class Linear:
-    """Y = act(X W^T + bias) + R for X (m, k), W (n, k), rows strided or not; owns the workspace."""
+class Linear(_Checked):
+    """Y = act(X W^T + bias) + R for X (m, k), W (n, k), rows strided or not; owns the workspace, so its
+    calls belong on one stream at a time."""
 
     def __init__(self, m, n, k, act="none", io=torch.bfloat16, device="cuda", backward=False):
         self.ld = linear_desc(m, n, k, act, _DTYPES[io])
+        super().__init__(self.ld)
         self.io, self.device, self.m, self.n, self.k = io, torch.device(device), m, n, k
         self.ws = alloc_bytes(max(luna_linear_workspace_size(self.ld, b) for b in ((False, True) if backward else (False,))),
                               self.device)
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
 
-    def _rows(self, name: str, t, shape) -> None:
-        if t is None:
-            return
-        _want(name, t, shape, self.io, self.device)
-        if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise ValueError(f"{name}: rows are not contiguous")
-        setattr(self.ld, "ld" + name, t.stride(0) if t.shape[0] > 1 else 0)
+    def _rows(self, kind: str, **matrices) -> None:
+        shapes = {"x": (self.m, self.k), "dx": (self.m, self.k), "w": (self.n, self.k)}
+        for name, t in matrices.items():
+            _set_rows(self._desc[kind], "ld" + name, name, t, shapes.get(name, (self.m, self.n)), self.io, self.device)
 
     def _vector(self, name: str, t, shape) -> None:
         _want(name, t, shape, self.io, self.device)
@@ -631,30 +710,31 @@ class Linear:
 
     def forward(self, x, W, bias=None, r=None, save_z=False, Y=None, Z=None, stream=None):
         """Y, or (Y, z) with save_z."""
-        out = (self.m, self.n)
         if Y is None:
-            Y = torch.empty(out, dtype=self.io, device=x.device)
+            Y = torch.empty((self.m, self.n), dtype=self.io, device=x.device)
         if save_z and Z is None:
-            Z = torch.empty(out, dtype=self.io, device=x.device)
-        for name, t, shape in (("x", x, (self.m, self.k)), ("w", W, (self.n, self.k)), ("r", r, out), ("y", Y, out),
-                               ("z", Z, out)):
-            self._rows(name, t, shape)
-        self._vector("bias", bias, (self.n,))
-        luna_linear_fwd(self.ld, x, W, bias, r, Y, Z, self.ws, stream)
+            Z = torch.empty((self.m, self.n), dtype=self.io, device=x.device)
+        if not self._looked_at("forward", x, W, bias, r, Y, Z):
+            self._rows("forward", x=x, w=W, r=r, y=Y, z=Z)
+            self._vector("bias", bias, (self.n,))
+            self._accept()
+        _check(_lib.luna_linear_fwd(self._ref["forward"], x.data_ptr(), W.data_ptr(), _addr(bias), _addr(r), Y.data_ptr(),
+                                    _addr(Z), *self._ws, _handle(stream)), "luna_linear_fwd")
         return (Y, Z) if save_z else Y
 
     def backward(self, x, W, dY, Z=None, bias=False, out=None, stream=None):
         """dX, dW and with `bias` db; Z is forward's z (needed with an activation)."""
         if out is None:
-            new = dict(dtype=self.io, device=dY.device)
-            out = {"dX": torch.empty((self.m, self.k), **new), "dW": torch.empty((self.n, self.k), **new)}
+            out = {"dX": torch.empty((self.m, self.k), dtype=self.io, device=dY.device),
+                   "dW": torch.empty((self.n, self.k), dtype=self.io, device=dY.device)}
             if bias:
-                out["db"] = torch.empty(self.n, **new)
+                out["db"] = torch.empty(self.n, dtype=self.io, device=dY.device)
         dX, dW, db = out.get("dX"), out.get("dW"), out.get("db")
-        for name, t, shape in (("x", x, (self.m, self.k)), ("w", W, (self.n, self.k)), ("z", Z, (self.m, self.n)),
-                               ("dy", dY, (self.m, self.n)), ("dx", dX, (self.m, self.k))):
-            self._rows(name, t, shape)
-        self._vector("dW", dW, (self.n, self.k))
-        self._vector("db", db, (self.n,))
-        luna_linear_bwd(self.ld, x, W, Z, dY, dX, dW, db, self.ws, stream)
+        if not self._looked_at("backward", x, W, Z, dY, dX, dW, db):
+            self._rows("backward", x=x, w=W, z=Z, dy=dY, dx=dX)
+            self._vector("dW", dW, (self.n, self.k))
+            self._vector("db", db, (self.n,))
+            self._accept()
+        _check(_lib.luna_linear_bwd(self._ref["backward"], x.data_ptr(), W.data_ptr(), _addr(Z), dY.data_ptr(), _addr(dX),
+                                    _addr(dW), _addr(db), *self._ws, _handle(stream)), "luna_linear_bwd")
         return out
