@@ -372,6 +372,7 @@ cudaError_t launch_product_tc(const Product &p, cudaStream_t s) {
         return p.M <= 32 && !p.A.kt ? launch<1, 32>(a, s) : launch<1, 64>(a, s);
     }
     const int64_t sms = tc_sm_count();
+    if (cdiv(p.M, 256) * cdiv(p.N, 256) * 2 >= sms) return launch<2, 256>(a, s);
     if (cdiv(p.M, 128) * cdiv(p.N, 256) >= sms) return launch<1, 256>(a, s);
     return launch<1, 128>(a, s);
 }

@@ -28,11 +28,17 @@ namespace {
 
 constexpr int kMaxCols = 16384;
 
-// Threads of a row at most: with one or two vectors a thread, small blocks (several an SM) forward and
-// blocks of 128 registers a thread backward; beyond that, what kMaxCols columns need.
-template <int VEC, int NV>
-constexpr int max_threads(bool backward) {
-    return VEC == 1 ? 1024 : NV < 4 ? (backward ? 512 : 256) : kMaxCols / VEC / NV;
+// Launch shapes.  A thread takes NV vectors (16 bytes, or one value where rows are not aligned) of a row.
+// `threads`: the threads of a row at most; `resident`: the threads an SM holds, which sets a thread's
+// registers (65536 / resident) and the grid.
+struct Limits {
+    int threads, resident;
+};
+constexpr Limits limits(int vec, int nv, bool backward) {
+    if (vec == 1) return nv == 4 ? Limits{256, backward ? 512 : 1024} : nv == 8 ? Limits{512, 512} : Limits{1024, 1024};
+    if (nv == 1) return backward ? Limits{512, 512} : Limits{256, 1024};
+    if (nv == 2) return backward ? Limits{512, 512} : Limits{256, 512};
+    return Limits{kMaxCols / vec / nv, kMaxCols / vec / nv};
 }
 
 struct NormArgs {
@@ -112,12 +118,13 @@ struct RowTeam {
     }
 
     // Sum of (a, b) over the row, to every thread.
-    __device__ __forceinline__ float2 row_sum(float2 v) {
+    // `two`: b as well (the same for all threads).
+    __device__ __forceinline__ float2 row_sum(float2 v, bool two) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-            v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-        }
+        for (int o = 16; o > 0; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        if (two)
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
         if (warp_row) return v;
         float2 *r = reinterpret_cast<float2 *>(red) + 32 * buf;
         buf ^= 1;  // the buffer after next is free: every thread has passed the barrier in between
@@ -129,12 +136,12 @@ struct RowTeam {
     }
 
     // Sums over each group of the thread's vectors (v in, sums of the vector's group out).
-    __device__ __forceinline__ void group_sum(float2 (&v)[NV], const NormArgs &a, const int (&grp)[NV]) {
+    __device__ __forceinline__ void group_sum(float2 (&v)[NV], const NormArgs &a, const int (&grp)[NV], bool two) {
         if (a.gmode == 0) {
             float2 s = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < NV; ++i) { s.x += v[i].x; s.y += v[i].y; }
-            s = row_sum(s);
+            s = row_sum(s, two);
 #pragma unroll
             for (int i = 0; i < NV; ++i) v[i] = s;
         } else if (a.gmode == 1) {
@@ -142,7 +149,7 @@ struct RowTeam {
             for (int i = 0; i < NV; ++i)
                 for (int o = a.gvec >> 1; o > 0; o >>= 1) {
                     v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, o);
-                    v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, o);
+                    if (two) v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, o);
                 }
         } else {
             float2 *p = reinterpret_cast<float2 *>(gsm), *g = p + nvec;
@@ -192,12 +199,12 @@ __device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], R
     float2 s[NV];
     auto sum = [&]() {
         if (grouped) {
-            tm.group_sum(s, a, grp);
+            tm.group_sum(s, a, grp, false);
         } else {
             float2 q = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < NV; ++i) { q.x += s[i].x; q.y += s[i].y; }
-            q = tm.row_sum(q);
+            q = tm.row_sum(q, false);
 #pragma unroll
             for (int i = 0; i < NV; ++i) s[i] = q;
         }
@@ -275,7 +282,8 @@ __device__ __forceinline__ int my_vectors(const NormArgs &a, int nvec, int (&grp
 }
 
 template <typename IO, int VEC, int NV>
-__global__ void __launch_bounds__(max_threads<VEC, NV>(false)) k_norm_fwd(NormArgs a) {
+__global__ void __launch_bounds__(limits(VEC, NV, false).threads, limits(VEC, NV, false).resident / limits(VEC, NV, false).threads)
+    k_norm_fwd(NormArgs a) {
     extern __shared__ float sm[];
     const int nvec = a.cols / VEC;
     RowTeam<NV> tm = make_team<NV>(a, nvec, sm);
@@ -382,12 +390,12 @@ __device__ __forceinline__ void normalise_grad(float (&d)[NV][VEC], const float 
         }
     }
     if (grouped) {
-        tm.group_sum(s, a, grp);
+        tm.group_sum(s, a, grp, a.layer);
     } else {
         float2 q = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < NV; ++i) { q.x += s[i].x; q.y += s[i].y; }
-        q = tm.row_sum(q);
+        q = tm.row_sum(q, a.layer);
 #pragma unroll
         for (int i = 0; i < NV; ++i) s[i] = q;
     }
@@ -402,7 +410,8 @@ __device__ __forceinline__ void normalise_grad(float (&d)[NV][VEC], const float 
 
 // BIAS: the biases' gradients are summed too.
 template <typename IO, int VEC, int NV, bool BIAS>
-__global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArgs a) {
+__global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV, true).resident / limits(VEC, NV, true).threads)
+    k_norm_bwd(NormArgs a) {
     extern __shared__ float sm[];
     const int nvec = a.cols / VEC;
     RowTeam<NV> tm = make_team<NV>(a, nvec, sm);
@@ -418,7 +427,7 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArg
             if (BIAS) sb_post[i][e] = sb_pre[i][e] = 0.0f;
         }
     const int64_t slots = (int64_t)gridDim.x * blockDim.y, slot = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    constexpr bool AHEAD = VEC > 1 && NV <= 2;  // as in the forward pass
+    constexpr bool AHEAD = VEC > 1 && NV == 1;  // as in the forward pass, where the registers suffice
     RowPart<IO, VEC, NV> px, py, pg, pdX, pdH;
     auto fetch = [&](int64_t row) {
         py.fetch(a.y, row * a.ldy, t, T, active);
@@ -438,40 +447,41 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArg
         pdH.get(a.dH, dh, active);
         if (AHEAD && row + slots < a.rows) fetch(row + slots);
         if (a.y && a.w_post) normalise<VEC, NV>(z, ry, tm, a, true, grp, active);
-        // u of vector i (post-norm output, before the gate)
-        auto u_of = [&](int i, float (&u)[VEC]) {
+        // u (kept in place of y where there is no norm), and the gate's value and slope in place of the gate
+        float u[NV][VEC], act[NV][VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) u[e] = z[i][e];
-            if (a.w_post) {
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) u[i][e] = z[i][e];
+            if (a.w_post && i < active) {
                 const int c = (t + i * T) * VEC;
                 float w[VEC];
                 load_w<VEC>(a.w_post, c, w);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) u[e] *= w[e];
+                for (int e = 0; e < VEC; ++e) u[i][e] *= w[e];
                 if (a.b_post) {
                     load_w<VEC>(a.b_post, c, w);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) u[e] += w[e];
+                    for (int e = 0; e < VEC; ++e) u[i][e] += w[e];
                 }
             }
-        };
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                act[i][e] = 1.0f;
+                if (a.gate && i < active) {
+                    const float sg = sigmoidf(g[i][e]);
+                    act[i][e] = a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
+                    g[i][e] = a.act == LUNA_GATE_SILU ? fmaf(act[i][e], 1.0f - sg, sg) : sg * (1.0f - sg);
+                }
+            }
+        }
         if (a.w_pre) {
             if (a.y) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (i < active) {
-                        float u[VEC];
-                        u_of(i, u);
+                    if (i < active)
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            float v = u[e];
-                            if (a.gate) {
-                                const float sg = sigmoidf(g[i][e]);
-                                v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
-                            }
-                            x[i][e] = fmaf(a.alpha, v, x[i][e]);
-                        }
-                    }
+                        for (int e = 0; e < VEC; ++e) x[i][e] = fmaf(a.alpha * u[i][e], act[i][e], x[i][e]);
             }
             normalise<VEC, NV>(x, rx, tm, a, false, grp, active);
 #pragma unroll
@@ -499,15 +509,11 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(true)) k_norm_bwd(NormArg
             if (i < active) {
                 float dg[VEC];
                 if (a.gate) {
-                    float u[VEC];
-                    u_of(i, u);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const float sg = sigmoidf(g[i][e]), dt = a.alpha * d[i][e];
-                        const float act = a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
-                        const float slope = a.act == LUNA_GATE_SILU ? sg * (1.0f + g[i][e] * (1.0f - sg)) : sg * (1.0f - sg);
-                        dg[e] = dt * u[e] * slope;
-                        d[i][e] = dt * act;
+                        const float dt = a.alpha * d[i][e];
+                        dg[e] = dt * u[i][e] * g[i][e];
+                        d[i][e] = dt * act[i][e];
                     }
                     Vec<IO, VEC>::store(static_cast<IO *>(a.dgate) + row * a.lddgate + (int64_t)(t + i * T) * VEC, dg);
                 } else {
@@ -577,25 +583,27 @@ __global__ void __launch_bounds__(256) k_norm_sum(NormSum a) {
 // ---------------------------------------------------------------------------
 
 struct Shape {
-    int vec, nv, threads, rows_per_block;
+    int vec, nv, threads, rows_per_block, blocks;
     size_t smem;
 };
 
-// Vectors of a thread and threads of a row.  A row of at most 32 vectors is a warp's.
+// The fewest vectors a thread with which a row fits its threads.  A row of at most 32 vectors is a warp's.
 Shape shape_of(int cols, bool vectors, int vec_io, bool backward) {
     Shape s;
     s.vec = vectors ? vec_io : 1;
     const int nvec = cols / s.vec;
-    if (vectors) {
-        const int most = backward ? 512 : 256;
-        s.nv = nvec <= most ? 1 : nvec <= 2 * most ? 2 : 4;
-    } else {
-        s.nv = cols <= 4096 ? 4 : 16;
-    }
+    s.nv = vectors ? 1 : 4;
+    while (s.nv < (vectors ? 4 : 16) && nvec > s.nv * limits(s.vec, s.nv, backward).threads) s.nv *= 2;
     s.threads = ((nvec + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.rows_per_block = s.threads == 32 ? 8 : 1;
+    s.blocks = 152 * std::max(1, limits(s.vec, s.nv, backward).resident / (s.threads * s.rows_per_block));
     s.smem = sizeof(float) * 128;
     return s;
+}
+
+// Blocks that stay for all rows: no more than the device holds at once.
+int grid_of(int64_t rows, const Shape &sh) {
+    return (int)std::min<int64_t>(sh.blocks, (rows + sh.rows_per_block - 1) / sh.rows_per_block);
 }
 
 void group_mode(NormArgs &a, Shape &s) {
@@ -630,9 +638,7 @@ template <typename IO, int VEC, int NV>
 cudaError_t fwd_launch(const NormArgs &a, const Shape &sh, cudaStream_t s) {
     cudaError_t e = big_smem(k_norm_fwd<IO, VEC, NV>, sh.smem);
     if (e != cudaSuccess) return e;
-    // as many blocks as the device holds at once, 1024 threads an SM
-    const int64_t most = (int64_t)152 * std::max(1, 1024 / (sh.threads * sh.rows_per_block));
-    const unsigned grid = (unsigned)std::min<int64_t>(most, (a.rows + sh.rows_per_block - 1) / sh.rows_per_block);
+    const int grid = grid_of(a.rows, sh);
     LUNA_LAUNCH("norm_fwd", (k_norm_fwd<IO, VEC, NV>), grid, dim3(sh.threads, sh.rows_per_block), sh.smem, s, a);
     return cudaGetLastError();
 }
@@ -648,14 +654,8 @@ cudaError_t fwd(NormArgs a, cudaStream_t s) {
         return fwd_launch<IO, VECIO, 4>(a, sh, s);
     }
     if (sh.nv == 4) return fwd_launch<IO, 1, 4>(a, sh, s);
+    if (sh.nv == 8) return fwd_launch<IO, 1, 8>(a, sh, s);
     return fwd_launch<IO, 1, 16>(a, sh, s);
-}
-
-// Blocks of the backward pass: each sums its rows' weight gradients in registers, so no more than
-// fill the device (512 threads an SM).
-int bwd_grid(int64_t rows, const Shape &sh) {
-    const int64_t blocks = (int64_t)152 * std::max(1, 512 / (sh.threads * sh.rows_per_block));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(blocks, (rows + sh.rows_per_block - 1) / sh.rows_per_block));
 }
 
 template <typename IO, int VEC, int NV, bool BIAS>
@@ -671,7 +671,7 @@ cudaError_t bwd(NormArgs a, float *const (&out)[4], cudaStream_t s) {
     const bool v = vectors_ok(a, VECIO);
     Shape sh = shape_of(a.cols, v, VECIO, true);
     group_mode(a, sh);
-    const int grid = bwd_grid(a.rows, sh);
+    const int grid = grid_of(a.rows, sh);
     cudaError_t e;
     if (v) {
         if (sh.nv == 1) e = bwd_launch<IO, VECIO, 1, BIAS>(a, sh, grid, s);
@@ -679,6 +679,7 @@ cudaError_t bwd(NormArgs a, float *const (&out)[4], cudaStream_t s) {
         else e = bwd_launch<IO, VECIO, 4, BIAS>(a, sh, grid, s);
     } else {
         if (sh.nv == 4) e = bwd_launch<IO, 1, 4, BIAS>(a, sh, grid, s);
+        else if (sh.nv == 8) e = bwd_launch<IO, 1, 8, BIAS>(a, sh, grid, s);
         else e = bwd_launch<IO, 1, 16, BIAS>(a, sh, grid, s);
     }
     if (e != cudaSuccess || !a.part) return e;
@@ -732,7 +733,7 @@ size_t partial_bytes(const luna_norm_desc *nd) {
     size_t slots = 0;
     for (bool v : {false, true}) {
         const Shape sh = shape_of(nd->cols, v, nd->io == LUNA_F32 ? 4 : 8, true);
-        slots = std::max(slots, (size_t)bwd_grid(nd->rows, sh) * sh.rows_per_block);
+        slots = std::max(slots, (size_t)grid_of(nd->rows, sh) * sh.rows_per_block);
     }
     return slots * 4 * nd->cols * sizeof(float);
 }
