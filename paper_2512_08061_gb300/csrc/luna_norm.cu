@@ -89,6 +89,78 @@ template <typename IO> struct Vec<IO, 1> {
     static __device__ __forceinline__ void store(IO *p, const float (&v)[1]) { io_store(p, v[0]); }
 };
 
+// Element-wise work on VEC values, two an instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <int VEC> struct V {
+    // d = a b + c
+    static __device__ __forceinline__ void fma(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC], const float (&c)[VEC]) {
+        if (VEC == 1) { d[0] = fmaf(a[0], b[0], c[0]); return; }
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2) {
+            uint64_t r;
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])), "l"(pair(c[e], c[e + 1])));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
+        }
+    }
+    // d = a s + c
+    static __device__ __forceinline__ void fma(float (&d)[VEC], const float (&a)[VEC], float k, const float (&c)[VEC]) {
+        if (VEC == 1) { d[0] = fmaf(a[0], k, c[0]); return; }
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2) {
+            uint64_t r;
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(k, k)), "l"(pair(c[e], c[e + 1])));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
+        }
+    }
+    static __device__ __forceinline__ void mul(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC]) {
+        if (VEC == 1) { d[0] = a[0] * b[0]; return; }
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2) {
+            uint64_t r;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
+        }
+    }
+    static __device__ __forceinline__ void mul(float (&d)[VEC], const float (&a)[VEC], float k) {
+        if (VEC == 1) { d[0] = a[0] * k; return; }
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2) {
+            uint64_t r;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(k, k)));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
+        }
+    }
+    static __device__ __forceinline__ void add(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC]) {
+        if (VEC == 1) { d[0] = a[0] + b[0]; return; }
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2) {
+            uint64_t r;
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
+        }
+    }
+    static __device__ __forceinline__ float dot(const float (&a)[VEC], const float (&b)[VEC]) {
+        if (VEC == 1) return a[0] * b[0];
+        uint64_t r = pair(0.0f, 0.0f);
+#pragma unroll
+        for (int e = 0; e + 1 < VEC; e += 2)
+            asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
+        float x, y;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r));
+        return x + y;
+    }
+    static __device__ __forceinline__ float sum(const float (&a)[VEC]) {
+        float s = a[0];
+#pragma unroll
+        for (int e = 1; e < VEC; ++e) s += a[e];
+        return s;
+    }
+};
+
 template <int VEC>
 __device__ __forceinline__ void load_w(const float *p, int c, float (&v)[VEC]) {
     if (VEC == 1) {
@@ -130,9 +202,13 @@ struct RowTeam {
         buf ^= 1;  // the buffer after next is free: every thread has passed the barrier in between
         if ((t & 31) == 0) r[t >> 5] = v;
         __syncthreads();
-        float2 s = make_float2(0.f, 0.f);
-        for (int w = 0; w < threads / 32; ++w) { s.x += r[w].x; s.y += r[w].y; }
-        return s;
+        v = (t & 31) < threads / 32 ? r[t & 31] : make_float2(0.f, 0.f);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        if (two)
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+        return v;
     }
 
     // Sums over each group of the thread's vectors (v in, sums of the vector's group out).
@@ -147,10 +223,12 @@ struct RowTeam {
         } else if (a.gmode == 1) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                for (int o = a.gvec >> 1; o > 0; o >>= 1) {
-                    v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, o);
-                    if (two) v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, o);
-                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1)
+                    if (o < a.gvec) {
+                        v[i].x += __shfl_xor_sync(0xffffffffu, v[i].x, o);
+                        if (two) v[i].y += __shfl_xor_sync(0xffffffffu, v[i].y, o);
+                    }
         } else {
             float2 *p = reinterpret_cast<float2 *>(gsm), *g = p + nvec;
             sync();  // the last call's sums have been read
@@ -176,7 +254,14 @@ struct RowTeam {
     }
 };
 
-__device__ __forceinline__ float sigmoidf(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+// 1 / (1 + e^-g) by the hardware's exponential and reciprocal (2 ulp each), without their handling of
+// denormal results, which would be as many operations again: those values count as 0.
+__device__ __forceinline__ float sigmoidf(float g) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * g));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
 
 template <int NV>
 __device__ __forceinline__ RowTeam<NV> make_team(const NormArgs &a, int nvec, float *sm) {
@@ -211,11 +296,7 @@ __device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], R
     };
     if (a.layer) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            s[i] = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s[i].x += z[i][e];
-        }
+        for (int i = 0; i < NV; ++i) s[i] = make_float2(V<VEC>::sum(z[i]), 0.f);
         sum();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -224,23 +305,22 @@ __device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], R
                 for (int e = 0; e < VEC; ++e) z[i][e] -= s[i].x * inv;
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        s[i] = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) s[i].x = fmaf(z[i][e], z[i][e], s[i].x);
-    }
+    for (int i = 0; i < NV; ++i) s[i] = make_float2(V<VEC>::dot(z[i], z[i]), 0.f);
     sum();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         r[i] = rsqrtf(fmaf(s[i].x, inv, a.eps));
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) z[i][e] *= r[i];
+        V<VEC>::mul(z[i], z[i], r[i]);
     }
 }
 
-// A thread's part of one row of a matrix, as loaded; nothing of an absent matrix.
+// A thread's part of one row of a matrix, as loaded; zeros for an absent matrix and past the row's end.
 template <typename IO, int VEC, int NV> struct RowPart {
     typename Vec<IO, VEC>::Raw raw[NV];
+    __device__ __forceinline__ RowPart() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) memset(&raw[i], 0, sizeof(raw[i]));
+    }
     __device__ __forceinline__ void fetch(const void *p, int64_t off, int t, int threads, int active) {
         if (!p) return;
 #pragma unroll
@@ -249,17 +329,42 @@ template <typename IO, int VEC, int NV> struct RowPart {
                 raw[i] = *reinterpret_cast<const typename Vec<IO, VEC>::Raw *>(static_cast<const IO *>(p) + off +
                                                                               (int64_t)(t + i * threads) * VEC);
     }
-    __device__ __forceinline__ void get(const void *p, float (&v)[NV][VEC], int active) const {  // zeros where there is nothing
+    __device__ __forceinline__ void get(float (&v)[NV][VEC]) const {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (p && i < active) {
-                Vec<IO, VEC>::unpack(raw[i], v[i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) v[i][e] = 0.0f;
-            }
+        for (int i = 0; i < NV; ++i) Vec<IO, VEC>::unpack(raw[i], v[i]);
     }
 };
+
+// Gates of VEC values: v *= act(g), the choice once for all of them.
+template <int VEC> __device__ __forceinline__ void apply_gate(int act, const float (&g)[VEC], float (&v)[VEC]) {
+    if (act == LUNA_GATE_SILU) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] *= g[e] * sigmoidf(g[e]);
+    } else if (act == LUNA_GATE_SIGMOID) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] *= sigmoidf(g[e]);
+    }
+}
+// act(g) into `value` and its slope into g.
+template <int VEC> __device__ __forceinline__ void gate_and_slope(int act, float (&g)[VEC], float (&value)[VEC]) {
+    if (act == LUNA_GATE_SILU) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float sg = sigmoidf(g[e]);
+            value[e] = g[e] * sg;
+            g[e] = fmaf(value[e], 1.0f - sg, sg);
+        }
+    } else if (act == LUNA_GATE_SIGMOID) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            value[e] = sigmoidf(g[e]);
+            g[e] = value[e] * (1.0f - value[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) value[e] = 1.0f;
+    }
+}
 
 template <typename IO, int VEC, int NV>
 __device__ __forceinline__ void store_row(void *p, int64_t off, const float (&v)[NV][VEC], int t, int threads, int active) {
@@ -304,9 +409,9 @@ __global__ void __launch_bounds__(limits(VEC, NV, false).threads, limits(VEC, NV
     for (; row < a.rows; row += slots) {
         if (!AHEAD) fetch(row);
         float z[NV][VEC], x[NV][VEC], g[NV][VEC], r[NV];
-        px.get(a.x, x, active);
-        py.get(a.y, z, active);
-        pg.get(a.gate, g, active);
+        px.get(x);
+        py.get(z);
+        pg.get(g);
         if (AHEAD && row + slots < a.rows) fetch(row + slots);
         if (a.y) {
             if (a.w_post) {
@@ -317,26 +422,18 @@ __global__ void __launch_bounds__(limits(VEC, NV, false).threads, limits(VEC, NV
                         const int c = (tm.t + i * tm.threads) * VEC;
                         float w[VEC];
                         load_w<VEC>(a.w_post, c, w);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
+                        V<VEC>::mul(z[i], z[i], w);
                         if (a.b_post) {
                             load_w<VEC>(a.b_post, c, w);
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
+                            V<VEC>::add(z[i], z[i], w);
                         }
                     }
             }
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float v = z[i][e];
-                    if (a.gate && i < active) {
-                        const float sg = sigmoidf(g[i][e]);
-                        v *= a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
-                    }
-                    z[i][e] = a.x ? fmaf(a.alpha, v, x[i][e]) : a.alpha * v;
-                }
+            for (int i = 0; i < NV; ++i) {
+                apply_gate<VEC>(a.act, g[i], z[i]);
+                V<VEC>::fma(z[i], z[i], a.alpha, x[i]);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -352,12 +449,10 @@ __global__ void __launch_bounds__(limits(VEC, NV, false).threads, limits(VEC, NV
                     const int c = (tm.t + i * tm.threads) * VEC;
                     float w[VEC];
                     load_w<VEC>(a.w_pre, c, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) z[i][e] *= w[e];
+                    V<VEC>::mul(z[i], z[i], w);
                     if (a.b_pre) {
                         load_w<VEC>(a.b_pre, c, w);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) z[i][e] += w[e];
+                        V<VEC>::add(z[i], z[i], w);
                     }
                 }
             store_row<IO, VEC, NV>(a.H, row * a.ldH, z, tm.t, tm.threads, active);
@@ -382,12 +477,7 @@ __device__ __forceinline__ void normalise_grad(float (&d)[NV][VEC], const float 
     float2 s[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        s[i] = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            s[i].x = fmaf(d[i][e], zhat[i][e], s[i].x);
-            s[i].y += d[i][e];
-        }
+        s[i] = make_float2(V<VEC>::dot(d[i], zhat[i]), a.layer ? V<VEC>::sum(d[i]) : 0.0f);
     }
     if (grouped) {
         tm.group_sum(s, a, grp, a.layer);
@@ -402,9 +492,13 @@ __device__ __forceinline__ void normalise_grad(float (&d)[NV][VEC], const float 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const float mz = s[i].x * inv, md = a.layer ? s[i].y * inv : 0.0f;
-        if (i < active)
+        if (i < active) {
+            if (a.layer)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) d[i][e] = r[i] * (d[i][e] - md - zhat[i][e] * mz);
+                for (int e = 0; e < VEC; ++e) d[i][e] -= md;
+            V<VEC>::fma(d[i], zhat[i], -mz, d[i]);
+            V<VEC>::mul(d[i], d[i], r[i]);
+        }
     }
 }
 
@@ -440,11 +534,11 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
     for (int64_t row = slot; row < a.rows; row += slots) {
         if (!AHEAD) fetch(row);
         float z[NV][VEC], g[NV][VEC], x[NV][VEC], d[NV][VEC], dh[NV][VEC], ry[NV], rx[NV];
-        py.get(a.y, z, active);
-        pg.get(a.gate, g, active);
-        px.get(a.x, x, active);
-        pdX.get(a.dX, d, active);
-        pdH.get(a.dH, dh, active);
+        py.get(z);
+        pg.get(g);
+        px.get(x);
+        pdX.get(d);
+        pdH.get(dh);
         if (AHEAD && row + slots < a.rows) fetch(row + slots);
         if (a.y && a.w_post) normalise<VEC, NV>(z, ry, tm, a, true, grp, active);
         // u (kept in place of y where there is no norm), and the gate's value and slope in place of the gate
@@ -457,31 +551,23 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
                 const int c = (t + i * T) * VEC;
                 float w[VEC];
                 load_w<VEC>(a.w_post, c, w);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) u[i][e] *= w[e];
+                V<VEC>::mul(u[i], u[i], w);
                 if (a.b_post) {
                     load_w<VEC>(a.b_post, c, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) u[i][e] += w[e];
+                    V<VEC>::add(u[i], u[i], w);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                act[i][e] = 1.0f;
-                if (a.gate && i < active) {
-                    const float sg = sigmoidf(g[i][e]);
-                    act[i][e] = a.act == LUNA_GATE_SILU ? g[i][e] * sg : sg;
-                    g[i][e] = a.act == LUNA_GATE_SILU ? fmaf(act[i][e], 1.0f - sg, sg) : sg * (1.0f - sg);
-                }
-            }
+            gate_and_slope<VEC>(a.act, g[i], act[i]);
         }
         if (a.w_pre) {
             if (a.y) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (i < active)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) x[i][e] = fmaf(a.alpha * u[i][e], act[i][e], x[i][e]);
+                    if (i < active) {
+                        float v[VEC];
+                        V<VEC>::mul(v, u[i], act[i]);
+                        V<VEC>::fma(x[i], v, a.alpha, x[i]);
+                    }
             }
             normalise<VEC, NV>(x, rx, tm, a, false, grp, active);
 #pragma unroll
@@ -489,18 +575,13 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
                 if (i < active) {
                     float w[VEC];
                     load_w<VEC>(a.w_pre, (t + i * T) * VEC, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        sw_pre[i][e] = fmaf(dh[i][e], x[i][e], sw_pre[i][e]);
-                        if (BIAS) sb_pre[i][e] += dh[i][e];
-                        dh[i][e] *= w[e];
-                    }
+                    V<VEC>::fma(sw_pre[i], dh[i], x[i], sw_pre[i]);
+                    if (BIAS) V<VEC>::add(sb_pre[i], sb_pre[i], dh[i]);
+                    V<VEC>::mul(dh[i], dh[i], w);
                 }
             normalise_grad<VEC, NV>(dh, x, rx, tm, a, false, grp, active);
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) d[i][e] += dh[i][e];
+            for (int i = 0; i < NV; ++i) V<VEC>::add(d[i], d[i], dh[i]);
         }
         if (a.dx) store_row<IO, VEC, NV>(a.dx, row * a.lddx, d, t, T, active);
         if (!a.y) continue;
@@ -508,27 +589,19 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
         for (int i = 0; i < NV; ++i)
             if (i < active) {
                 float dg[VEC];
+                V<VEC>::mul(d[i], d[i], a.alpha);
                 if (a.gate) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float dt = a.alpha * d[i][e];
-                        dg[e] = dt * u[i][e] * g[i][e];
-                        d[i][e] = dt * act[i][e];
-                    }
+                    V<VEC>::mul(dg, d[i], u[i]);
+                    V<VEC>::mul(dg, dg, g[i]);
+                    V<VEC>::mul(d[i], d[i], act[i]);
                     Vec<IO, VEC>::store(static_cast<IO *>(a.dgate) + row * a.lddgate + (int64_t)(t + i * T) * VEC, dg);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) d[i][e] *= a.alpha;
                 }
                 if (a.w_post) {
                     float w[VEC];
                     load_w<VEC>(a.w_post, (t + i * T) * VEC, w);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        sw_post[i][e] = fmaf(d[i][e], z[i][e], sw_post[i][e]);
-                        if (BIAS) sb_post[i][e] += d[i][e];
-                        d[i][e] *= w[e];
-                    }
+                    V<VEC>::fma(sw_post[i], d[i], z[i], sw_post[i]);
+                    if (BIAS) V<VEC>::add(sb_post[i], sb_post[i], d[i]);
+                    V<VEC>::mul(d[i], d[i], w);
                 }
             }
         if (a.w_post) normalise_grad<VEC, NV>(d, z, ry, tm, a, true, grp, active);
