@@ -179,6 +179,7 @@ __device__ __forceinline__ void load_w(const float *p, int c, float (&v)[VEC]) {
 template <int NV>
 struct RowTeam {
     int t, threads;     // this thread's number in the row, threads of the row
+    int wpad;           // warps of the row, rounded up to a power of two
     bool warp_row;
     float *red;         // block rows: [2][32][2] sums of the warps
     float *gsm;         // group sums through shared memory: [vectors][2] then [groups][2]
@@ -202,12 +203,15 @@ struct RowTeam {
         buf ^= 1;  // the buffer after next is free: every thread has passed the barrier in between
         if ((t & 31) == 0) r[t >> 5] = v;
         __syncthreads();
-        v = (t & 31) < threads / 32 ? r[t & 31] : make_float2(0.f, 0.f);
+        // every group of `wpad` lanes holds the warps' sums
+        const int w = t & (wpad - 1);
+        v = w < threads / 32 ? r[w] : make_float2(0.f, 0.f);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        if (two)
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+        for (int o = 16; o > 0; o >>= 1)
+            if (o < wpad) {
+                v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+                if (two) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+            }
         return v;
     }
 
@@ -269,6 +273,7 @@ __device__ __forceinline__ RowTeam<NV> make_team(const NormArgs &a, int nvec, fl
     t.warp_row = blockDim.y > 1;
     t.t = threadIdx.x;
     t.threads = blockDim.x;
+    t.wpad = next_pow2(blockDim.x / 32);
     t.red = sm;
     t.nvec = nvec;
     t.gsm = sm + 128 + threadIdx.y * 2 * (nvec + a.groups);
@@ -569,7 +574,32 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
                         V<VEC>::fma(x[i], v, a.alpha, x[i]);
                     }
             }
-            normalise<VEC, NV>(x, rx, tm, a, false, grp, active);
+            // without a mean, norm's statistic and the sum that its gradient needs are one reduction over x':
+            // sum d xhat = r sum d x'
+            const bool fused = !a.layer && a.cols > 1;
+            float mz = 0.0f;
+            if (!fused) {
+                normalise<VEC, NV>(x, rx, tm, a, false, grp, active);
+            } else {
+                float2 q = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if (i < active) {
+                        float w[VEC];
+                        load_w<VEC>(a.w_pre, (t + i * T) * VEC, w);
+                        V<VEC>::mul(w, w, dh[i]);
+                        q.x += V<VEC>::dot(x[i], x[i]);
+                        q.y += V<VEC>::dot(x[i], w);
+                    }
+                q = tm.row_sum(q, true);
+                const float inv = 1.0f / (float)a.cols, r = rsqrtf(fmaf(q.x, inv, a.eps));
+                mz = q.y * r * inv;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    rx[i] = r;
+                    V<VEC>::mul(x[i], x[i], r);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < active) {
@@ -579,9 +609,17 @@ __global__ void __launch_bounds__(limits(VEC, NV, true).threads, limits(VEC, NV,
                     if (BIAS) V<VEC>::add(sb_pre[i], sb_pre[i], dh[i]);
                     V<VEC>::mul(dh[i], dh[i], w);
                 }
-            normalise_grad<VEC, NV>(dh, x, rx, tm, a, false, grp, active);
+            if (!fused) {
+                normalise_grad<VEC, NV>(dh, x, rx, tm, a, false, grp, active);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) V<VEC>::add(d[i], d[i], dh[i]);
+                for (int i = 0; i < NV; ++i) V<VEC>::add(d[i], d[i], dh[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    V<VEC>::fma(dh[i], x[i], -mz, dh[i]);
+                    V<VEC>::fma(d[i], dh[i], rx[i], d[i]);
+                }
+            }
         }
         if (a.dx) store_row<IO, VEC, NV>(a.dx, row * a.lddx, d, t, T, active);
         if (!a.y) continue;
