@@ -8,33 +8,57 @@
 namespace luna {
 namespace {
 
-constexpr int kCh = 32;        // rows of a chunk
-constexpr int kCols = 32;      // columns of c of a block
+constexpr int kCh = kDecaySimtRows;
 constexpr int kMixThreads = 256;
+constexpr int kCols = 32;      // state columns of a block of the single-token step
 
 template <typename T>
 __device__ __forceinline__ const T *row_base(const RowView &v, int b, int h, int H) {
     return static_cast<const T *>(v.p) + b * v.sb + (int64_t)(h / (H / v.heads)) * v.sh;
 }
 
-// One block: piece s of head (b, h), columns [32 * blockIdx.y, +32) of c.  The columns of the
-// state are independent, so blocks that share a head read a and b again but exchange nothing.
-// The state slice (da x 32) stays in shared memory; per chunk of 32 rows
+// Four consecutive values of a row, zeros past `width`.
+template <typename IO>
+__device__ __forceinline__ float4 load4(const IO *p, int c, int width, bool vec) {
+    if (vec && c + 4 <= width) {
+        if (sizeof(IO) == 4) return *reinterpret_cast<const float4 *>(p + c);
+        const uint2 w = *reinterpret_cast<const uint2 *>(p + c);
+        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                           __uint_as_float(w.y & 0xffff0000u));
+    }
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = c + i < width ? io_load(p + c + i) : 0.0f;
+    return make_float4(v[0], v[1], v[2], v[3]);
+}
+template <typename OUT>
+__device__ __forceinline__ void store4(OUT *p, int c, int width, bool vec, const float *v) {
+    if (vec && c + 4 <= width && sizeof(OUT) == 4) {
+        *reinterpret_cast<float4 *>(p + c) = make_float4(v[0], v[1], v[2], v[3]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c + i < width) io_store(p + c + i, v[i]);
+}
+
+// One block: piece s of head (b, h), chunks of 64 rows.  DA, DC: widths rounded up (64 or 128).
 //     P = (a b^T) masked and decayed,  out = p P c + x lambda^{m+e} a X,  X = lambda^{nv} X + u (b w)^T c
-// Bound by the shared-memory reads of the three small products (fp32 on CUDA cores).
-template <typename IO, typename OUT>
-__global__ void __launch_bounds__(kMixThreads) k_decay_mix(DecayMix a) {
-    extern __shared__ float sm[];
+// Every product runs from shared memory with a register tile a thread (4 x 4 scores, 4 rows x DC / 16
+// outputs, DA / 16 x DC / 16 of the state, which stays in registers and is copied to shared memory for
+// the outputs), 16-byte reads without bank conflicts, two multiply-adds an instruction.  Bound by the
+// fp32 FMA rate at width 128, by the loads' latency at small widths, where two blocks share an SM.
+template <typename IO, typename OUT, int DA, int DC>
+__global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_mix(DecayMix a) {
+    extern __shared__ float4 sm4[];
     clear_status(a);
-    const int da = a.da, lda = da + 1;
-    float *sa = sm, *sb = sa + kCh * lda, *sc = sb + kCh * lda, *sP = sc + kCh * (kCols + 1);
-    float *sX = sP + kCh * (kCh + 1), *pw = sX + da * kCols;
-    const int tid = threadIdx.x;
-    const int64_t item = blockIdx.x;
-    const int seg = (int)(item % a.nseg);
-    const int64_t bh = item / a.nseg;
+    constexpr int LA = DA + 4, LC = DC + 4, LP = kCh + 4, FT = DA / 64, CT = DC / 64;
+    float *sa = reinterpret_cast<float *>(sm4), *sb = sa + kCh * LA, *sc = sb + kCh * LA, *sP = sc + kCh * LC;
+    float *sX = sP + kCh * LP, *pw = sX + DA * LC;
+    const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+    const int seg = (int)(blockIdx.x % a.nseg);
+    const int64_t bh = blockIdx.x / a.nseg;
     const int b = (int)(bh / a.H), h = (int)(bh % a.H);
-    const int col0 = blockIdx.y * kCols;
     const int e = a.reverse ? 0 : 1;
     const float g = decay_log(a.log_decay, h);
     for (int i = tid; i <= kCh; i += kMixThreads) pw[i] = expf(g * (float)i);
@@ -43,87 +67,188 @@ __global__ void __launch_bounds__(kMixThreads) k_decay_mix(DecayMix a) {
     const int r1 = max(r0, min(len, rend));
     const IO *A = row_base<IO>(a.a, b, h, a.H), *Bm = row_base<IO>(a.b, b, h, a.H), *Cm = row_base<IO>(a.c, b, h, a.H);
     OUT *O = a.out ? static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh : nullptr;
+    // this thread's part of the state: rows 4 ty + 64 i + k, columns 4 tx + 64 j + l
+    uint64_t X[4 * FT][2 * CT];  // columns in pairs
     {
-        const float *X = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * da * a.dc : nullptr;
-        for (int i = tid; i < da * kCols; i += kMixThreads) {
-            const int f = i / kCols, c = col0 + i % kCols;
-            sX[i] = X && c < a.dc ? (a.x_trans ? X[(int64_t)c * da + f] : X[(int64_t)f * a.dc + c]) : 0.0f;
-        }
+        const float *x = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
+#pragma unroll
+        for (int i = 0; i < 4 * FT; ++i)
+#pragma unroll
+            for (int j = 0; j < 2 * CT; ++j) {
+                const int f = 4 * ty + 64 * (i / 4) + i % 4, c = 4 * tx + 64 * (j / 2) + 2 * (j % 2);
+                float v[2];
+#pragma unroll
+                for (int l = 0; l < 2; ++l)
+                    v[l] = x && f < a.da && c + l < a.dc
+                               ? (a.x_trans ? x[(int64_t)(c + l) * a.da + f] : x[(int64_t)f * a.dc + c + l]) : 0.0f;
+                X[i][j] = f2(v[0], v[1]);
+            }
     }
+    const int na = (a.da + 3) / 4, nc = (a.dc + 3) / 4;  // float4 pieces of a row
     const int nch = (r1 - r0 + kCh - 1) / kCh;
     for (int ci = 0; ci < nch; ++ci) {
         const int row0 = r0 + (a.reverse ? nch - 1 - ci : ci) * kCh;
         const int nv = min(kCh, r1 - row0);
         __syncthreads();
-        for (int i = tid; i < kCh * da; i += kMixThreads) {
-            const int r = i / da, f = i % da;
-            const bool on = r < nv;
-            if (O) sa[r * lda + f] = on ? io_load(A + (int64_t)(row0 + r) * a.a.st + f) : 0.0f;
-            sb[r * lda + f] = on ? io_load(Bm + (int64_t)(row0 + r) * a.b.st + f) : 0.0f;
+        // the pieces of b, c and (where outputs are wanted) a, eight loads of a thread in flight
+        const int nb = kCh * na, total = nb + kCh * nc + (O ? nb : 0);
+#pragma unroll 1
+        for (int i0 = tid; i0 < total; i0 += 8 * kMixThreads) {
+            float4 v[8];
+            float *to[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                int i = i0 + q * kMixThreads;
+                const bool is_b = i < nb, is_c = !is_b && i < nb + kCh * nc;
+                const int per = is_c ? nc : na;
+                to[q] = i < total ? (is_b ? sb : is_c ? sc : sa) : nullptr;
+                i -= is_b ? 0 : is_c ? nb : nb + kCh * nc;
+                const int r = i / per, c = 4 * (i % per);
+                const RowView &w = is_b ? a.b : is_c ? a.c : a.a;
+                const IO *p = is_b ? Bm : is_c ? Cm : A;
+                v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (to[q]) {
+                    to[q] += r * (is_c ? LC : LA) + c;
+                    if (r < nv) v[q] = load4<IO>(p + (int64_t)(row0 + r) * w.st, c, is_c ? a.dc : a.da, w.vec);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (to[q]) *reinterpret_cast<float4 *>(to[q]) = v[q];
         }
-        for (int i = tid; i < kCh * kCols; i += kMixThreads) {
-            const int r = i / kCols, c = i % kCols;
-            sc[r * (kCols + 1) + c] =
-                r < nv && col0 + c < a.dc ? io_load(Cm + (int64_t)(row0 + r) * a.c.st + col0 + c) : 0.0f;
+        if (O) {
+#pragma unroll
+            for (int i = 0; i < 4 * FT; ++i)
+#pragma unroll
+                for (int j = 0; j < CT; ++j)
+                    *reinterpret_cast<ulonglong2 *>(sX + (4 * ty + 64 * (i / 4) + i % 4) * LC + 4 * tx + 64 * j) =
+                        make_ulonglong2(X[i][2 * j], X[i][2 * j + 1]);
         }
         __syncthreads();
         if (O) {
-            const int r = tid / 8, j0 = tid % 8;
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int f = 0; f < da; ++f) {
-                const float av = sa[r * lda + f];
+            {  // scores of rows ty + 16 i, columns tx + 16 j
+                uint64_t acc[4][4];  // two partial sums each
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] = fmaf(av, sb[(j0 + 8 * t) * lda + f], acc[t]);
-            }
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int j = j0 + 8 * t, dist = a.reverse ? j - r : r - j;
-                sP[r * (kCh + 1) + j] = dist >= 0 ? a.p * acc[t] * pw[dist] : 0.0f;
+                    for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+#pragma unroll 2
+                for (int k = 0; k < na; ++k) {
+                    float4 u[4], v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        u[i] = *reinterpret_cast<const float4 *>(sa + (ty + 16 * i) * LA + 4 * k);
+                        v[i] = *reinterpret_cast<const float4 *>(sb + (tx + 16 * i) * LA + 4 * k);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            acc[i][j] = fma2(f2(u[i].x, u[i].y), f2(v[j].x, v[j].y), acc[i][j]);
+                            acc[i][j] = fma2(f2(u[i].z, u[i].w), f2(v[j].z, v[j].w), acc[i][j]);
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = ty + 16 * i, c = tx + 16 * j, dist = a.reverse ? c - r : r - c;
+                        float lo, hi;
+                        unpack2(acc[i][j], lo, hi);
+                        sP[r * LP + c] = dist >= 0 ? a.p * (lo + hi) * pw[dist] : 0.0f;
+                    }
             }
             __syncthreads();
-            float in[4] = {0.f, 0.f, 0.f, 0.f}, ex[4] = {0.f, 0.f, 0.f, 0.f};
-            const int c0 = (tid % 8) * 4;
-            for (int j = 0; j < nv; ++j) {
-                const float pv = sP[r * (kCh + 1) + j];
+            uint64_t out[4][2 * CT];  // rows ty + 16 i, columns 4 tx + 64 j + l in pairs
 #pragma unroll
-                for (int t = 0; t < 4; ++t) in[t] = fmaf(pv, sc[j * (kCols + 1) + c0 + t], in[t]);
-            }
-            for (int f = 0; f < da; ++f) {
-                const float av = sa[r * lda + f];
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) ex[t] = fmaf(av, sX[f * kCols + c0 + t], ex[t]);
-            }
-            if (r < nv) {
-                const float w = a.x * pw[(a.reverse ? nv - 1 - r : r) + e];
+                for (int j = 0; j < 2 * CT; ++j) out[i][j] = 0;
+            // out (+)= left (rows of lda) times right (rows of LC), over n pieces of four
+            auto product = [&](const float *left, int lda, const float *right, int n) {
+#pragma unroll 1
+                for (int k = 0; k < n; ++k) {
+                    float4 u[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (col0 + c0 + t < a.dc) io_store(O + (int64_t)(row0 + r) * a.ot + col0 + c0 + t, fmaf(w, ex[t], in[t]));
+                    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const float4 *>(left + (ty + 16 * i) * lda + 4 * k);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int j = 0; j < CT; ++j) {
+                            const float4 v = *reinterpret_cast<const float4 *>(right + (4 * k + q) * LC + 4 * tx + 64 * j);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float w = q == 0 ? u[i].x : q == 1 ? u[i].y : q == 2 ? u[i].z : u[i].w;
+                                out[i][2 * j] = fma2(f2(w, w), f2(v.x, v.y), out[i][2 * j]);
+                                out[i][2 * j + 1] = fma2(f2(w, w), f2(v.z, v.w), out[i][2 * j + 1]);
+                            }
+                        }
+                }
+            };
+            product(sa, LA, sX, na);  // (a's columns past da are zeros to a whole piece, and so are X's rows)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty + 16 * i;
+                const float w = a.x * pw[max(0, a.reverse ? nv - 1 - r : min(r, kCh - 1)) + e];
+#pragma unroll
+                for (int j = 0; j < 2 * CT; ++j) out[i][j] = mul2(out[i][j], f2(w, w));
             }
-            __syncthreads();
+            product(sP, LP, sc, kCh / 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty + 16 * i;
+                if (r < nv)
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        float v[4];
+                        unpack2(out[i][2 * j], v[0], v[1]);
+                        unpack2(out[i][2 * j + 1], v[2], v[3]);
+                        store4<OUT>(O + (int64_t)(row0 + r) * a.ot, 4 * tx + 64 * j, a.dc, a.ovec, v);
+                    }
+            }
         }
         const float dec = pw[nv];
-        const int c = tid % kCols;
-        for (int f = tid / kCols; f < da; f += kMixThreads / kCols) {
-            float acc = 0.0f;
-            for (int r = 0; r < nv; ++r) {
-                const int m = a.reverse ? nv - 1 - r : r;
-                acc = fmaf(pw[nv - m - e] * sb[r * lda + f], sc[r * (kCols + 1) + c], acc);
+#pragma unroll
+        for (int i = 0; i < 4 * FT; ++i)
+#pragma unroll
+            for (int j = 0; j < 2 * CT; ++j) X[i][j] = mul2(X[i][j], f2(dec, dec));
+#pragma unroll 2
+        for (int r = 0; r < nv; ++r) {
+            const float w = a.u * pw[nv - (a.reverse ? nv - 1 - r : r) - e];
+            float4 v[CT];
+#pragma unroll
+            for (int j = 0; j < CT; ++j) v[j] = *reinterpret_cast<const float4 *>(sc + r * LC + 4 * tx + 64 * j);
+#pragma unroll
+            for (int i = 0; i < FT; ++i) {
+                const float4 u = *reinterpret_cast<const float4 *>(sb + r * LA + 4 * ty + 64 * i);
+                const float uw[4] = {w * u.x, w * u.y, w * u.z, w * u.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) {
+                        X[4 * i + k][2 * j] = fma2(f2(uw[k], uw[k]), f2(v[j].x, v[j].y), X[4 * i + k][2 * j]);
+                        X[4 * i + k][2 * j + 1] = fma2(f2(uw[k], uw[k]), f2(v[j].z, v[j].w), X[4 * i + k][2 * j + 1]);
+                    }
             }
-            sX[f * kCols + c] = fmaf(dec, sX[f * kCols + c], a.u * acc);
         }
     }
-    __syncthreads();
-    if (O) {  // rows at and past the length
-        const int w = min(kCols, a.dc - col0);
-        for (int64_t i = tid; i < (int64_t)(rend - r1) * w; i += kMixThreads)
-            io_store(O + (r1 + i / w) * a.ot + col0 + i % w, 0.0f);
-    }
+    if (O)  // rows at and past the length
+        for (int i = tid; i < (rend - r1) * nc; i += kMixThreads) {  // (under 2^29: a row has at most 32 pieces)
+            const float z[4] = {0.f, 0.f, 0.f, 0.f};
+            store4<OUT>(O + (int64_t)(r1 + i / nc) * a.ot, 4 * (i % nc), a.dc, a.ovec, z);
+        }
     if (a.Xout) {
-        float *X = a.Xout + (bh * a.nseg + seg) * da * a.dc;
-        for (int i = tid; i < da * kCols; i += kMixThreads) {
-            const int f = i / kCols, cc = col0 + i % kCols;
-            if (cc < a.dc) X[(int64_t)f * a.dc + cc] = sX[i];
-        }
+        float *x = a.Xout + (bh * a.nseg + seg) * a.da * a.dc;
+#pragma unroll
+        for (int i = 0; i < 4 * FT; ++i)
+#pragma unroll
+            for (int j = 0; j < 2 * CT; ++j) {
+                const int f = 4 * ty + 64 * (i / 4) + i % 4, c = 4 * tx + 64 * (j / 2) + 2 * (j % 2);
+                float v[2];
+                unpack2(X[i][j], v[0], v[1]);
+                if (f < a.da && c < a.dc) x[(int64_t)f * a.dc + c] = v[0];
+                if (f < a.da && c + 1 < a.dc) x[(int64_t)f * a.dc + c + 1] = v[1];
+            }
     }
 }
 
@@ -257,14 +382,26 @@ __global__ void __launch_bounds__(kStepThreads) k_decay_step(DecayStep a) {
 
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-template <typename IO, typename OUT>
-cudaError_t mix(const DecayMix &a, cudaStream_t s) {
-    const size_t smem = sizeof(float) * (2 * kCh * (a.da + 1) + kCh * (kCols + 1) + kCh * (kCh + 1) + a.da * kCols + kCh + 1);
-    cudaError_t e = cudaFuncSetAttribute(k_decay_mix<IO, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+template <typename IO, typename OUT, int DA, int DC>
+cudaError_t mix_launch(const DecayMix &a, cudaStream_t s) {
+    const size_t smem = sizeof(float) * (2 * kCh * (DA + 4) + kCh * (DC + 4) + kCh * (kCh + 4) + DA * (DC + 4) + kCh + 4);
+    cudaError_t e = cudaFuncSetAttribute(k_decay_mix<IO, OUT, DA, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.nseg), cdiv(a.dc, kCols));
-    LUNA_LAUNCH("decay_mix", (k_decay_mix<IO, OUT>), grid, kMixThreads, smem, s, a);
+    const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nseg);
+    LUNA_LAUNCH("decay_mix", (k_decay_mix<IO, OUT, DA, DC>), grid, kMixThreads, smem, s, a);
     return cudaGetLastError();
+}
+
+template <typename IO, typename OUT>
+cudaError_t mix(DecayMix a, cudaStream_t s) {
+    // loads of four values: rows that start on their boundary
+    auto quad = [](const void *p, int64_t sb, int64_t sh, int64_t st, size_t size) {
+        return (reinterpret_cast<uintptr_t>(p) % (4 * size)) == 0 && sb % 4 == 0 && sh % 4 == 0 && st % 4 == 0;
+    };
+    for (RowView *v : {&a.a, &a.b, &a.c}) v->vec = quad(v->p, v->sb, v->sh, v->st, sizeof(IO));
+    a.ovec = quad(a.out, a.ob, a.oh, a.ot, sizeof(OUT));
+    if (a.da <= 64) return a.dc <= 64 ? mix_launch<IO, OUT, 64, 64>(a, s) : mix_launch<IO, OUT, 64, 128>(a, s);
+    return a.dc <= 64 ? mix_launch<IO, OUT, 128, 64>(a, s) : mix_launch<IO, OUT, 128, 128>(a, s);
 }
 
 }  // namespace

@@ -25,12 +25,14 @@ struct RowView {          // rows of a (B, heads, n, width) tensor; strides in e
     const void *p;
     int64_t sb, sh, st;
     int heads;            // heads of the tensor: query head h reads head h / (H / heads)
+    bool vec = false;     // (CUDA-core form) rows start on boundaries of four values
 };
 
 struct DecayMix {
     RowView a, b, c;
     void *out;            // NULL: only the carry is computed
     int64_t ob, oh, ot;   // strides of out (one head for each of the H)
+    bool ovec;            // as RowView::vec
     const float *log_decay;
     const int32_t *lengths;
     int B, H, n, da, dc;
@@ -72,11 +74,33 @@ __device__ __forceinline__ void clear_status(const DecayMix &a) {
     if (a.clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = 0;
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t f2(uint32_t lo, uint32_t hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t f2(float lo, float hi) { return f2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpack2(uint64_t v, float &lo, float &hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 // log lambda of a head, with -inf (lambda = 0) as a finite value so that 0 * log lambda is 0.
 __device__ __forceinline__ float decay_log(const float *log_decay, int h) {
     const float g = log_decay[h];
     return g < -1e30f ? -1e30f : g;
 }
+
+constexpr int kDecaySimtRows = 64;  // rows of a chunk of the CUDA-core form (128 on tensor cores)
 
 cudaError_t launch_decay_mix(const DecayMix &a, luna_dtype io, luna_dtype out, cudaStream_t s);
 bool decay_tc_ok(const DecayMix &a, luna_dtype io, luna_dtype out);  // shapes and alignments of the tensor-core form

@@ -60,18 +60,19 @@ struct Plan {
 // blocks) x (chunks of a block, and about one for its start) x (passes) is taken.
 Plan make_plan(const luna_decay_desc *dd) {
     Plan p;
-    const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), 128);
     const bool tc = dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0;
-    // blocks an SM holds: tensor-core form one (two up to width 64), else three, one for each 32 columns of a head
-    const double room = 152.0 * (tc ? (std::max(dd->d, dd->dv) <= 64 ? 2 : 1) : 3.0 / cdiv(std::max(dd->d, dd->dv), 32));
+    const int rows = tc ? 128 : kDecaySimtRows;
+    const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), rows);
+    // blocks an SM holds: one, or two of the CUDA-core form at small widths
+    const double room = 152.0 * (!tc && std::max(dd->d, dd->dv) <= 64 ? 2 : 1);
     int64_t best = 1;
     double least = 1e300;
-    for (int64_t ns = 1; ns <= std::min<int64_t>(64, std::max<int64_t>(1, chunks / 2)); ++ns) {
+    for (int64_t ns = 1; ns <= std::min<int64_t>(64, chunks); ++ns) {
         const double rounds = ceil((double)(BH * ns) / room);
         const double cost = rounds * (double)(cdiv(chunks, ns) + 1) * (ns > 1 ? 1.45 : 1.0);
         if (cost < least) { least = cost; best = ns; }
     }
-    p.seg_len = (int)(cdiv(chunks, best) * 128);
+    p.seg_len = (int)(cdiv(chunks, best) * rows);
     p.nseg = (int)cdiv(std::max(1, dd->n), p.seg_len);
     p.state = (size_t)align256((int64_t)BH * p.nseg * dd->d * dd->dv * 4);
     p.o_X = p.o_U + p.state;
@@ -90,8 +91,7 @@ RowView view(const void *p, const luna_strides &s, int heads) { return RowView{p
 
 // What all passes of a call share.
 DecayMix base(const luna_decay_desc *dd, const Plan &p, const float *log_decay, const int32_t *lengths, char *ws) {
-    DecayMix a;
-    memset(&a, 0, sizeof(a));
+    DecayMix a{};
     a.status = reinterpret_cast<int *>(ws);
     a.log_decay = log_decay;
     a.lengths = lengths;
