@@ -63,8 +63,7 @@ Plan make_plan(const luna_decay_desc *dd) {
     const bool tc = dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0;
     const int rows = tc ? 128 : kDecaySimtRows;
     const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), rows);
-    // blocks an SM holds: one, or two of the CUDA-core form at small widths
-    const double room = 152.0 * (!tc && std::max(dd->d, dd->dv) <= 64 ? 2 : 1);
+    const double room = 152.0 * (std::max(dd->d, dd->dv) <= 64 ? 2 : 1);  // blocks the SMs hold, in either form
     int64_t best = 1;
     double least = 1e300;
     for (int64_t ns = 1; ns <= std::min<int64_t>(64, chunks); ++ns) {

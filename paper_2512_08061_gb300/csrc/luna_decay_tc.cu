@@ -32,13 +32,18 @@ namespace {
 using namespace sm100;
 
 constexpr int kRows = 128;   // rows of a chunk
-constexpr int kSlots = 4;
 constexpr int kAhead = 2;
 
-constexpr int kScaleWarps = 8, kStateWarps = 8, kScoreWarps = 8;  // the three groups (multiples of four warps)
 
 template <int D, int NT, bool STATE> struct Cfg {
-    static constexpr int WARPS = kScaleWarps + kStateWarps + (STATE ? 0 : kScoreWarps);
+    // Warps of each of the three groups.  At D = 128 one block fills an SM; at D = 64 two share it, each with
+    // half the warps, so that one block's start, waits and end pass under the other's work.
+    static constexpr int GROUP = D / 16, SCALE = GROUP, STATEW = GROUP, SCORE = GROUP;
+    static constexpr int WARPS = SCALE + STATEW + (STATE ? 0 : SCORE), BLOCKS = D == 64 ? 2 : 1;
+    static constexpr int SLOTS = D == 64 ? 3 : 4;
+    // X between chunks: in TMEM, or where two blocks share that, in shared memory (rows of XS floats)
+    static constexpr bool XSMEM = D == 64;
+    static constexpr int XS = D + 4;
     static constexpr int THREADS = WARPS * 32 + 64;
     static constexpr int KB = D / 64;               // 64-column blocks of a row
     static constexpr uint32_t BLK = kRows * 128;    // one block of a tile
@@ -46,13 +51,14 @@ template <int D, int NT, bool STATE> struct Cfg {
     static constexpr uint32_t XBLK = D * 128, XOP = KB * XBLK;  // X operand: [64-column block][feature][64]
     // the terms of b, half a chunk at a time: b1 takes b's own place where there is no room beside it, and
     // then waits for P to have read b
-    static constexpr bool INPLACE = D == 128 && NT == 3;
+    static constexpr bool INPLACE = NT == 3;
     static constexpr int TERMS = INPLACE ? NT - 1 : NT;
-    static constexpr uint32_t SMEM = kSlots * TILE + TERMS * TILE + (STATE ? 0 : XOP) + 2048 + 1024;
-    static_assert(SMEM <= 227 * 1024, "shared memory");
-    // TMEM columns: U | X | E | P (the bf16 form of each 64 columns in their first 32)
-    static constexpr uint32_t cU = 0, cX = D, cE = 2 * D, cP = 3 * D;
-    static constexpr uint32_t COLS = STATE ? 2 * D : 512;
+    static constexpr uint32_t XBYTES = XSMEM ? D * XS * 4 : 0;
+    static constexpr uint32_t SMEM = SLOTS * TILE + TERMS * TILE + (STATE ? 0 : XOP) + XBYTES + 2048 + 1024;
+    static_assert((SMEM + 1024) * BLOCKS <= 228 * 1024, "shared memory");
+    // TMEM columns: U | E | P (the bf16 form of each 64 columns in their first 32) | X
+    static constexpr uint32_t cU = 0, cE = D, cP = 2 * D, cX = STATE ? D : 2 * D + 128;
+    static constexpr uint32_t COLS = XSMEM ? (STATE ? 64 : 256) : STATE ? 2 * D : 512;
 };
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -133,18 +139,20 @@ __device__ __forceinline__ void decay_scores(uint32_t taddr, int i, int jb, bool
 }
 
 template <int D, int NT, bool STATE, typename OUT>
-__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
+__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>::BLOCKS)
     k_decay_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapO,
                const __grid_constant__ DecayMix a) {
     using C = Cfg<D, NT, STATE>;
     constexpr bool STAGED = !STATE && sizeof(OUT) == 2;  // bf16 outputs leave by TMA from the chunk's c slot
+    constexpr int kSlots = C::SLOTS, kScaleWarps = C::SCALE, kStateWarps = C::STATEW, kScoreWarps = C::SCORE;
     extern __shared__ uint8_t smem_raw[];
     clear_status(a);
     uint8_t *sm = align_1024(smem_raw);
     uint8_t *terms = sm + kSlots * C::TILE;
     uint8_t *Xop = terms + C::TERMS * C::TILE;
-    float *pw = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));  // lambda^0 .. lambda^128
+    float *Xs = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));
+    float *pw = Xs + C::XBYTES / 4;  // lambda^0 .. lambda^128
     float *diag = pw + 132;
     uint64_t *bars = reinterpret_cast<uint64_t *>(diag + 4 * kDiagCopy);
     uint64_t *full = bars, *freeb = bars + kSlots, *pready = bars + 2 * kSlots;
@@ -154,7 +162,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     uint32_t *tslot = reinterpret_cast<uint32_t *>(pready + 12);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     constexpr int kTma = C::WARPS, kMma = kTma + 1;
-    constexpr int kStateWarp0 = kScaleWarps, kScoreWarp0 = kScaleWarps + kStateWarps;
+    constexpr int kScoreWarp0 = kScaleWarps + kStateWarps;
 
     const int seg = blockIdx.x % a.nseg;
     const int64_t bh = blockIdx.x / a.nseg;
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         mbar_init(pready, 1); mbar_init(eready, 1); mbar_init(oready, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(scaled + i, kScaleWarps); mbar_init(uread + i, 1); }
         mbar_init(xready, kStateWarps); mbar_init(ufree, kStateWarps);
-        mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps * D / 128);
+        mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps);
         fence_mbar_init();
     }
     if (warp == kMma) { tmem_alloc(tslot, C::COLS); tmem_relinquish(); }
@@ -187,7 +195,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     const uint32_t tb = *tslot;
     bool failed = false;
     auto wait = [&](uint64_t *bar, uint32_t parity) {  // bounded; a no-op once it has run out
-        if (!failed && !mbar_wait(bar, parity)) {
+        if (!failed && !mbar_wait_long(bar, parity)) {
             failed = true;
             atomicOr(a.status, 1);
         }
@@ -364,9 +372,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             }
         }
     } else if (warp < kScoreWarp0) {
-        // state: thread (feature f, half of the columns); an accumulator's row f is lane f, or with 64 rows lane
+        constexpr int SC = D / (kStateWarps / 4);
+        // state: thread (feature f, SC of the columns); an accumulator's row f is lane f, or with 64 rows lane
         // 32 (f / 16) + f % 16
-        const int quarter = warp & 3, cc0 = ((warp - kScaleWarps) >> 2) * (D / 2);
+        const int quarter = warp & 3, cc0 = ((warp - kScaleWarps) >> 2) * SC;
         const bool own = D == 128 || lane < 16;
         const int f = D == 128 ? quarter * 32 + lane : quarter * 16 + (lane & 15);
         const uint32_t lb = (uint32_t)(quarter * 32) << 16;
@@ -379,9 +388,29 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                                    pack2(x[k + 6], x[k + 7]));
             }
         };
+        auto put_state = [&](int cc, const uint32_t (&x)[16]) {  // columns cc .. of X
+            if (!C::XSMEM) {
+                tmem_st16(tb + lb + C::cX + cc, x);
+            } else if (own) {
+#pragma unroll
+                for (int k = 0; k < 16; k += 4)
+                    *reinterpret_cast<uint4 *>(Xs + f * C::XS + cc + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+            }
+        };
+        auto get_state = [&](int cc, uint32_t (&x)[16]) {  // (a TMEM load still to be waited for)
+            if (!C::XSMEM) {
+                tmem_ld16(tb + lb + C::cX + cc, x);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; k += 4) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(Xs + f * C::XS + cc + k);
+                    x[k] = v.x; x[k + 1] = v.y; x[k + 2] = v.z; x[k + 3] = v.w;
+                }
+            }
+        };
         const float *X0 = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
 #pragma unroll 1
-        for (int cc = cc0; cc < cc0 + D / 2; cc += 16) {
+        for (int cc = cc0; cc < cc0 + SC; cc += 16) {
             float x[16];
             uint32_t y[16];
 #pragma unroll
@@ -390,7 +419,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                            ? (a.x_trans ? X0[(int64_t)(cc + k) * a.da + f] : X0[(int64_t)f * a.dc + cc + k]) : 0.0f;
                 y[k] = __float_as_uint(x[k]);
             }
-            tmem_st16(tb + lb + C::cX + cc, y);
+            put_state(cc, y);
             if (!STATE) put_operand(cc, x);
         }
         tmem_wait_st();
@@ -407,11 +436,11 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             const float dec = pw[nv];
             const uint64_t dec2 = f2(dec, dec);
 #pragma unroll
-            for (int c1 = 0; c1 < D / 2; c1 += 16) {
+            for (int c1 = 0; c1 < SC; c1 += 16) {
                 const int cc = cc0 + c1;
                 uint32_t xu[16], xx[16];
                 tmem_ld16(tb + lb + C::cU + cc, xu);
-                tmem_ld16(tb + lb + C::cX + cc, xx);
+                get_state(cc, xx);
                 tmem_wait_ld();
                 float x[16];
 #pragma unroll
@@ -420,7 +449,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                     xx[k] = __float_as_uint(x[k]);
                     xx[k + 1] = __float_as_uint(x[k + 1]);
                 }
-                tmem_st16(tb + lb + C::cX + cc, xx);
+                put_state(cc, xx);
                 if (!STATE && c + 1 < nch) put_operand(cc, x);
             }
             tmem_wait_st();
@@ -435,9 +464,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         if (a.Xout) {
             float *X = a.Xout + (bh * a.nseg + seg) * a.da * a.dc + (int64_t)f * a.dc;
 #pragma unroll 1
-            for (int cc = cc0; cc < cc0 + D / 2; cc += 16) {
+            for (int cc = cc0; cc < cc0 + SC; cc += 16) {
                 uint32_t x[16];
-                tmem_ld16(tb + lb + C::cX + cc, x);
+                get_state(cc, x);
                 tmem_wait_ld();
                 if (own && f < a.da) {
 #pragma unroll
@@ -448,12 +477,12 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             }
         }
     } else if (!STATE) {
-        // scores and outputs: thread (row, column half); the two warps of a quarter share its rows
-        constexpr int PC = kRows / 2, EC = D / 2;
+        // scores and outputs: thread (row, 1 / PARTS of the columns); PARTS warps share a quarter's rows
+        constexpr int PARTS = kScoreWarps / 4, PC = kRows / PARTS, EC = D / PARTS;
         const int gw = warp - kScoreWarp0, quarter = warp & 3, part = gw >> 2, i = quarter * 32 + lane;
         const uint32_t lb = (uint32_t)(quarter * 32) << 16;
         OUT *O = static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh;
-        const bool stores = lane == 0 && (D == 128 || part == 0);
+        const bool stores = lane == 0;
         auto give_slot = [&]() {  // the last chunk's outputs have left their slot
             if (stores) {
                 bulk_wait_read();
@@ -464,15 +493,17 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         for (int c = 0; c < nch; ++c) {
             const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
             const uint32_t ph = c & 1;
+            if (STAGED && kSlots == 3 && c > 0) give_slot();
             wait(pready, ph);
             tc_fence_after();
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {  // the bf16 scores take the place of columns that this warp has read
+            for (int q = 0; q < PC / 32; ++q) {  // the bf16 scores take the place of columns that this warp has read
+                const int blk = part * (PC / 32) + q;
                 uint32_t w[16];
-                decay_scores(tb + lb + C::cP + part * PC + 32 * q, i, part * 2 + q, a.reverse != 0, nv, a.p, pw, diag, w);
-                tmem_st16(tb + lb + C::cP + part * PC + 16 * q, w);
+                decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, w);
+                tmem_st16(tb + lb + C::cP + 64 * (blk / 2) + 16 * (blk % 2), w);
             }
-            if (STAGED && c > 0) give_slot();
+            if (STAGED && kSlots == 4 && c > 0) give_slot();
             wait(eready, ph);
             tc_fence_after();
             const int m = a.reverse ? nv - 1 - i : i;
@@ -534,12 +565,12 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                 }
                 __syncwarp();
             }
-            if (STAGED) {  // 32 rows of a 64-column block at a time: a warp's own, or with D = 64 its pair's
+            if (STAGED) {  // a warp's 32 rows of a 64-column block
+                static_assert(EC == 64, "one block of columns a warp");
                 fence_proxy_async_smem();
-                if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
-                else __syncwarp();
+                __syncwarp();
                 if (stores) {
-                    const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
+                    const int blk = part, row = row0 + quarter * 32;
                     if (row < a.n && 64 * blk < a.dc)
                         tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, h, b);
                     bulk_commit();
