@@ -56,19 +56,19 @@ struct Plan {
 };
 
 // Pieces of the rows.  More pieces fill more SMs, but with more than one the states before each have to
-// be summed first, a pass over two of the four tensors; the piece count with the least of (rounds of
-// blocks) x (chunks of a block, and about one for its start) x (passes) is taken.
+// be summed first, a pass over two of the four tensors; the piece count with the least of (pieces of a
+// block) x (chunks of a piece, and about half of one to start it) x (passes) is taken.
 Plan make_plan(const luna_decay_desc *dd) {
     Plan p;
     const bool tc = dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0;
     const int rows = tc ? 128 : kDecaySimtRows;
     const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), rows);
-    const double room = 152.0 * (std::max(dd->d, dd->dv) <= 64 ? 2 : 1);  // blocks the SMs hold, in either form
+    const double room = 152.0 * (!tc && std::max(dd->d, dd->dv) <= 64 ? 2 : 1);  // blocks the SMs hold
     int64_t best = 1;
     double least = 1e300;
     for (int64_t ns = 1; ns <= std::min<int64_t>(64, chunks); ++ns) {
         const double rounds = ceil((double)(BH * ns) / room);
-        const double cost = rounds * (double)(cdiv(chunks, ns) + 1) * (ns > 1 ? 1.45 : 1.0);
+        const double cost = (rounds * ((double)cdiv(chunks, ns) + 0.5) + 1) * (ns > 1 ? 1.45 : 1.0);
         if (cost < least) { least = cost; best = ns; }
     }
     p.seg_len = (int)(cdiv(chunks, best) * rows);

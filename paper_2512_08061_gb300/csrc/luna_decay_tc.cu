@@ -1,6 +1,6 @@
 // Linear attention with a decay for each head on tensor cores (bf16, tcgen05 / TMEM / TMA).
 //
-// A block walks one piece of a head's rows in chunks of 128 (a, b, c as in luna_decay.cuh) and keeps the
+// A block walks pieces of heads' rows, one after another, in chunks of 128 (a, b, c as in luna_decay.cuh) and keeps the
 // state X (da x dc, fp32) in TMEM.  Per chunk of nv rows, m a row's number in processing order:
 //     MMA    P = a b^T,  E = a X                       (X as a bf16 operand)
 //     warps  P masked and decayed, as bf16 back into TMEM;  E scaled by x lambda^{m+e} in place
@@ -25,6 +25,7 @@
 
 namespace luna {
 
+int tc_sm_count();
 bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
                     const uint32_t *box);
 
@@ -36,14 +37,13 @@ constexpr int kAhead = 2;
 
 
 template <int D, int NT, bool STATE> struct Cfg {
-    // Warps of each of the three groups.  At D = 128 one block fills an SM; at D = 64 two share it, each with
-    // half the warps, so that one block's start, waits and end pass under the other's work.
-    static constexpr int GROUP = D / 16, SCALE = GROUP, STATEW = GROUP, SCORE = GROUP;
-    static constexpr int WARPS = SCALE + STATEW + (STATE ? 0 : SCORE), BLOCKS = D == 64 ? 2 : 1;
-    static constexpr int SLOTS = D == 64 ? 3 : 4;
-    // X between chunks: in TMEM, or where two blocks share that, in shared memory (rows of XS floats)
-    static constexpr bool XSMEM = D == 64;
-    static constexpr int XS = D + 4;
+    static constexpr int SCALE = 8, STATEW = 8, SCORE = 8;  // warps of each of the three groups
+    static constexpr int WARPS = SCALE + STATEW + (STATE ? 0 : SCORE);
+    // At D = 64 there is room for two chunks and more, and a block stays for many (short) pieces, whose
+    // starts and ends then pass under each other's work; at D = 128 that costs registers that the score
+    // warps do not have (5 % at 152 long pieces).
+    static constexpr int SLOTS = D == 64 ? 8 : 4;
+    static constexpr bool STAYS = D == 64;
     static constexpr int THREADS = WARPS * 32 + 64;
     static constexpr int KB = D / 64;               // 64-column blocks of a row
     static constexpr uint32_t BLK = kRows * 128;    // one block of a tile
@@ -51,14 +51,13 @@ template <int D, int NT, bool STATE> struct Cfg {
     static constexpr uint32_t XBLK = D * 128, XOP = KB * XBLK;  // X operand: [64-column block][feature][64]
     // the terms of b, half a chunk at a time: b1 takes b's own place where there is no room beside it, and
     // then waits for P to have read b
-    static constexpr bool INPLACE = NT == 3;
+    static constexpr bool INPLACE = D == 128 && NT == 3;
     static constexpr int TERMS = INPLACE ? NT - 1 : NT;
-    static constexpr uint32_t XBYTES = XSMEM ? D * XS * 4 : 0;
-    static constexpr uint32_t SMEM = SLOTS * TILE + TERMS * TILE + (STATE ? 0 : XOP) + XBYTES + 2048 + 1024;
-    static_assert((SMEM + 1024) * BLOCKS <= 228 * 1024, "shared memory");
+    static constexpr uint32_t SMEM = SLOTS * TILE + TERMS * TILE + (STATE ? 0 : XOP) + 2048 + 1024;
+    static_assert(SMEM <= 227 * 1024, "shared memory");
     // TMEM columns: U | E | P (the bf16 form of each 64 columns in their first 32) | X
     static constexpr uint32_t cU = 0, cE = D, cP = 2 * D, cX = STATE ? D : 2 * D + 128;
-    static constexpr uint32_t COLS = XSMEM ? (STATE ? 64 : 256) : STATE ? 2 * D : 512;
+    static constexpr uint32_t COLS = STATE ? 2 * D : 512;
 };
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -138,8 +137,30 @@ __device__ __forceinline__ void decay_scores(uint32_t taddr, int i, int jb, bool
     }
 }
 
+// One piece of a head's rows.
+struct Piece {
+    int seg, b, h, r0, rend, r1, nch, reverse;  // rows r0 .. rend, those below r1 valid, nch chunks of them
+    int64_t bh;
+    float g;
+    __device__ __forceinline__ Piece(const DecayMix &a, int item) {
+        seg = item % a.nseg;
+        bh = item / a.nseg;
+        b = (int)(bh / a.H);
+        h = (int)(bh % a.H);
+        r0 = seg * a.seg_len;
+        rend = min(a.n, r0 + a.seg_len);
+        r1 = max(r0, min(head_length(a.lengths, b, a.n), rend));
+        nch = (r1 - r0 + kRows - 1) / kRows;
+        reverse = a.reverse;
+        g = decay_log(a.log_decay, h);
+    }
+    __device__ __forceinline__ int row(int c) const { return r0 + (reverse ? nch - 1 - c : c) * kRows; }
+    __device__ __forceinline__ int valid(int c) const { return min(kRows, r1 - row(c)); }
+    __device__ __forceinline__ float power(int k) const { return expf(g * (float)k); }
+};
+
 template <int D, int NT, bool STATE, typename OUT>
-__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>::BLOCKS)
+__global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     k_decay_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const __grid_constant__ CUtensorMap mapC, const __grid_constant__ CUtensorMap mapO,
                const __grid_constant__ DecayMix a) {
@@ -151,8 +172,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
     uint8_t *sm = align_1024(smem_raw);
     uint8_t *terms = sm + kSlots * C::TILE;
     uint8_t *Xop = terms + C::TERMS * C::TILE;
-    float *Xs = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));
-    float *pw = Xs + C::XBYTES / 4;  // lambda^0 .. lambda^128
+    float *pw = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));  // lambda^0 .. lambda^128 of the scores' warps' piece
     float *diag = pw + 132;
     uint64_t *bars = reinterpret_cast<uint64_t *>(diag + 4 * kDiagCopy);
     uint64_t *full = bars, *freeb = bars + kSlots, *pready = bars + 2 * kSlots;
@@ -164,31 +184,17 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
     constexpr int kTma = C::WARPS, kMma = kTma + 1;
     constexpr int kScoreWarp0 = kScaleWarps + kStateWarps;
 
-    const int seg = blockIdx.x % a.nseg;
-    const int64_t bh = blockIdx.x / a.nseg;
-    const int b = (int)(bh / a.H), h = (int)(bh % a.H);
-    const int len = head_length(a.lengths, b, a.n);
-    const int r0 = seg * a.seg_len, rend = min(a.n, r0 + a.seg_len), r1 = max(r0, min(len, rend));
-    const int nch = (r1 - r0 + kRows - 1) / kRows;
-    const int e = a.reverse ? 0 : 1;
-    const float g = decay_log(a.log_decay, h);
-    auto chunk_row = [&](int c) { return r0 + (a.reverse ? nch - 1 - c : c) * kRows; };
+    const int items = a.B * a.H * a.nseg, e = a.reverse ? 0 : 1;
 
     if (tid == 0) {
         for (int i = 0; i < kSlots; ++i) { mbar_init(full + i, 1); mbar_init(freeb + i, 1); }
         mbar_init(pready, 1); mbar_init(eready, 1); mbar_init(oready, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(scaled + i, kScaleWarps); mbar_init(uread + i, 1); }
         mbar_init(xready, kStateWarps); mbar_init(ufree, kStateWarps);
-        mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps);
+        mbar_init(masked, kScoreWarps); mbar_init(efree, kScoreWarps); mbar_init(stored, kScoreWarps * D / 128);
         fence_mbar_init();
     }
     if (warp == kMma) { tmem_alloc(tslot, C::COLS); tmem_relinquish(); }
-    for (int i = tid; i <= kRows; i += C::THREADS) pw[i] = expf(g * (float)i);
-    if (!STATE)
-        for (int i = tid; i < 4 * kDiagCopy; i += C::THREADS) {
-            const int dist = (i % kDiagCopy + i / kDiagCopy - 31) * (a.reverse ? 1 : -1);
-            diag[i] = dist >= 0 && dist < 32 ? a.p * expf(g * (float)dist) : 0.0f;
-        }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -204,39 +210,44 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
     };
-    // the slot and use of load number L: a (not for states), b, c of each chunk in turn
+    // the slot and use of load number L: a (not for states), b, c of each chunk in turn; every role counts the
+    // chunks of all its block's pieces (gc), and barrier phases and loads go by that count
     constexpr int LOADS = STATE ? 2 : 3;
+    int base_c = 0;
 
     if (warp == kTma) {
         if (lane == 0) {
-            const int ha = h / (a.H / a.a.heads), hb = h / (a.H / a.b.heads), hc = h / (a.H / a.c.heads);
-            int L = 0;
             uint32_t uses = 0;  // bit s: parity of the phases of freeb[s] waited for
-            for (int c = 0; c < nch && !failed; ++c) {
-                const int row = chunk_row(c);
-                // the slots hold little more than a chunk, less than a load's way from DRAM: ask L2 for the tiles
-                // two chunks ahead
-                for (int cp = c == 0 ? 1 : c + kAhead; cp <= c + kAhead && cp < nch; ++cp)
-                    for (int w = 3 - LOADS; w < 3; ++w)
-                        for (int k = 0; k < C::KB; ++k)
-                            tma_prefetch_4d(w == 0 ? &mapA : w == 1 ? &mapB : &mapC, 64 * k, chunk_row(cp),
-                                            w == 0 ? ha : w == 1 ? hb : hc, b);
+            for (int item = blockIdx.x; item < items && !failed; item += gridDim.x) {
+                const Piece t(a, item);
+                const int head[3] = {t.h / (a.H / a.a.heads), t.h / (a.H / a.b.heads), t.h / (a.H / a.c.heads)};
+                for (int c = 0; c < t.nch && !failed; ++c) {
+                    // the slots hold little more than a chunk, less than a load's way from DRAM: ask L2 for the tiles
+                    // two chunks ahead
+                    for (int cp = c == 0 ? 1 : c + kAhead; cp <= c + kAhead && cp < t.nch; ++cp)
 #pragma unroll
-                for (int w = 3 - LOADS; w < 3; ++w, ++L) {
-                    const int s = L % kSlots;
-                    if (STAGED && L >= kSlots && (L - kSlots) % LOADS == LOADS - 1) {
-                        wait(stored, ((L - kSlots) / LOADS) & 1);  // the slot held c and then the outputs
-                    } else if (L >= kSlots) {
-                        wait(freeb + s, (uses >> s) & 1);
-                        uses ^= 1u << s;
+                        for (int w = 3 - LOADS; w < 3; ++w)
+                            for (int k = 0; k < C::KB; ++k)
+                                tma_prefetch_4d(w == 0 ? &mapA : w == 1 ? &mapB : &mapC, 64 * k, t.row(cp), head[w], t.b);
+                    const int row = t.row(c);
+#pragma unroll
+                    for (int w = 3 - LOADS; w < 3; ++w) {
+                        const int L = (base_c + c) * LOADS + w - (3 - LOADS), s = L % kSlots;
+                        if (STAGED && L >= kSlots && (L - kSlots) % LOADS == LOADS - 1) {
+                            wait(stored, ((L - kSlots) / LOADS) & 1);  // the slot held c and then the outputs
+                        } else if (L >= kSlots) {
+                            wait(freeb + s, (uses >> s) & 1);
+                            uses ^= 1u << s;
+                        }
+                        if (failed) break;
+                        const CUtensorMap *m = w == 0 ? &mapA : w == 1 ? &mapB : &mapC;
+                        mbar_arrive_expect_tx(full + s, C::TILE);
+                        for (int k = 0; k < C::KB; ++k)
+                            tma_load_4d(sm + s * C::TILE + k * C::BLK, m, 64 * k, row, head[w], t.b, full + s);
                     }
-                    if (failed) break;
-                    const CUtensorMap *m = w == 0 ? &mapA : w == 1 ? &mapB : &mapC;
-                    const int hh = w == 0 ? ha : w == 1 ? hb : hc;
-                    mbar_arrive_expect_tx(full + s, C::TILE);
-                    for (int k = 0; k < C::KB; ++k)
-                        tma_load_4d(sm + s * C::TILE + k * C::BLK, m, 64 * k, row, hh, b, full + s);
                 }
+                if (!C::STAYS) break;
+                base_c += t.nch;
             }
         }
     } else if (warp == kMma) {
@@ -248,8 +259,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
             constexpr uint32_t idE = idesc_bf16(128, D, false, true);
             constexpr uint32_t idU = idesc_bf16(D, D, true, true);
             auto slot_addr = [&](int L) { return base + (L % kSlots) * C::TILE; };
-            auto scores = [&](int c) {  // P = a b^T of chunk c
-                const int La = c * LOADS, Lb = La + 1;
+            auto scores = [&](int gc) {  // P = a b^T of chunk gc
+                const int La = gc * LOADS, Lb = La + 1;
                 wait(full + La % kSlots, (La / kSlots) & 1);
                 wait(full + Lb % kSlots, (Lb / kSlots) & 1);
                 if (failed) return;
@@ -262,13 +273,15 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                 }
                 mma_commit(pready);
             };
-            if (!STATE && nch > 0) scores(0);
+            for (int item = blockIdx.x; item < items && !failed; item += gridDim.x) {
+            const int nch = Piece(a, item).nch;
             for (int c = 0; c < nch && !failed; ++c) {
-                const int La = c * LOADS, Lb = La + LOADS - 2, Lc = Lb + 1;
-                const uint32_t ph = c & 1;
+                const int gc = base_c + c, La = gc * LOADS, Lb = La + LOADS - 2, Lc = Lb + 1;
+                const uint32_t ph = gc & 1;
+                if (!STATE && c == 0) scores(gc);
                 if (!STATE) {
                     wait(xready, ph);
-                    if (c > 0) wait(efree, (c - 1) & 1);
+                    if (gc > 0) wait(efree, (gc - 1) & 1);
                     if (failed) break;
                     tc_fence_after();
                     const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128);
@@ -281,7 +294,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                     mma_commit(freeb + La % kSlots);
                 }
                 wait(full + Lc % kSlots, (Lc / kSlots) & 1);
-                if (STATE && c > 0) wait(ufree, (c - 1) & 1);  // (otherwise before X was ready)
+                if (STATE && gc > 0) wait(ufree, (gc - 1) & 1);  // (otherwise before X was ready)
                 const uint64_t dB1 = sdesc(C::INPLACE ? slot_addr(Lb) : smem_u32(terms), C::BLK, 1024, kSwizzle128);
                 const uint64_t dB2 = sdesc(smem_u32(terms) + (C::INPLACE ? 0 : C::TILE), C::BLK, 1024, kSwizzle128);
                 const uint64_t dC = sdesc(slot_addr(Lc), C::BLK, 1024, kSwizzle128);
@@ -311,18 +324,23 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                         mma_bf16_ts(tb + C::cE, tb + C::cP + 64 * (k / 4) + 8 * (k % 4), dadd(dC, 2048 * k), idE, 1);
                     mma_commit(oready);
                     if (!STAGED) mma_commit(freeb + Lc % kSlots);
-                    if (c + 1 < nch) scores(c + 1);
+                    if (c + 1 < nch) scores(gc + 1);
                 }
+            }
+            if (!C::STAYS) break;
+            base_c += nch;
             }
         }
     } else if (warp < kScaleWarps) {
         // the scaled terms of b, rows of the first half and then of the second: thread (row, part of its pieces)
         constexpr int PIECES = D / 8 / (kScaleWarps * 32 / 64);
         const int hr = tid & 63, piece0 = (tid >> 6) * PIECES;
-        for (int c = 0; c < nch; ++c) {
-            const int nv = min(kRows, r1 - chunk_row(c));
-            const uint32_t ph = c & 1;
-            const int Lb = c * LOADS + LOADS - 2, Lc = Lb + 1;
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const Piece t(a, item);
+        for (int c = 0; c < t.nch; ++c) {
+            const int nv = t.valid(c), gc = base_c + c;
+            const uint32_t ph = gc & 1;
+            const int Lb = gc * LOADS + LOADS - 2, Lc = Lb + 1;
             uint8_t *tbb = sm + (Lb % kSlots) * C::TILE, *tcc = sm + (Lc % kSlots) * C::TILE;
             uint8_t *t1 = C::INPLACE ? tbb : terms, *t2 = terms + (C::INPLACE ? 0 : C::TILE);
             wait(full + Lb % kSlots, (Lb / kSlots) & 1);
@@ -331,14 +349,14 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
             for (int half = 0; half < 2; ++half) {
                 const int r = half * 64 + hr;
                 const bool on = r < nv;
-                const float w = on ? a.u * pw[nv - (a.reverse ? nv - 1 - r : r) - e] : 0.0f;
+                const float w = on ? a.u * t.power(nv - (a.reverse ? nv - 1 - r : r) - e) : 0.0f;
                 const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
                 uint4 in4[PIECES];
 #pragma unroll
                 for (int q = 0; q < PIECES; ++q)
                     in4[q] = *reinterpret_cast<const uint4 *>(tbb + ((piece0 + q) / 8) * C::BLK +
                                                               sw128_chunk(r, (piece0 + q) % 8));
-                if (c > 0) wait(uread + half, (c - 1) & 1);  // the last chunk's terms have been read
+                if (gc > 0) wait(uread + half, (gc - 1) & 1);  // the last chunk's terms have been read
 #pragma unroll
                 for (int q = 0; q < PIECES; ++q) {
                     const uint32_t off = ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8);
@@ -371,6 +389,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                 arrive(scaled + half);
             }
         }
+        if (!C::STAYS) break;
+        base_c += t.nch;
+        }
     } else if (warp < kScoreWarp0) {
         constexpr int SC = D / (kStateWarps / 4);
         // state: thread (feature f, SC of the columns); an accumulator's row f is lane f, or with 64 rows lane
@@ -388,27 +409,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                                    pack2(x[k + 6], x[k + 7]));
             }
         };
-        auto put_state = [&](int cc, const uint32_t (&x)[16]) {  // columns cc .. of X
-            if (!C::XSMEM) {
-                tmem_st16(tb + lb + C::cX + cc, x);
-            } else if (own) {
-#pragma unroll
-                for (int k = 0; k < 16; k += 4)
-                    *reinterpret_cast<uint4 *>(Xs + f * C::XS + cc + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-            }
-        };
-        auto get_state = [&](int cc, uint32_t (&x)[16]) {  // (a TMEM load still to be waited for)
-            if (!C::XSMEM) {
-                tmem_ld16(tb + lb + C::cX + cc, x);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 16; k += 4) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(Xs + f * C::XS + cc + k);
-                    x[k] = v.x; x[k + 1] = v.y; x[k + 2] = v.z; x[k + 3] = v.w;
-                }
-            }
-        };
-        const float *X0 = a.X ? a.X + (bh * a.x_pieces + (a.x_pieces > 1 ? seg : 0)) * a.da * a.dc : nullptr;
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const Piece t(a, item);
+        const float *X0 = a.X ? a.X + (t.bh * a.x_pieces + (a.x_pieces > 1 ? t.seg : 0)) * a.da * a.dc : nullptr;
 #pragma unroll 1
         for (int cc = cc0; cc < cc0 + SC; cc += 16) {
             float x[16];
@@ -419,28 +422,27 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                            ? (a.x_trans ? X0[(int64_t)(cc + k) * a.da + f] : X0[(int64_t)f * a.dc + cc + k]) : 0.0f;
                 y[k] = __float_as_uint(x[k]);
             }
-            put_state(cc, y);
-            if (!STATE) put_operand(cc, x);
+            tmem_st16(tb + lb + C::cX + cc, y);
+            if (!STATE && t.nch > 0) put_operand(cc, x);
         }
         tmem_wait_st();
-        if (!STATE) {
+        if (!STATE && t.nch > 0) {
             fence_proxy_async_smem();
             arrive(xready);
         }
-        for (int c = 0; c < nch; ++c) {
-            const int nv = min(kRows, r1 - chunk_row(c));
-            const uint32_t ph = c & 1;
+        for (int c = 0; c < t.nch; ++c) {
+            const uint32_t ph = (base_c + c) & 1;
+            const float dec = t.power(t.valid(c));
             wait(uread + 1, ph);
             if (!STATE) wait(eready, ph);  // E has read the operand
             tc_fence_after();
-            const float dec = pw[nv];
             const uint64_t dec2 = f2(dec, dec);
 #pragma unroll
             for (int c1 = 0; c1 < SC; c1 += 16) {
                 const int cc = cc0 + c1;
                 uint32_t xu[16], xx[16];
                 tmem_ld16(tb + lb + C::cU + cc, xu);
-                get_state(cc, xx);
+                tmem_ld16(tb + lb + C::cX + cc, xx);
                 tmem_wait_ld();
                 float x[16];
 #pragma unroll
@@ -449,24 +451,24 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                     xx[k] = __float_as_uint(x[k]);
                     xx[k + 1] = __float_as_uint(x[k + 1]);
                 }
-                put_state(cc, xx);
-                if (!STATE && c + 1 < nch) put_operand(cc, x);
+                tmem_st16(tb + lb + C::cX + cc, xx);
+                if (!STATE && c + 1 < t.nch) put_operand(cc, x);
             }
             tmem_wait_st();
             tc_fence_before();
             if (STATE) {
                 arrive(ufree);
-            } else if (c + 1 < nch) {
+            } else if (c + 1 < t.nch) {
                 fence_proxy_async_smem();
                 arrive(xready);
             }
         }
         if (a.Xout) {
-            float *X = a.Xout + (bh * a.nseg + seg) * a.da * a.dc + (int64_t)f * a.dc;
+            float *X = a.Xout + (t.bh * a.nseg + t.seg) * a.da * a.dc + (int64_t)f * a.dc;
 #pragma unroll 1
             for (int cc = cc0; cc < cc0 + SC; cc += 16) {
                 uint32_t x[16];
-                get_state(cc, x);
+                tmem_ld16(tb + lb + C::cX + cc, x);
                 tmem_wait_ld();
                 if (own && f < a.da) {
 #pragma unroll
@@ -476,13 +478,17 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                 __syncwarp();
             }
         }
+        if (!C::STAYS) break;
+        base_c += t.nch;
+        }
     } else if (!STATE) {
         // scores and outputs: thread (row, 1 / PARTS of the columns); PARTS warps share a quarter's rows
         constexpr int PARTS = kScoreWarps / 4, PC = kRows / PARTS, EC = D / PARTS;
         const int gw = warp - kScoreWarp0, quarter = warp & 3, part = gw >> 2, i = quarter * 32 + lane;
         const uint32_t lb = (uint32_t)(quarter * 32) << 16;
-        OUT *O = static_cast<OUT *>(a.out) + b * a.ob + (int64_t)h * a.oh;
-        const bool stores = lane == 0;
+        constexpr int GT = kScoreWarps * 32;
+        const int gt = tid - kScoreWarp0 * 32;
+        const bool stores = lane == 0 && (D == 128 || part == 0);
         auto give_slot = [&]() {  // the last chunk's outputs have left their slot
             if (stores) {
                 bulk_wait_read();
@@ -490,10 +496,20 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
             }
             __syncwarp();
         };
-        for (int c = 0; c < nch; ++c) {
-            const int row0 = chunk_row(c), nv = min(kRows, r1 - row0);
-            const uint32_t ph = c & 1;
-            if (STAGED && kSlots == 3 && c > 0) give_slot();
+        auto group_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(GT) : "memory"); };
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const Piece t(a, item);
+        OUT *O = static_cast<OUT *>(a.out) + t.b * a.ob + (int64_t)t.h * a.oh;
+        group_sync();  // the last piece's decays have been used
+        for (int k = gt; k <= kRows; k += GT) pw[k] = t.power(k);
+        for (int k = gt; k < 4 * kDiagCopy; k += GT) {
+            const int dist = (k % kDiagCopy + k / kDiagCopy - 31) * (a.reverse ? 1 : -1);
+            diag[k] = dist >= 0 && dist < 32 ? a.p * t.power(dist) : 0.0f;
+        }
+        group_sync();
+        for (int c = 0; c < t.nch; ++c) {
+            const int row0 = t.row(c), nv = t.valid(c), gc = base_c + c;
+            const uint32_t ph = gc & 1;
             wait(pready, ph);
             tc_fence_after();
 #pragma unroll
@@ -503,7 +519,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                 decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, w);
                 tmem_st16(tb + lb + C::cP + 64 * (blk / 2) + 16 * (blk % 2), w);
             }
-            if (STAGED && kSlots == 4 && c > 0) give_slot();
+            if (STAGED && gc > 0) give_slot();
             wait(eready, ph);
             tc_fence_after();
             const int m = a.reverse ? nv - 1 - i : i;
@@ -532,7 +548,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
             arrive(masked);
             wait(oready, ph);
             tc_fence_after();
-            const int Lc = c * LOADS + LOADS - 1;
+            const int Lc = gc * LOADS + LOADS - 1;
             uint8_t *tcc = sm + (Lc % kSlots) * C::TILE;  // U and the scores' product have read c
             OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
 #pragma unroll
@@ -565,29 +581,31 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, Cfg<D, NT, STATE>:
                 }
                 __syncwarp();
             }
-            if (STAGED) {  // a warp's 32 rows of a 64-column block
-                static_assert(EC == 64, "one block of columns a warp");
+            if (STAGED) {  // 32 rows of a 64-column block at a time: a warp's own, or with D = 64 its pair's
                 fence_proxy_async_smem();
-                __syncwarp();
+                if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(2 + quarter) : "memory");
+                else __syncwarp();
                 if (stores) {
-                    const int blk = part, row = row0 + quarter * 32;
+                    const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
                     if (row < a.n && 64 * blk < a.dc)
-                        tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, h, b);
+                        tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, t.h, t.b);
                     bulk_commit();
                 }
                 __syncwarp();
             }
         }
-        if (STAGED && stores) bulk_wait();
         // rows at and past the length
-        constexpr int ZB = 16 / (int)sizeof(OUT), GT = kScoreWarps * 32;
-        const int gt = tid - kScoreWarp0 * 32, pieces = a.dc / ZB, step = GT / pieces;
-        const int z0 = min(rend, r0 + nch * kRows);  // staged chunks have written theirs
-        const int zr = STAGED ? z0 : r1;
+        constexpr int ZB = 16 / (int)sizeof(OUT);
+        const int pieces = a.dc / ZB, step = GT / pieces;
+        const int zr = STAGED ? min(t.rend, t.r0 + t.nch * kRows) : t.r1;  // staged chunks have written theirs
         OUT *z = O + (int64_t)zr * a.ot + (gt % pieces) * ZB;
         if (gt < step * pieces)
-            for (int k = gt / pieces; k < rend - zr; k += step)
+            for (int k = gt / pieces; k < t.rend - zr; k += step)
                 *reinterpret_cast<uint4 *>(z + (int64_t)k * a.ot) = make_uint4(0, 0, 0, 0);
+        if (!C::STAYS) break;
+        base_c += t.nch;
+        }
+        if (STAGED && stores) bulk_wait();
     }
     __syncwarp();
     tc_fence_before();
@@ -622,7 +640,8 @@ cudaError_t launch(const DecayMix &a, cudaStream_t s) {
         return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(k_decay_tc<D, NT, STATE, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nseg);
+    const int64_t items = (int64_t)a.B * a.H * a.nseg;
+    const unsigned grid = (unsigned)(C::STAYS && items > tc_sm_count() ? tc_sm_count() : items);
     LUNA_LAUNCH(STATE ? "decay_state_tc" : "decay_mix_tc", (k_decay_tc<D, NT, STATE, OUT>), grid, C::THREADS, C::SMEM, s, mA,
                 mB, mC, mO, a);
     return cudaGetLastError();
