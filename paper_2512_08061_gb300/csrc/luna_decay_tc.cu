@@ -95,7 +95,7 @@ constexpr int kDiagCopy = 72;
 // Off the diagonal block the decay is a factor of the row times one of the column (both at most 1 for
 // lambda <= 1), on it it comes from the table of decays by distance, 0 where the distance is negative.
 __device__ __forceinline__ void decay_scores(uint32_t taddr, int i, int jb, bool reverse, int nv, float p,
-                                             const float *pw, const float *diag, uint32_t (&w)[16]) {
+                                             const float *pw, const float *diag, const float *cols, uint32_t (&w)[16]) {
     const int ib = i >> 5, li = i & 31, j0 = 32 * jb;
     if (reverse ? jb < ib : jb > ib) {  // the same for the whole warp
 #pragma unroll
@@ -117,15 +117,13 @@ __device__ __forceinline__ void decay_scores(uint32_t taddr, int i, int jb, bool
     } else {
         const float row = p * (reverse ? pw[j0 - i] : pw[i - j0 - 31]);
         const uint64_t row2 = f2(row, row);
-        const float4 *t = reinterpret_cast<const float4 *>(pw);
+        const float4 *t = reinterpret_cast<const float4 *>(cols);
         tmem_wait_ld();
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            // forward: column j of the block decays by 31 - j, reverse: by j
-            const float4 c = reverse ? t[q] : t[7 - q];
-            const uint64_t c0 = reverse ? f2(c.x, c.y) : f2(c.w, c.z), c1 = reverse ? f2(c.z, c.w) : f2(c.y, c.x);
-            w[2 * q] = pack2(mul2(f2(x[4 * q], x[4 * q + 1]), mul2(row2, c0)));
-            w[2 * q + 1] = pack2(mul2(f2(x[4 * q + 2], x[4 * q + 3]), mul2(row2, c1)));
+            const float4 c = t[q];
+            w[2 * q] = pack2(mul2(f2(x[4 * q], x[4 * q + 1]), mul2(row2, f2(c.x, c.y))));
+            w[2 * q + 1] = pack2(mul2(f2(x[4 * q + 2], x[4 * q + 3]), mul2(row2, f2(c.z, c.w))));
         }
     }
     if (nv < kRows) {
@@ -174,7 +172,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     uint8_t *Xop = terms + C::TERMS * C::TILE;
     float *pw = reinterpret_cast<float *>(Xop + (STATE ? 0 : C::XOP));  // lambda^0 .. lambda^128 of the scores' warps' piece
     float *diag = pw + 132;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(diag + 4 * kDiagCopy);
+    float *cols = diag + 4 * kDiagCopy;  // of column j of a block: lambda^{31 - j}, in reverse order lambda^j
+    uint64_t *bars = reinterpret_cast<uint64_t *>(cols + 32);
     uint64_t *full = bars, *freeb = bars + kSlots, *pready = bars + 2 * kSlots;
     uint64_t *eready = pready + 1, *scaled = pready + 2 /* of each half */, *uread = pready + 4 /* of each half */;
     uint64_t *xready = pready + 6, *masked = pready + 7, *oready = pready + 8, *efree = pready + 9, *ufree = pready + 10;
@@ -201,7 +200,8 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     const uint32_t tb = *tslot;
     bool failed = false;
     auto wait = [&](uint64_t *bar, uint32_t parity) {  // bounded; a no-op once it has run out
-        if (!failed && !mbar_wait_long(bar, parity)) {
+        // (the states' kernel, whose code is small, has the waits in line: 9 % there)
+        if (!failed && !(STATE ? mbar_wait(bar, parity) : mbar_wait_long(bar, parity))) {
             failed = true;
             atomicOr(a.status, 1);
         }
@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                 const int La = gc * LOADS, Lb = La + 1;
                 wait(full + La % kSlots, (La / kSlots) & 1);
                 wait(full + Lb % kSlots, (Lb / kSlots) & 1);
+                if (gc > 0) wait(oready, (gc - 1) & 1);  // the last chunk's scores have been read
                 if (failed) return;
                 tc_fence_after();
                 const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128), dB = sdesc(slot_addr(Lb), 16, 1024, kSwizzle128);
@@ -437,7 +438,9 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             if (!STATE) wait(eready, ph);  // E has read the operand
             tc_fence_after();
             const uint64_t dec2 = f2(dec, dec);
-#pragma unroll
+            // (one copy of the code where two more groups of warps compete for the instruction cache)
+            constexpr int kUnroll = STATE ? SC / 16 : 1;
+#pragma unroll kUnroll
             for (int c1 = 0; c1 < SC; c1 += 16) {
                 const int cc = cc0 + c1;
                 uint32_t xu[16], xx[16];
@@ -506,17 +509,18 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             const int dist = (k % kDiagCopy + k / kDiagCopy - 31) * (a.reverse ? 1 : -1);
             diag[k] = dist >= 0 && dist < 32 ? a.p * t.power(dist) : 0.0f;
         }
+        if (gt < 32) cols[gt] = t.power(a.reverse ? gt : 31 - gt);
         group_sync();
         for (int c = 0; c < t.nch; ++c) {
             const int row0 = t.row(c), nv = t.valid(c), gc = base_c + c;
             const uint32_t ph = gc & 1;
             wait(pready, ph);
             tc_fence_after();
-#pragma unroll
+#pragma unroll 1
             for (int q = 0; q < PC / 32; ++q) {  // the bf16 scores take the place of columns that this warp has read
                 const int blk = part * (PC / 32) + q;
                 uint32_t w[16];
-                decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, w);
+                decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, cols, w);
                 tmem_st16(tb + lb + C::cP + 64 * (blk / 2) + 16 * (blk % 2), w);
             }
             if (STAGED && gc > 0) give_slot();
@@ -525,7 +529,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             const int m = a.reverse ? nv - 1 - i : i;
             const float xs = a.x * pw[max(0, m) + e];
             const uint64_t xs2 = f2(xs, xs);
-#pragma unroll
+#pragma unroll 1
             for (int q = 0; q < EC / 32; ++q) {
                 uint32_t x[32];
                 tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
@@ -551,7 +555,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             const int Lc = gc * LOADS + LOADS - 1;
             uint8_t *tcc = sm + (Lc % kSlots) * C::TILE;  // U and the scores' product have read c
             OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
-#pragma unroll
+#pragma unroll 1
             for (int q = 0; q < EC / 32; ++q) {
                 uint32_t x[32];
                 tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);

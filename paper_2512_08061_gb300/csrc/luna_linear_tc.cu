@@ -315,6 +315,24 @@ bool operand_map(CUtensorMap *m, const MatView &v, int64_t rows, int64_t K, int 
     return tc_make_map_nd(m, v.p, 2, dims, strides, box);
 }
 
+// Cycles of a tile's 64-deep step (its products at 8/10 to 9/10 of the tensor rate, measured on large
+// products) and of what a block does around its steps, for choosing between tiles.
+template <int CG, int BN> constexpr int step_cycles() { return CG == 2 ? 560 : BN == 256 ? 640 : BN == 128 ? 360 : 250; }
+constexpr int kTileCycles = 2500;
+
+struct Choice {
+    int splits;
+    double cycles;
+};
+template <int CG, int BN>
+Choice cost(const Product &p) {
+    const int64_t tiles = ((p.M + 128 * CG - 1) / (128 * CG)) * ((p.N + BN - 1) / BN), steps = (p.K + kDepth - 1) / kDepth;
+    const int splits = linear_splits(p, tiles * CG, 256);
+    const int64_t rounds = (tiles * splits * CG + tc_sm_count() - 1) / tc_sm_count();
+    return Choice{splits, (double)rounds * ((double)((steps + splits - 1) / splits) * step_cycles<CG, BN>()) + kTileCycles +
+                              (splits > 1 ? kTileCycles : 0)};
+}
+
 template <int CG, int BN>
 cudaError_t launch(ProductTc a, cudaStream_t s) {
     using T = Tile<CG, BN>;
@@ -371,10 +389,9 @@ cudaError_t launch_product_tc(const Product &p, cudaStream_t s) {
         // (an MN-major slice is 64 wide)
         return p.M <= 32 && !p.A.kt ? launch<1, 32>(a, s) : launch<1, 64>(a, s);
     }
-    const int64_t sms = tc_sm_count();
-    if (cdiv(p.M, 256) * cdiv(p.N, 256) * 2 >= sms) return launch<2, 256>(a, s);
-    if (cdiv(p.M, 128) * cdiv(p.N, 256) >= sms) return launch<1, 256>(a, s);
-    return launch<1, 128>(a, s);
+    const double pair = cost<2, 256>(p).cycles, wide = cost<1, 256>(p).cycles, half = cost<1, 128>(p).cycles;
+    if (pair <= wide && pair <= half) return launch<2, 256>(a, s);
+    return wide <= half ? launch<1, 256>(a, s) : launch<1, 128>(a, s);
 }
 
 }  // namespace luna

@@ -67,11 +67,10 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, uint64
     }
 }
 
-// The same wait for kernels with many warps at barriers: the thread stays suspended in hardware for up to
-// 20 us at a time instead of the default, so that waiting warps take fewer issue slots and shared-memory
-// accesses from the working ones.
-__device__ __forceinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns = 1000000000ull) {
-    if (mbar_try_wait(bar, parity)) return true;
+// The same wait for kernels with many warps at many barriers: the thread stays suspended in hardware for up
+// to 20 us at a time instead of the default, so that waiting warps take fewer issue slots and shared-memory
+// accesses from the working ones, and the loop is one copy of code for all its callers.
+static __device__ __noinline__ bool mbar_wait_loop(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
     const uint64_t t0 = globaltimer_ns();
     while (true) {
         for (int i = 0; i < 16; ++i) {
@@ -81,12 +80,15 @@ __device__ __forceinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, u
                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
                 "selp.u32 %0, 1, 0, p;\n\t}"
                 : "=r"(ok)
-                : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+                : "r"(bar), "r"(parity), "r"(20000u)
                 : "memory");
             if (ok) return true;
         }
         if (globaltimer_ns() - t0 > limit_ns) return false;
     }
+}
+__device__ __forceinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns = 1000000000ull) {
+    return mbar_try_wait(bar, parity) || mbar_wait_loop(smem_u32(bar), parity, limit_ns);
 }
 
 // ---------------------------------------------------------------------------
