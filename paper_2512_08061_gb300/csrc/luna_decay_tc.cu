@@ -27,7 +27,7 @@ namespace luna {
 
 int tc_sm_count();
 bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
-                    const uint32_t *box);
+                    const uint32_t *box, int swizzle = 128);
 
 namespace {
 using namespace sm100;

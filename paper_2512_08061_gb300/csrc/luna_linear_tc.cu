@@ -10,7 +10,9 @@
 // CG = 2: two CTAs of a cluster share a 256 x BN tile.  Each holds its 128 rows of A and half of B
 // (a CTA alone has to read A and all of B from its shared memory for every product, which the
 // shared-memory bandwidth does not sustain at 128 x 256), and the leader's thread issues the products
-// of both.  TMA zero-fills past every edge, so ragged sizes only guard the stores.
+// of both.  TMA zero-fills past every edge and drops what a store holds past it.  The epilogue's warps
+// hand 32 x 32 pieces to TMA stores (a lane's own row, written directly, would touch 32 lines an
+// instruction: 20 to 40 % of the whole product at a depth of 1024).
 #include "luna_linear.cuh"
 
 #include <algorithm>
@@ -22,7 +24,7 @@ namespace luna {
 
 int tc_sm_count();
 bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
-                    const uint32_t *box);
+                    const uint32_t *box, int swizzle = 128);
 
 namespace {
 using namespace sm100;
@@ -35,16 +37,18 @@ template <int CG, int BN> struct Tile {
     static constexpr int NB = BN / CG;                // B rows a CTA holds
     static constexpr int NBL = NB < 64 ? 64 : NB;     // ... and loads (an MN-major slice is 64 wide)
     static constexpr uint32_t A_BYTES = BM * 128, B_BYTES = NBL * 128, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = (int)((208 * 1024) / STAGE) > 8 ? 8 : (int)((208 * 1024) / STAGE);
+    static constexpr int STAGES = (int)((192 * 1024) / STAGE) > 8 ? 8 : (int)((192 * 1024) / STAGE);
     static constexpr uint32_t COLS = 2 * BN;          // two accumulators
-    static constexpr uint32_t SMEM = STAGES * STAGE + 1024 + 256;
+    static constexpr uint32_t OUT = kEpiWarps * 4096;   // two 32 x 32 pieces of every epilogue warp
+    static constexpr uint32_t SMEM = STAGES * STAGE + OUT + 1024 + 256;
+    static_assert(SMEM <= 227 * 1024, "shared memory");
 };
 
 struct ProductTc {
     Product p;
     int tiles_m, tiles_n, splits, k_steps, steps_per_split;  // tiles of BM * CG rows, BN columns
     bool swap;      // the product is computed transposed: A = the layer's B (few rows of X)
-    bool vec;       // outputs and residual on 16-byte boundaries
+    bool vec;       // outputs and residual on 16-byte boundaries: the epilogue stores by TMA
 };
 
 __device__ __forceinline__ uint8_t *align_1024(uint8_t *p) {
@@ -67,65 +71,56 @@ __device__ __forceinline__ void unit_tile(const ProductTc &a, int u, int &tm, in
     tn = r / rows;
 }
 
-// Epilogue of 32 columns of one row, all inside the output, 16-byte accesses.
-template <int ACT>
-__device__ __forceinline__ void finish_vec(const Product &p, int64_t row, int64_t col, float (&v)[32]) {
-    using B = __nv_bfloat16;
-    if (p.bias) {
-        const uint4 *b = reinterpret_cast<const uint4 *>(static_cast<const B *>(p.bias) + col);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint4 w = __ldg(b + q);
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
-                v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
-            }
-        }
-    }
-    if (p.Z) {
-        uint4 *z = reinterpret_cast<uint4 *>(static_cast<B *>(p.Z) + row * p.ldz + col);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            z[q] = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
-                              pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
-    }
-    if (ACT != LUNA_LINEAR_NONE) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = linear_act<B>(v[i], ACT);
-    }
-    if (p.R) {
-        const uint4 *r = reinterpret_cast<const uint4 *>(static_cast<const B *>(p.R) + row * p.ldr + col);
-        uint4 w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = r[q];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t x[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
-                v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
-            }
-        }
-    }
-    uint4 *o = reinterpret_cast<uint4 *>(static_cast<B *>(p.out) + row * p.ldo + col);
+// 32 columns of a lane's row into the warp's piece (64-byte rows, swizzled) and on to the output's rows
+// row0 .. row0 + 31.  `piece` alternates between two.
+__device__ __forceinline__ void store_piece(uint8_t *piece, const CUtensorMap *map, int64_t col, int64_t row0,
+                                            const float (&v)[32], int lane) {
+    if (lane == 0) bulk_wait_read_but_one();
+    __syncwarp();
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        o[q] = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
-                          pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+        *reinterpret_cast<uint4 *>(piece + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
+            make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]), pack2(v[8 * q + 4], v[8 * q + 5]),
+                       pack2(v[8 * q + 6], v[8 * q + 7]));
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+        tma_store_2d(map, piece, (int)col, (int)row0);
+        bulk_commit();
+    }
+}
+
+__device__ __forceinline__ void add32(float (&v)[32], const uint4 *p) {
+    uint4 w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = p[q];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t x[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
+            v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
+        }
+    }
+}
+
+template <int ACT> __device__ __forceinline__ void act32(float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = linear_act<__nv_bfloat16>(v[i], ACT);
 }
 
 template <int CG, int BN>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_product_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+                 const __grid_constant__ CUtensorMap mapO, const __grid_constant__ CUtensorMap mapZ,
                  const __grid_constant__ ProductTc a) {
     using T = Tile<CG, BN>;
     constexpr int S = T::STAGES;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = align_1024(smem_raw);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(sm + S * T::STAGE);
+    uint8_t *pieces = sm + S * T::STAGE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(pieces + T::OUT);
     uint64_t *full = bars, *empty = bars + S, *tfull = bars + 2 * S, *tempty = tfull + 2;
     uint32_t *tslot = reinterpret_cast<uint32_t *>(tempty + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -227,7 +222,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tempty_leader[2] = {CG == 2 ? leader_addr(tempty) : 0, CG == 2 ? leader_addr(tempty + 1) : 0};
-        int n = 0;
+        int n = 0, stored = 0;
         for (int u = first; u < units && !failed; u += stride, ++n) {
             int tm, tn, sp;
             unit_tile(a, u, tm, tn, sp);
@@ -249,7 +244,39 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 for (int i = 0; i < 32; ++i) v[i] = last_split_empty ? 0.0f : __uint_as_float(x[i]);
                 const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;  // of the computed product
                 const int w = row < M ? (int)max((int64_t)0, min((int64_t)32, N - col)) : 0;
-                if (w == 0) {
+                if (a.vec) {  // the whole warp, for its 32 rows
+                    using B = __nv_bfloat16;
+                    const int64_t row0 = row - lane;
+                    if (row0 < M && col < N) {
+                        if (p.bias) {
+                            if (N - col >= 32) {
+                                add32(v, reinterpret_cast<const uint4 *>(static_cast<const B *>(p.bias) + col));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (col + i < N) v[i] += io_load(static_cast<const B *>(p.bias) + col + i);
+                            }
+                        }
+                        if (p.Z) store_piece(pieces + warp * 4096 + (stored++ & 1) * 2048, &mapZ, col, row0, v, lane);
+                        switch (p.act) {
+                            case LUNA_LINEAR_RELU: act32<LUNA_LINEAR_RELU>(v); break;
+                            case LUNA_LINEAR_GELU: act32<LUNA_LINEAR_GELU>(v); break;
+                            case LUNA_LINEAR_SILU: act32<LUNA_LINEAR_SILU>(v); break;
+                            default: break;
+                        }
+                        if (p.R && row < M) {
+                            const B *r = static_cast<const B *>(p.R) + row * p.ldr + col;
+                            if (N - col >= 32) {
+                                add32(v, reinterpret_cast<const uint4 *>(r));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (col + i < N) v[i] += io_load(r + i);
+                            }
+                        }
+                        store_piece(pieces + warp * 4096 + (stored++ & 1) * 2048, &mapO, col, row0, v, lane);
+                    }
+                } else if (w == 0) {
                     // nothing of the row in this chunk
                 } else if (a.swap) {
                     if (a.splits > 1) {
@@ -272,13 +299,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         for (int i = 0; i < 32; ++i)
                             if (i < w) o[i] = v[i];
                     }
-                } else if (a.vec && w == 32) {
-                    switch (p.act) {
-                        case LUNA_LINEAR_NONE: finish_vec<LUNA_LINEAR_NONE>(p, row, col, v); break;
-                        case LUNA_LINEAR_RELU: finish_vec<LUNA_LINEAR_RELU>(p, row, col, v); break;
-                        case LUNA_LINEAR_GELU: finish_vec<LUNA_LINEAR_GELU>(p, row, col, v); break;
-                        default: finish_vec<LUNA_LINEAR_SILU>(p, row, col, v);
-                    }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
@@ -293,6 +313,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 else mbar_arrive(tempty + acc);
             }
         }
+        if (lane == 0) bulk_wait();
     }
     __syncwarp();
     tc_fence_before();
@@ -313,6 +334,12 @@ bool operand_map(CUtensorMap *m, const MatView &v, int64_t rows, int64_t K, int 
     const uint64_t strides[1] = {(uint64_t)v.ld * 2};
     const uint32_t box[2] = {64, (uint32_t)(v.kt ? kDepth : slice_rows)};
     return tc_make_map_nd(m, v.p, 2, dims, strides, box);
+}
+
+bool output_map(CUtensorMap *m, const void *p, int64_t ld, int64_t M, int64_t N) {
+    const uint64_t dims[2] = {(uint64_t)N, (uint64_t)M}, strides[1] = {(uint64_t)ld * 2};
+    const uint32_t box[2] = {32, 32};
+    return tc_make_map_nd(m, p, 2, dims, strides, box, 64);
 }
 
 // Cycles of a tile's 64-deep step (its products at 8/10 to 9/10 of the tensor rate, measured on large
@@ -346,8 +373,12 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     a.splits = linear_splits(p, tiles * CG, 256);
     a.steps_per_split = (int)cdiv(a.k_steps, a.splits);
     a.splits = (int)cdiv(a.k_steps, a.steps_per_split);
-    CUtensorMap mA, mB;
+    CUtensorMap mA, mB, mO, mZ;
+    a.vec = a.vec && !a.swap && a.splits == 1;
     if (!operand_map(&mA, p.A, M, p.K, T::BM) || !operand_map(&mB, p.B, N, p.K, T::NBL)) return cudaErrorInvalidValue;
+    mO = mZ = mA;
+    if (a.vec && (!output_map(&mO, p.out, p.ldo, M, N) || (p.Z && !output_map(&mZ, p.Z, p.ldz, M, N))))
+        return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(k_product_tc<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
     if (e != cudaSuccess) return e;
     const int sms = tc_sm_count() / CG * CG;
@@ -365,7 +396,7 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     cfg.attrs = at;
     cfg.numAttrs = CG == 2 ? 1 : 0;
     prof_before("product_tc", s);
-    e = cudaLaunchKernelEx(&cfg, k_product_tc<CG, BN>, mA, mB, a);
+    e = cudaLaunchKernelEx(&cfg, k_product_tc<CG, BN>, mA, mB, mO, mZ, a);
     prof_after("product_tc", s);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || splits == 1) return e;
     return launch_product_finish(p, splits, LUNA_BF16, s);

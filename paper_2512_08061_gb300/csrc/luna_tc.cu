@@ -918,8 +918,9 @@ bool tc_make_map(CUtensorMap *m, const void *base, int width, int n, int BH, int
 bool tc_make_map_rows(CUtensorMap *m, const void *base, int width, int n, int BH, int rows, int hs_mul) {
     return make_map_impl(m, base, width, n, BH, rows, hs_mul);
 }
+// `swizzle`: bytes of the swizzle pattern, 128 or 64 (at least the box's inner extent).
 bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *dims, const uint64_t *strides,
-                    const uint32_t *box) {
+                    const uint32_t *box, int swizzle) {
     EncodeTiledFn enc = encoder();
     if (!enc) return false;
     cuuint64_t d[5], st[5];
@@ -927,7 +928,7 @@ bool tc_make_map_nd(CUtensorMap *m, const void *base, int rank, const uint64_t *
     for (int i = 0; i < rank; ++i) { d[i] = dims[i]; b[i] = box[i]; es[i] = 1; }
     for (int i = 0; i + 1 < rank; ++i) st[i] = strides[i];
     return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), d, st, b, es,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 int tc_sm_count() { return sm_count_impl(); }
