@@ -387,6 +387,10 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                     }
                 }
                 fence_proxy_async_smem();
+                // These warps read b alone, and b's slot held an a before: its load is known to be complete only by P
+                // of that chunk, and without that the wait for b would take the phase before a's load for b's.  Before
+                // the arrival that lets this chunk's last products go ahead, so that P is never two phases on.
+                if (!STATE && !C::INPLACE && half == 1) wait(pready, ph);
                 arrive(scaled + half);
             }
         }

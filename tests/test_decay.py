@@ -139,6 +139,28 @@ def test_prompts_and_gradients(L, B, H, Hkv, n, d, dv, io, layout, lengths, stat
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H,Hkv,n,d,dv", [(8, 8, 1024, 128, 128), (8, 2, 900, 128, 64), (6, 6, 1100, 64, 64), (12, 4, 700, 32, 64)])
+def test_many_heads_of_many_chunks(L, H, Hkv, n, d, dv):
+    """Every SM at work on pieces of many chunks (few heads are cut into pieces of one or two), against the
+    fp32 form of the same call on the same values: both within the bf16 tolerance of the definition."""
+    B = 40
+    Q, K, V, dO, ld, _, _ = inputs(B, H, Hkv, n, d, dv, BF, "tokens", 21, False)
+    lens = torch.randint(n // 2, n + 1, (B,), device="cuda", dtype=torch.int32)
+    p, f = L.Decay(B, H, n, d, dv, Hkv=Hkv, io=BF, backward=True), L.Decay(B, H, n, d, dv, Hkv=Hkv, io=F, backward=True)
+    wide = [x.float() for x in (Q, K, V, dO)]
+    want, S = f.forward(*wide[:3], ld, lens, want_state=True)
+    grads = f.backward(*wide, ld, lens)
+    for _ in range(3):
+        got, S1 = p.forward(Q, K, V, ld, lens, want_state=True)
+        pairs = {"O": (got, want), "S1": (S1, S), "O without state": (p.forward(Q, K, V, ld, lens), want)}
+        pairs.update({k: (v, grads[k]) for k, v in p.backward(Q, K, V, dO, ld, lens).items()})
+        assert L.luna_device_status(p.ws) == 0
+        for name, (a, b) in pairs.items():
+            by_head = (a.double() - b).flatten(2).norm(dim=2) / b.double().flatten(2).norm(dim=2)
+            assert by_head.max() < TOL[a.dtype], name
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("io", [F, BF])
 def test_padding_may_hold_anything(L, io):
     """NaN in rows at and past the length reaches no output; lengths outside [0, n] are clamped."""
