@@ -433,8 +433,11 @@ luna_status luna_norm_bwd(const luna_norm_desc *nd, const void *x, const void *y
  * that).  bias and R may be NULL; R may be Y.  Z, where not NULL, receives the
  * pre-activation, which luna_linear_bwd needs with an activation.  GELU is the
  * erf form.  Sums are fp32.
- * bf16 with 16-byte aligned matrices and leading dimensions that are multiples
- * of 8 runs on tensor cores; everything else in fp32 on CUDA cores.
+ * bf16 runs on tensor cores (with n or k that is not a multiple of 8 from
+ * aligned copies of the operands in the workspace; a matrix that is off a
+ * 16-byte boundary, or whose leading dimension is not a multiple of 8, although
+ * n and k are, is multiplied on CUDA cores), up to eight rows of X and fp32 on
+ * CUDA cores.
  * Supported: m <= 2^23, n, k <= 2^20; k = 0 sums nothing. */
 typedef enum {
     LUNA_LINEAR_NONE = 0, LUNA_LINEAR_RELU = 1, LUNA_LINEAR_GELU = 2, LUNA_LINEAR_SILU = 3

@@ -63,20 +63,20 @@ __device__ __forceinline__ void store_vec(IO *p, const float (&v)[VEC]) {
 }
 
 // 128 x 128 tile of A B^T over one piece of K: operands staged in shared memory 16 deep, eight by
-// eight sums a thread in fp32, the next step's values loaded while this one's are multiplied.
+// eight sums a thread in fp32, two multiply-adds an instruction, the next step's values loaded while this one's are multiplied.
 // Bound by the fp32 FMA rate.
 template <typename IO>
 __global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, int splits) {
-    __shared__ float sA[kK][kT + 4], sB[kK][kT + 4];
+    __shared__ __align__(16) float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
     clear_status(p.clear, p.status);
     const int64_t row0 = (int64_t)blockIdx.x * kT, col0 = (int64_t)blockIdx.y * kT;
     const int64_t k0 = (int64_t)blockIdx.z * depth, k1 = min(p.K, k0 + depth);
-    float acc[8][8];
+    uint64_t acc[8][4];  // pairs of columns
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = 0.0f;
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0;
     float ra[8], rb[8];
     // element i of a thread: along the contiguous dimension of each operand
     auto place = [&](bool kt, int i, int &r, int &k) {
@@ -108,15 +108,19 @@ __global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, 
         if (kb + kK < k1) fetch(kb + kK);
 #pragma unroll
         for (int k = 0; k < kK; ++k) {
-            float a[8], b[8];
+            float a[8];
+            uint64_t b[4];
             *reinterpret_cast<float4 *>(a) = *reinterpret_cast<const float4 *>(&sA[k][ty * 4]);
             *reinterpret_cast<float4 *>(a + 4) = *reinterpret_cast<const float4 *>(&sA[k][64 + ty * 4]);
-            *reinterpret_cast<float4 *>(b) = *reinterpret_cast<const float4 *>(&sB[k][tx * 4]);
-            *reinterpret_cast<float4 *>(b + 4) = *reinterpret_cast<const float4 *>(&sB[k][64 + tx * 4]);
+            *reinterpret_cast<ulonglong2 *>(b) = *reinterpret_cast<const ulonglong2 *>(&sB[k][tx * 4]);
+            *reinterpret_cast<ulonglong2 *>(b + 2) = *reinterpret_cast<const ulonglong2 *>(&sB[k][64 + tx * 4]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i) {
+                uint64_t aa;
+                asm("mov.b64 %0, {%1, %1};" : "=l"(aa) : "f"(a[i]));
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+                for (int j = 0; j < 4; ++j) asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[i][j]) : "l"(aa), "l"(b[j]));
+            }
         }
     }
 #pragma unroll
@@ -126,8 +130,10 @@ __global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, 
         for (int j = 0; j < 8; ++j) {
             const int64_t col = col0 + (j < 4 ? tx * 4 + j : 60 + tx * 4 + j);
             if (row >= p.M || col >= p.N) continue;
-            if (splits > 1) p.part[((int64_t)blockIdx.z * p.M + row) * p.N + col] = acc[i][j];
-            else linear_finish<IO>(p, row, col, acc[i][j]);
+            float v[2];
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(v[0]), "=f"(v[1]) : "l"(acc[i][j / 2]));
+            if (splits > 1) p.part[((int64_t)blockIdx.z * p.M + row) * p.N + col] = v[j % 2];
+            else linear_finish<IO>(p, row, col, v[j % 2]);
         }
     }
 }
@@ -199,10 +205,10 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
     }
 }
 
-// dZ = dY act'(Z) (not written where there is no activation) and the column sums of dZ over a
+// dZ = dY act'(Z) (not written where there is no activation; rows lddz apart) and the column sums of dZ over a
 // block's rows, one partial row a block.  32 column pieces x 8 rows of threads; bound by the bytes.
 template <typename IO, int VEC>
-__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ, int64_t m,
+__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ, int64_t lddz, int64_t m,
                                                    int n, int act, int64_t rows, float *part, int *status) {
     __shared__ float s[8][32 * VEC + 1];
     clear_status(1, status);
@@ -221,7 +227,7 @@ __global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, c
                 load_vec<IO, VEC>(Z + r * ldz + c, z);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) d[e] *= linear_slope<IO>(z[e], act);
-                store_vec<IO, VEC>(dZ + r * n + c, d);
+                store_vec<IO, VEC>(dZ + r * lddz + c, d);
             }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) acc[e] += d[e];
@@ -240,6 +246,22 @@ __global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, c
         }
 }
 
+// Rows of `width` bf16 values, `ld` apart, into rows `ldp` (a multiple of 8) apart: 16 bytes a thread.
+__global__ void __launch_bounds__(256) k_pad_rows(const __nv_bfloat16 *src, int64_t ld, __nv_bfloat16 *dst, int64_t ldp,
+                                                  int64_t rows, int64_t width) {
+    const int64_t per = ldp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * per) return;
+    const int64_t r = i / per, c = (i % per) * 8;
+    const uint16_t *p = reinterpret_cast<const uint16_t *>(src) + r * ld + c;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = c + 2 * k < width ? p[2 * k] : 0, hi = c + 2 * k + 1 < width ? p[2 * k + 1] : 0;
+        w[k] = lo | (hi << 16);
+    }
+    *reinterpret_cast<uint4 *>(dst + r * ldp + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 template <typename IO>
 __global__ void __launch_bounds__(256) k_linear_db(const float *part, int parts, int n, IO *db) {
     const int c = blockIdx.x * 256 + threadIdx.x;
@@ -256,7 +278,7 @@ luna_status cuda_status(cudaError_t e) { return e == cudaSuccess ? LUNA_OK : LUN
 template <typename IO>
 cudaError_t simt(const Product &p, cudaStream_t s) {
     const int64_t gx = cdiv(p.M, kT), gy = cdiv(p.N, kT);
-    const int splits = linear_splits(p, gx * gy, 512);
+    const int splits = linear_splits(p, gx * gy, 64);  // (a step of 16 takes about a microsecond when alone)
     const int64_t depth = std::max<int64_t>(1, cdiv(cdiv(p.K, splits), kK)) * kK;
     const int used = (int)std::max<int64_t>(1, cdiv(p.K, depth));
     LUNA_LAUNCH("product", k_product<IO>, dim3((unsigned)gx, (unsigned)gy, used), kThreads, 0, s, p, depth, used);
@@ -270,23 +292,23 @@ constexpr int64_t kDzRows = 256;  // rows of a block of the column sums
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 template <typename IO, int VEC>
-void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t m, int n, int act, float *part,
+void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act, float *part,
                int parts, int *status, cudaStream_t s) {
     LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC>), dim3((unsigned)cdiv(n, 32 * VEC), parts), 256, 0, s,
-                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), m, n, act, kDzRows,
+                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, m, n, act, kDzRows,
                 part, status);
 }
 
 template <typename IO>
-cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t m, int n, int act, float *part,
-               void *db, int *status, cudaStream_t s) {
+cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act,
+               float *part, void *db, int *status, cudaStream_t s) {
     constexpr int VEC = 16 / (int)sizeof(IO);
     const int parts = (int)cdiv(m, kDzRows);
     const bool a = act != LUNA_LINEAR_NONE;
     if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
-        dz_launch<IO, VEC>(dY, lddy, Z, ldz, dZ, m, n, act, db ? part : nullptr, parts, status, s);
+        dz_launch<IO, VEC>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
     else
-        dz_launch<IO, 1>(dY, lddy, Z, ldz, dZ, m, n, act, db ? part : nullptr, parts, status, s);
+        dz_launch<IO, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !db) return e;
     LUNA_LAUNCH("linear_db", k_linear_db<IO>, (unsigned)cdiv(n, 256), 256, 0, s, part, parts, n, static_cast<IO *>(db));
@@ -320,8 +342,10 @@ luna_status check(const luna_linear_desc *ld) {
 }
 
 struct Plan {
-    size_t o_part = 256, o_dz, part_fwd, part_bwd, fwd, bwd;
+    size_t o_part = 256, o_dz, o_pad_fwd, o_pad_bwd, pad_fwd = 0, pad_bwd = 0, part_fwd, part_bwd, fwd, bwd;
 };
+
+int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
 
 // Partial products: up to 32 pieces of K of a product with few tiles, at most 64 MiB.
 size_t part_bytes(int64_t M, int64_t N) { return (size_t)std::min<int64_t>(M * N * 4 * 32, int64_t(64) << 20); }
@@ -335,7 +359,17 @@ Plan make_plan(const luna_linear_desc *ld) {
     p.part_bwd = (size_t)align256((int64_t)p.part_bwd);
     p.fwd = p.o_part + p.part_fwd;
     p.o_dz = p.o_part + p.part_bwd;
-    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * ld->n * eb));
+    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * up8(ld->n) * eb));
+    p.o_pad_fwd = p.fwd;
+    p.o_pad_bwd = p.bwd;
+    // bf16 widths that are not multiples of 8: copies of the operands whose rows are 16-byte aligned
+    if (ld->io == LUNA_BF16 && (ld->n % 8 || ld->k % 8)) {
+        const int64_t X = align256(ld->m * up8(ld->k) * 2), W = align256(ld->n * up8(ld->k) * 2);
+        p.pad_fwd = ld->k % 8 ? (size_t)(X + W) : 0;
+        p.pad_bwd = (size_t)(align256(ld->m * up8(ld->n) * 2) + std::max(X, W));  // dz and one of the others at a time
+        p.fwd += p.pad_fwd;
+        p.bwd += p.pad_bwd;
+    }
     return p;
 }
 
@@ -363,6 +397,28 @@ cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, c
     return cudaGetLastError();
 }
 
+// Copies what TMA cannot read of p's operands into p.pad and points p at the copies; false if there is no
+// room (an operand whose width would do, but whose address or leading dimension does not).
+static bool pad_operands(Product &p, cudaStream_t s, cudaError_t *err) {
+    size_t used = 0;
+    *err = cudaSuccess;
+    for (int i = 0; i < 2; ++i) {
+        MatView &v = i ? p.B : p.A;
+        if (al16(v.p) && v.ld % 8 == 0) continue;
+        const int64_t width = v.kt ? (i ? p.N : p.M) : p.K, rows = v.kt ? p.K : (i ? p.N : p.M), ldp = up8(width);
+        const size_t bytes = (size_t)align256(rows * ldp * 2);
+        if (!p.pad || used + bytes > p.pad_bytes) return false;
+        __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(static_cast<char *>(p.pad) + used);
+        used += bytes;
+        LUNA_LAUNCH("pad_rows", k_pad_rows, (unsigned)cdiv(rows * (ldp / 8), 256), 256, 0, s,
+                    static_cast<const __nv_bfloat16 *>(v.p), v.ld, dst, ldp, rows, width);
+        if ((*err = cudaGetLastError()) != cudaSuccess) return false;
+        v.p = dst;
+        v.ld = ldp;
+    }
+    return true;
+}
+
 bool product_rows_ok(const Product &p) { return p.M <= 8 && p.K > 0 && !p.A.kt && !p.B.kt; }
 
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s) {
@@ -373,10 +429,17 @@ cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s)
 }
 
 // Up to eight rows of X the product is a read of W (at m = 8, n = 8192, k = 4096 the fp32 sums take about
-// as long as the bytes); tensor cores take what is aligned beyond that.
+// as long as the bytes); beyond that tensor cores take bf16, if need be from aligned copies of the operands
+// (which cost their bytes twice over; the CUDA-core product would take ten to thirty times the tensor cores').
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
     if (product_rows_ok(p)) return launch_product_rows(p, io, s);
-    return io == LUNA_BF16 && product_tc_ok(p) ? launch_product_tc(p, s) : launch_product_simt(p, io, s);
+    if (io == LUNA_BF16 && p.K >= 1) {
+        Product q = p;
+        cudaError_t e;
+        if (pad_operands(q, s, &e)) return launch_product_tc(q, s);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_product_simt(p, io, s);
 }
 
 }  // namespace luna
@@ -412,6 +475,7 @@ luna_status luna_linear_fwd(const luna_linear_desc *ld, const void *X, const voi
     p.bias = bias; p.act = ld->act; p.R = R; p.Z = Z; p.out = Y;
     p.ldr = ld->ldr ? ld->ldr : ld->n; p.ldz = ld->ldz ? ld->ldz : ld->n; p.ldo = ld->ldy ? ld->ldy : ld->n;
     p.part = reinterpret_cast<float *>(ws + pl.o_part); p.part_bytes = pl.part_fwd;
+    p.pad = pl.pad_fwd ? ws + pl.o_pad_fwd : nullptr; p.pad_bytes = pl.pad_fwd;
     p.status = reinterpret_cast<int *>(ws);
     p.clear = 1;
     return cuda_status(launch_product(p, ld->io, s));
@@ -442,17 +506,18 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     cudaError_t e = cudaSuccess;
     if (act || db) {
         void *dZ = ws + pl.o_dz;
-        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, status, s)
-                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, m, (int)n, ld->act, part, db, status, s);
+        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, status, s)
+                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, status, s);
         if (e != cudaSuccess) return LUNA_ERR_CUDA;
     }
     if (k == 0) return LUNA_OK;
     const void *G = act ? ws + pl.o_dz : dY;
-    const int64_t ldg = act ? n : lddy, ldx = ld->ldx ? ld->ldx : k, ldw = ld->ldw ? ld->ldw : k;
+    const int64_t ldg = act ? up8(n) : lddy, ldx = ld->ldx ? ld->ldx : k, ldw = ld->ldw ? ld->ldw : k;
     Product p;
     memset(&p, 0, sizeof(p));
     p.act = LUNA_LINEAR_NONE;
     p.part = part; p.part_bytes = pl.part_bwd;
+    p.pad = pl.pad_bwd ? ws + pl.o_pad_bwd : nullptr; p.pad_bytes = pl.pad_bwd;
     p.status = status;
     p.clear = !(act || db);
     if (dX) {

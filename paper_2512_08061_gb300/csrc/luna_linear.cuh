@@ -28,6 +28,8 @@ struct Product {
     int64_t ldr, ldz, ldo;
     float *part;           // fp32 partial products [split][M][N]
     size_t part_bytes;
+    void *pad;             // room for copies of operands that TMA cannot read (bf16 with widths that are not
+    size_t pad_bytes;      // multiples of 8), or NULL
     int *status;           // device status word
     int clear;             // first launch of the call: clears it
 };
@@ -103,7 +105,6 @@ cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);    
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
 bool product_rows_ok(const Product &p);                                               // a few rows of X
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s);
-bool product_tc_ok(const Product &p);                                                 // aligned operands
 cudaError_t launch_product_tc(const Product &p, cudaStream_t s);                      // bf16, tensor cores
 cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);
 

@@ -105,6 +105,35 @@ __device__ __forceinline__ void add32(float (&v)[32], const uint4 *p) {
     }
 }
 
+// Element (r, c) of a piece.
+__device__ __forceinline__ __nv_bfloat16 *piece_at(uint8_t *piece, int r, int c) {
+    return reinterpret_cast<__nv_bfloat16 *>(piece + r * 64 + (((c >> 3) ^ ((r >> 1) & 3)) << 4)) + (c & 7);
+}
+
+// The same for outputs that TMA cannot write: the piece's rows one after another, a lane for each column.
+__device__ __forceinline__ void write_piece(uint8_t *piece, __nv_bfloat16 *out, int64_t ld, int rows, int cols,
+                                            const float (&v)[32], int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) *piece_at(piece, lane, i) = __float2bfloat16_rn(v[i]);
+    __syncwarp();
+    if (lane < cols)
+        for (int r = 0; r < rows; ++r) out[r * ld + lane] = *piece_at(piece, r, lane);
+    __syncwarp();
+}
+__device__ __forceinline__ void add_piece(uint8_t *piece, const __nv_bfloat16 *in, int64_t ld, int rows, int cols,
+                                          float (&v)[32], int lane) {
+    __syncwarp();
+    for (int r = 0; r < rows; ++r)
+        if (lane < cols) *piece_at(piece, r, lane) = in[r * ld + lane];
+    __syncwarp();
+    if (lane < rows)
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < cols) v[i] += __bfloat162float(*piece_at(piece, lane, i));
+    __syncwarp();
+}
+
 template <int ACT> __device__ __forceinline__ void act32(float (&v)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = linear_act<__nv_bfloat16>(v[i], ACT);
@@ -244,37 +273,43 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 for (int i = 0; i < 32; ++i) v[i] = last_split_empty ? 0.0f : __uint_as_float(x[i]);
                 const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;  // of the computed product
                 const int w = row < M ? (int)max((int64_t)0, min((int64_t)32, N - col)) : 0;
-                if (a.vec) {  // the whole warp, for its 32 rows
+                if (!a.swap && a.splits == 1) {  // the whole warp, for its 32 rows
                     using B = __nv_bfloat16;
                     const int64_t row0 = row - lane;
                     if (row0 < M && col < N) {
+                        const int rows = (int)min((int64_t)32, M - row0), cols = (int)min((int64_t)32, N - col);
+                        uint8_t *piece = pieces + warp * 4096;
                         if (p.bias) {
-                            if (N - col >= 32) {
+                            if (a.vec && cols == 32) {
                                 add32(v, reinterpret_cast<const uint4 *>(static_cast<const B *>(p.bias) + col));
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (col + i < N) v[i] += io_load(static_cast<const B *>(p.bias) + col + i);
+                                    if (i < cols) v[i] += io_load(static_cast<const B *>(p.bias) + col + i);
                             }
                         }
-                        if (p.Z) store_piece(pieces + warp * 4096 + (stored++ & 1) * 2048, &mapZ, col, row0, v, lane);
+                        if (p.Z) {
+                            if (a.vec) store_piece(piece + (stored++ & 1) * 2048, &mapZ, col, row0, v, lane);
+                            else write_piece(piece, static_cast<B *>(p.Z) + row0 * p.ldz + col, p.ldz, rows, cols, v, lane);
+                        }
                         switch (p.act) {
                             case LUNA_LINEAR_RELU: act32<LUNA_LINEAR_RELU>(v); break;
                             case LUNA_LINEAR_GELU: act32<LUNA_LINEAR_GELU>(v); break;
                             case LUNA_LINEAR_SILU: act32<LUNA_LINEAR_SILU>(v); break;
                             default: break;
                         }
-                        if (p.R && row < M) {
-                            const B *r = static_cast<const B *>(p.R) + row * p.ldr + col;
-                            if (N - col >= 32) {
-                                add32(v, reinterpret_cast<const uint4 *>(r));
-                            } else {
+                        if (p.R) {
+                            if (!a.vec)
+                                add_piece(piece, static_cast<const B *>(p.R) + row0 * p.ldr + col, p.ldr, rows, cols, v, lane);
+                            else if (row < M && cols == 32)
+                                add32(v, reinterpret_cast<const uint4 *>(static_cast<const B *>(p.R) + row * p.ldr + col));
+                            else if (row < M)
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
-                                    if (col + i < N) v[i] += io_load(r + i);
-                            }
+                                    if (i < cols) v[i] += io_load(static_cast<const B *>(p.R) + row * p.ldr + col + i);
                         }
-                        store_piece(pieces + warp * 4096 + (stored++ & 1) * 2048, &mapO, col, row0, v, lane);
+                        if (a.vec) store_piece(piece + (stored++ & 1) * 2048, &mapO, col, row0, v, lane);
+                        else write_piece(piece, static_cast<B *>(p.out) + row0 * p.ldo + col, p.ldo, rows, cols, v, lane);
                     }
                 } else if (w == 0) {
                     // nothing of the row in this chunk
@@ -288,7 +323,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         for (int i = 0; i < 32; ++i)
                             if (i < w) linear_finish<__nv_bfloat16>(p, col + i, row, v[i]);
                     }
-                } else if (a.splits > 1) {
+                } else {
                     float *o = p.part + ((int64_t)sp * p.M + row) * p.N + col;
                     if (w == 32 && p.N % 4 == 0) {
 #pragma unroll
@@ -299,10 +334,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         for (int i = 0; i < 32; ++i)
                             if (i < w) o[i] = v[i];
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (i < w) linear_finish<__nv_bfloat16>(p, row, col + i, v[i]);
                 }
                 __syncwarp();  // the TMEM load of the next chunk is the whole warp's
             }
@@ -403,12 +434,6 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
 }
 
 }  // namespace
-
-bool product_tc_ok(const Product &p) {
-    for (const MatView *v : {&p.A, &p.B})
-        if (!al16(v->p) || v->ld % 8 != 0) return false;
-    return p.K >= 1;
-}
 
 cudaError_t launch_product_tc(const Product &p, cudaStream_t s) {
     ProductTc a;

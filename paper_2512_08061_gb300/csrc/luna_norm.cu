@@ -35,7 +35,7 @@ struct Limits {
     int threads, resident;
 };
 constexpr Limits limits(int vec, int nv, bool backward) {
-    if (vec == 1) return nv == 4 ? Limits{256, backward ? 512 : 1024} : nv == 8 ? Limits{512, 512} : Limits{1024, 1024};
+    if (vec == 1) return nv == 4 ? Limits{256, backward ? 512 : 1024} : Limits{512, 512};
     if (nv == 1) return backward ? Limits{512, 512} : Limits{256, 1024};
     if (nv == 2) return backward ? Limits{512, 512} : Limits{256, 512};
     return Limits{kMaxCols / vec / nv, kMaxCols / vec / nv};
@@ -704,7 +704,7 @@ Shape shape_of(int cols, bool vectors, int vec_io, bool backward) {
     s.vec = vectors ? vec_io : 1;
     const int nvec = cols / s.vec;
     s.nv = vectors ? 1 : 4;
-    while (s.nv < (vectors ? 4 : 16) && nvec > s.nv * limits(s.vec, s.nv, backward).threads) s.nv *= 2;
+    while (s.nv < (vectors ? 4 : 32) && nvec > s.nv * limits(s.vec, s.nv, backward).threads) s.nv *= 2;
     s.threads = ((nvec + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.rows_per_block = s.threads == 32 ? 8 : 1;
     s.blocks = 152 * std::max(1, limits(s.vec, s.nv, backward).resident / (s.threads * s.rows_per_block));
@@ -766,7 +766,8 @@ cudaError_t fwd(NormArgs a, cudaStream_t s) {
     }
     if (sh.nv == 4) return fwd_launch<IO, 1, 4>(a, sh, s);
     if (sh.nv == 8) return fwd_launch<IO, 1, 8>(a, sh, s);
-    return fwd_launch<IO, 1, 16>(a, sh, s);
+    if (sh.nv == 16) return fwd_launch<IO, 1, 16>(a, sh, s);
+    return fwd_launch<IO, 1, 32>(a, sh, s);
 }
 
 template <typename IO, int VEC, int NV, bool BIAS>
@@ -791,7 +792,8 @@ cudaError_t bwd(NormArgs a, float *const (&out)[4], cudaStream_t s) {
     } else {
         if (sh.nv == 4) e = bwd_launch<IO, 1, 4, BIAS>(a, sh, grid, s);
         else if (sh.nv == 8) e = bwd_launch<IO, 1, 8, BIAS>(a, sh, grid, s);
-        else e = bwd_launch<IO, 1, 16, BIAS>(a, sh, grid, s);
+        else if (sh.nv == 16) e = bwd_launch<IO, 1, 16, BIAS>(a, sh, grid, s);
+        else e = bwd_launch<IO, 1, 32, BIAS>(a, sh, grid, s);
     }
     if (e != cudaSuccess || !a.part) return e;
     NormSum n{a.part, {out[0], out[1], out[2], out[3]}, grid * sh.rows_per_block, BIAS ? 4 : 2, a.cols};
