@@ -5,10 +5,12 @@
 #include "luna_decay.cuh"
 #include "luna_prof.cuh"
 
+#include <string.h>
+
 namespace luna {
 namespace {
 
-constexpr int kCh = kDecaySimtRows;
+
 constexpr int kMixThreads = 256;
 constexpr int kCols = 32;      // state columns of a block of the single-token step
 
@@ -48,20 +50,21 @@ __device__ __forceinline__ void store4(OUT *p, int c, int width, bool vec, const
 // outputs, DA / 16 x DC / 16 of the state, which stays in registers and is copied to shared memory for
 // the outputs), 16-byte reads without bank conflicts, two multiply-adds an instruction.  Bound by the
 // fp32 FMA rate at width 128, by the loads' latency at small widths, where two blocks share an SM.
-template <typename IO, typename OUT, int DA, int DC>
+// CH: rows of a chunk, 64, or 16 where no sequence is longer than that.
+template <typename IO, typename OUT, int DA, int DC, int CH>
 __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_mix(DecayMix a) {
     extern __shared__ float4 sm4[];
     clear_status(a);
-    constexpr int LA = DA + 4, LC = DC + 4, LP = kCh + 4, FT = DA / 64, CT = DC / 64;
-    float *sa = reinterpret_cast<float *>(sm4), *sb = sa + kCh * LA, *sc = sb + kCh * LA, *sP = sc + kCh * LC;
-    float *sX = sP + kCh * LP, *pw = sX + DA * LC;
+    constexpr int LA = DA + 4, LC = DC + 4, LP = CH + 4, RT = CH / 16, FT = DA / 64, CT = DC / 64;
+    float *sa = reinterpret_cast<float *>(sm4), *sb = sa + CH * LA, *sc = sb + CH * LA, *sP = sc + CH * LC;
+    float *sX = sP + CH * LP, *pw = sX + DA * LC;
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
     const int seg = (int)(blockIdx.x % a.nseg);
     const int64_t bh = blockIdx.x / a.nseg;
     const int b = (int)(bh / a.H), h = (int)(bh % a.H);
     const int e = a.reverse ? 0 : 1;
     const float g = decay_log(a.log_decay, h);
-    for (int i = tid; i <= kCh; i += kMixThreads) pw[i] = expf(g * (float)i);
+    for (int i = tid; i <= CH; i += kMixThreads) pw[i] = expf(g * (float)i);
     const int len = head_length(a.lengths, b, a.n);
     const int r0 = seg * a.seg_len, rend = min(a.n, r0 + a.seg_len);
     const int r1 = max(r0, min(len, rend));
@@ -85,13 +88,13 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
             }
     }
     const int na = (a.da + 3) / 4, nc = (a.dc + 3) / 4;  // float4 pieces of a row
-    const int nch = (r1 - r0 + kCh - 1) / kCh;
+    const int nch = (r1 - r0 + CH - 1) / CH;
     for (int ci = 0; ci < nch; ++ci) {
-        const int row0 = r0 + (a.reverse ? nch - 1 - ci : ci) * kCh;
-        const int nv = min(kCh, r1 - row0);
+        const int row0 = r0 + (a.reverse ? nch - 1 - ci : ci) * CH;
+        const int nv = min(CH, r1 - row0);
         __syncthreads();
         // the pieces of b, c and (where outputs are wanted) a, eight loads of a thread in flight
-        const int nb = kCh * na, total = nb + kCh * nc + (O ? nb : 0);
+        const int nb = CH * na, total = nb + CH * nc + (O ? nb : 0);
 #pragma unroll 1
         for (int i0 = tid; i0 < total; i0 += 8 * kMixThreads) {
             float4 v[8];
@@ -99,10 +102,10 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 int i = i0 + q * kMixThreads;
-                const bool is_b = i < nb, is_c = !is_b && i < nb + kCh * nc;
+                const bool is_b = i < nb, is_c = !is_b && i < nb + CH * nc;
                 const int per = is_c ? nc : na;
                 to[q] = i < total ? (is_b ? sb : is_c ? sc : sa) : nullptr;
-                i -= is_b ? 0 : is_c ? nb : nb + kCh * nc;
+                i -= is_b ? 0 : is_c ? nb : nb + CH * nc;
                 const int r = i / per, c = 4 * (i % per);
                 const RowView &w = is_b ? a.b : is_c ? a.c : a.a;
                 const IO *p = is_b ? Bm : is_c ? Cm : A;
@@ -127,31 +130,31 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
         __syncthreads();
         if (O) {
             {  // scores of rows ty + 16 i, columns tx + 16 j
-                uint64_t acc[4][4];  // two partial sums each
+                uint64_t acc[RT][RT];  // two partial sums each
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+                    for (int j = 0; j < RT; ++j) acc[i][j] = 0;
 #pragma unroll 2
                 for (int k = 0; k < na; ++k) {
-                    float4 u[4], v[4];
+                    float4 u[RT], v[RT];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < RT; ++i) {
                         u[i] = *reinterpret_cast<const float4 *>(sa + (ty + 16 * i) * LA + 4 * k);
                         v[i] = *reinterpret_cast<const float4 *>(sb + (tx + 16 * i) * LA + 4 * k);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < RT; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
+                        for (int j = 0; j < RT; ++j) {
                             acc[i][j] = fma2(f2(u[i].x, u[i].y), f2(v[j].x, v[j].y), acc[i][j]);
                             acc[i][j] = fma2(f2(u[i].z, u[i].w), f2(v[j].z, v[j].w), acc[i][j]);
                         }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < RT; ++j) {
                         const int r = ty + 16 * i, c = tx + 16 * j, dist = a.reverse ? c - r : r - c;
                         float lo, hi;
                         unpack2(acc[i][j], lo, hi);
@@ -159,25 +162,25 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
                     }
             }
             __syncthreads();
-            uint64_t out[4][2 * CT];  // rows ty + 16 i, columns 4 tx + 64 j + l in pairs
+            uint64_t out[RT][2 * CT];  // rows ty + 16 i, columns 4 tx + 64 j + l in pairs
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
                 for (int j = 0; j < 2 * CT; ++j) out[i][j] = 0;
             // out (+)= left (rows of lda) times right (rows of LC), over n pieces of four
             auto product = [&](const float *left, int lda, const float *right, int n) {
 #pragma unroll 1
                 for (int k = 0; k < n; ++k) {
-                    float4 u[4];
+                    float4 u[RT];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const float4 *>(left + (ty + 16 * i) * lda + 4 * k);
+                    for (int i = 0; i < RT; ++i) u[i] = *reinterpret_cast<const float4 *>(left + (ty + 16 * i) * lda + 4 * k);
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
 #pragma unroll
                         for (int j = 0; j < CT; ++j) {
                             const float4 v = *reinterpret_cast<const float4 *>(right + (4 * k + q) * LC + 4 * tx + 64 * j);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
+                            for (int i = 0; i < RT; ++i) {
                                 const float w = q == 0 ? u[i].x : q == 1 ? u[i].y : q == 2 ? u[i].z : u[i].w;
                                 out[i][2 * j] = fma2(f2(w, w), f2(v.x, v.y), out[i][2 * j]);
                                 out[i][2 * j + 1] = fma2(f2(w, w), f2(v.z, v.w), out[i][2 * j + 1]);
@@ -187,15 +190,15 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
             };
             product(sa, LA, sX, na);  // (a's columns past da are zeros to a whole piece, and so are X's rows)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < RT; ++i) {
                 const int r = ty + 16 * i;
-                const float w = a.x * pw[max(0, a.reverse ? nv - 1 - r : min(r, kCh - 1)) + e];
+                const float w = a.x * pw[max(0, a.reverse ? nv - 1 - r : min(r, CH - 1)) + e];
 #pragma unroll
                 for (int j = 0; j < 2 * CT; ++j) out[i][j] = mul2(out[i][j], f2(w, w));
             }
-            product(sP, LP, sc, kCh / 4);
+            product(sP, LP, sc, CH / 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < RT; ++i) {
                 const int r = ty + 16 * i;
                 if (r < nv)
 #pragma unroll
@@ -269,20 +272,33 @@ __global__ void __launch_bounds__(256) k_decay_scan(DecayScan a) {
     if (a.last) a.last[bh * a.E + i] = x;
 }
 
+// Four columns a thread; bound by the bytes of src.
 template <typename IO>
 __global__ void __launch_bounds__(256) k_decay_group_sum(const float *src, int H, int G, int n, int width, IO *dst,
-                                                         int64_t sb, int64_t sh, int64_t st, int64_t total) {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= total) return;
-    const int w = (int)(i % width);
-    const int64_t row = i / width;
-    const int t = (int)(row % n);
-    const int64_t bk = row / n;
-    const int Hk = H / G, b = (int)(bk / Hk), hk = (int)(bk % Hk);
-    const float *p = src + (((int64_t)b * H + (int64_t)hk * G) * n + t) * width + w;
-    float acc = 0.0f;
-    for (int j = 0; j < G; ++j) acc += p[(int64_t)j * n * width];
-    io_store(dst + b * sb + (int64_t)hk * sh + (int64_t)t * st + w, acc);
+                                                         int64_t sb, int64_t sh, int64_t st) {
+    const int per = (width + 3) / 4, Hk = H / G, b = blockIdx.x / Hk, hk = blockIdx.x % Hk;
+    const float *head = src + ((int64_t)b * H + (int64_t)hk * G) * n * width;
+    IO *out = dst + b * sb + (int64_t)hk * sh;
+    const bool vec = width % 4 == 0 && st % 4 == 0 && sb % 4 == 0 && sh % 4 == 0 && reinterpret_cast<uintptr_t>(dst) % 16 == 0;
+    const int total = n * per;  // under 2^29
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < total; i += gridDim.y * 256) {
+        const int t = i / per, c = (i - t * per) * 4;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < G; ++j) {
+            const float4 v = load4<float>(head + ((int64_t)j * n + t) * width, c, width, width % 4 == 0);
+            acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
+        }
+        IO *o = out + (int64_t)t * st;
+        if (vec && sizeof(IO) == 2) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0], acc[1]), hi = __floats2bfloat162_rn(acc[2], acc[3]);
+            uint2 w;
+            memcpy(&w.x, &lo, 4);
+            memcpy(&w.y, &hi, 4);
+            *reinterpret_cast<uint2 *>(o + c) = w;
+        } else {
+            store4<IO>(o, c, width, vec, acc);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -382,14 +398,20 @@ __global__ void __launch_bounds__(kStepThreads) k_decay_step(DecayStep a) {
 
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-template <typename IO, typename OUT, int DA, int DC>
+template <typename IO, typename OUT, int DA, int DC, int CH>
 cudaError_t mix_launch(const DecayMix &a, cudaStream_t s) {
-    const size_t smem = sizeof(float) * (2 * kCh * (DA + 4) + kCh * (DC + 4) + kCh * (kCh + 4) + DA * (DC + 4) + kCh + 4);
-    cudaError_t e = cudaFuncSetAttribute(k_decay_mix<IO, OUT, DA, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const size_t smem = sizeof(float) * (2 * CH * (DA + 4) + CH * (DC + 4) + CH * (CH + 4) + DA * (DC + 4) + CH + 4);
+    cudaError_t e = cudaFuncSetAttribute(k_decay_mix<IO, OUT, DA, DC, CH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nseg);
-    LUNA_LAUNCH("decay_mix", (k_decay_mix<IO, OUT, DA, DC>), grid, kMixThreads, smem, s, a);
+    LUNA_LAUNCH("decay_mix", (k_decay_mix<IO, OUT, DA, DC, CH>), grid, kMixThreads, smem, s, a);
     return cudaGetLastError();
+}
+
+template <typename IO, typename OUT, int CH>
+cudaError_t mix_width(const DecayMix &a, cudaStream_t s) {
+    if (a.da <= 64) return a.dc <= 64 ? mix_launch<IO, OUT, 64, 64, CH>(a, s) : mix_launch<IO, OUT, 64, 128, CH>(a, s);
+    return a.dc <= 64 ? mix_launch<IO, OUT, 128, 64, CH>(a, s) : mix_launch<IO, OUT, 128, 128, CH>(a, s);
 }
 
 template <typename IO, typename OUT>
@@ -400,8 +422,7 @@ cudaError_t mix(DecayMix a, cudaStream_t s) {
     };
     for (RowView *v : {&a.a, &a.b, &a.c}) v->vec = quad(v->p, v->sb, v->sh, v->st, sizeof(IO));
     a.ovec = quad(a.out, a.ob, a.oh, a.ot, sizeof(OUT));
-    if (a.da <= 64) return a.dc <= 64 ? mix_launch<IO, OUT, 64, 64>(a, s) : mix_launch<IO, OUT, 64, 128>(a, s);
-    return a.dc <= 64 ? mix_launch<IO, OUT, 128, 64>(a, s) : mix_launch<IO, OUT, 128, 128>(a, s);
+    return a.n <= 16 ? mix_width<IO, OUT, 16>(a, s) : mix_width<IO, OUT, kDecaySimtRows>(a, s);
 }
 
 }  // namespace
@@ -419,14 +440,14 @@ cudaError_t launch_decay_scan(const DecayScan &a, cudaStream_t s) {
 
 cudaError_t launch_decay_group_sum(const float *src, int B, int H, int G, int n, int width, void *dst, int64_t sb,
                                    int64_t sh, int64_t st, luna_dtype io, cudaStream_t s) {
-    const int64_t total = (int64_t)B * (H / G) * n * width;
-    const unsigned grid = (unsigned)cdiv(total, 256);
+    const int64_t blocks = ((int64_t)n * ((width + 3) / 4) + 255) / 256;
+    const dim3 grid((unsigned)(B * (H / G)), (unsigned)(blocks < 4096 ? blocks : 4096));
     if (io == LUNA_F32)
         LUNA_LAUNCH("decay_group_sum", k_decay_group_sum<float>, grid, 256, 0, s, src, H, G, n, width,
-                    static_cast<float *>(dst), sb, sh, st, total);
+                    static_cast<float *>(dst), sb, sh, st);
     else
         LUNA_LAUNCH("decay_group_sum", k_decay_group_sum<__nv_bfloat16>, grid, 256, 0, s, src, H, G, n, width,
-                    static_cast<__nv_bfloat16 *>(dst), sb, sh, st, total);
+                    static_cast<__nv_bfloat16 *>(dst), sb, sh, st);
     return cudaGetLastError();
 }
 

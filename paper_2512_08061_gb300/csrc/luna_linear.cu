@@ -62,11 +62,25 @@ __device__ __forceinline__ void store_vec(IO *p, const float (&v)[VEC]) {
     }
 }
 
+// Four consecutive values as fp32.
+template <typename IO>
+__device__ __forceinline__ void load_quad(const IO *p, float (&v)[4]) {
+    if (sizeof(IO) == 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(p);
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else {
+        const uint2 w = *reinterpret_cast<const uint2 *>(p);
+        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+    }
+}
+
 // 128 x 128 tile of A B^T over one piece of K: operands staged in shared memory 16 deep, eight by
 // eight sums a thread in fp32, two multiply-adds an instruction, the next step's values loaded while this one's are multiplied.
 // Bound by the fp32 FMA rate.
-template <typename IO>
-__global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, int splits) {
+// QUAD: loads of four values along the contiguous dimension (rows on their boundaries).
+template <typename IO, bool QUAD>
+__global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t depth, int splits) {
     __shared__ __align__(16) float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
     clear_status(p.clear, p.status);
@@ -78,32 +92,47 @@ __global__ void __launch_bounds__(kThreads) k_product(Product p, int64_t depth, 
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = 0;
     float ra[8], rb[8];
-    // element i of a thread: along the contiguous dimension of each operand
+    constexpr int W = QUAD ? 4 : 1;  // values of a load
+    // load i of a thread, along the contiguous dimension of each operand: its first row and depth in the tile
     auto place = [&](bool kt, int i, int &r, int &k) {
         const int e = tid + i * kThreads;
-        if (kt) { r = e % kT; k = e / kT; } else { k = e % kK; r = e / kK; }
+        if (kt) { r = e % (kT / W) * W; k = e / (kT / W); } else { k = e % (kK / W) * W; r = e / (kK / W); }
+    };
+    auto fetch_one = [&](const MatView &v, int64_t base, int64_t rows, int64_t kb, float (&out)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8 / W; ++i) {
+            int r, k;
+            place(v.kt, i, r, k);
+            if (QUAD) {  // (four rows or four depths are in or out together)
+                const bool in = base + r < rows && kb + k < k1;
+                const IO *q = static_cast<const IO *>(v.p) + (v.kt ? (kb + k) * v.ld + base + r : (base + r) * v.ld + kb + k);
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+                if (in) load_quad<IO>(q, x);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[(4 * i + j) % 8] = x[j];
+            } else {
+                out[i % 8] = at<IO>(v, base + r, rows, kb + k, k1);
+            }
+        }
+    };
+    auto put_one = [&](const MatView &v, float (&tile)[kK][kT + 4], const float (&in)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8 / W; ++i) {
+            int r, k;
+            place(v.kt, i, r, k);
+#pragma unroll
+            for (int j = 0; j < W; ++j) tile[k + (v.kt ? 0 : j)][r + (v.kt ? j : 0)] = in[(W * i + j) % 8];
+        }
     };
     auto fetch = [&](int64_t kb) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int r, k;
-            place(p.A.kt, i, r, k);
-            ra[i] = at<IO>(p.A, row0 + r, p.M, kb + k, k1);
-            place(p.B.kt, i, r, k);
-            rb[i] = at<IO>(p.B, col0 + r, p.N, kb + k, k1);
-        }
+        fetch_one(p.A, row0, p.M, kb, ra);
+        fetch_one(p.B, col0, p.N, kb, rb);
     };
     fetch(k0);
     for (int64_t kb = k0; kb < k1; kb += kK) {
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int r, k;
-            place(p.A.kt, i, r, k);
-            sA[k][r] = ra[i];
-            place(p.B.kt, i, r, k);
-            sB[k][r] = rb[i];
-        }
+        put_one(p.A, sA, ra);
+        put_one(p.B, sB, rb);
         __syncthreads();
         if (kb + kK < k1) fetch(kb + kK);
 #pragma unroll
@@ -281,7 +310,14 @@ cudaError_t simt(const Product &p, cudaStream_t s) {
     const int splits = linear_splits(p, gx * gy, 64);  // (a step of 16 takes about a microsecond when alone)
     const int64_t depth = std::max<int64_t>(1, cdiv(cdiv(p.K, splits), kK)) * kK;
     const int used = (int)std::max<int64_t>(1, cdiv(p.K, depth));
-    LUNA_LAUNCH("product", k_product<IO>, dim3((unsigned)gx, (unsigned)gy, used), kThreads, 0, s, p, depth, used);
+    auto quad = [](const MatView &v, int64_t rows, int64_t K) {
+        return reinterpret_cast<uintptr_t>(v.p) % (4 * sizeof(IO)) == 0 && v.ld % 4 == 0 && (v.kt ? rows : K) % 4 == 0;
+    };
+    const dim3 grid((unsigned)gx, (unsigned)gy, used);
+    if (quad(p.A, p.M, p.K) && quad(p.B, p.N, p.K))
+        LUNA_LAUNCH("product", (k_product<IO, true>), grid, kThreads, 0, s, p, depth, used);
+    else
+        LUNA_LAUNCH("product", (k_product<IO, false>), grid, kThreads, 0, s, p, depth, used);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || used == 1) return e;
     return launch_product_finish(p, used, IOType<IO>::code, s);
