@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
     __shared__ __align__(16) float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
     clear_status(p.clear, p.status);
+    if (p.flags && !flagged(p)) return;
     const int64_t row0 = (int64_t)blockIdx.x * kT, col0 = (int64_t)blockIdx.y * kT;
     const int64_t k0 = (int64_t)blockIdx.z * depth, k1 = min(p.K, k0 + depth);
     uint64_t acc[8][4];  // pairs of columns
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
 template <typename IO>
 __global__ void __launch_bounds__(256) k_product_finish(Product p, int splits) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, MN = p.M * p.N;
+    if (p.flags && flagged(p)) return;
     if (i >= MN) return;
     float acc = 0.0f;
 #pragma unroll 8
@@ -291,6 +293,55 @@ __global__ void __launch_bounds__(256) k_pad_rows(const __nv_bfloat16 *src, int6
     *reinterpret_cast<uint4 *>(dst + r * ldp + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// An fp32 operand as three bf16 planes, x = x0 + x1 + x2: each takes the upper eight bits of what the last
+// one left, cut off, not rounded (a value near the largest stays finite), and the third takes the rest.
+// Rows (of K where the operand is stored k x rows) and columns that only fill up to whole slices are zeros.
+// An infinity or a NaN sets the block's flag: its planes' products would be NaN where the product is not.
+struct Split {
+    const float *src;
+    int64_t ld, rows, cols;           // as stored
+    __nv_bfloat16 *dst;
+    int64_t ldp, prow, pcol, plane;   // rows and columns (a multiple of 8) to write, from plane to plane
+    bool vec;                         // 16-byte loads
+};
+__global__ void __launch_bounds__(256) k_split(Split a, Split b, int *flags, int clear, int *status) {
+    const Split &v = blockIdx.y ? b : a;
+    clear_status(clear, status);
+    const uint32_t per = (uint32_t)(v.pcol / 8);
+    const int64_t total = v.prow * per;
+    int bad = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = total >> 32 ? i / per : (int64_t)((uint32_t)i / per), c = (i - r * per) * 8;
+        float x[8];
+        const float *p = v.src + r * v.ld + c;
+        if (v.vec && r < v.rows && c + 8 <= v.cols) {
+            const float4 lo = reinterpret_cast<const float4 *>(p)[0], hi = reinterpret_cast<const float4 *>(p)[1];
+            x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
+            x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = r < v.rows && c + k < v.cols ? p[k] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bad |= (__float_as_uint(x[k]) & 0x7f800000u) == 0x7f800000u;
+        __nv_bfloat16 *o = v.dst + r * v.ldp + c;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t lo = __float_as_uint(x[2 * k]) & 0xffff0000u, hi = __float_as_uint(x[2 * k + 1]) & 0xffff0000u;
+                w[k] = lo >> 16 | hi;
+                x[2 * k] -= __uint_as_float(lo);
+                x[2 * k + 1] -= __uint_as_float(hi);
+            }
+            *reinterpret_cast<uint4 *>(o + q * v.plane) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) flags[blockIdx.y * kFlagBlocks + blockIdx.x] = bad;
+}
+
 template <typename IO>
 __global__ void __launch_bounds__(256) k_linear_db(const float *part, int parts, int n, IO *db) {
     const int c = blockIdx.x * 256 + threadIdx.x;
@@ -307,7 +358,7 @@ luna_status cuda_status(cudaError_t e) { return e == cudaSuccess ? LUNA_OK : LUN
 template <typename IO>
 cudaError_t simt(const Product &p, cudaStream_t s) {
     const int64_t gx = cdiv(p.M, kT), gy = cdiv(p.N, kT);
-    const int splits = linear_splits(p, gx * gy, 64);  // (a step of 16 takes about a microsecond when alone)
+    const int splits = p.flags ? 1 : linear_splits(p, gx * gy, 64);  // (a step of 16 takes about a microsecond when alone)
     const int64_t depth = std::max<int64_t>(1, cdiv(cdiv(p.K, splits), kK)) * kK;
     const int used = (int)std::max<int64_t>(1, cdiv(p.K, depth));
     auto quad = [](const MatView &v, int64_t rows, int64_t K) {
@@ -386,6 +437,23 @@ int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
 // Partial products: up to 32 pieces of K of a product with few tiles, at most 64 MiB.
 size_t part_bytes(int64_t M, int64_t N) { return (size_t)std::min<int64_t>(M * N * 4 * 32, int64_t(64) << 20); }
 
+int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+
+// Whether an fp32 product is taken to tensor cores in bf16 planes: estimated microseconds of both ways.  The
+// CUDA cores carry 35 TFLOP/s in whole tiles; the planes take three launches, 16 bytes a value of the operands
+// and six products at 1 PFLOP/s.
+bool planes_pay(int64_t M, int64_t N, int64_t K) {
+    const double macs = (double)M * N * K;
+    const double simt = 2.0 * (double)(cdiv(M, kT) * kT) * (double)(cdiv(N, kT) * kT) * K / 35e6;
+    return M > 8 && K > 0 && simt > 12.0 + 12.0 * macs / 1e9 + 16.0 * (double)(M + N) * K / 4e6;
+}
+// Bytes of the planes of an operand of `rows` rows.
+int64_t plane_bytes(int64_t rows, int64_t K, bool kt) { return align256(3 * up64(K) * (kt ? up8(rows) : rows) * 2); }
+constexpr int64_t kFlagBytes = 2 * kFlagBlocks * sizeof(int) / 256 * 256 + 256;
+int64_t planes_room(int64_t M, int64_t N, int64_t K, bool akt, bool bkt) {
+    return planes_pay(M, N, K) ? kFlagBytes + plane_bytes(M, K, akt) + plane_bytes(N, K, bkt) : 0;
+}
+
 Plan make_plan(const luna_linear_desc *ld) {
     Plan p;
     const int64_t eb = ld->io == LUNA_F32 ? 4 : 2;
@@ -403,6 +471,12 @@ Plan make_plan(const luna_linear_desc *ld) {
         const int64_t X = align256(ld->m * up8(ld->k) * 2), W = align256(ld->n * up8(ld->k) * 2);
         p.pad_fwd = ld->k % 8 ? (size_t)(X + W) : 0;
         p.pad_bwd = (size_t)(align256(ld->m * up8(ld->n) * 2) + std::max(X, W));  // dz and one of the others at a time
+        p.fwd += p.pad_fwd;
+        p.bwd += p.pad_bwd;
+    }
+    if (ld->io == LUNA_F32) {  // fp32 operands in three bf16 planes
+        p.pad_fwd = (size_t)planes_room(ld->m, ld->n, ld->k, false, false);
+        p.pad_bwd = (size_t)std::max(planes_room(ld->m, ld->k, ld->n, false, true), planes_room(ld->n, ld->k, ld->m, true, true));
         p.fwd += p.pad_fwd;
         p.bwd += p.pad_bwd;
     }
@@ -455,6 +529,36 @@ static bool pad_operands(Product &p, cudaStream_t s, cudaError_t *err) {
     return true;
 }
 
+// The operands of p into three planes each in p.pad; p then points at them.
+static cudaError_t split_operands(Product &p, cudaStream_t s) {
+    int *flags = static_cast<int *>(p.pad);
+    char *to = static_cast<char *>(p.pad) + kFlagBytes;
+    Split sp[2];
+    for (int i = 0; i < 2; ++i) {
+        MatView &v = i ? p.B : p.A;
+        Split &q = sp[i];
+        const int64_t rows = i ? p.N : p.M, Kp = up64(p.K);
+        q.src = static_cast<const float *>(v.p);
+        q.ld = v.ld;
+        q.rows = v.kt ? p.K : rows;
+        q.cols = v.kt ? rows : p.K;
+        q.dst = reinterpret_cast<__nv_bfloat16 *>(to);
+        q.prow = v.kt ? Kp : rows;
+        q.pcol = v.kt ? up8(rows) : Kp;
+        q.ldp = v.kt ? q.pcol : 3 * Kp;
+        q.plane = v.kt ? Kp * q.ldp : Kp;
+        q.vec = al16(v.p) && v.ld % 4 == 0;
+        to += plane_bytes(rows, p.K, v.kt);
+        v.p = q.dst;
+        v.ld = q.ldp;
+    }
+    LUNA_LAUNCH("split", k_split, dim3(kFlagBlocks, 2), 256, 0, s, sp[0], sp[1], flags, p.clear, p.status);
+    p.clear = 0;
+    p.flags = flags;
+    p.n_flags = 2 * kFlagBlocks;
+    return cudaGetLastError();
+}
+
 bool product_rows_ok(const Product &p) { return p.M <= 8 && p.K > 0 && !p.A.kt && !p.B.kt; }
 
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s) {
@@ -472,8 +576,20 @@ cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
     if (io == LUNA_BF16 && p.K >= 1) {
         Product q = p;
         cudaError_t e;
-        if (pad_operands(q, s, &e)) return launch_product_tc(q, s);
+        if (pad_operands(q, s, &e)) return launch_product_tc(q, io, s);
         if (e != cudaSuccess) return e;
+    }
+    if (io == LUNA_F32 && planes_pay(p.M, p.N, p.K) &&
+        p.pad_bytes >= (size_t)planes_room(p.M, p.N, p.K, p.A.kt, p.B.kt)) {
+        Product q = p;
+        cudaError_t e = split_operands(q, s);
+        if (e == cudaSuccess) e = launch_product_tc(q, io, s);
+        if (e != cudaSuccess) return e;
+        Product r = p;  // takes the product if an operand holds an infinity or a NaN
+        r.clear = 0;
+        r.flags = q.flags;
+        r.n_flags = q.n_flags;
+        return launch_product_simt(r, io, s);
     }
     return launch_product_simt(p, io, s);
 }

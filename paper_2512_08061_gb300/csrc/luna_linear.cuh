@@ -32,7 +32,19 @@ struct Product {
     size_t pad_bytes;      // multiples of 8), or NULL
     int *status;           // device status word
     int clear;             // first launch of the call: clears it
+    const int *flags;      // n_flags words of which one is set where an fp32 operand holds an infinity or a
+    int n_flags;           // NaN (or NULL): the tensor-core kernel then leaves the product to the other one
 };
+
+constexpr int kFlagBlocks = 304;  // blocks that look at an operand, a word for each
+
+// One of p's flags is set; for the whole block.
+__device__ __forceinline__ bool flagged(const Product &p) {
+    int f = 0;
+    if (p.flags)
+        for (int i = threadIdx.x; i < p.n_flags; i += blockDim.x) f |= p.flags[i];
+    return __syncthreads_or(f) != 0;
+}
 
 // The first block of a call's first kernel clears the status word; the waits that set it run for a second.
 __device__ __forceinline__ void clear_status(int clear, int *status) {
@@ -105,7 +117,8 @@ cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);    
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
 bool product_rows_ok(const Product &p);                                               // a few rows of X
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s);
-cudaError_t launch_product_tc(const Product &p, cudaStream_t s);                      // bf16, tensor cores
+// On tensor cores: bf16 operands, or with LUNA_F32 operands in three bf16 planes along K (see k_split).
+cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s);
 cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);
 
 }  // namespace luna

@@ -13,6 +13,12 @@
 // of both.  TMA zero-fills past every edge and drops what a store holds past it.  The epilogue's warps
 // hand 32 x 32 pieces to TMA stores (a lane's own row, written directly, would touch 32 lines an
 // instruction: 20 to 40 % of the whole product at a depth of 1024).
+//
+// fp32 operands come as three bf16 planes, x = x0 + x1 + x2 exactly (eight bits each), and a b is the sum
+// of the six products a2 b0 + a1 b1 + a0 b2 + a1 b0 + a0 b1 + a0 b0; what is left out is under 2^-21 of
+// |a| |b|.  The tensor cores add to their fp32 accumulator by cutting off, which at a depth of 1024 has
+// lost 1.7e-6 of a sum of positive products and at 256 3e-7 (measured), so after every 256 of K the
+// epilogue's warps add the accumulator to an fp32 sum that they keep in TMEM beside it.
 #include "luna_linear.cuh"
 
 #include <algorithm>
@@ -32,13 +38,14 @@ using namespace sm100;
 constexpr int kEpiWarps = 8, kWarpTma = 8, kWarpMma = 9, kTcThreads = 320;
 constexpr int kDepth = 64;  // K of a stage
 
-template <int CG, int BN> struct Tile {
+template <typename IO, int CG, int BN> struct Tile {
+    static constexpr bool PLANES = sizeof(IO) == 4;   // fp32 operands in three bf16 planes
     static constexpr int BM = 128;                    // rows of a CTA
     static constexpr int NB = BN / CG;                // B rows a CTA holds
     static constexpr int NBL = NB < 64 ? 64 : NB;     // ... and loads (an MN-major slice is 64 wide)
     static constexpr uint32_t A_BYTES = BM * 128, B_BYTES = NBL * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = (int)((192 * 1024) / STAGE) > 8 ? 8 : (int)((192 * 1024) / STAGE);
-    static constexpr uint32_t COLS = 2 * BN;          // two accumulators
+    static constexpr uint32_t COLS = PLANES ? 4 * BN : 2 * BN;  // two accumulators (and the fp32 sum)
     static constexpr uint32_t OUT = kEpiWarps * 4096;   // two 32 x 32 pieces of every epilogue warp
     static constexpr uint32_t SMEM = STAGES * STAGE + OUT + 1024 + 256;
     static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -47,6 +54,7 @@ template <int CG, int BN> struct Tile {
 struct ProductTc {
     Product p;
     int tiles_m, tiles_n, splits, k_steps, steps_per_split;  // tiles of BM * CG rows, BN columns
+    int per;        // 64-deep slices of an operand (of each plane of it)
     bool swap;      // the product is computed transposed: A = the layer's B (few rows of X)
     bool vec;       // outputs and residual on 16-byte boundaries: the epilogue stores by TMA
 };
@@ -71,80 +79,121 @@ __device__ __forceinline__ void unit_tile(const ProductTc &a, int u, int &tm, in
     tn = r / rows;
 }
 
-// 32 columns of a lane's row into the warp's piece (64-byte rows, swizzled) and on to the output's rows
-// row0 .. row0 + 31.  `piece` alternates between two.
-__device__ __forceinline__ void store_piece(uint8_t *piece, const CUtensorMap *map, int64_t col, int64_t row0,
-                                            const float (&v)[32], int lane) {
-    if (lane == 0) bulk_wait_read_but_one();
-    __syncwarp();
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<uint4 *>(piece + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
-            make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]), pack2(v[8 * q + 4], v[8 * q + 5]),
-                       pack2(v[8 * q + 6], v[8 * q + 7]));
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-        tma_store_2d(map, piece, (int)col, (int)row0);
-        bulk_commit();
+// Slice s of the walk over K.  Of fp32 operands: 256 of K at a time, the six products one after another,
+// the small ones first.
+constexpr int kSegment = 4, kTerms = 6;  // slices of a plane, products
+template <bool PLANES>
+__device__ __forceinline__ void slice_of(int s, int per, int &xa, int &xb) {
+    if (!PLANES) {
+        xa = xb = s * kDepth;
+    } else {
+        const int seg = s / (kSegment * kTerms), r = s - seg * kSegment * kTerms, n = min(kSegment, per - seg * kSegment);
+        const int term = r / n, k = seg * kSegment + r - term * n;
+        xa = ((0x001012 >> (4 * term) & 15) * per + k) * kDepth;
+        xb = ((0x010210 >> (4 * term) & 15) * per + k) * kDepth;
     }
 }
 
-__device__ __forceinline__ void add32(float (&v)[32], const uint4 *p) {
-    uint4 w[4];
+// 32 columns of a lane's row (`cols` of them inside the output) into the warp's pieces (64-byte rows,
+// swizzled) and on to the output's rows row0 .. row0 + 31; there are two pieces.
+template <typename IO>
+__device__ __forceinline__ void store_piece(uint8_t *pieces, int &stored, const CUtensorMap *map, int64_t col, int64_t row0,
+                                            int cols, const float (&v)[32], int lane) {
+    constexpr int N = 64 / sizeof(IO);  // columns of a piece
 #pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = p[q];
+    for (int h = 0; h < 32 / N; ++h) {
+        if (h * N >= cols) break;
+        uint8_t *piece = pieces + (stored++ & 1) * 2048;
+        if (lane == 0) bulk_wait_read_but_one();
+        __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint32_t x[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[8 * q + 2 * i] += __uint_as_float(x[i] << 16);
-            v[8 * q + 2 * i + 1] += __uint_as_float(x[i] & 0xffff0000u);
+        for (int q = 0; q < 4; ++q) {
+            uint4 w;
+            if (sizeof(IO) == 2)
+                w = make_uint4(pack2(v[8 * q], v[8 * q + 1]), pack2(v[8 * q + 2], v[8 * q + 3]),
+                               pack2(v[8 * q + 4], v[8 * q + 5]), pack2(v[8 * q + 6], v[8 * q + 7]));
+            else
+                w = make_uint4(__float_as_uint(v[(h * N + 4 * q) % 32]), __float_as_uint(v[(h * N + 4 * q + 1) % 32]),
+                               __float_as_uint(v[(h * N + 4 * q + 2) % 32]), __float_as_uint(v[(h * N + 4 * q + 3) % 32]));
+            *reinterpret_cast<uint4 *>(piece + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = w;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(map, piece, (int)((col + h * N) * (sizeof(IO) / 2)), (int)row0);  // (the map counts 2 bytes)
+            bulk_commit();
         }
     }
 }
 
-// Element (r, c) of a piece.
-__device__ __forceinline__ __nv_bfloat16 *piece_at(uint8_t *piece, int r, int c) {
-    return reinterpret_cast<__nv_bfloat16 *>(piece + r * 64 + (((c >> 3) ^ ((r >> 1) & 3)) << 4)) + (c & 7);
+// v += 32 values on a 16-byte boundary
+template <typename IO>
+__device__ __forceinline__ void add32(float (&v)[32], const IO *p) {
+#pragma unroll
+    for (int h = 0; h < 32; h += 64 / sizeof(IO)) {  // 64 bytes at a time
+        uint4 w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = reinterpret_cast<const uint4 *>(p + h)[q];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t x[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (sizeof(IO) == 2) {
+                    v[(8 * q + 2 * i) % 32] += __uint_as_float(x[i] << 16);
+                    v[(8 * q + 2 * i + 1) % 32] += __uint_as_float(x[i] & 0xffff0000u);
+                } else {
+                    v[(h + 4 * q + i) % 32] += __uint_as_float(x[i]);
+                }
+            }
+        }
+    }
+}
+
+// Element (r, c) of a warp's 4096 bytes as a piece of 32 x 32.
+template <typename IO>
+__device__ __forceinline__ IO *piece_at(uint8_t *piece, int r, int c) {
+    if (sizeof(IO) == 4) return reinterpret_cast<IO *>(piece) + r * 32 + (c ^ r);
+    return reinterpret_cast<IO *>(piece + r * 64 + (((c >> 3) ^ ((r >> 1) & 3)) << 4)) + (c & 7);
 }
 
 // The same for outputs that TMA cannot write: the piece's rows one after another, a lane for each column.
-__device__ __forceinline__ void write_piece(uint8_t *piece, __nv_bfloat16 *out, int64_t ld, int rows, int cols,
-                                            const float (&v)[32], int lane) {
+template <typename IO>
+__device__ __forceinline__ void write_piece(uint8_t *piece, IO *out, int64_t ld, int rows, int cols, const float (&v)[32],
+                                            int lane) {
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) *piece_at(piece, lane, i) = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 32; ++i) io_store(piece_at<IO>(piece, lane, i), v[i]);
     __syncwarp();
     if (lane < cols)
-        for (int r = 0; r < rows; ++r) out[r * ld + lane] = *piece_at(piece, r, lane);
+        for (int r = 0; r < rows; ++r) out[r * ld + lane] = *piece_at<IO>(piece, r, lane);
     __syncwarp();
 }
-__device__ __forceinline__ void add_piece(uint8_t *piece, const __nv_bfloat16 *in, int64_t ld, int rows, int cols,
-                                          float (&v)[32], int lane) {
+template <typename IO>
+__device__ __forceinline__ void add_piece(uint8_t *piece, const IO *in, int64_t ld, int rows, int cols, float (&v)[32],
+                                          int lane) {
     __syncwarp();
     for (int r = 0; r < rows; ++r)
-        if (lane < cols) *piece_at(piece, r, lane) = in[r * ld + lane];
+        if (lane < cols) *piece_at<IO>(piece, r, lane) = in[r * ld + lane];
     __syncwarp();
     if (lane < rows)
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-            if (i < cols) v[i] += __bfloat162float(*piece_at(piece, lane, i));
+            if (i < cols) v[i] += io_load(piece_at<IO>(piece, lane, i));
     __syncwarp();
 }
 
-template <int ACT> __device__ __forceinline__ void act32(float (&v)[32]) {
+template <typename IO, int ACT> __device__ __forceinline__ void act32(float (&v)[32]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = linear_act<__nv_bfloat16>(v[i], ACT);
+    for (int i = 0; i < 32; ++i) v[i] = linear_act<IO>(v[i], ACT);
 }
 
-template <int CG, int BN>
+template <typename IO, int CG, int BN>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_product_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                  const __grid_constant__ CUtensorMap mapO, const __grid_constant__ CUtensorMap mapZ,
                  const __grid_constant__ ProductTc a) {
-    using T = Tile<CG, BN>;
+    using T = Tile<IO, CG, BN>;
     constexpr int S = T::STAGES;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = align_1024(smem_raw);
@@ -155,6 +204,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     clear_status(a.p.clear, a.p.status);
+    if (T::PLANES && flagged(a.p)) return;
     if (tid == 0) {
         for (int i = 0; i < S; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(tfull + i, 1); mbar_init(tempty + i, CG * kEpiWarps); }
@@ -199,15 +249,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         if (CG == 2) tma_load_2d_pair(dst, m, x, y, bar);
                         else tma_load_2d(dst, m, x, y, full + st);
                     };
+                    int ka, kb;
+                    slice_of<T::PLANES>(s, a.per, ka, kb);
                     if (p.A.kt) {
-                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, s * kDepth);
+                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, ka);
                     } else {
-                        load(sa, &mapA, s * kDepth, ra);
+                        load(sa, &mapA, ka, ra);
                     }
                     if (p.B.kt) {
-                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, s * kDepth);
+                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, kb);
                     } else {
-                        load(sb, &mapB, s * kDepth, rb);
+                        load(sb, &mapB, kb, rb);
                     }
                 }
             }
@@ -218,10 +270,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const uint32_t lboA = p.A.kt ? 8192 : 16, lboB = p.B.kt ? 8192 : 16;
             const uint32_t stepA = p.A.kt ? 2048 : 32, stepB = p.B.kt ? 2048 : 32;  // bytes of 16 of K
             int it = 0, n = 0;
-            for (int u = first; u < units && !failed; u += stride, ++n) {
+            for (int u = first; u < units && !failed; u += stride) {
                 int tm, tn, sp;
                 unit_tile(a, u, tm, tn, sp);
-                const int s0 = sp * a.steps_per_split, s1 = min(a.k_steps, s0 + a.steps_per_split);
+                const int from = sp * a.steps_per_split, to = min(a.k_steps, from + a.steps_per_split);
+                // (one accumulator of all of them, or of every 256 of K)
+                for (int s0 = from, s1; s0 < to && !failed; s0 = s1, ++n) {
+                s1 = T::PLANES ? min(to, s0 + kSegment * kTerms) : to;
                 const int acc = n & 1;
                 wait(tempty + acc, ((n >> 1) & 1) ^ 1);
                 tc_fence_after();
@@ -245,6 +300,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 if (failed) break;
                 if (CG == 2) mma_commit_pair(tfull + acc);
                 else mma_commit(tfull + acc);
+                }
             }
         }
     } else {
@@ -252,18 +308,53 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tempty_leader[2] = {CG == 2 ? leader_addr(tempty) : 0, CG == 2 ? leader_addr(tempty + 1) : 0};
         int n = 0, stored = 0;
+        constexpr int CH = BN / 32;  // chunks of 32 columns, in halves
+        const int c0 = half * ((CH + 1) / 2), c1 = half ? CH : (CH + 1) / 2;
+        const uint32_t sum = tbase + lane_base + 2 * BN;
         for (int u = first; u < units && !failed; u += stride, ++n) {
             int tm, tn, sp;
             unit_tile(a, u, tm, tn, sp);
+            int more = 0;  // accumulators before the last one
+            if (T::PLANES) {
+                const int steps = min(a.k_steps - sp * a.steps_per_split, a.steps_per_split);
+                more = (steps - 1) / (kSegment * kTerms);
+                for (int i = 0; i < more && !failed; ++i, ++n) {
+                    wait(tfull + (n & 1), (n >> 1) & 1);
+                    if (__any_sync(0xffffffffu, failed)) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = c0; c < c1; ++c) {
+                        uint32_t x[32];
+                        tmem_ld32(tbase + lane_base + (n & 1) * BN + 32 * c, x);
+                        if (i) {
+                            uint32_t y[32];
+                            tmem_ld32(sum + 32 * c, y);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) + __uint_as_float(y[j]));
+                        } else {
+                            tmem_wait_ld();
+                        }
+                        tmem_st32(sum + 32 * c, x);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (CG == 2) mbar_arrive_cluster(tempty_leader[n & 1]);
+                        else mbar_arrive(tempty + (n & 1));
+                    }
+                }
+                if (__any_sync(0xffffffffu, failed)) break;
+            }
             const int acc = n & 1;
             wait(tfull + acc, (n >> 1) & 1);
             if (__any_sync(0xffffffffu, failed)) break;
             tc_fence_after();
             const int64_t row = (int64_t)(tm * CG + (int)rank) * T::BM + quarter * 32 + lane;
-            constexpr int CH = BN / 32;  // chunks of 32 columns, in halves
             const bool last_split_empty = a.steps_per_split * sp >= a.k_steps;
 #pragma unroll 1
-            for (int c = half * ((CH + 1) / 2); c < (half ? CH : (CH + 1) / 2); ++c) {
+            for (int c = c0; c < c1; ++c) {
                 const int64_t col = (int64_t)tn * BN + 32 * c;
                 uint32_t x[32];
                 tmem_ld32(tbase + lane_base + acc * BN + 32 * c, x);
@@ -271,17 +362,23 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = last_split_empty ? 0.0f : __uint_as_float(x[i]);
+                if (T::PLANES && more) {
+                    tmem_ld32(sum + 32 * c, x);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(x[i]);
+                }
                 const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;  // of the computed product
                 const int w = row < M ? (int)max((int64_t)0, min((int64_t)32, N - col)) : 0;
                 if (!a.swap && a.splits == 1) {  // the whole warp, for its 32 rows
-                    using B = __nv_bfloat16;
+                    using B = IO;
                     const int64_t row0 = row - lane;
                     if (row0 < M && col < N) {
                         const int rows = (int)min((int64_t)32, M - row0), cols = (int)min((int64_t)32, N - col);
                         uint8_t *piece = pieces + warp * 4096;
                         if (p.bias) {
                             if (a.vec && cols == 32) {
-                                add32(v, reinterpret_cast<const uint4 *>(static_cast<const B *>(p.bias) + col));
+                                add32<B>(v, static_cast<const B *>(p.bias) + col);
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
@@ -289,26 +386,26 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                             }
                         }
                         if (p.Z) {
-                            if (a.vec) store_piece(piece + (stored++ & 1) * 2048, &mapZ, col, row0, v, lane);
+                            if (a.vec) store_piece<B>(piece, stored, &mapZ, col, row0, cols, v, lane);
                             else write_piece(piece, static_cast<B *>(p.Z) + row0 * p.ldz + col, p.ldz, rows, cols, v, lane);
                         }
                         switch (p.act) {
-                            case LUNA_LINEAR_RELU: act32<LUNA_LINEAR_RELU>(v); break;
-                            case LUNA_LINEAR_GELU: act32<LUNA_LINEAR_GELU>(v); break;
-                            case LUNA_LINEAR_SILU: act32<LUNA_LINEAR_SILU>(v); break;
+                            case LUNA_LINEAR_RELU: act32<B, LUNA_LINEAR_RELU>(v); break;
+                            case LUNA_LINEAR_GELU: act32<B, LUNA_LINEAR_GELU>(v); break;
+                            case LUNA_LINEAR_SILU: act32<B, LUNA_LINEAR_SILU>(v); break;
                             default: break;
                         }
                         if (p.R) {
                             if (!a.vec)
                                 add_piece(piece, static_cast<const B *>(p.R) + row0 * p.ldr + col, p.ldr, rows, cols, v, lane);
                             else if (row < M && cols == 32)
-                                add32(v, reinterpret_cast<const uint4 *>(static_cast<const B *>(p.R) + row * p.ldr + col));
+                                add32<B>(v, static_cast<const B *>(p.R) + row * p.ldr + col);
                             else if (row < M)
 #pragma unroll
                                 for (int i = 0; i < 32; ++i)
                                     if (i < cols) v[i] += io_load(static_cast<const B *>(p.R) + row * p.ldr + col + i);
                         }
-                        if (a.vec) store_piece(piece + (stored++ & 1) * 2048, &mapO, col, row0, v, lane);
+                        if (a.vec) store_piece<B>(piece, stored, &mapO, col, row0, cols, v, lane);
                         else write_piece(piece, static_cast<B *>(p.out) + row0 * p.ldo + col, p.ldo, rows, cols, v, lane);
                     }
                 } else if (w == 0) {
@@ -321,7 +418,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     } else {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (i < w) linear_finish<__nv_bfloat16>(p, col + i, row, v[i]);
+                            if (i < w) linear_finish<IO>(p, col + i, row, v[i]);
                     }
                 } else {
                     float *o = p.part + ((int64_t)sp * p.M + row) * p.N + col;
@@ -367,50 +464,56 @@ bool operand_map(CUtensorMap *m, const MatView &v, int64_t rows, int64_t K, int 
     return tc_make_map_nd(m, v.p, 2, dims, strides, box);
 }
 
-bool output_map(CUtensorMap *m, const void *p, int64_t ld, int64_t M, int64_t N) {
-    const uint64_t dims[2] = {(uint64_t)N, (uint64_t)M}, strides[1] = {(uint64_t)ld * 2};
+// (an fp32 output as twice as many columns of 2 bytes)
+bool output_map(CUtensorMap *m, const void *p, int64_t ld, int64_t M, int64_t N, int halves) {
+    const uint64_t dims[2] = {(uint64_t)(N * halves), (uint64_t)M}, strides[1] = {(uint64_t)ld * 2 * halves};
     const uint32_t box[2] = {32, 32};
     return tc_make_map_nd(m, p, 2, dims, strides, box, 64);
 }
 
 // Cycles of a tile's 64-deep step (its products at 8/10 to 9/10 of the tensor rate, measured on large
 // products) and of what a block does around its steps, for choosing between tiles.
-template <int CG, int BN> constexpr int step_cycles() { return CG == 2 ? 560 : BN == 256 ? 640 : BN == 128 ? 360 : 250; }
+template <int CG, int BN> constexpr int step_cycles() {
+    return CG == 2 ? (BN == 256 ? 560 : 300) : BN == 256 ? 640 : BN == 128 ? 360 : 250;
+}
 constexpr int kTileCycles = 2500;
 
 struct Choice {
     int splits;
     double cycles;
 };
-template <int CG, int BN>
+template <typename IO, int CG, int BN>
 Choice cost(const Product &p) {
-    const int64_t tiles = ((p.M + 128 * CG - 1) / (128 * CG)) * ((p.N + BN - 1) / BN), steps = (p.K + kDepth - 1) / kDepth;
+    const int64_t tiles = ((p.M + 128 * CG - 1) / (128 * CG)) * ((p.N + BN - 1) / BN), steps = (p.K + kDepth - 1) / kDepth * (sizeof(IO) == 4 ? kTerms : 1);
     const int splits = linear_splits(p, tiles * CG, 256);
     const int64_t rounds = (tiles * splits * CG + tc_sm_count() - 1) / tc_sm_count();
     return Choice{splits, (double)rounds * ((double)((steps + splits - 1) / splits) * step_cycles<CG, BN>()) + kTileCycles +
                               (splits > 1 ? kTileCycles : 0)};
 }
 
-template <int CG, int BN>
+template <typename IO, int CG, int BN>
 cudaError_t launch(ProductTc a, cudaStream_t s) {
-    using T = Tile<CG, BN>;
+    using T = Tile<IO, CG, BN>;
     Product &p = a.p;
     const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;
     if (a.swap) std::swap(p.A, p.B);
     a.tiles_m = (int)cdiv(M, T::BM * CG);
     a.tiles_n = (int)cdiv(N, BN);
-    a.k_steps = (int)cdiv(p.K, kDepth);
+    a.per = (int)cdiv(p.K, kDepth);
+    a.k_steps = a.per * (T::PLANES ? kTerms : 1);
+    const int64_t K = T::PLANES ? 3 * (int64_t)a.per * kDepth : p.K;  // of the operands as they are stored
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     a.splits = linear_splits(p, tiles * CG, 256);
     a.steps_per_split = (int)cdiv(a.k_steps, a.splits);
+    if (T::PLANES) a.steps_per_split = (int)cdiv(a.steps_per_split, kSegment * kTerms) * kSegment * kTerms;
     a.splits = (int)cdiv(a.k_steps, a.steps_per_split);
     CUtensorMap mA, mB, mO, mZ;
     a.vec = a.vec && !a.swap && a.splits == 1;
-    if (!operand_map(&mA, p.A, M, p.K, T::BM) || !operand_map(&mB, p.B, N, p.K, T::NBL)) return cudaErrorInvalidValue;
+    if (!operand_map(&mA, p.A, M, K, T::BM) || !operand_map(&mB, p.B, N, K, T::NBL)) return cudaErrorInvalidValue;
     mO = mZ = mA;
-    if (a.vec && (!output_map(&mO, p.out, p.ldo, M, N) || (p.Z && !output_map(&mZ, p.Z, p.ldz, M, N))))
+    if (a.vec && (!output_map(&mO, p.out, p.ldo, M, N, sizeof(IO) / 2) || (p.Z && !output_map(&mZ, p.Z, p.ldz, M, N, sizeof(IO) / 2))))
         return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(k_product_tc<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(k_product_tc<IO, CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
     if (e != cudaSuccess) return e;
     const int sms = tc_sm_count() / CG * CG;
     const int grid = (int)std::min<int64_t>(tiles * a.splits * CG, sms);
@@ -427,27 +530,33 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     cfg.attrs = at;
     cfg.numAttrs = CG == 2 ? 1 : 0;
     prof_before("product_tc", s);
-    e = cudaLaunchKernelEx(&cfg, k_product_tc<CG, BN>, mA, mB, mO, mZ, a);
+    e = cudaLaunchKernelEx(&cfg, k_product_tc<IO, CG, BN>, mA, mB, mO, mZ, a);
     prof_after("product_tc", s);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || splits == 1) return e;
-    return launch_product_finish(p, splits, LUNA_BF16, s);
+    return launch_product_finish(p, splits, T::PLANES ? LUNA_F32 : LUNA_BF16, s);
 }
 
 }  // namespace
 
-cudaError_t launch_product_tc(const Product &p, cudaStream_t s) {
+cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s) {
+    using B = __nv_bfloat16;
+    const int unit = io == LUNA_F32 ? 4 : 8;
     ProductTc a;
     a.p = p;
     a.swap = false;
-    a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % 8 == 0 && p.ldr % 8 == 0 && p.ldz % 8 == 0;
+    a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % unit == 0 && p.ldr % unit == 0 && p.ldz % unit == 0;
     if (p.M <= 64) {  // few rows of X: the weight's rows fill the tile's 128 rows, X's are its columns
         a.swap = true;
         // (an MN-major slice is 64 wide)
-        return p.M <= 32 && !p.A.kt ? launch<1, 32>(a, s) : launch<1, 64>(a, s);
+        if (io == LUNA_F32) return p.M <= 32 && !p.A.kt ? launch<float, 1, 32>(a, s) : launch<float, 1, 64>(a, s);
+        return p.M <= 32 && !p.A.kt ? launch<B, 1, 32>(a, s) : launch<B, 1, 64>(a, s);
     }
-    const double pair = cost<2, 256>(p).cycles, wide = cost<1, 256>(p).cycles, half = cost<1, 128>(p).cycles;
-    if (pair <= wide && pair <= half) return launch<2, 256>(a, s);
-    return wide <= half ? launch<1, 256>(a, s) : launch<1, 128>(a, s);
+    if (io == LUNA_F32)  // (the fp32 sum leaves no room for 256 columns in TMEM)
+        return cost<float, 2, 128>(p).cycles <= cost<float, 1, 128>(p).cycles ? launch<float, 2, 128>(a, s)
+                                                                             : launch<float, 1, 128>(a, s);
+    const double pair = cost<B, 2, 256>(p).cycles, wide = cost<B, 1, 256>(p).cycles, half = cost<B, 1, 128>(p).cycles;
+    if (pair <= wide && pair <= half) return launch<B, 2, 256>(a, s);
+    return wide <= half ? launch<B, 1, 256>(a, s) : launch<B, 1, 128>(a, s);
 }
 
 }  // namespace luna

@@ -203,3 +203,64 @@ def test_refusals(L):
         p.forward(torch.zeros(16, 4).t(), torch.zeros(8, 16))
     with pytest.raises(TypeError):
         p.forward(torch.zeros(4, 16, dtype=BF), torch.zeros(8, 16))
+
+
+PLANES = [  # m, n, k, act, bias, residual, pad: fp32 products large enough for tensor cores
+    (700, 650, 577, "none", True, True, 0),
+    (1025, 520, 1100, "gelu", True, True, 4),
+    (2000, 1032, 320, "silu", False, True, 3),
+    (48, 4096, 4096, "relu", True, False, 0),
+    (20, 6000, 2051, "none", False, True, 0),
+    (4100, 264, 256, "none", True, False, 0),
+    (513, 515, 5000, "none", False, False, 1),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k,act,bias,res,pad", PLANES)
+def test_wide_products_in_fp32(L, m, n, k, act, bias, res, pad):
+    """Three bf16 planes carry an fp32 value whole, and sums of 256 products lose about 3e-7 before they
+    are joined in fp32: without an activation 1e-6 holds, with signs mixed or not."""
+    g = torch.Generator("cuda").manual_seed(m + n + k)
+    x, W = matrix(g, m, k, F, pad), matrix(g, n, k, F, pad, k ** -0.5)
+    if not res:
+        x, W = x.abs(), W.abs()
+    b = torch.randn(n, generator=g, device="cuda") if bias else None
+    r, dY = matrix(g, m, n, F, pad) if res else None, matrix(g, m, n, F, pad)
+    leaf = [t.double().requires_grad_() if t is not None else None for t in (x, W, b)]
+    z = leaf[0] @ leaf[1].t() + (leaf[2] if bias else 0.0)
+    y = act_of(z, act) + (r.double() if res else 0.0)
+    y.backward(dY.double())
+    p = L.Linear(m, n, k, act, F, backward=True)
+    Y, Z = p.forward(x, W, b, r, save_z=True)
+    got = {"Y": Y, "Z": Z, **p.backward(x, W, dY, Z, bias=bias)}
+    assert L.luna_device_status(p.ws) == 0
+    for name, v in {"Y": y, "Z": z, "dX": leaf[0].grad, "dW": leaf[1].grad}.items():
+        v = v.detach()
+        assert (got[name].double() - v).norm() < (1e-6 if act == "none" else TOL[F]) * v.norm(), name
+    if res:
+        keep = r.clone()
+        assert torch.equal(p.forward(x, W, b, keep, Y=keep), Y)
+
+
+@pytest.mark.gpu
+def test_wide_products_with_infinities_and_large_values(L):
+    """An infinity times a finite value is an infinity of its sign, a NaN stays in its row, and values near
+    the largest one are values."""
+    m, n, k = 640, 768, 700
+    g = torch.Generator("cuda").manual_seed(9)
+    x, W = matrix(g, m, k, F, 0), matrix(g, n, k, F, 0).sign() * 0.5
+    r = matrix(g, m, n, F, 0)
+    p = L.Linear(m, n, k, "none", F)
+    clean = p.forward(x, W, None, r)
+    x[3, 5], x[10, 699], x[600, 0] = float("inf"), float("-inf"), float("nan")
+    keep = r.clone()
+    y = p.forward(x, W, None, keep, Y=keep)
+    assert torch.equal(y[3], float("inf") * W[:, 5]) and torch.equal(y[10], float("-inf") * W[:, 699])
+    assert y[600].isnan().all()
+    rest = [i for i in range(m) if i not in (3, 10, 600)]
+    assert (y[rest].double() - clean[rest].double()).norm() < 1e-5 * clean[rest].double().norm()
+    x = torch.zeros((m, k), device="cuda")
+    x[:, 7] = torch.finfo(F).max
+    assert torch.equal(p.forward(x, W), x[:, 7:8] * W[:, 7])
+    assert L.luna_device_status(p.ws) == 0
