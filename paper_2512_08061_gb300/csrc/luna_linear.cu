@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, int splits) {
     linear_finish<IO>(p, i / p.N, i % p.N, acc);
 }
 
-// A few rows of X (at most eight) against rows of W, both along k: a warp owns RW rows of W and `split`
+// A few rows of X (eight of them, or the blockIdx.y-th eight) against rows of W, both along k: a warp owns RW rows of W and `split`
 // warps share them, each with its part of k; every lane has its sums for all rows of X, so W is read
 // once, 16 bytes a lane and RW loads in flight, and X comes from the first-level cache.  Bound by the
 // bytes of W.
@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
     const int64_t units = p.K / VEC;  // (VEC = 1 otherwise)
     const int64_t u0 = units * (warp % split) / split, u1 = units * (warp % split + 1) / split;
     const IO *W = static_cast<const IO *>(p.B.p), *X = static_cast<const IO *>(p.A.p);
+    const int64_t m0 = (int64_t)blockIdx.y * MR;
     float acc[MR][RW];
 #pragma unroll
     for (int i = 0; i < MR; ++i)
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
 #pragma unroll
         for (int i = 0; i < MR; ++i) {
             float xv[VEC];
-            load_vec<IO, VEC>(X + min((int64_t)i, p.M - 1) * p.A.ld + u * VEC, xv);
+            load_vec<IO, VEC>(X + min(m0 + i, p.M - 1) * p.A.ld + u * VEC, xv);
 #pragma unroll
             for (int r = 0; r < RW; ++r)
 #pragma unroll
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
     // one thread an output: group of `split` warps, row of X, row of W
     for (int t = threadIdx.x; t < (8 / split) * MR * RW; t += 256) {
         const int g = t / (MR * RW), j = t % (MR * RW);
-        const int64_t row = j / RW, col = ((int64_t)blockIdx.x * (8 / split) + g) * RW + j % RW;
+        const int64_t row = m0 + j / RW, col = ((int64_t)blockIdx.x * (8 / split) + g) * RW + j % RW;
         float sum = 0.0f;
         for (int k = 0; k < split; ++k) sum += part[g * split + k][j];
         if (row < p.M && col < p.N) linear_finish<IO>(p, row, col, sum);
@@ -407,7 +408,7 @@ cudaError_t rows_launch(const Product &p, cudaStream_t s) {
     // warps that share four rows of W: as many as keep some 2000 warps at work, with 16 loads each at least
     int split = 1;
     while (split < 8 && cdiv(p.N, 4) * split < 2000 && p.K / VEC / (split * 2) >= 128) split *= 2;
-    const unsigned grid = (unsigned)cdiv(cdiv(p.N, 4) * split, 8);
+    const dim3 grid((unsigned)cdiv(cdiv(p.N, 4) * split, 8), (unsigned)cdiv(p.M, 8));
     if (p.M == 1) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 1>), grid, 256, 0, s, p, split);
     else if (p.M == 2) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 2>), grid, 256, 0, s, p, split);
     else if (p.M <= 4) LUNA_LAUNCH("product_rows", (k_product_rows<IO, VEC, 4>), grid, 256, 0, s, p, split);
@@ -447,6 +448,8 @@ bool planes_pay(int64_t M, int64_t N, int64_t K) {
     const double simt = 2.0 * (double)(cdiv(M, kT) * kT) * (double)(cdiv(N, kT) * kT) * K / 35e6;
     return M > 8 && K > 0 && simt > 12.0 + 12.0 * macs / 1e9 + 16.0 * (double)(M + N) * K / 4e6;
 }
+// Rows of X up to which fp32 goes to the kernel for a few rows, eight at a time.
+constexpr int kRowsF32 = 32;
 // Bytes of the planes of an operand of `rows` rows.
 int64_t plane_bytes(int64_t rows, int64_t K, bool kt) { return align256(3 * up64(K) * (kt ? up8(rows) : rows) * 2); }
 constexpr int64_t kFlagBytes = 2 * kFlagBlocks * sizeof(int) / 256 * 256 + 256;
@@ -475,7 +478,7 @@ Plan make_plan(const luna_linear_desc *ld) {
         p.bwd += p.pad_bwd;
     }
     if (ld->io == LUNA_F32) {  // fp32 operands in three bf16 planes
-        p.pad_fwd = (size_t)planes_room(ld->m, ld->n, ld->k, false, false);
+        p.pad_fwd = ld->m <= kRowsF32 ? 0 : (size_t)planes_room(ld->m, ld->n, ld->k, false, false);
         p.pad_bwd = (size_t)std::max(planes_room(ld->m, ld->k, ld->n, false, true), planes_room(ld->n, ld->k, ld->m, true, true));
         p.fwd += p.pad_fwd;
         p.bwd += p.pad_bwd;
@@ -559,7 +562,9 @@ static cudaError_t split_operands(Product &p, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-bool product_rows_ok(const Product &p) { return p.M <= 8 && p.K > 0 && !p.A.kt && !p.B.kt; }
+bool product_rows_ok(const Product &p, luna_dtype io) {
+    return p.M <= (io == LUNA_F32 ? kRowsF32 : 8) && p.K > 0 && !p.A.kt && !p.B.kt;
+}
 
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s) {
     const int vec = io == LUNA_F32 ? 4 : 8;
@@ -572,7 +577,7 @@ cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s)
 // as long as the bytes); beyond that tensor cores take bf16, if need be from aligned copies of the operands
 // (which cost their bytes twice over; the CUDA-core product would take ten to thirty times the tensor cores').
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
-    if (product_rows_ok(p)) return launch_product_rows(p, io, s);
+    if (product_rows_ok(p, io)) return launch_product_rows(p, io, s);
     if (io == LUNA_BF16 && p.K >= 1) {
         Product q = p;
         cudaError_t e;

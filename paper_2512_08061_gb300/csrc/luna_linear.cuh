@@ -115,7 +115,7 @@ int linear_splits(const Product &p, int64_t tiles, int64_t least);
 
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s);          // picks a kernel
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s);     // any operands
-bool product_rows_ok(const Product &p);                                               // a few rows of X
+bool product_rows_ok(const Product &p, luna_dtype io);                                // a few rows of X
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s);
 // On tensor cores: bf16 operands, or with LUNA_F32 operands in three bf16 planes along K (see k_split).
 cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s);

@@ -16,9 +16,12 @@
 //
 // fp32 operands come as three bf16 planes, x = x0 + x1 + x2 exactly (eight bits each), and a b is the sum
 // of the six products a2 b0 + a1 b1 + a0 b2 + a1 b0 + a0 b1 + a0 b0; what is left out is under 2^-21 of
-// |a| |b|.  The tensor cores add to their fp32 accumulator by cutting off, which at a depth of 1024 has
-// lost 1.7e-6 of a sum of positive products and at 256 3e-7 (measured), so after every 256 of K the
-// epilogue's warps add the accumulator to an fp32 sum that they keep in TMEM beside it.
+// |a| |b|.  A stage holds one plane of both operands, and the products of three stages run together, the
+// small ones first: loading each product's planes anew took the L2 twice the bytes and half as long
+// again (917 us at 4096 x 4096 x 4096).  The tensor cores add to their fp32 accumulator by cutting off,
+// which at a depth of 1024 has lost 1.7e-6 of a sum of positive products and at 64 1e-7 (measured), so
+// after every 64 of K the epilogue's warps add the accumulator to an fp32 sum that they keep in TMEM
+// beside it.
 #include "luna_linear.cuh"
 
 #include <algorithm>
@@ -79,20 +82,7 @@ __device__ __forceinline__ void unit_tile(const ProductTc &a, int u, int &tm, in
     tn = r / rows;
 }
 
-// Slice s of the walk over K.  Of fp32 operands: 256 of K at a time, the six products one after another,
-// the small ones first.
-constexpr int kSegment = 4, kTerms = 6;  // slices of a plane, products
-template <bool PLANES>
-__device__ __forceinline__ void slice_of(int s, int per, int &xa, int &xb) {
-    if (!PLANES) {
-        xa = xb = s * kDepth;
-    } else {
-        const int seg = s / (kSegment * kTerms), r = s - seg * kSegment * kTerms, n = min(kSegment, per - seg * kSegment);
-        const int term = r / n, k = seg * kSegment + r - term * n;
-        xa = ((0x001012 >> (4 * term) & 15) * per + k) * kDepth;
-        xb = ((0x010210 >> (4 * term) & 15) * per + k) * kDepth;
-    }
-}
+constexpr int kPlanes = 3, kTerms = 6;
 
 // 32 columns of a lane's row (`cols` of them inside the output) into the warp's pieces (64-byte rows,
 // swizzled) and on to the output's rows row0 .. row0 + 31; there are two pieces.
@@ -249,17 +239,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         if (CG == 2) tma_load_2d_pair(dst, m, x, y, bar);
                         else tma_load_2d(dst, m, x, y, full + st);
                     };
-                    int ka, kb;
-                    slice_of<T::PLANES>(s, a.per, ka, kb);
+                    const int k = (T::PLANES ? s % kPlanes * a.per + s / kPlanes : s) * kDepth;
                     if (p.A.kt) {
-                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, ka);
+                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, k);
                     } else {
-                        load(sa, &mapA, ka, ra);
+                        load(sa, &mapA, k, ra);
                     }
                     if (p.B.kt) {
-                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, kb);
+                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, k);
                     } else {
-                        load(sb, &mapB, kb, rb);
+                        load(sb, &mapB, k, rb);
                     }
                 }
             }
@@ -274,32 +263,54 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 int tm, tn, sp;
                 unit_tile(a, u, tm, tn, sp);
                 const int from = sp * a.steps_per_split, to = min(a.k_steps, from + a.steps_per_split);
-                // (one accumulator of all of them, or of every 256 of K)
-                for (int s0 = from, s1; s0 < to && !failed; s0 = s1, ++n) {
-                s1 = T::PLANES ? min(to, s0 + kSegment * kTerms) : to;
-                const int acc = n & 1;
-                wait(tempty + acc, ((n >> 1) & 1) ^ 1);
-                tc_fence_after();
-                const uint32_t d = tbase + acc * BN;
-                for (int s = s0; s < s1 && !failed; ++s, ++it) {
-                    const int st = it % S;
-                    wait(full + st, (it / S) & 1);
-                    if (failed) break;
-                    tc_fence_after();
-                    const uint32_t sa = smem_u32(sm + st * T::STAGE);
-                    const uint64_t da = sdesc(sa, lboA, 1024, kSwizzle128), db = sdesc(sa + T::A_BYTES, lboB, 1024, kSwizzle128);
+                auto product = [&](uint32_t d, int sa, int sb, bool fresh) {  // of A in one stage, B in another
+                    const uint64_t da = sdesc(smem_u32(sm + sa * T::STAGE), lboA, 1024, kSwizzle128);
+                    const uint64_t db = sdesc(smem_u32(sm + sb * T::STAGE) + T::A_BYTES, lboB, 1024, kSwizzle128);
 #pragma unroll
                     for (int k = 0; k < kDepth / 16; ++k) {
                         const uint64_t ka = da + ((k * stepA) >> 4), kb = db + ((k * stepB) >> 4);
-                        if (CG == 2) mma_bf16_ss_pair(d, ka, kb, id, s > s0 || k > 0);
-                        else mma_bf16_ss(d, ka, kb, id, s > s0 || k > 0);
+                        if (CG == 2) mma_bf16_ss_pair(d, ka, kb, id, !fresh || k > 0);
+                        else mma_bf16_ss(d, ka, kb, id, !fresh || k > 0);
                     }
+                };
+                auto release = [&](int st) {
                     if (CG == 2) mma_commit_pair(empty + st);
                     else mma_commit(empty + st);
-                }
-                if (failed) break;
-                if (CG == 2) mma_commit_pair(tfull + acc);
-                else mma_commit(tfull + acc);
+                };
+                // (one accumulator for all of them, or for every three planes)
+                for (int s = from; s < to && !failed; ++n) {
+                    const int acc = n & 1;
+                    wait(tempty + acc, ((n >> 1) & 1) ^ 1);
+                    tc_fence_after();
+                    const uint32_t d = tbase + acc * BN;
+                    if (T::PLANES) {
+                        int st[kPlanes];
+                        for (int q = 0; q < kPlanes; ++q, ++s, ++it) {
+                            st[q] = it % S;
+                            wait(full + st[q], (it / S) & 1);
+                        }
+                        if (failed) break;
+                        tc_fence_after();
+                        product(d, st[2], st[0], true);
+                        product(d, st[1], st[1], false);
+                        product(d, st[0], st[2], false);
+                        product(d, st[1], st[0], false);
+                        product(d, st[0], st[1], false);
+                        product(d, st[0], st[0], false);
+                        for (int q = 0; q < kPlanes; ++q) release(st[q]);
+                    } else {
+                        for (; s < to; ++s, ++it) {
+                            const int st = it % S;
+                            wait(full + st, (it / S) & 1);
+                            if (failed) break;
+                            tc_fence_after();
+                            product(d, st, st, s == from);
+                            release(st);
+                        }
+                        if (failed) break;
+                    }
+                    if (CG == 2) mma_commit_pair(tfull + acc);
+                    else mma_commit(tfull + acc);
                 }
             }
         }
@@ -317,7 +328,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             int more = 0;  // accumulators before the last one
             if (T::PLANES) {
                 const int steps = min(a.k_steps - sp * a.steps_per_split, a.steps_per_split);
-                more = (steps - 1) / (kSegment * kTerms);
+                more = steps / kPlanes - 1;
                 for (int i = 0; i < more && !failed; ++i, ++n) {
                     wait(tfull + (n & 1), (n >> 1) & 1);
                     if (__any_sync(0xffffffffu, failed)) break;
@@ -500,12 +511,12 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     a.tiles_m = (int)cdiv(M, T::BM * CG);
     a.tiles_n = (int)cdiv(N, BN);
     a.per = (int)cdiv(p.K, kDepth);
-    a.k_steps = a.per * (T::PLANES ? kTerms : 1);
+    a.k_steps = a.per * (T::PLANES ? kPlanes : 1);
     const int64_t K = T::PLANES ? 3 * (int64_t)a.per * kDepth : p.K;  // of the operands as they are stored
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     a.splits = linear_splits(p, tiles * CG, 256);
     a.steps_per_split = (int)cdiv(a.k_steps, a.splits);
-    if (T::PLANES) a.steps_per_split = (int)cdiv(a.steps_per_split, kSegment * kTerms) * kSegment * kTerms;
+    if (T::PLANES) a.steps_per_split = (int)cdiv(a.steps_per_split, kPlanes) * kPlanes;
     a.splits = (int)cdiv(a.k_steps, a.steps_per_split);
     CUtensorMap mA, mB, mO, mZ;
     a.vec = a.vec && !a.swap && a.splits == 1;
