@@ -20,7 +20,7 @@
 
 #include <algorithm>
 
-#include "luna_common.cuh"
+#include "luna_norm.cuh"
 #include "luna_prof.cuh"
 
 namespace luna {
@@ -35,143 +35,10 @@ struct Limits {
     int threads, resident;
 };
 constexpr Limits limits(int vec, int nv, bool backward) {
-    if (vec == 1) return nv == 4 ? Limits{256, backward ? 512 : 1024} : Limits{512, 512};
+    if (vec == 1) return nv == 4 ? Limits{256, backward ? 512 : 1024} : Limits{512, 512};  // (32: narrow groups alone)
     if (nv == 1) return backward ? Limits{512, 512} : Limits{256, 1024};
     if (nv == 2) return backward ? Limits{512, 512} : Limits{256, 512};
     return Limits{kMaxCols / vec / nv, kMaxCols / vec / nv};
-}
-
-struct NormArgs {
-    const void *x, *y, *gate, *dX, *dH;
-    void *X, *H, *dx, *dy, *dgate;
-    const float *w_post, *b_post, *w_pre, *b_pre;
-    float *part;       // [slot][array][cols]: weight-gradient partials (dw_post, db_post, dw_pre, db_pre)
-    int64_t rows;
-    int cols, groups, layer, act;
-    float alpha, eps;
-    int64_t ldx, ldy, ldgate, ldX, ldH, lddX, lddH, lddx, lddy, lddgate;
-    int gvec;          // vectors of a group
-    int gmode;         // how a group is summed: 0 whole row, 1 lanes of a warp, 2 through shared memory
-};
-
-// VEC values as they are loaded (16 bytes, or one value), and as fp32.
-template <typename IO, int VEC> struct Vec;
-template <> struct Vec<float, 4> {
-    using Raw = float4;
-    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[4]) { v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w; }
-    static __device__ __forceinline__ void store(float *p, const float (&v)[4]) {
-        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    }
-};
-template <> struct Vec<__nv_bfloat16, 8> {
-    using Raw = uint4;
-    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[8]) {
-        const uint32_t b[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(b[i] << 16);
-            v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u);
-        }
-    }
-    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&v)[8]) {
-        uint32_t b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 w = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            memcpy(&b[i], &w, 4);
-        }
-        *reinterpret_cast<uint4 *>(p) = make_uint4(b[0], b[1], b[2], b[3]);
-    }
-};
-template <typename IO> struct Vec<IO, 1> {
-    using Raw = IO;
-    static __device__ __forceinline__ void unpack(const Raw &w, float (&v)[1]) { v[0] = io_load(&w); }
-    static __device__ __forceinline__ void store(IO *p, const float (&v)[1]) { io_store(p, v[0]); }
-};
-
-// Element-wise work on VEC values, two an instruction.
-__device__ __forceinline__ uint64_t pair(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-template <int VEC> struct V {
-    // d = a b + c
-    static __device__ __forceinline__ void fma(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC], const float (&c)[VEC]) {
-        if (VEC == 1) { d[0] = fmaf(a[0], b[0], c[0]); return; }
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2) {
-            uint64_t r;
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])), "l"(pair(c[e], c[e + 1])));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
-        }
-    }
-    // d = a s + c
-    static __device__ __forceinline__ void fma(float (&d)[VEC], const float (&a)[VEC], float k, const float (&c)[VEC]) {
-        if (VEC == 1) { d[0] = fmaf(a[0], k, c[0]); return; }
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2) {
-            uint64_t r;
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(k, k)), "l"(pair(c[e], c[e + 1])));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
-        }
-    }
-    static __device__ __forceinline__ void mul(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC]) {
-        if (VEC == 1) { d[0] = a[0] * b[0]; return; }
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2) {
-            uint64_t r;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
-        }
-    }
-    static __device__ __forceinline__ void mul(float (&d)[VEC], const float (&a)[VEC], float k) {
-        if (VEC == 1) { d[0] = a[0] * k; return; }
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2) {
-            uint64_t r;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(k, k)));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
-        }
-    }
-    static __device__ __forceinline__ void add(float (&d)[VEC], const float (&a)[VEC], const float (&b)[VEC]) {
-        if (VEC == 1) { d[0] = a[0] + b[0]; return; }
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2) {
-            uint64_t r;
-            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(d[e]), "=f"(d[e + 1]) : "l"(r));
-        }
-    }
-    static __device__ __forceinline__ float dot(const float (&a)[VEC], const float (&b)[VEC]) {
-        if (VEC == 1) return a[0] * b[0];
-        uint64_t r = pair(0.0f, 0.0f);
-#pragma unroll
-        for (int e = 0; e + 1 < VEC; e += 2)
-            asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(r) : "l"(pair(a[e], a[e + 1])), "l"(pair(b[e], b[e + 1])));
-        float x, y;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r));
-        return x + y;
-    }
-    static __device__ __forceinline__ float sum(const float (&a)[VEC]) {
-        float s = a[0];
-#pragma unroll
-        for (int e = 1; e < VEC; ++e) s += a[e];
-        return s;
-    }
-};
-
-template <int VEC>
-__device__ __forceinline__ void load_w(const float *p, int c, float (&v)[VEC]) {
-    if (VEC == 1) {
-        v[0] = p[c];
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-            const float4 w = *reinterpret_cast<const float4 *>(p + c + i);
-            v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
-        }
-    }
 }
 
 // The threads of one row: a warp (eight rows a block) or the whole block.  Vector i of thread t is
@@ -258,15 +125,6 @@ struct RowTeam {
     }
 };
 
-// 1 / (1 + e^-g) by the hardware's exponential and reciprocal (2 ulp each), without their handling of
-// denormal results, which would be as many operations again: those values count as 0.
-__device__ __forceinline__ float sigmoidf(float g) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * g));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-    return r;
-}
-
 template <int NV>
 __device__ __forceinline__ RowTeam<NV> make_team(const NormArgs &a, int nvec, float *sm) {
     RowTeam<NV> t;
@@ -339,37 +197,6 @@ template <typename IO, int VEC, int NV> struct RowPart {
         for (int i = 0; i < NV; ++i) Vec<IO, VEC>::unpack(raw[i], v[i]);
     }
 };
-
-// Gates of VEC values: v *= act(g), the choice once for all of them.
-template <int VEC> __device__ __forceinline__ void apply_gate(int act, const float (&g)[VEC], float (&v)[VEC]) {
-    if (act == LUNA_GATE_SILU) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] *= g[e] * sigmoidf(g[e]);
-    } else if (act == LUNA_GATE_SIGMOID) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] *= sigmoidf(g[e]);
-    }
-}
-// act(g) into `value` and its slope into g.
-template <int VEC> __device__ __forceinline__ void gate_and_slope(int act, float (&g)[VEC], float (&value)[VEC]) {
-    if (act == LUNA_GATE_SILU) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float sg = sigmoidf(g[e]);
-            value[e] = g[e] * sg;
-            g[e] = fmaf(value[e], 1.0f - sg, sg);
-        }
-    } else if (act == LUNA_GATE_SIGMOID) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            value[e] = sigmoidf(g[e]);
-            g[e] = value[e] * (1.0f - value[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) value[e] = 1.0f;
-    }
-}
 
 template <typename IO, int VEC, int NV>
 __device__ __forceinline__ void store_row(void *p, int64_t off, const float (&v)[NV][VEC], int t, int threads, int active) {
@@ -693,18 +520,38 @@ __global__ void __launch_bounds__(256) k_norm_sum(NormSum a) {
 
 // ---------------------------------------------------------------------------
 
+// Vectors of a group from which a row may go to the kernels for wide rows (8192 bf16 columns, backward: groups of
+// 64 vectors 242 us against 296, of 16 vectors 390 against 252; not aligned, registers cost four times as much).
+constexpr int wide_group(bool vectors) { return vectors ? 32 : 8; }
+
 struct Shape {
     int vec, nv, threads, rows_per_block, blocks;
     size_t smem;
+    bool wide, shared;   // the kernels for wide rows; sums of the weight gradients in shared memory
 };
 
 // The fewest vectors a thread with which a row fits its threads.  A row of at most 32 vectors is a warp's.
-Shape shape_of(int cols, bool vectors, int vec_io, bool backward) {
+// Rows that would take more values a thread than its registers hold go to the kernels for wide rows, unless
+// their groups are narrow (a warp takes a group at a time).  Aligned rows keep to registers in the forward pass,
+// which needs fewer (4104 bf16 columns 48 us against 104).
+Shape shape_of(int cols, int groups, bool vectors, int vec_io, bool backward, bool bias) {
     Shape s;
+    s.wide = s.shared = false;
     s.vec = vectors ? vec_io : 1;
     const int nvec = cols / s.vec;
     s.nv = vectors ? 1 : 4;
-    while (s.nv < (vectors ? 4 : 32) && nvec > s.nv * limits(s.vec, s.nv, backward).threads) s.nv *= 2;
+    while (s.nv < (vectors ? 4 : 32) && nvec > s.nv * limits(s.vec, s.nv, backward).threads) s.nv *= vectors ? 2 : 8;
+    if (s.nv * s.vec > (vectors ? 8 : 4) && (backward || !vectors) && nvec / groups >= wide_group(vectors)) {
+        const size_t row = sizeof(float) * wide_floats(cols, groups);
+        const size_t sums = sizeof(float) * (cols + 3) / 4 * 4 * (bias ? 4 : 2);
+        s.wide = true;
+        s.shared = backward && row + sums <= 200 * 1024;
+        s.smem = row + (s.shared ? sums : 0);
+        s.rows_per_block = 1;
+        s.threads = s.smem <= 100 * 1024 ? 512 : 1024;
+        s.blocks = 152 * (s.threads == 512 ? 2 : 1);
+        return s;
+    }
     s.threads = ((nvec + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.rows_per_block = s.threads == 32 ? 8 : 1;
     s.blocks = 152 * std::max(1, limits(s.vec, s.nv, backward).resident / (s.threads * s.rows_per_block));
@@ -757,7 +604,9 @@ cudaError_t fwd_launch(const NormArgs &a, const Shape &sh, cudaStream_t s) {
 template <typename IO, int VECIO>
 cudaError_t fwd(NormArgs a, cudaStream_t s) {
     const bool v = vectors_ok(a, VECIO);
-    Shape sh = shape_of(a.cols, v, VECIO, false);
+    Shape sh = shape_of(a.cols, a.w_post ? a.groups : 1, v, VECIO, false, false);
+    if (sh.wide)
+        return launch_norm_fwd_wide(a, IOType<IO>::code, vectors_ok(a, 2), grid_of(a.rows, sh), sh.threads, sh.smem, s);
     group_mode(a, sh);
     if (v) {
         if (sh.nv == 1) return fwd_launch<IO, VECIO, 1>(a, sh, s);
@@ -765,8 +614,6 @@ cudaError_t fwd(NormArgs a, cudaStream_t s) {
         return fwd_launch<IO, VECIO, 4>(a, sh, s);
     }
     if (sh.nv == 4) return fwd_launch<IO, 1, 4>(a, sh, s);
-    if (sh.nv == 8) return fwd_launch<IO, 1, 8>(a, sh, s);
-    if (sh.nv == 16) return fwd_launch<IO, 1, 16>(a, sh, s);
     return fwd_launch<IO, 1, 32>(a, sh, s);
 }
 
@@ -781,18 +628,19 @@ cudaError_t bwd_launch(const NormArgs &a, const Shape &sh, int grid, cudaStream_
 template <typename IO, int VECIO, bool BIAS>
 cudaError_t bwd(NormArgs a, float *const (&out)[4], cudaStream_t s) {
     const bool v = vectors_ok(a, VECIO);
-    Shape sh = shape_of(a.cols, v, VECIO, true);
-    group_mode(a, sh);
+    Shape sh = shape_of(a.cols, a.w_post ? a.groups : 1, v, VECIO, true, BIAS);
+    if (!sh.wide) group_mode(a, sh);
     const int grid = grid_of(a.rows, sh);
     cudaError_t e;
-    if (v) {
+    if (sh.wide) {
+        e = launch_norm_bwd_wide(a, IOType<IO>::code, v ? VECIO : vectors_ok(a, 2) ? 2 : 1, BIAS, sh.shared, grid, sh.threads,
+                                 sh.smem, s);
+    } else if (v) {
         if (sh.nv == 1) e = bwd_launch<IO, VECIO, 1, BIAS>(a, sh, grid, s);
         else if (sh.nv == 2) e = bwd_launch<IO, VECIO, 2, BIAS>(a, sh, grid, s);
         else e = bwd_launch<IO, VECIO, 4, BIAS>(a, sh, grid, s);
     } else {
         if (sh.nv == 4) e = bwd_launch<IO, 1, 4, BIAS>(a, sh, grid, s);
-        else if (sh.nv == 8) e = bwd_launch<IO, 1, 8, BIAS>(a, sh, grid, s);
-        else if (sh.nv == 16) e = bwd_launch<IO, 1, 16, BIAS>(a, sh, grid, s);
         else e = bwd_launch<IO, 1, 32, BIAS>(a, sh, grid, s);
     }
     if (e != cudaSuccess || !a.part) return e;
@@ -844,8 +692,8 @@ bool combination_ok(const luna_norm_desc *nd, const void *x, const void *y, cons
 // The partial sums of the launch shape with vectors or without, whichever has more.
 size_t partial_bytes(const luna_norm_desc *nd) {
     size_t slots = 0;
-    for (bool v : {false, true}) {
-        const Shape sh = shape_of(nd->cols, v, nd->io == LUNA_F32 ? 4 : 8, true);
+    for (int form = 0; form < 8; ++form) {
+        const Shape sh = shape_of(nd->cols, form & 1 ? nd->groups : 1, form & 2, nd->io == LUNA_F32 ? 4 : 8, true, form & 4);
         slots = std::max(slots, (size_t)grid_of(nd->rows, sh) * sh.rows_per_block);
     }
     return slots * 4 * nd->cols * sizeof(float);

@@ -217,3 +217,40 @@ def test_refusals(L):
         p.forward(torch.zeros(8, 4).t(), torch.zeros(4, 8), w_pre=torch.zeros(8))
     with pytest.raises(TypeError):
         p.forward(torch.zeros(4, 8), torch.zeros(4, 8), w_pre=torch.zeros(8, dtype=BF))
+
+
+WIDE = [  # more rows than blocks, and rows that a block walks in passes
+    (700, 7094, 1, "rms", "none", "xpq", F),
+    (310, 5001, 3, "layer", "silu", "xpqb", F),
+    (305, 5001, 3, "rms", "sigmoid", "xpq", BF),
+    (400, 8140, 4, "rms", "none", "pq", BF),
+    (330, 8192, 16, "layer", "silu", "xpqb", BF),
+    (320, 16384, 16, "rms", "silu", "xpqb", F),
+    (306, 9000, 250, "layer", "sigmoid", "xpqb", BF),  # groups of 36, in pieces of several to a warp
+    (200, 16001, 1, "layer", "none", "qyb", F),
+    (199, 4400, 1, "layer", "silu", "xp", F),
+    (198, 6000, 5, "rms", "silu", "x", BF),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,groups,kind,gate,parts,io", WIDE)
+def test_wide_rows(L, rows, cols, groups, kind, gate, parts, io):
+    test_values_and_gradients(L, rows, cols, groups, kind, gate, parts, io)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols,groups", [(6000, 4), (6001, 1)])
+def test_wide_rows_in_place(L, cols, groups):
+    g = torch.Generator("cuda").manual_seed(12)
+    x, y, gate, dX, dH = (torch.randn((320, cols), generator=g, device="cuda") for _ in range(5))
+    wq, wp = torch.randn(cols, generator=g, device="cuda"), torch.randn(cols, generator=g, device="cuda")
+    p = L.BlockNorm(320, cols, groups=groups, gate="silu", io=F, backward=True)
+    f = p.forward(x, y, gate, wp, wq)
+    want = p.backward(x, y, gate, wp, wq, dX, dH)
+    out = {"dx": dX.clone(), "dy": y.clone(), "dgate": gate.clone()}
+    got = p.backward(x, out["dy"], out["dgate"], wp, wq, out["dx"], dH, out=out)
+    assert all(torch.equal(got[k], want[k]) for k in ("dx", "dy", "dgate"))
+    a, b = x.clone(), y.clone()
+    p.forward(a, b, gate, wp, wq, X=a, H=b)
+    assert torch.equal(a, f["X"]) and torch.equal(b, f["H"])
