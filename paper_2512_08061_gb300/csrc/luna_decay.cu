@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_m
                     }
             }
         }
+        if (ci == nch - 1 && !a.Xout) break;  // (the state is wanted no further)
         const float dec = pw[nv];
 #pragma unroll
         for (int i = 0; i < 4 * FT; ++i)

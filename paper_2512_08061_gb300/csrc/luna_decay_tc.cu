@@ -275,61 +275,61 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                 mma_commit(pready);
             };
             for (int item = blockIdx.x; item < items && !failed; item += gridDim.x) {
-            const int nch = Piece(a, item).nch;
-            for (int c = 0; c < nch && !failed; ++c) {
-                const int gc = base_c + c, La = gc * LOADS, Lb = La + LOADS - 2, Lc = Lb + 1;
-                const uint32_t ph = gc & 1;
-                if (!STATE && c == 0) scores(gc);
-                if (!STATE) {
-                    wait(xready, ph);
-                    if (gc > 0) wait(efree, (gc - 1) & 1);
-                    if (failed) break;
-                    tc_fence_after();
-                    const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128);
+                const int nch = Piece(a, item).nch;
+                for (int c = 0; c < nch && !failed; ++c) {
+                    const int gc = base_c + c, La = gc * LOADS, Lb = La + LOADS - 2, Lc = Lb + 1;
+                    const uint32_t ph = gc & 1;
+                    if (!STATE && c == 0) scores(gc);
+                    if (!STATE) {
+                        wait(xready, ph);
+                        if (gc > 0) wait(efree, (gc - 1) & 1);
+                        if (failed) break;
+                        tc_fence_after();
+                        const uint64_t dA = sdesc(slot_addr(La), 16, 1024, kSwizzle128);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t o = (k / 4) * C::BLK + 32 * (k % 4);
-                        mma_bf16_ss(tb + C::cE, dadd(dA, o), dadd(dX, 2048 * k), idE, k > 0);
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t o = (k / 4) * C::BLK + 32 * (k % 4);
+                            mma_bf16_ss(tb + C::cE, dadd(dA, o), dadd(dX, 2048 * k), idE, k > 0);
+                        }
+                        mma_commit(eready);
+                        mma_commit(freeb + La % kSlots);
                     }
-                    mma_commit(eready);
-                    mma_commit(freeb + La % kSlots);
-                }
-                wait(full + Lc % kSlots, (Lc / kSlots) & 1);
-                if (STATE && gc > 0) wait(ufree, (gc - 1) & 1);  // (otherwise before X was ready)
-                const uint64_t dB1 = sdesc(C::INPLACE ? slot_addr(Lb) : smem_u32(terms), C::BLK, 1024, kSwizzle128);
-                const uint64_t dB2 = sdesc(smem_u32(terms) + (C::INPLACE ? 0 : C::TILE), C::BLK, 1024, kSwizzle128);
-                const uint64_t dC = sdesc(slot_addr(Lc), C::BLK, 1024, kSwizzle128);
+                    wait(full + Lc % kSlots, (Lc / kSlots) & 1);
+                    if (STATE && gc > 0) wait(ufree, (gc - 1) & 1);  // (otherwise before X was ready)
+                    const uint64_t dB1 = sdesc(C::INPLACE ? slot_addr(Lb) : smem_u32(terms), C::BLK, 1024, kSwizzle128);
+                    const uint64_t dB2 = sdesc(smem_u32(terms) + (C::INPLACE ? 0 : C::TILE), C::BLK, 1024, kSwizzle128);
+                    const uint64_t dC = sdesc(slot_addr(Lc), C::BLK, 1024, kSwizzle128);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    wait(scaled + half, ph);
+                    for (int half = 0; half < 2; ++half) {
+                        wait(scaled + half, ph);
+                        if (failed) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int q = 0; q < NT; ++q)
+#pragma unroll
+                            for (int k = 4 * half; k < 4 * half + 4; ++k)
+                                mma_bf16_ss(tb + C::cU, q == 0 ? dadd(dB1, 2048 * k) : dadd(dB2, (q - 1) * C::TILE + 2048 * k),
+                                            dadd(dC, 2048 * k), idU, (half | q | (k & 3)) != 0);
+                        mma_commit(uread + half);
+                    }
                     if (failed) break;
-                    tc_fence_after();
+                    mma_commit(freeb + Lb % kSlots);
+                    if (STATE) {
+                        mma_commit(freeb + Lc % kSlots);
+                    } else {
+                        wait(masked, ph);
+                        if (failed) break;
+                        tc_fence_after();
 #pragma unroll
-                    for (int q = 0; q < NT; ++q)
-#pragma unroll
-                        for (int k = 4 * half; k < 4 * half + 4; ++k)
-                            mma_bf16_ss(tb + C::cU, q == 0 ? dadd(dB1, 2048 * k) : dadd(dB2, (q - 1) * C::TILE + 2048 * k),
-                                        dadd(dC, 2048 * k), idU, (half | q | (k & 3)) != 0);
-                    mma_commit(uread + half);
+                        for (int k = 0; k < kRows / 16; ++k)
+                            mma_bf16_ts(tb + C::cE, tb + C::cP + 64 * (k / 4) + 8 * (k % 4), dadd(dC, 2048 * k), idE, 1);
+                        mma_commit(oready);
+                        if (!STAGED) mma_commit(freeb + Lc % kSlots);
+                        if (c + 1 < nch) scores(gc + 1);
+                    }
                 }
-                if (failed) break;
-                mma_commit(freeb + Lb % kSlots);
-                if (STATE) {
-                    mma_commit(freeb + Lc % kSlots);
-                } else {
-                    wait(masked, ph);
-                    if (failed) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int k = 0; k < kRows / 16; ++k)
-                        mma_bf16_ts(tb + C::cE, tb + C::cP + 64 * (k / 4) + 8 * (k % 4), dadd(dC, 2048 * k), idE, 1);
-                    mma_commit(oready);
-                    if (!STAGED) mma_commit(freeb + Lc % kSlots);
-                    if (c + 1 < nch) scores(gc + 1);
-                }
-            }
-            if (!C::STAYS) break;
-            base_c += nch;
+                if (!C::STAYS) break;
+                base_c += nch;
             }
         }
     } else if (warp < kScaleWarps) {
@@ -337,65 +337,65 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         constexpr int PIECES = D / 8 / (kScaleWarps * 32 / 64);
         const int hr = tid & 63, piece0 = (tid >> 6) * PIECES;
         for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const Piece t(a, item);
-        for (int c = 0; c < t.nch; ++c) {
-            const int nv = t.valid(c), gc = base_c + c;
-            const uint32_t ph = gc & 1;
-            const int Lb = gc * LOADS + LOADS - 2, Lc = Lb + 1;
-            uint8_t *tbb = sm + (Lb % kSlots) * C::TILE, *tcc = sm + (Lc % kSlots) * C::TILE;
-            uint8_t *t1 = C::INPLACE ? tbb : terms, *t2 = terms + (C::INPLACE ? 0 : C::TILE);
-            wait(full + Lb % kSlots, (Lb / kSlots) & 1);
-            if (!STATE && C::INPLACE) wait(pready, ph);  // P has read b
+            const Piece t(a, item);
+            for (int c = 0; c < t.nch; ++c) {
+                const int nv = t.valid(c), gc = base_c + c;
+                const uint32_t ph = gc & 1;
+                const int Lb = gc * LOADS + LOADS - 2, Lc = Lb + 1;
+                uint8_t *tbb = sm + (Lb % kSlots) * C::TILE, *tcc = sm + (Lc % kSlots) * C::TILE;
+                uint8_t *t1 = C::INPLACE ? tbb : terms, *t2 = terms + (C::INPLACE ? 0 : C::TILE);
+                wait(full + Lb % kSlots, (Lb / kSlots) & 1);
+                if (!STATE && C::INPLACE) wait(pready, ph);  // P has read b
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                const int r = half * 64 + hr;
-                const bool on = r < nv;
-                const float w = on ? a.u * t.power(nv - (a.reverse ? nv - 1 - r : r) - e) : 0.0f;
-                const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
-                uint4 in4[PIECES];
+                for (int half = 0; half < 2; ++half) {
+                    const int r = half * 64 + hr;
+                    const bool on = r < nv;
+                    const float w = on ? a.u * t.power(nv - (a.reverse ? nv - 1 - r : r) - e) : 0.0f;
+                    const uint64_t w2 = f2(w, w), minus = f2(-1.0f, -1.0f);
+                    uint4 in4[PIECES];
 #pragma unroll
-                for (int q = 0; q < PIECES; ++q)
-                    in4[q] = *reinterpret_cast<const uint4 *>(tbb + ((piece0 + q) / 8) * C::BLK +
-                                                              sw128_chunk(r, (piece0 + q) % 8));
-                if (gc > 0) wait(uread + half, (gc - 1) & 1);  // the last chunk's terms have been read
+                    for (int q = 0; q < PIECES; ++q)
+                        in4[q] = *reinterpret_cast<const uint4 *>(tbb + ((piece0 + q) / 8) * C::BLK +
+                                                                  sw128_chunk(r, (piece0 + q) % 8));
+                    if (gc > 0) wait(uread + half, (gc - 1) & 1);  // the last chunk's terms have been read
 #pragma unroll
-                for (int q = 0; q < PIECES; ++q) {
-                    const uint32_t off = ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8);
-                    uint4 v = in4[q];
-                    if (!on) v = make_uint4(0, 0, 0, 0);  // rows past the length may hold anything
-                    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t o1[4], o2[4], o3[4];
+                    for (int q = 0; q < PIECES; ++q) {
+                        const uint32_t off = ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8);
+                        uint4 v = in4[q];
+                        if (!on) v = make_uint4(0, 0, 0, 0);  // rows past the length may hold anything
+                        const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+                        uint32_t o1[4], o2[4], o3[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint64_t x = mul2(widen2(in[k]), w2);
-                        o1[k] = pack2(x);
-                        x = fma2(widen2(o1[k]), minus, x);
-                        o2[k] = pack2(x);
-                        if (NT == 3) o3[k] = pack2(fma2(widen2(o2[k]), minus, x));
+                        for (int k = 0; k < 4; ++k) {
+                            uint64_t x = mul2(widen2(in[k]), w2);
+                            o1[k] = pack2(x);
+                            x = fma2(widen2(o1[k]), minus, x);
+                            o2[k] = pack2(x);
+                            if (NT == 3) o3[k] = pack2(fma2(widen2(o2[k]), minus, x));
+                        }
+                        *reinterpret_cast<uint4 *>(t1 + off) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+                        *reinterpret_cast<uint4 *>(t2 + off) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
+                        if (NT == 3) *reinterpret_cast<uint4 *>(t2 + C::TILE + off) = make_uint4(o3[0], o3[1], o3[2], o3[3]);
                     }
-                    *reinterpret_cast<uint4 *>(t1 + off) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
-                    *reinterpret_cast<uint4 *>(t2 + off) = make_uint4(o2[0], o2[1], o2[2], o2[3]);
-                    if (NT == 3) *reinterpret_cast<uint4 *>(t2 + C::TILE + off) = make_uint4(o3[0], o3[1], o3[2], o3[3]);
-                }
-                if (nv < kRows) {  // c without the rows past the length
-                    wait(full + Lc % kSlots, (Lc / kSlots) & 1);
-                    if (!on) {
+                    if (nv < kRows) {  // c without the rows past the length
+                        wait(full + Lc % kSlots, (Lc / kSlots) & 1);
+                        if (!on) {
 #pragma unroll
-                        for (int q = 0; q < PIECES; ++q)
-                            *reinterpret_cast<uint4 *>(tcc + ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8)) =
-                                make_uint4(0, 0, 0, 0);
+                            for (int q = 0; q < PIECES; ++q)
+                                *reinterpret_cast<uint4 *>(tcc + ((piece0 + q) / 8) * C::BLK + sw128_chunk(r, (piece0 + q) % 8)) =
+                                    make_uint4(0, 0, 0, 0);
+                        }
                     }
+                    fence_proxy_async_smem();
+                    // These warps read b alone, and b's slot held an a before: its load is known to be complete only by P
+                    // of that chunk, and without that the wait for b would take the phase before a's load for b's.  Before
+                    // the arrival that lets this chunk's last products go ahead, so that P is never two phases on.
+                    if (!STATE && !C::INPLACE && half == 1) wait(pready, ph);
+                    arrive(scaled + half);
                 }
-                fence_proxy_async_smem();
-                // These warps read b alone, and b's slot held an a before: its load is known to be complete only by P
-                // of that chunk, and without that the wait for b would take the phase before a's load for b's.  Before
-                // the arrival that lets this chunk's last products go ahead, so that P is never two phases on.
-                if (!STATE && !C::INPLACE && half == 1) wait(pready, ph);
-                arrive(scaled + half);
             }
-        }
-        if (!C::STAYS) break;
-        base_c += t.nch;
+            if (!C::STAYS) break;
+            base_c += t.nch;
         }
     } else if (warp < kScoreWarp0) {
         constexpr int SC = D / (kStateWarps / 4);
@@ -415,78 +415,78 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
             }
         };
         for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const Piece t(a, item);
-        const float *X0 = a.X ? a.X + (t.bh * a.x_pieces + (a.x_pieces > 1 ? t.seg : 0)) * a.da * a.dc : nullptr;
+            const Piece t(a, item);
+            const float *X0 = a.X ? a.X + (t.bh * a.x_pieces + (a.x_pieces > 1 ? t.seg : 0)) * a.da * a.dc : nullptr;
 #pragma unroll 1
-        for (int cc = cc0; cc < cc0 + SC; cc += 16) {
-            float x[16];
-            uint32_t y[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                x[k] = X0 && own && f < a.da && cc + k < a.dc
-                           ? (a.x_trans ? X0[(int64_t)(cc + k) * a.da + f] : X0[(int64_t)f * a.dc + cc + k]) : 0.0f;
-                y[k] = __float_as_uint(x[k]);
-            }
-            tmem_st16(tb + lb + C::cX + cc, y);
-            if (!STATE && t.nch > 0) put_operand(cc, x);
-        }
-        tmem_wait_st();
-        if (!STATE && t.nch > 0) {
-            fence_proxy_async_smem();
-            arrive(xready);
-        }
-        for (int c = 0; c < t.nch; ++c) {
-            const uint32_t ph = (base_c + c) & 1;
-            const float dec = t.power(t.valid(c));
-            wait(uread + 1, ph);
-            if (!STATE) wait(eready, ph);  // E has read the operand
-            tc_fence_after();
-            const uint64_t dec2 = f2(dec, dec);
-            // (one copy of the code where two more groups of warps compete for the instruction cache)
-            constexpr int kUnroll = STATE ? SC / 16 : 1;
-#pragma unroll kUnroll
-            for (int c1 = 0; c1 < SC; c1 += 16) {
-                const int cc = cc0 + c1;
-                uint32_t xu[16], xx[16];
-                tmem_ld16(tb + lb + C::cU + cc, xu);
-                tmem_ld16(tb + lb + C::cX + cc, xx);
-                tmem_wait_ld();
+            for (int cc = cc0; cc < cc0 + SC; cc += 16) {
                 float x[16];
+                uint32_t y[16];
 #pragma unroll
-                for (int k = 0; k < 16; k += 2) {
-                    unpack2(fma2(dec2, f2(xx[k], xx[k + 1]), f2(xu[k], xu[k + 1])), x[k], x[k + 1]);
-                    xx[k] = __float_as_uint(x[k]);
-                    xx[k + 1] = __float_as_uint(x[k + 1]);
+                for (int k = 0; k < 16; ++k) {
+                    x[k] = X0 && own && f < a.da && cc + k < a.dc
+                               ? (a.x_trans ? X0[(int64_t)(cc + k) * a.da + f] : X0[(int64_t)f * a.dc + cc + k]) : 0.0f;
+                    y[k] = __float_as_uint(x[k]);
                 }
-                tmem_st16(tb + lb + C::cX + cc, xx);
-                if (!STATE && c + 1 < t.nch) put_operand(cc, x);
+                tmem_st16(tb + lb + C::cX + cc, y);
+                if (!STATE && t.nch > 0) put_operand(cc, x);
             }
             tmem_wait_st();
-            tc_fence_before();
-            if (STATE) {
-                arrive(ufree);
-            } else if (c + 1 < t.nch) {
+            if (!STATE && t.nch > 0) {
                 fence_proxy_async_smem();
                 arrive(xready);
             }
-        }
-        if (a.Xout) {
-            float *X = a.Xout + (t.bh * a.nseg + t.seg) * a.da * a.dc + (int64_t)f * a.dc;
-#pragma unroll 1
-            for (int cc = cc0; cc < cc0 + SC; cc += 16) {
-                uint32_t x[16];
-                tmem_ld16(tb + lb + C::cX + cc, x);
-                tmem_wait_ld();
-                if (own && f < a.da) {
+            for (int c = 0; c < t.nch; ++c) {
+                const uint32_t ph = (base_c + c) & 1;
+                const float dec = t.power(t.valid(c));
+                wait(uread + 1, ph);
+                if (!STATE) wait(eready, ph);  // E has read the operand
+                tc_fence_after();
+                const uint64_t dec2 = f2(dec, dec);
+                // (one copy of the code where two more groups of warps compete for the instruction cache)
+                constexpr int kUnroll = STATE ? SC / 16 : 1;
+#pragma unroll kUnroll
+                for (int c1 = 0; c1 < SC; c1 += 16) {
+                    const int cc = cc0 + c1;
+                    uint32_t xu[16], xx[16];
+                    tmem_ld16(tb + lb + C::cU + cc, xu);
+                    tmem_ld16(tb + lb + C::cX + cc, xx);
+                    tmem_wait_ld();
+                    float x[16];
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4)
-                        if (cc + k < a.dc) *reinterpret_cast<uint4 *>(X + cc + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                    for (int k = 0; k < 16; k += 2) {
+                        unpack2(fma2(dec2, f2(xx[k], xx[k + 1]), f2(xu[k], xu[k + 1])), x[k], x[k + 1]);
+                        xx[k] = __float_as_uint(x[k]);
+                        xx[k + 1] = __float_as_uint(x[k + 1]);
+                    }
+                    tmem_st16(tb + lb + C::cX + cc, xx);
+                    if (!STATE && c + 1 < t.nch) put_operand(cc, x);
                 }
-                __syncwarp();
+                tmem_wait_st();
+                tc_fence_before();
+                if (STATE) {
+                    arrive(ufree);
+                } else if (c + 1 < t.nch) {
+                    fence_proxy_async_smem();
+                    arrive(xready);
+                }
             }
-        }
-        if (!C::STAYS) break;
-        base_c += t.nch;
+            if (a.Xout) {
+                float *X = a.Xout + (t.bh * a.nseg + t.seg) * a.da * a.dc + (int64_t)f * a.dc;
+#pragma unroll 1
+                for (int cc = cc0; cc < cc0 + SC; cc += 16) {
+                    uint32_t x[16];
+                    tmem_ld16(tb + lb + C::cX + cc, x);
+                    tmem_wait_ld();
+                    if (own && f < a.da) {
+#pragma unroll
+                        for (int k = 0; k < 16; k += 4)
+                            if (cc + k < a.dc) *reinterpret_cast<uint4 *>(X + cc + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!C::STAYS) break;
+            base_c += t.nch;
         }
     } else if (!STATE) {
         // scores and outputs: thread (row, 1 / PARTS of the columns); PARTS warps share a quarter's rows
@@ -505,113 +505,113 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
         };
         auto group_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(GT) : "memory"); };
         for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const Piece t(a, item);
-        OUT *O = static_cast<OUT *>(a.out) + t.b * a.ob + (int64_t)t.h * a.oh;
-        group_sync();  // the last piece's decays have been used
-        for (int k = gt; k <= kRows; k += GT) pw[k] = t.power(k);
-        for (int k = gt; k < 4 * kDiagCopy; k += GT) {
-            const int dist = (k % kDiagCopy + k / kDiagCopy - 31) * (a.reverse ? 1 : -1);
-            diag[k] = dist >= 0 && dist < 32 ? a.p * t.power(dist) : 0.0f;
-        }
-        if (gt < 32) cols[gt] = t.power(a.reverse ? gt : 31 - gt);
-        group_sync();
-        for (int c = 0; c < t.nch; ++c) {
-            const int row0 = t.row(c), nv = t.valid(c), gc = base_c + c;
-            const uint32_t ph = gc & 1;
-            wait(pready, ph);
-            tc_fence_after();
-#pragma unroll 1
-            for (int q = 0; q < PC / 32; ++q) {  // the bf16 scores take the place of columns that this warp has read
-                const int blk = part * (PC / 32) + q;
-                uint32_t w[16];
-                decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, cols, w);
-                tmem_st16(tb + lb + C::cP + 64 * (blk / 2) + 16 * (blk % 2), w);
+            const Piece t(a, item);
+            OUT *O = static_cast<OUT *>(a.out) + t.b * a.ob + (int64_t)t.h * a.oh;
+            group_sync();  // the last piece's decays have been used
+            for (int k = gt; k <= kRows; k += GT) pw[k] = t.power(k);
+            for (int k = gt; k < 4 * kDiagCopy; k += GT) {
+                const int dist = (k % kDiagCopy + k / kDiagCopy - 31) * (a.reverse ? 1 : -1);
+                diag[k] = dist >= 0 && dist < 32 ? a.p * t.power(dist) : 0.0f;
             }
-            if (STAGED && gc > 0) give_slot();
-            wait(eready, ph);
-            tc_fence_after();
-            const int m = a.reverse ? nv - 1 - i : i;
-            const float xs = a.x * pw[max(0, m) + e];
-            const uint64_t xs2 = f2(xs, xs);
+            if (gt < 32) cols[gt] = t.power(a.reverse ? gt : 31 - gt);
+            group_sync();
+            for (int c = 0; c < t.nch; ++c) {
+                const int row0 = t.row(c), nv = t.valid(c), gc = base_c + c;
+                const uint32_t ph = gc & 1;
+                wait(pready, ph);
+                tc_fence_after();
 #pragma unroll 1
-            for (int q = 0; q < EC / 32; ++q) {
-                uint32_t x[32];
-                tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
-                tmem_wait_ld();
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    uint32_t y[16];
-#pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        float lo, hi;
-                        unpack2(mul2(xs2, f2(x[16 * s + k], x[16 * s + k + 1])), lo, hi);
-                        y[k] = __float_as_uint(lo);
-                        y[k + 1] = __float_as_uint(hi);
-                    }
-                    tmem_st16(tb + lb + C::cE + part * EC + 32 * q + 16 * s, y);
+                for (int q = 0; q < PC / 32; ++q) {  // the bf16 scores take the place of columns that this warp has read
+                    const int blk = part * (PC / 32) + q;
+                    uint32_t w[16];
+                    decay_scores(tb + lb + C::cP + 32 * blk, i, blk, a.reverse != 0, nv, a.p, pw, diag, cols, w);
+                    tmem_st16(tb + lb + C::cP + 64 * (blk / 2) + 16 * (blk % 2), w);
                 }
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            arrive(masked);
-            wait(oready, ph);
-            tc_fence_after();
-            const int Lc = gc * LOADS + LOADS - 1;
-            uint8_t *tcc = sm + (Lc % kSlots) * C::TILE;  // U and the scores' product have read c
-            OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
+                if (STAGED && gc > 0) give_slot();
+                wait(eready, ph);
+                tc_fence_after();
+                const int m = a.reverse ? nv - 1 - i : i;
+                const float xs = a.x * pw[max(0, m) + e];
+                const uint64_t xs2 = f2(xs, xs);
 #pragma unroll 1
-            for (int q = 0; q < EC / 32; ++q) {
-                uint32_t x[32];
-                tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
-                tmem_wait_ld();
-                if (q == EC / 32 - 1) {
-                    tc_fence_before();
-                    arrive(efree);
-                }
-                const int cc = part * EC + 32 * q;
-                if (STAGED) {
+                for (int q = 0; q < EC / 32; ++q) {
+                    uint32_t x[32];
+                    tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (i < nv)
-                            v = make_uint4(pack2(f2(x[k], x[k + 1])), pack2(f2(x[k + 2], x[k + 3])),
-                                           pack2(f2(x[k + 4], x[k + 5])), pack2(f2(x[k + 6], x[k + 7])));
-                        *reinterpret_cast<uint4 *>(tcc + (cc / 64) * C::BLK + sw128_chunk(i, (cc % 64 + k) / 8)) = v;
-                    }
-                } else if (i < nv) {
+                    for (int s = 0; s < 2; ++s) {
+                        uint32_t y[16];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8)
-                        if (cc + k < a.dc) {  // dc is a multiple of 8
-                            uint4 *dst = reinterpret_cast<uint4 *>(o + 32 * q + k);
-                            dst[0] = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-                            dst[1] = make_uint4(x[k + 4], x[k + 5], x[k + 6], x[k + 7]);
+                        for (int k = 0; k < 16; k += 2) {
+                            float lo, hi;
+                            unpack2(mul2(xs2, f2(x[16 * s + k], x[16 * s + k + 1])), lo, hi);
+                            y[k] = __float_as_uint(lo);
+                            y[k + 1] = __float_as_uint(hi);
                         }
+                        tmem_st16(tb + lb + C::cE + part * EC + 32 * q + 16 * s, y);
+                    }
                 }
-                __syncwarp();
-            }
-            if (STAGED) {  // 32 rows of a 64-column block at a time: a warp's own, or with D = 64 its pair's
-                fence_proxy_async_smem();
-                if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(2 + quarter) : "memory");
-                else __syncwarp();
-                if (stores) {
-                    const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
-                    if (row < a.n && 64 * blk < a.dc)
-                        tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, t.h, t.b);
-                    bulk_commit();
+                tmem_wait_st();
+                tc_fence_before();
+                arrive(masked);
+                wait(oready, ph);
+                tc_fence_after();
+                const int Lc = gc * LOADS + LOADS - 1;
+                uint8_t *tcc = sm + (Lc % kSlots) * C::TILE;  // U and the scores' product have read c
+                OUT *o = O + (int64_t)(row0 + i) * a.ot + part * EC;
+#pragma unroll 1
+                for (int q = 0; q < EC / 32; ++q) {
+                    uint32_t x[32];
+                    tmem_ld32(tb + lb + C::cE + part * EC + 32 * q, x);
+                    tmem_wait_ld();
+                    if (q == EC / 32 - 1) {
+                        tc_fence_before();
+                        arrive(efree);
+                    }
+                    const int cc = part * EC + 32 * q;
+                    if (STAGED) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+                            uint4 v = make_uint4(0, 0, 0, 0);
+                            if (i < nv)
+                                v = make_uint4(pack2(f2(x[k], x[k + 1])), pack2(f2(x[k + 2], x[k + 3])),
+                                               pack2(f2(x[k + 4], x[k + 5])), pack2(f2(x[k + 6], x[k + 7])));
+                            *reinterpret_cast<uint4 *>(tcc + (cc / 64) * C::BLK + sw128_chunk(i, (cc % 64 + k) / 8)) = v;
+                        }
+                    } else if (i < nv) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8)
+                            if (cc + k < a.dc) {  // dc is a multiple of 8
+                                uint4 *dst = reinterpret_cast<uint4 *>(o + 32 * q + k);
+                                dst[0] = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                                dst[1] = make_uint4(x[k + 4], x[k + 5], x[k + 6], x[k + 7]);
+                            }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (STAGED) {  // 32 rows of a 64-column block at a time: a warp's own, or with D = 64 its pair's
+                    fence_proxy_async_smem();
+                    if (D == 64) asm volatile("bar.sync %0, 64;" ::"r"(2 + quarter) : "memory");
+                    else __syncwarp();
+                    if (stores) {
+                        const int blk = D == 128 ? part : 0, row = row0 + quarter * 32;
+                        if (row < a.n && 64 * blk < a.dc)
+                            tma_store_4d(&mapO, tcc + blk * C::BLK + quarter * 4096, 64 * blk, row, t.h, t.b);
+                        bulk_commit();
+                    }
+                    __syncwarp();
+                }
             }
-        }
-        // rows at and past the length
-        constexpr int ZB = 16 / (int)sizeof(OUT);
-        const int pieces = a.dc / ZB, step = GT / pieces;
-        const int zr = STAGED ? min(t.rend, t.r0 + t.nch * kRows) : t.r1;  // staged chunks have written theirs
-        OUT *z = O + (int64_t)zr * a.ot + (gt % pieces) * ZB;
-        if (gt < step * pieces)
-            for (int k = gt / pieces; k < t.rend - zr; k += step)
-                *reinterpret_cast<uint4 *>(z + (int64_t)k * a.ot) = make_uint4(0, 0, 0, 0);
-        if (!C::STAYS) break;
-        base_c += t.nch;
+            // rows at and past the length
+            constexpr int ZB = 16 / (int)sizeof(OUT);
+            const int pieces = a.dc / ZB, step = GT / pieces;
+            const int zr = STAGED ? min(t.rend, t.r0 + t.nch * kRows) : t.r1;  // staged chunks have written theirs
+            OUT *z = O + (int64_t)zr * a.ot + (gt % pieces) * ZB;
+            if (gt < step * pieces)
+                for (int k = gt / pieces; k < t.rend - zr; k += step)
+                    *reinterpret_cast<uint4 *>(z + (int64_t)k * a.ot) = make_uint4(0, 0, 0, 0);
+            if (!C::STAYS) break;
+            base_c += t.nch;
         }
         if (STAGED && stores) bulk_wait();
     }
