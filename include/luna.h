@@ -436,8 +436,12 @@ luna_status luna_norm_bwd(const luna_norm_desc *nd, const void *x, const void *y
  * bf16 runs on tensor cores (with n or k that is not a multiple of 8 from
  * aligned copies of the operands in the workspace; a matrix that is off a
  * 16-byte boundary, or whose leading dimension is not a multiple of 8, although
- * n and k are, is multiplied on CUDA cores), up to eight rows of X and fp32 on
- * CUDA cores.
+ * n and k are, is multiplied on CUDA cores), up to eight rows of X on CUDA
+ * cores.  fp32 products large enough to gain from it run on tensor cores too,
+ * each operand written to the workspace as three bf16 values that sum to it
+ * exactly (6 bytes a value); the result is as close as fp32 sums are (2e-7 of
+ * its norm), and operands with an infinity or a NaN go to CUDA cores, where
+ * these spread as in any fp32 product.  Small fp32 products run there always.
  * Supported: m <= 2^23, n, k <= 2^20; k = 0 sums nothing. */
 typedef enum {
     LUNA_LINEAR_NONE = 0, LUNA_LINEAR_RELU = 1, LUNA_LINEAR_GELU = 2, LUNA_LINEAR_SILU = 3
@@ -453,7 +457,8 @@ typedef struct {
 } luna_linear_desc;
 
 /* Bytes of the workspace of luna_linear_fwd (backward = 0) or luna_linear_bwd
- * (1): partial sums and, with an activation, dLoss/dz.  256-byte aligned. */
+ * (1): partial sums, copies of the operands where the product needs them and,
+ * with an activation, dLoss/dz.  256-byte aligned. */
 luna_status luna_linear_workspace_size(const luna_linear_desc *ld, int backward, size_t *bytes);
 
 luna_status luna_linear_fwd(const luna_linear_desc *ld, const void *X, const void *W, const void *bias, const void *R,

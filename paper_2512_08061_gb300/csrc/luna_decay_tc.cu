@@ -12,7 +12,8 @@
 // the others two (their state only enters outputs as one more bf16 rounding).  X is not accumulated by
 // the products themselves: their additions onto a large X round toward zero, chunk after chunk.
 //
-// Bound: by its bytes the pass is (da + dc) * 4 bytes a row at HBM rate; the shared-memory traffic of
+// Measured: 115 us for 128 heads of 4096 rows at d = dv = 128 (537 MB, 4.7 TB/s), issue 34 %, tensor 31 %.
+// Bound: the chain of the steps above, some 5000 cycles a chunk at d = 128.  By its bytes the pass is (da + dc) * 4 bytes a row at HBM rate; the shared-memory traffic of
 // the products' operands and of the scaled terms comes next (about 2/3 of that at d = 128).  Three
 // groups of warps (the scaled b; X; P and out) work on their parts of neighbouring chunks side by side,
 // and the next tiles load while they do: a ring of four slots takes a, b, c in turn.
@@ -33,8 +34,7 @@ namespace {
 using namespace sm100;
 
 constexpr int kRows = 128;   // rows of a chunk
-constexpr int kAhead = 2;
-
+constexpr int kAhead = 2;    // chunks whose tiles L2 is asked for in advance
 
 template <int D, int NT, bool STATE> struct Cfg {
     static constexpr int SCALE = 8, STATEW = 8, SCORE = 8;  // warps of each of the three groups
