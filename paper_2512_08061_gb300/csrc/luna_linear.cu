@@ -79,7 +79,7 @@ __device__ __forceinline__ void load_quad(const IO *p, float (&v)[4]) {
 // sums a thread in fp32, two multiply-adds an instruction, the next step's values loaded while this one's
 // are multiplied.  Bound by the fp32 FMA rate (116 us at 5727 x 656 x 576: 37 TFLOP/s).
 // QUAD: loads of four values along the contiguous dimension (rows on their boundaries).
-template <typename IO, bool QUAD>
+template <typename TA, typename IO, bool QUAD>
 __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t depth, int splits) {
     __shared__ __align__(16) float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
@@ -99,20 +99,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
         const int e = tid + i * kThreads;
         if (kt) { r = e % (kT / W) * W; k = e / (kT / W); } else { k = e % (kK / W) * W; r = e / (kK / W); }
     };
-    auto fetch_one = [&](const MatView &v, int64_t base, int64_t rows, int64_t kb, float (&out)[8]) {
+    auto fetch_one = [&](auto type, const MatView &v, int64_t base, int64_t rows, int64_t kb, float (&out)[8]) {
+        using T = decltype(type);
 #pragma unroll
         for (int i = 0; i < 8 / W; ++i) {
             int r, k;
             place(v.kt, i, r, k);
             if (QUAD) {  // (four rows or four depths are in or out together)
                 const bool in = base + r < rows && kb + k < k1;
-                const IO *q = static_cast<const IO *>(v.p) + (v.kt ? (kb + k) * v.ld + base + r : (base + r) * v.ld + kb + k);
+                const T *q = static_cast<const T *>(v.p) + (v.kt ? (kb + k) * v.ld + base + r : (base + r) * v.ld + kb + k);
                 float x[4] = {0.f, 0.f, 0.f, 0.f};
-                if (in) load_quad<IO>(q, x);
+                if (in) load_quad<T>(q, x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) out[(4 * i + j) % 8] = x[j];
             } else {
-                out[i % 8] = at<IO>(v, base + r, rows, kb + k, k1);
+                out[i % 8] = at<T>(v, base + r, rows, kb + k, k1);
             }
         }
     };
@@ -126,8 +127,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
         }
     };
     auto fetch = [&](int64_t kb) {
-        fetch_one(p.A, row0, p.M, kb, ra);
-        fetch_one(p.B, col0, p.N, kb, rb);
+        fetch_one(TA{}, p.A, row0, p.M, kb, ra);
+        fetch_one(IO{}, p.B, col0, p.N, kb, rb);
     };
     fetch(k0);
     for (int64_t kb = k0; kb < k1; kb += kK) {
@@ -239,9 +240,11 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
 
 // dZ = dY act'(Z) (not written where there is no activation; rows lddz apart) and the column sums of dZ over a
 // block's rows, one partial row a block.  32 column pieces x 8 rows of threads; bound by the bytes.
-template <typename IO, int VEC>
-__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ, int64_t lddz, int64_t m,
-                                                   int n, int act, int64_t rows, float *part, int *status) {
+// OUT: dZ's type.
+template <typename IO, typename OUT, int VEC>
+__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, OUT *dZ,
+                                                   int64_t lddz, int64_t m, int n, int act, int64_t rows, float *part,
+                                                   int *status) {
     __shared__ float s[8][32 * VEC + 1];
     clear_status(1, status);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * VEC;
@@ -259,7 +262,7 @@ __global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, c
                 load_vec<IO, VEC>(Z + r * ldz + c, z);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) d[e] *= linear_slope<IO>(z[e], act);
-                store_vec<IO, VEC>(dZ + r * lddz + c, d);
+                store_vec<OUT, VEC>(dZ + r * lddz + c, d);
             }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) acc[e] += d[e];
@@ -367,10 +370,12 @@ cudaError_t simt(const Product &p, cudaStream_t s) {
         return reinterpret_cast<uintptr_t>(v.p) % (4 * sizeof(IO)) == 0 && v.ld % 4 == 0 && (v.kt ? rows : K) % 4 == 0;
     };
     const dim3 grid((unsigned)gx, (unsigned)gy, used);
-    if (quad(p.A, p.M, p.K) && quad(p.B, p.N, p.K))
-        LUNA_LAUNCH("product", (k_product<IO, true>), grid, kThreads, 0, s, p, depth, used);
+    if (p.wide_a)
+        LUNA_LAUNCH("product", (k_product<float, IO, false>), grid, kThreads, 0, s, p, depth, used);
+    else if (quad(p.A, p.M, p.K) && quad(p.B, p.N, p.K))
+        LUNA_LAUNCH("product", (k_product<IO, IO, true>), grid, kThreads, 0, s, p, depth, used);
     else
-        LUNA_LAUNCH("product", (k_product<IO, false>), grid, kThreads, 0, s, p, depth, used);
+        LUNA_LAUNCH("product", (k_product<IO, IO, false>), grid, kThreads, 0, s, p, depth, used);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || used == 1) return e;
     return launch_product_finish(p, used, IOType<IO>::code, s);
@@ -380,24 +385,26 @@ constexpr int64_t kDzRows = 256;  // rows of a block of the column sums
 
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <typename IO, int VEC>
+template <typename IO, typename OUT, int VEC>
 void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act, float *part,
                int parts, int *status, cudaStream_t s) {
-    LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC>), dim3((unsigned)cdiv(n, 32 * VEC), parts), 256, 0, s,
-                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, m, n, act, kDzRows,
+    LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, OUT, VEC>), dim3((unsigned)cdiv(n, 32 * VEC), parts), 256, 0, s,
+                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<OUT *>(dZ), lddz, m, n, act, kDzRows,
                 part, status);
 }
 
 template <typename IO>
 cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act,
-               float *part, void *db, int *status, cudaStream_t s) {
+               float *part, void *db, bool whole, int *status, cudaStream_t s) {
     constexpr int VEC = 16 / (int)sizeof(IO);
     const int parts = (int)cdiv(m, kDzRows);
     const bool a = act != LUNA_LINEAR_NONE;
-    if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
-        dz_launch<IO, VEC>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
+    if (whole)
+        dz_launch<IO, float, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
+    else if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
+        dz_launch<IO, IO, VEC>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
     else
-        dz_launch<IO, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
+        dz_launch<IO, IO, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !db) return e;
     LUNA_LAUNCH("linear_db", k_linear_db<IO>, (unsigned)cdiv(n, 256), 256, 0, s, part, parts, n, static_cast<IO *>(db));
@@ -436,6 +443,17 @@ struct Plan {
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
 
+// dZ stays in fp32 in bf16 layers with few values, where its own rounding does not average out (over a few
+// hundred values, of it or of a gradient, it can weigh more than the gradient's).  Their products then run on
+// CUDA cores, which costs 30 us of 60 (2 x 3680 x 128), up to 50; beyond that dZ is rounded to bf16 once for
+// the tensor cores, which a gradient sees as sqrt(2) of its own rounding.
+bool whole_dz(const luna_linear_desc *ld) {
+    const int64_t limit = int64_t(1) << 29;
+    const auto tiles = [](int64_t x) { return cdiv(x, kT) * kT; };
+    return ld->io == LUNA_BF16 && ld->act != LUNA_LINEAR_NONE && std::min({ld->m * ld->n, ld->m * ld->k, (int64_t)ld->n * ld->k}) <= 1024 &&
+           tiles(ld->m) * tiles(ld->k) * ld->n <= limit && tiles(ld->n) * tiles(ld->k) * ld->m <= limit;
+}
+
 // Partial products: up to 32 pieces of K of a product with few tiles, at most 64 MiB.
 size_t part_bytes(int64_t M, int64_t N) { return (size_t)std::min<int64_t>(M * N * 4 * 32, int64_t(64) << 20); }
 
@@ -467,7 +485,7 @@ Plan make_plan(const luna_linear_desc *ld) {
     p.part_bwd = (size_t)align256((int64_t)p.part_bwd);
     p.fwd = p.o_part + p.part_fwd;
     p.o_dz = p.o_part + p.part_bwd;
-    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * up8(ld->n) * eb));
+    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * up8(ld->n) * (whole_dz(ld) ? 4 : eb)));
     p.o_pad_fwd = p.fwd;
     p.o_pad_bwd = p.bwd;
     // bf16 widths that are not multiples of 8: copies of the operands whose rows are 16-byte aligned
@@ -579,7 +597,7 @@ cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s)
 // (which cost their bytes twice over; the CUDA-core product would take ten to thirty times the tensor cores').
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
     if (product_rows_ok(p, io)) return launch_product_rows(p, io, s);
-    if (io == LUNA_BF16 && p.K >= 1) {
+    if (io == LUNA_BF16 && p.K >= 1 && !p.wide_a) {
         Product q = p;
         cudaError_t e;
         if (pad_operands(q, s, &e)) return launch_product_tc(q, io, s);
@@ -662,10 +680,11 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     int *status = reinterpret_cast<int *>(ws);
     const int64_t lddy = ld->lddy ? ld->lddy : n, ldz = ld->ldz ? ld->ldz : n;
     cudaError_t e = cudaSuccess;
+    const bool whole = whole_dz(ld);
     if (act || db) {
         void *dZ = ws + pl.o_dz;
-        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, status, s)
-                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, status, s);
+        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, false, status, s)
+                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, whole, status, s);
         if (e != cudaSuccess) return LUNA_ERR_CUDA;
     }
     if (k == 0) return LUNA_OK;
@@ -678,6 +697,7 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     p.pad = pl.pad_bwd ? ws + pl.o_pad_bwd : nullptr; p.pad_bytes = pl.pad_bwd;
     p.status = status;
     p.clear = !(act || db);
+    p.wide_a = whole;
     if (dX) {
         p.A = MatView{G, ldg, false};
         p.B = MatView{W, ldw, true};

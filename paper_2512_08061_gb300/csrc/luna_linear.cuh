@@ -21,6 +21,7 @@ struct MatView {           // element (row, k) at p[row * ld + k], or with kt at
 struct Product {
     MatView A, B;
     int64_t M, N, K;
+    bool wide_a;           // A is fp32 though the rest is bf16 (CUDA cores alone)
     const void *bias;      // N values, or NULL
     int act;               // luna_linear_act
     const void *R;         // residual M x N, or NULL

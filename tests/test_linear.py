@@ -264,3 +264,23 @@ def test_wide_products_with_infinities_and_large_values(L):
     x[:, 7] = torch.finfo(F).max
     assert torch.equal(p.forward(x, W), x[:, 7:8] * W[:, 7])
     assert L.luna_device_status(p.ws) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k,act", [(5, 1, 300, "gelu"), (40, 3, 129, "silu"), (1, 60, 2048, "gelu"), (130, 31, 77, "relu"),
+                                       (20, 16, 4096, "silu")])
+def test_small_gradients_round_once(L, m, n, k, act):
+    """The gradients of a small layer carry the rounding of their own bf16 values alone (half a unit in the
+    last of eight bits: at most 2^-8 of each) and what fp32 sums and slopes lose."""
+    g = torch.Generator("cuda").manual_seed(m * n + k)
+    x, W, dY = matrix(g, m, k, BF, 0), matrix(g, n, k, BF, 0, k ** -0.5), matrix(g, m, n, BF, 0)
+    p = L.Linear(m, n, k, act, BF, backward=True)
+    _, Z = p.forward(x, W, save_z=True)
+    got = p.backward(x, W, dY, Z)
+    z = Z.double().requires_grad_()
+    act_of(z, act).backward(dY.double())
+    for name, v, size in (("dX", z.grad @ W.double(), z.grad.abs() @ W.double().abs()),
+                          ("dW", z.grad.t() @ x.double(), z.grad.abs().t() @ x.double().abs())):
+        err = (got[name].double() - v).abs()
+        assert (err <= 2.0 ** -8 * v.abs() + 1e-4 * size).all(), name
+    assert L.luna_device_status(p.ws) == 0
