@@ -172,9 +172,10 @@ __device__ __forceinline__ void normalise(float (&z)[NV][VEC], float (&r)[NV], R
 #pragma unroll
     for (int i = 0; i < NV; ++i) s[i] = make_float2(V<VEC>::dot(z[i], z[i]), 0.f);
     sum();
+    // (a vector past the row's end may be a group of its own, whose root of 0 + eps with eps = 0 has no reciprocal)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        r[i] = rsqrtf(fmaf(s[i].x, inv, a.eps));
+        r[i] = i < active ? rsqrtf(fmaf(s[i].x, inv, a.eps)) : 0.0f;
         V<VEC>::mul(z[i], z[i], r[i]);
     }
 }

@@ -1,0 +1,52 @@
+"""The norms around a block where their statistics are extreme or their launch shapes leave threads idle.
+
+Tolerances (relative 2-norms) as in test_block_norm.py: a bf16 output carries one rounding (1.7e-3 in the root
+mean square), taken as 2.5e-3; fp32 values sum terms rounded at 2^-24, taken as 1e-5.
+"""
+import pytest
+import torch
+
+from test_block_norm import BF, F, TOL, formula
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2512_08061_gb300 import build
+    build.build()
+    import paper_2512_08061_gb300.luna as L
+    return L
+
+
+def leaves(rows, cols, io, seed, gate=True):
+    g = torch.Generator("cuda").manual_seed(seed)
+
+    def rn(*shape, dtype=io):
+        return (torch.randn(shape, generator=g, device="cuda") * 1.5 + 0.3).to(dtype)
+
+    t = {"x": rn(rows, cols), "y": rn(rows, cols), "gate": rn(rows, cols) if gate else None}
+    t.update({k: rn(cols, dtype=F) for k in ("w_post", "b_post", "w_pre", "b_pre")})
+    return t, rn(rows, cols), rn(rows, cols)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [0.0, 1e-30])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("cols,groups,io", [(40, 5, F), (96, 3, F), (1152, 9, BF), (1008, 2, BF), (771, 3, F), (1544, 8, F),
+                                            (2056, 257, BF)])
+def test_no_eps(L, cols, groups, io, kind, eps):
+    """eps = 0, or too small to matter, is the bare formula on rows that vary: rows that leave threads without a
+    vector, groups within a warp and through shared memory."""
+    for rows, gate in ((11, "silu"), (300, "none")):
+        t, dX, dH = leaves(rows, cols, io, cols + rows, gate != "none")
+        leaf = {k: None if v is None else v.double().requires_grad_() for k, v in t.items()}
+        x, h = formula(leaf, groups, kind, gate, 0.7, eps)
+        ((x * dX.double()).sum() + (h * dH.double()).sum()).backward()
+        p = L.BlockNorm(rows, cols, groups, kind, gate, 0.7, eps, io, backward=True)
+        got = p.forward(t["x"], t["y"], t["gate"], t["w_post"], t["w_pre"], t["b_post"], t["b_pre"])
+        got.update(p.backward(t["x"], t["y"], t["gate"], t["w_post"], t["w_pre"], dX, dH, t["b_post"], t["b_pre"]))
+        want = {"X": x, "H": h, **{"d" + k: v.grad for k, v in leaf.items() if v is not None}}
+        assert set(got) == set(want)
+        for k, v in want.items():
+            v = v.detach()
+            assert torch.isfinite(got[k]).all(), k
+            assert (got[k].double() - v).norm() < TOL[got[k].dtype] * v.norm(), k
