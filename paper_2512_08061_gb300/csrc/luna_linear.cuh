@@ -52,7 +52,8 @@ __device__ __forceinline__ void clear_status(int clear, int *status) {
     if (clear && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *status = 0;
 }
 
-// The standard normal distribution function and its density.  With fp32 outputs by erff; with bf16
+// The standard normal distribution function and its density.  With fp32 outputs by erfcf, which keeps the
+// lower tail (1 + erff(z / sqrt 2) cancels there: 2e-2 of it at z = -4.8, all of it at -6); with bf16
 // outputs the upper tail from Abramowitz and Stegun 7.1.26 (erfc(x) = t (a1 + ... + a5 t^4) e^{-x^2},
 // t = 1 / (1 + p x)), which shares its exponential with the density and keeps Phi(z) below zero to
 // 2^-9 relative down to z = -5: 12 operations against about 40 an element, which the epilogue of a
@@ -61,7 +62,7 @@ template <typename IO>
 __device__ __forceinline__ float normal_cdf(float z, float &density) {
     const float e = __expf(-0.5f * z * z);
     density = 0.39894228040143268f * e;
-    if (sizeof(IO) == 4) return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    if (sizeof(IO) == 4) return 0.5f * erfcf(z * -0.70710678118654752f);
     const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
     float q = fmaf(t, 1.061405429f, -1.453152027f);
     q = fmaf(t, q, 1.421413741f);
