@@ -60,9 +60,12 @@ __device__ __forceinline__ void clear_status(int clear, int *status) {
 // product of depth 1024 has no time for.
 template <typename IO>
 __device__ __forceinline__ float normal_cdf(float z, float &density) {
+    if (sizeof(IO) == 4) {
+        density = 0.39894228040143268f * expf(-0.5f * z * z);
+        return 0.5f * erfcf(z * -0.70710678118654752f);
+    }
     const float e = __expf(-0.5f * z * z);
     density = 0.39894228040143268f * e;
-    if (sizeof(IO) == 4) return 0.5f * erfcf(z * -0.70710678118654752f);
     const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
     float q = fmaf(t, 1.061405429f, -1.453152027f);
     q = fmaf(t, q, 1.421413741f);
@@ -72,13 +75,22 @@ __device__ __forceinline__ float normal_cdf(float z, float &density) {
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
+// s = 1 / (1 + e^-z) and 1 - s for fp32 outputs, both whole in their tails; the exponential never overflows, and
+// the divisor in [1, 2] costs __fdividef 2 units at most.
+// (The bf16 forms below use __expf and __fdividef, whose errors grow with |z| to some 2^-17, far under a bf16 unit.)
+__device__ __forceinline__ float sigmoid_pair(float z, float &rest) {
+    const float e = expf(-fabsf(z)), big = __fdividef(1.0f, 1.0f + e), small = e * big;
+    rest = z < 0.0f ? big : small;
+    return z < 0.0f ? small : big;
+}
+
 template <typename IO>
 __device__ __forceinline__ float linear_act(float z, int act) {
     float d;
     switch (act) {
         case LUNA_LINEAR_RELU: return z > 0.0f ? z : (z == z ? 0.0f : z);
         case LUNA_LINEAR_GELU: return z * normal_cdf<IO>(z, d);
-        case LUNA_LINEAR_SILU: return __fdividef(z, 1.0f + __expf(-z));
+        case LUNA_LINEAR_SILU: return sizeof(IO) == 4 ? z * sigmoid_pair(z, d) : __fdividef(z, 1.0f + __expf(-z));
     }
     return z;
 }
@@ -94,8 +106,14 @@ __device__ __forceinline__ float linear_slope(float z, int act) {
             return fmaf(z, d, c);
         }
         case LUNA_LINEAR_SILU: {
-            const float s = __fdividef(1.0f, 1.0f + __expf(-z));
-            return s * (1.0f + z * (1.0f - s));
+            float s, rest;
+            if (sizeof(IO) == 4) {
+                s = sigmoid_pair(z, rest);
+            } else {
+                s = __fdividef(1.0f, 1.0f + __expf(-z));
+                rest = 1.0f - s;
+            }
+            return s * (1.0f + z * rest);
         }
     }
     return 1.0f;

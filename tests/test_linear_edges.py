@@ -36,3 +36,42 @@ def test_gelu_below_zero_in_fp32(L, m, n, k, shift):
     y.backward(dY.double())
     for name, v in (("Y", y.detach()), ("dX", z.grad @ W.double()), ("dW", z.grad.t() @ x.double())):
         assert (got[name].double() - v).norm() < TOL[F] * v.norm(), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_fp32_activations_element_by_element(L, act):
+    """A layer of one weight of 1: its pre-activations are the inputs and its input gradients the slopes, both to
+    fp32 accuracy of each value.  Bounds by CUDA's stated errors, in units of 2^-23 of a value or, for a slope, of
+    its two terms: SiLU at most 2 for expf, 1 for the sum, 2 for the quotient, 1 a product: 7, taken as 8.  GELU
+    4 for erfcf and 2 for expf, 2 for the products and z^2 / 2 for the rounding of z^2 and of z / sqrt 2 (at most
+    2^-23 of it, and the tail's logarithm is -z^2 / 2, to twice that with the density's): z^2 + 8."""
+    unit = 2.0 ** -23
+    x = torch.linspace(-12.5 if act == "gelu" else -86.0, 30.0, 4099, device="cuda").view(-1, 1)
+    W = torch.ones((1, 1), device="cuda")
+    p = L.Linear(x.shape[0], 1, 1, act, F, backward=True)
+    Y, Z = p.forward(x, W, save_z=True)
+    assert torch.equal(Z, x)
+    got = p.backward(x, W, torch.ones_like(x), Z)["dX"].double()
+    z = x.double()
+    if act == "gelu":
+        terms = [0.5 * torch.erfc(-z * 0.5 ** 0.5), z * torch.exp(-0.5 * z * z) * (2 * torch.pi) ** -0.5]
+        bound = (z * z + 8) * unit
+        value = z * terms[0]
+    else:
+        s, rest = 1 / (1 + torch.exp(-z)), 1 / (1 + torch.exp(z))
+        terms, bound, value = [s, z * s * rest], 8 * unit, z * s
+    tiny = 2.0 ** -126  # (below it fp32 has fewer bits)
+    assert ((Y.double() - value).abs() <= bound * value.abs() + tiny).all()
+    assert ((got - sum(terms)).abs() <= bound * sum(t.abs() for t in terms) + tiny).all()
+
+
+@pytest.mark.gpu
+def test_fp32_silu_ends(L):
+    """Down to the smallest normal result, and at the infinities."""
+    x = torch.tensor([[-87.5], [-89.0], [-90.5], [-1e30], [1e30], [float("inf")], [float("nan")], [0.0]], device="cuda")
+    W = torch.ones((1, 1), device="cuda")
+    y = L.Linear(8, 1, 1, "silu", F).forward(x, W).double()
+    want = x.double() * torch.sigmoid(x.double())
+    assert ((y - want)[:3].abs() <= 8 * 2.0 ** -23 * want[:3].abs() + 100 * 2.0 ** -149).all() and (y[:3] < 0).all()
+    assert y[3] == 0 and y[4] == x[4] and y[5] == float("inf") and y[6].isnan() and y[7] == 0
