@@ -432,7 +432,9 @@ luna_status luna_norm_bwd(const luna_norm_desc *nd, const void *x, const void *y
  * leading dimension apart (ld*, in elements; 0 = the row's width, else at least
  * that).  bias and R may be NULL; R may be Y.  Z, where not NULL, receives the
  * pre-activation, which luna_linear_bwd needs with an activation.  GELU is the
- * erf form.  Sums are fp32.
+ * erf form.  Sums are fp32; the tensor cores' additions cut off instead of
+ * rounding (1e-4 of a sum of 65536 positive products), so longer sums are joined
+ * by rounded additions every 16384 products.
  * bf16 runs on tensor cores (with n or k that is not a multiple of 8 from
  * aligned copies of the operands in the workspace; a matrix that is off a
  * 16-byte boundary, or whose leading dimension is not a multiple of 8, although

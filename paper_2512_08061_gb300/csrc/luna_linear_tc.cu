@@ -22,7 +22,10 @@
 // again (917 us at 4096 x 4096 x 4096, now 719 us, of which the splitting takes 60).  The tensor cores add to their fp32 accumulator by cutting off,
 // which at a depth of 1024 has lost 1.7e-6 of a sum of positive products and at 64 1e-7 (measured), so
 // after every 64 of K the epilogue's warps add the accumulator to an fp32 sum that they keep in TMEM
-// beside it.
+// beside it.  bf16 sums over more than 65536 of K are joined like this every 16384 (LONG): cut off all the
+// way, 2^20 rows of positive products lost 6.9e-3 of a weight's gradient, twice its bf16 rounding, 65536 rows
+// 1e-4.  The fp32 sum takes the place of the second accumulator there (5.14 ms at 2^20 x 1600
+// x 1600 against 5.05 without it).
 #include "luna_linear.cuh"
 
 #include <algorithm>
@@ -42,14 +45,16 @@ using namespace sm100;
 constexpr int kEpiWarps = 8, kWarpTma = 8, kWarpMma = 9, kTcThreads = 320;
 constexpr int kDepth = 64;  // K of a stage
 
-template <typename IO, int CG, int BN> struct Tile {
+template <typename IO, int CG, int BN, bool LONG = false> struct Tile {
     static constexpr bool PLANES = sizeof(IO) == 4;   // fp32 operands in three bf16 planes
+    static constexpr bool JOIN = PLANES || LONG;      // accumulators joined in an fp32 sum
     static constexpr int BM = 128;                    // rows of a CTA
     static constexpr int NB = BN / CG;                // B rows a CTA holds
     static constexpr int NBL = NB < 64 ? 64 : NB;     // ... and loads (an MN-major slice is 64 wide)
     static constexpr uint32_t A_BYTES = BM * 128, B_BYTES = NBL * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = (int)((192 * 1024) / STAGE) > 8 ? 8 : (int)((192 * 1024) / STAGE);
-    static constexpr uint32_t COLS = PLANES ? 4 * BN : 2 * BN;  // two accumulators (and the fp32 sum)
+    static constexpr int ACCS = LONG ? 1 : 2;         // accumulators, and after them the fp32 sum
+    static constexpr uint32_t COLS = PLANES ? 4 * BN : 2 * BN;
     static constexpr uint32_t OUT = kEpiWarps * 4096;   // two 32 x 32 pieces of every epilogue warp
     static constexpr uint32_t SMEM = STAGES * STAGE + OUT + 1024 + 256;
     static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -59,6 +64,7 @@ struct ProductTc {
     Product p;
     int tiles_m, tiles_n, splits, k_steps, steps_per_split;  // tiles of BM * CG rows, BN columns
     int per;        // 64-deep slices of an operand (of each plane of it)
+    int join;       // steps of an accumulator, where they are joined
     bool swap;      // the product is computed transposed: A = the layer's B (few rows of X)
     bool vec;       // outputs and residual on 16-byte boundaries: the epilogue stores by TMA
 };
@@ -84,6 +90,7 @@ __device__ __forceinline__ void unit_tile(const ProductTc &a, int u, int &tm, in
 }
 
 constexpr int kPlanes = 3, kTerms = 6;
+constexpr int kLong = 65536, kJoin = 16384;  // K of a bf16 sum from which it is joined, and every how many
 
 // 32 columns of a lane's row (`cols` of them inside the output) into the warp's pieces (64-byte rows,
 // swizzled) and on to the output's rows row0 .. row0 + 31; there are two pieces.
@@ -179,12 +186,12 @@ template <typename IO, int ACT> __device__ __forceinline__ void act32(float (&v)
     for (int i = 0; i < 32; ++i) v[i] = linear_act<IO>(v[i], ACT);
 }
 
-template <typename IO, int CG, int BN>
+template <typename IO, int CG, int BN, bool LONG>
 __global__ void __launch_bounds__(kTcThreads, 1)
     k_product_tc(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                  const __grid_constant__ CUtensorMap mapO, const __grid_constant__ CUtensorMap mapZ,
                  const __grid_constant__ ProductTc a) {
-    using T = Tile<IO, CG, BN>;
+    using T = Tile<IO, CG, BN, LONG>;
     constexpr int S = T::STAGES;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = align_1024(smem_raw);
@@ -278,10 +285,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     if (CG == 2) mma_commit_pair(empty + st);
                     else mma_commit(empty + st);
                 };
-                // (one accumulator for all of them, or for every three planes)
+                // (one accumulator for all of them, for every three planes, or for every `join` steps)
                 for (int s = from; s < to && !failed; ++n) {
-                    const int acc = n & 1;
-                    wait(tempty + acc, ((n >> 1) & 1) ^ 1);
+                    const int acc = n % T::ACCS;
+                    wait(tempty + acc, ((n / T::ACCS) & 1) ^ 1);
                     tc_fence_after();
                     const uint32_t d = tbase + acc * BN;
                     if (T::PLANES) {
@@ -300,12 +307,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         product(d, st[0], st[0], false);
                         for (int q = 0; q < kPlanes; ++q) release(st[q]);
                     } else {
-                        for (; s < to; ++s, ++it) {
+                        const int end = T::JOIN ? min(to, s + a.join) : to;
+                        for (bool fresh = true; s < end; ++s, ++it, fresh = false) {
                             const int st = it % S;
                             wait(full + st, (it / S) & 1);
                             if (failed) break;
                             tc_fence_after();
-                            product(d, st, st, s == from);
+                            product(d, st, st, fresh);
                             release(st);
                         }
                         if (failed) break;
@@ -322,22 +330,23 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         int n = 0, stored = 0;
         constexpr int CH = BN / 32;  // chunks of 32 columns, in halves
         const int c0 = half * ((CH + 1) / 2), c1 = half ? CH : (CH + 1) / 2;
-        const uint32_t sum = tbase + lane_base + 2 * BN;
+        const uint32_t sum = tbase + lane_base + T::ACCS * BN;
         for (int u = first; u < units && !failed; u += stride, ++n) {
             int tm, tn, sp;
             unit_tile(a, u, tm, tn, sp);
             int more = 0;  // accumulators before the last one
-            if (T::PLANES) {
+            if (T::JOIN) {
                 const int steps = min(a.k_steps - sp * a.steps_per_split, a.steps_per_split);
-                more = steps / kPlanes - 1;
+                more = (steps - 1) / a.join;
                 for (int i = 0; i < more && !failed; ++i, ++n) {
-                    wait(tfull + (n & 1), (n >> 1) & 1);
+                    const int acc = n % T::ACCS;
+                    wait(tfull + acc, (n / T::ACCS) & 1);
                     if (__any_sync(0xffffffffu, failed)) break;
                     tc_fence_after();
 #pragma unroll 1
                     for (int c = c0; c < c1; ++c) {
                         uint32_t x[32];
-                        tmem_ld32(tbase + lane_base + (n & 1) * BN + 32 * c, x);
+                        tmem_ld32(tbase + lane_base + acc * BN + 32 * c, x);
                         if (i) {
                             uint32_t y[32];
                             tmem_ld32(sum + 32 * c, y);
@@ -353,14 +362,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
-                        if (CG == 2) mbar_arrive_cluster(tempty_leader[n & 1]);
-                        else mbar_arrive(tempty + (n & 1));
+                        if (CG == 2) mbar_arrive_cluster(tempty_leader[acc]);
+                        else mbar_arrive(tempty + acc);
                     }
                 }
                 if (__any_sync(0xffffffffu, failed)) break;
             }
-            const int acc = n & 1;
-            wait(tfull + acc, (n >> 1) & 1);
+            const int acc = n % T::ACCS;
+            wait(tfull + acc, (n / T::ACCS) & 1);
             if (__any_sync(0xffffffffu, failed)) break;
             tc_fence_after();
             const int64_t row = (int64_t)(tm * CG + (int)rank) * T::BM + quarter * 32 + lane;
@@ -374,7 +383,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 float v[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = last_split_empty ? 0.0f : __uint_as_float(x[i]);
-                if (T::PLANES && more) {
+                if (T::JOIN && more) {
                     tmem_ld32(sum + 32 * c, x);
                     tmem_wait_ld();
 #pragma unroll
@@ -503,9 +512,9 @@ Choice cost(const Product &p) {
                               (splits > 1 ? kTileCycles : 0)};
 }
 
-template <typename IO, int CG, int BN>
+template <typename IO, int CG, int BN, bool LONG = false>
 cudaError_t launch(ProductTc a, cudaStream_t s) {
-    using T = Tile<IO, CG, BN>;
+    using T = Tile<IO, CG, BN, LONG>;
     Product &p = a.p;
     const int64_t M = a.swap ? p.N : p.M, N = a.swap ? p.M : p.N;
     if (a.swap) std::swap(p.A, p.B);
@@ -513,6 +522,7 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     a.tiles_n = (int)cdiv(N, BN);
     a.per = (int)cdiv(p.K, kDepth);
     a.k_steps = a.per * (T::PLANES ? kPlanes : 1);
+    a.join = T::PLANES ? kPlanes : kJoin / kDepth;
     const int64_t K = T::PLANES ? 3 * (int64_t)a.per * kDepth : p.K;  // of the operands as they are stored
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     a.splits = linear_splits(p, tiles * CG, 256);
@@ -525,7 +535,7 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     mO = mZ = mA;
     if (a.vec && (!output_map(&mO, p.out, p.ldo, M, N, sizeof(IO) / 2) || (p.Z && !output_map(&mZ, p.Z, p.ldz, M, N, sizeof(IO) / 2))))
         return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(k_product_tc<IO, CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(k_product_tc<IO, CG, BN, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM);
     if (e != cudaSuccess) return e;
     const int sms = tc_sm_count() / CG * CG;
     const int grid = (int)std::min<int64_t>(tiles * a.splits * CG, sms);
@@ -542,7 +552,7 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     cfg.attrs = at;
     cfg.numAttrs = CG == 2 ? 1 : 0;
     prof_before("product_tc", s);
-    e = cudaLaunchKernelEx(&cfg, k_product_tc<IO, CG, BN>, mA, mB, mO, mZ, a);
+    e = cudaLaunchKernelEx(&cfg, k_product_tc<IO, CG, BN, LONG>, mA, mB, mO, mZ, a);
     prof_after("product_tc", s);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || splits == 1) return e;
     return launch_product_finish(p, splits, T::PLANES ? LUNA_F32 : LUNA_BF16, s);
@@ -557,18 +567,24 @@ cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s) {
     a.p = p;
     a.swap = false;
     a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % unit == 0 && p.ldr % unit == 0 && p.ldz % unit == 0;
+    const auto is_long = [&](int splits) { return cdiv(p.K, splits) > kLong; };
     if (p.M <= 64) {  // few rows of X: the weight's rows fill the tile's 128 rows, X's are its columns
         a.swap = true;
         // (an MN-major slice is 64 wide)
-        if (io == LUNA_F32) return p.M <= 32 && !p.A.kt ? launch<float, 1, 32>(a, s) : launch<float, 1, 64>(a, s);
-        return p.M <= 32 && !p.A.kt ? launch<B, 1, 32>(a, s) : launch<B, 1, 64>(a, s);
+        const bool narrow = p.M <= 32 && !p.A.kt;
+        if (io == LUNA_F32) return narrow ? launch<float, 1, 32>(a, s) : launch<float, 1, 64>(a, s);
+        if (is_long(linear_splits(p, cdiv(p.N, 128), 256))) return launch<B, 1, 64, true>(a, s);
+        return narrow ? launch<B, 1, 32>(a, s) : launch<B, 1, 64>(a, s);
     }
     if (io == LUNA_F32)  // (the fp32 sum leaves no room for 256 columns in TMEM)
         return cost<float, 2, 128>(p).cycles <= cost<float, 1, 128>(p).cycles ? launch<float, 2, 128>(a, s)
                                                                              : launch<float, 1, 128>(a, s);
-    const double pair = cost<B, 2, 256>(p).cycles, wide = cost<B, 1, 256>(p).cycles, half = cost<B, 1, 128>(p).cycles;
-    if (pair <= wide && pair <= half) return launch<B, 2, 256>(a, s);
-    return wide <= half ? launch<B, 1, 256>(a, s) : launch<B, 1, 128>(a, s);
+    const Choice pair = cost<B, 2, 256>(p), wide = cost<B, 1, 256>(p), half = cost<B, 1, 128>(p);
+    const bool paired = pair.cycles <= wide.cycles && pair.cycles <= half.cycles, widest = wide.cycles <= half.cycles;
+    if (is_long(paired ? pair.splits : widest ? wide.splits : half.splits))
+        return pair.cycles <= wide.cycles ? launch<B, 2, 256, true>(a, s) : launch<B, 1, 256, true>(a, s);
+    if (paired) return launch<B, 2, 256>(a, s);
+    return widest ? launch<B, 1, 256>(a, s) : launch<B, 1, 128>(a, s);
 }
 
 }  // namespace luna

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_linear import F, TOL, matrix
+from test_linear import BF, F, TOL, matrix
 
 
 @pytest.fixture(scope="module")
@@ -75,3 +75,35 @@ def test_fp32_silu_ends(L):
     want = x.double() * torch.sigmoid(x.double())
     assert ((y - want)[:3].abs() <= 8 * 2.0 ** -23 * want[:3].abs() + 100 * 2.0 ** -149).all() and (y[:3] < 0).all()
     assert y[3] == 0 and y[4] == x[4] and y[5] == float("inf") and y[6].isnan() and y[7] == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k,direction", [((1 << 20) + 37, 1600, 1600, "dW"), (131100, 40, 20000, "dW"), (20, 20000, 131136, "Y"),
+                                             (300, 16000, 70000, "Y")])
+def test_long_sums_of_positive_products(L, m, n, k, direction):
+    """Tensor cores cut their fp32 additions off, which on sums of one sign adds up: 1024 additions of 16 products
+    lose at most 2^-13, and then the sum is joined with the others in rounded additions.  With the value's own
+    rounding (half a unit of eight bits: 2^-8 at most) every value is within 2^-8 + 2^-13."""
+    g = torch.Generator("cuda").manual_seed(6)
+
+    def positive(rows, cols):
+        t = torch.empty((rows, cols), device="cuda", dtype=BF)
+        for a in range(0, rows, 1 << 16):
+            t[a:a + (1 << 16)] = torch.rand(t[a:a + (1 << 16)].shape, generator=g, device="cuda") * 0.5 + 0.5
+        return t
+
+    p = L.Linear(m, n, k, "none", BF, backward=direction == "dW")
+    x = positive(m, k)
+    want = 0.0
+    if direction == "dW":
+        dY, W = positive(m, n), torch.empty((n, k), device="cuda", dtype=BF)
+        got = p.backward(x, W, dY, out={"dW": W})["dW"][:16]
+        for a in range(0, m, 1 << 16):
+            want = want + dY[a:a + (1 << 16), :16].double().t() @ x[a:a + (1 << 16)].double()
+    else:
+        W = positive(n, k)
+        got = p.forward(x, W)[:16]
+        for a in range(0, k, 1 << 12):
+            want = want + x[:16, a:a + (1 << 12)].double() @ W[:, a:a + (1 << 12)].double().t()
+    assert L.luna_device_status(p.ws) == 0
+    assert ((got.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -13) * want).all()
