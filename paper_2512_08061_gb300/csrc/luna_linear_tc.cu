@@ -566,7 +566,8 @@ cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s) {
     ProductTc a;
     a.p = p;
     a.swap = false;
-    a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % unit == 0 && p.ldr % unit == 0 && p.ldz % unit == 0;
+    a.vec = al16(p.out) && al16(p.R) && al16(p.Z) && al16(p.bias) && p.ldo % unit == 0 && (!p.R || p.ldr % unit == 0) &&
+            (!p.Z || p.ldz % unit == 0);
     const auto is_long = [&](int splits) { return cdiv(p.K, splits) > kLong; };
     if (p.M <= 64) {  // few rows of X: the weight's rows fill the tile's 128 rows, X's are its columns
         a.swap = true;

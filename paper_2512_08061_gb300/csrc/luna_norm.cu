@@ -580,12 +580,14 @@ bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 bool vectors_ok(const NormArgs &a, int vec) {
     if (a.cols % vec || (a.w_post && (a.cols / a.groups) % vec)) return false;
-    for (const void *p : {a.x, a.y, a.gate, a.dX, a.dH, (const void *)a.X, (const void *)a.H, (const void *)a.dx,
-                          (const void *)a.dy, (const void *)a.dgate, (const void *)a.w_post, (const void *)a.b_post,
-                          (const void *)a.w_pre, (const void *)a.b_pre})
+    for (const void *p : {a.w_post, a.b_post, a.w_pre, a.b_pre})
         if (!al16(p)) return false;
-    for (int64_t ld : {a.ldx, a.ldy, a.ldgate, a.ldX, a.ldH, a.lddX, a.lddH, a.lddx, a.lddy, a.lddgate})
-        if (ld % vec) return false;
+    // (the leading dimension of a matrix that the call does not have means nothing)
+    const struct { const void *p; int64_t ld; } rows[] = {{a.x, a.ldx}, {a.y, a.ldy}, {a.gate, a.ldgate}, {a.X, a.ldX},
+                                                          {a.H, a.ldH}, {a.dX, a.lddX}, {a.dH, a.lddH}, {a.dx, a.lddx},
+                                                          {a.dy, a.lddy}, {a.dgate, a.lddgate}};
+    for (const auto &r : rows)
+        if (r.p && (!al16(r.p) || r.ld % vec)) return false;
     return true;
 }
 

@@ -622,6 +622,7 @@ class Decay(_Checked):
 def _set_rows(desc, field: str, name: str, t, shape, dtype, device) -> None:
     """Checks a matrix of contiguous rows and puts the distance of its rows into a descriptor."""
     if t is None:
+        setattr(desc, field, 0)
         return
     _want(name, t, shape, dtype, device)
     if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):

@@ -50,3 +50,28 @@ def test_no_eps(L, cols, groups, io, kind, eps):
             v = v.detach()
             assert torch.isfinite(got[k]).all(), k
             assert (got[k].double() - v).norm() < TOL[got[k].dtype] * v.norm(), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols,groups,io", [(512, 4, F), (2048, 1, BF)])
+def test_rows_of_absent_matrices(L, cols, groups, io):
+    """A leading dimension of a matrix that the call does not have changes nothing: equal bits (the form for rows
+    off their boundaries sums in another order)."""
+    t, _, dH = leaves(64, cols, io, 5, gate=False)
+    p = L.BlockNorm(64, cols, groups, "rms", "none", 0.5, io=io, backward=True)
+    odd = torch.randn((64, cols + 1), device="cuda").to(io)[:, :cols]
+
+    def call(x, dX):
+        return {**p.forward(x, t["y"], None, t["w_post"], t["w_pre"]),
+                **p.backward(x, t["y"], None, t["w_post"], t["w_pre"], dX, dH)}
+
+    want = call(None, None)
+    call(odd, odd)
+    got = call(None, None)
+    assert set(got) == set(want) and all(torch.equal(got[k], want[k]) for k in want)
+    # the same of a descriptor's own fields
+    nd = L.norm_desc(64, cols, groups, res_scale=0.5, io=L._DTYPES[io])
+    nd.ldx = nd.ldgate = nd.ldX = cols + 1
+    h = torch.empty_like(t["y"])
+    L.luna_norm_fwd(nd, None, t["y"], None, t["w_post"], None, t["w_pre"], None, None, h)
+    assert torch.equal(h, want["H"])
