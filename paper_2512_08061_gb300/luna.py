@@ -464,8 +464,16 @@ def _want(name: str, t, shape, dtype, device) -> None:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: {t.dtype}, expected {dtype}")
-    if t.device.type != device.type or (device.index is not None and t.device.index != device.index):
+    if t.device != device:
         raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _place(device) -> torch.device:
+    """A device with its number: "cuda" is the GPU that is current now, and tensors of another one are refused."""
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        return torch.device("cuda", torch.cuda.current_device())
+    return device
 
 
 def _dense(name: str, t) -> None:
@@ -527,7 +535,7 @@ class Decay(_Checked):
     def __init__(self, B, H, n, d, dv, Hkv=None, scale=None, io=torch.bfloat16, device="cuda", backward=False):
         self.dd = decay_desc(B, H, n, d, dv, Hkv, scale, _DTYPES[io])
         super().__init__(self.dd)
-        self.io, self.device = io, torch.device(device)
+        self.io, self.device = io, _place(device)
         self.ws = alloc_bytes(luna_decay_workspace_size(self.dd, backward), self.device)
         self._ws = (self.ws.data_ptr(), self.ws.numel())
         self.shapes = {"q": (B, H, n, d), "k": (B, self.dd.Hkv, n, d), "v": (B, self.dd.Hkv, n, dv), "o": (B, H, n, dv)}
@@ -639,7 +647,7 @@ class BlockNorm(_Checked):
                  device="cuda", backward=False):
         self.nd = norm_desc(rows, cols, groups, kind, gate, res_scale, eps, _DTYPES[io])
         super().__init__(self.nd)
-        self.io, self.device, self.shape = io, torch.device(device), (rows, cols)
+        self.io, self.device, self.shape = io, _place(device), (rows, cols)
         self.ws = alloc_bytes(luna_norm_workspace_size(self.nd), self.device) if backward else None
         self._ws = (self.ws.data_ptr(), self.ws.numel()) if backward else (None, 0)
 
@@ -695,7 +703,7 @@ class Linear(_Checked):
     def __init__(self, m, n, k, act="none", io=torch.bfloat16, device="cuda", backward=False):
         self.ld = linear_desc(m, n, k, act, _DTYPES[io])
         super().__init__(self.ld)
-        self.io, self.device, self.m, self.n, self.k = io, torch.device(device), m, n, k
+        self.io, self.device, self.m, self.n, self.k = io, _place(device), m, n, k
         self.ws = alloc_bytes(max(luna_linear_workspace_size(self.ld, b) for b in ((False, True) if backward else (False,))),
                               self.device)
         self._ws = (self.ws.data_ptr(), self.ws.numel())
