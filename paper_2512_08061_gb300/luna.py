@@ -502,6 +502,15 @@ def _handle(stream):
     return _raw_stream(torch.cuda.current_device())
 
 
+def _new(stream, make, *args, **kwargs):
+    """A new tensor for a call on `stream` (None: the current one), from that stream's memory: the allocator may
+    hand it out again only behind the call's kernels."""
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(stream):
+        return make(*args, **kwargs)
+
+
 class _Checked:
     """Calls of one problem shape.  The arguments' shapes, strides, types and devices are looked at in full
     when they differ from those of the last call of the same kind, and their strides put into that
@@ -511,6 +520,21 @@ class _Checked:
         self._desc = {kind: type(desc).from_buffer_copy(desc) for kind in ("forward", "backward", "step")}
         self._ref = {kind: ctypes.byref(d) for kind, d in self._desc.items()}
         self._seen = {}
+        self.ws, self._ws, self._streams = None, (None, 0), set()
+
+    def _workspace(self, nbytes: int) -> None:
+        self.ws = alloc_bytes(nbytes, self.device)
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
+        if self.device.type == "cuda":
+            self._streams = {_handle(None)}
+
+    def _on(self, stream):
+        """The handle of the stream of a call; the workspace stays until what is queued there is done."""
+        handle = _handle(stream)
+        if handle not in self._streams and self.ws is not None:
+            self.ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
+            self._streams.add(handle)
+        return handle
 
     def _looked_at(self, kind: str, *tensors) -> bool:
         """Whether these layouts are the last call's; the caller checks and fills in the descriptor if not."""
@@ -536,8 +560,7 @@ class Decay(_Checked):
         self.dd = decay_desc(B, H, n, d, dv, Hkv, scale, _DTYPES[io])
         super().__init__(self.dd)
         self.io, self.device = io, _place(device)
-        self.ws = alloc_bytes(luna_decay_workspace_size(self.dd, backward), self.device)
-        self._ws = (self.ws.data_ptr(), self.ws.numel())
+        self._workspace(luna_decay_workspace_size(self.dd, backward))
         self.shapes = {"q": (B, H, n, d), "k": (B, self.dd.Hkv, n, d), "v": (B, self.dd.Hkv, n, dv), "o": (B, H, n, dv)}
         self.state_shape = (B, H, d, dv)
 
@@ -575,29 +598,29 @@ class Decay(_Checked):
             self._states(S0=S0, S1=S1)
             # a new output lies as V does, or Q
             self._like = next((tuple(torch.empty_like(t).stride()) for t in (V, Q) if t.shape == self.shapes["o"]), None)
-            self._view("forward", "o", self._new_output(Q) if O is None else O)
+            self._view("forward", "o", self._new_output(Q, stream) if O is None else O)
             self._accept()
         if O is None:
-            O = self._new_output(Q)
+            O = self._new_output(Q, stream)
         if want_state and S1 is None:
-            S1 = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
+            S1 = _new(stream, torch.empty, self.state_shape, dtype=torch.float32, device=Q.device)
         _check(_lib.luna_decay_fwd(self._ref["forward"], log_decay.data_ptr(), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-                                   _addr(lengths), _addr(S0), O.data_ptr(), _addr(S1), *self._ws, _handle(stream)),
+                                   _addr(lengths), _addr(S0), O.data_ptr(), _addr(S1), *self._ws, self._on(stream)),
                "luna_decay_fwd")
         return (O, S1) if want_state else O
 
-    def _new_output(self, Q):
+    def _new_output(self, Q, stream):
         shape = self.shapes["o"]
         if self._like is None:
-            return torch.empty(shape, dtype=self.io, device=Q.device)
-        return torch.empty_strided(shape, self._like, dtype=self.io, device=Q.device)
+            return _new(stream, torch.empty, shape, dtype=self.io, device=Q.device)
+        return _new(stream, torch.empty_strided, shape, self._like, dtype=self.io, device=Q.device)
 
     def backward(self, Q, K, V, dO, log_decay, lengths=None, S0=None, dS1=None, out=None, stream=None):
         """dQ, dK, dV, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
         if out is None:
-            out = {"dQ": torch.empty_like(Q), "dK": torch.empty_like(K), "dV": torch.empty_like(V)}
+            out = {"d" + k: _new(stream, torch.empty_like, t) for k, t in (("Q", Q), ("K", K), ("V", V))}
             if S0 is not None:
-                out["dS0"] = torch.empty(self.state_shape, dtype=torch.float32, device=Q.device)
+                out["dS0"] = _new(stream, torch.empty, self.state_shape, dtype=torch.float32, device=Q.device)
         dQ, dK, dV, dS0 = out["dQ"], out["dK"], out["dV"], out.get("dS0")
         if not self._looked_at("backward", Q, K, V, dO, log_decay, lengths, S0, dS1, dQ, dK, dV, dS0):
             for field, t in (("q", Q), ("k", K), ("v", V), ("go", dO), ("gq", dQ), ("gk", dK), ("gv", dV)):
@@ -607,13 +630,13 @@ class Decay(_Checked):
             self._accept()
         _check(_lib.luna_decay_bwd(self._ref["backward"], log_decay.data_ptr(), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
                                    dO.data_ptr(), _addr(lengths), _addr(S0), _addr(dS1), dQ.data_ptr(), dK.data_ptr(),
-                                   dV.data_ptr(), _addr(dS0), *self._ws, _handle(stream)), "luna_decay_bwd")
+                                   dV.data_ptr(), _addr(dS0), *self._ws, self._on(stream)), "luna_decay_bwd")
         return out
 
     def step(self, q, k, v, log_decay, S, slots=None, o=None, stream=None):
         """One token: q (B, H, d), k (B, Hkv, d), v (B, Hkv, dv); S (nslots, H, d, dv) is advanced in place."""
         if o is None:
-            o = torch.empty(self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=q.device)
+            o = _new(stream, torch.empty, self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=q.device)
         if not self._looked_at("step", q, k, v, log_decay, S, slots, o):
             for field, t in (("q", q), ("k", k), ("v", v), ("o", o)):
                 self._view("step", field, t)
@@ -622,7 +645,7 @@ class Decay(_Checked):
             self._vectors(log_decay, slots, "slots")
             self._accept()
         _check(_lib.luna_decay_step(self._ref["step"], log_decay.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                    _addr(slots), S.shape[0], S.data_ptr(), o.data_ptr(), _handle(stream)),
+                                    _addr(slots), S.shape[0], S.data_ptr(), o.data_ptr(), self._on(stream)),
                "luna_decay_step")
         return o
 
@@ -648,8 +671,8 @@ class BlockNorm(_Checked):
         self.nd = norm_desc(rows, cols, groups, kind, gate, res_scale, eps, _DTYPES[io])
         super().__init__(self.nd)
         self.io, self.device, self.shape = io, _place(device), (rows, cols)
-        self.ws = alloc_bytes(luna_norm_workspace_size(self.nd), self.device) if backward else None
-        self._ws = (self.ws.data_ptr(), self.ws.numel()) if backward else (None, 0)
+        if backward:
+            self._workspace(luna_norm_workspace_size(self.nd))
 
     def _rows(self, kind: str, **matrices) -> None:
         for name, t in matrices.items():
@@ -663,15 +686,15 @@ class BlockNorm(_Checked):
     def forward(self, x, y, gate=None, w_post=None, w_pre=None, b_post=None, b_pre=None, X=None, H=None, stream=None):
         """{"X": x'} where there is a residual or no second norm (or X is given), {"H": h} with w_pre."""
         if X is None and ((x is not None and y is not None) or w_pre is None):
-            X = torch.empty(self.shape, dtype=self.io, device=(y if x is None else x).device)
+            X = _new(stream, torch.empty, self.shape, dtype=self.io, device=(y if x is None else x).device)
         if H is None and w_pre is not None:
-            H = torch.empty(self.shape, dtype=self.io, device=(y if x is None else x).device)
+            H = _new(stream, torch.empty, self.shape, dtype=self.io, device=(y if x is None else x).device)
         if not self._looked_at("forward", x, y, gate, w_post, w_pre, b_post, b_pre, X, H):
             self._rows("forward", x=x, y=y, gate=gate, X=X, H=H)
             self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre)
             self._accept()
         _check(_lib.luna_norm_fwd(self._ref["forward"], _addr(x), _addr(y), _addr(gate), _addr(w_post), _addr(b_post),
-                                  _addr(w_pre), _addr(b_pre), _addr(X), _addr(H), _handle(stream)), "luna_norm_fwd")
+                                  _addr(w_pre), _addr(b_pre), _addr(X), _addr(H), self._on(stream)), "luna_norm_fwd")
         if X is None:
             return {"H": H}
         return {"X": X} if H is None else {"X": X, "H": H}
@@ -679,9 +702,9 @@ class BlockNorm(_Checked):
     def backward(self, x, y, gate, w_post, w_pre, dX, dH, b_post=None, b_pre=None, out=None, stream=None):
         """dx, dy, dgate, dw_post, dw_pre of what forward was given, and db_post, db_pre of given biases."""
         if out is None:
-            out = {k: torch.empty(self.shape, dtype=self.io, device=t.device)
+            out = {k: _new(stream, torch.empty, self.shape, dtype=self.io, device=t.device)
                    for k, t in (("dx", x), ("dy", y), ("dgate", gate)) if t is not None}
-            out.update({k: torch.empty_like(t)
+            out.update({k: _new(stream, torch.empty_like, t)
                         for k, t in (("dw_post", w_post), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
                         if t is not None})
         g = [out.get(k) for k in ("dx", "dy", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")]
@@ -692,7 +715,7 @@ class BlockNorm(_Checked):
             self._accept()
         _check(_lib.luna_norm_bwd(self._ref["backward"], _addr(x), _addr(y), _addr(gate), _addr(w_post), _addr(b_post),
                                   _addr(w_pre), _addr(dX), _addr(dH), *[_addr(t) for t in g], *self._ws,
-                                  _handle(stream)), "luna_norm_bwd")
+                                  self._on(stream)), "luna_norm_bwd")
         return out
 
 
@@ -704,9 +727,7 @@ class Linear(_Checked):
         self.ld = linear_desc(m, n, k, act, _DTYPES[io])
         super().__init__(self.ld)
         self.io, self.device, self.m, self.n, self.k = io, _place(device), m, n, k
-        self.ws = alloc_bytes(max(luna_linear_workspace_size(self.ld, b) for b in ((False, True) if backward else (False,))),
-                              self.device)
-        self._ws = (self.ws.data_ptr(), self.ws.numel())
+        self._workspace(max(luna_linear_workspace_size(self.ld, b) for b in ((False, True) if backward else (False,))))
 
     def _rows(self, kind: str, **matrices) -> None:
         shapes = {"x": (self.m, self.k), "dx": (self.m, self.k), "w": (self.n, self.k)}
@@ -720,24 +741,24 @@ class Linear(_Checked):
     def forward(self, x, W, bias=None, r=None, save_z=False, Y=None, Z=None, stream=None):
         """Y, or (Y, z) with save_z."""
         if Y is None:
-            Y = torch.empty((self.m, self.n), dtype=self.io, device=x.device)
+            Y = _new(stream, torch.empty, (self.m, self.n), dtype=self.io, device=x.device)
         if save_z and Z is None:
-            Z = torch.empty((self.m, self.n), dtype=self.io, device=x.device)
+            Z = _new(stream, torch.empty, (self.m, self.n), dtype=self.io, device=x.device)
         if not self._looked_at("forward", x, W, bias, r, Y, Z):
             self._rows("forward", x=x, w=W, r=r, y=Y, z=Z)
             self._vector("bias", bias, (self.n,))
             self._accept()
         _check(_lib.luna_linear_fwd(self._ref["forward"], x.data_ptr(), W.data_ptr(), _addr(bias), _addr(r), Y.data_ptr(),
-                                    _addr(Z), *self._ws, _handle(stream)), "luna_linear_fwd")
+                                    _addr(Z), *self._ws, self._on(stream)), "luna_linear_fwd")
         return (Y, Z) if save_z else Y
 
     def backward(self, x, W, dY, Z=None, bias=False, out=None, stream=None):
         """dX, dW and with `bias` db; Z is forward's z (needed with an activation)."""
         if out is None:
-            out = {"dX": torch.empty((self.m, self.k), dtype=self.io, device=dY.device),
-                   "dW": torch.empty((self.n, self.k), dtype=self.io, device=dY.device)}
+            out = {"dX": _new(stream, torch.empty, (self.m, self.k), dtype=self.io, device=dY.device),
+                   "dW": _new(stream, torch.empty, (self.n, self.k), dtype=self.io, device=dY.device)}
             if bias:
-                out["db"] = torch.empty(self.n, dtype=self.io, device=dY.device)
+                out["db"] = _new(stream, torch.empty, self.n, dtype=self.io, device=dY.device)
         dX, dW, db = out.get("dX"), out.get("dW"), out.get("db")
         if not self._looked_at("backward", x, W, Z, dY, dX, dW, db):
             self._rows("backward", x=x, w=W, z=Z, dy=dY, dx=dX)
@@ -745,5 +766,5 @@ class Linear(_Checked):
             self._vector("db", db, (self.n,))
             self._accept()
         _check(_lib.luna_linear_bwd(self._ref["backward"], x.data_ptr(), W.data_ptr(), _addr(Z), dY.data_ptr(), _addr(dX),
-                                    _addr(dW), _addr(db), *self._ws, _handle(stream)), "luna_linear_bwd")
+                                    _addr(dW), _addr(db), *self._ws, self._on(stream)), "luna_linear_bwd")
         return out

@@ -24,3 +24,49 @@ def test_a_device_has_its_number(L, monkeypatch):
         L._want("x", elsewhere, (4, 8), torch.float32, p.device)
     assert L.BlockNorm(4, 8, device="cpu").device == torch.device("cpu")
     assert L.BlockNorm(4, 8, device="cuda:1").device == torch.device("cuda", 1)
+
+
+@pytest.mark.gpu
+def test_memory_of_a_call_on_another_stream(L):
+    """What a call on a stream allocates is that stream's, and the workspace outlives what is queued there: neither
+    is handed out on the current stream while the call may still run.  (Sizes over 10 MB have blocks of their own,
+    which the allocator otherwise hands out again at once.)"""
+    io = dict(device="cuda", dtype=torch.bfloat16)
+    s = torch.cuda.Stream()
+    x, W = torch.randn((4096, 1024), **io), torch.randn((4096, 1024), **io)
+    q = torch.randn((2, 32, 1024, 128), **io)
+    rates = torch.full((32,), -0.1, device="cuda")
+    w = torch.ones(4096, device="cuda")
+    li = L.Linear(4096, 4096, 1024, "gelu", backward=True)
+    at = L.Decay(2, 32, 1024, 128, 128, backward=True)
+    nm = L.BlockNorm(4096, 4096, backward=True)
+    want, z = li.forward(x, W, save_z=True)
+    torch.cuda.synchronize()
+    calls = {
+        "linear": lambda: li.forward(x, W, save_z=True, stream=s),
+        "linear gradients": lambda: tuple(li.backward(x, W, want, z, stream=s).values())[:2],
+        "decay": lambda: at.forward(q, q, q, rates, stream=s),
+        "decay gradients": lambda: tuple(at.backward(q, q, q, q, rates, stream=s).values()),
+        "norm": lambda: tuple(nm.forward(None, want, None, w, w, stream=s).values()),
+        "norm gradients": lambda: (nm.backward(None, want, None, w, None, want, None, stream=s)["dy"],),
+    }
+    for name, call in calls.items():
+        out = call()
+        out = out if isinstance(out, tuple) else (out,)
+        there = {t.data_ptr(): (t.shape, t.dtype) for t in out}
+        del out
+        mine = [torch.empty(shape, dtype=dtype, device="cuda") for shape, dtype in there.values()]
+        assert not any(t.data_ptr() in there for t in mine), name
+        del mine
+    torch.cuda.synchronize()
+    assert torch.equal(li.forward(x, W, stream=s), want)
+    # the workspace of a plan that is gone
+    torch.cuda.synchronize()
+    size, there = li.ws.numel(), li.ws.data_ptr()
+    assert size > 11 << 20
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)  # (some 50 ms of the stream's time)
+    li.backward(x, W, want, z, stream=s)
+    del li
+    assert torch.empty(size, dtype=torch.uint8, device="cuda").data_ptr() != there
+    torch.cuda.synchronize()
