@@ -51,7 +51,7 @@ luna_status check(const luna_decay_desc *dd) {
 
 struct Plan {
     int seg_len, nseg;
-    size_t state;  // bytes of one set of piece states
+    size_t state;  // bytes of one set of piece states (none with one piece: the pass itself carries the state)
     size_t o_U = 256, o_X = 0, o_R = 0, o_part = 0, fwd = 0, bwd = 0;
 };
 
@@ -73,7 +73,7 @@ Plan make_plan(const luna_decay_desc *dd) {
     }
     p.seg_len = (int)(cdiv(chunks, best) * rows);
     p.nseg = (int)cdiv(std::max(1, dd->n), p.seg_len);
-    p.state = (size_t)align256((int64_t)BH * p.nseg * dd->d * dd->dv * 4);
+    p.state = p.nseg == 1 ? 0 : (size_t)align256((int64_t)BH * p.nseg * dd->d * dd->dv * 4);
     p.o_X = p.o_U + p.state;
     p.fwd = p.o_X + p.state;
     p.o_R = p.fwd;

@@ -26,6 +26,19 @@ def test_a_device_has_its_number(L, monkeypatch):
     assert L.BlockNorm(4, 8, device="cuda:1").device == torch.device("cuda", 1)
 
 
+def test_decay_workspace_is_what_the_call_uses(L):
+    """One piece a head keeps no states of pieces; shared heads keep their gradients, one for each query head."""
+    size = L.luna_decay_workspace_size
+    for n, d, io in ((100, 128, L.LUNA_BF16), (64, 128, L.LUNA_F32), (100, 40, L.LUNA_BF16)):
+        one = L.decay_desc(64, 32, n, d, d, io=io)
+        assert size(one, False) <= 256 and size(one, True) <= 256
+        shared = L.decay_desc(64, 32, n, d, d, Hkv=8, io=io)
+        assert size(shared, False) <= 256 and size(shared, True) == 256 + 64 * 32 * n * d * 4
+    long = L.decay_desc(1, 2, 1 << 16, 128, 128)
+    state = 2 * 128 * 128 * 4
+    assert size(long, False) > 2 * 2 * state and size(long, True) > 3 * 2 * state
+
+
 @pytest.mark.gpu
 def test_memory_of_a_call_on_another_stream(L):
     """What a call on a stream allocates is that stream's, and the workspace outlives what is queued there: neither
