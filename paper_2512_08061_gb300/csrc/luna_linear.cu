@@ -454,8 +454,28 @@ bool whole_dz(const luna_linear_desc *ld) {
            tiles(ld->m) * tiles(ld->k) * ld->n <= limit && tiles(ld->n) * tiles(ld->k) * ld->m <= limit;
 }
 
-// Partial products: up to 32 pieces of K of a product with few tiles, at most 64 MiB.
-size_t part_bytes(int64_t M, int64_t N) { return (size_t)std::min<int64_t>(M * N * 4 * 32, int64_t(64) << 20); }
+// Pieces of K of a product of M x N x K on a launch of `tiles` blocks: enough to give every SM a block, none
+// under `least` of K, at most 32, and at most 64 MiB of partial products.
+int pieces(int64_t M, int64_t N, int64_t K, int64_t tiles, int64_t least) {
+    if (tiles >= tc_sm_count()) return 1;
+    int64_t s = std::min<int64_t>(tc_sm_count() / tiles, K / least);
+    s = std::min<int64_t>(s, (int64_t(64) << 20) / (4 * M * N));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 32));
+}
+
+// Room for the partial products of the kernels that may take a product (`rows`: the one for a few rows takes it
+// whole): every tile shape on tensor cores, and the CUDA cores' for operands off their boundaries.
+size_t part_bytes(int64_t M, int64_t N, int64_t K, bool rows) {
+    if (M == 0 || N == 0 || rows) return 0;
+    int most = pieces(M, N, K, cdiv(M, kT) * cdiv(N, kT), 64);
+    if (M <= 64) {
+        most = std::max(most, pieces(M, N, K, cdiv(N, 128), 256));
+    } else {
+        for (const int64_t tiles : {2 * cdiv(M, 256) * cdiv(N, 256), cdiv(M, 128) * cdiv(N, 256), 2 * cdiv(M, 256) * cdiv(N, 128)})
+            most = std::max(most, pieces(M, N, K, tiles, 256));
+    }
+    return most > 1 ? (size_t)(M * N * 4 * most) : 0;
+}
 
 int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 
@@ -467,8 +487,8 @@ bool planes_pay(int64_t M, int64_t N, int64_t K) {
     const double simt = 2.0 * (double)(cdiv(M, kT) * kT) * (double)(cdiv(N, kT) * kT) * K / 35e6;
     return M > 8 && K > 0 && simt > 12.0 + 12.0 * macs / 1e9 + 16.0 * (double)(M + N) * K / 4e6;
 }
-// Rows of X up to which fp32 goes to the kernel for a few rows, eight at a time.
-constexpr int kRowsF32 = 32;
+// Rows of X that go to the kernel for a few rows, eight at a time in fp32.
+constexpr int kRows = 8, kRowsF32 = 32;
 // Bytes of the planes of an operand of `rows` rows.
 int64_t plane_bytes(int64_t rows, int64_t K, bool kt) { return align256(3 * up64(K) * (kt ? up8(rows) : rows) * 2); }
 constexpr int64_t kFlagBytes = 2 * kFlagBlocks * sizeof(int) / 256 * 256 + 256;
@@ -479,8 +499,9 @@ int64_t planes_room(int64_t M, int64_t N, int64_t K, bool akt, bool bkt) {
 Plan make_plan(const luna_linear_desc *ld) {
     Plan p;
     const int64_t eb = ld->io == LUNA_F32 ? 4 : 2;
-    p.part_fwd = (size_t)align256((int64_t)part_bytes(ld->m, ld->n));
-    p.part_bwd = std::max(part_bytes(ld->m, ld->k), part_bytes(ld->n, ld->k));
+    const bool few = ld->k > 0 && ld->m <= (ld->io == LUNA_F32 ? kRowsF32 : kRows);
+    p.part_fwd = (size_t)align256((int64_t)part_bytes(ld->m, ld->n, ld->k, few));
+    p.part_bwd = std::max(part_bytes(ld->m, ld->k, ld->n, false), part_bytes(ld->n, ld->k, ld->m, false));
     p.part_bwd = std::max(p.part_bwd, (size_t)(cdiv(ld->m, kDzRows) * ld->n * 4));  // the bias gradient's
     p.part_bwd = (size_t)align256((int64_t)p.part_bwd);
     p.fwd = p.o_part + p.part_fwd;
@@ -510,10 +531,8 @@ bool ws_ok(const void *ws) { return ws && (reinterpret_cast<uintptr_t>(ws) & 255
 }  // namespace
 
 int linear_splits(const Product &p, int64_t tiles, int64_t least) {
-    if (!p.part || tiles >= tc_sm_count()) return 1;
-    int64_t s = std::min<int64_t>(tc_sm_count() / tiles, p.K / least);
-    s = std::min<int64_t>(s, (int64_t)(p.part_bytes / (sizeof(float) * p.M * p.N)));
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 32));
+    const int64_t room = (int64_t)(p.part_bytes / (sizeof(float) * p.M * p.N));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(pieces(p.M, p.N, p.K, tiles, least), room));
 }
 
 cudaError_t launch_product_simt(const Product &p, luna_dtype io, cudaStream_t s) {
@@ -582,7 +601,7 @@ static cudaError_t split_operands(Product &p, cudaStream_t s) {
 }
 
 bool product_rows_ok(const Product &p, luna_dtype io) {
-    return p.M <= (io == LUNA_F32 ? kRowsF32 : 8) && p.K > 0 && !p.A.kt && !p.B.kt;
+    return p.M <= (io == LUNA_F32 ? kRowsF32 : kRows) && p.K > 0 && !p.A.kt && !p.B.kt;
 }
 
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s) {

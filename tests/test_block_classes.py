@@ -39,6 +39,18 @@ def test_decay_workspace_is_what_the_call_uses(L):
     assert size(long, False) > 2 * 2 * state and size(long, True) > 3 * 2 * state
 
 
+def test_linear_workspace_is_what_the_call_uses(L):
+    """Partial products are kept for products that may be cut along their depth alone."""
+    size, F, BF = L.luna_linear_workspace_size, L.LUNA_F32, L.LUNA_BF16
+    for m, n, k, io in ((65536, 4096, 4096, BF), (1, 8192, 4096, BF), (8, 8192, 4096, BF), (32, 512, 4096, F), (1 << 20, 512, 64, BF)):
+        assert size(L.linear_desc(m, n, k, io=io), False) <= 256, (m, n, k, io)
+    # dX and dW of a large layer: the bias gradient's sums over 256 rows, and dz where there is an activation
+    assert size(L.linear_desc(65536, 4096, 4096, io=BF), True) == 256 + 256 * 4096 * 4
+    assert size(L.linear_desc(65536, 4096, 4096, "gelu", io=BF), True) == 256 + 256 * 4096 * 4 + 65536 * 4096 * 2
+    # few tiles and a depth to cut
+    assert 256 < size(L.linear_desc(128, 128, 8192, io=BF), False) <= 256 + 128 * 128 * 4 * 32
+
+
 @pytest.mark.gpu
 def test_memory_of_a_call_on_another_stream(L):
     """What a call on a stream allocates is that stream's, and the workspace outlives what is queued there: neither
