@@ -6,6 +6,9 @@
 
 #include "luna_decay.cuh"
 
+namespace luna {
+int tc_sm_count();
+}
 using namespace luna;
 
 namespace {
@@ -63,7 +66,7 @@ Plan make_plan(const luna_decay_desc *dd) {
     const bool tc = dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0;
     const int rows = tc ? 128 : kDecaySimtRows;
     const int64_t BH = (int64_t)dd->B * dd->H, chunks = cdiv(std::max(1, dd->n), rows);
-    const double room = 152.0 * (!tc && std::max(dd->d, dd->dv) <= 64 ? 2 : 1);  // blocks the SMs hold
+    const double room = (double)tc_sm_count() * (!tc && std::max(dd->d, dd->dv) <= 64 ? 2 : 1);  // blocks the SMs hold
     int64_t best = 1;
     double least = 1e300;
     for (int64_t ns = 1; ns <= std::min<int64_t>(64, chunks); ++ns) {

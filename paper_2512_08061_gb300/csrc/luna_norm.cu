@@ -26,6 +26,9 @@
 #include "luna_prof.cuh"
 
 namespace luna {
+
+int tc_sm_count();
+
 namespace {
 
 constexpr int kMaxCols = 16384;
@@ -552,12 +555,12 @@ Shape shape_of(int cols, int groups, bool vectors, int vec_io, bool backward, bo
         s.smem = row + (s.shared ? sums : 0);
         s.rows_per_block = 1;
         s.threads = s.smem <= 100 * 1024 ? 512 : 1024;
-        s.blocks = 152 * (s.threads == 512 ? 2 : 1);
+        s.blocks = tc_sm_count() * (s.threads == 512 ? 2 : 1);
         return s;
     }
     s.threads = ((nvec + s.nv - 1) / s.nv + 31) / 32 * 32;
     s.rows_per_block = s.threads == 32 ? 8 : 1;
-    s.blocks = 152 * std::max(1, limits(s.vec, s.nv, backward).resident / (s.threads * s.rows_per_block));
+    s.blocks = tc_sm_count() * std::max(1, limits(s.vec, s.nv, backward).resident / (s.threads * s.rows_per_block));
     s.smem = sizeof(float) * 128;
     return s;
 }

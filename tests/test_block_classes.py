@@ -51,6 +51,15 @@ def test_linear_workspace_is_what_the_call_uses(L):
     assert 256 < size(L.linear_desc(128, 128, 8192, io=BF), False) <= 256 + 128 * 128 * 4 * 32
 
 
+def test_grids_are_the_devices(L):
+    """Grids that stay for all rows, and with them the weight gradients' partial sums, go by the device's SMs."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count if torch.cuda.is_available() else 148  # (as the library's own default)
+    for cols, io in ((4096, L.LUNA_BF16), (16384, L.LUNA_F32), (5001, L.LUNA_BF16)):
+        size = L.luna_norm_workspace_size(L.norm_desc(1 << 20, cols, io=io))
+        sums = size // (16 * cols) // sms * sms * 16 * cols  # (four arrays of fp32 a block)
+        assert sums > 0 and size == (sums + 255) // 256 * 256
+
+
 @pytest.mark.gpu
 def test_memory_of_a_call_on_another_stream(L):
     """What a call on a stream allocates is that stream's, and the workspace outlives what is queued there: neither
