@@ -93,7 +93,10 @@ def test_memory_of_a_call_on_another_stream(L):
         assert not any(t.data_ptr() in there for t in mine), name
         del mine
     torch.cuda.synchronize()
-    assert torch.equal(li.forward(x, W, stream=s), want)
+    again = li.forward(x, W, stream=s)
+    s.synchronize()
+    assert torch.equal(again, want)
+    del again
     # the workspace of a plan that is gone
     torch.cuda.synchronize()
     size, there = li.ws.numel(), li.ws.data_ptr()
