@@ -468,8 +468,9 @@ luna_status luna_linear_fwd(const luna_linear_desc *ld, const void *X, const voi
 
 /* dX = dz W, dW = dz^T X (contiguous n x k), db = the column sums of dz (n), with
  * dz = dY act'(z); each is written where not NULL (the gradient of R is dY).
- * The bias gradient sums dz before dz is rounded to io for the products.  No
- * atomics: equal inputs give equal bits. */
+ * The bias gradient sums dz before dz is rounded to io for the products; bf16
+ * layers of at most 64 rows whose products are short keep 16 bits of dz in them
+ * instead of 8.  No atomics: equal inputs give equal bits. */
 luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const void *W, const void *Z, const void *dY,
                             void *dX, void *dW, void *db, void *workspace, size_t ws_bytes, void *stream);
 

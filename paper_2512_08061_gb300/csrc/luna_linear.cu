@@ -79,7 +79,7 @@ __device__ __forceinline__ void load_quad(const IO *p, float (&v)[4]) {
 // sums a thread in fp32, two multiply-adds an instruction, the next step's values loaded while this one's
 // are multiplied.  Bound by the fp32 FMA rate (116 us at 5727 x 656 x 576: 37 TFLOP/s).
 // QUAD: loads of four values along the contiguous dimension (rows on their boundaries).
-template <typename TA, typename IO, bool QUAD>
+template <typename IO, bool QUAD>
 __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t depth, int splits) {
     __shared__ __align__(16) float sA[kK][kT + 4], sB[kK][kT + 4];
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
@@ -99,21 +99,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
         const int e = tid + i * kThreads;
         if (kt) { r = e % (kT / W) * W; k = e / (kT / W); } else { k = e % (kK / W) * W; r = e / (kK / W); }
     };
-    auto fetch_one = [&](auto type, const MatView &v, int64_t base, int64_t rows, int64_t kb, float (&out)[8]) {
-        using T = decltype(type);
+    auto fetch_one = [&](const MatView &v, int64_t base, int64_t rows, int64_t kb, float (&out)[8]) {
 #pragma unroll
         for (int i = 0; i < 8 / W; ++i) {
             int r, k;
             place(v.kt, i, r, k);
             if (QUAD) {  // (four rows or four depths are in or out together)
                 const bool in = base + r < rows && kb + k < k1;
-                const T *q = static_cast<const T *>(v.p) + (v.kt ? (kb + k) * v.ld + base + r : (base + r) * v.ld + kb + k);
+                const IO *q = static_cast<const IO *>(v.p) + (v.kt ? (kb + k) * v.ld + base + r : (base + r) * v.ld + kb + k);
                 float x[4] = {0.f, 0.f, 0.f, 0.f};
-                if (in) load_quad<T>(q, x);
+                if (in) load_quad<IO>(q, x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) out[(4 * i + j) % 8] = x[j];
             } else {
-                out[i % 8] = at<T>(v, base + r, rows, kb + k, k1);
+                out[i % 8] = at<IO>(v, base + r, rows, kb + k, k1);
             }
         }
     };
@@ -127,8 +126,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(Product p, int64_t dept
         }
     };
     auto fetch = [&](int64_t kb) {
-        fetch_one(TA{}, p.A, row0, p.M, kb, ra);
-        fetch_one(IO{}, p.B, col0, p.N, kb, rb);
+        fetch_one(p.A, row0, p.M, kb, ra);
+        fetch_one(p.B, col0, p.N, kb, rb);
     };
     fetch(k0);
     for (int64_t kb = k0; kb < k1; kb += kK) {
@@ -240,11 +239,12 @@ __global__ void __launch_bounds__(256) k_product_rows(Product p, int split) {
 
 // dZ = dY act'(Z) (not written where there is no activation; rows lddz apart) and the column sums of dZ over a
 // block's rows, one partial row a block.  32 column pieces x 8 rows of threads; bound by the bytes.
-// OUT: dZ's type.
-template <typename IO, typename OUT, int VEC>
-__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, OUT *dZ,
-                                                   int64_t lddz, int64_t m, int n, int act, int64_t rows, float *part,
-                                                   int *status) {
+// TWO: a value's rounding error goes into a second term lo elements on, and the columns between
+// are set to 0 (an infinity or a NaN is its first term alone).
+template <typename IO, int VEC, bool TWO>
+__global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, const IO *Z, int64_t ldz, IO *dZ,
+                                                   int64_t lddz, int64_t lo, int64_t m, int n, int act, int64_t rows,
+                                                   float *part, int *status) {
     __shared__ float s[8][32 * VEC + 1];
     clear_status(1, status);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * VEC;
@@ -262,11 +262,23 @@ __global__ void __launch_bounds__(256) k_linear_dz(const IO *dY, int64_t lddy, c
                 load_vec<IO, VEC>(Z + r * ldz + c, z);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) d[e] *= linear_slope<IO>(z[e], act);
-                store_vec<OUT, VEC>(dZ + r * lddz + c, d);
+                store_vec<IO, VEC>(dZ + r * lddz + c, d);
+                if (TWO) {
+                    float rest[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float first = __bfloat162float(__float2bfloat16_rn(d[e]));
+                        rest[e] = fabsf(first) < INFINITY ? d[e] - first : 0.0f;
+                    }
+                    store_vec<IO, VEC>(dZ + r * lddz + lo + c, rest);
+                }
             }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) acc[e] += d[e];
         }
+    } else if (TWO && c < lo) {
+        const float none[VEC] = {};
+        for (int64_t r = r0 + w; r < r1; r += 8) store_vec<IO, VEC>(dZ + r * lddz + c, none);
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s[w][lane * VEC + e] = acc[e];
@@ -370,12 +382,10 @@ cudaError_t simt(const Product &p, cudaStream_t s) {
         return reinterpret_cast<uintptr_t>(v.p) % (4 * sizeof(IO)) == 0 && v.ld % 4 == 0 && (v.kt ? rows : K) % 4 == 0;
     };
     const dim3 grid((unsigned)gx, (unsigned)gy, used);
-    if (p.wide_a)
-        LUNA_LAUNCH("product", (k_product<float, IO, false>), grid, kThreads, 0, s, p, depth, used);
-    else if (quad(p.A, p.M, p.K) && quad(p.B, p.N, p.K))
-        LUNA_LAUNCH("product", (k_product<IO, IO, true>), grid, kThreads, 0, s, p, depth, used);
+    if (quad(p.A, p.M, p.K) && quad(p.B, p.N, p.K))
+        LUNA_LAUNCH("product", (k_product<IO, true>), grid, kThreads, 0, s, p, depth, used);
     else
-        LUNA_LAUNCH("product", (k_product<IO, IO, false>), grid, kThreads, 0, s, p, depth, used);
+        LUNA_LAUNCH("product", (k_product<IO, false>), grid, kThreads, 0, s, p, depth, used);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || used == 1) return e;
     return launch_product_finish(p, used, IOType<IO>::code, s);
@@ -385,26 +395,28 @@ constexpr int64_t kDzRows = 256;  // rows of a block of the column sums
 
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <typename IO, typename OUT, int VEC>
-void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act, float *part,
-               int parts, int *status, cudaStream_t s) {
-    LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, OUT, VEC>), dim3((unsigned)cdiv(n, 32 * VEC), parts), 256, 0, s,
-                static_cast<const IO *>(dY), lddy, static_cast<const IO *>(Z), ldz, static_cast<OUT *>(dZ), lddz, m, n, act, kDzRows,
-                part, status);
+template <typename IO, int VEC>
+void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t lo, int64_t m, int n,
+               int act, float *part, int parts, int *status, cudaStream_t s) {
+    const dim3 grid((unsigned)cdiv(std::max<int64_t>(n, lo), 32 * VEC), parts);
+    if (lo)
+        LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, true>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
+                    static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
+    else
+        LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, false>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
+                    static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
 }
 
 template <typename IO>
-cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t m, int n, int act,
-               float *part, void *db, bool whole, int *status, cudaStream_t s) {
+cudaError_t dz(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t lo, int64_t m, int n,
+               int act, float *part, void *db, int *status, cudaStream_t s) {
     constexpr int VEC = 16 / (int)sizeof(IO);
     const int parts = (int)cdiv(m, kDzRows);
     const bool a = act != LUNA_LINEAR_NONE;
-    if (whole)
-        dz_launch<IO, float, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
-    else if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
-        dz_launch<IO, IO, VEC>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
+    if (n % VEC == 0 && al16(dY) && lddy % VEC == 0 && (!a || (al16(Z) && ldz % VEC == 0)))
+        dz_launch<IO, VEC>(dY, lddy, Z, ldz, dZ, lddz, lo, m, n, act, db ? part : nullptr, parts, status, s);
     else
-        dz_launch<IO, IO, 1>(dY, lddy, Z, ldz, dZ, lddz, m, n, act, db ? part : nullptr, parts, status, s);
+        dz_launch<IO, 1>(dY, lddy, Z, ldz, dZ, lddz, lo, m, n, act, db ? part : nullptr, parts, status, s);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !db) return e;
     LUNA_LAUNCH("linear_db", k_linear_db<IO>, (unsigned)cdiv(n, 256), 256, 0, s, part, parts, n, static_cast<IO *>(db));
@@ -442,17 +454,23 @@ struct Plan {
 };
 
 int64_t up8(int64_t x) { return (x + 7) / 8 * 8; }
+constexpr double kTwoTermCycles = 2000;
+constexpr int64_t kTwoTermRows = 64;
 
-// dZ stays in fp32 in bf16 layers with few values, where its own rounding does not average out (over a few
-// hundred values, of it or of a gradient, it can weigh more than the gradient's).  Their products then run on
-// CUDA cores, which costs 30 us of 60 (2 x 3680 x 128), up to 50; beyond that dZ is rounded to bf16 once for
-// the tensor cores, which a gradient sees as sqrt(2) of its own rounding.
-bool whole_dz(const luna_linear_desc *ld) {
-    const int64_t limit = int64_t(1) << 29;
-    const auto tiles = [](int64_t x) { return cdiv(x, kT) * kT; };
-    return ld->io == LUNA_BF16 && ld->act != LUNA_LINEAR_NONE && std::min({ld->m * ld->n, ld->m * ld->k, (int64_t)ld->n * ld->k}) <= 1024 &&
-           tiles(ld->m) * tiles(ld->k) * ld->n <= limit && tiles(ld->n) * tiles(ld->k) * ld->m <= limit;
+int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+
+// bf16 layers: whether dZ goes to its products in two bf16 terms (2^-17 of it) instead of one.  One rounding of
+// dZ adds to each gradient as much as the gradient's own (sqrt 2 of it in all, and more where few values have to
+// average it out); two terms take that away for twice the products' steps, and are taken where the launches nearly
+// hide them: to 64 rows and 2000 cycles of steps that costs 0.8 to 2.3 us of 15 to 25 (20 x 16 x 4096 22.8 -> 23.6 us,
+// 2 x 3680 x 128 16.2 -> 17.9, 64 x 512 x 512 18.9 -> 21.2), beyond them 3.5 to 12 (128^3 19.7 -> 23.2, 2048 x 64 x 64
+// 28.9 -> 34.3, 4 x 4096 x 4096 32.0 -> 36.9, 2048 x 1024 x 1024 49.0 -> 60.5).
+bool two_terms(const luna_linear_desc *ld) {
+    return ld->io == LUNA_BF16 && ld->act != LUNA_LINEAR_NONE && ld->m > 0 && ld->m <= kTwoTermRows && ld->n > 0 && ld->k > 0 &&
+           product_tc_cycles(ld->m, ld->k, ld->n) + product_tc_cycles(ld->n, ld->k, ld->m) <= kTwoTermCycles;
 }
+// Bytes of a row of dZ.
+int64_t dz_row(const luna_linear_desc *ld) { return two_terms(ld) ? 4 * up64(ld->n) : up8(ld->n) * (ld->io == LUNA_F32 ? 4 : 2); }
 
 // Pieces of K of a product of M x N x K on a launch of `tiles` blocks: enough to give every SM a block, none
 // under `least` of K, at most 32, and at most 64 MiB of partial products.
@@ -477,8 +495,6 @@ size_t part_bytes(int64_t M, int64_t N, int64_t K, bool rows) {
     return most > 1 ? (size_t)(M * N * 4 * most) : 0;
 }
 
-int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
-
 // Whether an fp32 product is taken to tensor cores in bf16 planes: estimated microseconds of both ways.  The
 // CUDA cores carry 35 TFLOP/s in whole tiles; the planes take three launches, 16 bytes a value of the operands
 // and six products at 1 PFLOP/s.
@@ -498,7 +514,6 @@ int64_t planes_room(int64_t M, int64_t N, int64_t K, bool akt, bool bkt) {
 
 Plan make_plan(const luna_linear_desc *ld) {
     Plan p;
-    const int64_t eb = ld->io == LUNA_F32 ? 4 : 2;
     const bool few = ld->k > 0 && ld->m <= (ld->io == LUNA_F32 ? kRowsF32 : kRows);
     p.part_fwd = (size_t)align256((int64_t)part_bytes(ld->m, ld->n, ld->k, few));
     p.part_bwd = std::max(part_bytes(ld->m, ld->k, ld->n, false), part_bytes(ld->n, ld->k, ld->m, false));
@@ -506,7 +521,7 @@ Plan make_plan(const luna_linear_desc *ld) {
     p.part_bwd = (size_t)align256((int64_t)p.part_bwd);
     p.fwd = p.o_part + p.part_fwd;
     p.o_dz = p.o_part + p.part_bwd;
-    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * up8(ld->n) * (whole_dz(ld) ? 4 : eb)));
+    p.bwd = p.o_dz + (ld->act == LUNA_LINEAR_NONE ? 0 : (size_t)align256(ld->m * dz_row(ld)));
     p.o_pad_fwd = p.fwd;
     p.o_pad_bwd = p.bwd;
     // bf16 widths that are not multiples of 8: copies of the operands whose rows are 16-byte aligned
@@ -515,6 +530,9 @@ Plan make_plan(const luna_linear_desc *ld) {
         p.pad_fwd = ld->k % 8 ? (size_t)(X + W) : 0;
         p.pad_bwd = (size_t)(align256(ld->m * up8(ld->n) * 2) + std::max(X, W));  // dz and one of the others at a time
         p.fwd += p.pad_fwd;
+        p.bwd += p.pad_bwd;
+    } else if (two_terms(ld)) {  // (the CUDA cores' product, for operands off their boundaries, takes no second term)
+        p.pad_bwd = (size_t)align256(std::max(ld->m, (int64_t)ld->n) * up8(ld->k) * 2);
         p.bwd += p.pad_bwd;
     }
     if (ld->io == LUNA_F32) {  // fp32 operands in three bf16 planes
@@ -616,11 +634,12 @@ cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s)
 // (which cost their bytes twice over; the CUDA-core product would take ten to thirty times the tensor cores').
 cudaError_t launch_product(const Product &p, luna_dtype io, cudaStream_t s) {
     if (product_rows_ok(p, io)) return launch_product_rows(p, io, s);
-    if (io == LUNA_BF16 && p.K >= 1 && !p.wide_a) {
+    if (io == LUNA_BF16 && p.K >= 1) {
         Product q = p;
         cudaError_t e;
         if (pad_operands(q, s, &e)) return launch_product_tc(q, io, s);
         if (e != cudaSuccess) return e;
+        if (p.A.lo) return cudaErrorInvalidValue;  // (has its copies always)
     }
     if (io == LUNA_F32 && planes_pay(p.M, p.N, p.K) &&
         p.pad_bytes >= (size_t)planes_room(p.M, p.N, p.K, p.A.kt, p.B.kt)) {
@@ -699,16 +718,16 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     int *status = reinterpret_cast<int *>(ws);
     const int64_t lddy = ld->lddy ? ld->lddy : n, ldz = ld->ldz ? ld->ldz : n;
     cudaError_t e = cudaSuccess;
-    const bool whole = whole_dz(ld);
+    const int64_t lo = act && two_terms(ld) ? up64(n) : 0, ldg = act ? dz_row(ld) / eb : lddy;
     if (act || db) {
         void *dZ = ws + pl.o_dz;
-        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, false, status, s)
-                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, up8(n), m, (int)n, ld->act, part, db, whole, status, s);
+        e = ld->io == LUNA_F32 ? dz<float>(dY, lddy, Z, ldz, dZ, ldg, lo, m, (int)n, ld->act, part, db, status, s)
+                               : dz<__nv_bfloat16>(dY, lddy, Z, ldz, dZ, ldg, lo, m, (int)n, ld->act, part, db, status, s);
         if (e != cudaSuccess) return LUNA_ERR_CUDA;
     }
     if (k == 0) return LUNA_OK;
     const void *G = act ? ws + pl.o_dz : dY;
-    const int64_t ldg = act ? up8(n) : lddy, ldx = ld->ldx ? ld->ldx : k, ldw = ld->ldw ? ld->ldw : k;
+    const int64_t ldx = ld->ldx ? ld->ldx : k, ldw = ld->ldw ? ld->ldw : k;
     Product p;
     memset(&p, 0, sizeof(p));
     p.act = LUNA_LINEAR_NONE;
@@ -716,9 +735,8 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
     p.pad = pl.pad_bwd ? ws + pl.o_pad_bwd : nullptr; p.pad_bytes = pl.pad_bwd;
     p.status = status;
     p.clear = !(act || db);
-    p.wide_a = whole;
     if (dX) {
-        p.A = MatView{G, ldg, false};
+        p.A = MatView{G, ldg, false, lo};
         p.B = MatView{W, ldw, true};
         p.M = m; p.N = k; p.K = n;
         p.out = dX; p.ldo = ld->lddx ? ld->lddx : k;
@@ -726,7 +744,7 @@ luna_status luna_linear_bwd(const luna_linear_desc *ld, const void *X, const voi
         p.clear = 0;
     }
     if (dW) {
-        p.A = MatView{G, ldg, true};
+        p.A = MatView{G, ldg, true, lo};
         p.B = MatView{X, ldx, true};
         p.M = n; p.N = k; p.K = m;
         p.out = dW; p.ldo = k;

@@ -16,12 +16,12 @@ struct MatView {           // element (row, k) at p[row * ld + k], or with kt at
     const void *p;
     int64_t ld;
     bool kt;
+    int64_t lo = 0;        // a value's second bf16 term so many elements on, or 0 (tensor cores alone)
 };
 
 struct Product {
     MatView A, B;
     int64_t M, N, K;
-    bool wide_a;           // A is fp32 though the rest is bf16 (CUDA cores alone)
     const void *bias;      // N values, or NULL
     int act;               // luna_linear_act
     const void *R;         // residual M x N, or NULL
@@ -139,6 +139,8 @@ bool product_rows_ok(const Product &p, luna_dtype io);                          
 cudaError_t launch_product_rows(const Product &p, luna_dtype io, cudaStream_t s);
 // On tensor cores: bf16 operands, or with LUNA_F32 operands in three bf16 planes along K (see k_split).
 cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s);
+// Estimated cycles of the 64-deep steps that a block of that form runs one after another in a bf16 product.
+double product_tc_cycles(int64_t M, int64_t N, int64_t K);
 cudaError_t launch_product_finish(const Product &p, int splits, luna_dtype io, cudaStream_t s);
 
 }  // namespace luna

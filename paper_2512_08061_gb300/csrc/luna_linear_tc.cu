@@ -65,6 +65,7 @@ struct ProductTc {
     int tiles_m, tiles_n, splits, k_steps, steps_per_split;  // tiles of BM * CG rows, BN columns
     int per;        // 64-deep slices of an operand (of each plane of it)
     int join;       // steps of an accumulator, where they are joined
+    int terms;      // of a bf16 operand's values: steps of the first and of the second alternate
     bool swap;      // the product is computed transposed: A = the layer's B (few rows of X)
     bool vec;       // outputs and residual on 16-byte boundaries: the epilogue stores by TMA
 };
@@ -247,16 +248,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         if (CG == 2) tma_load_2d_pair(dst, m, x, y, bar);
                         else tma_load_2d(dst, m, x, y, full + st);
                     };
-                    const int k = (T::PLANES ? s % kPlanes * a.per + s / kPlanes : s) * kDepth;
+                    const int second = !T::PLANES && a.terms == 2 ? s & 1 : 0;
+                    const int k = (T::PLANES ? s % kPlanes * a.per + s / kPlanes : a.terms == 2 ? s >> 1 : s) * kDepth;
+                    const int xa = second * (int)p.A.lo, xb = second * (int)p.B.lo;  // (multiples of 64)
                     if (p.A.kt) {
-                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, ra + 64 * b, k);
+                        for (int b = 0; b < T::BM / 64; ++b) load(sa + b * 8192, &mapA, xa + ra + 64 * b, k);
                     } else {
-                        load(sa, &mapA, k, ra);
+                        load(sa, &mapA, xa + k, ra);
                     }
                     if (p.B.kt) {
-                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, rb + 64 * b, k);
+                        for (int b = 0; b < T::NBL / 64; ++b) load(sb + b * 8192, &mapB, xb + rb + 64 * b, k);
                     } else {
-                        load(sb, &mapB, k, rb);
+                        load(sb, &mapB, xb + k, rb);
                     }
                 }
             }
@@ -477,9 +480,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Map of an operand whose slices are `rows` rows x 64 deep.
+// Map of an operand whose slices are `rows` rows x 64 deep.  (Where values have a second term, what lies between
+// the terms is read too: of rows past the operand's, whose outputs are dropped, or of depths past its, zeros.)
 bool operand_map(CUtensorMap *m, const MatView &v, int64_t rows, int64_t K, int slice_rows) {
-    const uint64_t dims[2] = {(uint64_t)(v.kt ? rows : K), (uint64_t)(v.kt ? K : rows)};
+    const uint64_t dims[2] = {(uint64_t)(v.lo + (v.kt ? rows : K)), (uint64_t)(v.kt ? K : rows)};
     const uint64_t strides[1] = {(uint64_t)v.ld * 2};
     const uint32_t box[2] = {64, (uint32_t)(v.kt ? kDepth : slice_rows)};
     return tc_make_map_nd(m, v.p, 2, dims, strides, box);
@@ -501,15 +505,15 @@ constexpr int kTileCycles = 2500;
 
 struct Choice {
     int splits;
-    double cycles;
+    double steps, cycles;  // cycles of the steps, and with what is around them
 };
 template <typename IO, int CG, int BN>
 Choice cost(const Product &p) {
     const int64_t tiles = ((p.M + 128 * CG - 1) / (128 * CG)) * ((p.N + BN - 1) / BN), steps = (p.K + kDepth - 1) / kDepth * (sizeof(IO) == 4 ? kTerms : 1);
     const int splits = linear_splits(p, tiles * CG, 256);
     const int64_t rounds = (tiles * splits * CG + tc_sm_count() - 1) / tc_sm_count();
-    return Choice{splits, (double)rounds * ((double)((steps + splits - 1) / splits) * step_cycles<CG, BN>()) + kTileCycles +
-                              (splits > 1 ? kTileCycles : 0)};
+    const double run = (double)rounds * ((double)((steps + splits - 1) / splits) * step_cycles<CG, BN>());
+    return Choice{splits, run, run + kTileCycles + (splits > 1 ? kTileCycles : 0)};
 }
 
 template <typename IO, int CG, int BN, bool LONG = false>
@@ -521,7 +525,8 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
     a.tiles_m = (int)cdiv(M, T::BM * CG);
     a.tiles_n = (int)cdiv(N, BN);
     a.per = (int)cdiv(p.K, kDepth);
-    a.k_steps = a.per * (T::PLANES ? kPlanes : 1);
+    a.terms = p.A.lo || p.B.lo ? 2 : 1;
+    a.k_steps = a.per * (T::PLANES ? kPlanes : a.terms);
     a.join = T::PLANES ? kPlanes : kJoin / kDepth;
     const int64_t K = T::PLANES ? 3 * (int64_t)a.per * kDepth : p.K;  // of the operands as they are stored
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
@@ -559,6 +564,19 @@ cudaError_t launch(ProductTc a, cudaStream_t s) {
 }
 
 }  // namespace
+
+double product_tc_cycles(int64_t M, int64_t N, int64_t K) {
+    using B = __nv_bfloat16;
+    Product p{};
+    p.M = M; p.N = N; p.K = K;
+    p.part_bytes = size_t(64) << 20;  // (what the partial products take at most)
+    if (M <= 64) {  // transposed, as below
+        std::swap(p.M, p.N);
+        return cost<B, 1, 64>(p).steps;
+    }
+    const Choice pair = cost<B, 2, 256>(p), wide = cost<B, 1, 256>(p), half = cost<B, 1, 128>(p);
+    return pair.cycles <= wide.cycles && pair.cycles <= half.cycles ? pair.steps : wide.cycles <= half.cycles ? wide.steps : half.steps;
+}
 
 cudaError_t launch_product_tc(const Product &p, luna_dtype io, cudaStream_t s) {
     using B = __nv_bfloat16;

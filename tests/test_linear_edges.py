@@ -107,3 +107,32 @@ def test_long_sums_of_positive_products(L, m, n, k, direction):
             want = want + x[:16, a:a + (1 << 12)].double() @ W[:, a:a + (1 << 12)].double().t()
     assert L.luna_device_status(p.ws) == 0
     assert ((got.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -13) * want).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(2, 3680, 128), (64, 96, 200), (33, 131, 77), (64, 512, 512), (7, 64, 4096)])
+def test_gradients_of_few_rows_round_once(L, m, n, k):
+    """Layers of few rows keep dz to 2^-17 in its products: a gradient carries half a unit of its own eight bits
+    (2^-8 at most) and 2^-17 of its terms' size, with 1e-4 of that for fp32 sums and bf16-grade slopes.  Views off
+    their boundaries, and an infinity, which has no second term."""
+    g = torch.Generator("cuda").manual_seed(m * n + k)
+    x, W, dY = matrix(g, m, k, BF, 0), matrix(g, n, k, BF, 0, k ** -0.5), matrix(g, m, n, BF, 0)
+    Z = matrix(g, m, n, BF, 0)
+    p = L.Linear(m, n, k, "silu", BF, backward=True)
+    got = p.backward(x, W, dY, Z)
+    z = Z.double().requires_grad_()
+    (z * torch.sigmoid(z)).backward(dY.double())
+    for name, v, size in (("dX", z.grad @ W.double(), z.grad.abs() @ W.double().abs()),
+                          ("dW", z.grad.t() @ x.double(), z.grad.abs().t() @ x.double().abs())):
+        assert ((got[name].double() - v).abs() <= 2.0 ** -8 * v.abs() + 1e-4 * size).all(), name
+
+    def odd(t):
+        return torch.empty(t.numel() + 1, dtype=BF, device="cuda")[1:].view(t.shape).copy_(t)
+
+    again = p.backward(odd(x), odd(W), odd(dY), odd(Z))
+    assert all(torch.equal(got[name], again[name]) for name in got)
+    dY[1, 3] = float("inf")
+    W = W.abs() + 0.125
+    dX = p.backward(x, W, dY, Z.abs())["dX"]
+    assert (dX[1] == float("inf")).all() and torch.isfinite(dX[0]).all() and torch.isfinite(dX[2:]).all()
+    assert L.luna_device_status(p.ws) == 0
