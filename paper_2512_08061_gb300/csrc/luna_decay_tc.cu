@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
     if (warp == kTma) {
         if (lane == 0) {
             uint32_t uses = 0;  // bit s: parity of the phases of freeb[s] waited for
+            int issued = 0;
             for (int item = blockIdx.x; item < items && !failed; item += gridDim.x) {
                 const Piece t(a, item);
                 const int head[3] = {t.h / (a.H / a.a.heads), t.h / (a.H / a.b.heads), t.h / (a.H / a.c.heads)};
@@ -244,11 +245,14 @@ __global__ void __launch_bounds__(Cfg<D, NT, STATE>::THREADS, 1)
                         mbar_arrive_expect_tx(full + s, C::TILE);
                         for (int k = 0; k < C::KB; ++k)
                             tma_load_4d(sm + s * C::TILE + k * C::BLK, m, 64 * k, row, head[w], t.b, full + s);
+                        issued = L + 1;
                     }
                 }
                 if (!C::STAYS) break;
                 base_c += t.nch;
             }
+            // no load may be on its way when the block ends, which one that has given up elsewhere would not wait for
+            for (int L = max(0, issued - kSlots); L < issued; ++L) mbar_wait(full + L % kSlots, (L / kSlots) & 1, kDrainNs);
         }
     } else if (warp == kMma) {
         if (lane == 0) {

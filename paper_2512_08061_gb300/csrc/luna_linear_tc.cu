@@ -263,6 +263,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     }
                 }
             }
+            // no load may be on its way when the block ends, which one that has given up elsewhere would not wait for
+            // (the leader's barriers count the pair's, and the other block waits for it)
+            if (rank == 0)
+                for (int i = max(0, it - S); i < it; ++i) mbar_wait(full + i % S, (i / S) & 1, kDrainNs);
         }
     } else if (warp == kWarpMma) {
         if (lane == 0 && rank == 0) {

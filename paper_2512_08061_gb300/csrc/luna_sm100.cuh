@@ -91,6 +91,8 @@ __device__ __forceinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, u
     return mbar_try_wait(bar, parity) || mbar_wait_loop(smem_u32(bar), parity, limit_ns);
 }
 
+constexpr uint64_t kDrainNs = 100000000ull;  // the limit of a wait for a block's own copies at its end
+
 // ---------------------------------------------------------------------------
 // 32-byte global accesses (sm_100 family): one whole sector per thread and
 // instruction.  The address must be 32-byte aligned.
