@@ -502,13 +502,17 @@ def _handle(stream):
     return _raw_stream(torch.cuda.current_device())
 
 
-def _new(stream, make, *args, **kwargs):
-    """A new tensor for a call on `stream` (None: the current one), from that stream's memory: the allocator may
-    hand it out again only behind the call's kernels."""
+def _new(stream, make=torch.empty):
+    """torch.empty (or what `make` is) for a call on `stream` (None: the current one), from that stream's memory: the
+    allocator may hand it out again only behind the call's kernels."""
     if stream is None:
-        return make(*args, **kwargs)
-    with torch.cuda.stream(stream):
-        return make(*args, **kwargs)
+        return make
+
+    def on_stream(*args, **kwargs):
+        with torch.cuda.stream(stream):
+            return make(*args, **kwargs)
+
+    return on_stream
 
 
 class _Checked:
@@ -530,7 +534,10 @@ class _Checked:
 
     def _on(self, stream):
         """The handle of the stream of a call; the workspace stays until what is queued there is done."""
-        handle = _handle(stream)
+        if stream is None and _raw_stream is not None:  # (as _handle, without its call)
+            handle = _raw_stream(torch.cuda.current_device())
+        else:
+            handle = _handle(stream)
         if handle not in self._streams and self.ws is not None:
             self.ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
             self._streams.add(handle)
@@ -603,7 +610,7 @@ class Decay(_Checked):
         if O is None:
             O = self._new_output(Q, stream)
         if want_state and S1 is None:
-            S1 = _new(stream, torch.empty, self.state_shape, dtype=torch.float32, device=Q.device)
+            S1 = _new(stream)(self.state_shape, dtype=torch.float32, device=Q.device)
         _check(_lib.luna_decay_fwd(self._ref["forward"], log_decay.data_ptr(), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
                                    _addr(lengths), _addr(S0), O.data_ptr(), _addr(S1), *self._ws, self._on(stream)),
                "luna_decay_fwd")
@@ -612,15 +619,15 @@ class Decay(_Checked):
     def _new_output(self, Q, stream):
         shape = self.shapes["o"]
         if self._like is None:
-            return _new(stream, torch.empty, shape, dtype=self.io, device=Q.device)
-        return _new(stream, torch.empty_strided, shape, self._like, dtype=self.io, device=Q.device)
+            return _new(stream)(shape, dtype=self.io, device=Q.device)
+        return _new(stream, torch.empty_strided)(shape, self._like, dtype=self.io, device=Q.device)
 
     def backward(self, Q, K, V, dO, log_decay, lengths=None, S0=None, dS1=None, out=None, stream=None):
         """dQ, dK, dV, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
         if out is None:
-            out = {"d" + k: _new(stream, torch.empty_like, t) for k, t in (("Q", Q), ("K", K), ("V", V))}
+            out = {"d" + k: _new(stream, torch.empty_like)(t) for k, t in (("Q", Q), ("K", K), ("V", V))}
             if S0 is not None:
-                out["dS0"] = _new(stream, torch.empty, self.state_shape, dtype=torch.float32, device=Q.device)
+                out["dS0"] = _new(stream)(self.state_shape, dtype=torch.float32, device=Q.device)
         dQ, dK, dV, dS0 = out["dQ"], out["dK"], out["dV"], out.get("dS0")
         if not self._looked_at("backward", Q, K, V, dO, log_decay, lengths, S0, dS1, dQ, dK, dV, dS0):
             for field, t in (("q", Q), ("k", K), ("v", V), ("go", dO), ("gq", dQ), ("gk", dK), ("gv", dV)):
@@ -636,7 +643,7 @@ class Decay(_Checked):
     def step(self, q, k, v, log_decay, S, slots=None, o=None, stream=None):
         """One token: q (B, H, d), k (B, Hkv, d), v (B, Hkv, dv); S (nslots, H, d, dv) is advanced in place."""
         if o is None:
-            o = _new(stream, torch.empty, self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=q.device)
+            o = _new(stream)(self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=q.device)
         if not self._looked_at("step", q, k, v, log_decay, S, slots, o):
             for field, t in (("q", q), ("k", k), ("v", v), ("o", o)):
                 self._view("step", field, t)
@@ -686,9 +693,9 @@ class BlockNorm(_Checked):
     def forward(self, x, y, gate=None, w_post=None, w_pre=None, b_post=None, b_pre=None, X=None, H=None, stream=None):
         """{"X": x'} where there is a residual or no second norm (or X is given), {"H": h} with w_pre."""
         if X is None and ((x is not None and y is not None) or w_pre is None):
-            X = _new(stream, torch.empty, self.shape, dtype=self.io, device=(y if x is None else x).device)
+            X = _new(stream)(self.shape, dtype=self.io, device=(y if x is None else x).device)
         if H is None and w_pre is not None:
-            H = _new(stream, torch.empty, self.shape, dtype=self.io, device=(y if x is None else x).device)
+            H = _new(stream)(self.shape, dtype=self.io, device=(y if x is None else x).device)
         if not self._looked_at("forward", x, y, gate, w_post, w_pre, b_post, b_pre, X, H):
             self._rows("forward", x=x, y=y, gate=gate, X=X, H=H)
             self._weights(w_post=w_post, w_pre=w_pre, b_post=b_post, b_pre=b_pre)
@@ -702,9 +709,9 @@ class BlockNorm(_Checked):
     def backward(self, x, y, gate, w_post, w_pre, dX, dH, b_post=None, b_pre=None, out=None, stream=None):
         """dx, dy, dgate, dw_post, dw_pre of what forward was given, and db_post, db_pre of given biases."""
         if out is None:
-            out = {k: _new(stream, torch.empty, self.shape, dtype=self.io, device=t.device)
+            out = {k: _new(stream)(self.shape, dtype=self.io, device=t.device)
                    for k, t in (("dx", x), ("dy", y), ("dgate", gate)) if t is not None}
-            out.update({k: _new(stream, torch.empty_like, t)
+            out.update({k: _new(stream, torch.empty_like)(t)
                         for k, t in (("dw_post", w_post), ("dw_pre", w_pre), ("db_post", b_post), ("db_pre", b_pre))
                         if t is not None})
         g = [out.get(k) for k in ("dx", "dy", "dgate", "dw_post", "db_post", "dw_pre", "db_pre")]
@@ -741,9 +748,9 @@ class Linear(_Checked):
     def forward(self, x, W, bias=None, r=None, save_z=False, Y=None, Z=None, stream=None):
         """Y, or (Y, z) with save_z."""
         if Y is None:
-            Y = _new(stream, torch.empty, (self.m, self.n), dtype=self.io, device=x.device)
+            Y = _new(stream)((self.m, self.n), dtype=self.io, device=x.device)
         if save_z and Z is None:
-            Z = _new(stream, torch.empty, (self.m, self.n), dtype=self.io, device=x.device)
+            Z = _new(stream)((self.m, self.n), dtype=self.io, device=x.device)
         if not self._looked_at("forward", x, W, bias, r, Y, Z):
             self._rows("forward", x=x, w=W, r=r, y=Y, z=Z)
             self._vector("bias", bias, (self.n,))
@@ -755,10 +762,10 @@ class Linear(_Checked):
     def backward(self, x, W, dY, Z=None, bias=False, out=None, stream=None):
         """dX, dW and with `bias` db; Z is forward's z (needed with an activation)."""
         if out is None:
-            out = {"dX": _new(stream, torch.empty, (self.m, self.k), dtype=self.io, device=dY.device),
-                   "dW": _new(stream, torch.empty, (self.n, self.k), dtype=self.io, device=dY.device)}
+            out = {"dX": _new(stream)((self.m, self.k), dtype=self.io, device=dY.device),
+                   "dW": _new(stream)((self.n, self.k), dtype=self.io, device=dY.device)}
             if bias:
-                out["db"] = _new(stream, torch.empty, self.n, dtype=self.io, device=dY.device)
+                out["db"] = _new(stream)(self.n, dtype=self.io, device=dY.device)
         dX, dW, db = out.get("dX"), out.get("dW"), out.get("db")
         if not self._looked_at("backward", x, W, Z, dY, dX, dW, db):
             self._rows("backward", x=x, w=W, z=Z, dy=dY, dx=dX)
