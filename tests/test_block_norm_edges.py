@@ -75,3 +75,35 @@ def test_rows_of_absent_matrices(L, cols, groups, io):
     h = torch.empty_like(t["y"])
     L.luna_norm_fwd(nd, None, t["y"], None, t["w_post"], None, t["w_pre"], None, None, h)
     assert torch.equal(h, want["H"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("gate", ["none", "sigmoid", "silu"])
+def test_gradients_against_extrapolated_differences(L, kind, gate):
+    """Central differences of the 32-bit forward at steps of 1e-2 and 2e-2, extrapolated: what is left of the
+    curvature is under 3e-7 of the terms' norm (in 64 bits, over 20 draws of this problem), and 576 outputs rounded at
+    some 1.5 2^-24 leave about sqrt(576) 9e-8 / 2e-2 * 5/3 = 2e-4 beside terms of a norm of 10 and more: 1e-3."""
+    rows, cols, step = 6, 48, 1e-2
+    g = torch.Generator("cuda").manual_seed(2)
+    t = {k: torch.randn((rows, cols), generator=g, device="cuda") for k in ("x", "y", "gate")}
+    t.update({k: torch.randn(cols, generator=g, device="cuda") for k in ("w_post", "w_pre", "b_post", "b_pre")})
+    dX, dH = (torch.randn((rows, cols), generator=g, device="cuda") for _ in range(2))
+    if gate == "none":
+        t["gate"] = None
+    p = L.BlockNorm(rows, cols, 3, kind, gate, 0.5, 1e-2, F, backward=True)
+    args = ("x", "y", "gate", "w_post", "w_pre", "b_post", "b_pre")
+    back = p.backward(*(t[k] for k in args[:5]), dX, dH, t["b_post"], t["b_pre"])
+    for k in args:
+        if t[k] is None:
+            continue
+        by = torch.randn(t[k].shape, generator=g, device="cuda")
+        slope = []
+        for h in (step, 2 * step):
+            loss = []
+            for sign in (1, -1):
+                o = p.forward(*(t[j] + sign * h * by if j == k else t[j] for j in args))
+                loss.append((o["X"].double() * dX).sum() + (o["H"].double() * dH).sum())
+            slope.append((loss[0] - loss[1]) / (2 * h))
+        terms = back["d" + k].double() * by
+        assert abs((4 * slope[0] - slope[1]) / 3 - terms.sum()) < 1e-3 * terms.norm(), k
