@@ -308,12 +308,14 @@ __global__ void __launch_bounds__(256) k_decay_group_sum(const float *src, int H
 // block at a time, every load of a thread in flight before the first is used.  The state is
 // read and written once, which bounds the step (47 us for 270 MB of states and tokens, 5.7 TB/s);
 // the column split keeps one sequence's 32 heads on 128 blocks.
+// lambda has a second term: rounded to fp32 alone it is off by up to 3e-8 the same way at every token, which
+// after 30000 tokens of slow decay has been 1.1e-3 of the state.
 
 constexpr int kStepThreads = 256;
 
 template <typename IO, bool VEC>
 __global__ void __launch_bounds__(kStepThreads) k_decay_step(DecayStep a) {
-    __shared__ float sq[kMaxD], sk[kMaxD];
+    __shared__ float sq[kMaxD], sk[kMaxD], slam[2];
     __shared__ float so[kStepThreads / 32][kCols];
     const int tid = threadIdx.x;
     const int64_t bh = blockIdx.x;
@@ -354,8 +356,14 @@ __global__ void __launch_bounds__(kStepThreads) k_decay_step(DecayStep a) {
     for (int i = tid; i < a.d; i += kStepThreads) { sq[i] = io_load(q + i); sk[i] = io_load(k + i); }
 #pragma unroll
     for (int t = 0; t < 4; ++t) vc[t] = c + t < a.dv ? io_load(v + c + t) : 0.0f;
-    const float lam = expf(decay_log(a.log_decay, h));
+    if (tid == kStepThreads - 1) {  // (once a block: by every thread 16.4 us at 64 x 32 heads of 64 x 64, so 14.5)
+        const float g = decay_log(a.log_decay, h), m1 = expm1f(g);
+        const bool slow = fabsf(g) < 0.5f;  // (beyond that a state forgets, or overflows, in some ten tokens)
+        slam[0] = slow ? 1.0f + m1 : expf(g);
+        slam[1] = slow ? m1 - (slam[0] - 1.0f) : 0.0f;
+    }
     __syncthreads();
+    const float lam = slam[0], rest = slam[1];
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -363,8 +371,8 @@ __global__ void __launch_bounds__(kStepThreads) k_decay_step(DecayStep a) {
         if (f < a.d) {
             const float kf = sk[f], qf = sq[f];
             float4 w = s[i];
-            w.x = fmaf(lam, w.x, kf * vc[0]); w.y = fmaf(lam, w.y, kf * vc[1]);
-            w.z = fmaf(lam, w.z, kf * vc[2]); w.w = fmaf(lam, w.w, kf * vc[3]);
+            w.x = fmaf(lam, w.x, fmaf(rest, w.x, kf * vc[0])); w.y = fmaf(lam, w.y, fmaf(rest, w.y, kf * vc[1]));
+            w.z = fmaf(lam, w.z, fmaf(rest, w.z, kf * vc[2])); w.w = fmaf(lam, w.w, fmaf(rest, w.w, kf * vc[3]));
             float *p = S + (int64_t)f * a.dv + c;
             if (VEC) {
                 if (c < a.dv) *reinterpret_cast<float4 *>(p) = w;
