@@ -48,8 +48,8 @@ __device__ __forceinline__ void store4(OUT *p, int c, int width, bool vec, const
 // Every product runs from shared memory with a register tile a thread (4 x 4 scores, 4 rows x DC / 16
 // outputs, DA / 16 x DC / 16 of the state, which stays in registers and is copied to shared memory for
 // the outputs), 16-byte reads without bank conflicts, two multiply-adds an instruction.  Bound by the
-// fp32 FMA rate at width 128 (2.2 ms in two passes for 160 heads of 5276 rows at 128 x 64 in fp32, some
-// 28 TFLOP/s), by the loads' latency at small widths, where two blocks share an SM.
+// fp32 FMA rate at width 128 (2.6 ms in two passes for 160 heads of 5276 rows at 128 x 64 in fp32, some
+// 24 TFLOP/s), by the loads' latency at small widths, where two blocks share an SM.
 // CH: rows of a chunk, 64, or 16 where no sequence is longer than that.
 template <typename IO, typename OUT, int DA, int DC, int CH>
 __global__ void __launch_bounds__(kMixThreads, DA + DC <= 128 ? 2 : 1) k_decay_mix(DecayMix a) {
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(256) k_decay_group_sum(const float *src, int H
 // One token: S <- lambda S + k v^T, o = scale q^T S.  A block owns 32 columns of one
 // head's state: 8 lanes x 16 bytes cover a row's 128 bytes, four rows a warp, 32 rows a
 // block at a time, every load of a thread in flight before the first is used.  The state is
-// read and written once, which bounds the step (47 us for 270 MB of states and tokens, 5.7 TB/s);
+// read and written once, which bounds the step (45 to 47 us for 270 MB of states and tokens, 5.7 to 6 TB/s);
 // the column split keeps one sequence's 32 heads on 128 blocks.
 // lambda has a second term: rounded to fp32 alone it is off by up to 3e-8 the same way at every token, which
 // after 30000 tokens of slow decay has been 1.1e-3 of the state.

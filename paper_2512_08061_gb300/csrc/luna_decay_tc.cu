@@ -12,9 +12,14 @@
 // the others two (their state only enters outputs as one more bf16 rounding).  X is not accumulated by
 // the products themselves: their additions onto a large X round toward zero, chunk after chunk.
 //
+// P and the operand X are one bf16 rounding each, which outputs carry beside their own (2.3e-3 to 2.5e-3 off where
+// that alone leaves 1.7e-3) and no state does.  A second term of both would add a D-deep and a 128-deep product to the
+// chain below, and at D = 128 another 32 KB of operand to shared memory, which is full.
+//
 // Measured: 115 us for 128 heads of 4096 rows at d = dv = 128 (537 MB, 4.7 TB/s), issue 34 %, tensor 31 %.
-// Bound: the chain of the steps above, some 5000 cycles a chunk at d = 128.  By its bytes the pass is (da + dc) * 4 bytes a row at HBM rate; the shared-memory traffic of
-// the products' operands and of the scaled terms comes next (about 2/3 of that at d = 128).  Three
+// Bound: the chain of the steps above, some 5000 cycles a chunk at d = 128.  By its bytes the pass is (da + dc) * 4
+// bytes a row at HBM rate; the shared-memory traffic of the products' operands and of the scaled terms comes next
+// (about 2/3 of that at d = 128).  Three
 // groups of warps (the scaled b; X; P and out) work on their parts of neighbouring chunks side by side,
 // and the next tiles load while they do: a ring of four slots takes a, b, c in turn.
 #include <math.h>

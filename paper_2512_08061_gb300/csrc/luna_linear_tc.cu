@@ -19,10 +19,10 @@
 // of the six products a2 b0 + a1 b1 + a0 b2 + a1 b0 + a0 b1 + a0 b0; what is left out is under 2^-21 of
 // |a| |b|.  A stage holds one plane of both operands, and the products of three stages run together, the
 // small ones first: loading each product's planes anew took the L2 twice the bytes and half as long
-// again (917 us at 4096 x 4096 x 4096, now 719 us, of which the splitting takes 60).  The tensor cores add to their fp32 accumulator by cutting off,
-// which at a depth of 1024 has lost 1.7e-6 of a sum of positive products and at 64 1e-7 (measured), so
-// after every 64 of K the epilogue's warps add the accumulator to an fp32 sum that they keep in TMEM
-// beside it.  bf16 sums over more than 65536 of K are joined like this every 16384 (LONG): cut off all the
+// again (917 us at 4096 x 4096 x 4096, now 719 to 726 us, of which the splitting takes 60).  The tensor
+// cores add to their fp32 accumulator by cutting off, which at a depth of 1024 has lost 1.7e-6 of a sum of
+// positive products and at 64 1e-7 (measured), so after every 64 of K the epilogue's warps add the
+// accumulator to an fp32 sum that they keep in TMEM beside it.  bf16 sums over more than 65536 of K are joined like this every 16384 (LONG): cut off all the
 // way, 2^20 rows of positive products lost 6.9e-3 of a weight's gradient, twice its bf16 rounding, 65536 rows
 // 1e-4.  The fp32 sum takes the place of the second accumulator there (5.14 ms at 2^20 x 1600
 // x 1600 against 5.05 without it).
