@@ -399,12 +399,14 @@ template <typename IO, int VEC>
 void dz_launch(const void *dY, int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, int64_t lo, int64_t m, int n,
                int act, float *part, int parts, int *status, cudaStream_t s) {
     const dim3 grid((unsigned)cdiv(std::max<int64_t>(n, lo), 32 * VEC), parts);
-    if (lo)
-        LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, true>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
-                    static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
-    else
-        LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, false>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
-                    static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
+    if constexpr (sizeof(IO) == 2)
+        if (lo) {
+            LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, true>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
+                        static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
+            return;
+        }
+    LUNA_LAUNCH("linear_dz", (k_linear_dz<IO, VEC, false>), grid, 256, 0, s, static_cast<const IO *>(dY), lddy,
+                static_cast<const IO *>(Z), ldz, static_cast<IO *>(dZ), lddz, lo, m, n, act, kDzRows, part, status);
 }
 
 template <typename IO>
