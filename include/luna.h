@@ -372,6 +372,109 @@ luna_status luna_decay_bwd(const luna_decay_desc *dd, const float *log_decay, co
 luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, const void *q, const void *k,
                             const void *v, const int32_t *slots, int nslots, float *S, void *o, void *stream);
 
+/* The gated delta rule: linear attention whose state forgets by a gate of each
+ * token and takes in the difference between a value and what the state already
+ * gives for its key.  With a_t = exp(g_t) and the state S (d x dv, fp32) of each
+ * (b, h):
+ *
+ *     S_t = a_t (S_{t-1} - beta_t k_t (k_t^T S_{t-1})) + beta_t k_t v_t^T,    o_t = scale * S_t^T q_t
+ *
+ * H heads of values, states and gates share Hk heads of queries and keys (H a
+ * multiple of Hk): head h reads head h / (H / Hk).  log_decay (g) and beta are
+ * (B, H, n) tensors of type io with strides of their own (g, beta; all three 0:
+ * contiguous); g = -inf (a = 0: the state starts anew) is valid and takes a
+ * gradient of 0.  Keys are meant to have length one and beta to lie in [0, 2];
+ * with beta |k|^2 above 2 the recurrence itself grows, and nothing checks that.
+ * Rows at or past a sequence's length neither enter the state nor are read; their
+ * outputs and gradients are 0.  A value that is not finite in a valid row may
+ * reach any valid row of the sequence.
+ * Supported: 1 <= d, dv <= 128, n <= 2^24, B * H <= 2^24, B * H * n <= 2^36;
+ * empty problems are no-ops (n = 0 copies the initial state). */
+typedef struct {
+    int B, H, Hk, n, d, dv;
+    float scale;
+    luna_dtype io;
+    luna_strides q, k, v, o, g, beta;              /* Q, K, V, O, log_decay, beta */
+    luna_strides gq, gk, gv, go, gg, gbeta;        /* dQ, dK, dV, dO, dlog_decay, dbeta (luna_delta_bwd only) */
+} luna_delta_desc;
+
+/* Bytes of scratch memory of luna_delta_fwd (backward = 0) or luna_delta_bwd
+ * (1); the workspace must be 256-byte aligned.  The size does not depend on the
+ * strides. */
+luna_status luna_delta_workspace_size(const luna_delta_desc *dd, int backward, size_t *bytes);
+
+/* Whole prompts.  S0: NULL (zero) or the initial states, fp32 [B][H][d][dv];
+ * S1: NULL or the states after each sequence's last valid token, the same
+ * layout (S1 may be S0 itself). */
+luna_status luna_delta_fwd(const luna_delta_desc *dd, const void *log_decay, const void *beta, const void *Q,
+                           const void *K, const void *V, const int32_t *lengths, const float *S0, void *O, float *S1,
+                           void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradients of luna_delta_fwd on the same inputs.  dS1: NULL (zero) or the
+ * gradient of the final states; dS0: NULL or the gradient of the initial states
+ * (dS0 may be dS1 itself).  The gradients of shared queries and keys are summed
+ * over their heads in fp32, in head order.  No atomics: equal inputs give equal
+ * bits. */
+luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, const void *beta, const void *Q,
+                           const void *K, const void *V, const void *dO, const int32_t *lengths, const float *S0,
+                           const float *dS1, void *dQ, void *dK, void *dV, void *dlog_decay, void *dbeta, float *dS0,
+                           void *workspace, size_t ws_bytes, void *stream);
+
+/* One token of each of B sequences, in place in a pool of states, fp32
+ * [nslots][H][d][dv]; slots as in luna_decay_step.  q, k, v, o, log_decay and
+ * beta are one token for each head; the strides .b and .h of the descriptor apply
+ * (all three 0: contiguous) and n and .t are ignored. */
+luna_status luna_delta_step(const luna_delta_desc *dd, const void *log_decay, const void *beta, const void *q,
+                            const void *k, const void *v, const int32_t *slots, int nslots, float *S, void *o,
+                            void *stream);
+
+/* Beam search over recurrent states: K beams of each of B sequences, a
+ * vocabulary of V tokens.
+ *
+ * luna_beam_select takes the logits of the next token, B * K rows of V (type io,
+ * ld elements apart; 0 = V), and the beams' running log-probabilities `scores`
+ * (fp32, B x K), and gives the K best of a sequence's candidates
+ *
+ *     scores[k] + logits[k][t] - log sum_t' exp(logits[k][t'])
+ *
+ * over all k and t, best first: their scores (fp32), tokens and parent beams
+ * (int32, B x K).  Scores are compared in 64 bits; equal ones go by the lower
+ * beam, then the lower token.  A beam of score -inf (one that is not in use yet),
+ * with a score or a logit that is NaN or +inf, or whose logits are all -inf, has
+ * candidates of score -inf alone, which come behind all others.
+ * end: the token that ends a sequence, or -1 (none; done and done_out are then
+ * NULL).  done: NULL (none) or B x K bytes, not 0 where a beam has ended: its
+ * logits are not read, and its one candidate is itself with the token `end` and
+ * the score it has.  done_out: NULL, or where the new beams have ended.
+ * scores_out and done_out may be scores and done themselves.
+ *
+ * luna_beam_reorder lets the states in a pool follow their beams.  The pool has
+ * nslots slots of slot_bytes each; slots (int32, B x K) says where each old
+ * beam's state is, and new_slots (another array) receives where the new beams'
+ * states are: the first child of a beam keeps its slot, further children get
+ * copies in the slots of beams without a child, in order.  No two beams may share
+ * a slot.  Slots outside [0, nslots) are neither read nor written; a parent
+ * outside [0, K) stands for none (the beam takes a free slot as it is).  Several
+ * pools are reordered by one call each with the same slots; pool may be NULL with
+ * slot_bytes = 0 (new_slots alone).
+ * Supported: K <= 32, V <= 2^24, B * K <= 65535; B = 0 is a no-op. */
+typedef struct {
+    int B, K, V;
+    luna_dtype io;
+    int64_t ld;
+    int end;
+} luna_beam_desc;
+
+/* Bytes of the workspace of luna_beam_select (256-byte aligned). */
+luna_status luna_beam_workspace_size(const luna_beam_desc *bd, size_t *bytes);
+
+luna_status luna_beam_select(const luna_beam_desc *bd, const void *logits, const float *scores, const uint8_t *done,
+                             float *scores_out, int32_t *tokens, int32_t *parents, uint8_t *done_out, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+luna_status luna_beam_reorder(const luna_beam_desc *bd, const int32_t *parents, const int32_t *slots, int nslots,
+                              void *pool, size_t slot_bytes, int32_t *new_slots, void *stream);
+
 /* The norms after and before a block, fused with its gate and its residual
  * scale, over `rows` rows of `cols` values:
  *

@@ -1,0 +1,434 @@
+// Beam search over recurrent states: the best continuations of every sequence, and the states that follow them.
+#include <math.h>
+
+#include <algorithm>
+
+#include "luna_common.cuh"
+#include "luna_prof.cuh"
+
+namespace luna {
+int tc_sm_count();
+
+namespace {
+
+constexpr int kMaxBeams = 32;                  // a warp's lanes
+constexpr int kThreads = 256, kPer = 32;       // values of a piece that a thread holds
+constexpr int kPiece = kThreads * kPer;
+
+// Values as integers in the same order; larger is better.
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) {
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ uint64_t ordered(double x) {
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    return u >> 63 ? ~u : u | (uint64_t(1) << 63);
+}
+__device__ __forceinline__ double unordered(uint64_t u) {
+    return __longlong_as_double((long long)(u >> 63 ? u & ~(uint64_t(1) << 63) : ~u));
+}
+
+// A candidate of one row: its logit, and at equal logits the lower token first.  0: none.
+struct RowKey {
+    uint64_t v = 0;
+    __device__ bool over(const RowKey &o) const { return v > o.v; }
+    __device__ RowKey lane_xor(int w) const { return RowKey{__shfl_xor_sync(0xffffffffu, v, w)}; }
+};
+// A candidate of a sequence: its score, and at equal scores the lower beam, then the lower token first.  v = 0: none.
+struct SeqKey {
+    uint64_t v = 0;
+    uint32_t i = 0;  // ~(beam * V + token)
+    __device__ bool over(const SeqKey &o) const { return v > o.v || (v == o.v && i > o.i); }
+    __device__ SeqKey lane_xor(int w) const {
+        return SeqKey{__shfl_xor_sync(0xffffffffu, v, w), __shfl_xor_sync(0xffffffffu, i, w)};
+    }
+};
+
+// The place of every thread's candidate among the block's 256: each warp sorts its own by exchanges, then each looks
+// its candidate up in the other warps' lists.  Equal ones (none at all) go by their place in `list`.  `key` becomes
+// the candidate that the returned place is of.  All threads call it; `list` may be written again after a barrier.
+template <typename Key>
+__device__ int place_in_block(Key &key, Key *list) {
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int w = size / 2; w > 0; w /= 2) {
+            const Key other = key.lane_xor(w);
+            const bool low = (lane & w) == 0, down = (lane & size) == 0 || size == 32;  // the larger one goes low where `down`
+            if (low == down ? other.over(key) : key.over(other)) key = other;
+        }
+    list[threadIdx.x] = key;
+    __syncthreads();
+    int place = lane;
+    for (int o = 0; o < kThreads / 32; ++o) {
+        if (o == warp) continue;
+        const Key *l = list + 32 * o;
+        auto before = [&](const Key &x) { return o < warp ? !key.over(x) : x.over(key); };
+        int n = 0;
+#pragma unroll
+        for (int w = 16; w > 0; w /= 2)
+            if (before(l[n + w - 1])) n += w;
+        if (before(l[n])) ++n;
+        place += n;
+    }
+    return place;
+}
+
+// The K best of `count` candidates in `from`, in order, into best (its first `have` are candidates too): 256 at a time.
+template <typename Key>
+__device__ void best_of(const Key *from, int count, Key *best, int have, int K, Key *list) {
+    const int tid = threadIdx.x;
+    int at = 0;
+    do {
+        __syncthreads();
+        Key key = tid < have ? best[tid] : Key{};
+        const int take = min(count - at, kThreads - have);
+        if (tid >= have && tid - have < take) key = from[at + tid - have];
+        at += take;
+        const int place = place_in_block(key, list);  // (every best[] is read before its barrier)
+        if (place < K) best[place] = key;
+        have = K;
+    } while (at < count);
+    __syncthreads();
+}
+
+struct BeamArgs {
+    const void *logits;
+    int64_t ld;
+    const float *scores;
+    const uint8_t *done;
+    float *scores_out;
+    int32_t *tokens, *parents;
+    uint8_t *done_out;
+    int B, K, V, end, S;  // S: pieces of a row
+    uint64_t *keys;       // [B K][S][K]
+    float2 *stats;        // [B K][S]: maximum, sum of exp over it
+};
+
+// One part of one row: its maximum, its sum of exponentials and its K best values, in one reading.  A thread holds 32
+// values of a piece of 8192; only values that reach the K-th best of the threads' maxima (there are K as good) and the
+// K-th best so far are looked at again, so that of a piece a few dozen are sorted, at most 32 K.  Bound by the bytes
+// of the logits.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
+    constexpr int VEC = 16 / sizeof(T), NV = kPer / VEC;
+    __shared__ RowKey list[kThreads], best[kMaxBeams], pool[kMaxBeams * kPer], least;
+    __shared__ int count;
+    __shared__ float smax[kThreads / 32], ssum[kThreads / 32];
+    const int tid = threadIdx.x, row = blockIdx.y, part = blockIdx.x;
+    if (a.done && a.done[row]) return;
+    const T *x = static_cast<const T *>(a.logits) + row * a.ld;
+    // vectors that start on 16-byte boundaries: the first may begin before the row
+    const int off = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));
+    const int vectors = (a.V + off + VEC - 1) / VEC, pieces = (vectors + kPiece / VEC - 1) / (kPiece / VEC);
+    const int first = (int)((int64_t)pieces * part / a.S), last = (int)((int64_t)pieces * (part + 1) / a.S);
+    const float log2e = 1.4426950408889634f;
+    float top = -INFINITY, sum = 0.0f;
+    int have = 0;
+    for (int piece = first; piece < last; ++piece) {
+        float val[kPer];
+        const int v0 = piece * (kPiece / VEC) + tid;  // vectors of a thread: every 256th
+        auto token = [&](int i) { return (v0 + i / VEC * kThreads) * VEC - off + i % VEC; };
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int t = token(j * VEC);
+            if (t >= 0 && t + VEC <= a.V) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(x + t);
+                T e[VEC];
+                memcpy(e, &w, 16);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) val[j * VEC + i] = io_load(&e[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    val[j * VEC + i] = t + i >= 0 && t + i < a.V ? io_load(x + t + i) : -INFINITY;
+            }
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) m = fmaxf(m, val[i]);
+        const float now = fmaxf(top, m), base = now == -INFINITY ? 0.0f : now;
+        sum *= exp2f((top - base) * log2e);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sum += exp2f((val[i] - base) * log2e);
+        top = now;
+        auto key = [&](int i) {
+            const int t = token(i);
+            RowKey k;
+            if (t >= 0 && t < a.V && val[i] == val[i])  // (a row with a NaN has no scores; k_beam_join sees that by its sum)
+                k.v = (uint64_t)ordered(val[i] + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
+            return k;
+        };
+        // the thread's best: the first of its largest (tokens rise with i)
+        RowKey mine;
+#pragma unroll
+        for (int i = kPer - 1; i >= 0; --i)
+            if (val[i] == m) mine = key(i).over(mine) ? key(i) : mine;
+        const RowKey bar = have ? best[a.K - 1] : RowKey{};  // (none while fewer than K are found: v = 0)
+        if (__syncthreads_count(mine.over(bar)) == 0) continue;
+        RowKey k = mine;
+        const int place = place_in_block(k, list);
+        if (place == a.K - 1) least = k;
+        if (tid == 0) count = 0;
+        __syncthreads();
+        const RowKey need = least;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const RowKey c = key(i);
+            if (c.v && !need.over(c) && c.over(bar)) pool[atomicAdd(&count, 1)] = c;
+        }
+        __syncthreads();
+        best_of(pool, count, best, have, a.K, list);
+        have = a.K;
+    }
+    if (!have) {  // (fewer pieces than parts)
+        if (tid < a.K) best[tid] = RowKey{};
+        __syncthreads();
+    }
+    const int64_t at = (int64_t)row * a.S + part;
+    if (tid < a.K) a.keys[at * a.K + tid] = best[tid].v;
+    float m = top;
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    const float mb = m == -INFINITY ? 0.0f : m;
+    float s = sum * exp2f((top - mb) * log2e);
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
+    if (tid % 32 == 0) { smax[tid / 32] = m; ssum[tid / 32] = s; }
+    __syncthreads();
+    if (tid == 0) {
+        float all = 0.0f;
+        m = smax[0];
+        for (int w = 1; w < kThreads / 32; ++w) m = fmaxf(m, smax[w]);
+        const float b = m == -INFINITY ? 0.0f : m;
+        for (int w = 0; w < kThreads / 32; ++w) all += ssum[w] * exp2f((smax[w] - b) * log2e);
+        a.stats[at] = make_float2(m, all);
+    }
+}
+
+// The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that which of two near ones is better
+// does not hang on a rounding.  One block a sequence: K S K candidates, looked at twice as in k_beam_rows.
+__global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
+    extern __shared__ char raw[];
+    SeqKey *pool = reinterpret_cast<SeqKey *>(raw);
+    __shared__ SeqKey list[kThreads], best[kMaxBeams], least;
+    __shared__ double base[kMaxBeams];
+    __shared__ float score[kMaxBeams];
+    __shared__ uint8_t done[kMaxBeams];
+    __shared__ int count;
+    const int tid = threadIdx.x, b = blockIdx.x, K = a.K, S = a.S;
+    for (int k = tid / 32; k < K; k += kThreads / 32) {  // a warp a row
+        const int row = b * K + k, lane = tid % 32;
+        const bool over = a.done && a.done[row];
+        float m = -INFINITY;
+        double sum = 0.0;
+        if (!over) {
+            for (int s = lane; s < S; s += 32) m = fmaxf(m, a.stats[(int64_t)row * S + s].x);
+#pragma unroll
+            for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+            for (int s = lane; s < S; s += 32) {
+                const float2 p = a.stats[(int64_t)row * S + s];
+                sum += p.x == -INFINITY && p.y == 0.0f ? 0.0 : (double)p.y * exp((double)p.x - (double)m);
+            }
+#pragma unroll
+            for (int w = 16; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        }
+        if (lane == 0) {
+            score[k] = a.scores[row];
+            done[k] = over;
+            base[k] = over ? 0.0 : (double)score[k] - ((double)m + log(sum));
+        }
+    }
+    if (tid == 0) count = 0;
+    __syncthreads();
+    const int N = K * S * K;
+    auto candidate = [&](int n) {
+        const int k = n / (S * K), j = n - k * (S * K);
+        SeqKey c;
+        double v = -INFINITY;
+        int token;
+        if (done[k] || !isfinite(base[k])) {
+            // an ended beam goes on as itself; what no score can be given to comes behind everything, by its place
+            if (j >= K) return c;
+            token = done[k] ? (j == 0 ? a.end : j - (j <= a.end)) : j;
+            if (token >= a.V) return c;
+            if (done[k] && j == 0 && !(score[k] != score[k])) v = (double)score[k];
+        } else {
+            const uint64_t key = a.keys[(int64_t)b * N + n];
+            if (!key) return c;
+            token = (int)~(uint32_t)key;
+            v = base[k] + (double)unordered((uint32_t)(key >> 32));
+        }
+        c.v = ordered(v + 0.0);
+        c.i = ~(uint32_t)(k * a.V + token);
+        return c;
+    };
+    SeqKey mine;
+    for (int n = tid; n < N; n += kThreads) {
+        const SeqKey c = candidate(n);
+        if (c.over(mine)) mine = c;
+    }
+    const int place = place_in_block(mine, list);
+    if (place == K - 1) least = mine;
+    __syncthreads();
+    const SeqKey need = least;
+    for (int n = tid; n < N; n += kThreads) {
+        const SeqKey c = candidate(n);
+        if (c.v && !need.over(c)) pool[atomicAdd(&count, 1)] = c;
+    }
+    __syncthreads();
+    best_of(pool, count, best, 0, K, list);
+    if (tid < K) {
+        const uint32_t at = ~best[tid].i;
+        const int parent = (int)(at / a.V), token = (int)(at - (uint32_t)parent * a.V);
+        a.scores_out[b * K + tid] = (float)unordered(best[tid].v);
+        a.tokens[b * K + tid] = token;
+        a.parents[b * K + tid] = parent;
+        if (a.done_out) a.done_out[b * K + tid] = done[parent] || token == a.end;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The states follow their beams: the first child of a beam keeps its slot, further children get copies in the slots
+// of beams without a child, so that sources and destinations of the copies never meet and each copied state moves
+// once.  A block works out the K beams of its sequence in one warp and copies its part of every state that moves;
+// bound by the bytes of those.
+
+constexpr int kCopyThreads = 256, kCopyVecs = 4;
+
+template <typename V>
+__global__ void __launch_bounds__(kCopyThreads) k_beam_reorder(const int32_t *parents, const int32_t *slots, int K,
+                                                               int nslots, char *pool, int64_t slot_bytes, int32_t *out) {
+    __shared__ int from[kMaxBeams], to[kMaxBeams], moves;
+    const int tid = threadIdx.x, b = blockIdx.y;
+    if (tid < 32) {
+        const bool in = tid < K;
+        int p = in ? parents[b * K + tid] : -1;
+        if (p < 0 || p >= K) p = -1;
+        const unsigned same = __match_any_sync(0xffffffffu, p), below = (1u << tid) - 1;
+        const bool keeps = p >= 0 && (same & below) == 0;
+        const unsigned kept = __reduce_or_sync(0xffffffffu, p >= 0 ? 1u << p : 0u);
+        const unsigned others = __ballot_sync(0xffffffffu, in && !keeps);
+        const unsigned beams = K == 32 ? 0xffffffffu : (1u << K) - 1;
+        int place = p;
+        if (in && !keeps) place = __fns(beams & ~kept, 0, __popc(others & below) + 1);
+        const int slot = in ? slots[b * K + place] : -1;
+        if (in && blockIdx.x == 0) out[b * K + tid] = slot;
+        const int src = in && p >= 0 ? slots[b * K + p] : -1;
+        const bool copies = in && !keeps && p >= 0 && src >= 0 && src < nslots && slot >= 0 && slot < nslots;
+        const unsigned all = __ballot_sync(0xffffffffu, copies);
+        if (copies) {
+            from[__popc(all & below)] = src;
+            to[__popc(all & below)] = slot;
+        }
+        if (tid == 0) moves = __popc(all);
+    }
+    __syncthreads();
+    const int64_t vecs = slot_bytes / (int64_t)sizeof(V), step = (int64_t)gridDim.x * kCopyThreads * kCopyVecs;
+    for (int64_t v0 = (int64_t)blockIdx.x * kCopyThreads * kCopyVecs + tid; v0 < vecs; v0 += step)
+        for (int c = 0; c < moves; ++c) {
+            const V *src = reinterpret_cast<const V *>(pool + (int64_t)from[c] * slot_bytes);
+            V *dst = reinterpret_cast<V *>(pool + (int64_t)to[c] * slot_bytes);
+            V w[kCopyVecs];
+#pragma unroll
+            for (int i = 0; i < kCopyVecs; ++i)
+                if (v0 + i * kCopyThreads < vecs) w[i] = src[v0 + i * kCopyThreads];
+#pragma unroll
+            for (int i = 0; i < kCopyVecs; ++i)
+                if (v0 + i * kCopyThreads < vecs) dst[v0 + i * kCopyThreads] = w[i];
+        }
+}
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+luna_status check(const luna_beam_desc *bd) {
+    if (!bd || bd->B < 0 || bd->K < 1 || bd->V < 0) return LUNA_ERR_INVALID_ARG;
+    if (bd->io != LUNA_F32 && bd->io != LUNA_BF16) return LUNA_ERR_INVALID_ARG;
+    if (bd->end < -1 || (bd->V > 0 && bd->end >= bd->V) || bd->ld < 0 || (bd->ld > 0 && bd->ld < bd->V))
+        return LUNA_ERR_INVALID_ARG;
+    if (bd->K > kMaxBeams || bd->V > (1 << 24) || (int64_t)bd->B * bd->K > 65535) return LUNA_ERR_UNSUPPORTED;
+    return LUNA_OK;
+}
+
+// Parts of a row: enough blocks for eight on every SM, a piece of 8192 values at least for each.
+int parts(const luna_beam_desc *bd) {
+    const int64_t rows = (int64_t)bd->B * bd->K, pieces = cdiv((int64_t)bd->V + 8, kPiece);
+    return (int)std::max<int64_t>(1, std::min(pieces, cdiv((int64_t)8 * tc_sm_count(), std::max<int64_t>(rows, 1))));
+}
+
+size_t workspace(const luna_beam_desc *bd) {
+    const int64_t rows = (int64_t)bd->B * bd->K, S = parts(bd);
+    return (size_t)(256 + align256(rows * S * bd->K * 8) + align256(rows * S * 8));
+}
+
+}  // namespace
+}  // namespace luna
+
+using namespace luna;
+
+extern "C" {
+
+luna_status luna_beam_workspace_size(const luna_beam_desc *bd, size_t *bytes) {
+    if (!bytes) return LUNA_ERR_INVALID_ARG;
+    const luna_status st = check(bd);
+    if (st != LUNA_OK) return st;
+    *bytes = bd->V > 0 ? workspace(bd) : 256;
+    return LUNA_OK;
+}
+
+luna_status luna_beam_select(const luna_beam_desc *bd, const void *logits, const float *scores, const uint8_t *done,
+                             float *scores_out, int32_t *tokens, int32_t *parents, uint8_t *done_out, void *ws,
+                             size_t ws_bytes, void *stream) {
+    const luna_status st = check(bd);
+    if (st != LUNA_OK) return st;
+    if (bd->V < 1 || (bd->end < 0 && (done || done_out))) return LUNA_ERR_INVALID_ARG;
+    if (bd->B == 0) return LUNA_OK;
+    if (!logits || !scores || !scores_out || !tokens || !parents || !ws || reinterpret_cast<uintptr_t>(ws) % 256 != 0)
+        return LUNA_ERR_INVALID_ARG;
+    if (ws_bytes < workspace(bd)) return LUNA_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    BeamArgs a{logits, bd->ld ? bd->ld : bd->V, scores, done, scores_out, tokens, parents, done_out,
+               bd->B, bd->K, bd->V, bd->end, parts(bd)};
+    a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + 256);
+    a.stats = reinterpret_cast<float2 *>(static_cast<char *>(ws) + 256 + align256((int64_t)bd->B * bd->K * a.S * bd->K * 8));
+    const dim3 grid((unsigned)a.S, (unsigned)(bd->B * bd->K));
+    if (bd->io == LUNA_F32)
+        LUNA_LAUNCH("beam_rows", k_beam_rows<float>, grid, kThreads, 0, s, a);
+    else
+        LUNA_LAUNCH("beam_rows", k_beam_rows<__nv_bfloat16>, grid, kThreads, 0, s, a);
+    // at most K threads hold a candidate that reaches the K-th best of the threads' maxima
+    const size_t pool = sizeof(SeqKey) * bd->K * (size_t)cdiv((int64_t)bd->K * a.S * bd->K, kThreads);
+    if (cudaFuncSetAttribute(k_beam_join, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pool) != cudaSuccess)
+        return LUNA_ERR_CUDA;
+    LUNA_LAUNCH("beam_join", k_beam_join, (unsigned)bd->B, kThreads, pool, s, a);
+    return cudaGetLastError() == cudaSuccess ? LUNA_OK : LUNA_ERR_CUDA;
+}
+
+luna_status luna_beam_reorder(const luna_beam_desc *bd, const int32_t *parents, const int32_t *slots, int nslots,
+                              void *pool, size_t slot_bytes, int32_t *new_slots, void *stream) {
+    const luna_status st = check(bd);
+    if (st != LUNA_OK) return st;
+    if (nslots < 0 || slot_bytes > (size_t(1) << 40)) return LUNA_ERR_INVALID_ARG;
+    if (bd->B == 0) return LUNA_OK;
+    if (!parents || !slots || !new_slots || new_slots == slots || (slot_bytes > 0 && nslots > 0 && !pool)) return LUNA_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(pool) | slot_bytes;
+    const int vec = at % 16 == 0 ? 16 : at % 4 == 0 ? 4 : 1;
+    const int64_t blocks = cdiv((int64_t)slot_bytes, (int64_t)vec * kCopyThreads * kCopyVecs);
+    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(blocks, 4096)), (unsigned)bd->B);
+    const int n = slot_bytes > 0 ? nslots : 0;
+    char *p = static_cast<char *>(pool);
+    if (vec == 16)
+        LUNA_LAUNCH("beam_reorder", k_beam_reorder<uint4>, grid, kCopyThreads, 0, s, parents, slots, bd->K, n, p, (int64_t)slot_bytes, new_slots);
+    else if (vec == 4)
+        LUNA_LAUNCH("beam_reorder", k_beam_reorder<uint32_t>, grid, kCopyThreads, 0, s, parents, slots, bd->K, n, p, (int64_t)slot_bytes, new_slots);
+    else
+        LUNA_LAUNCH("beam_reorder", k_beam_reorder<uint8_t>, grid, kCopyThreads, 0, s, parents, slots, bd->K, n, p, (int64_t)slot_bytes, new_slots);
+    return cudaGetLastError() == cudaSuccess ? LUNA_OK : LUNA_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,563 @@
+// The gated delta rule on CUDA cores: the recurrence row by row, its gradients by chunk, single tokens.
+#include <math.h>
+
+#include "luna_delta.cuh"
+#include "luna_prof.cuh"
+
+namespace luna {
+namespace {
+
+// ---------------------------------------------------------------------------
+// The recurrence, forward (S, from which u and o) and in reverse (R, from which x and dV).
+//
+// A column of the state takes part in no other: eight lanes hold one column, 16 rows each at d = 128, and a block
+// of 128 threads 16 columns.  A row is a dot product of the column with k (eight lanes' sums joined by three
+// shuffles), what the token writes, the update and the dot product with q.  Rows come in tiles of 16 through shared
+// memory, the next tile's on their way in registers.  Bound by that chain of some 200 cycles a row, whatever the
+// width.
+
+constexpr int kRowCols = 16, kRowThreads = 128, kTile = 16;
+
+// sums over the eight lanes of a column
+__device__ __forceinline__ float lanes8(float x) {
+    x += __shfl_xor_sync(0xffffffffu, x, 1);
+    x += __shfl_xor_sync(0xffffffffu, x, 2);
+    return x + __shfl_xor_sync(0xffffffffu, x, 4);
+}
+
+// a s + x for a in two terms, rounded once: where the state moves by a little at every row the same way, a rounding
+// of a s alone would be off the same way at every row too (2e-4 of the state after 20000 rows of a = 1 - 1e-6).
+__device__ __forceinline__ float decayed(float a, float rest, float s, float x) { return fmaf(a, s, fmaf(rest, s, x)); }
+
+template <typename IO, int JD, bool REV>
+__global__ void __launch_bounds__(kRowThreads) k_delta_rows(DeltaArgs a) {
+    constexpr int DP = 32 * JD, PER = kTile * DP / kRowThreads;  // padded width; values of k (and q) a thread loads
+    __shared__ float4 sk[kTile][DP / 4], sq[kTile][DP / 4];
+    __shared__ float sx[kTile][kRowCols], sy[kTile][kRowCols], sz[kTile][kRowCols];
+    __shared__ float sa[kTile], sr[kTile], sb[kTile];
+    const int tid = threadIdx.x, p = tid % 8, cl = tid / 8;
+    const int64_t bh = blockIdx.x;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * kRowCols, col = col0 + cl;
+    const int len = head_length(a.lengths, b, a.n), tiles = (len + kTile - 1) / kTile;
+    const int hk = h / (a.H / a.k.heads);
+    const IO *k = static_cast<const IO *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
+    const IO *q = static_cast<const IO *>(a.q.p) + b * a.q.sb + hk * a.q.sh;
+    const RowView &xv = REV ? a.go : a.v;
+    const IO *x = static_cast<const IO *>(xv.p) + b * xv.sb + h * xv.sh;
+    IO *o = a.o ? static_cast<IO *>(a.o) + b * a.ob + h * a.oh : nullptr;
+    float *U = REV ? a.X : a.U;
+    if (U) U += bh * a.n * a.dv;
+    const int64_t E = (int64_t)a.d * a.dv;
+    float *ends = REV ? a.after : a.before;
+    if (ends) ends += bh * (a.m + 1) * E;
+    const float *init = REV ? a.dS1 : a.S0;
+    float *last = REV ? a.dS0 : a.S1;
+
+    float s[JD][4], fade = 1.0f, fade2 = 0.0f;  // (reverse) the decay of the row before is still to be applied
+    auto row = [&](int j, int e) { return j * 32 + p * 4 + e; };
+    auto keep = [&](float *to) {
+        if (col < a.dv)
+#pragma unroll
+            for (int j = 0; j < JD; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (row(j, e) < a.d) to[(int64_t)row(j, e) * a.dv + col] = decayed(fade, fade2, s[j][e], 0.0f);
+    };
+#pragma unroll
+    for (int j = 0; j < JD; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            s[j][e] = init && col < a.dv && row(j, e) < a.d ? init[bh * E + (int64_t)row(j, e) * a.dv + col] : 0.0f;
+    if (REV && ends) keep(ends + (int64_t)((len + kDeltaRows - 1) / kDeltaRows) * E);
+
+    float nk[PER], nq[PER], nx[2], ng = 0.0f, nb = 0.0f;
+    auto fetch = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = tid + i * kRowThreads, t = tile * kTile + at / DP, c = at % DP;
+            const bool in = t < len && c < a.d;
+            nk[i] = in ? io_load(k + t * a.k.st + c) : 0.0f;
+            nq[i] = in ? io_load(q + t * a.q.st + c) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = tid + i * kRowThreads, t = tile * kTile + at / kRowCols, c = col0 + at % kRowCols;
+            nx[i] = t < len && c < a.dv ? io_load(x + t * xv.st + c) : 0.0f;
+        }
+        if (tid < kTile && tile * kTile + tid < len) {
+            ng = gate_at<IO>(a.g, b, h, tile * kTile + tid);
+            nb = gate_at<IO>(a.b, b, h, tile * kTile + tid);
+        }
+    };
+    if (tiles > 0) fetch(REV ? tiles - 1 : 0);
+    for (int step = 0; step < tiles; ++step) {
+        const int tile = REV ? tiles - 1 - step : step, rows = min(kTile, len - tile * kTile);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int at = tid + i * kRowThreads;
+            reinterpret_cast<float *>(sk)[at] = nk[i];
+            reinterpret_cast<float *>(sq)[at] = nq[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) (&sx[0][0])[tid + i * kRowThreads] = nx[i];
+        if (tid < kTile) {
+            gate_terms(ng, sa[tid], sr[tid]);
+            sb[tid] = nb;
+        }
+        __syncthreads();
+        if (step + 1 < tiles) fetch(REV ? tile - 1 : tile + 1);
+        if (!REV && ends && tile % (kDeltaRows / kTile) == 0) keep(ends + (int64_t)(tile / (kDeltaRows / kTile)) * E);
+        for (int r = 0; r < rows; ++r) {
+            const int t = REV ? rows - 1 - r : r;
+            const float lam = sa[t], rest = sr[t], beta = sb[t], xc = sx[t][cl];
+            float4 kk[JD], qq[JD];
+#pragma unroll
+            for (int j = 0; j < JD; ++j) { kk[j] = sk[t][j * 8 + p]; qq[j] = sq[t][j * 8 + p]; }
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            if (!REV) {
+#pragma unroll
+                for (int j = 0; j < JD; ++j) {
+                    acc[0] = fmaf(kk[j].x, s[j][0], acc[0]); acc[1] = fmaf(kk[j].y, s[j][1], acc[1]);
+                    acc[2] = fmaf(kk[j].z, s[j][2], acc[2]); acc[3] = fmaf(kk[j].w, s[j][3], acc[3]);
+                }
+                const float dot = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3]));
+                const float u = beta * (xc - fmaf(lam, dot, rest * dot));
+                acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < JD; ++j) {
+                    s[j][0] = decayed(lam, rest, s[j][0], kk[j].x * u); s[j][1] = decayed(lam, rest, s[j][1], kk[j].y * u);
+                    s[j][2] = decayed(lam, rest, s[j][2], kk[j].z * u); s[j][3] = decayed(lam, rest, s[j][3], kk[j].w * u);
+                    acc[0] = fmaf(qq[j].x, s[j][0], acc[0]); acc[1] = fmaf(qq[j].y, s[j][1], acc[1]);
+                    acc[2] = fmaf(qq[j].z, s[j][2], acc[2]); acc[3] = fmaf(qq[j].w, s[j][3], acc[3]);
+                }
+                const float y = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3]));
+                if (p == 0) { sy[t][cl] = a.scale * y; sz[t][cl] = u; }
+            } else {
+                const float g = a.scale * xc;
+#pragma unroll
+                for (int j = 0; j < JD; ++j) {
+                    s[j][0] = decayed(fade, fade2, s[j][0], qq[j].x * g); s[j][1] = decayed(fade, fade2, s[j][1], qq[j].y * g);
+                    s[j][2] = decayed(fade, fade2, s[j][2], qq[j].z * g); s[j][3] = decayed(fade, fade2, s[j][3], qq[j].w * g);
+                    acc[0] = fmaf(kk[j].x, s[j][0], acc[0]); acc[1] = fmaf(kk[j].y, s[j][1], acc[1]);
+                    acc[2] = fmaf(kk[j].z, s[j][2], acc[2]); acc[3] = fmaf(kk[j].w, s[j][3], acc[3]);
+                }
+                const float du = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3])), w = -beta * du;
+#pragma unroll
+                for (int j = 0; j < JD; ++j) {
+                    s[j][0] = fmaf(kk[j].x, w, s[j][0]); s[j][1] = fmaf(kk[j].y, w, s[j][1]);
+                    s[j][2] = fmaf(kk[j].z, w, s[j][2]); s[j][3] = fmaf(kk[j].w, w, s[j][3]);
+                }
+                fade = lam;
+                fade2 = rest;
+                if (p == 0) { sy[t][cl] = -w; sz[t][cl] = du; }
+            }
+        }
+        if (REV && ends && tile % (kDeltaRows / kTile) == 0) keep(ends + (int64_t)(tile / (kDeltaRows / kTile)) * E);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = tid + i * kRowThreads, t = at / kRowCols, c = at % kRowCols;
+            if (t < rows && col0 + c < a.dv) {
+                const int64_t r = tile * kTile + t;
+                if (o) io_store(o + r * a.ot + col0 + c, sy[t][c]);
+                if (U) U[r * a.dv + col0 + c] = sz[t][c];
+            }
+        }
+    }
+    if (!REV && ends) keep(ends + (int64_t)((len + kDeltaRows - 1) / kDeltaRows) * E);
+    if (last) keep(last + bh * E);
+    if (o)
+        for (int64_t i = tid; i < (int64_t)(a.n - len) * kRowCols; i += kRowThreads) {
+            const int c = col0 + (int)(i % kRowCols);
+            if (c < a.dv) io_store(o + (len + i / kRowCols) * a.ot + c, 0.0f);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of q, k and the gates from the states at the two ends of a chunk: seven products of 64 rows, each
+// thread with 4 rows and every 16th column of them.  The operands come from L2 in steps of 16 of the summed index;
+// bound by the shared-memory loads of the products (12 values for 32 multiply-adds).
+
+constexpr int kGradThreads = 256, kGradK = 16;
+
+struct GradShared {
+    float A[kDeltaRows][kGradK + 1], B[kGradK][kMaxD + 1];
+    float P[kDeltaRows][kDeltaRows + 1], W[kDeltaRows][kDeltaRows + 1];
+    float hi[kDeltaRows], lo[kDeltaRows], b[kDeltaRows], past[kDeltaRows], left[kDeltaRows];
+    float read[kDeltaRows], wrote[kDeltaRows], wstate[kDeltaRows], total[kGradThreads / 32];
+};
+
+// acc[r][c] += sum_k A(ty * 4 + r, k) B(k, tx + 16 c); BT: B is stored with k contiguous
+template <bool BT, int NC, typename FA, typename FB>
+__device__ __forceinline__ void grad_product(GradShared &sm, float (&acc)[4][NC], int K, FA fa, FB fb) {
+    const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+    for (int k0 = 0; k0 < K; k0 += kGradK) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = k0 + tid % kGradK, r = tid / kGradK + 16 * i;
+            sm.A[r][k - k0] = k < K ? fa(r, k) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int at = tid + i * kGradThreads;
+            const int k = BT ? k0 + at % kGradK : k0 + at / (16 * NC), c = BT ? at / kGradK : at % (16 * NC);
+            sm.B[k - k0][c] = k < K ? fb(k, c) : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kGradK; ++k) {
+            float x[4], y[NC];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = sm.A[ty * 4 + r][k];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) y[c] = sm.B[k][tx + 16 * c];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int c = 0; c < NC; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+        }
+    }
+}
+
+template <typename IO, typename OUT>
+__global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
+    extern __shared__ char raw[];
+    GradShared &sm = *reinterpret_cast<GradShared *>(raw);
+    constexpr int NC = kMaxD / 16, C = kDeltaRows;
+    const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+    const int64_t bh = blockIdx.x / a.m;
+    const int chunk = (int)(blockIdx.x % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
+    const int len = head_length(a.lengths, b, a.n), rows = max(0, min(C, len - t0));
+    const int hk = h / (a.H / a.k.heads);
+    const IO *q = static_cast<const IO *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st;
+    const IO *k = static_cast<const IO *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st;
+    const IO *v = static_cast<const IO *>(a.v.p) + b * a.v.sb + h * a.v.sh + t0 * a.v.st;
+    const IO *go = static_cast<const IO *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st;
+    OUT *dq = static_cast<OUT *>(a.dq) + b * a.dqb + h * a.dqh + t0 * a.dqt;
+    OUT *dk = static_cast<OUT *>(a.dk) + b * a.dkb + h * a.dkh + t0 * a.dkt;
+    IO *dg = static_cast<IO *>(a.dg.p) + b * a.dg.sb + h * a.dg.sh + t0 * a.dg.st;
+    IO *db = static_cast<IO *>(a.db.p) + b * a.db.sb + h * a.db.sh + t0 * a.db.st;
+    const int out_rows = min(C, a.n - t0);
+    for (int i = tid; i < (out_rows - rows) * a.d; i += kGradThreads) {
+        const int t = rows + i / a.d, c = i % a.d;
+        io_store(dq + t * a.dqt + c, 0.0f);
+        io_store(dk + t * a.dkt + c, 0.0f);
+    }
+    if (tid >= rows && tid < out_rows) {
+        io_store(dg + tid * a.dg.st, 0.0f);
+        io_store(db + tid * a.db.st, 0.0f);
+    }
+    if (rows == 0) return;
+    const int64_t E = (int64_t)a.d * a.dv;
+    const float *S = a.before + (bh * (a.m + 1) + chunk) * E, *R = a.after + (bh * (a.m + 1) + chunk + 1) * E;
+    const float *U = a.U + (bh * a.n + t0) * a.dv, *X = a.X + (bh * a.n + t0) * a.dv;
+    const int d = a.d, dv = a.dv;
+
+    if (tid < 32)
+        delta_gate_sums(tid, [&](int t) { return t < rows ? gate_at<IO>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
+                        sm.past, sm.left);
+    else if (tid < 32 + C)
+        sm.b[tid - 32] = tid - 32 < rows ? gate_at<IO>(a.b, b, h, t0 + tid - 32) : 0.0f;
+    __syncthreads();
+    const float whole = sm.past[C - 1];
+    auto gap = [&](int i, int j) { return expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])); };
+    auto at = [&](const IO *x, int64_t st, int t, int c, int w) { return t < rows && c < w ? io_load(x + t * st + c) : 0.0f; };
+    auto in = [&](const float *x, int t, int c) { return t < rows && c < dv ? x[(int64_t)t * dv + c] : 0.0f; };
+    auto fK = [&](int kk, int c) { return at(k, a.k.st, kk, c, d); };
+    auto fQ = [&](int kk, int c) { return at(q, a.q.st, kk, c, d); };
+    auto zero = [](auto &acc) {
+#pragma unroll
+        for (auto &r : acc)
+#pragma unroll
+            for (auto &x : r) x = 0.0f;
+    };
+    // sums over the 16 threads of a row
+    auto rowsum = [&](float x) {
+#pragma unroll
+        for (int w = 1; w < 16; w *= 2) x += __shfl_xor_sync(0xffffffffu, x, w);
+        return x;
+    };
+
+    {  // P and W
+        float acc[4][4];
+        zero(acc);
+        grad_product<true>(sm, acc, dv, [&](int r, int kk) { return at(go, a.go.st, r, kk, dv); }, [&](int kk, int c) { return in(U, c, kk); });
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = ty * 4 + r, j = tx + 16 * c;
+                sm.P[i][j] = j <= i ? a.scale * gap(i, j) * acc[r][c] : 0.0f;
+            }
+        zero(acc);
+        grad_product<true>(sm, acc, dv, [&](int r, int kk) { return in(X, r, kk); }, [&](int kk, int c) { return in(U, c, kk); });
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = ty * 4 + r, j = tx + 16 * c;
+                sm.W[i][j] = j < i ? gap(i, j) * acc[r][c] : 0.0f;
+            }
+    }
+    float acc[4][NC], z[4][NC];
+    auto fS = [&](int kk, int c) { return c < d && kk < dv ? S[(int64_t)c * dv + kk] : 0.0f; };
+    auto fR = [&](int kk, int c) { return c < d && kk < dv ? R[(int64_t)c * dv + kk] : 0.0f; };
+    // dQ
+    zero(acc);
+    grad_product<true>(sm, acc, dv, [&](int r, int kk) { return at(go, a.go.st, r, kk, dv); }, fS);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[r][c] *= a.scale * sm.past[ty * 4 + r];
+    grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[r][kk]; }, fK);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = ty * 4 + r;
+        float dot = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int cc = tx + 16 * c;
+            if (i < rows && cc < d) {
+                dot = fmaf(io_load(q + i * a.q.st + cc), acc[r][c], dot);
+                io_store(dq + i * a.dqt + cc, acc[r][c]);
+            }
+        }
+        dot = rowsum(dot);
+        if (tx == 0) sm.read[i] = dot;
+    }
+    // Z, and with it db
+    zero(z);
+    grad_product<true>(sm, z, dv, [&](int r, int kk) { return in(X, r, kk); }, fS);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) z[r][c] *= sm.past[ty * 4 + r];
+    grad_product<false>(sm, z, C, [&](int r, int kk) { return sm.W[r][kk]; }, fK);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = ty * 4 + r;
+        float dot = 0.0f, xv = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int cc = tx + 16 * c;
+            if (i < rows && cc < d) dot = fmaf(io_load(k + i * a.k.st + cc), z[r][c], dot);
+            if (i < rows && cc < dv) xv = fmaf(io_load(v + i * a.v.st + cc), X[(int64_t)i * dv + cc], xv);
+        }
+        dot = rowsum(dot);
+        xv = rowsum(xv);
+        if (tx == 0 && i < rows) {
+            io_store(db + i * a.db.st, xv - dot);
+            sm.read[i] -= sm.b[i] * dot;
+        }
+    }
+    // dK
+    zero(acc);
+    grad_product<true>(sm, acc, dv, [&](int r, int kk) { return in(U, r, kk); }, fR);
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = ty * 4 + r;
+            float dot = 0.0f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                if (pass == 0) acc[r][c] *= sm.left[i];
+                if (i < rows && tx + 16 * c < d) dot = fmaf(io_load(k + i * a.k.st + tx + 16 * c), acc[r][c], dot);
+            }
+            dot = rowsum(dot);
+            if (tx == 0) (pass == 0 ? sm.wstate : sm.wrote)[i] = dot;
+        }
+        if (pass == 0) {
+            grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[kk][r]; }, fQ);
+            grad_product<false>(sm, acc, C, [&](int r, int kk) { return -sm.b[kk] * sm.W[kk][r]; }, fK);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = ty * 4 + r;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (i < rows && tx + 16 * c < d) io_store(dk + i * a.dkt + tx + 16 * c, fmaf(-sm.b[i], z[r][c], acc[r][c]));
+    }
+    // dg: what passes row t of <S, R> and of the pairs of rows
+    float pass = 0.0f;
+    for (int64_t i = tid; i < E; i += kGradThreads) pass = fmaf(S[i], R[i], pass);
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) pass += __shfl_xor_sync(0xffffffffu, pass, w);
+    if (tid % 32 == 0) sm.total[tid / 32] = pass;
+    __syncthreads();
+    if (tid < 32) {
+        float all = 0.0f;
+        for (int w = 0; w < kGradThreads / 32; ++w) all += sm.total[w];
+        delta_gate_grads(all * whole, sm.read, sm.wrote, sm.wstate, rows, tid, [&](int t, float x) {
+            io_store(dg + t * a.dg.st, expf(gate_at<IO>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
+        });
+    }
+}
+
+// ---------------------------------------------------------------------------
+// One token.  A block owns 32 columns of one head's state, a float4 of columns and every 32nd row a thread, all of
+// them in registers before the first is used; the sums with k over the rows are joined through shared memory, then
+// what the token writes goes in and the sums with q are joined the same way.  The state is read and written once,
+// which bounds the step.
+
+constexpr int kStepThreads = 256, kStepCols = 32;
+
+template <typename IO, bool VEC>
+__global__ void __launch_bounds__(kStepThreads) k_delta_step(DeltaStep a) {
+    __shared__ float sq[kMaxD], sk[kMaxD], sgate[3];
+    __shared__ float so[2][kStepThreads / 32][kStepCols];
+    const int tid = threadIdx.x;
+    const int64_t bh = blockIdx.x;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), hk = h / (a.H / a.Hk);
+    const int col0 = blockIdx.y * kStepCols;
+    const int slot = a.slots ? a.slots[b] : b;
+    IO *o = static_cast<IO *>(a.o) + b * a.ob + h * a.oh;
+    if (slot < 0 || slot >= a.nslots) {
+        if (tid < kStepCols && col0 + tid < a.dv) io_store(o + col0 + tid, 0.0f);
+        return;
+    }
+    const IO *q = static_cast<const IO *>(a.q) + b * a.qb + hk * a.qh;
+    const IO *k = static_cast<const IO *>(a.k) + b * a.kb + hk * a.kh;
+    const IO *v = static_cast<const IO *>(a.v) + b * a.vb + h * a.vh;
+    float *S = a.S + ((int64_t)slot * a.H + h) * a.d * a.dv;
+    const int cg = tid % 8, rg = tid / 8, c = col0 + 4 * cg;  // column group of four, row
+    constexpr int R = kMaxD / (kStepThreads / 8);
+    float s[R][4];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int f = rg + i * (kStepThreads / 8);
+        const float *p = S + (int64_t)f * a.dv + c;
+        if (VEC) {
+            const float4 w = f < a.d && c < a.dv ? *reinterpret_cast<const float4 *>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+            s[i][0] = w.x; s[i][1] = w.y; s[i][2] = w.z; s[i][3] = w.w;
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[i][t] = f < a.d && c + t < a.dv ? p[t] : 0.0f;
+        }
+    }
+    for (int i = tid; i < kMaxD; i += kStepThreads) {
+        sq[i] = i < a.d ? io_load(q + i) : 0.0f;
+        sk[i] = i < a.d ? io_load(k + i) : 0.0f;
+    }
+    float vc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) vc[t] = c + t < a.dv ? io_load(v + c + t) : 0.0f;
+    if (tid == kStepThreads - 1) {
+        gate_terms(gate_at<IO>(a.g, b, h, 0), sgate[0], sgate[1]);
+        sgate[2] = gate_at<IO>(a.b, b, h, 0);
+    }
+    __syncthreads();
+    const float lam = sgate[0], rest = sgate[1], beta = sgate[2];
+    // the four rows of a warp, then the warps in order
+    auto join = [&](float (&acc)[4], float (*to)[kStepCols]) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            acc[t] += __shfl_xor_sync(0xffffffffu, acc[t], 8);
+            acc[t] += __shfl_xor_sync(0xffffffffu, acc[t], 16);
+        }
+        if ((tid & 31) < 8) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) to[tid / 32][4 * cg + t] = acc[t];
+        }
+        __syncthreads();
+    };
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const float kf = sk[rg + i * (kStepThreads / 8)];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = fmaf(kf, s[i][t], acc[t]);
+    }
+    join(acc, so[0]);
+    float u[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        float y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kStepThreads / 32; ++w) y += so[0][w][4 * cg + t];
+        u[t] = beta * (vc[t] - fmaf(lam, y, rest * y));
+        acc[t] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int f = rg + i * (kStepThreads / 8);
+        const float kf = sk[f], qf = sq[f];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[i][t] = decayed(lam, rest, s[i][t], kf * u[t]);
+            acc[t] = fmaf(qf, s[i][t], acc[t]);
+        }
+        float *p = S + (int64_t)f * a.dv + c;
+        if (f < a.d) {
+            if (VEC) {
+                if (c < a.dv) *reinterpret_cast<float4 *>(p) = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (c + t < a.dv) p[t] = s[i][t];
+            }
+        }
+    }
+    join(acc, so[1]);
+    if (tid < kStepCols && col0 + tid < a.dv) {
+        float y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kStepThreads / 32; ++w) y += so[1][w][tid];
+        io_store(o + col0 + tid, a.scale * y);
+    }
+}
+
+unsigned cdiv(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
+
+template <typename IO, bool REV>
+cudaError_t rows(const DeltaArgs &a, cudaStream_t s) {
+    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, kRowCols));
+    if (a.d <= 32)
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 1, REV>), grid, kRowThreads, 0, s, a);
+    else if (a.d <= 64)
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 2, REV>), grid, kRowThreads, 0, s, a);
+    else
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 4, REV>), grid, kRowThreads, 0, s, a);
+    return cudaGetLastError();
+}
+
+template <typename IO, typename OUT>
+cudaError_t grad(const DeltaArgs &a, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(k_delta_grad<IO, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GradShared));
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("delta_grad", (k_delta_grad<IO, OUT>), (unsigned)((int64_t)a.B * a.H * a.m), kGradThreads, sizeof(GradShared), s, a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s) {
+    if (io == LUNA_F32) return reverse ? rows<float, true>(a, s) : rows<float, false>(a, s);
+    return reverse ? rows<__nv_bfloat16, true>(a, s) : rows<__nv_bfloat16, false>(a, s);
+}
+
+cudaError_t launch_delta_grad(const DeltaArgs &a, luna_dtype io, luna_dtype out, cudaStream_t s) {
+    if (io == LUNA_F32) return grad<float, float>(a, s);
+    return out == LUNA_F32 ? grad<__nv_bfloat16, float>(a, s) : grad<__nv_bfloat16, __nv_bfloat16>(a, s);
+}
+
+cudaError_t launch_delta_step(const DeltaStep &a, luna_dtype io, cudaStream_t s) {
+    // 16-byte accesses need rows of whole float4s and an aligned state
+    const bool vec = a.dv % 4 == 0 && (reinterpret_cast<uintptr_t>(a.S) & 15) == 0;
+    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, kStepCols));
+    if (io == LUNA_F32) {
+        if (vec)
+            LUNA_LAUNCH("delta_step", (k_delta_step<float, true>), grid, kStepThreads, 0, s, a);
+        else
+            LUNA_LAUNCH("delta_step", (k_delta_step<float, false>), grid, kStepThreads, 0, s, a);
+    } else {
+        if (vec)
+            LUNA_LAUNCH("delta_step", (k_delta_step<__nv_bfloat16, true>), grid, kStepThreads, 0, s, a);
+        else
+            LUNA_LAUNCH("delta_step", (k_delta_step<__nv_bfloat16, false>), grid, kStepThreads, 0, s, a);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace luna

@@ -1,0 +1,151 @@
+// The gated delta rule: argument blocks and launchers.
+//
+//     S_t = a_t (S_{t-1} - b_t k_t (k_t^T S_{t-1})) + b_t k_t v_t^T,   o_t = scale S_t^T q_t,   a_t = exp(g_t)
+//
+// With u_t = b_t (v_t - a_t S_{t-1}^T k_t), what a token writes, S_t = a_t S_{t-1} + k_t u_t^T.  The gradients
+// carry R, that of the state after a token (R_n = dS1), back through the rows:
+//
+//     R_t += scale q_t dO_t^T;   x_t = R_t^T k_t;   dV_t = b_t x_t;   R_{t-1} = a_t (R_t - b_t k_t x_t^T)
+//     dQ_t = scale S_t dO_t;   Z_t = a_t S_{t-1} x_t;   dK_t = R_t u_t - b_t Z_t
+//     db_t = x_t . v_t - k_t . Z_t;   dg_t = <a_t S_{t-1}, R_t - b_t k_t x_t^T>
+//
+// The columns of S and R (dv of them) never meet, so that S, u and R, x walk the rows in blocks of a few columns;
+// what needs whole rows of S and R is then a product over a chunk of 64 rows from the states at its two ends.
+// With G_i the sum of a chunk's g to row i, c(i, j) = exp(G_i - G_j), S the state before and R the gradient after
+// the chunk, and P_ij = scale c(i, j) dO_i . u_j (j <= i), W_ij = b_i c(i, j) x_i . u_j (j < i):
+//
+//     dQ_i = scale c(i, 0) S dO_i + sum_j P_ij k_j
+//     dK_j = c(C, j) R u_j + sum_i P_ij q_i - sum_i W_ij k_i  -  b_j c(j, 0) S x_j - sum_{l < j} W_jl k_l
+//
+// and dg is a sum over all pairs of a row at or behind t that reads and a row before t (or S) that was written:
+// each of the parts q_i . dQ_i, k_j . dK_j adds to the rows up to i, or takes from those up to j.
+#pragma once
+
+#include "luna_decay.cuh"
+
+namespace luna {
+
+constexpr int kDeltaRows = 64;  // rows of a chunk
+
+struct GateView {  // a (B, H, n) tensor
+    const void *p;
+    int64_t sb, sh, st;
+};
+struct GateOut {
+    void *p;
+    int64_t sb, sh, st;
+};
+
+struct DeltaArgs {
+    RowView q, k, v, go;    // go: dO (backward)
+    GateView g, b;
+    void *o;                // O; (backward) dV
+    int64_t ob, oh, ot;
+    void *dq, *dk;          // gradients, of type io with strides, or (shared heads) fp32 [B][H][n][d]
+    int64_t dqb, dqh, dqt, dkb, dkh, dkt;
+    GateOut dg, db;
+    const int32_t *lengths;
+    const float *S0, *dS1;  // NULL: zero
+    float *S1, *dS0;        // NULL: not wanted
+    int B, H, n, d, dv, m;  // m: chunks of a head
+    float scale;
+    // intermediate results
+    float *U, *X;           // rows written and their gradients, [B H][n][dv] (CUDA-core form)
+    float *before, *after;  // states before chunk i, gradients of the states before chunk i, [B H][m + 1][d][dv]
+    __nv_bfloat16 *Tp, *Pp; // tensor-core form: planes of the chunks' inverses and scores, [B H][m][2][64][64]
+    float *rows;            // tensor-core form: c(i, 0), c(C, i), b_i of every row, [B H][m][3][64]
+    __nv_bfloat16 *Up, *Xp; // tensor-core form: planes of U and X, [B H][m][2][64][dv padded]
+    __nv_bfloat16 *Sp, *Rp; // tensor-core form: the states at the chunks' ends, [B H][m][d padded][dv padded]
+};
+
+struct DeltaStep {
+    const void *q, *k, *v;
+    void *o;
+    int64_t qb, qh, kb, kh, vb, vh, ob, oh;
+    GateView g, b;
+    const int32_t *slots;
+    float *S;
+    int nslots, B, H, Hk, d, dv;
+    float scale;
+};
+
+template <typename T>
+__device__ __forceinline__ float gate_at(const GateView &v, int b, int h, int t) {
+    return io_load(static_cast<const T *>(v.p) + b * v.sb + h * v.sh + t * v.st);
+}
+
+// exp(g) in two terms: one rounded to fp32 is off the same way at every token of a head whose gate stands still.
+__device__ __forceinline__ void gate_terms(float g, float &a, float &rest) {
+    if (fabsf(g) < 0.5f) {  // (beyond that a state forgets, or overflows, in some ten tokens)
+        const float m1 = expm1f(g);
+        a = 1.0f + m1;
+        rest = m1 - (a - 1.0f);
+    } else {
+        a = expf(g);
+        rest = 0.0f;
+    }
+}
+
+// Gates below this forget everything (exp is 0 in fp32); sums of a chunk's gates stay finite.
+constexpr float kGateLeast = -120.0f;
+
+// A chunk's gates, by one warp: their sums to each row in 64 bits, kept as two fp32 terms so that differences of near
+// rows stay exact, and the factors from the chunk's start (past) and to its end (left).  gate(t) is 0 behind the end.
+template <typename F>
+__device__ __forceinline__ void delta_gate_sums(int lane, F gate, float *hi, float *lo, float *past, float *left) {
+    const double g0 = (double)fmaxf(gate(2 * lane), kGateLeast), g1 = (double)fmaxf(gate(2 * lane + 1), kGateLeast);
+    double sum = g0 + g1;
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) {
+        const double up = __shfl_up_sync(0xffffffffu, sum, w);
+        if (lane >= w) sum += up;
+    }
+    const double total = __shfl_sync(0xffffffffu, sum, 31);
+    auto factor = [](double x, float &h, float &l) {
+        h = (float)x;
+        l = (float)(x - (double)h);
+        const float e = expf(h);
+        return fmaf(e, l, e);
+    };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const double G = i ? sum : sum - g1;
+        float h, l, rh, rl;
+        past[2 * lane + i] = factor(G, h, l);
+        left[2 * lane + i] = factor(total - G, rh, rl);
+        hi[2 * lane + i] = h;
+        lo[2 * lane + i] = l;
+    }
+}
+
+// dg of a chunk's rows, by one warp: `base` is what the states at the chunk's ends give across all of it, read_i
+// what row i's reads of S and of the rows before it give to the gates up to i, wrote_j what the reads of row j give
+// (they do not cross the gates up to j), wstate_j the part of wrote_j that is read behind the chunk.
+template <typename F>
+__device__ __forceinline__ void delta_gate_grads(float base, const float *read, const float *wrote, const float *wstate,
+                                                 int rows, int lane, F store) {
+    float x[2], tail = 0.0f, state = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = 2 * lane + i;
+        x[i] = t < rows ? read[t] - wrote[t] : 0.0f;
+        state += t < rows ? wstate[t] : 0.0f;
+        tail += x[i];
+    }
+#pragma unroll
+    for (int w = 1; w < 32; w *= 2) {
+        state += __shfl_xor_sync(0xffffffffu, state, w);
+        const float up = __shfl_down_sync(0xffffffffu, tail, w);
+        if (lane + w < 32) tail += up;
+    }
+    tail = __shfl_down_sync(0xffffffffu, tail, 1);  // the rows behind this lane's
+    base += state + (lane < 31 ? tail : 0.0f);
+    if (2 * lane + 1 < rows) store(2 * lane + 1, base + x[1]);
+    if (2 * lane < rows) store(2 * lane, base + x[1] + x[0]);
+}
+
+cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s);
+cudaError_t launch_delta_grad(const DeltaArgs &a, luna_dtype io, luna_dtype out, cudaStream_t s);
+cudaError_t launch_delta_step(const DeltaStep &a, luna_dtype io, cudaStream_t s);
+
+}  // namespace luna

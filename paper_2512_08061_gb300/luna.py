@@ -67,6 +67,17 @@ class DecayDesc(ctypes.Structure):
                 *[(k, Strides) for k in ("q", "k", "v", "o", "gq", "gk", "gv", "go")]]
 
 
+class DeltaDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("Hk", ctypes.c_int), ("n", ctypes.c_int),
+                ("d", ctypes.c_int), ("dv", ctypes.c_int), ("scale", ctypes.c_float), ("io", ctypes.c_int),
+                *[(k, Strides) for k in ("q", "k", "v", "o", "g", "beta", "gq", "gk", "gv", "go", "gg", "gbeta")]]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("K", ctypes.c_int), ("V", ctypes.c_int), ("io", ctypes.c_int),
+                ("ld", ctypes.c_int64), ("end", ctypes.c_int)]
+
+
 class NormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int), ("groups", ctypes.c_int), ("kind", ctypes.c_int),
                 ("gate", ctypes.c_int), ("alpha", ctypes.c_float), ("eps", ctypes.c_float), ("io", ctypes.c_int),
@@ -98,6 +109,7 @@ def _load():
     P, S, I, I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
     pd, ad = ctypes.POINTER(PhiDesc), ctypes.POINTER(AttnDesc)
     dd, nd, ld = ctypes.POINTER(DecayDesc), ctypes.POINTER(NormDesc), ctypes.POINTER(LinearDesc)
+    td, bd = ctypes.POINTER(DeltaDesc), ctypes.POINTER(BeamDesc)
     sig = {
         "luna_status_string": ([I], ctypes.c_char_p),
         "luna_version": ([], I),
@@ -123,6 +135,13 @@ def _load():
         "luna_decay_fwd": ([dd, P, P, P, P, P, P, P, P, P, S, P], I),
         "luna_decay_bwd": ([dd, P, P, P, P, P, P, P, P, P, P, P, P, P, S, P], I),
         "luna_decay_step": ([dd, P, P, P, P, P, I, P, P, P], I),
+        "luna_delta_workspace_size": ([td, I, ctypes.POINTER(S)], I),
+        "luna_delta_fwd": ([td] + [P] * 10 + [S, P], I),
+        "luna_delta_bwd": ([td] + [P] * 16 + [S, P], I),
+        "luna_delta_step": ([td, P, P, P, P, P, P, I, P, P, P], I),
+        "luna_beam_workspace_size": ([bd, ctypes.POINTER(S)], I),
+        "luna_beam_select": ([bd] + [P] * 8 + [S, P], I),
+        "luna_beam_reorder": ([bd, P, P, I, P, S, P, P], I),
         "luna_norm_workspace_size": ([nd, ctypes.POINTER(S)], I),
         "luna_norm_fwd": ([nd] + [P] * 10, I),
         "luna_norm_bwd": ([nd] + [P] * 16 + [S, P], I),
@@ -144,6 +163,8 @@ EXPORTED = ("luna_status_string", "luna_version", "luna_phi_table_size", "luna_p
             "luna_state_final", "luna_attn_decode", "luna_selftest_wait", "luna_noalloc_scratch",
             "luna_attn_weights",
             "luna_decay_workspace_size", "luna_decay_fwd", "luna_decay_bwd", "luna_decay_step",
+            "luna_delta_workspace_size", "luna_delta_fwd", "luna_delta_bwd", "luna_delta_step",
+            "luna_beam_workspace_size", "luna_beam_select", "luna_beam_reorder",
             "luna_norm_workspace_size", "luna_norm_fwd", "luna_norm_bwd",
             "luna_linear_workspace_size", "luna_linear_fwd", "luna_linear_bwd")
 
@@ -300,6 +321,64 @@ def luna_decay_bwd(dd, log_decay, Q, K, V, dO, lengths, S0, dS1, dQ, dK, dV, dS0
 def luna_decay_step(dd, log_decay, q, k, v, slots, nslots: int, S, o, stream=None) -> None:
     _check(_lib.luna_decay_step(ctypes.byref(dd), _ptr(log_decay), _ptr(q), _ptr(k), _ptr(v), _ptr(slots), nslots,
                                 _ptr(S), _ptr(o), _stream(stream)), "luna_decay_step")
+
+
+# ---------------------------------------------------------------------------
+# the gated delta rule
+
+def delta_desc(B, H, n, d, dv, Hk=None, scale=None, io=LUNA_BF16) -> DeltaDesc:
+    """Contiguous tensors; set the strides q, k, v, o, g, beta (gq, gk, gv, go, gg, gbeta) for views."""
+    return DeltaDesc(B, H, H if Hk is None else Hk, n, d, dv, max(d, 1) ** -0.5 if scale is None else scale, io)
+
+
+def luna_delta_workspace_size(dd: DeltaDesc, backward: bool) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.luna_delta_workspace_size(ctypes.byref(dd), int(bool(backward)), ctypes.byref(out)),
+           "luna_delta_workspace_size")
+    return out.value
+
+
+def luna_delta_fwd(dd, log_decay, beta, Q, K, V, lengths, S0, O, S1, workspace, stream=None) -> None:
+    _check(_lib.luna_delta_fwd(ctypes.byref(dd), _ptr(log_decay), _ptr(beta), _ptr(Q), _ptr(K), _ptr(V), _ptr(lengths),
+                               _ptr(S0), _ptr(O), _ptr(S1), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream(stream)), "luna_delta_fwd")
+
+
+def luna_delta_bwd(dd, log_decay, beta, Q, K, V, dO, lengths, S0, dS1, dQ, dK, dV, dlog_decay, dbeta, dS0, workspace,
+                   stream=None) -> None:
+    _check(_lib.luna_delta_bwd(ctypes.byref(dd), _ptr(log_decay), _ptr(beta), _ptr(Q), _ptr(K), _ptr(V), _ptr(dO),
+                               _ptr(lengths), _ptr(S0), _ptr(dS1), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(dlog_decay),
+                               _ptr(dbeta), _ptr(dS0), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                               _stream(stream)), "luna_delta_bwd")
+
+
+def luna_delta_step(dd, log_decay, beta, q, k, v, slots, nslots: int, S, o, stream=None) -> None:
+    _check(_lib.luna_delta_step(ctypes.byref(dd), _ptr(log_decay), _ptr(beta), _ptr(q), _ptr(k), _ptr(v), _ptr(slots),
+                                nslots, _ptr(S), _ptr(o), _stream(stream)), "luna_delta_step")
+
+
+# ---------------------------------------------------------------------------
+# beam search over recurrent states
+
+def beam_desc(B, K, V=0, end=-1, io=LUNA_BF16) -> BeamDesc:
+    return BeamDesc(B, K, V, io, 0, end)
+
+
+def luna_beam_workspace_size(bd: BeamDesc) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.luna_beam_workspace_size(ctypes.byref(bd), ctypes.byref(out)), "luna_beam_workspace_size")
+    return out.value
+
+
+def luna_beam_select(bd, logits, scores, done, scores_out, tokens, parents, done_out, workspace, stream=None) -> None:
+    _check(_lib.luna_beam_select(ctypes.byref(bd), _ptr(logits), _ptr(scores), _ptr(done), _ptr(scores_out),
+                                 _ptr(tokens), _ptr(parents), _ptr(done_out), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream(stream)), "luna_beam_select")
+
+
+def luna_beam_reorder(bd, parents, slots, nslots: int, pool, slot_bytes: int, new_slots, stream=None) -> None:
+    _check(_lib.luna_beam_reorder(ctypes.byref(bd), _ptr(parents), _ptr(slots), nslots, _ptr(pool), slot_bytes,
+                                  _ptr(new_slots), _stream(stream)), "luna_beam_reorder")
 
 
 # ---------------------------------------------------------------------------
@@ -655,6 +734,160 @@ class Decay(_Checked):
                                     _addr(slots), S.shape[0], S.data_ptr(), o.data_ptr(), self._on(stream)),
                "luna_decay_step")
         return o
+
+
+class Delta(_Checked):
+    """The gated delta rule at one problem shape; owns the workspace, so its calls belong on one stream at a time.
+    Q, K: (B, Hk, n, d), V: (B, H, n, dv), any strides with a contiguous last dimension; log_decay, beta: (B, H, n) of
+    the tensors' type, any strides; lengths: (B,) int32 or None; states: (B, H, d, dv) fp32."""
+
+    def __init__(self, B, H, n, d, dv, Hk=None, scale=None, io=torch.bfloat16, device="cuda", backward=False):
+        self.td = delta_desc(B, H, n, d, dv, Hk, scale, _DTYPES[io])
+        super().__init__(self.td)
+        self.io, self.device = io, _place(device)
+        self._workspace(max(luna_delta_workspace_size(self.td, b) for b in ((False, True) if backward else (False,))))
+        qk, vo, gate = (B, self.td.Hk, n, d), (B, H, n, dv), (B, H, n)
+        self.shapes = {"q": qk, "k": qk, "v": vo, "o": vo, "g": gate, "beta": gate}
+        self.state_shape = (B, H, d, dv)
+
+    def _view(self, kind: str, field: str, name: str, t) -> None:
+        """Checks a tensor of rows or gates (of single ones for a step) and notes its strides."""
+        shape = self.shapes[field if field in self.shapes else field[1:]]
+        rows = len(shape) == 4
+        if kind == "step":
+            shape = shape[:2] + shape[3:]
+        _want(name, t, shape, self.io, self.device)
+        s = t.stride()
+        if rows and s[-1] != 1 and t.shape[-1] != 1:
+            raise ValueError(f"{name}: the last dimension is not contiguous")
+        if not any(s[:-1] if rows else s) and (t[..., 0] if rows and t.shape[-1] else t).numel() > 1:
+            raise ValueError(f"{name}: one {'row' if rows else 'value'} repeated")
+        setattr(self._desc[kind], field, Strides(s[0], s[1], s[2] if kind != "step" else 0))
+
+    def _vector(self, name: str, t) -> None:
+        _want(name, t, self.state_shape[:1], torch.int32, self.device)
+        _dense(name, t)
+
+    def _states(self, **states) -> None:
+        for name, t in states.items():
+            _want(name, t, self.state_shape, torch.float32, self.device)
+            _dense(name, t)
+
+    def forward(self, Q, K, V, log_decay, beta, lengths=None, S0=None, want_state=False, O=None, S1=None, stream=None):
+        """O, or (O, S1) with want_state."""
+        if O is None:
+            O = _new(stream, torch.empty_like)(V)
+        if not self._looked_at("forward", Q, K, V, log_decay, beta, lengths, S0, O, S1):
+            for field, name, t in (("q", "Q", Q), ("k", "K", K), ("v", "V", V), ("g", "log_decay", log_decay),
+                                   ("beta", "beta", beta), ("o", "O", O)):
+                self._view("forward", field, name, t)
+            self._vector("lengths", lengths)
+            self._states(S0=S0, S1=S1)
+            self._accept()
+        if want_state and S1 is None:
+            S1 = _new(stream)(self.state_shape, dtype=torch.float32, device=self.device)
+        _check(_lib.luna_delta_fwd(self._ref["forward"], log_decay.data_ptr(), beta.data_ptr(), Q.data_ptr(), K.data_ptr(),
+                                   V.data_ptr(), _addr(lengths), _addr(S0), O.data_ptr(), _addr(S1), *self._ws,
+                                   self._on(stream)), "luna_delta_fwd")
+        return (O, S1) if want_state else O
+
+    def backward(self, Q, K, V, dO, log_decay, beta, lengths=None, S0=None, dS1=None, out=None, stream=None):
+        """dQ, dK, dV, dlog_decay, dbeta, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
+        if out is None:
+            out = {"d" + k: _new(stream, torch.empty_like)(t)
+                   for k, t in (("Q", Q), ("K", K), ("V", V), ("log_decay", log_decay), ("beta", beta))}
+            if S0 is not None:
+                out["dS0"] = _new(stream)(self.state_shape, dtype=torch.float32, device=self.device)
+        dQ, dK, dV, dg, db, dS0 = (out.get("d" + k) for k in ("Q", "K", "V", "log_decay", "beta", "S0"))
+        if not self._looked_at("backward", Q, K, V, dO, log_decay, beta, lengths, S0, dS1, dQ, dK, dV, dg, db, dS0):
+            for field, name, t in (("q", "Q", Q), ("k", "K", K), ("v", "V", V), ("g", "log_decay", log_decay),
+                                   ("beta", "beta", beta), ("go", "dO", dO), ("gq", "dQ", dQ), ("gk", "dK", dK),
+                                   ("gv", "dV", dV), ("gg", "dlog_decay", dg), ("gbeta", "dbeta", db)):
+                self._view("backward", field, name, t)
+            self._vector("lengths", lengths)
+            self._states(S0=S0, dS1=dS1, dS0=dS0)
+            self._accept()
+        _check(_lib.luna_delta_bwd(self._ref["backward"], log_decay.data_ptr(), beta.data_ptr(), Q.data_ptr(), K.data_ptr(),
+                                   V.data_ptr(), dO.data_ptr(), _addr(lengths), _addr(S0), _addr(dS1), dQ.data_ptr(),
+                                   dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), db.data_ptr(), _addr(dS0), *self._ws,
+                                   self._on(stream)), "luna_delta_bwd")
+        return out
+
+    def step(self, q, k, v, log_decay, beta, S, slots=None, o=None, stream=None):
+        """One token: q, k (B, Hk, d), v (B, H, dv), log_decay, beta (B, H); S (nslots, H, d, dv) is advanced in place."""
+        if o is None:
+            o = _new(stream)(self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=self.device)
+        if not self._looked_at("step", q, k, v, log_decay, beta, S, slots, o):
+            for field, name, t in (("q", "q", q), ("k", "k", k), ("v", "v", v), ("g", "log_decay", log_decay),
+                                   ("beta", "beta", beta), ("o", "o", o)):
+                self._view("step", field, name, t)
+            _want("S", S, (S.shape[0],) + self.state_shape[1:], torch.float32, self.device)
+            _dense("S", S)
+            self._vector("slots", slots)
+            self._accept()
+        _check(_lib.luna_delta_step(self._ref["step"], log_decay.data_ptr(), beta.data_ptr(), q.data_ptr(), k.data_ptr(),
+                                    v.data_ptr(), _addr(slots), S.shape[0], S.data_ptr(), o.data_ptr(),
+                                    self._on(stream)), "luna_delta_step")
+        return o
+
+
+class Beam(_Checked):
+    """Beam search over recurrent states: `beams` beams of each of B sequences.  Owns the workspace of select, whose
+    calls belong on one stream at a time.  vocab is not needed for reorder; end: the token that ends a sequence, or -1."""
+
+    def __init__(self, B, beams, vocab=0, end=-1, io=torch.bfloat16, device="cuda"):
+        self.bd = beam_desc(B, beams, vocab, end, _DTYPES[io])
+        super().__init__(self.bd)
+        self.io, self.device, self.shape = io, _place(device), (B, beams)
+        self._workspace(luna_beam_workspace_size(self.bd))
+
+    def _beams(self, dtype, **tensors) -> None:
+        for name, t in tensors.items():
+            _want(name, t, self.shape, dtype, self.device)
+            _dense(name, t)
+
+    def select(self, logits, scores, done=None, out=None, stream=None):
+        """The best continuations of every sequence from logits (B * beams, vocab), running log-probabilities scores
+        (B, beams) fp32 and, with an end token, done (B, beams) bool: {"scores", "tokens", "parents"} and with an end
+        token "done", each (B, beams), best first.  `out` may hold scores and done themselves."""
+        if out is None:
+            new, at = _new(stream), dict(device=self.device)
+            out = {"scores": new(self.shape, dtype=torch.float32, **at), "tokens": new(self.shape, dtype=torch.int32, **at),
+                   "parents": new(self.shape, dtype=torch.int32, **at)}
+            if self.bd.end >= 0:
+                out["done"] = new(self.shape, dtype=torch.bool, **at)
+        to = [out.get(k) for k in ("scores", "tokens", "parents", "done")]
+        if not self._looked_at("select", logits, scores, done, *to):
+            _set_rows(self._desc["forward"], "ld", "logits", logits, (self.shape[0] * self.shape[1], self.bd.V), self.io,
+                      self.device)
+            if any(t is None for t in to[:3]):
+                raise ValueError("out: needs scores, tokens and parents")
+            self._beams(torch.float32, scores=scores, scores_out=to[0])
+            self._beams(torch.int32, tokens=to[1], parents=to[2])
+            self._beams(torch.bool, done=done, done_out=to[3])
+            self._accept()
+        _check(_lib.luna_beam_select(self._ref["forward"], logits.data_ptr(), scores.data_ptr(), _addr(done),
+                                     *[_addr(t) for t in to], *self._ws, self._on(stream)), "luna_beam_select")
+        return out
+
+    def reorder(self, parents, slots, *pools, out=None, stream=None):
+        """The states in `pools` (each (nslots, ...), contiguous) follow their beams in place; returns the new beams'
+        slots (B, beams), for slots (B, beams) int32 of the old ones."""
+        if out is None:
+            out = _new(stream)(self.shape, dtype=torch.int32, device=self.device)
+        if not self._looked_at("reorder", parents, slots, out, *pools):
+            self._beams(torch.int32, parents=parents, slots=slots, out=out)
+            for i, t in enumerate(pools):
+                _want(f"pools[{i}]", t, t.shape, t.dtype, self.device)
+                if t.dim() < 1:
+                    raise ValueError(f"pools[{i}]: no slots")
+                _dense(f"pools[{i}]", t)
+            self._accept()
+        handle = self._on(stream)
+        for at, n, size in [(t.data_ptr(), t.shape[0], t[0].numel() * t.element_size() if t.shape[0] else 0) for t in pools] or [(None, 0, 0)]:
+            _check(_lib.luna_beam_reorder(self._ref["forward"], parents.data_ptr(), slots.data_ptr(), n, at, size,
+                                          out.data_ptr(), handle), "luna_beam_reorder")
+        return out
 
 
 def _set_rows(desc, field: str, name: str, t, shape, dtype, device) -> None:
