@@ -21,11 +21,15 @@
 // each of the parts q_i . dQ_i, k_j . dK_j adds to the rows up to i, or takes from those up to j.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "luna_decay.cuh"
 
 namespace luna {
 
-constexpr int kDeltaRows = 64;  // rows of a chunk
+constexpr int kDeltaRows = 64;      // rows of a chunk
+// tensor-core form: fp32 values of a chunk's factors, and of the scales of 16 columns of it
+constexpr int kDeltaFactors = 4 * kDeltaRows + 4, kDeltaScales = 8;
 
 struct GateView {  // a (B, H, n) tensor
     const void *p;
@@ -52,10 +56,13 @@ struct DeltaArgs {
     // intermediate results
     float *U, *X;           // rows written and their gradients, [B H][n][dv] (CUDA-core form)
     float *before, *after;  // states before chunk i, gradients of the states before chunk i, [B H][m + 1][d][dv]
-    __nv_bfloat16 *Tp, *Pp; // tensor-core form: planes of the chunks' inverses and scores, [B H][m][2][64][64]
-    float *rows;            // tensor-core form: c(i, 0), c(C, i), b_i of every row, [B H][m][3][64]
-    __nv_bfloat16 *Up, *Xp; // tensor-core form: planes of U and X, [B H][m][2][64][dv padded]
-    __nv_bfloat16 *Sp, *Rp; // tensor-core form: the states at the chunks' ends, [B H][m][d padded][dv padded]
+    // tensor-core form (fp16, scaled; dvp: dv to a multiple of 16, dp: d to 64 or 128), for every chunk: its rows of K
+    // and Q ([B Hk][m][64][dp]), the inverse T in two planes and the scores P in `planes` of them ([64][64] each),
+    // factors of its rows; and for every 16 columns of a chunk U and X ([16][64], transposed), the states at its two
+    // ends (S before, R behind; [16][dp], transposed), and what S, R, U, X and dO were scaled down by
+    __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Sp, *Rp;
+    float *rows, *scales;
+    int planes, dvp;
 };
 
 struct DeltaStep {
@@ -146,6 +153,9 @@ __device__ __forceinline__ void delta_gate_grads(float base, const float *read, 
 
 cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s);
 cudaError_t launch_delta_grad(const DeltaArgs &a, luna_dtype io, luna_dtype out, cudaStream_t s);
+cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s);
+cudaError_t launch_delta_chain(const DeltaArgs &a, bool reverse, cudaStream_t s);
+cudaError_t launch_delta_grad_tc(const DeltaArgs &a, luna_dtype out, cudaStream_t s);
 cudaError_t launch_delta_step(const DeltaStep &a, luna_dtype io, cudaStream_t s);
 
 }  // namespace luna

@@ -52,30 +52,65 @@ luna_status check(const luna_delta_desc *dd) {
 
 bool empty(const luna_delta_desc *dd) { return (int64_t)dd->B * dd->H == 0; }
 
-// Bytes of the parts of a workspace.
+// Offsets of the parts of a workspace.  Which form runs is known at the call alone (by the tensors' alignment): both
+// lie in the same bytes.
 struct Plan {
-    int m;
-    size_t U = 0, X = 0, before = 0, after = 0, dq = 0, dk = 0;  // offsets, CUDA-core form
+    int m, dvp, dp;
+    size_t dq = 0, dk = 0;                          // gradients of shared queries and keys, one for each head
+    size_t U = 0, X = 0, before = 0, after = 0;      // CUDA-core form
+    size_t K = 0, Q = 0, T = 0, P = 0, rows = 0;     // tensor-core form, in a forward pass too
+    size_t Up = 0, Xp = 0, Sp = 0, Rp = 0, scales = 0;  // (gradients)
     size_t fwd = 256, bwd = 256;
 };
+
+// Widths that the tensor-core form takes.
+bool tc_widths(const luna_delta_desc *dd) { return dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0; }
 
 Plan make_plan(const luna_delta_desc *dd) {
     Plan p;
     const int64_t BH = (int64_t)dd->B * dd->H;
     p.m = (int)cdiv(dd->n, kDeltaRows);
+    p.dvp = (int)cdiv(dd->dv, 16) * 16;
+    p.dp = dd->d <= 64 ? 64 : 128;
     size_t at = 256;
     auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)align256(bytes); return o; };
-    if (dd->H != dd->Hk) {  // gradients of shared queries and keys, one for each value head
-        p.dq = take(BH * dd->n * dd->d * 4);
-        p.dk = take(BH * dd->n * dd->d * 4);
+    const int64_t tile = (int64_t)kDeltaRows * kDeltaRows * 2, chunks = BH * p.m;
+    const bool tc = tc_widths(dd);
+    if (tc) {
+        p.rows = take(chunks * kDeltaFactors * 4);
+        p.K = take((int64_t)dd->B * dd->Hk * p.m * kDeltaRows * p.dp * 2);
+        p.Q = take((int64_t)dd->B * dd->Hk * p.m * kDeltaRows * p.dp * 2);
+        p.T = take(chunks * 2 * tile);
+        p.P = take(chunks * tile);
+        p.fwd = at;
+        at = p.P;
+        take(chunks * 2 * tile);  // (in two planes)
+        p.Up = take(chunks * p.dvp * kDeltaRows * 2);
+        p.Xp = take(chunks * p.dvp * kDeltaRows * 2);
+        p.Sp = take(chunks * p.dvp * p.dp * 2);
+        p.Rp = take(chunks * p.dvp * p.dp * 2);
+        p.scales = take(chunks * (p.dvp / 16) * kDeltaScales * 4);
     }
+    const size_t end_tc = at;
+    at = 256;
     p.U = take(BH * dd->n * dd->dv * 4);
     p.X = take(BH * dd->n * dd->dv * 4);
     p.before = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
     p.after = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
+    at = std::max(at, end_tc);
+    if (dd->H != dd->Hk) {
+        p.dq = take(BH * dd->n * dd->d * 4);
+        p.dk = take(BH * dd->n * dd->d * 4);
+    }
     p.bwd = at;
     return p;
 }
+
+// Whether rows start on 16-byte boundaries.
+bool rows16(const void *p, const luna_strides &s) {
+    return aligned(p, 16) && s.b % 8 == 0 && s.h % 8 == 0 && s.t % 8 == 0;
+}
+bool rows16(const RowView &v) { return rows16(v.p, luna_strides{v.sb, v.sh, v.st}); }
 
 RowView view(const void *p, const luna_strides &s, int heads) { return RowView{p, s.b, s.h, s.t, heads}; }
 GateView gate(const void *p, const luna_strides &s) { return GateView{p, s.b, s.h, s.t}; }
@@ -92,7 +127,19 @@ DeltaArgs base(const luna_delta_desc *dd, const Plan &p, const void *g, const vo
     a.lengths = lengths;
     a.B = dd->B; a.H = dd->H; a.n = dd->n; a.d = dd->d; a.dv = dd->dv; a.m = p.m;
     a.scale = dd->scale;
+    a.dvp = p.dvp;
     return a;
+}
+
+// The tensor-core form's parts of the workspace.
+void tc_parts(DeltaArgs &a, const Plan &p, char *ws, bool backward) {
+    auto at = [&](size_t o) { return reinterpret_cast<__half *>(ws + o); };
+    a.rows = reinterpret_cast<float *>(ws + p.rows);
+    a.Kp = at(p.K); a.Qp = at(p.Q); a.Tp = at(p.T); a.Pp = at(p.P);
+    a.planes = backward ? 2 : 1;
+    if (!backward) return;
+    a.Up = at(p.Up); a.Xp = at(p.Xp); a.Sp = at(p.Sp); a.Rp = at(p.Rp);
+    a.scales = reinterpret_cast<float *>(ws + p.scales);
 }
 
 }  // namespace
@@ -129,7 +176,11 @@ luna_status luna_delta_fwd(const luna_delta_desc *dd, const void *log_decay, con
     a.o = O; a.ob = so.b; a.oh = so.h; a.ot = so.t;
     a.S0 = S0;
     a.S1 = S1;
-    return cuda_status(launch_delta_rows(a, dd->io, false, s));
+    if (!tc_widths(dd) || !rows16(a.q) || !rows16(a.k) || !rows16(a.v) || !rows16(O, so))
+        return cuda_status(launch_delta_rows(a, dd->io, false, s));
+    tc_parts(a, p, static_cast<char *>(workspace), false);
+    if (launch_delta_prepare(a, s) != cudaSuccess) return LUNA_ERR_CUDA;
+    return cuda_status(launch_delta_chain(a, false, s));
 }
 
 luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, const void *beta, const void *Q, const void *K,

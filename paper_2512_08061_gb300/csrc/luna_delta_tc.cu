@@ -1,0 +1,777 @@
+// The gated delta rule on tensor cores: bf16, chunks of 64 rows.
+//
+// With G_i the sum of a chunk's gates to row i, c(i, j) = exp(G_i - G_j), S the state before the chunk and
+//
+//     A_ij = b_i c(i, j) k_i . k_j  (j < i),   T = (1 + A)^-1,   P_ij = scale c(i, j) q_i . k_j  (j <= i)
+//
+// the rows that the chunk writes, its outputs and the state behind it are
+//
+//     U = T diag(b) (V - diag(c(i, 0)) K S),   O = scale diag(c(i, 0)) Q S + P U,   S' = c(C, 0) S + K^T diag(c(C, j)) U
+//
+// and with R the gradient of S', that of U's right-hand side and of S
+//
+//     X = T^T (P^T dO + diag(c(C, j)) K R),   R' = c(C, 0) R + scale Q^T diag(c(i, 0)) dO - K^T diag(b_i c(i, 0)) X.
+//
+// T and P come from one launch over all chunks; the chains over the chunks then run column by column of the state, a
+// warp holding 16 columns (of S^T or R^T: 16 rows by d) in its accumulators.  The accumulators of one product have the
+// layout that the next one's left operand wants, so that the whole chain of a chunk stays in a warp's registers and
+// warps meet only where tiles arrive in shared memory.  That is why these products are the warps' own matrix
+// instructions: through TMEM each of the chain's three products would wait for a round trip and a barrier, in tiles of
+// 128 columns, one block a head (32 blocks for a prompt of 32 heads, where this form has 128).
+// Precision.  Operands are fp16, scaled by powers of two: 11 bits where bf16 has 8, two terms 22.  The state, U and X
+// enter products in two terms, T and (in reverse) P too, so that states and U are off by a few 1e-7; the outputs take
+// one term of S, U and P (1.4e-4, under their own rounding).  Rows of K and Q are scaled to a largest value of 2^12 to
+// 2^13, T and P by chunk, what a warp holds by its largest value, so that whatever is 2^-15 of its neighbours still has
+// its 22 bits; K, Q and dO are exact down to 2^-26 of their row's or tile's largest value.  What a chunk adds to the
+// state is summed by itself and added in fp32, because the tensor cores cut sums off.
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include "luna_delta.cuh"
+#include "luna_prof.cuh"
+
+namespace luna {
+int tc_sm_count();
+
+namespace {
+
+constexpr int C = kDeltaRows;
+constexpr int kTileB = C * C * 2;  // bytes of a 64 x 64 bf16 tile: rows of 128 bytes, 16-byte pieces swizzled
+constexpr int kRowsF = kDeltaFactors;
+
+// ---- tiles in shared memory: panels of 64 columns, row r's 16-byte piece p at place p ^ (r % 8)
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t tile_at(uint32_t base, int rows, int r, int piece) {
+    return base + (piece >> 3) * rows * 128 + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// a tile of `rows` rows (64 of them, DP columns) of a tensor of d columns; zeros behind both
+template <int DP>
+__device__ __forceinline__ void load_rows(uint32_t dst, const __nv_bfloat16 *src, int64_t st, int rows, int d, int tid, int threads) {
+    for (int i = tid; i < C * DP / 8; i += threads) {
+        const int r = i / (DP / 8), p = i % (DP / 8);
+        const bool in = r < rows && p * 8 < d;
+        copy16(tile_at(dst, C, r, p), in ? src + r * st + p * 8 : src, in);
+    }
+}
+// a tile of 64 rows of W columns that lie one behind the other
+template <int W>
+__device__ __forceinline__ void load_plane(uint32_t dst, const __half *src, int tid, int threads) {
+    for (int i = tid; i < C * W / 8; i += threads) copy16(tile_at(dst, C, i / (W / 8), i % (W / 8)), src + i * 8, true);
+}
+
+// ---- matrix instructions
+
+using Frag = uint32_t[4];
+
+__device__ __forceinline__ void ldm(Frag &f, uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3]) : "r"(at));
+}
+__device__ __forceinline__ void ldm_t(Frag &f, uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3]) : "r"(at));
+}
+__device__ __forceinline__ void stm_t(uint32_t at, const Frag &f) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const Frag &a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const Frag &a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Right operands of 16 summed indices and 16 columns (two n-tiles) from a tile that holds a row for each column (n) or
+// for each summed index (k).
+__device__ __forceinline__ void right_n(Frag &f, uint32_t base, int rows, int n0, int k0, int lane) {
+    ldm(f, tile_at(base, rows, n0 + (lane >> 4) * 8 + (lane & 7), (k0 >> 3) + ((lane >> 3) & 1)));
+}
+__device__ __forceinline__ void right_k(Frag &f, uint32_t base, int rows, int k0, int n0, int lane) {
+    ldm_t(f, tile_at(base, rows, k0 + ((lane >> 3) & 1) * 8 + (lane & 7), (n0 >> 3) + (lane >> 4)));
+}
+// Left operands of 16 rows and 16 summed indices from a tile that holds a row for each row (m) or summed index (k).
+__device__ __forceinline__ void left_m(Frag &f, uint32_t base, int rows, int m0, int k0, int lane) {
+    ldm(f, tile_at(base, rows, m0 + ((lane >> 3) & 1) * 8 + (lane & 7), (k0 >> 3) + (lane >> 4)));
+}
+__device__ __forceinline__ void left_k(Frag &f, uint32_t base, int rows, int k0, int m0, int lane) {
+    ldm_t(f, tile_at(base, rows, k0 + (lane >> 4) * 8 + (lane & 7), (m0 >> 3) + ((lane >> 3) & 1)));
+}
+
+// pairs of bf16 (outputs, V, dO) and of fp16 (operands)
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float low(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// x = hi + lo to 22 bits
+__device__ __forceinline__ void split(float x0, float x1, uint32_t &hi, uint32_t &lo) {
+    hi = pack(x0, x1);
+    __half2 h;
+    memcpy(&h, &hi, 4);
+    const float2 f = __half22float2(h);
+    lo = pack(x0 - f.x, x1 - f.y);
+}
+// The power of two that takes a largest value of 2^E (to 2^(E+1)) to 2^12, and its inverse.  (Below 2^-113 all is 0.)
+struct Scale {
+    float by, back;
+};
+__device__ __forceinline__ Scale scale_of(float most) {
+    const uint32_t e = max((__float_as_uint(most) >> 23) & 255u, 14u);
+    return Scale{__uint_as_float((254u + 12u - e) << 23), __uint_as_float((e - 12u) << 23)};
+}
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+    return x;
+}
+// one scale for all that a warp holds
+template <int N>
+__device__ __forceinline__ Scale scale_of(const float (&c)[N][4]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, fmaxf(fmaxf(fabsf(c[i][0]), fabsf(c[i][1])), fmaxf(fabsf(c[i][2]), fabsf(c[i][3]))));
+    return scale_of(warp_max(m));
+}
+// the left operand whose 16 summed indices are two neighbouring n-tiles of accumulators
+__device__ __forceinline__ void split_left(const float (&c0)[4], const float (&c1)[4], float by, Frag &hi, Frag &lo) {
+    split(by * c0[0], by * c0[1], hi[0], lo[0]);
+    split(by * c0[2], by * c0[3], hi[1], lo[1]);
+    split(by * c1[0], by * c1[1], hi[2], lo[2]);
+    split(by * c1[2], by * c1[3], hi[3], lo[3]);
+}
+
+template <int N>
+__device__ __forceinline__ void zero(float (&c)[N][4]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[i][j] = 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// T, P and the factors of every chunk.  A block of four warps a chunk, a warp 16 rows of K K^T and Q K^T.  The inverse
+// is taken in fp32: the diagonal blocks of 16 rows by substitution, a thread a column, then those of 32 and of 64 rows
+// from T21 = -T22 A21 T11.
+
+constexpr int kPrepThreads = 128, kLdA = C + 4;
+
+// What it leaves in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b, scale c(i, 0) 2^eq of its rows (2^ek, 2^eq: what
+// the rows of K and Q were scaled down by), then c(C, 0) in two terms and what T and P were scaled down by.
+
+template <int DP>
+struct PrepShared {
+    alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB];
+    float A[C][kLdA], T[C][kLdA];
+    float hi[C], lo[C], past[C], left[C], b[C], ek[C], eq[C], most[2][kPrepThreads / 32];
+};
+
+// The rows of a bf16 tile (two threads each) in fp16, scaled: to `out` (unless it is null); what they were scaled
+// down by to back[]
+template <int DP>
+__device__ __forceinline__ void prep_scale(uint32_t tile, __half *out, float *back, int tid) {
+    const int r = tid / 2, p0 = tid % 2 * (DP / 16);
+    uint4 w[DP / 16];
+    uint32_t most = 0;
+#pragma unroll
+    for (int p = 0; p < DP / 16; ++p) {
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(tile_at(tile, C, r, p0 + p)));
+        const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, max((u[i] << 16) & 0x7fff0000u, u[i] & 0x7fff0000u));
+    }
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    const Scale s = scale_of(__uint_as_float(most));
+    if (tid % 2 == 0) back[r] = s.back;
+    if (!out) return;
+#pragma unroll
+    for (int p = 0; p < DP / 16; ++p) {
+        const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+        uint32_t f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = pack(s.by * low(u[i]), s.by * high(u[i]));
+        *reinterpret_cast<uint4 *>(out + r * DP + (p0 + p) * 8) = make_uint4(f[0], f[1], f[2], f[3]);
+    }
+}
+
+// out = sign X Y for W x W matrices of rows kLdA apart, by `threads` threads: four neighbouring columns of a row each
+template <int W>
+__device__ __forceinline__ void prep_product(float *out, const float *X, const float *Y, float sign, int t, int threads) {
+    for (int i = t; i < W * W / 4; i += threads) {
+        const int r = i / (W / 4), c = i % (W / 4) * 4;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int l = 0; l < W; ++l) {
+            const float x = X[r * kLdA + l];
+            const float4 y = *reinterpret_cast<const float4 *>(Y + l * kLdA + c);
+            acc.x = fmaf(x, y.x, acc.x); acc.y = fmaf(x, y.y, acc.y); acc.z = fmaf(x, y.z, acc.z); acc.w = fmaf(x, y.w, acc.w);
+        }
+        *reinterpret_cast<float4 *>(out + r * kLdA + c) = make_float4(sign * acc.x, sign * acc.y, sign * acc.z, sign * acc.w);
+    }
+}
+
+template <int DP, bool TERMS>  // TERMS: P in two terms
+__global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
+    extern __shared__ __align__(128) char raw[];
+    PrepShared<DP> &sm = *reinterpret_cast<PrepShared<DP> *>(raw);
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const int64_t at = blockIdx.x, bh = at / a.m;
+    const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
+    const int rows = min(C, head_length(a.lengths, b, a.n) - t0);
+    if (rows <= 0) return;
+    const int hk = h / (a.H / a.k.heads);
+    const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q);
+    load_rows<DP>(sk, static_cast<const __nv_bfloat16 *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st, a.k.st, rows, a.d, tid, kPrepThreads);
+    load_rows<DP>(sq, static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st, a.q.st, rows, a.d, tid, kPrepThreads);
+    copies_end();
+    if (warp == 0)
+        delta_gate_sums(lane, [&](int t) { return t < rows ? gate_at<__nv_bfloat16>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
+                        sm.past, sm.left);
+    else if (warp < 3)
+        sm.b[tid - 32] = tid - 32 < rows ? gate_at<__nv_bfloat16>(a.b, b, h, t0 + tid - 32) : 0.0f;
+    copies_wait<0>();
+    __syncthreads();
+    {  // one head of those that share queries and keys writes them
+        const bool writes = h % (a.H / a.k.heads) == 0;
+        const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+        prep_scale<DP>(sk, writes ? a.Kp + to * C * DP : nullptr, sm.ek, tid);
+        prep_scale<DP>(sq, writes ? a.Qp + to * C * DP : nullptr, sm.eq, tid);
+    }
+    float *rowf = a.rows + at * kRowsF;
+
+    const int r0 = warp * 16;
+    float kk[8][4], qk[8][4];
+    zero(kk);
+    zero(qk);
+#pragma unroll
+    for (int k0 = 0; k0 < DP; k0 += 16) {
+        Frag fk, fq;
+        left_m(fk, sk, C, r0, k0, lane);
+        left_m(fq, sq, C, r0, k0, lane);
+#pragma unroll
+        for (int n0 = 0; n0 < C; n0 += 16) {
+            if (n0 > r0) continue;
+            Frag f;
+            right_n(f, sk, C, n0, k0, lane);
+            mma_bf16(kk[n0 / 8], fk, f[0], f[1]);
+            mma_bf16(kk[n0 / 8 + 1], fk, f[2], f[3]);
+            mma_bf16(qk[n0 / 8], fq, f[0], f[1]);
+            mma_bf16(qk[n0 / 8 + 1], fq, f[2], f[3]);
+        }
+    }
+    float most = 0.0f;
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = r0 + lane / 4 + half * 8, j = nt * 8 + lane % 4 * 2;
+            float w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float c = j + e <= i ? expf((sm.hi[i] - sm.hi[j + e]) + (sm.lo[i] - sm.lo[j + e])) : 0.0f;
+                float &p = qk[nt][half * 2 + e];
+                p = j + e <= i ? a.scale * c * p : 0.0f;
+                most = fmaxf(most, fabsf(p));
+                w[e] = j + e < i ? sm.b[i] * c * kk[nt][half * 2 + e] : 0.0f;
+            }
+            *reinterpret_cast<float2 *>(&sm.A[i][j]) = make_float2(w[0], w[1]);
+            *reinterpret_cast<float2 *>(&sm.T[i][j]) = make_float2(0.0f, 0.0f);
+        }
+    most = warp_max(most);
+    if (lane == 0) sm.most[0][warp] = most;
+    __syncthreads();
+    auto block_scale = [&](int which) {
+        const float *m = sm.most[which];
+        return scale_of(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+    };
+    const Scale ps = block_scale(0);
+    __half *P = a.Pp + at * (TERMS ? 2 : 1) * C * C;
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int i = r0 + lane / 4 + half * 8, j = nt * 8 + lane % 4 * 2;
+            uint32_t hi, lo;
+            split(ps.by * qk[nt][half * 2], ps.by * qk[nt][half * 2 + 1], hi, lo);
+            *reinterpret_cast<uint32_t *>(P + i * C + j) = hi;
+            if (TERMS) *reinterpret_cast<uint32_t *>(P + C * C + i * C + j) = lo;
+        }
+    if (tid < C) {
+        rowf[tid] = sm.past[tid] * sm.ek[tid];
+        rowf[C + tid] = sm.left[tid] * sm.ek[tid];
+        rowf[2 * C + tid] = sm.b[tid];
+        rowf[3 * C + tid] = a.scale * sm.past[tid] * sm.eq[tid];
+    }
+    if (tid == 0) {
+        gate_terms(sm.hi[C - 1], rowf[4 * C], rowf[4 * C + 1]);
+        rowf[4 * C + 3] = ps.back;
+    }
+    if (lane < 16) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = i == lane ? 1.0f : 0.0f;
+#pragma unroll
+            for (int l = 0; l < i; ++l) x[i] = fmaf(-sm.A[r0 + i][r0 + l], x[l], x[i]);
+            sm.T[r0 + i][r0 + lane] = x[i];
+        }
+    }
+    __syncthreads();
+    // T21 = -T22 (A21 T11), with A21 T11 above A's diagonal, where nothing is needed
+    auto A = [&](int r, int c) { return &sm.A[r][c]; };
+    auto T = [&](int r, int c) { return &sm.T[r][c]; };
+    const int o = warp / 2 * 32, t64 = tid % 64;
+    prep_product<16>(A(o, o + 16), A(o + 16, o), T(o, o), 1.0f, t64, 64);
+    __syncthreads();
+    prep_product<16>(T(o + 16, o), T(o + 16, o + 16), A(o, o + 16), -1.0f, t64, 64);
+    __syncthreads();
+    prep_product<32>(A(0, 32), A(32, 0), T(0, 0), 1.0f, tid, kPrepThreads);
+    __syncthreads();
+    prep_product<32>(T(32, 0), T(32, 32), A(0, 32), -1.0f, tid, kPrepThreads);
+    __syncthreads();
+    float2 x[C * C / 2 / kPrepThreads];
+    most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i) {
+        const int p = tid + i * kPrepThreads;
+        x[i] = *reinterpret_cast<const float2 *>(&sm.T[p / (C / 2)][p % (C / 2) * 2]);
+        most = fmaxf(most, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
+    }
+    most = warp_max(most);
+    if (lane == 0) sm.most[1][warp] = most;
+    __syncthreads();
+    const Scale ts = block_scale(1);
+    if (tid == 0) rowf[4 * C + 2] = ts.back;
+    uint32_t *planes = reinterpret_cast<uint32_t *>(a.Tp + at * 2 * C * C) + tid;
+#pragma unroll
+    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i)
+        split(ts.by * x[i].x, ts.by * x[i].y, planes[i * kPrepThreads], planes[i * kPrepThreads + C * C / 2]);
+}
+
+// ---------------------------------------------------------------------------
+// The chains.  A block of NW warps has 16 NW columns of one head's state.  The tiles of a chunk come by asynchronous
+// copies while the chunk before is worked on; one barrier a chunk.
+
+template <int DP, int NW, bool REV>
+struct ChainShared {
+    static constexpr int kPitch = NW * 32 + 16;  // bytes of a row of V or dO: eight rows start in eight banks
+    static constexpr int kPlanes = REV ? 2 : 1;  // of P
+    struct Stage {
+        alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], T[2][kTileB], P[kPlanes][kTileB], x[C * kPitch];
+        alignas(16) float rows[kRowsF];
+    } stage[2];
+    alignas(16) char out[NW][C * 48];  // a warp's 16 columns of the outputs, rows of 32 bytes 48 apart
+};
+
+template <int DP, int NW, bool REV>
+__device__ __forceinline__ void chain_load(typename ChainShared<DP, NW, REV>::Stage &st, const DeltaArgs &a, int64_t bh, int b, int h,
+                                           int chunk, int len, int col0, int tid) {
+    using Sh = ChainShared<DP, NW, REV>;
+    constexpr int TH = NW * 32;
+    const int hk = h / (a.H / a.k.heads), t0 = chunk * C, rows = min(C, len - t0);
+    const int64_t at = bh * a.m + chunk;
+    const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+    load_plane<DP>(smem_u32(st.k), a.Kp + kat * C * DP, tid, TH);
+    if (REV || a.o) load_plane<DP>(smem_u32(st.q), a.Qp + kat * C * DP, tid, TH);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_plane<C>(smem_u32(st.T[i]), a.Tp + (at * 2 + i) * C * C, tid, TH);
+    if (REV || a.o)
+#pragma unroll
+        for (int i = 0; i < Sh::kPlanes; ++i) load_plane<C>(smem_u32(st.P[i]), a.Pp + (at * a.planes + i) * C * C, tid, TH);
+    const RowView &xv = REV ? a.go : a.v;
+    const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(xv.p) + b * xv.sb + h * xv.sh + t0 * xv.st + col0;
+    const uint32_t sx = smem_u32(st.x);
+    for (int i = tid; i < C * NW * 2; i += TH) {
+        const int r = i / (NW * 2), p = i % (NW * 2);
+        const bool in = r < rows && col0 + p * 8 < a.dv;
+        copy16(sx + r * Sh::kPitch + p * 16, in ? x + r * xv.st + p * 8 : static_cast<const __nv_bfloat16 *>(xv.p), in);
+    }
+    for (int i = tid; i < kRowsF / 4; i += TH) copy16(smem_u32(st.rows) + i * 16, a.rows + at * kRowsF + i * 4, true);
+    copies_end();
+}
+
+// Rows of a warp's 16 columns, given column by column, to the output: transposed through shared memory
+template <int N>
+__device__ __forceinline__ void chain_store(const float (&acc)[N][4], char *mem, __nv_bfloat16 *out, int64_t st, int rows, int col, int dv, int lane) {
+    const uint32_t base = smem_u32(mem);
+#pragma unroll
+    for (int nt = 0; nt < 8; nt += 2) {
+        const Frag f = {pack_bf16(acc[nt][0], acc[nt][1]), pack_bf16(acc[nt][2], acc[nt][3]),
+                        pack_bf16(acc[nt + 1][0], acc[nt + 1][1]), pack_bf16(acc[nt + 1][2], acc[nt + 1][3])};
+        stm_t(base + (nt * 8 + (lane >> 4) * 8 + (lane & 7)) * 48 + ((lane >> 3) & 1) * 16, f);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 16 + lane / 2, half = lane % 2;
+        if (r < rows && col + half * 8 < dv)
+            *reinterpret_cast<uint4 *>(out + r * st + col + half * 8) = *reinterpret_cast<const uint4 *>(mem + r * 48 + half * 16);
+    }
+    __syncwarp();
+}
+
+// one plane's 16 x 16 piece of a left operand (rows of a tensor of `ld` columns)
+__device__ __forceinline__ void plane_store(__half *p, int64_t ld, int k0, const Frag &f, int lane) {
+    uint32_t *at = reinterpret_cast<uint32_t *>(p + lane / 4 * ld + k0 + lane % 4 * 2);
+    at[0] = f[0];
+    at[4 * ld] = f[1];
+    at[4] = f[2];
+    at[4 * ld + 4] = f[3];
+}
+
+template <int DP, int NW, bool REV>
+__global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
+    using Sh = ChainShared<DP, NW, REV>;
+    extern __shared__ __align__(128) char raw[];
+    Sh &sm = *reinterpret_cast<Sh *>(raw);
+    constexpr int ND = DP / 8;  // n-tiles of a state's row
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const int64_t bh = blockIdx.x;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * NW * 16, col = col0 + warp * 16;
+    const int len = head_length(a.lengths, b, a.n), chunks = (len + C - 1) / C, q2 = lane % 4 * 2;
+    const bool mine = col < a.dv;  // the warp has columns
+    __nv_bfloat16 *o = a.o ? static_cast<__nv_bfloat16 *>(a.o) + b * a.ob + h * a.oh : nullptr;
+    __half *planes = REV ? a.Xp : a.Up, *ends = REV ? a.Rp : a.Sp;
+
+    // S^T or R^T: row lane / 4 (and 8 more) of the warp's columns, values 8 nt + q2 and the next
+    float S[ND][4];
+    const float *init = REV ? a.dS1 : a.S0;
+    auto place = [&](int nt, int e, int64_t &at) {
+        const int c = col + lane / 4 + (e >> 1) * 8, r = nt * 8 + q2 + (e & 1);
+        at = (bh * a.d + r) * a.dv + c;
+        return r < a.d && c < a.dv;
+    };
+#pragma unroll
+    for (int nt = 0; nt < ND; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            int64_t at;
+            S[nt][e] = init && place(nt, e, at) ? init[at] : 0.0f;
+        }
+
+    if (chunks > 0) chain_load<DP, NW, REV>(sm.stage[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
+    for (int step = 0; step < chunks; ++step) {
+        const int chunk = REV ? chunks - 1 - step : step, t0 = chunk * C;
+        typename Sh::Stage &st = sm.stage[step & 1];
+        copies_wait<0>();
+        __syncthreads();
+        if (step + 1 < chunks)
+            chain_load<DP, NW, REV>(sm.stage[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
+        if (!mine) continue;
+        const uint32_t sk = smem_u32(st.k), sq = smem_u32(st.q), sT = smem_u32(st.T), sP = smem_u32(st.P);
+        const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + warp * 32 + ((lane >> 3) & 1) * 16;
+        const float whole = st.rows[4 * C], rest = st.rows[4 * C + 1], back_T = st.rows[4 * C + 2], back_P = st.rows[4 * C + 3];
+        auto factor = [&](int which, int t) { return *reinterpret_cast<const float2 *>(st.rows + which * C + t); };
+        const int64_t group = (bh * a.m + chunk) * (a.dvp / 16) + col / 16;  // the warp's columns in the planes
+        __half *keep = planes ? planes + group * 16 * C : nullptr;
+        float *scales = a.scales ? a.scales + group * kDeltaScales : nullptr;  // S, R, U, X, dO
+        // S <- c(C, 0) S (first) + F M for a left operand F of 64 summed rows and the tile M (a row for each)
+        auto update = [&](const Frag (&fh)[4], const Frag (&fl)[4], float back, uint32_t tile, bool decay) {
+#pragma unroll
+            for (int np = 0; np < DP / 16; ++np) {
+                float acc[2][4];
+                zero(acc);
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) {
+                    Frag f;
+                    right_k(f, tile, C, kt * 16, np * 16, lane);
+                    mma(acc[0], fh[kt], f[0], f[1]);
+                    mma(acc[1], fh[kt], f[2], f[3]);
+                    mma(acc[0], fl[kt], f[0], f[1]);
+                    mma(acc[1], fl[kt], f[2], f[3]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float &s = S[2 * np + i][e];
+                        s = decay ? fmaf(whole, s, fmaf(rest, s, back * acc[i][e])) : fmaf(back, acc[i][e], s);
+                    }
+            }
+        };
+        float x[8][4], y[8][4];
+        zero(x);
+        zero(y);
+        // x = K S (or K R), with it Q S
+        const Scale ss = scale_of(S);
+#pragma unroll
+        for (int kt = 0; kt < DP / 16; ++kt) {
+            Frag hi, lo;
+            split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
+            if (ends) plane_store(ends + group * 16 * DP, DP, kt * 16, hi, lane);
+#pragma unroll
+            for (int np = 0; np < 4; ++np) {
+                Frag f;
+                right_n(f, sk, C, np * 16, kt * 16, lane);
+                mma(x[2 * np], hi, f[0], f[1]);
+                mma(x[2 * np + 1], hi, f[2], f[3]);
+                mma(x[2 * np], lo, f[0], f[1]);
+                mma(x[2 * np + 1], lo, f[2], f[3]);
+                if (!REV && o) {
+                    right_n(f, sq, C, np * 16, kt * 16, lane);
+                    mma(y[2 * np], hi, f[0], f[1]);
+                    mma(y[2 * np + 1], hi, f[2], f[3]);
+                }
+            }
+        }
+        if (scales && lane == 0) scales[REV ? 1 : 0] = ss.back;
+        Frag fh[4], fl[4];
+        if (!REV) {
+            // x = b (V - c(i, 0) K S)
+#pragma unroll
+            for (int np = 0; np < 4; ++np) {
+                Frag v;
+                ldm_t(v, sx + np * 16 * Sh::kPitch);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int nt = 2 * np + i, t = nt * 8 + q2;
+                    const float2 past = factor(0, t), beta = factor(2, t);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = ss.back * (e & 1 ? past.y : past.x), vv = e & 1 ? high(v[2 * i + (e >> 1)]) : low(v[2 * i + (e >> 1)]);
+                        x[nt][e] = (e & 1 ? beta.y : beta.x) * fmaf(-p, x[nt][e], vv);
+                    }
+                }
+            }
+            // U = T x
+            float u[8][4];
+            zero(u);
+            const Scale xs = scale_of(x);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                Frag hi, lo;
+                split_left(x[2 * kt], x[2 * kt + 1], xs.by, hi, lo);
+#pragma unroll
+                for (int np = kt; np < 4; ++np) {
+                    Frag f;
+                    right_n(f, sT, C, np * 16, kt * 16, lane);
+                    mma(u[2 * np], hi, f[0], f[1]);
+                    mma(u[2 * np + 1], hi, f[2], f[3]);
+                    mma(u[2 * np], lo, f[0], f[1]);
+                    mma(u[2 * np + 1], lo, f[2], f[3]);
+                    right_n(f, sT + kTileB, C, np * 16, kt * 16, lane);
+                    mma(u[2 * np], hi, f[0], f[1]);
+                    mma(u[2 * np + 1], hi, f[2], f[3]);
+                }
+            }
+            const float back_u = xs.back * back_T;
+            if (o || keep) {  // P U; U's plane
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { u[nt][e] *= back_u; x[nt][e] = 0.0f; }
+                const Scale us = scale_of(u);
+#pragma unroll
+                for (int kt = 0; kt < 4; ++kt) {
+                    const Frag hi = {pack(us.by * u[2 * kt][0], us.by * u[2 * kt][1]), pack(us.by * u[2 * kt][2], us.by * u[2 * kt][3]),
+                                     pack(us.by * u[2 * kt + 1][0], us.by * u[2 * kt + 1][1]), pack(us.by * u[2 * kt + 1][2], us.by * u[2 * kt + 1][3])};
+                    if (keep) plane_store(keep, C, kt * 16, hi, lane);
+                    if (o)
+#pragma unroll
+                        for (int np = kt; np < 4; ++np) {
+                            Frag f;
+                            right_n(f, sP, C, np * 16, kt * 16, lane);
+                            mma(x[2 * np], hi, f[0], f[1]);
+                            mma(x[2 * np + 1], hi, f[2], f[3]);
+                        }
+                }
+                if (scales && lane == 0) scales[2] = us.back;
+                if (o) {  // scale c(i, 0) Q S + P U
+                    const float back = us.back * back_P;
+#pragma unroll
+                    for (int nt = 0; nt < 8; ++nt) {
+                        const float2 past = factor(3, nt * 8 + q2);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[nt][e] = fmaf(ss.back * (e & 1 ? past.y : past.x), y[nt][e], back * x[nt][e]);
+                    }
+                    chain_store(y, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+                }
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[nt][e] *= back_u;
+            }
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt) {
+                const float2 left = factor(1, nt * 8 + q2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[nt][e] *= e & 1 ? left.y : left.x;
+            }
+            const Scale ls = scale_of(u);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) split_left(u[2 * kt], u[2 * kt + 1], ls.by, fh[kt], fl[kt]);
+            update(fh, fl, ls.back, sk, true);
+        } else {
+            // y = P^T dO;  R <- c(C, 0) R + scale Q^T c(i, 0) dO
+            Frag g[4];
+            float m = 0.0f, mp = 0.0f;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                ldm_t(g[kt], sx + kt * 16 * Sh::kPitch);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 past = factor(3, kt * 16 + (i >> 1) * 8 + q2);
+                    const float g0 = fabsf(low(g[kt][i])), g1 = fabsf(high(g[kt][i]));
+                    m = fmaxf(m, fmaxf(g0, g1));
+                    mp = fmaxf(mp, fmaxf(g0 * fabsf(past.x), g1 * fabsf(past.y)));
+                }
+            }
+            const Scale gs = scale_of(warp_max(m)), ps = scale_of(warp_max(mp));
+            if (scales && lane == 0) scales[4] = gs.back;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                Frag gf;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 past = factor(3, kt * 16 + (i >> 1) * 8 + q2);
+                    const float g0 = low(g[kt][i]), g1 = high(g[kt][i]);
+                    gf[i] = pack(gs.by * g0, gs.by * g1);
+                    split(ps.by * (past.x * g0), ps.by * (past.y * g1), fh[kt][i], fl[kt][i]);
+                }
+#pragma unroll
+                for (int np = 0; np <= kt; ++np) {
+                    Frag f;
+                    right_k(f, sP, C, kt * 16, np * 16, lane);
+                    mma(y[2 * np], gf, f[0], f[1]);
+                    mma(y[2 * np + 1], gf, f[2], f[3]);
+                    right_k(f, sP + kTileB, C, kt * 16, np * 16, lane);
+                    mma(y[2 * np], gf, f[0], f[1]);
+                    mma(y[2 * np + 1], gf, f[2], f[3]);
+                }
+            }
+            update(fh, fl, ps.back, sq, true);
+            // x = c(C, j) K R + P^T dO;  X = T^T x
+            const float back = gs.back * back_P;
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt) {
+                const float2 left = factor(1, nt * 8 + q2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[nt][e] = fmaf(ss.back * (e & 1 ? left.y : left.x), x[nt][e], back * y[nt][e]);
+                    y[nt][e] = 0.0f;
+                }
+            }
+            const Scale xs = scale_of(x);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                Frag hi, lo;
+                split_left(x[2 * kt], x[2 * kt + 1], xs.by, hi, lo);
+#pragma unroll
+                for (int np = 0; np <= kt; ++np) {
+                    Frag f;
+                    right_k(f, sT, C, kt * 16, np * 16, lane);
+                    mma(y[2 * np], hi, f[0], f[1]);
+                    mma(y[2 * np + 1], hi, f[2], f[3]);
+                    mma(y[2 * np], lo, f[0], f[1]);
+                    mma(y[2 * np + 1], lo, f[2], f[3]);
+                    right_k(f, sT + kTileB, C, kt * 16, np * 16, lane);
+                    mma(y[2 * np], hi, f[0], f[1]);
+                    mma(y[2 * np + 1], hi, f[2], f[3]);
+                }
+            }
+            // X's plane;  dV = b X;  R <- R - K^T b c(i, 0) X
+            const float back_x = xs.back * back_T;
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[nt][e] *= back_x;
+            const Scale us = scale_of(y);
+            if (scales && lane == 0) scales[3] = us.back;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                const Frag hi = {pack(us.by * y[2 * kt][0], us.by * y[2 * kt][1]), pack(us.by * y[2 * kt][2], us.by * y[2 * kt][3]),
+                                 pack(us.by * y[2 * kt + 1][0], us.by * y[2 * kt + 1][1]), pack(us.by * y[2 * kt + 1][2], us.by * y[2 * kt + 1][3])};
+                plane_store(keep, C, kt * 16, hi, lane);
+            }
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt) {
+                const float2 past = factor(0, nt * 8 + q2), beta = factor(2, nt * 8 + q2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[nt][e] *= e & 1 ? beta.y : beta.x;
+                    x[nt][e] = -(e & 1 ? past.y : past.x) * y[nt][e];
+                }
+            }
+            const Scale ws = scale_of(x);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) split_left(x[2 * kt], x[2 * kt + 1], ws.by, fh[kt], fl[kt]);
+            update(fh, fl, ws.back, sk, false);
+            chain_store(y, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+        }
+    }
+    float *last = REV ? a.dS0 : a.S1;
+    if (last)
+#pragma unroll
+        for (int nt = 0; nt < ND; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                int64_t at;
+                if (place(nt, e, at)) last[at] = S[nt][e];
+            }
+    if (o)  // rows behind the end, eight columns at a time
+        for (int64_t i = tid; i < (int64_t)(a.n - len) * NW * 2; i += NW * 32) {
+            const int c = col0 + (int)(i % (NW * 2)) * 8;
+            if (c < a.dv) *reinterpret_cast<uint4 *>(o + (len + i / (NW * 2)) * a.ot + c) = make_uint4(0, 0, 0, 0);
+        }
+}
+
+unsigned cdiv(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
+
+template <int DP, bool TERMS>
+cudaError_t prepare(const DeltaArgs &a, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(k_delta_prepare<DP, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(PrepShared<DP>));
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("delta_prepare", (k_delta_prepare<DP, TERMS>), (unsigned)((int64_t)a.B * a.H * a.m), kPrepThreads, sizeof(PrepShared<DP>), s, a);
+    return cudaGetLastError();
+}
+
+template <int DP, int NW, bool REV>
+cudaError_t chain_launch(const DeltaArgs &a, cudaStream_t s) {
+    using Sh = ChainShared<DP, NW, REV>;
+    cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NW, REV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, NW * 16));
+    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NW, REV>), grid, NW * 32, sizeof(Sh), s, a);
+    return cudaGetLastError();
+}
+
+// Warps of a block: with few heads, few, so that the columns' chains spread over the SMs.
+template <int DP, bool REV>
+cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
+    const int64_t bh = (int64_t)a.B * a.H, sms = tc_sm_count();
+    if (a.dv > 64 && bh * cdiv(a.dv, 64) > sms) return chain_launch<DP, 8, REV>(a, s);
+    if (a.dv > 32 && bh * cdiv(a.dv, 32) > sms) return chain_launch<DP, 4, REV>(a, s);
+    return chain_launch<DP, 2, REV>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_grad_tc(const DeltaArgs &, luna_dtype, cudaStream_t) { return cudaErrorNotSupported; }
+
+cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s) {
+    if (a.d <= 64) return a.planes == 2 ? prepare<64, true>(a, s) : prepare<64, false>(a, s);
+    return a.planes == 2 ? prepare<128, true>(a, s) : prepare<128, false>(a, s);
+}
+
+cudaError_t launch_delta_chain(const DeltaArgs &a, bool reverse, cudaStream_t s) {
+    if (a.d <= 64) return reverse ? chain<64, true>(a, s) : chain<64, false>(a, s);
+    return reverse ? chain<128, true>(a, s) : chain<128, false>(a, s);
+}
+
+}  // namespace luna
