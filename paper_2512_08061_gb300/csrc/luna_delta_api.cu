@@ -229,13 +229,25 @@ luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, con
     a.dg = GateOut{dlog_decay, gg.b, gg.h, gg.t};
     a.db = GateOut{dbeta, gb.b, gb.h, gb.t};
 
-    cudaError_t e;
-    if ((e = launch_delta_rows(a, dd->io, false, s)) != cudaSuccess) return LUNA_ERR_CUDA;
+    const bool tc = tc_widths(dd) && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(a.go) && rows16(dV, gv) &&
+                    (shared || (rows16(dQ, gq) && rows16(dK, gk)));
+    cudaError_t e = cudaSuccess;
+    if (tc) {
+        tc_parts(a, p, ws, true);
+        e = launch_delta_prepare(a, s);
+        if (e == cudaSuccess) e = launch_delta_chain(a, false, s);
+    } else {
+        e = launch_delta_rows(a, dd->io, false, s);
+    }
+    if (e != cudaSuccess) return LUNA_ERR_CUDA;
     DeltaArgs r = a;
     r.o = dV; r.ob = gv.b; r.oh = gv.h; r.ot = gv.t;
     r.dS0 = dS0;
-    if ((e = launch_delta_rows(r, dd->io, true, s)) != cudaSuccess) return LUNA_ERR_CUDA;
-    if ((e = launch_delta_grad(a, dd->io, shared ? LUNA_F32 : dd->io, s)) != cudaSuccess) return LUNA_ERR_CUDA;
+    e = tc ? launch_delta_chain(r, true, s) : launch_delta_rows(r, dd->io, true, s);
+    if (e != cudaSuccess) return LUNA_ERR_CUDA;
+    const luna_dtype out = shared ? LUNA_F32 : dd->io;
+    e = tc ? launch_delta_grad_tc(a, out, s) : launch_delta_grad(a, dd->io, out, s);
+    if (e != cudaSuccess) return LUNA_ERR_CUDA;
     if (!shared) return LUNA_OK;
     e = launch_decay_group_sum(part_q, B, H, H / Hk, n, d, dQ, gq.b, gq.h, gq.t, dd->io, s);
     if (e != cudaSuccess) return LUNA_ERR_CUDA;

@@ -20,9 +20,9 @@
 // 128 columns, one block a head (32 blocks for a prompt of 32 heads, where this form has 128).
 // Precision.  Operands are fp16, scaled by powers of two: 11 bits where bf16 has 8, two terms 22.  The state, U and X
 // enter products in two terms, T and (in reverse) P too, so that states and U are off by a few 1e-7; the outputs take
-// one term of S, U and P (1.4e-4, under their own rounding).  Rows of K and Q are scaled to a largest value of 2^12 to
-// 2^13, T and P by chunk, what a warp holds by its largest value, so that whatever is 2^-15 of its neighbours still has
-// its 22 bits; K, Q and dO are exact down to 2^-26 of their row's or tile's largest value.  What a chunk adds to the
+// one term of S, U and P (1.4e-4, under their own rounding).  K, Q, T and P are scaled by chunk, to a largest value of
+// 2^12 to 2^13, what a warp holds by its own largest value, so that whatever is 2^-15 of its neighbours still has
+// its 22 bits; K, Q and dO are exact down to 2^-26 of their tile's largest value.  What a chunk adds to the
 // state is summed by itself and added in fp32, because the tensor cores cut sums off.
 #include <cuda_fp16.h>
 #include <math.h>
@@ -61,10 +61,10 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const __nv_bfloat16 *src
         copy16(tile_at(dst, C, r, p), in ? src + r * st + p * 8 : src, in);
     }
 }
-// a tile of 64 rows of W columns that lie one behind the other
+// a tile of `rows` rows of W columns that lie one behind the other
 template <int W>
-__device__ __forceinline__ void load_plane(uint32_t dst, const __half *src, int tid, int threads) {
-    for (int i = tid; i < C * W / 8; i += threads) copy16(tile_at(dst, C, i / (W / 8), i % (W / 8)), src + i * 8, true);
+__device__ __forceinline__ void load_plane(uint32_t dst, const __half *src, int tid, int threads, int rows = C) {
+    for (int i = tid; i < rows * W / 8; i += threads) copy16(tile_at(dst, rows, i / (W / 8), i % (W / 8)), src + i * 8, true);
 }
 
 // ---- matrix instructions
@@ -171,41 +171,39 @@ __device__ __forceinline__ void zero(float (&c)[N][4]) {
 
 constexpr int kPrepThreads = 128, kLdA = C + 4;
 
-// What it leaves in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b, scale c(i, 0) 2^eq of its rows (2^ek, 2^eq: what
-// the rows of K and Q were scaled down by), then c(C, 0) in two terms and what T and P were scaled down by.
+// What it leaves in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b, scale c(i, 0) 2^eq of its rows, then c(C, 0) in
+// two terms and what T, P, K and Q were scaled down by (the last two are 2^ek and 2^eq).
 
 template <int DP>
 struct PrepShared {
     alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB];
     float A[C][kLdA], T[C][kLdA];
-    float hi[C], lo[C], past[C], left[C], b[C], ek[C], eq[C], most[2][kPrepThreads / 32];
+    float hi[C], lo[C], past[C], left[C], b[C], most[4][kPrepThreads / 32];
 };
 
-// The rows of a bf16 tile (two threads each) in fp16, scaled: to `out` (unless it is null); what they were scaled
-// down by to back[]
+// The largest value of a bf16 tile's row half, and the half in fp16
 template <int DP>
-__device__ __forceinline__ void prep_scale(uint32_t tile, __half *out, float *back, int tid) {
-    const int r = tid / 2, p0 = tid % 2 * (DP / 16);
-    uint4 w[DP / 16];
+__device__ __forceinline__ float prep_most(uint32_t tile, uint4 (&w)[DP / 16], int tid) {
     uint32_t most = 0;
 #pragma unroll
     for (int p = 0; p < DP / 16; ++p) {
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(tile_at(tile, C, r, p0 + p)));
+        const uint32_t at = tile_at(tile, C, tid / 2, tid % 2 * (DP / 16) + p);
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(at));
         const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, max((u[i] << 16) & 0x7fff0000u, u[i] & 0x7fff0000u));
     }
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    const Scale s = scale_of(__uint_as_float(most));
-    if (tid % 2 == 0) back[r] = s.back;
-    if (!out) return;
+    return __uint_as_float(most);
+}
+template <int DP>
+__device__ __forceinline__ void prep_write(const uint4 (&w)[DP / 16], float by, __half *out, int tid) {
 #pragma unroll
     for (int p = 0; p < DP / 16; ++p) {
         const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
         uint32_t f[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = pack(s.by * low(u[i]), s.by * high(u[i]));
-        *reinterpret_cast<uint4 *>(out + r * DP + (p0 + p) * 8) = make_uint4(f[0], f[1], f[2], f[3]);
+        for (int i = 0; i < 4; ++i) f[i] = pack(by * low(u[i]), by * high(u[i]));
+        *reinterpret_cast<uint4 *>(out + tid / 2 * DP + (tid % 2 * (DP / 16) + p) * 8) = make_uint4(f[0], f[1], f[2], f[3]);
     }
 }
 
@@ -246,11 +244,27 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
         sm.b[tid - 32] = tid - 32 < rows ? gate_at<__nv_bfloat16>(a.b, b, h, t0 + tid - 32) : 0.0f;
     copies_wait<0>();
     __syncthreads();
-    {  // one head of those that share queries and keys writes them
-        const bool writes = h % (a.H / a.k.heads) == 0;
-        const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-        prep_scale<DP>(sk, writes ? a.Kp + to * C * DP : nullptr, sm.ek, tid);
-        prep_scale<DP>(sq, writes ? a.Qp + to * C * DP : nullptr, sm.eq, tid);
+    auto most_of = [&](int which, float x) {  // to be read after a barrier
+        x = warp_max(x);
+        if (lane == 0) sm.most[which][warp] = x;
+    };
+    auto block_scale = [&](int which) {
+        const float *m = sm.most[which];
+        return scale_of(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+    };
+    Scale ks, qs;
+    {
+        uint4 wk[DP / 16], wq[DP / 16];
+        most_of(2, prep_most<DP>(sk, wk, tid));
+        most_of(3, prep_most<DP>(sq, wq, tid));
+        __syncthreads();
+        ks = block_scale(2);
+        qs = block_scale(3);
+        if (h % (a.H / a.k.heads) == 0) {  // one head of those that share queries and keys
+            const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+            prep_write<DP>(wk, ks.by, a.Kp + to * C * DP, tid);
+            prep_write<DP>(wq, qs.by, a.Qp + to * C * DP, tid);
+        }
     }
     float *rowf = a.rows + at * kRowsF;
 
@@ -292,13 +306,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
             *reinterpret_cast<float2 *>(&sm.A[i][j]) = make_float2(w[0], w[1]);
             *reinterpret_cast<float2 *>(&sm.T[i][j]) = make_float2(0.0f, 0.0f);
         }
-    most = warp_max(most);
-    if (lane == 0) sm.most[0][warp] = most;
+    most_of(0, most);
     __syncthreads();
-    auto block_scale = [&](int which) {
-        const float *m = sm.most[which];
-        return scale_of(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-    };
     const Scale ps = block_scale(0);
     __half *P = a.Pp + at * (TERMS ? 2 : 1) * C * C;
 #pragma unroll
@@ -312,14 +321,16 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
             if (TERMS) *reinterpret_cast<uint32_t *>(P + C * C + i * C + j) = lo;
         }
     if (tid < C) {
-        rowf[tid] = sm.past[tid] * sm.ek[tid];
-        rowf[C + tid] = sm.left[tid] * sm.ek[tid];
+        rowf[tid] = sm.past[tid] * ks.back;
+        rowf[C + tid] = sm.left[tid] * ks.back;
         rowf[2 * C + tid] = sm.b[tid];
-        rowf[3 * C + tid] = a.scale * sm.past[tid] * sm.eq[tid];
+        rowf[3 * C + tid] = a.scale * sm.past[tid] * qs.back;
     }
     if (tid == 0) {
         gate_terms(sm.hi[C - 1], rowf[4 * C], rowf[4 * C + 1]);
         rowf[4 * C + 3] = ps.back;
+        rowf[4 * C + 4] = ks.back;
+        rowf[4 * C + 5] = qs.back;
     }
     if (lane < 16) {
         float x[16];
@@ -352,8 +363,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
         x[i] = *reinterpret_cast<const float2 *>(&sm.T[p / (C / 2)][p % (C / 2) * 2]);
         most = fmaxf(most, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
     }
-    most = warp_max(most);
-    if (lane == 0) sm.most[1][warp] = most;
+    most_of(1, most);
     __syncthreads();
     const Scale ts = block_scale(1);
     if (tid == 0) rowf[4 * C + 2] = ts.back;
@@ -731,6 +741,375 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
         }
 }
 
+// ---------------------------------------------------------------------------
+// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X and states.  A block of eight warps a chunk:
+// four groups of 16 rows by two halves of the columns.  What is summed over the columns of the state comes 16 of them at
+// a time, with what those were scaled down by.
+
+constexpr int kGradThreads = 256;
+
+template <int DP, int DVT>
+struct GradShared {
+    alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], go[DVT / 64][kTileB], u[DVT * 128], x[DVT * 128];
+    alignas(128) char s[DVT * DP * 2], r[DVT * DP * 2], P[kTileB], W[kTileB];
+    float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales];
+    // of a row's two halves of the columns: q . dQ, k . Z without the rows' part, k . (what it wrote) without and with
+    // the rows' part, W . K K^T, x . v, b k . Z
+    float sums[7][2][C];
+    float most[2][kGradThreads / 32], total[kGradThreads / 32], read[C], wrote[C], wstate[C];
+};
+
+__device__ __forceinline__ float inverse2(float back) {  // of a power of two
+    return __uint_as_float((254u << 23) - __float_as_uint(back));
+}
+__device__ __forceinline__ float2 half_pair(uint32_t tile, int rows, int r, int c) {
+    uint32_t u;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(tile_at(tile, rows, r, c >> 3) + (c & 7) * 2));
+    __half2 h;
+    memcpy(&h, &u, 4);
+    return __half22float2(h);
+}
+
+template <int DP, int DVT, typename OUT>
+__global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
+    using Sh = GradShared<DP, DVT>;
+    extern __shared__ __align__(128) char raw[];
+    Sh &sm = *reinterpret_cast<Sh *>(raw);
+    using Acc = float[DP / 16][4];
+    constexpr int NT = DP / 16;  // n-tiles of a warp's half of the columns of dQ, dK
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 4 * 16, half = warp / 4, q2 = lane % 4 * 2;
+    const int64_t at = blockIdx.x, bh = at / a.m;
+    const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
+    const int rows = max(0, min(C, head_length(a.lengths, b, a.n) - t0)), out_rows = min(C, a.n - t0);
+    const int hk = h / (a.H / a.k.heads);
+    OUT *dq = static_cast<OUT *>(a.dq) + b * a.dqb + h * a.dqh + t0 * a.dqt;
+    OUT *dk = static_cast<OUT *>(a.dk) + b * a.dkb + h * a.dkh + t0 * a.dkt;
+    __nv_bfloat16 *dg = static_cast<__nv_bfloat16 *>(a.dg.p) + b * a.dg.sb + h * a.dg.sh + t0 * a.dg.st;
+    __nv_bfloat16 *db = static_cast<__nv_bfloat16 *>(a.db.p) + b * a.db.sb + h * a.db.sh + t0 * a.db.st;
+    for (int i = tid; i < (out_rows - rows) * a.d; i += kGradThreads) {
+        const int t = rows + i / a.d, c = i % a.d;
+        io_store(dq + t * a.dqt + c, 0.0f);
+        io_store(dk + t * a.dkt + c, 0.0f);
+    }
+    if (tid >= rows && tid < out_rows) {
+        io_store(dg + tid * a.dg.st, 0.0f);
+        io_store(db + tid * a.db.st, 0.0f);
+    }
+    if (rows == 0) return;
+
+    const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q), sgo = smem_u32(sm.go), su = smem_u32(sm.u), sx = smem_u32(sm.x);
+    const uint32_t ss = smem_u32(sm.s), sr = smem_u32(sm.r), sP = smem_u32(sm.P), sW = smem_u32(sm.W);
+    const int dvp = a.dvp, groups = dvp / 16;
+    const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+    load_plane<DP>(sk, a.Kp + kat * C * DP, tid, kGradThreads);
+    load_rows<DVT>(sgo, static_cast<const __nv_bfloat16 *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st, a.go.st, rows, a.dv, tid, kGradThreads);
+    load_plane<C>(su, a.Up + at * dvp * C, tid, kGradThreads, dvp);
+    load_plane<C>(sx, a.Xp + at * dvp * C, tid, kGradThreads, dvp);
+    copies_end();
+    load_plane<DP>(ss, a.Sp + at * dvp * DP, tid, kGradThreads, dvp);
+    load_plane<DP>(sr, a.Rp + at * dvp * DP, tid, kGradThreads, dvp);
+    load_plane<DP>(sq, a.Qp + kat * C * DP, tid, kGradThreads);
+    copies_end();
+    const float *rowf = a.rows + at * kRowsF;
+    const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
+    if (warp == 0)
+        delta_gate_sums(lane, [&](int t) { return t < rows ? gate_at<__nv_bfloat16>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
+                        sm.past, sm.left);
+    else if (warp < 3)
+        sm.b[tid - 32] = rowf[2 * C + tid - 32];
+    for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[at * groups * kDeltaScales + i];
+    copies_wait<1>();
+    __syncthreads();
+
+    // 16 rows and 16 columns of dO in fp16
+    auto left_go = [&](Frag &f, int kt) {
+        left_m(f, sgo, C, r0, kt * 16, lane);
+        const float by = inverse2(sm.scales[kt][4]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = pack(by * low(f[i]), by * high(f[i]));
+    };
+    // sums over the four lanes of a row, for this half of the columns: rows lane / 4 and 8 more
+    auto row_sums = [&](float (&x)[2], int which) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x[i] += __shfl_xor_sync(0xffffffffu, x[i], 1);
+            x[i] += __shfl_xor_sync(0xffffffffu, x[i], 2);
+        }
+        if (lane % 4 == 0) {
+            sm.sums[which][half][r0 + lane / 4] = x[0];
+            sm.sums[which][half][r0 + lane / 4 + 8] = x[1];
+        }
+    };
+
+    {  // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 32 columns a warp; W . K K^T for db
+        float p[4][4], w[4][4], kk[4][4];
+        zero(p);
+        zero(w);
+        zero(kk);
+#pragma unroll 2
+        for (int kt = 0; kt < groups; ++kt) {
+            Frag fg, fx;
+            left_go(fg, kt);
+            left_k(fx, sx, dvp, kt * 16, r0, lane);
+            const float pb = sm.scales[kt][4] * sm.scales[kt][2], wb = sm.scales[kt][3] * sm.scales[kt][2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int n0 = half * 32 + n * 16;
+                if (n0 > r0) continue;
+                Frag f;
+                right_k(f, su, dvp, kt * 16, n0, lane);
+                float c[4][4];
+                zero(c);
+                mma(c[0], fg, f[0], f[1]);
+                mma(c[1], fg, f[2], f[3]);
+                mma(c[2], fx, f[0], f[1]);
+                mma(c[3], fx, f[2], f[3]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[2 * n + i][e] = fmaf(pb, c[i][e], p[2 * n + i][e]);
+                        w[2 * n + i][e] = fmaf(wb, c[2 + i][e], w[2 * n + i][e]);
+                    }
+            }
+        }
+#pragma unroll
+        for (int k0 = 0; k0 < DP; k0 += 16) {
+            Frag fk;
+            left_m(fk, sk, C, r0, k0, lane);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int n0 = half * 32 + n * 16;
+                if (n0 > r0) continue;
+                Frag f;
+                right_n(f, sk, C, n0, k0, lane);
+                mma(kk[2 * n], fk, f[0], f[1]);
+                mma(kk[2 * n + 1], fk, f[2], f[3]);
+            }
+        }
+        float dot[2] = {0.0f, 0.0f}, mp = 0.0f, mw = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = r0 + lane / 4 + (e >> 1) * 8, j = half * 32 + nt * 8 + q2 + (e & 1);
+                const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
+                p[nt][e] = j <= i ? a.scale * c * p[nt][e] : 0.0f;
+                w[nt][e] = j < i ? c * w[nt][e] : 0.0f;
+                if (j < i) dot[e >> 1] = fmaf(w[nt][e], kk[nt][e], dot[e >> 1]);
+                w[nt][e] *= sm.b[i];
+                mp = fmaxf(mp, fabsf(p[nt][e]));
+                mw = fmaxf(mw, fabsf(w[nt][e]));
+            }
+        row_sums(dot, 4);
+        mp = warp_max(mp);
+        mw = warp_max(mw);
+        if (lane == 0) {
+            sm.most[0][warp] = mp;
+            sm.most[1][warp] = mw;
+        }
+        copies_wait<0>();
+        __syncthreads();
+        mp = mw = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kGradThreads / 32; ++i) {
+            mp = fmaxf(mp, sm.most[0][i]);
+            mw = fmaxf(mw, sm.most[1][i]);
+        }
+        const float bp = scale_of(mp).by, bw = scale_of(mw).by;
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, half * 4 + nt) + q2 * 2;
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(bp * p[nt][e], bp * p[nt][e + 1])) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(bw * w[nt][e], bw * w[nt][e + 1])) : "memory");
+            }
+    }
+    // x . v: a thread a row and a quarter of the columns (joined two and two)
+    {
+        const int i = tid % C, part = tid / C;
+        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
+        float acc = 0.0f;
+        if (i < rows)
+            for (int c8 = part; c8 < a.dv / 8; c8 += 4) {
+                const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
+                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    unsigned short u;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
+                    sum = fmaf(e & 1 ? high(w[e / 2]) : low(w[e / 2]), __half2float(__ushort_as_half(u)), sum);
+                }
+                acc = fmaf(sm.scales[c8 / 2][3], sum, acc);
+            }
+        // (the two quarters of a sums[5] entry meet in two steps)
+        if (part >= 2) sm.sums[5][part - 2][i] = acc;
+        __syncthreads();
+        if (part < 2) sm.sums[5][part][i] += acc;
+    }
+    float back_p = 0.0f, back_w = 0.0f;
+    {
+        float mp = 0.0f, mw = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kGradThreads / 32; ++i) {
+            mp = fmaxf(mp, sm.most[0][i]);
+            mw = fmaxf(mw, sm.most[1][i]);
+        }
+        back_p = scale_of(mp).back;
+        back_w = scale_of(mw).back;
+    }
+
+    const int c0 = half * (DP / 2);  // first column of the warp's
+    const int ra = r0 + lane / 4, rb = ra + 8;
+    // acc += F M over the columns of the state: F by left(f, kt), M a tile of S or R, scaled down by back(kt)
+    auto over_columns = [&](Acc &acc, uint32_t tile, auto left, auto back) {
+#pragma unroll 2
+        for (int kt = 0; kt < groups; ++kt) {
+            Frag fl;
+            left(fl, kt);
+            const float s = back(kt);
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                right_k(f, tile, dvp, kt * 16, c0 + np * 16, lane);
+                float c[2][4];
+                zero(c);
+                mma(c[0], fl, f[0], f[1]);
+                mma(c[1], fl, f[2], f[3]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[2 * np + i][e] = fmaf(s, c[i][e], acc[2 * np + i][e]);
+            }
+        }
+    };
+    // acc += by F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q
+    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, float by) {
+        Frag fl[4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            if (trans)
+                left_k(fl[kt], from, C, kt * 16, r0, lane);
+            else
+                left_m(fl[kt], from, C, r0, kt * 16, lane);
+        }
+#pragma unroll
+        for (int np = 0; np < NT / 2; ++np) {
+            float c[2][4];
+            zero(c);
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                if (trans ? kt * 16 < r0 : kt * 16 > r0) continue;
+                Frag f;
+                right_k(f, tile, C, kt * 16, c0 + np * 16, lane);
+                mma(c[0], fl[kt], f[0], f[1]);
+                mma(c[1], fl[kt], f[2], f[3]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[2 * np + i][e] = fmaf(by, c[i][e], acc[2 * np + i][e]);
+        }
+    };
+    auto times_rows = [&](Acc &acc, float fa, float fb) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[nt][e] *= e & 2 ? fb : fa;
+    };
+    // sums of the rows with those of the tile of K or Q
+    auto dot_rows = [&](const Acc &acc, uint32_t tile, float back, int which) {
+        float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float2 x = half_pair(tile, C, ra, c0 + nt * 8 + q2), y = half_pair(tile, C, rb, c0 + nt * 8 + q2);
+            dot[0] = fmaf(x.x, acc[nt][0], fmaf(x.y, acc[nt][1], dot[0]));
+            dot[1] = fmaf(y.x, acc[nt][2], fmaf(y.y, acc[nt][3], dot[1]));
+        }
+        dot[0] *= back;
+        dot[1] *= back;
+        row_sums(dot, which);
+    };
+    auto store_rows = [&](const Acc &acc, OUT *out, int64_t st) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int c = c0 + nt * 8 + q2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = i ? rb : ra;
+                if (r >= rows || c >= a.d) continue;
+                if (sizeof(OUT) == 2)
+                    *reinterpret_cast<uint32_t *>(out + r * st + c) = pack_bf16(acc[nt][2 * i], acc[nt][2 * i + 1]);
+                else
+                    *reinterpret_cast<float2 *>(out + r * st + c) = make_float2(acc[nt][2 * i], acc[nt][2 * i + 1]);
+            }
+        }
+    };
+
+    Acc acc, z;
+    zero(acc);
+    over_columns(acc, ss, left_go, [&](int kt) { return sm.scales[kt][4] * sm.scales[kt][0]; });
+    times_rows(acc, a.scale * sm.past[ra], a.scale * sm.past[rb]);
+    over_rows(acc, sP, false, sk, back_p * back_k);
+    dot_rows(acc, sq, back_q, 0);
+    store_rows(acc, dq, a.dqt);
+
+    zero(z);
+    over_columns(z, ss, [&](Frag &f, int kt) { left_k(f, sx, dvp, kt * 16, r0, lane); }, [&](int kt) { return sm.scales[kt][3] * sm.scales[kt][0]; });
+    times_rows(z, sm.past[ra], sm.past[rb]);
+    dot_rows(z, sk, back_k, 1);  // (for db, without b and the rows' part)
+    times_rows(z, sm.b[ra], sm.b[rb]);
+    over_rows(z, sW, false, sk, back_w * back_k);
+    dot_rows(z, sk, back_k, 6);
+
+    zero(acc);
+    over_columns(acc, sr, [&](Frag &f, int kt) { left_k(f, su, dvp, kt * 16, r0, lane); }, [&](int kt) { return sm.scales[kt][2] * sm.scales[kt][1]; });
+    times_rows(acc, sm.left[ra], sm.left[rb]);
+    dot_rows(acc, sk, back_k, 2);
+    over_rows(acc, sP, true, sq, back_p * back_q);
+    over_rows(acc, sW, true, sk, -back_w * back_k);
+    dot_rows(acc, sk, back_k, 3);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[nt][e] -= z[nt][e];
+    store_rows(acc, dk, a.dkt);
+
+    // <S, R>
+    float total = 0.0f;
+    for (int i = tid; i < dvp * (DP / 8); i += kGradThreads) {
+        const int r = i / (DP / 8), p = i % (DP / 8);
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float2 x = half_pair(ss, dvp, r, p * 8 + e), y = half_pair(sr, dvp, r, p * 8 + e);
+            sum = fmaf(x.x, y.x, fmaf(x.y, y.y, sum));
+        }
+        total = fmaf(sm.scales[r / 16][0] * sm.scales[r / 16][1], sum, total);
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) total += __shfl_xor_sync(0xffffffffu, total, w);
+    if (lane == 0) sm.total[warp] = total;
+    __syncthreads();
+    if (tid < rows) {
+        auto sum = [&](int which) { return sm.sums[which][0][tid] + sm.sums[which][1][tid]; };
+        io_store(db + tid * a.db.st, sum(5) - sum(1) - back_k * back_k * sum(4));
+        sm.read[tid] = sum(0) - sum(6);
+        sm.wrote[tid] = sum(3);
+        sm.wstate[tid] = sum(2);
+    }
+    __syncthreads();
+    if (warp == 0) {
+        total = 0.0f;
+        for (int w = 0; w < kGradThreads / 32; ++w) total += sm.total[w];
+        delta_gate_grads(total * sm.past[C - 1], sm.read, sm.wrote, sm.wstate, rows, lane, [&](int t, float x) {
+            io_store(dg + t * a.dg.st, expf(gate_at<__nv_bfloat16>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
+        });
+    }
+}
+
 unsigned cdiv(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
 
 template <int DP, bool TERMS>
@@ -762,7 +1141,24 @@ cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_delta_grad_tc(const DeltaArgs &, luna_dtype, cudaStream_t) { return cudaErrorNotSupported; }
+template <int DP, int DVT, typename OUT>
+static cudaError_t grad_launch(const DeltaArgs &a, cudaStream_t s) {
+    using Sh = GradShared<DP, DVT>;
+    cudaError_t e = cudaFuncSetAttribute(k_delta_grad_tc<DP, DVT, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("delta_grad_tc", (k_delta_grad_tc<DP, DVT, OUT>), (unsigned)((int64_t)a.B * a.H * a.m), kGradThreads, sizeof(Sh), s, a);
+    return cudaGetLastError();
+}
+
+template <typename OUT>
+static cudaError_t grad(const DeltaArgs &a, cudaStream_t s) {
+    if (a.d <= 64) return a.dv <= 64 ? grad_launch<64, 64, OUT>(a, s) : grad_launch<64, 128, OUT>(a, s);
+    return a.dv <= 64 ? grad_launch<128, 64, OUT>(a, s) : grad_launch<128, 128, OUT>(a, s);
+}
+
+cudaError_t launch_delta_grad_tc(const DeltaArgs &a, luna_dtype out, cudaStream_t s) {
+    return out == LUNA_F32 ? grad<float>(a, s) : grad<__nv_bfloat16>(a, s);
+}
 
 cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s) {
     if (a.d <= 64) return a.planes == 2 ? prepare<64, true>(a, s) : prepare<64, false>(a, s);
