@@ -12,8 +12,8 @@ int tc_sm_count();
 namespace {
 
 constexpr int kMaxBeams = 32;                  // a warp's lanes
-constexpr int kThreads = 256, kPer = 32;       // values of a piece that a thread holds
-constexpr int kPiece = kThreads * kPer;
+constexpr int kThreads = 256;
+constexpr int kPer = 32, kFew = 8;             // values of a piece that a thread holds, many rows or few
 
 // Values as integers in the same order; larger is better.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -64,8 +64,9 @@ __device__ int place_in_block(Key &key, Key *list) {
     list[threadIdx.x] = key;
     __syncthreads();
     int place = lane;
-    for (int o = 0; o < kThreads / 32; ++o) {
-        if (o == warp) continue;
+#pragma unroll
+    for (int i = 1; i < kThreads / 32; ++i) {
+        const int o = (warp + i) % (kThreads / 32);
         const Key *l = list + 32 * o;
         auto before = [&](const Key &x) { return o < warp ? !key.over(x) : x.over(key); };
         int n = 0;
@@ -96,6 +97,14 @@ __device__ void best_of(const Key *from, int count, Key *best, int have, int K, 
     __syncthreads();
 }
 
+// 2^x to 2^-22 of itself
+__device__ __forceinline__ float power2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
 struct BeamArgs {
     const void *logits;
     int64_t ld;
@@ -109,14 +118,15 @@ struct BeamArgs {
     float2 *stats;        // [B K][S]: maximum, sum of exp over it
 };
 
-// One part of one row: its maximum, its sum of exponentials and its K best values, in one reading.  A thread holds 32
-// values of a piece of 8192; only values that reach the K-th best of the threads' maxima (there are K as good) and the
-// K-th best so far are looked at again, so that of a piece a few dozen are sorted, at most 32 K.  Bound by the bytes
-// of the logits.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
-    constexpr int VEC = 16 / sizeof(T), NV = kPer / VEC;
-    __shared__ RowKey list[kThreads], best[kMaxBeams], pool[kMaxBeams * kPer], least;
+// One part of one row: its maximum, its sum of exponentials and its K best values, in one reading.  A thread holds PER
+// values of a piece of 256 PER; only values that reach the K-th best so far or the K-th best of the threads' largest
+// (there are K as good) are looked at again, so that of a piece a few dozen are sorted: those of at most K threads.
+// Few rows come in pieces of 2048 values, so that more SMs share them.  Bound by the bytes of the logits where there are
+// many rows, else by the chain of one piece.
+template <typename T, int PER>
+__global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
+    constexpr int VEC = 16 / sizeof(T), NV = PER / VEC, PIECE = kThreads * PER;
+    __shared__ RowKey list[kThreads], best[kMaxBeams], pool[kMaxBeams * PER], least;
     __shared__ int count;
     __shared__ float smax[kThreads / 32], ssum[kThreads / 32];
     const int tid = threadIdx.x, row = blockIdx.y, part = blockIdx.x;
@@ -124,14 +134,13 @@ __global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
     // vectors that start on 16-byte boundaries: the first may begin before the row
     const int off = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));
-    const int vectors = (a.V + off + VEC - 1) / VEC, pieces = (vectors + kPiece / VEC - 1) / (kPiece / VEC);
+    const int vectors = (a.V + off + VEC - 1) / VEC, pieces = (vectors + PIECE / VEC - 1) / (PIECE / VEC);
     const int first = (int)((int64_t)pieces * part / a.S), last = (int)((int64_t)pieces * (part + 1) / a.S);
-    const float log2e = 1.4426950408889634f;
     float top = -INFINITY, sum = 0.0f;
-    int have = 0;
+    bool have = false;
     for (int piece = first; piece < last; ++piece) {
-        float val[kPer];
-        const int v0 = piece * (kPiece / VEC) + tid;  // vectors of a thread: every 256th
+        float val[PER];
+        const int v0 = piece * (PIECE / VEC) + tid;  // vectors of a thread: every 256th
         auto token = [&](int i) { return (v0 + i / VEC * kThreads) * VEC - off + i % VEC; };
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -150,40 +159,51 @@ __global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
         }
         float m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) m = fmaxf(m, val[i]);
-        const float now = fmaxf(top, m), base = now == -INFINITY ? 0.0f : now;
-        sum *= exp2f((top - base) * log2e);
+        for (int i = 0; i < PER; ++i) m = fmaxf(m, val[i]);
+        const float now = fmaxf(top, m), shift = now == -INFINITY ? 0.0f : now;
+        sum *= power2((top - shift) * kLog2e);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += exp2f((val[i] - base) * log2e);
+        for (int i = 0; i < PER; ++i) sum += power2((val[i] - shift) * kLog2e);
         top = now;
+        // a value's key, or none: behind the row's ends, or a NaN (k_beam_join sees by the sum that such a row has no scores)
         auto key = [&](int i) {
             const int t = token(i);
             RowKey k;
-            if (t >= 0 && t < a.V && val[i] == val[i])  // (a row with a NaN has no scores; k_beam_join sees that by its sum)
-                k.v = (uint64_t)ordered(val[i] + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
+            if (t >= 0 && t < a.V && val[i] == val[i]) k.v = (uint64_t)ordered(val[i] + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
             return k;
         };
-        // the thread's best: the first of its largest (tokens rise with i)
-        RowKey mine;
-#pragma unroll
-        for (int i = kPer - 1; i >= 0; --i)
-            if (val[i] == m) mine = key(i).over(mine) ? key(i) : mine;
         const RowKey bar = have ? best[a.K - 1] : RowKey{};  // (none while fewer than K are found: v = 0)
-        if (__syncthreads_count(mine.over(bar)) == 0) continue;
-        RowKey k = mine;
-        const int place = place_in_block(k, list);
-        if (place == a.K - 1) least = k;
+        RowKey need = bar;
+        const float floor = bar.v ? unordered((uint32_t)(bar.v >> 32)) : -INFINITY;
+        const int hits = __syncthreads_count(m >= floor);
+        if (have && hits == 0) continue;
+        if (!have || hits > a.K) {
+            RowKey k;  // the thread's best: the first of its largest (tokens rise with i)
+#pragma unroll
+            for (int i = PER - 1; i >= 0; --i)
+                if (val[i] == m) {
+                    const RowKey c = key(i);
+                    if (c.v) k = c;
+                }
+            const int place = place_in_block(k, list);
+            if (place == a.K - 1) least = k;
+            __syncthreads();
+            if (!bar.over(least)) need = least;
+        }
         if (tid == 0) count = 0;
         __syncthreads();
-        const RowKey need = least;
+        const float lowest = need.v ? unordered((uint32_t)(need.v >> 32)) : -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const RowKey c = key(i);
-            if (c.v && !need.over(c) && c.over(bar)) pool[atomicAdd(&count, 1)] = c;
-        }
+        for (int i = 0; i < PER; ++i)
+            if (val[i] >= lowest) {
+                const RowKey c = key(i);
+                if (c.v && !need.over(c) && c.over(bar)) pool[atomicAdd(&count, 1)] = c;
+            }
         __syncthreads();
-        best_of(pool, count, best, have, a.K, list);
-        have = a.K;
+        const int found = count;
+        if (have && found == 0) continue;
+        best_of(pool, found, best, have ? a.K : 0, a.K, list);
+        have = true;
     }
     if (!have) {  // (fewer pieces than parts)
         if (tid < a.K) best[tid] = RowKey{};
@@ -194,8 +214,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
     float m = top;
 #pragma unroll
     for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
-    const float mb = m == -INFINITY ? 0.0f : m;
-    float s = sum * exp2f((top - mb) * log2e);
+    float s = sum * power2((top - (m == -INFINITY ? 0.0f : m)) * kLog2e);
 #pragma unroll
     for (int w = 16; w > 0; w /= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
     if (tid % 32 == 0) { smax[tid / 32] = m; ssum[tid / 32] = s; }
@@ -205,70 +224,85 @@ __global__ void __launch_bounds__(kThreads) k_beam_rows(BeamArgs a) {
         m = smax[0];
         for (int w = 1; w < kThreads / 32; ++w) m = fmaxf(m, smax[w]);
         const float b = m == -INFINITY ? 0.0f : m;
-        for (int w = 0; w < kThreads / 32; ++w) all += ssum[w] * exp2f((smax[w] - b) * log2e);
+        for (int w = 0; w < kThreads / 32; ++w) all += ssum[w] * power2((smax[w] - b) * kLog2e);
         a.stats[at] = make_float2(m, all);
     }
 }
 
 // The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that which of two near ones is better
-// does not hang on a rounding.  One block a sequence: K S K candidates, looked at twice as in k_beam_rows.
+// does not hang on a rounding: 64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once
+// and a candidate costs one sum (exponentials and logarithms by a warp a row took 16 to 37 us).  One block a sequence:
+// K S K candidates, looked at twice as in k_beam_rows.
+constexpr int kHeld = 4;  // candidates that a thread keeps from the first look
+
 __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
     extern __shared__ char raw[];
     SeqKey *pool = reinterpret_cast<SeqKey *>(raw);
     __shared__ SeqKey list[kThreads], best[kMaxBeams], least;
-    __shared__ double base[kMaxBeams];
-    __shared__ float score[kMaxBeams];
-    __shared__ uint8_t done[kMaxBeams];
+    __shared__ double base[kMaxBeams];  // score - log sum exp(logit - most)
+    __shared__ float score[kMaxBeams], most[kMaxBeams], sums[kMaxBeams];
+    __shared__ uint8_t done[kMaxBeams], dead[kMaxBeams];  // dead: no candidate of its has a score
     __shared__ int count;
     const int tid = threadIdx.x, b = blockIdx.x, K = a.K, S = a.S;
     for (int k = tid / 32; k < K; k += kThreads / 32) {  // a warp a row
         const int row = b * K + k, lane = tid % 32;
         const bool over = a.done && a.done[row];
-        float m = -INFINITY;
-        double sum = 0.0;
+        float m = -INFINITY, sum = 0.0f;
         if (!over) {
             for (int s = lane; s < S; s += 32) m = fmaxf(m, a.stats[(int64_t)row * S + s].x);
 #pragma unroll
             for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
             for (int s = lane; s < S; s += 32) {
                 const float2 p = a.stats[(int64_t)row * S + s];
-                sum += p.x == -INFINITY && p.y == 0.0f ? 0.0 : (double)p.y * exp((double)p.x - (double)m);
+                sum += p.x == -INFINITY ? p.y : p.y * power2((p.x - m) * kLog2e);
             }
 #pragma unroll
             for (int w = 16; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         }
         if (lane == 0) {
-            score[k] = a.scores[row];
             done[k] = over;
-            base[k] = over ? 0.0 : (double)score[k] - ((double)m + log(sum));
+            score[k] = a.scores[row];
+            most[k] = m;
+            sums[k] = sum;
         }
     }
     if (tid == 0) count = 0;
+    __syncthreads();
+    if (tid < K) {
+        const double x = (double)score[tid] - log((double)sums[tid]);
+        base[tid] = x;
+        dead[tid] = !done[tid] && !(isfinite(x) && isfinite(most[tid]));
+    }
     __syncthreads();
     const int N = K * S * K;
     auto candidate = [&](int n) {
         const int k = n / (S * K), j = n - k * (S * K);
         SeqKey c;
-        double v = -INFINITY;
         int token;
-        if (done[k] || !isfinite(base[k])) {
+        if (done[k] || dead[k]) {
             // an ended beam goes on as itself; what no score can be given to comes behind everything, by its place
             if (j >= K) return c;
             token = done[k] ? (j == 0 ? a.end : j - (j <= a.end)) : j;
             if (token >= a.V) return c;
-            if (done[k] && j == 0 && !(score[k] != score[k])) v = (double)score[k];
+            c.v = ordered(done[k] && j == 0 && score[k] == score[k] ? (double)(score[k] + 0.0f) : -(double)INFINITY);
         } else {
             const uint64_t key = a.keys[(int64_t)b * N + n];
             if (!key) return c;
             token = (int)~(uint32_t)key;
-            v = base[k] + (double)unordered((uint32_t)(key >> 32));
+            // (the largest logit comes off first: a row may be masked by its type's lowest value throughout)
+            const double v = base[k] + ((double)unordered((uint32_t)(key >> 32)) - (double)most[k]);
+            c.v = __double_as_longlong(v) << 1 == 0 ? uint64_t(1) << 63 : ordered(v);  // (-0 is 0)
         }
-        c.v = ordered(v + 0.0);
         c.i = ~(uint32_t)(k * a.V + token);
         return c;
     };
-    SeqKey mine;
-    for (int n = tid; n < N; n += kThreads) {
+    SeqKey mine, held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        if (tid + i * kThreads < N) held[i] = candidate(tid + i * kThreads);
+        if (held[i].over(mine)) mine = held[i];
+    }
+    for (int n = tid + kHeld * kThreads; n < N; n += kThreads) {
         const SeqKey c = candidate(n);
         if (c.over(mine)) mine = c;
     }
@@ -276,7 +310,10 @@ __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
     if (place == K - 1) least = mine;
     __syncthreads();
     const SeqKey need = least;
-    for (int n = tid; n < N; n += kThreads) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if (held[i].v && !need.over(held[i])) pool[atomicAdd(&count, 1)] = held[i];
+    for (int n = tid + kHeld * kThreads; n < N; n += kThreads) {
         const SeqKey c = candidate(n);
         if (c.v && !need.over(c)) pool[atomicAdd(&count, 1)] = c;
     }
@@ -354,14 +391,20 @@ luna_status check(const luna_beam_desc *bd) {
     return LUNA_OK;
 }
 
-// Parts of a row: enough blocks for eight on every SM, a piece of 8192 values at least for each.
-int parts(const luna_beam_desc *bd) {
-    const int64_t rows = (int64_t)bd->B * bd->K, pieces = cdiv((int64_t)bd->V + 8, kPiece);
-    return (int)std::max<int64_t>(1, std::min(pieces, cdiv((int64_t)8 * tc_sm_count(), std::max<int64_t>(rows, 1))));
+// How rows are cut: the values that a thread holds of a piece, and the parts of a row.  Many rows: pieces of 8192 values
+// and as many blocks as the SMs hold at four each; few, which pieces of 8192 leave most SMs without: pieces of 2048.
+struct Cut {
+    int per, parts;
+};
+Cut cut(const luna_beam_desc *bd) {
+    const int64_t rows = std::max<int64_t>(1, (int64_t)bd->B * bd->K), sms = tc_sm_count(), V = (int64_t)bd->V + 8;
+    const int per = rows * cdiv(V, kThreads * kPer) < sms ? kFew : kPer;
+    const int64_t most = std::max<int64_t>(1, 4 * sms / rows);
+    return Cut{per, (int)std::min(cdiv(V, kThreads * per), most)};
 }
 
 size_t workspace(const luna_beam_desc *bd) {
-    const int64_t rows = (int64_t)bd->B * bd->K, S = parts(bd);
+    const int64_t rows = (int64_t)bd->B * bd->K, S = cut(bd).parts;
     return (size_t)(256 + align256(rows * S * bd->K * 8) + align256(rows * S * 8));
 }
 
@@ -391,15 +434,22 @@ luna_status luna_beam_select(const luna_beam_desc *bd, const void *logits, const
         return LUNA_ERR_INVALID_ARG;
     if (ws_bytes < workspace(bd)) return LUNA_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const Cut how = cut(bd);
     BeamArgs a{logits, bd->ld ? bd->ld : bd->V, scores, done, scores_out, tokens, parents, done_out,
-               bd->B, bd->K, bd->V, bd->end, parts(bd)};
+               bd->B, bd->K, bd->V, bd->end, how.parts};
     a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + 256);
     a.stats = reinterpret_cast<float2 *>(static_cast<char *>(ws) + 256 + align256((int64_t)bd->B * bd->K * a.S * bd->K * 8));
     const dim3 grid((unsigned)a.S, (unsigned)(bd->B * bd->K));
-    if (bd->io == LUNA_F32)
-        LUNA_LAUNCH("beam_rows", k_beam_rows<float>, grid, kThreads, 0, s, a);
-    else
-        LUNA_LAUNCH("beam_rows", k_beam_rows<__nv_bfloat16>, grid, kThreads, 0, s, a);
+    if (bd->io == LUNA_F32) {
+        if (how.per == kFew)
+            LUNA_LAUNCH("beam_rows", (k_beam_rows<float, kFew>), grid, kThreads, 0, s, a);
+        else
+            LUNA_LAUNCH("beam_rows", (k_beam_rows<float, kPer>), grid, kThreads, 0, s, a);
+    } else if (how.per == kFew) {
+        LUNA_LAUNCH("beam_rows", (k_beam_rows<__nv_bfloat16, kFew>), grid, kThreads, 0, s, a);
+    } else {
+        LUNA_LAUNCH("beam_rows", (k_beam_rows<__nv_bfloat16, kPer>), grid, kThreads, 0, s, a);
+    }
     // at most K threads hold a candidate that reaches the K-th best of the threads' maxima
     const size_t pool = sizeof(SeqKey) * bd->K * (size_t)cdiv((int64_t)bd->K * a.S * bd->K, kThreads);
     if (cudaFuncSetAttribute(k_beam_join, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pool) != cudaSuccess)

@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(kRowThreads) k_delta_rows(DeltaArgs a) {
     const float *init = REV ? a.dS1 : a.S0;
     float *last = REV ? a.dS0 : a.S1;
 
+    if (!REV && bh == 0 && blockIdx.y == 0 && tid == 0) *a.status = 0;  // (the call's first kernel; none of this form sets it)
     float s[JD][4], fade = 1.0f, fade2 = 0.0f;  // (reverse) the decay of the row before is still to be applied
     auto row = [&](int j, int e) { return j * 32 + p * 4 + e; };
     auto keep = [&](float *to) {

@@ -63,6 +63,7 @@ struct DeltaArgs {
     __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Sp, *Rp;
     float *rows, *scales;
     int planes, dvp;
+    int *status;            // the call's status word
 };
 
 struct DeltaStep {

@@ -117,8 +117,9 @@ GateView gate(const void *p, const luna_strides &s) { return GateView{p, s.b, s.
 
 // What all passes of a call share.
 DeltaArgs base(const luna_delta_desc *dd, const Plan &p, const void *g, const void *beta, const void *Q, const void *K,
-               const void *V, const int32_t *lengths) {
+               const void *V, const int32_t *lengths, void *ws) {
     DeltaArgs a{};
+    a.status = static_cast<int *>(ws);
     a.q = view(Q, filled(dd->q, dd->Hk, dd->n, dd->d), dd->Hk);
     a.k = view(K, filled(dd->k, dd->Hk, dd->n, dd->d), dd->Hk);
     a.v = view(V, filled(dd->v, dd->H, dd->n, dd->dv), dd->H);
@@ -172,7 +173,7 @@ luna_status luna_delta_fwd(const luna_delta_desc *dd, const void *log_decay, con
     if (!disjoint(so, dd->B, dd->H, dd->n, dd->dv)) return LUNA_ERR_INVALID_ARG;
     const Plan p = make_plan(dd);
     if (ws_bytes < p.fwd) return LUNA_ERR_WORKSPACE;
-    DeltaArgs a = base(dd, p, log_decay, beta, Q, K, V, lengths);
+    DeltaArgs a = base(dd, p, log_decay, beta, Q, K, V, lengths, workspace);
     a.o = O; a.ob = so.b; a.oh = so.h; a.ot = so.t;
     a.S0 = S0;
     a.S1 = S1;
@@ -211,7 +212,7 @@ luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, con
     char *ws = static_cast<char *>(workspace);
     const bool shared = H != Hk;
 
-    DeltaArgs a = base(dd, p, log_decay, beta, Q, K, V, lengths);
+    DeltaArgs a = base(dd, p, log_decay, beta, Q, K, V, lengths, workspace);
     a.go = view(dO, filled(dd->go, H, n, dv), H);
     a.S0 = S0;
     a.dS1 = dS1;

@@ -29,11 +29,14 @@
 
 #include "luna_delta.cuh"
 #include "luna_prof.cuh"
+#include "luna_sm100.cuh"
 
 namespace luna {
 int tc_sm_count();
 
 namespace {
+
+using namespace sm100;
 
 constexpr int C = kDeltaRows;
 constexpr int kTileB = C * C * 2;  // bytes of a 64 x 64 bf16 tile: rows of 128 bytes, 16-byte pieces swizzled
@@ -41,7 +44,6 @@ constexpr int kRowsF = kDeltaFactors;
 
 // ---- tiles in shared memory: panels of 64 columns, row r's 16-byte piece p at place p ^ (r % 8)
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t tile_at(uint32_t base, int rows, int r, int piece) {
     return base + (piece >> 3) * rows * 128 + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
 }
@@ -61,10 +63,11 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const __nv_bfloat16 *src
         copy16(tile_at(dst, C, r, p), in ? src + r * st + p * 8 : src, in);
     }
 }
-// a tile of `rows` rows of W columns that lie one behind the other
-template <int W>
-__device__ __forceinline__ void load_plane(uint32_t dst, const __half *src, int tid, int threads, int rows = C) {
-    for (int i = tid; i < rows * W / 8; i += threads) copy16(tile_at(dst, rows, i / (W / 8), i % (W / 8)), src + i * 8, true);
+// What this file's kernels leave for each other lies in global memory as its tile does in shared memory: one copy a tile.
+__device__ __forceinline__ void load_tile(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
 }
 
 // ---- matrix instructions
@@ -81,12 +84,12 @@ __device__ __forceinline__ void stm_t(uint32_t at, const Frag &f) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
 }
 __device__ __forceinline__ void mma(float (&c)[4], const Frag &a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const Frag &a, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -203,7 +206,7 @@ __device__ __forceinline__ void prep_write(const uint4 (&w)[DP / 16], float by, 
         uint32_t f[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = pack(by * low(u[i]), by * high(u[i]));
-        *reinterpret_cast<uint4 *>(out + tid / 2 * DP + (tid % 2 * (DP / 16) + p) * 8) = make_uint4(f[0], f[1], f[2], f[3]);
+        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(out) + tile_at(0, C, tid / 2, tid % 2 * (DP / 16) + p)) = make_uint4(f[0], f[1], f[2], f[3]);
     }
 }
 
@@ -231,6 +234,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
     const int64_t at = blockIdx.x, bh = at / a.m;
     const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int rows = min(C, head_length(a.lengths, b, a.n) - t0);
+    if (at == 0 && tid == 0) *a.status = 0;  // (the waits that set it run for a second)
     if (rows <= 0) return;
     const int hk = h / (a.H / a.k.heads);
     const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q);
@@ -309,7 +313,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
     most_of(0, most);
     __syncthreads();
     const Scale ps = block_scale(0);
-    __half *P = a.Pp + at * (TERMS ? 2 : 1) * C * C;
+    char *P = reinterpret_cast<char *>(a.Pp + at * (TERMS ? 2 : 1) * C * C);
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
@@ -317,8 +321,9 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
             const int i = r0 + lane / 4 + half * 8, j = nt * 8 + lane % 4 * 2;
             uint32_t hi, lo;
             split(ps.by * qk[nt][half * 2], ps.by * qk[nt][half * 2 + 1], hi, lo);
-            *reinterpret_cast<uint32_t *>(P + i * C + j) = hi;
-            if (TERMS) *reinterpret_cast<uint32_t *>(P + C * C + i * C + j) = lo;
+            const uint32_t to = tile_at(0, C, i, nt) + lane % 4 * 4;
+            *reinterpret_cast<uint32_t *>(P + to) = hi;
+            if (TERMS) *reinterpret_cast<uint32_t *>(P + kTileB + to) = lo;
         }
     if (tid < C) {
         rowf[tid] = sm.past[tid] * ks.back;
@@ -367,10 +372,13 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
     __syncthreads();
     const Scale ts = block_scale(1);
     if (tid == 0) rowf[4 * C + 2] = ts.back;
-    uint32_t *planes = reinterpret_cast<uint32_t *>(a.Tp + at * 2 * C * C) + tid;
+    char *planes = reinterpret_cast<char *>(a.Tp + at * 2 * C * C);
 #pragma unroll
-    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i)
-        split(ts.by * x[i].x, ts.by * x[i].y, planes[i * kPrepThreads], planes[i * kPrepThreads + C * C / 2]);
+    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i) {
+        const int p = tid + i * kPrepThreads, j = p % (C / 2) * 2;
+        const uint32_t to = tile_at(0, C, p / (C / 2), j >> 3) + (j & 7) * 2;
+        split(ts.by * x[i].x, ts.by * x[i].y, *reinterpret_cast<uint32_t *>(planes + to), *reinterpret_cast<uint32_t *>(planes + kTileB + to));
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -385,33 +393,35 @@ struct ChainShared {
         alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], T[2][kTileB], P[kPlanes][kTileB], x[C * kPitch];
         alignas(16) float rows[kRowsF];
     } stage[2];
+    uint64_t bar[2];
     alignas(16) char out[NW][C * 48];  // a warp's 16 columns of the outputs, rows of 32 bytes 48 apart
 };
 
 template <int DP, int NW, bool REV>
-__device__ __forceinline__ void chain_load(typename ChainShared<DP, NW, REV>::Stage &st, const DeltaArgs &a, int64_t bh, int b, int h,
-                                           int chunk, int len, int col0, int tid) {
+__device__ __forceinline__ void chain_load(typename ChainShared<DP, NW, REV>::Stage &st, uint64_t *bar, const DeltaArgs &a, int64_t bh,
+                                           int b, int h, int chunk, int len, int col0, int tid) {
     using Sh = ChainShared<DP, NW, REV>;
     constexpr int TH = NW * 32;
-    const int hk = h / (a.H / a.k.heads), t0 = chunk * C, rows = min(C, len - t0);
-    const int64_t at = bh * a.m + chunk;
-    const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-    load_plane<DP>(smem_u32(st.k), a.Kp + kat * C * DP, tid, TH);
-    if (REV || a.o) load_plane<DP>(smem_u32(st.q), a.Qp + kat * C * DP, tid, TH);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) load_plane<C>(smem_u32(st.T[i]), a.Tp + (at * 2 + i) * C * C, tid, TH);
-    if (REV || a.o)
-#pragma unroll
-        for (int i = 0; i < Sh::kPlanes; ++i) load_plane<C>(smem_u32(st.P[i]), a.Pp + (at * a.planes + i) * C * C, tid, TH);
+    const int t0 = chunk * C, rows = min(C, len - t0);
+    if (tid == 0) {
+        const int64_t at = bh * a.m + chunk, kat = ((int64_t)b * a.k.heads + h / (a.H / a.k.heads)) * a.m + chunk;
+        const bool all = REV || a.o;
+        mbar_arrive_expect_tx(bar, sizeof(st.k) + sizeof(st.T) + sizeof(st.rows) + (all ? sizeof(st.q) + sizeof(st.P) : 0));
+        load_tile(st.k, a.Kp + kat * C * DP, sizeof(st.k), bar);
+        if (all) load_tile(st.q, a.Qp + kat * C * DP, sizeof(st.q), bar);
+        load_tile(st.rows, a.rows + at * kRowsF, sizeof(st.rows), bar);
+        load_tile(st.T, a.Tp + at * 2 * C * C, sizeof(st.T), bar);
+        if (all) load_tile(st.P, a.Pp + at * a.planes * C * C, sizeof(st.P), bar);
+    }
     const RowView &xv = REV ? a.go : a.v;
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(xv.p) + b * xv.sb + h * xv.sh + t0 * xv.st + col0;
     const uint32_t sx = smem_u32(st.x);
+#pragma unroll
     for (int i = tid; i < C * NW * 2; i += TH) {
         const int r = i / (NW * 2), p = i % (NW * 2);
         const bool in = r < rows && col0 + p * 8 < a.dv;
         copy16(sx + r * Sh::kPitch + p * 16, in ? x + r * xv.st + p * 8 : static_cast<const __nv_bfloat16 *>(xv.p), in);
     }
-    for (int i = tid; i < kRowsF / 4; i += TH) copy16(smem_u32(st.rows) + i * 16, a.rows + at * kRowsF + i * 4, true);
     copies_end();
 }
 
@@ -435,13 +445,14 @@ __device__ __forceinline__ void chain_store(const float (&acc)[N][4], char *mem,
     __syncwarp();
 }
 
-// one plane's 16 x 16 piece of a left operand (rows of a tensor of `ld` columns)
-__device__ __forceinline__ void plane_store(__half *p, int64_t ld, int k0, const Frag &f, int lane) {
-    uint32_t *at = reinterpret_cast<uint32_t *>(p + lane / 4 * ld + k0 + lane % 4 * 2);
-    at[0] = f[0];
-    at[4 * ld] = f[1];
-    at[4] = f[2];
-    at[4 * ld + 4] = f[3];
+// a 16 x 16 piece of a left operand into a tile of `rows` rows
+__device__ __forceinline__ void plane_store(__half *tile, int rows, int r0, int k0, const Frag &f, int lane) {
+    char *p = reinterpret_cast<char *>(tile) + lane % 4 * 4;
+    const int r = r0 + lane / 4;
+    *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r, k0 >> 3)) = f[0];
+    *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r + 8, k0 >> 3)) = f[1];
+    *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r, (k0 >> 3) + 1)) = f[2];
+    *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r + 8, (k0 >> 3) + 1)) = f[3];
 }
 
 template <int DP, int NW, bool REV>
@@ -474,21 +485,31 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
             S[nt][e] = init && place(nt, e, at) ? init[at] : 0.0f;
         }
 
-    if (chunks > 0) chain_load<DP, NW, REV>(sm.stage[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
+    if (tid < 2) mbar_init(&sm.bar[tid], 1);
+    fence_mbar_init();
+    __syncthreads();
+    if (chunks > 0) chain_load<DP, NW, REV>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
     for (int step = 0; step < chunks; ++step) {
         const int chunk = REV ? chunks - 1 - step : step, t0 = chunk * C;
         typename Sh::Stage &st = sm.stage[step & 1];
         copies_wait<0>();
-        __syncthreads();
+        const bool here = mbar_wait_long(&sm.bar[step & 1], (step >> 1) & 1);
+        if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
+            if (tid == 0) {
+                atomicOr(a.status, 1);
+                mbar_wait(&sm.bar[step & 1], (step >> 1) & 1, kDrainNs);
+            }
+            break;
+        }
         if (step + 1 < chunks)
-            chain_load<DP, NW, REV>(sm.stage[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
+            chain_load<DP, NW, REV>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
         if (!mine) continue;
         const uint32_t sk = smem_u32(st.k), sq = smem_u32(st.q), sT = smem_u32(st.T), sP = smem_u32(st.P);
         const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + warp * 32 + ((lane >> 3) & 1) * 16;
         const float whole = st.rows[4 * C], rest = st.rows[4 * C + 1], back_T = st.rows[4 * C + 2], back_P = st.rows[4 * C + 3];
         auto factor = [&](int which, int t) { return *reinterpret_cast<const float2 *>(st.rows + which * C + t); };
         const int64_t group = (bh * a.m + chunk) * (a.dvp / 16) + col / 16;  // the warp's columns in the planes
-        __half *keep = planes ? planes + group * 16 * C : nullptr;
+        __half *keep = planes ? planes + (bh * a.m + chunk) * a.dvp * C : nullptr;
         float *scales = a.scales ? a.scales + group * kDeltaScales : nullptr;  // S, R, U, X, dO
         // S <- c(C, 0) S (first) + F M for a left operand F of 64 summed rows and the tile M (a row for each)
         auto update = [&](const Frag (&fh)[4], const Frag (&fl)[4], float back, uint32_t tile, bool decay) {
@@ -523,7 +544,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
         for (int kt = 0; kt < DP / 16; ++kt) {
             Frag hi, lo;
             split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
-            if (ends) plane_store(ends + group * 16 * DP, DP, kt * 16, hi, lane);
+            if (ends) plane_store(ends + (bh * a.m + chunk) * a.dvp * DP, a.dvp, col, kt * 16, hi, lane);
 #pragma unroll
             for (int np = 0; np < 4; ++np) {
                 Frag f;
@@ -590,7 +611,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                 for (int kt = 0; kt < 4; ++kt) {
                     const Frag hi = {pack(us.by * u[2 * kt][0], us.by * u[2 * kt][1]), pack(us.by * u[2 * kt][2], us.by * u[2 * kt][3]),
                                      pack(us.by * u[2 * kt + 1][0], us.by * u[2 * kt + 1][1]), pack(us.by * u[2 * kt + 1][2], us.by * u[2 * kt + 1][3])};
-                    if (keep) plane_store(keep, C, kt * 16, hi, lane);
+                    if (keep) plane_store(keep, a.dvp, col, kt * 16, hi, lane);
                     if (o)
 #pragma unroll
                         for (int np = kt; np < 4; ++np) {
@@ -707,7 +728,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
             for (int kt = 0; kt < 4; ++kt) {
                 const Frag hi = {pack(us.by * y[2 * kt][0], us.by * y[2 * kt][1]), pack(us.by * y[2 * kt][2], us.by * y[2 * kt][3]),
                                  pack(us.by * y[2 * kt + 1][0], us.by * y[2 * kt + 1][1]), pack(us.by * y[2 * kt + 1][2], us.by * y[2 * kt + 1][3])};
-                plane_store(keep, C, kt * 16, hi, lane);
+                plane_store(keep, a.dvp, col, kt * 16, hi, lane);
             }
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) {
@@ -752,7 +773,9 @@ template <int DP, int DVT>
 struct GradShared {
     alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], go[DVT / 64][kTileB], u[DVT * 128], x[DVT * 128];
     alignas(128) char s[DVT * DP * 2], r[DVT * DP * 2], P[kTileB], W[kTileB];
+    uint64_t bar[2];
     float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales];
+    float steps[5][DVT / 16], all[5];  // of the products over columns: 16 columns' scale over the largest, that
     // of a row's two halves of the columns: q . dQ, k . Z without the rows' part, k . (what it wrote) without and with
     // the rows' part, W . K K^T, x . v, b k . Z
     float sums[7][2][C];
@@ -801,14 +824,21 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     const uint32_t ss = smem_u32(sm.s), sr = smem_u32(sm.r), sP = smem_u32(sm.P), sW = smem_u32(sm.W);
     const int dvp = a.dvp, groups = dvp / 16;
     const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-    load_plane<DP>(sk, a.Kp + kat * C * DP, tid, kGradThreads);
+    if (tid < 2) mbar_init(&sm.bar[tid], 1);
+    fence_mbar_init();
+    __syncthreads();
+    if (tid == 0) {
+        const uint32_t ux = dvp * C * 2, sr_ = dvp * DP * 2;
+        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 2 * ux);
+        load_tile(sm.u, a.Up + at * dvp * C, ux, &sm.bar[0]);
+        load_tile(sm.x, a.Xp + at * dvp * C, ux, &sm.bar[0]);
+        load_tile(sm.k, a.Kp + kat * C * DP, sizeof(sm.k), &sm.bar[0]);
+        mbar_arrive_expect_tx(&sm.bar[1], sizeof(sm.q) + 2 * sr_);
+        load_tile(sm.s, a.Sp + at * dvp * DP, sr_, &sm.bar[1]);
+        load_tile(sm.q, a.Qp + kat * C * DP, sizeof(sm.q), &sm.bar[1]);
+        load_tile(sm.r, a.Rp + at * dvp * DP, sr_, &sm.bar[1]);
+    }
     load_rows<DVT>(sgo, static_cast<const __nv_bfloat16 *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st, a.go.st, rows, a.dv, tid, kGradThreads);
-    load_plane<C>(su, a.Up + at * dvp * C, tid, kGradThreads, dvp);
-    load_plane<C>(sx, a.Xp + at * dvp * C, tid, kGradThreads, dvp);
-    copies_end();
-    load_plane<DP>(ss, a.Sp + at * dvp * DP, tid, kGradThreads, dvp);
-    load_plane<DP>(sr, a.Rp + at * dvp * DP, tid, kGradThreads, dvp);
-    load_plane<DP>(sq, a.Qp + kat * C * DP, tid, kGradThreads);
     copies_end();
     const float *rowf = a.rows + at * kRowsF;
     const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
@@ -818,15 +848,44 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     else if (warp < 3)
         sm.b[tid - 32] = rowf[2 * C + tid - 32];
     for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[at * groups * kDeltaScales + i];
-    copies_wait<1>();
+    copies_wait<0>();
+    bool here = mbar_wait_long(&sm.bar[0], 0);
     __syncthreads();
+    // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
+    // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U, dO S, X S, U R.
+    if (tid < 5) {
+        const int l[5] = {4, 3, 4, 3, 2}, r[5] = {2, 2, 0, 0, 1};
+        float most = 0.0f;
+        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, sm.scales[kt][l[tid]] * sm.scales[kt][r[tid]]);
+        sm.all[tid] = most;
+        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = most > 0.0f ? sm.scales[kt][l[tid]] * sm.scales[kt][r[tid]] / most : 0.0f;
+    }
+    here = mbar_wait_long(&sm.bar[1], 0) && here;
+    if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            for (int i = 0; i < 2; ++i) mbar_wait(&sm.bar[i], 0, kDrainNs);
+        }
+        return;
+    }
 
-    // 16 rows and 16 columns of dO in fp16
-    auto left_go = [&](Frag &f, int kt) {
+    // left operands: 16 rows and 16 columns of dO in fp16; of X, U
+    auto left_go = [&](Frag &f, int kt, int product) {
         left_m(f, sgo, C, r0, kt * 16, lane);
-        const float by = inverse2(sm.scales[kt][4]);
+        const float by = inverse2(sm.scales[kt][4]) * sm.steps[product][kt];
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = pack(by * low(f[i]), by * high(f[i]));
+    };
+    auto left_plane = [&](Frag &f, uint32_t tile, int kt, int product) {
+        left_k(f, tile, dvp, kt * 16, r0, lane);
+        const __half2 by = __float2half2_rn(sm.steps[product][kt]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 x;
+            memcpy(&x, &f[i], 4);
+            x = __hmul2(x, by);
+            memcpy(&f[i], &x, 4);
+        }
     };
     // sums over the four lanes of a row, for this half of the columns: rows lane / 4 and 8 more
     auto row_sums = [&](float (&x)[2], int which) {
@@ -849,28 +908,18 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
 #pragma unroll 2
         for (int kt = 0; kt < groups; ++kt) {
             Frag fg, fx;
-            left_go(fg, kt);
-            left_k(fx, sx, dvp, kt * 16, r0, lane);
-            const float pb = sm.scales[kt][4] * sm.scales[kt][2], wb = sm.scales[kt][3] * sm.scales[kt][2];
+            left_go(fg, kt, 0);
+            left_plane(fx, sx, kt, 1);
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 const int n0 = half * 32 + n * 16;
                 if (n0 > r0) continue;
                 Frag f;
                 right_k(f, su, dvp, kt * 16, n0, lane);
-                float c[4][4];
-                zero(c);
-                mma(c[0], fg, f[0], f[1]);
-                mma(c[1], fg, f[2], f[3]);
-                mma(c[2], fx, f[0], f[1]);
-                mma(c[3], fx, f[2], f[3]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[2 * n + i][e] = fmaf(pb, c[i][e], p[2 * n + i][e]);
-                        w[2 * n + i][e] = fmaf(wb, c[2 + i][e], w[2 * n + i][e]);
-                    }
+                mma(p[2 * n], fg, f[0], f[1]);
+                mma(p[2 * n + 1], fg, f[2], f[3]);
+                mma(w[2 * n], fx, f[0], f[1]);
+                mma(w[2 * n + 1], fx, f[2], f[3]);
             }
         }
 #pragma unroll
@@ -894,8 +943,8 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
             for (int e = 0; e < 4; ++e) {
                 const int i = r0 + lane / 4 + (e >> 1) * 8, j = half * 32 + nt * 8 + q2 + (e & 1);
                 const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
-                p[nt][e] = j <= i ? a.scale * c * p[nt][e] : 0.0f;
-                w[nt][e] = j < i ? c * w[nt][e] : 0.0f;
+                p[nt][e] = j <= i ? a.scale * sm.all[0] * c * p[nt][e] : 0.0f;
+                w[nt][e] = j < i ? sm.all[1] * c * w[nt][e] : 0.0f;
                 if (j < i) dot[e >> 1] = fmaf(w[nt][e], kk[nt][e], dot[e >> 1]);
                 w[nt][e] *= sm.b[i];
                 mp = fmaxf(mp, fabsf(p[nt][e]));
@@ -908,7 +957,6 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
             sm.most[0][warp] = mp;
             sm.most[1][warp] = mw;
         }
-        copies_wait<0>();
         __syncthreads();
         mp = mw = 0.0f;
 #pragma unroll
@@ -963,25 +1011,18 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
 
     const int c0 = half * (DP / 2);  // first column of the warp's
     const int ra = r0 + lane / 4, rb = ra + 8;
-    // acc += F M over the columns of the state: F by left(f, kt), M a tile of S or R, scaled down by back(kt)
-    auto over_columns = [&](Acc &acc, uint32_t tile, auto left, auto back) {
+    // acc += F M over the columns of the state: F by left(f, kt), M a tile of S or R
+    auto over_columns = [&](Acc &acc, uint32_t tile, auto left) {
 #pragma unroll 2
         for (int kt = 0; kt < groups; ++kt) {
             Frag fl;
             left(fl, kt);
-            const float s = back(kt);
 #pragma unroll
             for (int np = 0; np < NT / 2; ++np) {
                 Frag f;
                 right_k(f, tile, dvp, kt * 16, c0 + np * 16, lane);
-                float c[2][4];
-                zero(c);
-                mma(c[0], fl, f[0], f[1]);
-                mma(c[1], fl, f[2], f[3]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[2 * np + i][e] = fmaf(s, c[i][e], acc[2 * np + i][e]);
+                mma(acc[2 * np], fl, f[0], f[1]);
+                mma(acc[2 * np + 1], fl, f[2], f[3]);
             }
         }
     };
@@ -1050,23 +1091,23 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
 
     Acc acc, z;
     zero(acc);
-    over_columns(acc, ss, left_go, [&](int kt) { return sm.scales[kt][4] * sm.scales[kt][0]; });
-    times_rows(acc, a.scale * sm.past[ra], a.scale * sm.past[rb]);
+    over_columns(acc, ss, [&](Frag &f, int kt) { left_go(f, kt, 2); });
+    times_rows(acc, a.scale * sm.all[2] * sm.past[ra], a.scale * sm.all[2] * sm.past[rb]);
     over_rows(acc, sP, false, sk, back_p * back_k);
     dot_rows(acc, sq, back_q, 0);
     store_rows(acc, dq, a.dqt);
 
     zero(z);
-    over_columns(z, ss, [&](Frag &f, int kt) { left_k(f, sx, dvp, kt * 16, r0, lane); }, [&](int kt) { return sm.scales[kt][3] * sm.scales[kt][0]; });
-    times_rows(z, sm.past[ra], sm.past[rb]);
+    over_columns(z, ss, [&](Frag &f, int kt) { left_plane(f, sx, kt, 3); });
+    times_rows(z, sm.all[3] * sm.past[ra], sm.all[3] * sm.past[rb]);
     dot_rows(z, sk, back_k, 1);  // (for db, without b and the rows' part)
     times_rows(z, sm.b[ra], sm.b[rb]);
     over_rows(z, sW, false, sk, back_w * back_k);
     dot_rows(z, sk, back_k, 6);
 
     zero(acc);
-    over_columns(acc, sr, [&](Frag &f, int kt) { left_k(f, su, dvp, kt * 16, r0, lane); }, [&](int kt) { return sm.scales[kt][2] * sm.scales[kt][1]; });
-    times_rows(acc, sm.left[ra], sm.left[rb]);
+    over_columns(acc, sr, [&](Frag &f, int kt) { left_plane(f, su, kt, 4); });
+    times_rows(acc, sm.all[4] * sm.left[ra], sm.all[4] * sm.left[rb]);
     dot_rows(acc, sk, back_k, 2);
     over_rows(acc, sP, true, sq, back_p * back_q);
     over_rows(acc, sW, true, sk, -back_w * back_k);

@@ -26,9 +26,8 @@ def select(logits, scores, done, end):
     V = x.shape[-1]
     with np.errstate(all="ignore"):
         top = x.max(-1, keepdims=True)
-        lse = top + np.log(np.exp(x - top).sum(-1, keepdims=True))
-        base = scores.astype(np.float64)[..., None] - lse
-        cand = np.where(np.isfinite(base), base + x, -np.inf)
+        base = scores.astype(np.float64)[..., None] - np.log(np.exp(x - top).sum(-1, keepdims=True))
+        cand = np.where(np.isfinite(base) & np.isfinite(top), base + (x - top), -np.inf)
     if done is not None:
         stay = np.full_like(cand, -np.inf)
         stay[:, :, end] = scores

@@ -129,7 +129,9 @@ def check_all(L, B, H, Hk, n, d, dv, io, layout, lengths, state, gates=None, nan
         ref[x] = ref[x].reshape(B, Hk, G, n, -1).sum(2)
     p = L.Delta(B, H, n, d, dv, Hk=Hk, io=io, backward=True)
     O, S1 = p.forward(Q, K, V, lg, bt, lens, S0, want_state=True)
+    assert L.luna_device_status(p.ws) == 0
     g = p.backward(Q, K, V, dO, lg, bt, lens, S0, dS1)
+    assert L.luna_device_status(p.ws) == 0
     got = {"O": O, "S1": S1, **g}
     off = {name: rel(t, ref[name]) for name, t in got.items()}
     assert all(off[name] < tol(name, t.dtype) for name, t in got.items()), off
