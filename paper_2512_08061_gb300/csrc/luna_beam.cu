@@ -35,66 +35,73 @@ __device__ __forceinline__ double unordered(uint64_t u) {
 struct RowKey {
     uint64_t v = 0;
     __device__ bool over(const RowKey &o) const { return v > o.v; }
-    __device__ RowKey lane_xor(int w) const { return RowKey{__shfl_xor_sync(0xffffffffu, v, w)}; }
+    __device__ RowKey lane(int l) const { return RowKey{__shfl_sync(0xffffffffu, v, l)}; }
 };
 // A candidate of a sequence: its score, and at equal scores the lower beam, then the lower token first.  v = 0: none.
 struct SeqKey {
     uint64_t v = 0;
     uint32_t i = 0;  // ~(beam * V + token)
-    __device__ bool over(const SeqKey &o) const { return v > o.v || (v == o.v && i > o.i); }
-    __device__ SeqKey lane_xor(int w) const {
-        return SeqKey{__shfl_xor_sync(0xffffffffu, v, w), __shfl_xor_sync(0xffffffffu, i, w)};
-    }
+    __device__ bool over(const SeqKey &o) const { return (v > o.v) | ((v == o.v) & (i > o.i)); }
+    __device__ SeqKey lane(int l) const { return SeqKey{__shfl_sync(0xffffffffu, v, l), __shfl_sync(0xffffffffu, i, l)}; }
 };
 
-// The place of every thread's candidate among the block's 256: each warp sorts its own by exchanges, then each looks
-// its candidate up in the other warps' lists.  Equal ones (none at all) go by their place in `list`.  `key` becomes
-// the candidate that the returned place is of.  All threads call it; `list` may be written again after a barrier.
+// Exchanges of a warp's 32 candidates over lanes w apart, w = from, from / 2, .. 1: the better one goes to the lower lane
+// where `down`.
 template <typename Key>
-__device__ int place_in_block(Key &key, Key *list) {
+__device__ __forceinline__ void exchange(Key &key, int from, bool down) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int w = 16; w > 0; w /= 2) {
+        if (w > from) continue;
+        const Key other = key.lane(lane ^ w);
+        const bool take = other.over(key) == (((lane & w) == 0) == down);
+        key.v = take ? other.v : key.v;
+        if constexpr (sizeof(Key) > 8) key.i = take ? other.i : key.i;
+    }
+}
+// a warp's candidates in order, the best in lane 0
+template <typename Key>
+__device__ __forceinline__ void sort_warp(Key &key) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int size = 2; size <= 32; size *= 2) exchange(key, size / 2, (lane & size) == 0 || size == 32);
+}
+// The best 32 of two ordered lists, in order: lane by lane the better of the one and of the other from its end, which
+// are all that stay, and rise and fall once.
+template <typename Key>
+__device__ __forceinline__ void merge_warp(Key &key, const Key &from_end) {
+    const bool take = from_end.over(key);
+    key.v = take ? from_end.v : key.v;
+    if constexpr (sizeof(Key) > 8) key.i = take ? from_end.i : key.i;
+    exchange(key, 16, true);
+}
+// The best 32 of the block's candidates, given as the warps' ordered lists: in list[0..31] and in warp 0's lanes.  All
+// threads call it; `list` may be written again after a barrier.
+template <typename Key>
+__device__ __forceinline__ void join_warps(Key &key, Key *list) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-#pragma unroll
-    for (int size = 2; size <= 32; size *= 2)
-#pragma unroll
-        for (int w = size / 2; w > 0; w /= 2) {
-            const Key other = key.lane_xor(w);
-            const bool low = (lane & w) == 0, down = (lane & size) == 0 || size == 32;  // the larger one goes low where `down`
-            if (low == down ? other.over(key) : key.over(other)) key = other;
-        }
     list[threadIdx.x] = key;
     __syncthreads();
-    int place = lane;
 #pragma unroll
-    for (int i = 1; i < kThreads / 32; ++i) {
-        const int o = (warp + i) % (kThreads / 32);
-        const Key *l = list + 32 * o;
-        auto before = [&](const Key &x) { return o < warp ? !key.over(x) : x.over(key); };
-        int n = 0;
-#pragma unroll
-        for (int w = 16; w > 0; w /= 2)
-            if (before(l[n + w - 1])) n += w;
-        if (before(l[n])) ++n;
-        place += n;
-    }
-    return place;
-}
-
-// The K best of `count` candidates in `from`, in order, into best (its first `have` are candidates too): 256 at a time.
-template <typename Key>
-__device__ void best_of(const Key *from, int count, Key *best, int have, int K, Key *list) {
-    const int tid = threadIdx.x;
-    int at = 0;
-    do {
+    for (int w = kThreads / 64; w > 0; w /= 2) {
+        if (warp < w) {
+            merge_warp(key, list[(warp + w) * 32 + 31 - lane]);
+            list[threadIdx.x] = key;  // (in the next round read by another warp than it is written by)
+        }
         __syncthreads();
-        Key key = tid < have ? best[tid] : Key{};
-        const int take = min(count - at, kThreads - have);
-        if (tid >= have && tid - have < take) key = from[at + tid - have];
-        at += take;
-        const int place = place_in_block(key, list);  // (every best[] is read before its barrier)
-        if (place < K) best[place] = key;
-        have = K;
-    } while (at < count);
-    __syncthreads();
+    }
+}
+// The best 32 of candidate(0..count - 1), as join_warps
+template <typename Key, typename F>
+__device__ __forceinline__ void best_of(int count, F candidate, Key &key, Key *list) {
+    const int lane = threadIdx.x % 32;
+    key = Key{};
+    for (int at = threadIdx.x - lane; at < count; at += kThreads) {
+        Key next = at + lane < count ? candidate(at + lane) : Key{};
+        sort_warp(next);
+        merge_warp(key, next.lane(31 - lane));
+    }
+    join_warps(key, list);
 }
 
 // 2^x to 2^-22 of itself
@@ -119,14 +126,16 @@ struct BeamArgs {
 };
 
 // One part of one row: its maximum, its sum of exponentials and its K best values, in one reading.  A thread holds PER
-// values of a piece of 256 PER; only values that reach the K-th best so far or the K-th best of the threads' largest
-// (there are K as good) are looked at again, so that of a piece a few dozen are sorted: those of at most K threads.
+// values of a piece of 256 PER.  Of the first piece only what reaches the K-th best of the threads' largest is kept
+// (there are K as good, and at most K threads have some), of the others too; a few dozen values are sorted at the end,
+// or before, where the kept ones run out of room (values that rise along a row).
 // Few rows come in pieces of 2048 values, so that more SMs share them.  Bound by the bytes of the logits where there are
 // many rows, else by the chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
     constexpr int VEC = 16 / sizeof(T), NV = PER / VEC, PIECE = kThreads * PER;
-    __shared__ RowKey list[kThreads], best[kMaxBeams], pool[kMaxBeams * PER], least;
+    constexpr int POOL = kMaxBeams * (PER + 1) + 512;  // (of a piece at most kMaxBeams threads' after the block's best are known)
+    __shared__ RowKey list[kThreads], pool[POOL];
     __shared__ int count;
     __shared__ float smax[kThreads / 32], ssum[kThreads / 32];
     const int tid = threadIdx.x, row = blockIdx.y, part = blockIdx.x;
@@ -137,7 +146,8 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     const int vectors = (a.V + off + VEC - 1) / VEC, pieces = (vectors + PIECE / VEC - 1) / (PIECE / VEC);
     const int first = (int)((int64_t)pieces * part / a.S), last = (int)((int64_t)pieces * (part + 1) / a.S);
     float top = -INFINITY, sum = 0.0f;
-    bool have = false;
+    RowKey bar;  // K candidates are at least as good (none: v = 0)
+    auto floor_of = [](const RowKey &k) { return k.v ? unordered((uint32_t)(k.v >> 32)) : -INFINITY; };
     for (int piece = first; piece < last; ++piece) {
         float val[PER];
         const int v0 = piece * (PIECE / VEC) + tid;  // vectors of a thread: every 256th
@@ -172,45 +182,53 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
             if (t >= 0 && t < a.V && val[i] == val[i]) k.v = (uint64_t)ordered(val[i] + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
             return k;
         };
-        const RowKey bar = have ? best[a.K - 1] : RowKey{};  // (none while fewer than K are found: v = 0)
-        RowKey need = bar;
-        const float floor = bar.v ? unordered((uint32_t)(bar.v >> 32)) : -INFINITY;
-        const int hits = __syncthreads_count(m >= floor);
-        if (have && hits == 0) continue;
-        if (!have || hits > a.K) {
-            RowKey k;  // the thread's best: the first of its largest (tokens rise with i)
+        auto best_of_thread = [&]() {  // the first of its largest (tokens rise with i)
+            RowKey k;
 #pragma unroll
             for (int i = PER - 1; i >= 0; --i)
                 if (val[i] == m) {
                     const RowKey c = key(i);
                     if (c.v) k = c;
                 }
-            const int place = place_in_block(k, list);
-            if (place == a.K - 1) least = k;
-            __syncthreads();
-            if (!bar.over(least)) need = least;
+            return k;
+        };
+        // the K-th best of the threads' largest: K candidates are as good, and no more than K threads have some
+        auto threshold = [&]() {
+            RowKey k = best_of_thread();
+            sort_warp(k);
+            join_warps(k, list);
+            return list[a.K - 1];
+        };
+        if (piece == first) {
+            if (tid == 0) count = 0;
+            bar = threshold();  // (none where fewer than K threads have a value)
+        } else {
+            const int hits = __syncthreads_count(m >= floor_of(bar));
+            if (hits == 0) continue;
+            if (count + hits * PER > POOL) {
+                RowKey k;
+                best_of(count, [&](int i) { return pool[i]; }, k, list);
+                const RowKey kth = list[a.K - 1];
+                if (tid < a.K) pool[tid] = k;
+                __syncthreads();
+                if (tid == 0) count = a.K;  // (what is none among them stays so)
+                const RowKey least = threshold();
+                bar = least.over(kth) ? least : kth;
+            }
         }
-        if (tid == 0) count = 0;
-        __syncthreads();
-        const float lowest = need.v ? unordered((uint32_t)(need.v >> 32)) : -INFINITY;
+        const float lowest = floor_of(bar);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (val[i] >= lowest) {
                 const RowKey c = key(i);
-                if (c.v && !need.over(c) && c.over(bar)) pool[atomicAdd(&count, 1)] = c;
+                if (c.v && !bar.over(c)) pool[atomicAdd(&count, 1)] = c;
             }
         __syncthreads();
-        const int found = count;
-        if (have && found == 0) continue;
-        best_of(pool, found, best, have ? a.K : 0, a.K, list);
-        have = true;
     }
-    if (!have) {  // (fewer pieces than parts)
-        if (tid < a.K) best[tid] = RowKey{};
-        __syncthreads();
-    }
+    RowKey best;
+    best_of(last > first ? count : 0, [&](int i) { return pool[i]; }, best, list);  // (fewer pieces than parts)
     const int64_t at = (int64_t)row * a.S + part;
-    if (tid < a.K) a.keys[at * a.K + tid] = best[tid].v;
+    if (tid < a.K) a.keys[at * a.K + tid] = best.v;
     float m = top;
 #pragma unroll
     for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
@@ -232,17 +250,12 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
 // The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that which of two near ones is better
 // does not hang on a rounding: 64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once
 // and a candidate costs one sum (exponentials and logarithms by a warp a row took 16 to 37 us).  One block a sequence:
-// K S K candidates, looked at twice as in k_beam_rows.
-constexpr int kHeld = 4;  // candidates that a thread keeps from the first look
-
+// K S K candidates, which its warps sort 32 at a time.
 __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
-    extern __shared__ char raw[];
-    SeqKey *pool = reinterpret_cast<SeqKey *>(raw);
-    __shared__ SeqKey list[kThreads], best[kMaxBeams], least;
+    __shared__ SeqKey list[kThreads];
     __shared__ double base[kMaxBeams];  // score - log sum exp(logit - most)
     __shared__ float score[kMaxBeams], most[kMaxBeams], sums[kMaxBeams];
     __shared__ uint8_t done[kMaxBeams], dead[kMaxBeams];  // dead: no candidate of its has a score
-    __shared__ int count;
     const int tid = threadIdx.x, b = blockIdx.x, K = a.K, S = a.S;
     for (int k = tid / 32; k < K; k += kThreads / 32) {  // a warp a row
         const int row = b * K + k, lane = tid % 32;
@@ -266,7 +279,6 @@ __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
             sums[k] = sum;
         }
     }
-    if (tid == 0) count = 0;
     __syncthreads();
     if (tid < K) {
         const double x = (double)score[tid] - log((double)sums[tid]);
@@ -296,33 +308,12 @@ __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
         c.i = ~(uint32_t)(k * a.V + token);
         return c;
     };
-    SeqKey mine, held[kHeld];
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        if (tid + i * kThreads < N) held[i] = candidate(tid + i * kThreads);
-        if (held[i].over(mine)) mine = held[i];
-    }
-    for (int n = tid + kHeld * kThreads; n < N; n += kThreads) {
-        const SeqKey c = candidate(n);
-        if (c.over(mine)) mine = c;
-    }
-    const int place = place_in_block(mine, list);
-    if (place == K - 1) least = mine;
-    __syncthreads();
-    const SeqKey need = least;
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-        if (held[i].v && !need.over(held[i])) pool[atomicAdd(&count, 1)] = held[i];
-    for (int n = tid + kHeld * kThreads; n < N; n += kThreads) {
-        const SeqKey c = candidate(n);
-        if (c.v && !need.over(c)) pool[atomicAdd(&count, 1)] = c;
-    }
-    __syncthreads();
-    best_of(pool, count, best, 0, K, list);
+    SeqKey best;
+    best_of(N, candidate, best, list);
     if (tid < K) {
-        const uint32_t at = ~best[tid].i;
+        const uint32_t at = ~best.i;
         const int parent = (int)(at / a.V), token = (int)(at - (uint32_t)parent * a.V);
-        a.scores_out[b * K + tid] = (float)unordered(best[tid].v);
+        a.scores_out[b * K + tid] = (float)unordered(best.v);
         a.tokens[b * K + tid] = token;
         a.parents[b * K + tid] = parent;
         if (a.done_out) a.done_out[b * K + tid] = done[parent] || token == a.end;
@@ -450,11 +441,7 @@ luna_status luna_beam_select(const luna_beam_desc *bd, const void *logits, const
     } else {
         LUNA_LAUNCH("beam_rows", (k_beam_rows<__nv_bfloat16, kPer>), grid, kThreads, 0, s, a);
     }
-    // at most K threads hold a candidate that reaches the K-th best of the threads' maxima
-    const size_t pool = sizeof(SeqKey) * bd->K * (size_t)cdiv((int64_t)bd->K * a.S * bd->K, kThreads);
-    if (cudaFuncSetAttribute(k_beam_join, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pool) != cudaSuccess)
-        return LUNA_ERR_CUDA;
-    LUNA_LAUNCH("beam_join", k_beam_join, (unsigned)bd->B, kThreads, pool, s, a);
+    LUNA_LAUNCH("beam_join", k_beam_join, (unsigned)bd->B, kThreads, 0, s, a);
     return cudaGetLastError() == cudaSuccess ? LUNA_OK : LUNA_ERR_CUDA;
 }
 
