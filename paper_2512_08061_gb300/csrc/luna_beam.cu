@@ -13,7 +13,9 @@ namespace {
 
 constexpr int kMaxBeams = 32;                  // a warp's lanes
 constexpr int kThreads = 256;
-constexpr int kPer = 32, kFew = 8;             // values of a piece that a thread holds, many rows or few
+// values of a piece that a thread holds: of many rows 64 bytes, of few 8 values
+template <typename T> constexpr int kPer = 64 / (int)sizeof(T);
+constexpr int kFew = 8;
 
 // Values as integers in the same order; larger is better.
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -129,8 +131,9 @@ struct BeamArgs {
 // values of a piece of 256 PER.  Of the first piece only what reaches the K-th best of the threads' largest is kept
 // (there are K as good, and at most K threads have some), of the others too; a few dozen values are sorted at the end,
 // or before, where the kept ones run out of room (values that rise along a row).
-// Few rows come in pieces of 2048 values, so that more SMs share them.  Bound by the bytes of the logits where there are
-// many rows, else by the chain of one piece.
+// Few rows come in pieces of 2048 values, so that more SMs share them.  The next piece is on its way to shared memory
+// meanwhile, each thread's own part of it.  Bound by the bytes of the logits where there are many rows, else by the
+// chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
     constexpr int VEC = 16 / sizeof(T), NV = PER / VEC, PIECE = kThreads * PER;
@@ -148,15 +151,30 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     float top = -INFINITY, sum = 0.0f;
     RowKey bar;  // K candidates are at least as good (none: v = 0)
     auto floor_of = [](const RowKey &k) { return k.v ? unordered((uint32_t)(k.v >> 32)) : -INFINITY; };
+    extern __shared__ uint4 ahead[];  // [2][NV][kThreads]
+    auto first_of = [&](int piece, int j) { return (piece * (PIECE / VEC) + j * kThreads + tid) * VEC - off; };  // every 256th vector
+    auto fetch = [&](int piece) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int t = first_of(piece, j);
+            if (t >= 0 && t + VEC <= a.V) {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ahead[(((piece - first) & 1) * NV + j) * kThreads + tid]);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(x + t) : "memory");
+            }
+        }
+    };
+    if (first < last) fetch(first);
+    asm volatile("cp.async.commit_group;" ::: "memory");
     for (int piece = first; piece < last; ++piece) {
+        if (piece + 1 < last) fetch(piece + 1);
+        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
         float val[PER];
-        const int v0 = piece * (PIECE / VEC) + tid;  // vectors of a thread: every 256th
-        auto token = [&](int i) { return (v0 + i / VEC * kThreads) * VEC - off + i % VEC; };
+        auto token = [&](int i) { return first_of(piece, i / VEC) + i % VEC; };
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int t = token(j * VEC);
             if (t >= 0 && t + VEC <= a.V) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(x + t);
+                const uint4 w = ahead[(((piece - first) & 1) * NV + j) * kThreads + tid];
                 T e[VEC];
                 memcpy(e, &w, 16);
 #pragma unroll
@@ -171,25 +189,25 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
 #pragma unroll
         for (int i = 0; i < PER; ++i) m = fmaxf(m, val[i]);
         const float now = fmaxf(top, m), shift = now == -INFINITY ? 0.0f : now;
-        sum *= power2((top - shift) * kLog2e);
+        float part_sum[4] = {sum * power2((top - shift) * kLog2e), 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sum += power2((val[i] - shift) * kLog2e);
+        for (int i = 0; i < PER; ++i) part_sum[i % 4] += power2((val[i] - shift) * kLog2e);
+        sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
         top = now;
-        // a value's key, or none: behind the row's ends, or a NaN (k_beam_join sees by the sum that such a row has no scores)
-        auto key = [&](int i) {
+        // the key of a value, or none: behind the row's ends, or a NaN (k_beam_join sees by the sum that such a row has no scores)
+        auto key = [&](int i, float v) {
             const int t = token(i);
             RowKey k;
-            if (t >= 0 && t < a.V && val[i] == val[i]) k.v = (uint64_t)ordered(val[i] + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
+            if (t >= 0 && t < a.V && v == v) k.v = (uint64_t)ordered(v + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
             return k;
         };
-        auto best_of_thread = [&]() {  // the first of its largest (tokens rise with i)
+        auto best_of_thread = [&]() {  // the first of its largest (tokens rise with i) that is a token's
             RowKey k;
+            int at = -1;
 #pragma unroll
             for (int i = PER - 1; i >= 0; --i)
-                if (val[i] == m) {
-                    const RowKey c = key(i);
-                    if (c.v) k = c;
-                }
+                if (val[i] == m && token(i) >= 0 && token(i) < a.V) at = i;
+            if (at >= 0) k = key(at, m);
             return k;
         };
         // the K-th best of the threads' largest: K candidates are as good, and no more than K threads have some
@@ -217,12 +235,16 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
             }
         }
         const float lowest = floor_of(bar);
+        uint32_t mask = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (val[i] >= lowest) {
-                const RowKey c = key(i);
-                if (c.v && !bar.over(c)) pool[atomicAdd(&count, 1)] = c;
-            }
+        for (int i = 0; i < PER; ++i) mask |= val[i] >= lowest ? 1u << i : 0u;
+        while (mask) {  // (few: their values are read again)
+            const int i = __ffs(mask) - 1, t = token(i);
+            mask &= mask - 1;
+            if (t < 0 || t >= a.V) continue;
+            const RowKey c = key(i, io_load(x + t));
+            if (c.v && !bar.over(c)) pool[atomicAdd(&count, 1)] = c;
+        }
         __syncthreads();
     }
     RowKey best;
@@ -382,16 +404,26 @@ luna_status check(const luna_beam_desc *bd) {
     return LUNA_OK;
 }
 
-// How rows are cut: the values that a thread holds of a piece, and the parts of a row.  Many rows: pieces of 8192 values
-// and as many blocks as the SMs hold at four each; few, which pieces of 8192 leave most SMs without: pieces of 2048.
+// How rows are cut: the values that a thread holds of a piece, and the parts of a row.  Many rows: large pieces and as
+// many blocks as the SMs hold at four each; few, whose large pieces leave most SMs without one: small pieces.
 struct Cut {
     int per, parts;
 };
 Cut cut(const luna_beam_desc *bd) {
     const int64_t rows = std::max<int64_t>(1, (int64_t)bd->B * bd->K), sms = tc_sm_count(), V = (int64_t)bd->V + 8;
-    const int per = rows * cdiv(V, kThreads * kPer) < sms ? kFew : kPer;
+    const int large = bd->io == LUNA_F32 ? kPer<float> : kPer<__nv_bfloat16>;
+    const int per = rows * cdiv(V, kThreads * large) < sms ? kFew : large;
     const int64_t most = std::max<int64_t>(1, 4 * sms / rows);
     return Cut{per, (int)std::min(cdiv(V, kThreads * per), most)};
+}
+
+template <typename T, int PER>
+cudaError_t launch_rows(const BeamArgs &a, cudaStream_t s) {
+    const size_t ahead = 2 * sizeof(T) * PER * kThreads;
+    cudaError_t e = cudaFuncSetAttribute(k_beam_rows<T, PER>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ahead);
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("beam_rows", (k_beam_rows<T, PER>), dim3((unsigned)a.S, (unsigned)(a.B * a.K)), kThreads, ahead, s, a);
+    return cudaGetLastError();
 }
 
 size_t workspace(const luna_beam_desc *bd) {
@@ -430,17 +462,13 @@ luna_status luna_beam_select(const luna_beam_desc *bd, const void *logits, const
                bd->B, bd->K, bd->V, bd->end, how.parts};
     a.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + 256);
     a.stats = reinterpret_cast<float2 *>(static_cast<char *>(ws) + 256 + align256((int64_t)bd->B * bd->K * a.S * bd->K * 8));
-    const dim3 grid((unsigned)a.S, (unsigned)(bd->B * bd->K));
-    if (bd->io == LUNA_F32) {
-        if (how.per == kFew)
-            LUNA_LAUNCH("beam_rows", (k_beam_rows<float, kFew>), grid, kThreads, 0, s, a);
-        else
-            LUNA_LAUNCH("beam_rows", (k_beam_rows<float, kPer>), grid, kThreads, 0, s, a);
-    } else if (how.per == kFew) {
-        LUNA_LAUNCH("beam_rows", (k_beam_rows<__nv_bfloat16, kFew>), grid, kThreads, 0, s, a);
-    } else {
-        LUNA_LAUNCH("beam_rows", (k_beam_rows<__nv_bfloat16, kPer>), grid, kThreads, 0, s, a);
-    }
+    const bool few = how.per == kFew;
+    cudaError_t e;
+    if (bd->io == LUNA_F32)
+        e = few ? launch_rows<float, kFew>(a, s) : launch_rows<float, kPer<float>>(a, s);
+    else
+        e = few ? launch_rows<__nv_bfloat16, kFew>(a, s) : launch_rows<__nv_bfloat16, kPer<__nv_bfloat16>>(a, s);
+    if (e != cudaSuccess) return LUNA_ERR_CUDA;
     LUNA_LAUNCH("beam_join", k_beam_join, (unsigned)bd->B, kThreads, 0, s, a);
     return cudaGetLastError() == cudaSuccess ? LUNA_OK : LUNA_ERR_CUDA;
 }
