@@ -57,7 +57,7 @@ struct DeltaArgs {
     float *U, *X;           // rows written and their gradients, [B H][n][dv] (CUDA-core form)
     float *before, *after;  // states before chunk i, gradients of the states before chunk i, [B H][m + 1][d][dv]
     // tensor-core form (fp16, scaled; dvp: dv to a multiple of 16, dp: d to 64 or 128), for every chunk: its rows of K
-    // and Q ([B Hk][m][64][dp]), the inverse T in two planes and the scores P in `planes` of them ([64][64] each),
+    // and Q ([B Hk][m][64][dp]), the inverse T, transposed, in two planes and the scores P in `planes` of them ([64][64] each),
     // factors of its rows; and for every 16 columns of a chunk U and X ([16][64], transposed), the states at its two
     // ends (S before, R behind; [16][dp], transposed), and what S, R, U, X and dO were scaled down by
     __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Sp, *Rp;

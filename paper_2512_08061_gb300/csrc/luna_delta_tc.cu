@@ -169,75 +169,82 @@ __device__ __forceinline__ void zero(float (&c)[N][4]) {
 
 // ---------------------------------------------------------------------------
 // T, P and the factors of every chunk.  A block of four warps a chunk, a warp 16 rows of K K^T and Q K^T.  The inverse
-// is taken in fp32: the diagonal blocks of 16 rows by substitution, a thread a column, then those of 32 and of 64 rows
-// from T21 = -T22 A21 T11.
+// of the diagonal blocks of 16 rows is taken by substitution in fp32, a lane a column; a warp then goes down one block
+// column of T, transposed so that each product's accumulators are the next one's left operand:
+//
+//     T_IJ^T = -(sum_{J <= K < I} T_KJ^T A_IK^T) T_II^T
+//
+// with both operands in two terms.  It leaves T^T, P and in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b,
+// scale c(i, 0) 2^eq of its rows, then c(C, 0) in two terms and what T, P, K and Q were scaled down by (the last two
+// are 2^ek and 2^eq).  (With the inverse in fp32 by all threads, 13 barriers and 68 KB of shared memory: 248 us for 8192
+// chunks.)
 
-constexpr int kPrepThreads = 128, kLdA = C + 4;
-
-// What it leaves in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b, scale c(i, 0) 2^eq of its rows, then c(C, 0) in
-// two terms and what T, P, K and Q were scaled down by (the last two are 2^ek and 2^eq).
+constexpr int kPrepThreads = 128;
 
 template <int DP>
 struct PrepShared {
-    alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB];
-    float A[C][kLdA], T[C][kLdA];
-    float hi[C], lo[C], past[C], left[C], b[C], most[4][kPrepThreads / 32];
+    alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], A[2][kTileB];  // A: two planes; T_II in its diagonal blocks
+    float diag[4][16][17];
+    float hi[C], lo[C], past[C], left[C], b[C], most[5][kPrepThreads / 32], back_T[4];
 };
 
-// The largest value of a bf16 tile's row half, and the half in fp16
+// the half row of a bf16 tile that a thread scales: its largest value; in fp16 to `out`
 template <int DP>
-__device__ __forceinline__ float prep_most(uint32_t tile, uint4 (&w)[DP / 16], int tid) {
+__device__ __forceinline__ uint4 prep_piece(uint32_t tile, int tid, int p) {
+    uint4 w;
+    const uint32_t at = tile_at(tile, C, tid / 2, tid % 2 * (DP / 16) + p);
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at));
+    return w;
+}
+template <int DP>
+__device__ __forceinline__ float prep_most(uint32_t tile, int tid) {
     uint32_t most = 0;
 #pragma unroll
     for (int p = 0; p < DP / 16; ++p) {
-        const uint32_t at = tile_at(tile, C, tid / 2, tid % 2 * (DP / 16) + p);
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(at));
-        const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+        const uint4 w = prep_piece<DP>(tile, tid, p);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, max((u[i] << 16) & 0x7fff0000u, u[i] & 0x7fff0000u));
     }
     return __uint_as_float(most);
 }
 template <int DP>
-__device__ __forceinline__ void prep_write(const uint4 (&w)[DP / 16], float by, __half *out, int tid) {
+__device__ __forceinline__ void prep_write(uint32_t tile, float by, __half *out, int tid) {
 #pragma unroll
     for (int p = 0; p < DP / 16; ++p) {
-        const uint32_t u[4] = {w[p].x, w[p].y, w[p].z, w[p].w};
+        const uint4 w = prep_piece<DP>(tile, tid, p);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
         uint32_t f[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = pack(by * low(u[i]), by * high(u[i]));
         *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(out) + tile_at(0, C, tid / 2, tid % 2 * (DP / 16) + p)) = make_uint4(f[0], f[1], f[2], f[3]);
     }
 }
-
-// out = sign X Y for W x W matrices of rows kLdA apart, by `threads` threads: four neighbouring columns of a row each
-template <int W>
-__device__ __forceinline__ void prep_product(float *out, const float *X, const float *Y, float sign, int t, int threads) {
-    for (int i = t; i < W * W / 4; i += threads) {
-        const int r = i / (W / 4), c = i % (W / 4) * 4;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+// acc += F M^T in two terms each, for F of 16 rows and 16 summed indices, M the 16 x 16 block (n0, k0) of two planes
+__device__ __forceinline__ void prep_product(float (&acc)[2][4], const Frag &hi, const Frag &lo, uint32_t planes, int n0, int k0, int lane) {
+    Frag f, g;
+    right_n(f, planes, C, n0, k0, lane);
+    right_n(g, planes + kTileB, C, n0, k0, lane);
 #pragma unroll
-        for (int l = 0; l < W; ++l) {
-            const float x = X[r * kLdA + l];
-            const float4 y = *reinterpret_cast<const float4 *>(Y + l * kLdA + c);
-            acc.x = fmaf(x, y.x, acc.x); acc.y = fmaf(x, y.y, acc.y); acc.z = fmaf(x, y.z, acc.z); acc.w = fmaf(x, y.w, acc.w);
-        }
-        *reinterpret_cast<float4 *>(out + r * kLdA + c) = make_float4(sign * acc.x, sign * acc.y, sign * acc.z, sign * acc.w);
+    for (int i = 0; i < 2; ++i) {
+        mma(acc[i], hi, f[2 * i], f[2 * i + 1]);
+        mma(acc[i], lo, f[2 * i], f[2 * i + 1]);
+        mma(acc[i], hi, g[2 * i], g[2 * i + 1]);
     }
 }
 
 template <int DP, bool TERMS>  // TERMS: P in two terms
-__global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
+__global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) {
     extern __shared__ __align__(128) char raw[];
     PrepShared<DP> &sm = *reinterpret_cast<PrepShared<DP> *>(raw);
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, q2 = lane % 4 * 2;
     const int64_t at = blockIdx.x, bh = at / a.m;
     const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int rows = min(C, head_length(a.lengths, b, a.n) - t0);
     if (at == 0 && tid == 0) *a.status = 0;  // (the waits that set it run for a second)
     if (rows <= 0) return;
     const int hk = h / (a.H / a.k.heads);
-    const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q);
+    const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q), sA = smem_u32(sm.A);
     load_rows<DP>(sk, static_cast<const __nv_bfloat16 *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st, a.k.st, rows, a.d, tid, kPrepThreads);
     load_rows<DP>(sq, static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st, a.q.st, rows, a.d, tid, kPrepThreads);
     copies_end();
@@ -256,21 +263,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
         const float *m = sm.most[which];
         return scale_of(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
     };
-    Scale ks, qs;
-    {
-        uint4 wk[DP / 16], wq[DP / 16];
-        most_of(2, prep_most<DP>(sk, wk, tid));
-        most_of(3, prep_most<DP>(sq, wq, tid));
-        __syncthreads();
-        ks = block_scale(2);
-        qs = block_scale(3);
-        if (h % (a.H / a.k.heads) == 0) {  // one head of those that share queries and keys
-            const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-            prep_write<DP>(wk, ks.by, a.Kp + to * C * DP, tid);
-            prep_write<DP>(wq, qs.by, a.Qp + to * C * DP, tid);
-        }
-    }
-    float *rowf = a.rows + at * kRowsF;
+    most_of(2, prep_most<DP>(sk, tid));
+    most_of(3, prep_most<DP>(sq, tid));
 
     const int r0 = warp * 16;
     float kk[8][4], qk[8][4];
@@ -292,39 +286,29 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
             mma_bf16(qk[n0 / 8 + 1], fq, f[2], f[3]);
         }
     }
-    float most = 0.0f;
+    float most_p = 0.0f, most_a = 0.0f;
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = r0 + lane / 4 + half * 8, j = nt * 8 + lane % 4 * 2;
-            float w[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float c = j + e <= i ? expf((sm.hi[i] - sm.hi[j + e]) + (sm.lo[i] - sm.lo[j + e])) : 0.0f;
-                float &p = qk[nt][half * 2 + e];
-                p = j + e <= i ? a.scale * c * p : 0.0f;
-                most = fmaxf(most, fabsf(p));
-                w[e] = j + e < i ? sm.b[i] * c * kk[nt][half * 2 + e] : 0.0f;
-            }
-            *reinterpret_cast<float2 *>(&sm.A[i][j]) = make_float2(w[0], w[1]);
-            *reinterpret_cast<float2 *>(&sm.T[i][j]) = make_float2(0.0f, 0.0f);
+        for (int e = 0; e < 4; ++e) {
+            const int i = r0 + lane / 4 + (e >> 1) * 8, j = nt * 8 + q2 + (e & 1);
+            const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
+            qk[nt][e] = j <= i ? a.scale * c * qk[nt][e] : 0.0f;
+            kk[nt][e] = j < i ? sm.b[i] * c * kk[nt][e] : 0.0f;
+            most_p = fmaxf(most_p, fabsf(qk[nt][e]));
+            most_a = fmaxf(most_a, fabsf(kk[nt][e]));
+            if (nt / 2 == warp) sm.diag[warp][i - r0][j - r0] = kk[nt][e];
         }
-    most_of(0, most);
+    most_of(0, most_p);
+    most_of(1, most_a);
     __syncthreads();
-    const Scale ps = block_scale(0);
-    char *P = reinterpret_cast<char *>(a.Pp + at * (TERMS ? 2 : 1) * C * C);
-#pragma unroll
-    for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = r0 + lane / 4 + half * 8, j = nt * 8 + lane % 4 * 2;
-            uint32_t hi, lo;
-            split(ps.by * qk[nt][half * 2], ps.by * qk[nt][half * 2 + 1], hi, lo);
-            const uint32_t to = tile_at(0, C, i, nt) + lane % 4 * 4;
-            *reinterpret_cast<uint32_t *>(P + to) = hi;
-            if (TERMS) *reinterpret_cast<uint32_t *>(P + kTileB + to) = lo;
-        }
+    const Scale ps = block_scale(0), as = block_scale(1), ks = block_scale(2), qs = block_scale(3);
+    if (h % (a.H / a.k.heads) == 0) {  // one head of those that share queries and keys
+        const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+        prep_write<DP>(sk, ks.by, a.Kp + to * C * DP, tid);
+        prep_write<DP>(sq, qs.by, a.Qp + to * C * DP, tid);
+    }
+    float *rowf = a.rows + at * kRowsF;
     if (tid < C) {
         rowf[tid] = sm.past[tid] * ks.back;
         rowf[C + tid] = sm.left[tid] * ks.back;
@@ -337,48 +321,113 @@ __global__ void __launch_bounds__(kPrepThreads) k_delta_prepare(DeltaArgs a) {
         rowf[4 * C + 4] = ks.back;
         rowf[4 * C + 5] = qs.back;
     }
-    if (lane < 16) {
-        float x[16];
+    char *P = reinterpret_cast<char *>(a.Pp + at * (TERMS ? 2 : 1) * C * C);
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, nt) + q2 * 2;
+            uint32_t hi, lo;
+            split(ps.by * qk[nt][e], ps.by * qk[nt][e + 1], hi, lo);
+            *reinterpret_cast<uint32_t *>(P + to) = hi;
+            if (TERMS) *reinterpret_cast<uint32_t *>(P + kTileB + to) = lo;
+            if (nt / 2 >= warp) continue;  // (its diagonal block waits for T_II)
+            split(as.by * kk[nt][e], as.by * kk[nt][e + 1], hi, lo);
+            *reinterpret_cast<uint32_t *>(sm.A[0] + to) = hi;
+            *reinterpret_cast<uint32_t *>(sm.A[1] + to) = lo;
+        }
+    // T_II, a lane a column
+    {
+        float x[16], m = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = i == lane ? 1.0f : 0.0f;
 #pragma unroll
-            for (int l = 0; l < i; ++l) x[i] = fmaf(-sm.A[r0 + i][r0 + l], x[l], x[i]);
-            sm.T[r0 + i][r0 + lane] = x[i];
+            for (int l = 0; l < i; ++l) x[i] = fmaf(-sm.diag[warp][i][l], x[l], x[i]);
+            m = fmaxf(m, fabsf(x[i]));
+        }
+        const Scale s = scale_of(warp_max(m));  // (the lanes without a column hold zeros)
+        if (lane == 0) sm.back_T[warp] = s.back;
+        if (lane < 16)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float y = s.by * x[i];
+                const __half hi = __float2half_rn(y), lo = __float2half_rn(y - __half2float(hi));
+                const uint32_t to = tile_at(0, C, r0 + i, (r0 + lane) >> 3) + (lane & 7) * 2;
+                *reinterpret_cast<__half *>(sm.A[0] + to) = hi;
+                *reinterpret_cast<__half *>(sm.A[1] + to) = lo;
+                sm.diag[warp][i][lane] = x[i];
+            }
+    }
+    __syncthreads();
+    // block column J = warp of T, transposed: rows j, columns i
+    float T[4][2][4];
+    Frag hi[3], lo[3];
+    float back[3];
+#pragma unroll
+    for (int I = 0; I < 4; ++I) zero(T[I]);
+    left_k(hi[0], sA, C, r0, r0, lane);
+    left_k(lo[0], sA + kTileB, C, r0, r0, lane);
+    back[0] = sm.back_T[warp];
+#pragma unroll
+    for (int s = 1; s < 4; ++s) {
+        const int I = warp + s;
+        if (I > 3) break;
+        float acc[2][4], y[2][4];
+        zero(acc);
+#pragma unroll
+        for (int t = 0; t < s; ++t) {
+            zero(y);
+            prep_product(y, hi[t], lo[t], sA, I * 16, r0 + t * 16, lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(back[t] * as.back, y[i][e], acc[i][e]);
+        }
+        const Scale sc = scale_of(acc);
+        Frag fh, fl;
+        split_left(acc[0], acc[1], sc.by, fh, fl);
+        zero(y);
+        prep_product(y, fh, fl, sA, I * 16, I * 16, lane);
+        const float by = -sc.back * sm.back_T[I];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) T[s][i][e] = by * y[i][e];
+        if (s < 3) {
+            const Scale st = scale_of(T[s]);
+            split_left(T[s][0], T[s][1], st.by, hi[s], lo[s]);
+            back[s] = st.back;
         }
     }
-    __syncthreads();
-    // T21 = -T22 (A21 T11), with A21 T11 above A's diagonal, where nothing is needed
-    auto A = [&](int r, int c) { return &sm.A[r][c]; };
-    auto T = [&](int r, int c) { return &sm.T[r][c]; };
-    const int o = warp / 2 * 32, t64 = tid % 64;
-    prep_product<16>(A(o, o + 16), A(o + 16, o), T(o, o), 1.0f, t64, 64);
-    __syncthreads();
-    prep_product<16>(T(o + 16, o), T(o + 16, o + 16), A(o, o + 16), -1.0f, t64, 64);
-    __syncthreads();
-    prep_product<32>(A(0, 32), A(32, 0), T(0, 0), 1.0f, tid, kPrepThreads);
-    __syncthreads();
-    prep_product<32>(T(32, 0), T(32, 32), A(0, 32), -1.0f, tid, kPrepThreads);
-    __syncthreads();
-    float2 x[C * C / 2 / kPrepThreads];
-    most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i) {
-        const int p = tid + i * kPrepThreads;
-        x[i] = *reinterpret_cast<const float2 *>(&sm.T[p / (C / 2)][p % (C / 2) * 2]);
-        most = fmaxf(most, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
-    }
-    most_of(1, most);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) T[0][i][e] = sm.diag[warp][i * 8 + q2 + (e & 1)][lane / 4 + (e >> 1) * 8];
+    float m = 0.0f;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(T[s][i][e]));
+    most_of(4, m);
     __syncthreads();
-    const Scale ts = block_scale(1);
+    const Scale ts = block_scale(4);
     if (tid == 0) rowf[4 * C + 2] = ts.back;
     char *planes = reinterpret_cast<char *>(a.Tp + at * 2 * C * C);
 #pragma unroll
-    for (int i = 0; i < C * C / 2 / kPrepThreads; ++i) {
-        const int p = tid + i * kPrepThreads, j = p % (C / 2) * 2;
-        const uint32_t to = tile_at(0, C, p / (C / 2), j >> 3) + (j & 7) * 2;
-        split(ts.by * x[i].x, ts.by * x[i].y, *reinterpret_cast<uint32_t *>(planes + to), *reinterpret_cast<uint32_t *>(planes + kTileB + to));
-    }
+    for (int s = 0; s < 4; ++s)  // (block row J + s, or the empty ones before J)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                uint32_t th, tl;
+                split(ts.by * T[s][i][e], ts.by * T[s][i][e + 1], th, tl);
+                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, (warp + s) % 4 * 2 + i) + q2 * 2;
+                *reinterpret_cast<uint32_t *>(planes + to) = th;
+                *reinterpret_cast<uint32_t *>(planes + kTileB + to) = tl;
+            }
 }
 
 // ---------------------------------------------------------------------------
@@ -590,12 +639,12 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
                 for (int np = kt; np < 4; ++np) {
                     Frag f;
-                    right_n(f, sT, C, np * 16, kt * 16, lane);
+                    right_k(f, sT, C, kt * 16, np * 16, lane);
                     mma(u[2 * np], hi, f[0], f[1]);
                     mma(u[2 * np + 1], hi, f[2], f[3]);
                     mma(u[2 * np], lo, f[0], f[1]);
                     mma(u[2 * np + 1], lo, f[2], f[3]);
-                    right_n(f, sT + kTileB, C, np * 16, kt * 16, lane);
+                    right_k(f, sT + kTileB, C, kt * 16, np * 16, lane);
                     mma(u[2 * np], hi, f[0], f[1]);
                     mma(u[2 * np + 1], hi, f[2], f[3]);
                 }
@@ -706,12 +755,12 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
                 for (int np = 0; np <= kt; ++np) {
                     Frag f;
-                    right_k(f, sT, C, kt * 16, np * 16, lane);
+                    right_n(f, sT, C, np * 16, kt * 16, lane);
                     mma(y[2 * np], hi, f[0], f[1]);
                     mma(y[2 * np + 1], hi, f[2], f[3]);
                     mma(y[2 * np], lo, f[0], f[1]);
                     mma(y[2 * np + 1], lo, f[2], f[3]);
-                    right_k(f, sT + kTileB, C, kt * 16, np * 16, lane);
+                    right_n(f, sT + kTileB, C, np * 16, kt * 16, lane);
                     mma(y[2 * np], hi, f[0], f[1]);
                     mma(y[2 * np + 1], hi, f[2], f[3]);
                 }
@@ -763,11 +812,11 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X and states.  A block of eight warps a chunk:
-// four groups of 16 rows by two halves of the columns.  What is summed over the columns of the state comes 16 of them at
+// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X and states.  A block of 16 warps a chunk:
+// four groups of 16 rows by four quarters of the columns.  What is summed over the columns of the state comes 16 of them at
 // a time, with what those were scaled down by.
 
-constexpr int kGradThreads = 256;
+constexpr int kGradThreads = 512, kParts = 4;
 
 template <int DP, int DVT>
 struct GradShared {
@@ -776,9 +825,9 @@ struct GradShared {
     uint64_t bar[2];
     float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales];
     float steps[5][DVT / 16], all[5];  // of the products over columns: 16 columns' scale over the largest, that
-    // of a row's two halves of the columns: q . dQ, k . Z without the rows' part, k . (what it wrote) without and with
+    // of a row's quarters of the columns: q . dQ, k . Z without the rows' part, k . (what it wrote) without and with
     // the rows' part, W . K K^T, x . v, b k . Z
-    float sums[7][2][C];
+    float sums[7][kParts][C];
     float most[2][kGradThreads / 32], total[kGradThreads / 32], read[C], wrote[C], wstate[C];
 };
 
@@ -798,9 +847,9 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     using Sh = GradShared<DP, DVT>;
     extern __shared__ __align__(128) char raw[];
     Sh &sm = *reinterpret_cast<Sh *>(raw);
-    using Acc = float[DP / 16][4];
-    constexpr int NT = DP / 16;  // n-tiles of a warp's half of the columns of dQ, dK
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 4 * 16, half = warp / 4, q2 = lane % 4 * 2;
+    using Acc = float[DP / 32][4];
+    constexpr int NT = DP / 32;  // n-tiles of a warp's quarter of the columns of dQ, dK
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 4 * 16, quarter = warp / 4, q2 = lane % 4 * 2;
     const int64_t at = blockIdx.x, bh = at / a.m;
     const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int rows = max(0, min(C, head_length(a.lengths, b, a.n) - t0)), out_rows = min(C, a.n - t0);
@@ -854,11 +903,11 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
     // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U, dO S, X S, U R.
     if (tid < 5) {
-        const int l[5] = {4, 3, 4, 3, 2}, r[5] = {2, 2, 0, 0, 1};
+        const int l = tid == 4 ? 2 : 4 - tid % 2, r = tid == 4 ? 1 : tid < 2 ? 2 : 0;
         float most = 0.0f;
-        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, sm.scales[kt][l[tid]] * sm.scales[kt][r[tid]]);
+        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, sm.scales[kt][l] * sm.scales[kt][r]);
         sm.all[tid] = most;
-        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = most > 0.0f ? sm.scales[kt][l[tid]] * sm.scales[kt][r[tid]] / most : 0.0f;
+        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = most > 0.0f ? sm.scales[kt][l] * sm.scales[kt][r] / most : 0.0f;
     }
     here = mbar_wait_long(&sm.bar[1], 0) && here;
     if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
@@ -887,7 +936,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
             memcpy(&f[i], &x, 4);
         }
     };
-    // sums over the four lanes of a row, for this half of the columns: rows lane / 4 and 8 more
+    // sums over the four lanes of a row, for this quarter of the columns: rows lane / 4 and 8 more
     auto row_sums = [&](float (&x)[2], int which) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -895,53 +944,44 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
             x[i] += __shfl_xor_sync(0xffffffffu, x[i], 2);
         }
         if (lane % 4 == 0) {
-            sm.sums[which][half][r0 + lane / 4] = x[0];
-            sm.sums[which][half][r0 + lane / 4 + 8] = x[1];
+            sm.sums[which][quarter][r0 + lane / 4] = x[0];
+            sm.sums[which][quarter][r0 + lane / 4 + 8] = x[1];
         }
     };
 
-    {  // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 32 columns a warp; W . K K^T for db
-        float p[4][4], w[4][4], kk[4][4];
+    {  // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 16 columns a warp; W . K K^T for db
+        float p[2][4], w[2][4], kk[2][4];
         zero(p);
         zero(w);
         zero(kk);
+        const int n0 = quarter * 16;
+        if (n0 <= r0) {
 #pragma unroll 2
-        for (int kt = 0; kt < groups; ++kt) {
-            Frag fg, fx;
-            left_go(fg, kt, 0);
-            left_plane(fx, sx, kt, 1);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int n0 = half * 32 + n * 16;
-                if (n0 > r0) continue;
-                Frag f;
+            for (int kt = 0; kt < groups; ++kt) {
+                Frag fg, fx, f;
+                left_go(fg, kt, 0);
+                left_plane(fx, sx, kt, 1);
                 right_k(f, su, dvp, kt * 16, n0, lane);
-                mma(p[2 * n], fg, f[0], f[1]);
-                mma(p[2 * n + 1], fg, f[2], f[3]);
-                mma(w[2 * n], fx, f[0], f[1]);
-                mma(w[2 * n + 1], fx, f[2], f[3]);
+                mma(p[0], fg, f[0], f[1]);
+                mma(p[1], fg, f[2], f[3]);
+                mma(w[0], fx, f[0], f[1]);
+                mma(w[1], fx, f[2], f[3]);
             }
-        }
 #pragma unroll
-        for (int k0 = 0; k0 < DP; k0 += 16) {
-            Frag fk;
-            left_m(fk, sk, C, r0, k0, lane);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int n0 = half * 32 + n * 16;
-                if (n0 > r0) continue;
-                Frag f;
+            for (int k0 = 0; k0 < DP; k0 += 16) {
+                Frag fk, f;
+                left_m(fk, sk, C, r0, k0, lane);
                 right_n(f, sk, C, n0, k0, lane);
-                mma(kk[2 * n], fk, f[0], f[1]);
-                mma(kk[2 * n + 1], fk, f[2], f[3]);
+                mma(kk[0], fk, f[0], f[1]);
+                mma(kk[1], fk, f[2], f[3]);
             }
         }
         float dot[2] = {0.0f, 0.0f}, mp = 0.0f, mw = 0.0f;
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+        for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int i = r0 + lane / 4 + (e >> 1) * 8, j = half * 32 + nt * 8 + q2 + (e & 1);
+                const int i = r0 + lane / 4 + (e >> 1) * 8, j = n0 + nt * 8 + q2 + (e & 1);
                 const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
                 p[nt][e] = j <= i ? a.scale * sm.all[0] * c * p[nt][e] : 0.0f;
                 w[nt][e] = j < i ? sm.all[1] * c * w[nt][e] : 0.0f;
@@ -966,21 +1006,21 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
         }
         const float bp = scale_of(mp).by, bw = scale_of(mw).by;
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+        for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
-                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, half * 4 + nt) + q2 * 2;
+                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, quarter * 2 + nt) + q2 * 2;
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(bp * p[nt][e], bp * p[nt][e + 1])) : "memory");
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(bw * w[nt][e], bw * w[nt][e + 1])) : "memory");
             }
     }
-    // x . v: a thread a row and a quarter of the columns (joined two and two)
+    // x . v: a thread a row and an eighth of the columns (joined two and two)
     {
         const int i = tid % C, part = tid / C;
         const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
         float acc = 0.0f;
         if (i < rows)
-            for (int c8 = part; c8 < a.dv / 8; c8 += 4) {
+            for (int c8 = part; c8 < a.dv / 8; c8 += 2 * kParts) {
                 const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
                 const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
                 float sum = 0.0f;
@@ -992,10 +1032,10 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
                 }
                 acc = fmaf(sm.scales[c8 / 2][3], sum, acc);
             }
-        // (the two quarters of a sums[5] entry meet in two steps)
-        if (part >= 2) sm.sums[5][part - 2][i] = acc;
+        // (the two eighths of a sums[5] entry meet in two steps)
+        if (part >= kParts) sm.sums[5][part - kParts][i] = acc;
         __syncthreads();
-        if (part < 2) sm.sums[5][part][i] += acc;
+        if (part < kParts) sm.sums[5][part][i] += acc;
     }
     float back_p = 0.0f, back_w = 0.0f;
     {
@@ -1009,7 +1049,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
         back_w = scale_of(mw).back;
     }
 
-    const int c0 = half * (DP / 2);  // first column of the warp's
+    const int c0 = quarter * (DP / 4);  // first column of the warp's
     const int ra = r0 + lane / 4, rb = ra + 8;
     // acc += F M over the columns of the state: F by left(f, kt), M a tile of S or R
     auto over_columns = [&](Acc &acc, uint32_t tile, auto left) {
@@ -1135,7 +1175,9 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     if (lane == 0) sm.total[warp] = total;
     __syncthreads();
     if (tid < rows) {
-        auto sum = [&](int which) { return sm.sums[which][0][tid] + sm.sums[which][1][tid]; };
+        auto sum = [&](int which) {
+            return (sm.sums[which][0][tid] + sm.sums[which][1][tid]) + (sm.sums[which][2][tid] + sm.sums[which][3][tid]);
+        };
         io_store(db + tid * a.db.st, sum(5) - sum(1) - back_k * back_k * sum(4));
         sm.read[tid] = sum(0) - sum(6);
         sm.wrote[tid] = sum(3);
