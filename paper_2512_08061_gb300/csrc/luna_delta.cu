@@ -185,7 +185,7 @@ struct GradShared {
     float A[kDeltaRows][kGradK + 1], B[kGradK][kMaxD + 1];
     float P[kDeltaRows][kDeltaRows + 1], W[kDeltaRows][kDeltaRows + 1];
     float hi[kDeltaRows], lo[kDeltaRows], b[kDeltaRows], past[kDeltaRows], left[kDeltaRows];
-    float read[kDeltaRows], wrote[kDeltaRows], wstate[kDeltaRows], total[kGradThreads / 32];
+    float read[kDeltaRows], wrote[kDeltaRows], total[kGradThreads / 32];
 };
 
 // acc[r][c] += sum_k A(ty * 4 + r, k) B(k, tx + 16 c); BT: B is stored with k contiguous
@@ -252,6 +252,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     if (rows == 0) return;
     const int64_t E = (int64_t)a.d * a.dv;
     const float *S = a.before + (bh * (a.m + 1) + chunk) * E, *R = a.after + (bh * (a.m + 1) + chunk + 1) * E;
+    const float *R0 = a.after + (bh * (a.m + 1) + chunk) * E;  // before the chunk
     const float *U = a.U + (bh * a.n + t0) * a.dv, *X = a.X + (bh * a.n + t0) * a.dv;
     const int d = a.d, dv = a.dv;
 
@@ -261,7 +262,6 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     else if (tid < 32 + C)
         sm.b[tid - 32] = tid - 32 < rows ? gate_at<IO>(a.b, b, h, t0 + tid - 32) : 0.0f;
     __syncthreads();
-    const float whole = sm.past[C - 1];
     auto gap = [&](int i, int j) { return expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])); };
     auto at = [&](const IO *x, int64_t st, int t, int c, int w) { return t < rows && c < w ? io_load(x + t * st + c) : 0.0f; };
     auto in = [&](const float *x, int t, int c) { return t < rows && c < dv ? x[(int64_t)t * dv + c] : 0.0f; };
@@ -355,23 +355,21 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     // dK
     zero(acc);
     grad_product<true>(sm, acc, dv, [&](int r, int kk) { return in(U, r, kk); }, fR);
-    for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = ty * 4 + r;
-            float dot = 0.0f;
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (pass == 0) acc[r][c] *= sm.left[i];
-                if (i < rows && tx + 16 * c < d) dot = fmaf(io_load(k + i * a.k.st + tx + 16 * c), acc[r][c], dot);
-            }
-            dot = rowsum(dot);
-            if (tx == 0) (pass == 0 ? sm.wstate : sm.wrote)[i] = dot;
-        }
-        if (pass == 0) {
-            grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[kk][r]; }, fQ);
-            grad_product<false>(sm, acc, C, [&](int r, int kk) { return -sm.b[kk] * sm.W[kk][r]; }, fK);
-        }
+        for (int c = 0; c < NC; ++c) acc[r][c] *= sm.left[ty * 4 + r];
+    grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[kk][r]; }, fQ);
+    grad_product<false>(sm, acc, C, [&](int r, int kk) { return -sm.b[kk] * sm.W[kk][r]; }, fK);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = ty * 4 + r;
+        float dot = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (i < rows && tx + 16 * c < d) dot = fmaf(io_load(k + i * a.k.st + tx + 16 * c), acc[r][c], dot);
+        dot = rowsum(dot);
+        if (tx == 0) sm.wrote[i] = dot;
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -380,9 +378,9 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         for (int c = 0; c < NC; ++c)
             if (i < rows && tx + 16 * c < d) io_store(dk + i * a.dkt + tx + 16 * c, fmaf(-sm.b[i], z[r][c], acc[r][c]));
     }
-    // dg: what passes row t of <S, R> and of the pairs of rows
+    // dg
     float pass = 0.0f;
-    for (int64_t i = tid; i < E; i += kGradThreads) pass = fmaf(S[i], R[i], pass);
+    for (int64_t i = tid; i < E; i += kGradThreads) pass = fmaf(S[i], R0[i], pass);
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) pass += __shfl_xor_sync(0xffffffffu, pass, w);
     if (tid % 32 == 0) sm.total[tid / 32] = pass;
@@ -390,7 +388,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     if (tid < 32) {
         float all = 0.0f;
         for (int w = 0; w < kGradThreads / 32; ++w) all += sm.total[w];
-        delta_gate_grads(all * whole, sm.read, sm.wrote, sm.wstate, rows, tid, [&](int t, float x) {
+        delta_gate_grads(all, sm.read, sm.wrote, rows, tid, [&](int t, float x) {
             io_store(dg + t * a.dg.st, expf(gate_at<IO>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
         });
     }

@@ -58,9 +58,9 @@ struct DeltaArgs {
     float *before, *after;  // states before chunk i, gradients of the states before chunk i, [B H][m + 1][d][dv]
     // tensor-core form (fp16, scaled; dvp: dv to a multiple of 16, dp: d to 64 or 128), for every chunk: its rows of K
     // and Q ([B Hk][m][64][dp]), the inverse T, transposed, in two planes and the scores P in `planes` of them ([64][64] each),
-    // factors of its rows; and for every 16 columns of a chunk U and X ([16][64], transposed), the states at its two
-    // ends (S before, R behind; [16][dp], transposed), and what S, R, U, X and dO were scaled down by
-    __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Sp, *Rp;
+    // factors of its rows; and for every 16 columns of a chunk U, X and dO ([16][64], transposed), the states at its
+    // two ends (S before, R behind; [16][dp], transposed), what S, R, U, X and dO were scaled down by, and <S, R> before it
+    __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Gp, *Sp, *Rp;
     float *rows, *scales;
     int planes, dvp;
     int *status;            // the call's status word
@@ -126,30 +126,27 @@ __device__ __forceinline__ void delta_gate_sums(int lane, F gate, float *hi, flo
     }
 }
 
-// dg of a chunk's rows, by one warp: `base` is what the states at the chunk's ends give across all of it, read_i
-// what row i's reads of S and of the rows before it give to the gates up to i, wrote_j what the reads of row j give
-// (they do not cross the gates up to j), wstate_j the part of wrote_j that is read behind the chunk.
+// dg of a chunk's rows, by one warp: `base` = <S, R> of the states before the chunk is that of its first row (and more:
+// what R takes from all rows behind), read_i what row i's reads give to the gates up to i, wrote_j what the reads of row
+// j give, which do not cross the gates up to j; each row's dg is the one's before it less read - wrote of that row.
 template <typename F>
-__device__ __forceinline__ void delta_gate_grads(float base, const float *read, const float *wrote, const float *wstate,
-                                                 int rows, int lane, F store) {
-    float x[2], tail = 0.0f, state = 0.0f;
+__device__ __forceinline__ void delta_gate_grads(float base, const float *read, const float *wrote, int rows, int lane, F store) {
+    float x[2], head = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int t = 2 * lane + i;
         x[i] = t < rows ? read[t] - wrote[t] : 0.0f;
-        state += t < rows ? wstate[t] : 0.0f;
-        tail += x[i];
+        head += x[i];
     }
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) {
-        state += __shfl_xor_sync(0xffffffffu, state, w);
-        const float up = __shfl_down_sync(0xffffffffu, tail, w);
-        if (lane + w < 32) tail += up;
+        const float up = __shfl_up_sync(0xffffffffu, head, w);
+        if (lane >= w) head += up;
     }
-    tail = __shfl_down_sync(0xffffffffu, tail, 1);  // the rows behind this lane's
-    base += state + (lane < 31 ? tail : 0.0f);
-    if (2 * lane + 1 < rows) store(2 * lane + 1, base + x[1]);
-    if (2 * lane < rows) store(2 * lane, base + x[1] + x[0]);
+    head = __shfl_up_sync(0xffffffffu, head, 1);  // the rows before this lane's
+    base -= lane > 0 ? head : 0.0f;
+    if (2 * lane < rows) store(2 * lane, base);
+    if (2 * lane + 1 < rows) store(2 * lane + 1, base - x[0]);
 }
 
 cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s);

@@ -59,7 +59,7 @@ struct Plan {
     size_t dq = 0, dk = 0;                          // gradients of shared queries and keys, one for each head
     size_t U = 0, X = 0, before = 0, after = 0;      // CUDA-core form
     size_t K = 0, Q = 0, T = 0, P = 0, rows = 0;     // tensor-core form, in a forward pass too
-    size_t Up = 0, Xp = 0, Sp = 0, Rp = 0, scales = 0;  // (gradients)
+    size_t Up = 0, Xp = 0, Gp = 0, Sp = 0, Rp = 0, scales = 0;  // (gradients)
     size_t fwd = 256, bwd = 256;
 };
 
@@ -87,6 +87,7 @@ Plan make_plan(const luna_delta_desc *dd) {
         take(chunks * 2 * tile);  // (in two planes)
         p.Up = take(chunks * p.dvp * kDeltaRows * 2);
         p.Xp = take(chunks * p.dvp * kDeltaRows * 2);
+        p.Gp = take(chunks * p.dvp * kDeltaRows * 2);
         p.Sp = take(chunks * p.dvp * p.dp * 2);
         p.Rp = take(chunks * p.dvp * p.dp * 2);
         p.scales = take(chunks * (p.dvp / 16) * kDeltaScales * 4);
@@ -139,7 +140,7 @@ void tc_parts(DeltaArgs &a, const Plan &p, char *ws, bool backward) {
     a.Kp = at(p.K); a.Qp = at(p.Q); a.Tp = at(p.T); a.Pp = at(p.P);
     a.planes = backward ? 2 : 1;
     if (!backward) return;
-    a.Up = at(p.Up); a.Xp = at(p.Xp); a.Sp = at(p.Sp); a.Rp = at(p.Rp);
+    a.Up = at(p.Up); a.Xp = at(p.Xp); a.Gp = at(p.Gp); a.Sp = at(p.Sp); a.Rp = at(p.Rp);
     a.scales = reinterpret_cast<float *>(ws + p.scales);
 }
 

@@ -122,12 +122,15 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+__device__ __forceinline__ float2 half_pair(uint32_t u) {
+    __half2 h;
+    memcpy(&h, &u, 4);
+    return __half22float2(h);
+}
 // x = hi + lo to 22 bits
 __device__ __forceinline__ void split(float x0, float x1, uint32_t &hi, uint32_t &lo) {
     hi = pack(x0, x1);
-    __half2 h;
-    memcpy(&h, &hi, 4);
-    const float2 f = __half22float2(h);
+    const float2 f = half_pair(hi);
     lo = pack(x0 - f.x, x1 - f.y);
 }
 // The power of two that takes a largest value of 2^E (to 2^(E+1)) to 2^12, and its inverse.  (Below 2^-113 all is 0.)
@@ -559,7 +562,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
         auto factor = [&](int which, int t) { return *reinterpret_cast<const float2 *>(st.rows + which * C + t); };
         const int64_t group = (bh * a.m + chunk) * (a.dvp / 16) + col / 16;  // the warp's columns in the planes
         __half *keep = planes ? planes + (bh * a.m + chunk) * a.dvp * C : nullptr;
-        float *scales = a.scales ? a.scales + group * kDeltaScales : nullptr;  // S, R, U, X, dO
+        float *scales = a.scales ? a.scales + group * kDeltaScales : nullptr;  // S, R, U, X, dO; <S, R>
         // S <- c(C, 0) S (first) + F M for a left operand F of 64 summed rows and the tile M (a row for each)
         auto update = [&](const Frag (&fh)[4], const Frag (&fl)[4], float back, uint32_t tile, bool decay) {
 #pragma unroll
@@ -724,6 +727,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                     gf[i] = pack(gs.by * g0, gs.by * g1);
                     split(ps.by * (past.x * g0), ps.by * (past.y * g1), fh[kt][i], fl[kt][i]);
                 }
+                plane_store(a.Gp + (bh * a.m + chunk) * a.dvp * C, a.dvp, col, kt * 16, gf, lane);
 #pragma unroll
                 for (int np = 0; np <= kt; ++np) {
                     Frag f;
@@ -792,6 +796,20 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) split_left(x[2 * kt], x[2 * kt + 1], ws.by, fh[kt], fl[kt]);
             update(fh, fl, ws.back, sk, false);
+            {  // <S, R> before the chunk
+                const char *p = reinterpret_cast<const char *>(a.Sp + (bh * a.m + chunk) * a.dvp * DP) + q2 * 2;
+                float sum = 0.0f;
+#pragma unroll
+                for (int nt = 0; nt < ND; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float2 f = half_pair(*reinterpret_cast<const uint32_t *>(p + tile_at(0, a.dvp, col + lane / 4 + i * 8, nt)));
+                        sum = fmaf(f.x, S[nt][2 * i], fmaf(f.y, S[nt][2 * i + 1], sum));
+                    }
+#pragma unroll
+                for (int w = 16; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                if (lane == 0) scales[5] = scales[0] * sum;
+            }
             chain_store(y, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
         }
     }
@@ -812,44 +830,36 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X and states.  A block of 16 warps a chunk:
-// four groups of 16 rows by four quarters of the columns.  What is summed over the columns of the state comes 16 of them at
-// a time, with what those were scaled down by.
+// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X, dO and states.  A block of eight warps a chunk:
+// two groups of 32 rows by four quarters of the columns.  102 KB of shared memory, so that two blocks are on an SM and
+// the one's products cover the other's loads: R, then S, then Q lie in the same place, P and W in that of U.
 
-constexpr int kGradThreads = 512, kParts = 4;
+constexpr int kGradThreads = 256, kParts = 4;
 
 template <int DP, int DVT>
 struct GradShared {
-    alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], go[DVT / 64][kTileB], u[DVT * 128], x[DVT * 128];
-    alignas(128) char s[DVT * DP * 2], r[DVT * DP * 2], P[kTileB], W[kTileB];
-    uint64_t bar[2];
+    alignas(128) char k[DP / 64][kTileB], go[DVT * 128], x[DVT * 128], u[DVT * 128 > 2 * kTileB ? DVT * 128 : 2 * kTileB];
+    alignas(128) char s[DVT * DP * 2 > DP / 64 * kTileB ? DVT * DP * 2 : DP / 64 * kTileB];
+    uint64_t bar[4];
     float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales];
-    float steps[5][DVT / 16], all[5];  // of the products over columns: 16 columns' scale over the largest, that
-    // of a row's quarters of the columns: q . dQ, k . Z without the rows' part, k . (what it wrote) without and with
-    // the rows' part, W . K K^T, x . v, b k . Z
-    float sums[7][kParts][C];
-    float most[2][kGradThreads / 32], total[kGradThreads / 32], read[C], wrote[C], wstate[C];
+    __half2 steps[5][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
+    float all[5];
+    float sums[6][kParts][C];  // of a row's quarters: q . dQ, k . Z without the rows' part, k . (dK), W . K K^T, x . v, b k . Z
+    float most[2][kGradThreads / 32], read[C], wrote[C];
 };
 
 __device__ __forceinline__ float inverse2(float back) {  // of a power of two
     return __uint_as_float((254u << 23) - __float_as_uint(back));
 }
-__device__ __forceinline__ float2 half_pair(uint32_t tile, int rows, int r, int c) {
-    uint32_t u;
-    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(tile_at(tile, rows, r, c >> 3) + (c & 7) * 2));
-    __half2 h;
-    memcpy(&h, &u, 4);
-    return __half22float2(h);
-}
 
 template <int DP, int DVT, typename OUT>
-__global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
+__global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) {
     using Sh = GradShared<DP, DVT>;
+    using Acc = float[2][DP / 32][4];
     extern __shared__ __align__(128) char raw[];
     Sh &sm = *reinterpret_cast<Sh *>(raw);
-    using Acc = float[DP / 32][4];
     constexpr int NT = DP / 32;  // n-tiles of a warp's quarter of the columns of dQ, dK
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 4 * 16, quarter = warp / 4, q2 = lane % 4 * 2;
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 2 * 32, quarter = warp / 2, q2 = lane % 4 * 2;
     const int64_t at = blockIdx.x, bh = at / a.m;
     const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int rows = max(0, min(C, head_length(a.lengths, b, a.n) - t0)), out_rows = min(C, a.n - t0);
@@ -869,26 +879,26 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     }
     if (rows == 0) return;
 
-    const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q), sgo = smem_u32(sm.go), su = smem_u32(sm.u), sx = smem_u32(sm.x);
-    const uint32_t ss = smem_u32(sm.s), sr = smem_u32(sm.r), sP = smem_u32(sm.P), sW = smem_u32(sm.W);
+    const uint32_t sk = smem_u32(sm.k), sgo = smem_u32(sm.go), su = smem_u32(sm.u), sx = smem_u32(sm.x), ss = smem_u32(sm.s);
+    const uint32_t sP = su, sW = su + kTileB;
     const int dvp = a.dvp, groups = dvp / 16;
     const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-    if (tid < 2) mbar_init(&sm.bar[tid], 1);
+    const uint32_t of_rows = dvp * C * 2, of_state = dvp * DP * 2;
+    if (tid < 4) mbar_init(&sm.bar[tid], 1);
     fence_mbar_init();
     __syncthreads();
+    auto load_state = [&](const void *src, uint32_t bytes, int which) {  // (one thread)
+        mbar_arrive_expect_tx(&sm.bar[which], bytes);
+        load_tile(sm.s, src, bytes, &sm.bar[which]);
+    };
     if (tid == 0) {
-        const uint32_t ux = dvp * C * 2, sr_ = dvp * DP * 2;
-        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 2 * ux);
-        load_tile(sm.u, a.Up + at * dvp * C, ux, &sm.bar[0]);
-        load_tile(sm.x, a.Xp + at * dvp * C, ux, &sm.bar[0]);
+        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 3 * of_rows);
+        load_tile(sm.u, a.Up + at * dvp * C, of_rows, &sm.bar[0]);
+        load_tile(sm.x, a.Xp + at * dvp * C, of_rows, &sm.bar[0]);
+        load_tile(sm.go, a.Gp + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.k, a.Kp + kat * C * DP, sizeof(sm.k), &sm.bar[0]);
-        mbar_arrive_expect_tx(&sm.bar[1], sizeof(sm.q) + 2 * sr_);
-        load_tile(sm.s, a.Sp + at * dvp * DP, sr_, &sm.bar[1]);
-        load_tile(sm.q, a.Qp + kat * C * DP, sizeof(sm.q), &sm.bar[1]);
-        load_tile(sm.r, a.Rp + at * dvp * DP, sr_, &sm.bar[1]);
+        load_state(a.Rp + at * dvp * DP, of_state, 1);
     }
-    load_rows<DVT>(sgo, static_cast<const __nv_bfloat16 *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st, a.go.st, rows, a.dv, tid, kGradThreads);
-    copies_end();
     const float *rowf = a.rows + at * kRowsF;
     const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
     if (warp == 0)
@@ -897,8 +907,6 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
     else if (warp < 3)
         sm.b[tid - 32] = rowf[2 * C + tid - 32];
     for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[at * groups * kDeltaScales + i];
-    copies_wait<0>();
-    bool here = mbar_wait_long(&sm.bar[0], 0);
     __syncthreads();
     // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
     // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U, dO S, X S, U R.
@@ -907,120 +915,18 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
         float most = 0.0f;
         for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, sm.scales[kt][l] * sm.scales[kt][r]);
         sm.all[tid] = most;
-        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = most > 0.0f ? sm.scales[kt][l] * sm.scales[kt][r] / most : 0.0f;
+        for (int kt = 0; kt < groups; ++kt)
+            sm.steps[tid][kt] = __float2half2_rn(most > 0.0f ? sm.scales[kt][l] * sm.scales[kt][r] / most : 0.0f);
     }
-    here = mbar_wait_long(&sm.bar[1], 0) && here;
-    if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
-        if (tid == 0) {
-            atomicOr(a.status, 1);
-            for (int i = 0; i < 2; ++i) mbar_wait(&sm.bar[i], 0, kDrainNs);
-        }
-        return;
-    }
-
-    // left operands: 16 rows and 16 columns of dO in fp16; of X, U
-    auto left_go = [&](Frag &f, int kt, int product) {
-        left_m(f, sgo, C, r0, kt * 16, lane);
-        const float by = inverse2(sm.scales[kt][4]) * sm.steps[product][kt];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = pack(by * low(f[i]), by * high(f[i]));
-    };
-    auto left_plane = [&](Frag &f, uint32_t tile, int kt, int product) {
-        left_k(f, tile, dvp, kt * 16, r0, lane);
-        const __half2 by = __float2half2_rn(sm.steps[product][kt]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            __half2 x;
-            memcpy(&x, &f[i], 4);
-            x = __hmul2(x, by);
-            memcpy(&f[i], &x, 4);
-        }
-    };
-    // sums over the four lanes of a row, for this quarter of the columns: rows lane / 4 and 8 more
-    auto row_sums = [&](float (&x)[2], int which) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            x[i] += __shfl_xor_sync(0xffffffffu, x[i], 1);
-            x[i] += __shfl_xor_sync(0xffffffffu, x[i], 2);
-        }
-        if (lane % 4 == 0) {
-            sm.sums[which][quarter][r0 + lane / 4] = x[0];
-            sm.sums[which][quarter][r0 + lane / 4 + 8] = x[1];
-        }
-    };
-
-    {  // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 16 columns a warp; W . K K^T for db
-        float p[2][4], w[2][4], kk[2][4];
-        zero(p);
-        zero(w);
-        zero(kk);
-        const int n0 = quarter * 16;
-        if (n0 <= r0) {
-#pragma unroll 2
-            for (int kt = 0; kt < groups; ++kt) {
-                Frag fg, fx, f;
-                left_go(fg, kt, 0);
-                left_plane(fx, sx, kt, 1);
-                right_k(f, su, dvp, kt * 16, n0, lane);
-                mma(p[0], fg, f[0], f[1]);
-                mma(p[1], fg, f[2], f[3]);
-                mma(w[0], fx, f[0], f[1]);
-                mma(w[1], fx, f[2], f[3]);
-            }
-#pragma unroll
-            for (int k0 = 0; k0 < DP; k0 += 16) {
-                Frag fk, f;
-                left_m(fk, sk, C, r0, k0, lane);
-                right_n(f, sk, C, n0, k0, lane);
-                mma(kk[0], fk, f[0], f[1]);
-                mma(kk[1], fk, f[2], f[3]);
-            }
-        }
-        float dot[2] = {0.0f, 0.0f}, mp = 0.0f, mw = 0.0f;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = r0 + lane / 4 + (e >> 1) * 8, j = n0 + nt * 8 + q2 + (e & 1);
-                const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
-                p[nt][e] = j <= i ? a.scale * sm.all[0] * c * p[nt][e] : 0.0f;
-                w[nt][e] = j < i ? sm.all[1] * c * w[nt][e] : 0.0f;
-                if (j < i) dot[e >> 1] = fmaf(w[nt][e], kk[nt][e], dot[e >> 1]);
-                w[nt][e] *= sm.b[i];
-                mp = fmaxf(mp, fabsf(p[nt][e]));
-                mw = fmaxf(mw, fabsf(w[nt][e]));
-            }
-        row_sums(dot, 4);
-        mp = warp_max(mp);
-        mw = warp_max(mw);
-        if (lane == 0) {
-            sm.most[0][warp] = mp;
-            sm.most[1][warp] = mw;
-        }
-        __syncthreads();
-        mp = mw = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kGradThreads / 32; ++i) {
-            mp = fmaxf(mp, sm.most[0][i]);
-            mw = fmaxf(mw, sm.most[1][i]);
-        }
-        const float bp = scale_of(mp).by, bw = scale_of(mw).by;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, quarter * 2 + nt) + q2 * 2;
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(bp * p[nt][e], bp * p[nt][e + 1])) : "memory");
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(bw * w[nt][e], bw * w[nt][e + 1])) : "memory");
-            }
-    }
-    // x . v: a thread a row and an eighth of the columns (joined two and two)
+    // x . v: a thread a row and a quarter of the columns, while the tiles come
+    float xv = 0.0f;
+    bool here = mbar_wait_long(&sm.bar[0], 0);
+    __syncthreads();
     {
-        const int i = tid % C, part = tid / C;
+        const int i = tid % C;
         const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
-        float acc = 0.0f;
         if (i < rows)
-            for (int c8 = part; c8 < a.dv / 8; c8 += 2 * kParts) {
+            for (int c8 = tid / C; c8 < a.dv / 8; c8 += kParts) {
                 const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
                 const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
                 float sum = 0.0f;
@@ -1030,164 +936,325 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad_tc(DeltaArgs a) {
                     asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
                     sum = fmaf(e & 1 ? high(w[e / 2]) : low(w[e / 2]), __half2float(__ushort_as_half(u)), sum);
                 }
-                acc = fmaf(sm.scales[c8 / 2][3], sum, acc);
+                xv = fmaf(sm.scales[c8 / 2][3], sum, xv);
             }
-        // (the two eighths of a sums[5] entry meet in two steps)
-        if (part >= kParts) sm.sums[5][part - kParts][i] = acc;
-        __syncthreads();
-        if (part < kParts) sm.sums[5][part][i] += acc;
-    }
-    float back_p = 0.0f, back_w = 0.0f;
-    {
-        float mp = 0.0f, mw = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kGradThreads / 32; ++i) {
-            mp = fmaxf(mp, sm.most[0][i]);
-            mw = fmaxf(mw, sm.most[1][i]);
-        }
-        back_p = scale_of(mp).back;
-        back_w = scale_of(mw).back;
+        sm.sums[4][tid / C][i] = xv;
     }
 
-    const int c0 = quarter * (DP / 4);  // first column of the warp's
-    const int ra = r0 + lane / 4, rb = ra + 8;
-    // acc += F M over the columns of the state: F by left(f, kt), M a tile of S or R
-    auto over_columns = [&](Acc &acc, uint32_t tile, auto left) {
+    // 16 rows (m0) of a left operand from a plane, for the product's 16 columns kt
+    auto left_plane = [&](Frag &f, uint32_t tile, int m0, int kt, int product) {
+        left_k(f, tile, dvp, kt * 16, m0, lane);
+        const __half2 by = sm.steps[product][kt];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 x;
+            memcpy(&x, &f[i], 4);
+            x = __hmul2(x, by);
+            memcpy(&f[i], &x, 4);
+        }
+    };
+    // sums over the four lanes of a row, for this quarter of the columns: rows r0 + 16 mt + lane / 4 and 8 more
+    auto row_sums = [&](float x, float y, int mt, int which) {
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        y += __shfl_xor_sync(0xffffffffu, y, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        y += __shfl_xor_sync(0xffffffffu, y, 2);
+        if (lane % 4 == 0) {
+            sm.sums[which][quarter][r0 + mt * 16 + lane / 4] = x;
+            sm.sums[which][quarter][r0 + mt * 16 + lane / 4 + 8] = y;
+        }
+    };
+    const int c0 = quarter * (DP / 4), n0 = quarter * 16;  // first column of the warp's, of P and W
+    // acc += F M over the columns of the state: F a plane, M the tile of the state
+    auto over_columns = [&](Acc &acc, uint32_t plane, int product) {
 #pragma unroll 2
         for (int kt = 0; kt < groups; ++kt) {
-            Frag fl;
-            left(fl, kt);
+            Frag fl[2];
+            left_plane(fl[0], plane, r0, kt, product);
+            left_plane(fl[1], plane, r0 + 16, kt, product);
 #pragma unroll
             for (int np = 0; np < NT / 2; ++np) {
                 Frag f;
-                right_k(f, tile, dvp, kt * 16, c0 + np * 16, lane);
-                mma(acc[2 * np], fl, f[0], f[1]);
-                mma(acc[2 * np + 1], fl, f[2], f[3]);
+                right_k(f, ss, dvp, kt * 16, c0 + np * 16, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    mma(acc[mt][2 * np], fl[mt], f[0], f[1]);
+                    mma(acc[mt][2 * np + 1], fl[mt], f[2], f[3]);
+                }
             }
         }
     };
-    // acc += by F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q
-    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, float by) {
-        Frag fl[4];
+    // acc += F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q
+    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, uint32_t sign) {
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-            if (trans)
-                left_k(fl[kt], from, C, kt * 16, r0, lane);
-            else
-                left_m(fl[kt], from, C, r0, kt * 16, lane);
-        }
+            if (trans ? kt * 16 < r0 : kt * 16 > r0 + 16) continue;
+            Frag fl[2];
 #pragma unroll
-        for (int np = 0; np < NT / 2; ++np) {
-            float c[2][4];
-            zero(c);
+            for (int mt = 0; mt < 2; ++mt) {
+                if (trans)
+                    left_k(fl[mt], from, C, kt * 16, r0 + mt * 16, lane);
+                else
+                    left_m(fl[mt], from, C, r0 + mt * 16, kt * 16, lane);
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-                if (trans ? kt * 16 < r0 : kt * 16 > r0) continue;
-                Frag f;
-                right_k(f, tile, C, kt * 16, c0 + np * 16, lane);
-                mma(c[0], fl[kt], f[0], f[1]);
-                mma(c[1], fl[kt], f[2], f[3]);
+                for (int i = 0; i < 4; ++i) fl[mt][i] ^= sign;
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                right_k(f, tile, C, kt * 16, c0 + np * 16, lane);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[2 * np + i][e] = fmaf(by, c[i][e], acc[2 * np + i][e]);
+                for (int mt = 0; mt < 2; ++mt) {
+                    mma(acc[mt][2 * np], fl[mt], f[0], f[1]);
+                    mma(acc[mt][2 * np + 1], fl[mt], f[2], f[3]);
+                }
+            }
         }
     };
-    auto times_rows = [&](Acc &acc, float fa, float fb) {
+    // acc *= by row_factor (of every row)
+    auto times_rows = [&](Acc &acc, const float *row_factor, const float *more, float by) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int mt = 0; mt < 2; ++mt) {
+            const int ra = r0 + mt * 16 + lane / 4;
+            float fa = by * row_factor[ra], fb = by * row_factor[ra + 8];
+            if (more) {
+                fa *= more[ra];
+                fb *= more[ra + 8];
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[nt][e] *= e & 2 ? fb : fa;
-    };
-    // sums of the rows with those of the tile of K or Q
-    auto dot_rows = [&](const Acc &acc, uint32_t tile, float back, int which) {
-        float dot[2] = {0.0f, 0.0f};
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float2 x = half_pair(tile, C, ra, c0 + nt * 8 + q2), y = half_pair(tile, C, rb, c0 + nt * 8 + q2);
-            dot[0] = fmaf(x.x, acc[nt][0], fmaf(x.y, acc[nt][1], dot[0]));
-            dot[1] = fmaf(y.x, acc[nt][2], fmaf(y.y, acc[nt][3], dot[1]));
+                for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= e & 2 ? fb : fa;
         }
-        dot[0] *= back;
-        dot[1] *= back;
-        row_sums(dot, which);
+    };
+    auto times = [&](Acc &acc, float by) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= by;
+    };
+    // sums of the rows times those of K (whose left operands lie as the accumulators do)
+    auto dot_k = [&](const Acc &acc, int which) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float x = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                left_m(f, sk, C, r0 + mt * 16, c0 + np * 16, lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 k2 = half_pair(f[i]);
+                    const float *c = acc[mt][2 * np + i / 2] + (i & 1) * 2;
+                    float &to = i & 1 ? y : x;
+                    to = fmaf(k2.x, c[0], fmaf(k2.y, c[1], to));
+                }
+            }
+            row_sums(back_k * x, back_k * y, mt, which);
+        }
     };
     auto store_rows = [&](const Acc &acc, OUT *out, int64_t st) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int c = c0 + nt * 8 + q2;
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int r = i ? rb : ra;
-                if (r >= rows || c >= a.d) continue;
-                if (sizeof(OUT) == 2)
-                    *reinterpret_cast<uint32_t *>(out + r * st + c) = pack_bf16(acc[nt][2 * i], acc[nt][2 * i + 1]);
-                else
-                    *reinterpret_cast<float2 *>(out + r * st + c) = make_float2(acc[nt][2 * i], acc[nt][2 * i + 1]);
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+                if (r >= rows) continue;
+                OUT *to = out + r * st + c0 + q2;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (c0 + nt * 8 >= a.d) continue;
+                    if (sizeof(OUT) == 2)
+                        *reinterpret_cast<uint32_t *>(to + nt * 8) = pack_bf16(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
+                    else
+                        *reinterpret_cast<float2 *>(to + nt * 8) = make_float2(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
+                }
             }
-        }
+    };
+    auto clear = [&](Acc &acc) {
+        zero(acc[0]);
+        zero(acc[1]);
     };
 
-    Acc acc, z;
-    zero(acc);
-    over_columns(acc, ss, [&](Frag &f, int kt) { left_go(f, kt, 2); });
-    times_rows(acc, a.scale * sm.all[2] * sm.past[ra], a.scale * sm.all[2] * sm.past[rb]);
-    over_rows(acc, sP, false, sk, back_p * back_k);
-    dot_rows(acc, sq, back_q, 0);
-    store_rows(acc, dq, a.dqt);
-
-    zero(z);
-    over_columns(z, ss, [&](Frag &f, int kt) { left_plane(f, sx, kt, 3); });
-    times_rows(z, sm.all[3] * sm.past[ra], sm.all[3] * sm.past[rb]);
-    dot_rows(z, sk, back_k, 1);  // (for db, without b and the rows' part)
-    times_rows(z, sm.b[ra], sm.b[rb]);
-    over_rows(z, sW, false, sk, back_w * back_k);
-    dot_rows(z, sk, back_k, 6);
-
-    zero(acc);
-    over_columns(acc, sr, [&](Frag &f, int kt) { left_plane(f, su, kt, 4); });
-    times_rows(acc, sm.all[4] * sm.left[ra], sm.all[4] * sm.left[rb]);
-    dot_rows(acc, sk, back_k, 2);
-    over_rows(acc, sP, true, sq, back_p * back_q);
-    over_rows(acc, sW, true, sk, -back_w * back_k);
-    dot_rows(acc, sk, back_k, 3);
+    // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 16 columns a warp; W . K K^T for db
+    float p[2][2][4], w[2][2][4];
+    float mp = 0.0f, mw = 0.0f;
+    {
+        float kk[2][2][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[nt][e] -= z[nt][e];
-    store_rows(acc, dk, a.dkt);
-
-    // <S, R>
-    float total = 0.0f;
-    for (int i = tid; i < dvp * (DP / 8); i += kGradThreads) {
-        const int r = i / (DP / 8), p = i % (DP / 8);
-        float sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const float2 x = half_pair(ss, dvp, r, p * 8 + e), y = half_pair(sr, dvp, r, p * 8 + e);
-            sum = fmaf(x.x, y.x, fmaf(x.y, y.y, sum));
+        for (int mt = 0; mt < 2; ++mt) {
+            zero(p[mt]);
+            zero(w[mt]);
+            zero(kk[mt]);
         }
-        total = fmaf(sm.scales[r / 16][0] * sm.scales[r / 16][1], sum, total);
-    }
+        if (n0 <= r0 + 16) {
+#pragma unroll 2
+            for (int kt = 0; kt < groups; ++kt) {
+                Frag f;
+                right_k(f, su, dvp, kt * 16, n0, lane);
 #pragma unroll
-    for (int w = 16; w > 0; w /= 2) total += __shfl_xor_sync(0xffffffffu, total, w);
-    if (lane == 0) sm.total[warp] = total;
+                for (int mt = 0; mt < 2; ++mt) {
+                    Frag fg, fx;
+                    left_plane(fg, sgo, r0 + mt * 16, kt, 0);
+                    left_plane(fx, sx, r0 + mt * 16, kt, 1);
+                    mma(p[mt][0], fg, f[0], f[1]);
+                    mma(p[mt][1], fg, f[2], f[3]);
+                    mma(w[mt][0], fx, f[0], f[1]);
+                    mma(w[mt][1], fx, f[2], f[3]);
+                }
+            }
+#pragma unroll
+            for (int k0 = 0; k0 < DP; k0 += 16) {
+                Frag f;
+                right_n(f, sk, C, n0, k0, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    Frag fk;
+                    left_m(fk, sk, C, r0 + mt * 16, k0, lane);
+                    mma(kk[mt][0], fk, f[0], f[1]);
+                    mma(kk[mt][1], fk, f[2], f[3]);
+                }
+            }
+        }
+        const float by_p = a.scale * sm.all[0], by_w = sm.all[1];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = r0 + mt * 16 + lane / 4 + (e >> 1) * 8, j = n0 + nt * 8 + q2 + (e & 1);
+                    const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
+                    float &pp = p[mt][nt][e], &ww = w[mt][nt][e];
+                    pp = j <= i ? by_p * c * pp : 0.0f;
+                    ww = j < i ? by_w * c * ww : 0.0f;
+                    if (j < i) dot[e >> 1] = fmaf(ww, kk[mt][nt][e], dot[e >> 1]);
+                    ww *= sm.b[i];
+                    mp = fmaxf(mp, fabsf(pp));
+                    mw = fmaxf(mw, fabsf(ww));
+                }
+            row_sums(dot[0], dot[1], mt, 3);
+        }
+        mp = warp_max(mp);
+        mw = warp_max(mw);
+        if (lane == 0) {
+            sm.most[0][warp] = mp;
+            sm.most[1][warp] = mw;
+        }
+    }
+    // what dK takes from R
+    Acc acc, z;
+    clear(acc);
+    here = mbar_wait_long(&sm.bar[1], 0) && here;
+    if (here) over_columns(acc, su, 4);
+    if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            for (int i = 0; i < 2; ++i) mbar_wait(&sm.bar[i], 0, kDrainNs);
+        }
+        return;
+    }
+    if (tid == 0) load_state(a.Sp + at * dvp * DP, of_state, 2);
+    mp = mw = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kGradThreads / 32; ++i) {
+        mp = fmaxf(mp, sm.most[0][i]);
+        mw = fmaxf(mw, sm.most[1][i]);
+    }
+    // P Q and W K are scaled down alike, so that they add up in dK
+    const float by = fmaxf(fmaxf(scale_of(mp).back * back_q, scale_of(mw).back * back_k), 0x1p-100f), inv = inverse2(by);
+    const float to_p = back_q * inv, to_w = back_k * inv, by_pk = by * back_k * inverse2(back_q);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const uint32_t to = tile_at(0, C, r0 + mt * 16 + lane / 4 + e * 4, quarter * 2 + nt) + q2 * 2;
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(to_p * p[mt][nt][e], to_p * p[mt][nt][e + 1])) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(to_w * w[mt][nt][e], to_w * w[mt][nt][e + 1])) : "memory");
+            }
+    times_rows(acc, sm.left, nullptr, sm.all[4] * inv);
     __syncthreads();
+    over_rows(acc, sW, true, sk, 0x80008000u);
+
+    // dQ and Z from S
+    here = mbar_wait_long(&sm.bar[2], 0);
+    clear(z);
+    if (here) over_columns(z, sgo, 2);
+    times_rows(z, sm.past, nullptr, a.scale * sm.all[2] * inverse2(by_pk));
+    over_rows(z, sP, false, sk, 0);
+    times(z, by_pk);
+    store_rows(z, dq, a.dqt);
+    {  // q . dQ, with Q as it came
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint32_t u = r < rows && c0 + nt * 8 < a.d ? *reinterpret_cast<const uint32_t *>(q + r * a.q.st + nt * 8) : 0u;
+                    dot[i] = fmaf(low(u), z[mt][nt][2 * i], fmaf(high(u), z[mt][nt][2 * i + 1], dot[i]));
+                }
+            }
+            row_sums(dot[0], dot[1], mt, 0);
+        }
+    }
+    clear(z);
+    if (here) over_columns(z, sx, 3);
+    if (__syncthreads_or(!here)) {
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            mbar_wait(&sm.bar[2], 0, kDrainNs);
+        }
+        return;
+    }
+    if (tid == 0) load_state(a.Qp + kat * C * DP, sizeof(sm.k), 3);
+    times_rows(z, sm.past, nullptr, sm.all[3]);
+    dot_k(z, 1);
+    times_rows(z, sm.b, nullptr, inv);
+    over_rows(z, sW, false, sk, 0);
+    times(z, by);
+    dot_k(z, 5);
+
+    // dK
+    here = mbar_wait_long(&sm.bar[3], 0);
+    if (here) over_rows(acc, sP, true, ss, 0);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[mt][nt][e] = fmaf(by, acc[mt][nt][e], -z[mt][nt][e]);
+    dot_k(acc, 2);
+    store_rows(acc, dk, a.dkt);
+    if (__syncthreads_or(!here)) {
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            mbar_wait(&sm.bar[3], 0, kDrainNs);
+        }
+        return;
+    }
     if (tid < rows) {
         auto sum = [&](int which) {
             return (sm.sums[which][0][tid] + sm.sums[which][1][tid]) + (sm.sums[which][2][tid] + sm.sums[which][3][tid]);
         };
-        io_store(db + tid * a.db.st, sum(5) - sum(1) - back_k * back_k * sum(4));
-        sm.read[tid] = sum(0) - sum(6);
-        sm.wrote[tid] = sum(3);
-        sm.wstate[tid] = sum(2);
+        const float bz = sum(5);
+        io_store(db + tid * a.db.st, sum(4) - sum(1) - back_k * back_k * sum(3));
+        sm.read[tid] = sum(0) - bz;
+        sm.wrote[tid] = sum(2) + bz;
     }
     __syncthreads();
     if (warp == 0) {
-        total = 0.0f;
-        for (int w = 0; w < kGradThreads / 32; ++w) total += sm.total[w];
-        delta_gate_grads(total * sm.past[C - 1], sm.read, sm.wrote, sm.wstate, rows, lane, [&](int t, float x) {
+        float base = 0.0f;
+        for (int kt = 0; kt < groups; ++kt) base += sm.scales[kt][5];
+        delta_gate_grads(base, sm.read, sm.wrote, rows, lane, [&](int t, float x) {
             io_store(dg + t * a.dg.st, expf(gate_at<__nv_bfloat16>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
         });
     }
