@@ -58,8 +58,8 @@ struct DeltaArgs {
     float *before, *after;  // states before chunk i, gradients of the states before chunk i, [B H][m + 1][d][dv]
     // tensor-core form (fp16, scaled; dvp: dv to a multiple of 16, dp: d to 64 or 128), for every chunk: its rows of K
     // and Q ([B Hk][m][64][dp]), the inverse T, transposed, in two planes and the scores P in `planes` of them ([64][64] each),
-    // factors of its rows; and for every 16 columns of a chunk U, X and dO ([16][64], transposed), the states at its
-    // two ends (S before, R behind; [16][dp], transposed), what S, R, U, X and dO were scaled down by, and <S, R> before it
+    // factors of its rows; and for every 16 columns of a chunk U, X and dO ([16][64], transposed), and before it
+    // (R: behind the last one too, m + 1 to a head) the states ([16][dp], transposed) and what all these were scaled down by
     __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Gp, *Sp, *Rp;
     float *rows, *scales;
     int planes, dvp;

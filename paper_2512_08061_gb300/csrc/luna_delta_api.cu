@@ -89,8 +89,8 @@ Plan make_plan(const luna_delta_desc *dd) {
         p.Xp = take(chunks * p.dvp * kDeltaRows * 2);
         p.Gp = take(chunks * p.dvp * kDeltaRows * 2);
         p.Sp = take(chunks * p.dvp * p.dp * 2);
-        p.Rp = take(chunks * p.dvp * p.dp * 2);
-        p.scales = take(chunks * (p.dvp / 16) * kDeltaScales * 4);
+        p.Rp = take((chunks + BH) * p.dvp * p.dp * 2);
+        p.scales = take((chunks + BH) * (p.dvp / 16) * kDeltaScales * 4);
     }
     const size_t end_tc = at;
     at = 256;

@@ -434,26 +434,29 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
 }
 
 // ---------------------------------------------------------------------------
-// The chains.  A block of NW warps has 16 NW columns of one head's state.  The tiles of a chunk come by asynchronous
-// copies while the chunk before is worked on; one barrier a chunk.
+// The chains.  A block has NG groups of 16 columns of one head's state, a group SP warps: with few heads two, which hold
+// half of each column and exchange their shares of K S (and Q S) once a chunk; each then has 230 products a chunk where
+// one warp has 420.  The tiles of a chunk come by asynchronous copies while the chunk before is worked on; one barrier a
+// chunk.
 
-template <int DP, int NW, bool REV>
+template <int DP, int NG, int SP, bool REV>
 struct ChainShared {
-    static constexpr int kPitch = NW * 32 + 16;  // bytes of a row of V or dO: eight rows start in eight banks
+    static constexpr int kWarps = NG * SP;
+    static constexpr int kPitch = NG * 32 + 16;  // bytes of a row of V or dO: eight rows start in eight banks
     static constexpr int kPlanes = REV ? 2 : 1;  // of P
     struct Stage {
         alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], T[2][kTileB], P[kPlanes][kTileB], x[C * kPitch];
         alignas(16) float rows[kRowsF];
     } stage[2];
     uint64_t bar[2];
-    alignas(16) char out[NW][C * 48];  // a warp's 16 columns of the outputs, rows of 32 bytes 48 apart
+    alignas(16) char out[kWarps][C * 48];  // 16 columns of the outputs, rows of 32 bytes 48 apart
+    float4 shares[SP == 1 ? 1 : kWarps][SP == 1 ? 1 : 12][32];
 };
 
-template <int DP, int NW, bool REV>
-__device__ __forceinline__ void chain_load(typename ChainShared<DP, NW, REV>::Stage &st, uint64_t *bar, const DeltaArgs &a, int64_t bh,
-                                           int b, int h, int chunk, int len, int col0, int tid) {
-    using Sh = ChainShared<DP, NW, REV>;
-    constexpr int TH = NW * 32;
+template <int DP, int NG, int SP, bool REV>
+__device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, REV>::Stage &st, uint64_t *bar, const DeltaArgs &a,
+                                           int64_t bh, int b, int h, int chunk, int len, int col0, int tid) {
+    using Sh = ChainShared<DP, NG, SP, REV>;
     const int t0 = chunk * C, rows = min(C, len - t0);
     if (tid == 0) {
         const int64_t at = bh * a.m + chunk, kat = ((int64_t)b * a.k.heads + h / (a.H / a.k.heads)) * a.m + chunk;
@@ -469,28 +472,29 @@ __device__ __forceinline__ void chain_load(typename ChainShared<DP, NW, REV>::St
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(xv.p) + b * xv.sb + h * xv.sh + t0 * xv.st + col0;
     const uint32_t sx = smem_u32(st.x);
 #pragma unroll
-    for (int i = tid; i < C * NW * 2; i += TH) {
-        const int r = i / (NW * 2), p = i % (NW * 2);
+    for (int i = tid; i < C * NG * 2; i += Sh::kWarps * 32) {
+        const int r = i / (NG * 2), p = i % (NG * 2);
         const bool in = r < rows && col0 + p * 8 < a.dv;
         copy16(sx + r * Sh::kPitch + p * 16, in ? x + r * xv.st + p * 8 : static_cast<const __nv_bfloat16 *>(xv.p), in);
     }
     copies_end();
 }
 
-// Rows of a warp's 16 columns, given column by column, to the output: transposed through shared memory
-template <int N>
-__device__ __forceinline__ void chain_store(const float (&acc)[N][4], char *mem, __nv_bfloat16 *out, int64_t st, int rows, int col, int dv, int lane) {
+// Rows first, first + 1, .. (n of them) of a warp's 16 columns, given column by column, to the output: transposed through
+// shared memory
+__device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first, int n, char *mem, __nv_bfloat16 *out, int64_t st, int rows,
+                                            int col, int dv, int lane) {
     const uint32_t base = smem_u32(mem);
 #pragma unroll
     for (int nt = 0; nt < 8; nt += 2) {
+        if (nt * 8 < first || nt * 8 >= first + n) continue;
         const Frag f = {pack_bf16(acc[nt][0], acc[nt][1]), pack_bf16(acc[nt][2], acc[nt][3]),
                         pack_bf16(acc[nt + 1][0], acc[nt + 1][1]), pack_bf16(acc[nt + 1][2], acc[nt + 1][3])};
         stm_t(base + (nt * 8 + (lane >> 4) * 8 + (lane & 7)) * 48 + ((lane >> 3) & 1) * 16, f);
     }
     __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = i * 16 + lane / 2, half = lane % 2;
+    for (int i = 0; i < n / 16; ++i) {
+        const int r = first + i * 16 + lane / 2, half = lane % 2;
         if (r < rows && col + half * 8 < dv)
             *reinterpret_cast<uint4 *>(out + r * st + col + half * 8) = *reinterpret_cast<const uint4 *>(mem + r * 48 + half * 16);
     }
@@ -507,25 +511,27 @@ __device__ __forceinline__ void plane_store(__half *tile, int rows, int r0, int 
     *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r + 8, (k0 >> 3) + 1)) = f[3];
 }
 
-template <int DP, int NW, bool REV>
-__global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
-    using Sh = ChainShared<DP, NW, REV>;
+template <int DP, int NG, int SP, bool REV>
+__global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
+    using Sh = ChainShared<DP, NG, SP, REV>;
     extern __shared__ __align__(128) char raw[];
     Sh &sm = *reinterpret_cast<Sh *>(raw);
-    constexpr int ND = DP / 8;  // n-tiles of a state's row
-    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    constexpr int ND = DP / 8 / SP;  // n-tiles of a state's row that a warp holds
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, group = warp / SP, part = warp % SP, d0 = part * (DP / SP);
     const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * NW * 16, col = col0 + warp * 16;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * NG * 16, col = col0 + group * 16;
     const int len = head_length(a.lengths, b, a.n), chunks = (len + C - 1) / C, q2 = lane % 4 * 2;
     const bool mine = col < a.dv;  // the warp has columns
     __nv_bfloat16 *o = a.o ? static_cast<__nv_bfloat16 *>(a.o) + b * a.ob + h * a.oh : nullptr;
-    __half *planes = REV ? a.Xp : a.Up, *ends = REV ? a.Rp : a.Sp;
+    // n-tiles of rows that the warp finishes where a group's warps share that work, for 16 of them (np)
+    auto own = [&](int np) { return SP == 1 || np / 2 == part; };
+    const int first = SP == 1 ? 0 : part * (C / 2), some = C / SP;
 
-    // S^T or R^T: row lane / 4 (and 8 more) of the warp's columns, values 8 nt + q2 and the next
+    // S^T or R^T: row lane / 4 (and 8 more) of the warp's columns, values d0 + 8 nt + q2 and the next
     float S[ND][4];
     const float *init = REV ? a.dS1 : a.S0;
     auto place = [&](int nt, int e, int64_t &at) {
-        const int c = col + lane / 4 + (e >> 1) * 8, r = nt * 8 + q2 + (e & 1);
+        const int c = col + lane / 4 + (e >> 1) * 8, r = d0 + nt * 8 + q2 + (e & 1);
         at = (bh * a.d + r) * a.dv + c;
         return r < a.d && c < a.dv;
     };
@@ -536,11 +542,18 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
             int64_t at;
             S[nt][e] = init && place(nt, e, at) ? init[at] : 0.0f;
         }
+    // the scales of the warp's columns: 0, 1: of the halves of S before a chunk, 2, 3: of R, 4: U, 5: X, 6: dO
+    auto scales_of = [&](int chunk) { return a.scales + ((bh * (a.m + 1) + chunk) * (a.dvp / 16) + col / 16) * kDeltaScales; };
+    auto keep_scale = [&](int chunk, float back) {
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < 2 / SP; ++i) scales_of(chunk)[(REV ? 2 : 0) + part + i] = back;
+    };
 
     if (tid < 2) mbar_init(&sm.bar[tid], 1);
     fence_mbar_init();
     __syncthreads();
-    if (chunks > 0) chain_load<DP, NW, REV>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
+    if (chunks > 0) chain_load<DP, NG, SP, REV>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
     for (int step = 0; step < chunks; ++step) {
         const int chunk = REV ? chunks - 1 - step : step, t0 = chunk * C;
         typename Sh::Stage &st = sm.stage[step & 1];
@@ -554,32 +567,35 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
             break;
         }
         if (step + 1 < chunks)
-            chain_load<DP, NW, REV>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
+            chain_load<DP, NG, SP, REV>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
         if (!mine) continue;
         const uint32_t sk = smem_u32(st.k), sq = smem_u32(st.q), sT = smem_u32(st.T), sP = smem_u32(st.P);
-        const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + warp * 32 + ((lane >> 3) & 1) * 16;
+        const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + group * 32 + ((lane >> 3) & 1) * 16;
         const float whole = st.rows[4 * C], rest = st.rows[4 * C + 1], back_T = st.rows[4 * C + 2], back_P = st.rows[4 * C + 3];
         auto factor = [&](int which, int t) { return *reinterpret_cast<const float2 *>(st.rows + which * C + t); };
-        const int64_t group = (bh * a.m + chunk) * (a.dvp / 16) + col / 16;  // the warp's columns in the planes
-        __half *keep = planes ? planes + (bh * a.m + chunk) * a.dvp * C : nullptr;
-        float *scales = a.scales ? a.scales + group * kDeltaScales : nullptr;  // S, R, U, X, dO; <S, R>
+        const int64_t at = bh * a.m + chunk;
         // S <- c(C, 0) S (first) + F M for a left operand F of 64 summed rows and the tile M (a row for each)
         auto update = [&](const Frag (&fh)[4], const Frag (&fl)[4], float back, uint32_t tile, bool decay) {
 #pragma unroll
-            for (int np = 0; np < DP / 16; ++np) {
-                float acc[2][4];
+            for (int np = 0; np < ND / 2; np += 2) {
+                float acc[4][4];
                 zero(acc);
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt) {
-                    Frag f;
-                    right_k(f, tile, C, kt * 16, np * 16, lane);
+                    Frag f, g;
+                    right_k(f, tile, C, kt * 16, d0 + np * 16, lane);
+                    right_k(g, tile, C, kt * 16, d0 + np * 16 + 16, lane);
                     mma(acc[0], fh[kt], f[0], f[1]);
                     mma(acc[1], fh[kt], f[2], f[3]);
+                    mma(acc[2], fh[kt], g[0], g[1]);
+                    mma(acc[3], fh[kt], g[2], g[3]);
                     mma(acc[0], fl[kt], f[0], f[1]);
                     mma(acc[1], fl[kt], f[2], f[3]);
+                    mma(acc[2], fl[kt], g[0], g[1]);
+                    mma(acc[3], fl[kt], g[2], g[3]);
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float &s = S[2 * np + i][e];
@@ -587,34 +603,78 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                     }
             }
         };
+        // the other warp's share of x, and of y's own rows, added to this one's
+        auto exchange = [&](float (&x)[8][4], float (&y)[8][4], bool both) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sm.shares[warp][i][lane] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            if (both)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // (the rows that the other one finishes)
+                    const float *lo = y[i], *hi = y[4 + i];
+                    sm.shares[warp][8 + i][lane] = part ? make_float4(lo[0], lo[1], lo[2], lo[3]) : make_float4(hi[0], hi[1], hi[2], hi[3]);
+                }
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + group) : "memory");
+            const float4 (*other)[32] = sm.shares[warp ^ 1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 v = other[i][lane];
+                x[i][0] += v.x; x[i][1] += v.y; x[i][2] += v.z; x[i][3] += v.w;
+            }
+            if (both)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 v = other[8 + i][lane];
+                    const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[i][e] += part ? 0.0f : w[e];
+                        y[4 + i][e] += part ? w[e] : 0.0f;
+                    }
+                }
+        };
         float x[8][4], y[8][4];
         zero(x);
         zero(y);
         // x = K S (or K R), with it Q S
         const Scale ss = scale_of(S);
+        {
+            __half *ends = REV ? (a.Rp ? a.Rp + (bh * (a.m + 1) + chunk + 1) * a.dvp * DP : nullptr) : (a.Sp ? a.Sp + at * a.dvp * DP : nullptr);
+            if (ends) keep_scale(REV ? chunk + 1 : chunk, ss.back);
 #pragma unroll
-        for (int kt = 0; kt < DP / 16; ++kt) {
-            Frag hi, lo;
-            split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
-            if (ends) plane_store(ends + (bh * a.m + chunk) * a.dvp * DP, a.dvp, col, kt * 16, hi, lane);
+            for (int kt = 0; kt < ND / 2; ++kt) {
+                Frag hi, lo;
+                split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
+                if (ends) plane_store(ends, a.dvp, col, d0 + kt * 16, hi, lane);
 #pragma unroll
-            for (int np = 0; np < 4; ++np) {
-                Frag f;
-                right_n(f, sk, C, np * 16, kt * 16, lane);
-                mma(x[2 * np], hi, f[0], f[1]);
-                mma(x[2 * np + 1], hi, f[2], f[3]);
-                mma(x[2 * np], lo, f[0], f[1]);
-                mma(x[2 * np + 1], lo, f[2], f[3]);
-                if (!REV && o) {
-                    right_n(f, sq, C, np * 16, kt * 16, lane);
-                    mma(y[2 * np], hi, f[0], f[1]);
-                    mma(y[2 * np + 1], hi, f[2], f[3]);
+                for (int np = 0; np < 4; ++np) {
+                    Frag f;
+                    right_n(f, sk, C, np * 16, d0 + kt * 16, lane);
+                    mma(x[2 * np], hi, f[0], f[1]);
+                    mma(x[2 * np + 1], hi, f[2], f[3]);
+                    mma(x[2 * np], lo, f[0], f[1]);
+                    mma(x[2 * np + 1], lo, f[2], f[3]);
+                    if (!REV && o) {
+                        right_n(f, sq, C, np * 16, d0 + kt * 16, lane);
+                        mma(y[2 * np], hi, f[0], f[1]);
+                        mma(y[2 * np + 1], hi, f[2], f[3]);
+                    }
                 }
             }
         }
-        if (scales && lane == 0) scales[REV ? 1 : 0] = ss.back;
         Frag fh[4], fl[4];
         if (!REV) {
+            float back_s = ss.back;
+            if (SP == 2) {
+#pragma unroll
+                for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[nt][e] *= ss.back;
+                        y[nt][e] *= ss.back;
+                    }
+                exchange(x, y, o);
+                back_s = 1.0f;
+            }
             // x = b (V - c(i, 0) K S)
 #pragma unroll
             for (int np = 0; np < 4; ++np) {
@@ -626,7 +686,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                     const float2 past = factor(0, t), beta = factor(2, t);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float p = ss.back * (e & 1 ? past.y : past.x), vv = e & 1 ? high(v[2 * i + (e >> 1)]) : low(v[2 * i + (e >> 1)]);
+                        const float p = back_s * (e & 1 ? past.y : past.x), vv = e & 1 ? high(v[2 * i + (e >> 1)]) : low(v[2 * i + (e >> 1)]);
                         x[nt][e] = (e & 1 ? beta.y : beta.x) * fmaf(-p, x[nt][e], vv);
                     }
                 }
@@ -653,42 +713,42 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                 }
             }
             const float back_u = xs.back * back_T;
-            if (o || keep) {  // P U; U's plane
+#pragma unroll
+            for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[nt][e] *= back_u;
+            if (o || a.Up) {  // P U; U's plane
 #pragma unroll
                 for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { u[nt][e] *= back_u; x[nt][e] = 0.0f; }
+                    for (int e = 0; e < 4; ++e) x[nt][e] = 0.0f;
                 const Scale us = scale_of(u);
 #pragma unroll
                 for (int kt = 0; kt < 4; ++kt) {
                     const Frag hi = {pack(us.by * u[2 * kt][0], us.by * u[2 * kt][1]), pack(us.by * u[2 * kt][2], us.by * u[2 * kt][3]),
                                      pack(us.by * u[2 * kt + 1][0], us.by * u[2 * kt + 1][1]), pack(us.by * u[2 * kt + 1][2], us.by * u[2 * kt + 1][3])};
-                    if (keep) plane_store(keep, a.dvp, col, kt * 16, hi, lane);
+                    if (a.Up && own(kt)) plane_store(a.Up + at * a.dvp * C, a.dvp, col, kt * 16, hi, lane);
                     if (o)
 #pragma unroll
                         for (int np = kt; np < 4; ++np) {
+                            if (!own(np)) continue;
                             Frag f;
                             right_n(f, sP, C, np * 16, kt * 16, lane);
                             mma(x[2 * np], hi, f[0], f[1]);
                             mma(x[2 * np + 1], hi, f[2], f[3]);
                         }
                 }
-                if (scales && lane == 0) scales[2] = us.back;
+                if (a.Up && lane == 0) scales_of(chunk)[4] = us.back;
                 if (o) {  // scale c(i, 0) Q S + P U
                     const float back = us.back * back_P;
 #pragma unroll
                     for (int nt = 0; nt < 8; ++nt) {
                         const float2 past = factor(3, nt * 8 + q2);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) y[nt][e] = fmaf(ss.back * (e & 1 ? past.y : past.x), y[nt][e], back * x[nt][e]);
+                        for (int e = 0; e < 4; ++e) y[nt][e] = fmaf(back_s * (e & 1 ? past.y : past.x), y[nt][e], back * x[nt][e]);
                     }
-                    chain_store(y, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+                    chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
                 }
-            } else {
-#pragma unroll
-                for (int nt = 0; nt < 8; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[nt][e] *= back_u;
             }
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) {
@@ -701,7 +761,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
             for (int kt = 0; kt < 4; ++kt) split_left(u[2 * kt], u[2 * kt + 1], ls.by, fh[kt], fl[kt]);
             update(fh, fl, ls.back, sk, true);
         } else {
-            // y = P^T dO;  R <- c(C, 0) R + scale Q^T c(i, 0) dO
+            // y = P^T dO (this warp's share of the rows);  R <- c(C, 0) R + scale Q^T c(i, 0) dO
             Frag g[4];
             float m = 0.0f, mp = 0.0f;
 #pragma unroll
@@ -716,7 +776,7 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                 }
             }
             const Scale gs = scale_of(warp_max(m)), ps = scale_of(warp_max(mp));
-            if (scales && lane == 0) scales[4] = gs.back;
+            if (lane == 0) scales_of(chunk)[6] = gs.back;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
                 Frag gf;
@@ -727,7 +787,8 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                     gf[i] = pack(gs.by * g0, gs.by * g1);
                     split(ps.by * (past.x * g0), ps.by * (past.y * g1), fh[kt][i], fl[kt][i]);
                 }
-                plane_store(a.Gp + (bh * a.m + chunk) * a.dvp * C, a.dvp, col, kt * 16, gf, lane);
+                if (own(kt)) plane_store(a.Gp + at * a.dvp * C, a.dvp, col, kt * 16, gf, lane);
+                if (SP == 2 && (kt == 0 || kt == 3) != (part == 0)) continue;  // five of the ten blocks each
 #pragma unroll
                 for (int np = 0; np <= kt; ++np) {
                     Frag f;
@@ -739,18 +800,18 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                     mma(y[2 * np + 1], gf, f[2], f[3]);
                 }
             }
-            update(fh, fl, ps.back, sq, true);
-            // x = c(C, j) K R + P^T dO;  X = T^T x
+            // x = c(C, j) K R + P^T dO
             const float back = gs.back * back_P;
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) {
                 const float2 left = factor(1, nt * 8 + q2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[nt][e] = fmaf(ss.back * (e & 1 ? left.y : left.x), x[nt][e], back * y[nt][e]);
-                    y[nt][e] = 0.0f;
-                }
+                for (int e = 0; e < 4; ++e) x[nt][e] = fmaf(ss.back * (e & 1 ? left.y : left.x), x[nt][e], back * y[nt][e]);
             }
+            if (SP == 2) exchange(x, y, false);
+            update(fh, fl, ps.back, sq, true);
+            zero(y);
+            // X = T^T x
             const Scale xs = scale_of(x);
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
@@ -776,12 +837,13 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[nt][e] *= back_x;
             const Scale us = scale_of(y);
-            if (scales && lane == 0) scales[3] = us.back;
+            if (lane == 0) scales_of(chunk)[5] = us.back;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
+                if (!own(kt)) continue;
                 const Frag hi = {pack(us.by * y[2 * kt][0], us.by * y[2 * kt][1]), pack(us.by * y[2 * kt][2], us.by * y[2 * kt][3]),
                                  pack(us.by * y[2 * kt + 1][0], us.by * y[2 * kt + 1][1]), pack(us.by * y[2 * kt + 1][2], us.by * y[2 * kt + 1][3])};
-                plane_store(keep, a.dvp, col, kt * 16, hi, lane);
+                plane_store(a.Xp + at * a.dvp * C, a.dvp, col, kt * 16, hi, lane);
             }
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) {
@@ -796,21 +858,17 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) split_left(x[2 * kt], x[2 * kt + 1], ws.by, fh[kt], fl[kt]);
             update(fh, fl, ws.back, sk, false);
-            {  // <S, R> before the chunk
-                const char *p = reinterpret_cast<const char *>(a.Sp + (bh * a.m + chunk) * a.dvp * DP) + q2 * 2;
-                float sum = 0.0f;
+            chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+        }
+    }
+    if (REV && mine && chunks > 0) {  // R before the first chunk
+        const Scale ss = scale_of(S);
+        keep_scale(0, ss.back);
 #pragma unroll
-                for (int nt = 0; nt < ND; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float2 f = half_pair(*reinterpret_cast<const uint32_t *>(p + tile_at(0, a.dvp, col + lane / 4 + i * 8, nt)));
-                        sum = fmaf(f.x, S[nt][2 * i], fmaf(f.y, S[nt][2 * i + 1], sum));
-                    }
-#pragma unroll
-                for (int w = 16; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-                if (lane == 0) scales[5] = scales[0] * sum;
-            }
-            chain_store(y, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+        for (int kt = 0; kt < ND / 2; ++kt) {
+            Frag hi, lo;
+            split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
+            plane_store(a.Rp + bh * (a.m + 1) * a.dvp * DP, a.dvp, col, d0 + kt * 16, hi, lane);
         }
     }
     float *last = REV ? a.dS0 : a.S1;
@@ -823,9 +881,9 @@ __global__ void __launch_bounds__(NW * 32) k_delta_chain(DeltaArgs a) {
                 if (place(nt, e, at)) last[at] = S[nt][e];
             }
     if (o)  // rows behind the end, eight columns at a time
-        for (int64_t i = tid; i < (int64_t)(a.n - len) * NW * 2; i += NW * 32) {
-            const int c = col0 + (int)(i % (NW * 2)) * 8;
-            if (c < a.dv) *reinterpret_cast<uint4 *>(o + (len + i / (NW * 2)) * a.ot + c) = make_uint4(0, 0, 0, 0);
+        for (int64_t i = tid; i < (int64_t)(a.n - len) * NG * 2; i += Sh::kWarps * 32) {
+            const int c = col0 + (int)(i % (NG * 2)) * 8;
+            if (c < a.dv) *reinterpret_cast<uint4 *>(o + (len + i / (NG * 2)) * a.ot + c) = make_uint4(0, 0, 0, 0);
         }
 }
 
@@ -841,9 +899,9 @@ struct GradShared {
     alignas(128) char k[DP / 64][kTileB], go[DVT * 128], x[DVT * 128], u[DVT * 128 > 2 * kTileB ? DVT * 128 : 2 * kTileB];
     alignas(128) char s[DVT * DP * 2 > DP / 64 * kTileB ? DVT * DP * 2 : DP / 64 * kTileB];
     uint64_t bar[4];
-    float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales];
-    __half2 steps[5][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
-    float all[5];
+    float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales], behind[DVT / 16][2];  // (behind: of R)
+    __half2 steps[8][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
+    float all[8], total[kGradThreads / 32];
     float sums[6][kParts][C];  // of a row's quarters: q . dQ, k . Z without the rows' part, k . (dK), W . K K^T, x . v, b k . Z
     float most[2][kGradThreads / 32], read[C], wrote[C];
 };
@@ -860,6 +918,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     Sh &sm = *reinterpret_cast<Sh *>(raw);
     constexpr int NT = DP / 32;  // n-tiles of a warp's quarter of the columns of dQ, dK
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 2 * 32, quarter = warp / 2, q2 = lane % 4 * 2;
+    const int of_half = 2 + quarter / 2 * 3;  // the products with S and R of the warp's half of the columns
     const int64_t at = blockIdx.x, bh = at / a.m;
     const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int rows = max(0, min(C, head_length(a.lengths, b, a.n) - t0)), out_rows = min(C, a.n - t0);
@@ -883,6 +942,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     const uint32_t sP = su, sW = su + kTileB;
     const int dvp = a.dvp, groups = dvp / 16;
     const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+    const int64_t slot = bh * (a.m + 1) + chunk;
     const uint32_t of_rows = dvp * C * 2, of_state = dvp * DP * 2;
     if (tid < 4) mbar_init(&sm.bar[tid], 1);
     fence_mbar_init();
@@ -897,7 +957,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         load_tile(sm.x, a.Xp + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.go, a.Gp + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.k, a.Kp + kat * C * DP, sizeof(sm.k), &sm.bar[0]);
-        load_state(a.Rp + at * dvp * DP, of_state, 1);
+        load_state(a.Rp + (slot + 1) * dvp * DP, of_state, 1);
     }
     const float *rowf = a.rows + at * kRowsF;
     const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
@@ -906,17 +966,22 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                         sm.past, sm.left);
     else if (warp < 3)
         sm.b[tid - 32] = rowf[2 * C + tid - 32];
-    for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[at * groups * kDeltaScales + i];
+    for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[slot * groups * kDeltaScales + i];
+    if (tid < groups * 2) sm.behind[tid / 2][tid % 2] = a.scales[((slot + 1) * groups + tid / 2) * kDeltaScales + 2 + tid % 2];
     __syncthreads();
     // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
-    // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U, dO S, X S, U R.
-    if (tid < 5) {
-        const int l = tid == 4 ? 2 : 4 - tid % 2, r = tid == 4 ? 1 : tid < 2 ? 2 : 0;
+    // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U; of either half of the
+    // other columns dO S, X S, U R.
+    if (tid < 8) {
+        const int side = tid < 2 ? 0 : (tid - 2) / 3, which = tid < 2 ? tid : (tid - 2) % 3;
+        auto scale = [&](int kt) {
+            const float *f = sm.scales[kt];
+            return tid < 2 ? f[6 - which] * f[4] : which < 2 ? f[6 - which] * f[side] : f[4] * sm.behind[kt][side];
+        };
         float most = 0.0f;
-        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, sm.scales[kt][l] * sm.scales[kt][r]);
+        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, scale(kt));
         sm.all[tid] = most;
-        for (int kt = 0; kt < groups; ++kt)
-            sm.steps[tid][kt] = __float2half2_rn(most > 0.0f ? sm.scales[kt][l] * sm.scales[kt][r] / most : 0.0f);
+        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = __float2half2_rn(most > 0.0f ? scale(kt) / most : 0.0f);
     }
     // x . v: a thread a row and a quarter of the columns, while the tiles come
     float xv = 0.0f;
@@ -936,7 +1001,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                     asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
                     sum = fmaf(e & 1 ? high(w[e / 2]) : low(w[e / 2]), __half2float(__ushort_as_half(u)), sum);
                 }
-                xv = fmaf(sm.scales[c8 / 2][3], sum, xv);
+                xv = fmaf(sm.scales[c8 / 2][5], sum, xv);
             }
         sm.sums[4][tid / C][i] = xv;
     }
@@ -1149,7 +1214,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     Acc acc, z;
     clear(acc);
     here = mbar_wait_long(&sm.bar[1], 0) && here;
-    if (here) over_columns(acc, su, 4);
+    if (here) over_columns(acc, su, of_half + 2);
     if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
         if (tid == 0) {
             atomicOr(a.status, 1);
@@ -1177,15 +1242,15 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(to_p * p[mt][nt][e], to_p * p[mt][nt][e + 1])) : "memory");
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(to_w * w[mt][nt][e], to_w * w[mt][nt][e + 1])) : "memory");
             }
-    times_rows(acc, sm.left, nullptr, sm.all[4] * inv);
+    times_rows(acc, sm.left, nullptr, sm.all[of_half + 2] * inv);
     __syncthreads();
     over_rows(acc, sW, true, sk, 0x80008000u);
 
     // dQ and Z from S
     here = mbar_wait_long(&sm.bar[2], 0);
     clear(z);
-    if (here) over_columns(z, sgo, 2);
-    times_rows(z, sm.past, nullptr, a.scale * sm.all[2] * inverse2(by_pk));
+    if (here) over_columns(z, sgo, of_half);
+    times_rows(z, sm.past, nullptr, a.scale * sm.all[of_half] * inverse2(by_pk));
     over_rows(z, sP, false, sk, 0);
     times(z, by_pk);
     store_rows(z, dq, a.dqt);
@@ -1206,8 +1271,33 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
             row_sums(dot[0], dot[1], mt, 0);
         }
     }
+    {  // <S, R> before the chunk, R as it lies in memory
+        float sum = 0.0f;
+        const uint4 *r = reinterpret_cast<const uint4 *>(a.Rp + slot * dvp * DP);
+        if (here)
+#pragma unroll 2
+            for (int i = tid; i < dvp * (DP / 8); i += kGradThreads) {
+                const uint4 y4 = r[i], x4 = *reinterpret_cast<const uint4 *>(sm.s + i * 16);
+                const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w}, y[4] = {y4.x, y4.y, y4.z, y4.w};
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = half_pair(x[e]), g = half_pair(y[e]);
+                    part = fmaf(f.x, g.x, fmaf(f.y, g.y, part));
+                }
+                // (panels of 64 columns, in which pieces are swizzled among eight)
+                const int row = i / 8 % dvp, column = DP == 64 ? ((i & 7) ^ (row & 7)) * 8 : i / 8 / dvp * 64;
+                const float *f = sm.scales[row / 16];
+                const int side = column >= DP / 2;
+                sum = fmaf(f[side] * f[2 + side], part, sum);
+            }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+#pragma unroll
+        for (int w = 8; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        if (lane == 0) sm.total[warp] = sum;
+    }
     clear(z);
-    if (here) over_columns(z, sx, 3);
+    if (here) over_columns(z, sx, of_half + 1);
     if (__syncthreads_or(!here)) {
         if (tid == 0) {
             atomicOr(a.status, 1);
@@ -1216,7 +1306,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         return;
     }
     if (tid == 0) load_state(a.Qp + kat * C * DP, sizeof(sm.k), 3);
-    times_rows(z, sm.past, nullptr, sm.all[3]);
+    times_rows(z, sm.past, nullptr, sm.all[of_half + 1]);
     dot_k(z, 1);
     times_rows(z, sm.b, nullptr, inv);
     over_rows(z, sW, false, sk, 0);
@@ -1253,7 +1343,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     __syncthreads();
     if (warp == 0) {
         float base = 0.0f;
-        for (int kt = 0; kt < groups; ++kt) base += sm.scales[kt][5];
+        for (int w = 0; w < kGradThreads / 32; ++w) base += sm.total[w];
         delta_gate_grads(base, sm.read, sm.wrote, rows, lane, [&](int t, float x) {
             io_store(dg + t * a.dg.st, expf(gate_at<__nv_bfloat16>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
         });
@@ -1270,23 +1360,23 @@ cudaError_t prepare(const DeltaArgs &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-template <int DP, int NW, bool REV>
+template <int DP, int NG, int SP, bool REV>
 cudaError_t chain_launch(const DeltaArgs &a, cudaStream_t s) {
-    using Sh = ChainShared<DP, NW, REV>;
-    cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NW, REV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
+    using Sh = ChainShared<DP, NG, SP, REV>;
+    cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NG, SP, REV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, NW * 16));
-    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NW, REV>), grid, NW * 32, sizeof(Sh), s, a);
+    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, NG * 16));
+    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NG, SP, REV>), grid, NG * SP * 32, sizeof(Sh), s, a);
     return cudaGetLastError();
 }
 
-// Warps of a block: with few heads, few, so that the columns' chains spread over the SMs.
+// With few heads, few columns a block and two warps for 16 of them, so that the chains spread over the SMs.
 template <int DP, bool REV>
 cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
     const int64_t bh = (int64_t)a.B * a.H, sms = tc_sm_count();
-    if (a.dv > 64 && bh * cdiv(a.dv, 64) > sms) return chain_launch<DP, 8, REV>(a, s);
-    if (a.dv > 32 && bh * cdiv(a.dv, 32) > sms) return chain_launch<DP, 4, REV>(a, s);
-    return chain_launch<DP, 2, REV>(a, s);
+    if (a.dv > 64 && bh * cdiv(a.dv, 64) > sms) return chain_launch<DP, 8, 1, REV>(a, s);
+    if (a.dv > 32 && bh * cdiv(a.dv, 32) > sms) return chain_launch<DP, 4, 1, REV>(a, s);
+    return chain_launch<DP, 2, 2, REV>(a, s);
 }
 
 }  // namespace
