@@ -439,36 +439,44 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
 // one warp has 420.  The tiles of a chunk come by asynchronous copies while the chunk before is worked on; one barrier a
 // chunk.
 
-template <int DP, int NG, int SP, bool REV>
+enum ChainMode {
+    kOutputs,   // O (and the last state)
+    kKeep,      // U and the states, for the gradients
+    kReverse    // dV, X, dO and the gradients of the states
+};
+
+template <int DP, int NG, int SP, ChainMode MODE>
 struct ChainShared {
     static constexpr int kWarps = NG * SP;
     static constexpr int kPitch = NG * 32 + 16;  // bytes of a row of V or dO: eight rows start in eight banks
-    static constexpr int kPlanes = REV ? 2 : 1;  // of P
+    static constexpr bool kQ = MODE != kKeep;    // Q and P are needed
+    static constexpr int kPlanes = MODE == kReverse ? 2 : 1;  // of P
     struct Stage {
-        alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], T[2][kTileB], P[kPlanes][kTileB], x[C * kPitch];
+        alignas(128) char k[DP / 64][kTileB], q[kQ ? DP / 64 : 1][kQ ? kTileB : 16], T[2][kTileB];
+        alignas(128) char P[kPlanes][kQ ? kTileB : 16], x[C * kPitch];
         alignas(16) float rows[kRowsF];
     } stage[2];
     uint64_t bar[2];
-    alignas(16) char out[kWarps][C * 48];  // 16 columns of the outputs, rows of 32 bytes 48 apart
+    alignas(16) char out[kQ ? kWarps : 1][C * 48];  // 16 columns of the outputs, rows of 32 bytes 48 apart
+    alignas(128) char planes[MODE != kOutputs && SP == 1 ? kWarps : 1][DP * 32];  // 16 rows of a tile that is kept
     float4 shares[SP == 1 ? 1 : kWarps][SP == 1 ? 1 : 12][32];
 };
 
-template <int DP, int NG, int SP, bool REV>
-__device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, REV>::Stage &st, uint64_t *bar, const DeltaArgs &a,
+template <int DP, int NG, int SP, ChainMode MODE>
+__device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, MODE>::Stage &st, uint64_t *bar, const DeltaArgs &a,
                                            int64_t bh, int b, int h, int chunk, int len, int col0, int tid) {
-    using Sh = ChainShared<DP, NG, SP, REV>;
+    using Sh = ChainShared<DP, NG, SP, MODE>;
     const int t0 = chunk * C, rows = min(C, len - t0);
     if (tid == 0) {
         const int64_t at = bh * a.m + chunk, kat = ((int64_t)b * a.k.heads + h / (a.H / a.k.heads)) * a.m + chunk;
-        const bool all = REV || a.o;
-        mbar_arrive_expect_tx(bar, sizeof(st.k) + sizeof(st.T) + sizeof(st.rows) + (all ? sizeof(st.q) + sizeof(st.P) : 0));
+        mbar_arrive_expect_tx(bar, sizeof(st.k) + sizeof(st.T) + sizeof(st.rows) + (Sh::kQ ? sizeof(st.q) + sizeof(st.P) : 0));
         load_tile(st.k, a.Kp + kat * C * DP, sizeof(st.k), bar);
-        if (all) load_tile(st.q, a.Qp + kat * C * DP, sizeof(st.q), bar);
+        if (Sh::kQ) load_tile(st.q, a.Qp + kat * C * DP, sizeof(st.q), bar);
         load_tile(st.rows, a.rows + at * kRowsF, sizeof(st.rows), bar);
         load_tile(st.T, a.Tp + at * 2 * C * C, sizeof(st.T), bar);
-        if (all) load_tile(st.P, a.Pp + at * a.planes * C * C, sizeof(st.P), bar);
+        if (Sh::kQ) load_tile(st.P, a.Pp + at * a.planes * C * C, sizeof(st.P), bar);
     }
-    const RowView &xv = REV ? a.go : a.v;
+    const RowView &xv = MODE == kReverse ? a.go : a.v;
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(xv.p) + b * xv.sb + h * xv.sh + t0 * xv.st + col0;
     const uint32_t sx = smem_u32(st.x);
 #pragma unroll
@@ -501,7 +509,30 @@ __device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first,
     __syncwarp();
 }
 
-// a 16 x 16 piece of a left operand into a tile of `rows` rows
+// 16 rows of a tile that is kept for the gradients, from left operands: through shared memory, from where one copy a panel
+// takes them (stored from the registers, four bytes a lane in eight rows, they took a fifth of the chain's time)
+__device__ __forceinline__ void plane_room(int lane) {  // the copies before have read what they take
+    if (lane == 0) bulk_wait_read();
+    __syncwarp();
+}
+__device__ __forceinline__ void plane_put(char *mem, int k0, const Frag &f, int lane) {
+    const int r = (lane >> 3 & 1) * 8 + (lane & 7);
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(smem_u32(mem) + tile_at(0, 16, r, (k0 >> 3) + (lane >> 4))),
+                 "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3])
+                 : "memory");
+}
+__device__ __forceinline__ void plane_send(const char *mem, __half *tile, int rows, int r0, int panels, int lane) {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+        for (int p = 0; p < panels; ++p)
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 2048;" ::"l"(reinterpret_cast<char *>(tile) + (p * rows + r0) * 128),
+                         "r"(smem_u32(mem) + p * 2048)
+                         : "memory");
+        bulk_commit();
+    }
+}
+// (where a group's warps share rows of 128 bytes) from the registers
 __device__ __forceinline__ void plane_store(__half *tile, int rows, int r0, int k0, const Frag &f, int lane) {
     char *p = reinterpret_cast<char *>(tile) + lane % 4 * 4;
     const int r = r0 + lane / 4;
@@ -511,18 +542,33 @@ __device__ __forceinline__ void plane_store(__half *tile, int rows, int r0, int 
     *reinterpret_cast<uint32_t *>(p + tile_at(0, rows, r + 8, (k0 >> 3) + 1)) = f[3];
 }
 
-template <int DP, int NG, int SP, bool REV>
+template <int DP, int NG, int SP, ChainMode MODE>
 __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
-    using Sh = ChainShared<DP, NG, SP, REV>;
+    using Sh = ChainShared<DP, NG, SP, MODE>;
     extern __shared__ __align__(128) char raw[];
     Sh &sm = *reinterpret_cast<Sh *>(raw);
+    constexpr bool REV = MODE == kReverse;
     constexpr int ND = DP / 8 / SP;  // n-tiles of a state's row that a warp holds
     const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, group = warp / SP, part = warp % SP, d0 = part * (DP / SP);
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * NG * 16, col = col0 + group * 16;
     const int len = head_length(a.lengths, b, a.n), chunks = (len + C - 1) / C, q2 = lane % 4 * 2;
     const bool mine = col < a.dv;  // the warp has columns
-    __nv_bfloat16 *o = a.o ? static_cast<__nv_bfloat16 *>(a.o) + b * a.ob + h * a.oh : nullptr;
+    __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.o) + b * a.ob + h * a.oh;  // (not with kKeep)
+    // what is kept: by copies where a warp has whole rows of 128 bytes
+    char *const mem = sm.planes[SP == 1 ? warp : 0];
+    auto put = [&](__half *tile, int k0, const Frag &f) {
+        if (SP == 1)
+            plane_put(mem, k0, f, lane);
+        else
+            plane_store(tile, a.dvp, col, k0, f, lane);
+    };
+    auto room = [&]() {
+        if (SP == 1) plane_room(lane);
+    };
+    auto send = [&](__half *tile, int panels) {
+        if (SP == 1) plane_send(mem, tile, a.dvp, col, panels, lane);
+    };
     // n-tiles of rows that the warp finishes where a group's warps share that work, for 16 of them (np)
     auto own = [&](int np) { return SP == 1 || np / 2 == part; };
     const int first = SP == 1 ? 0 : part * (C / 2), some = C / SP;
@@ -553,7 +599,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     if (tid < 2) mbar_init(&sm.bar[tid], 1);
     fence_mbar_init();
     __syncthreads();
-    if (chunks > 0) chain_load<DP, NG, SP, REV>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
+    if (chunks > 0) chain_load<DP, NG, SP, MODE>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
     for (int step = 0; step < chunks; ++step) {
         const int chunk = REV ? chunks - 1 - step : step, t0 = chunk * C;
         typename Sh::Stage &st = sm.stage[step & 1];
@@ -567,7 +613,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
             break;
         }
         if (step + 1 < chunks)
-            chain_load<DP, NG, SP, REV>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
+            chain_load<DP, NG, SP, MODE>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
         if (!mine) continue;
         const uint32_t sk = smem_u32(st.k), sq = smem_u32(st.q), sT = smem_u32(st.T), sP = smem_u32(st.P);
         const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + group * 32 + ((lane >> 3) & 1) * 16;
@@ -638,13 +684,16 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
         // x = K S (or K R), with it Q S
         const Scale ss = scale_of(S);
         {
-            __half *ends = REV ? (a.Rp ? a.Rp + (bh * (a.m + 1) + chunk + 1) * a.dvp * DP : nullptr) : (a.Sp ? a.Sp + at * a.dvp * DP : nullptr);
-            if (ends) keep_scale(REV ? chunk + 1 : chunk, ss.back);
+            __half *ends = REV ? a.Rp + (bh * (a.m + 1) + chunk + 1) * a.dvp * DP : a.Sp + at * a.dvp * DP;
+            if (MODE != kOutputs) {
+                keep_scale(REV ? chunk + 1 : chunk, ss.back);
+                room();
+            }
 #pragma unroll
             for (int kt = 0; kt < ND / 2; ++kt) {
                 Frag hi, lo;
                 split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
-                if (ends) plane_store(ends, a.dvp, col, d0 + kt * 16, hi, lane);
+                if (MODE != kOutputs) put(ends, d0 + kt * 16, hi);
 #pragma unroll
                 for (int np = 0; np < 4; ++np) {
                     Frag f;
@@ -653,13 +702,14 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                     mma(x[2 * np + 1], hi, f[2], f[3]);
                     mma(x[2 * np], lo, f[0], f[1]);
                     mma(x[2 * np + 1], lo, f[2], f[3]);
-                    if (!REV && o) {
+                    if (MODE == kOutputs) {
                         right_n(f, sq, C, np * 16, d0 + kt * 16, lane);
                         mma(y[2 * np], hi, f[0], f[1]);
                         mma(y[2 * np + 1], hi, f[2], f[3]);
                     }
                 }
             }
+            if (MODE != kOutputs) send(ends, DP / 64);
         }
         Frag fh[4], fl[4];
         if (!REV) {
@@ -672,7 +722,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                         x[nt][e] *= ss.back;
                         y[nt][e] *= ss.back;
                     }
-                exchange(x, y, o);
+                exchange(x, y, MODE == kOutputs);
                 back_s = 1.0f;
             }
             // x = b (V - c(i, 0) K S)
@@ -717,7 +767,9 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
             for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) u[nt][e] *= back_u;
-            if (o || a.Up) {  // P U; U's plane
+            {  // P U, or U's plane
+                __half *tile = a.Up + at * a.dvp * C;
+                if (MODE == kKeep) room();
 #pragma unroll
                 for (int nt = 0; nt < 8; ++nt)
 #pragma unroll
@@ -727,8 +779,8 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                 for (int kt = 0; kt < 4; ++kt) {
                     const Frag hi = {pack(us.by * u[2 * kt][0], us.by * u[2 * kt][1]), pack(us.by * u[2 * kt][2], us.by * u[2 * kt][3]),
                                      pack(us.by * u[2 * kt + 1][0], us.by * u[2 * kt + 1][1]), pack(us.by * u[2 * kt + 1][2], us.by * u[2 * kt + 1][3])};
-                    if (a.Up && own(kt)) plane_store(a.Up + at * a.dvp * C, a.dvp, col, kt * 16, hi, lane);
-                    if (o)
+                    if (MODE == kKeep && own(kt)) put(tile, kt * 16, hi);
+                    if (MODE == kOutputs)
 #pragma unroll
                         for (int np = kt; np < 4; ++np) {
                             if (!own(np)) continue;
@@ -738,8 +790,10 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                             mma(x[2 * np + 1], hi, f[2], f[3]);
                         }
                 }
-                if (a.Up && lane == 0) scales_of(chunk)[4] = us.back;
-                if (o) {  // scale c(i, 0) Q S + P U
+                if (MODE == kKeep) {
+                    send(tile, 1);
+                    if (lane == 0) scales_of(chunk)[4] = us.back;
+                } else {  // scale c(i, 0) Q S + P U
                     const float back = us.back * back_P;
 #pragma unroll
                     for (int nt = 0; nt < 8; ++nt) {
@@ -776,7 +830,9 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                 }
             }
             const Scale gs = scale_of(warp_max(m)), ps = scale_of(warp_max(mp));
+            __half *const go = a.Gp + at * a.dvp * C;  // dO's plane
             if (lane == 0) scales_of(chunk)[6] = gs.back;
+            room();
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
                 Frag gf;
@@ -787,7 +843,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                     gf[i] = pack(gs.by * g0, gs.by * g1);
                     split(ps.by * (past.x * g0), ps.by * (past.y * g1), fh[kt][i], fl[kt][i]);
                 }
-                if (own(kt)) plane_store(a.Gp + at * a.dvp * C, a.dvp, col, kt * 16, gf, lane);
+                if (own(kt)) put(go, kt * 16, gf);
                 if (SP == 2 && (kt == 0 || kt == 3) != (part == 0)) continue;  // five of the ten blocks each
 #pragma unroll
                 for (int np = 0; np <= kt; ++np) {
@@ -800,6 +856,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                     mma(y[2 * np + 1], gf, f[2], f[3]);
                 }
             }
+            send(go, 1);
             // x = c(C, j) K R + P^T dO
             const float back = gs.back * back_P;
 #pragma unroll
@@ -838,13 +895,16 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                 for (int e = 0; e < 4; ++e) y[nt][e] *= back_x;
             const Scale us = scale_of(y);
             if (lane == 0) scales_of(chunk)[5] = us.back;
+            room();
+            __half *const kept = a.Xp + at * a.dvp * C;
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
                 if (!own(kt)) continue;
                 const Frag hi = {pack(us.by * y[2 * kt][0], us.by * y[2 * kt][1]), pack(us.by * y[2 * kt][2], us.by * y[2 * kt][3]),
                                  pack(us.by * y[2 * kt + 1][0], us.by * y[2 * kt + 1][1]), pack(us.by * y[2 * kt + 1][2], us.by * y[2 * kt + 1][3])};
-                plane_store(a.Xp + at * a.dvp * C, a.dvp, col, kt * 16, hi, lane);
+                put(kept, kt * 16, hi);
             }
+            send(kept, 1);
 #pragma unroll
             for (int nt = 0; nt < 8; ++nt) {
                 const float2 past = factor(0, nt * 8 + q2), beta = factor(2, nt * 8 + q2);
@@ -864,13 +924,17 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     if (REV && mine && chunks > 0) {  // R before the first chunk
         const Scale ss = scale_of(S);
         keep_scale(0, ss.back);
+        room();
+        __half *tile = a.Rp + bh * (a.m + 1) * a.dvp * DP;
 #pragma unroll
         for (int kt = 0; kt < ND / 2; ++kt) {
             Frag hi, lo;
             split_left(S[2 * kt], S[2 * kt + 1], ss.by, hi, lo);
-            plane_store(a.Rp + bh * (a.m + 1) * a.dvp * DP, a.dvp, col, d0 + kt * 16, hi, lane);
+            put(tile, d0 + kt * 16, hi);
         }
+        send(tile, DP / 64);
     }
+    if (lane == 0) bulk_wait();  // (shared memory is read to the end)
     float *last = REV ? a.dS0 : a.S1;
     if (last)
 #pragma unroll
@@ -880,7 +944,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                 int64_t at;
                 if (place(nt, e, at)) last[at] = S[nt][e];
             }
-    if (o)  // rows behind the end, eight columns at a time
+    if (MODE != kKeep)  // rows behind the end, eight columns at a time
         for (int64_t i = tid; i < (int64_t)(a.n - len) * NG * 2; i += Sh::kWarps * 32) {
             const int c = col0 + (int)(i % (NG * 2)) * 8;
             if (c < a.dv) *reinterpret_cast<uint4 *>(o + (len + i / (NG * 2)) * a.ot + c) = make_uint4(0, 0, 0, 0);
@@ -958,6 +1022,13 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         load_tile(sm.go, a.Gp + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.k, a.Kp + kat * C * DP, sizeof(sm.k), &sm.bar[0]);
         load_state(a.Rp + (slot + 1) * dvp * DP, of_state, 1);
+        // what comes later, as far as L2
+        auto ask = [](const void *p, uint32_t bytes) {
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+        };
+        ask(a.Sp + at * dvp * DP, of_state);
+        ask(a.Rp + slot * dvp * DP, of_state);
+        ask(a.Qp + kat * C * DP, sizeof(sm.k));
     }
     const float *rowf = a.rows + at * kRowsF;
     const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
@@ -1271,27 +1342,37 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
             row_sums(dot[0], dot[1], mt, 0);
         }
     }
-    {  // <S, R> before the chunk, R as it lies in memory
+    {  // <S, R> before the chunk: of every 16 columns the diagonal of S^T R, R as it lies in memory (in both the summed
+       // values lie in the same, permuted order: a lane's 16 bytes of a row are those of two products)
         float sum = 0.0f;
-        const uint4 *r = reinterpret_cast<const uint4 *>(a.Rp + slot * dvp * DP);
-        if (here)
-#pragma unroll 2
-            for (int i = tid; i < dvp * (DP / 8); i += kGradThreads) {
-                const uint4 y4 = r[i], x4 = *reinterpret_cast<const uint4 *>(sm.s + i * 16);
-                const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w}, y[4] = {y4.x, y4.y, y4.z, y4.w};
-                float part = 0.0f;
+        if (here && warp < groups) {
+            const char *r = reinterpret_cast<const char *>(a.Rp + slot * dvp * DP);
+            const int ra = warp * 16 + lane / 4;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = half_pair(x[e]), g = half_pair(y[e]);
-                    part = fmaf(f.x, g.x, fmaf(f.y, g.y, part));
+            for (int side = 0; side < 2; ++side) {
+                float c[2][4];
+                zero(c);
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) {
+                    const int piece = (side * (DP / 64) + i) * 4 + lane % 4;
+                    const uint32_t at0 = tile_at(0, dvp, ra, piece), at1 = tile_at(0, dvp, ra + 8, piece);
+                    const uint4 s0 = *reinterpret_cast<const uint4 *>(sm.s + at0), s1 = *reinterpret_cast<const uint4 *>(sm.s + at1);
+                    const uint4 r0_ = *reinterpret_cast<const uint4 *>(r + at0), r1 = *reinterpret_cast<const uint4 *>(r + at1);
+                    const Frag f = {s0.x, s1.x, s0.y, s1.y}, g = {s0.z, s1.z, s0.w, s1.w};
+                    mma(c[0], f, r0_.x, r0_.y);
+                    mma(c[0], g, r0_.z, r0_.w);
+                    mma(c[1], f, r1.x, r1.y);
+                    mma(c[1], g, r1.z, r1.w);
                 }
-                // (panels of 64 columns, in which pieces are swizzled among eight)
-                const int row = i / 8 % dvp, column = DP == 64 ? ((i & 7) ^ (row & 7)) * 8 : i / 8 / dvp * 64;
-                const float *f = sm.scales[row / 16];
-                const int side = column >= DP / 2;
-                sum = fmaf(f[side] * f[2 + side], part, sum);
+                const float *scale = sm.scales[warp];
+                float diag = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (lane / 4 == q2 + e) diag += c[0][e] + c[1][2 + e];
+                sum = fmaf(scale[side] * scale[2 + side], diag, sum);
             }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        }
+        sum = sum + __shfl_xor_sync(0xffffffffu, sum, 16);
 #pragma unroll
         for (int w = 8; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         if (lane == 0) sm.total[warp] = sum;
@@ -1360,23 +1441,23 @@ cudaError_t prepare(const DeltaArgs &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-template <int DP, int NG, int SP, bool REV>
+template <int DP, int NG, int SP, ChainMode MODE>
 cudaError_t chain_launch(const DeltaArgs &a, cudaStream_t s) {
-    using Sh = ChainShared<DP, NG, SP, REV>;
-    cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NG, SP, REV>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
+    using Sh = ChainShared<DP, NG, SP, MODE>;
+    cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NG, SP, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, NG * 16));
-    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NG, SP, REV>), grid, NG * SP * 32, sizeof(Sh), s, a);
+    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NG, SP, MODE>), grid, NG * SP * 32, sizeof(Sh), s, a);
     return cudaGetLastError();
 }
 
 // With few heads, few columns a block and two warps for 16 of them, so that the chains spread over the SMs.
-template <int DP, bool REV>
+template <int DP, ChainMode MODE>
 cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
     const int64_t bh = (int64_t)a.B * a.H, sms = tc_sm_count();
-    if (a.dv > 64 && bh * cdiv(a.dv, 64) > sms) return chain_launch<DP, 8, 1, REV>(a, s);
-    if (a.dv > 32 && bh * cdiv(a.dv, 32) > sms) return chain_launch<DP, 4, 1, REV>(a, s);
-    return chain_launch<DP, 2, 2, REV>(a, s);
+    if (a.dv > 64 && bh * cdiv(a.dv, 64) > sms) return chain_launch<DP, 8, 1, MODE>(a, s);
+    if (a.dv > 32 && bh * cdiv(a.dv, 32) > sms) return chain_launch<DP, 4, 1, MODE>(a, s);
+    return chain_launch<DP, 2, 2, MODE>(a, s);
 }
 
 }  // namespace
@@ -1406,8 +1487,8 @@ cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s) {
 }
 
 cudaError_t launch_delta_chain(const DeltaArgs &a, bool reverse, cudaStream_t s) {
-    if (a.d <= 64) return reverse ? chain<64, true>(a, s) : chain<64, false>(a, s);
-    return reverse ? chain<128, true>(a, s) : chain<128, false>(a, s);
+    if (a.d <= 64) return reverse ? chain<64, kReverse>(a, s) : a.Up ? chain<64, kKeep>(a, s) : chain<64, kOutputs>(a, s);
+    return reverse ? chain<128, kReverse>(a, s) : a.Up ? chain<128, kKeep>(a, s) : chain<128, kOutputs>(a, s);
 }
 
 }  // namespace luna
