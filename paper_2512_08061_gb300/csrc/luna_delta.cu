@@ -1,4 +1,5 @@
-// The gated delta rule on CUDA cores: the recurrence row by row, its gradients by chunk, single tokens.
+// The gated delta rule in fp32, on CUDA cores: the recurrence four rows at a time, its gradients by chunk; and single
+// tokens of either type.
 #include <math.h>
 
 #include "luna_delta.cuh"
@@ -10,13 +11,28 @@ namespace {
 // ---------------------------------------------------------------------------
 // The recurrence, forward (S, from which u and o) and in reverse (R, from which x and dV).
 //
-// A column of the state takes part in no other: eight lanes hold one column, 16 rows each at d = 128, and a block
-// of 128 threads 16 columns.  A row is a dot product of the column with k (eight lanes' sums joined by three
-// shuffles), what the token writes, the update and the dot product with q.  Rows come in tiles of 16 through shared
-// memory, the next tile's on their way in registers.  Bound by that chain of some 200 cycles a row, whatever the
-// width.
+// A column of the state takes part in no other: eight lanes hold one column, 16 values each at d = 128, and a block of
+// 128 threads 16 columns.  Four rows go at a time: their dot products with the state before them are summed over the
+// eight lanes together, and what they do to each other is known from the dot products of the rows themselves:
+//
+//     u_i = b_i (v_i - A_i k_i . S - sum_{j < i} M_ij u_j),   o_i = scale (A_i q_i . S + sum_{j <= i} N_ij u_j)
+//     S <- A S + sum_j L_j k_j u_j
+//
+// with A_i = exp(g_0 + .. + g_i), M_ij and N_ij = exp(g_{j+1} + .. + g_i) times k_i . k_j and q_i . k_j.  In reverse the
+// rows of the four count from the last, G_i is scale dO_i, N_ij from k_i . q_j, a row's decay comes behind it, and
+//
+//     x_i = A_i k_i . R + sum_{j <= i} N_ij G_j - sum_{j < i} M_ij b_j x_j,   R <- A R + sum_j L_j (q_j G_j - b_j k_j x_j)
+//
+// Rows come in tiles of 16 through shared memory.  Four warps carry the columns; four more fetch the tile after the next,
+// work out the rows' own products of the next and write the outputs of the one before, so that the columns' warps, whose
+// chain bounds the pass, do nothing else (with all of that in the same warps a row took 435 ns at d = 128, and as long
+// with one row at a time).
 
-constexpr int kRowCols = 16, kRowThreads = 128, kTile = 16;
+constexpr int kRowCols = 16, kRowThreads = 256, kTile = 16, kFour = 4;
+
+struct Four {  // of four rows
+    float b[kFour], A[kFour], L[kFour], M[kFour][kFour], N[kFour][kFour], all, rest;
+};
 
 // sums over the eight lanes of a column
 __device__ __forceinline__ float lanes8(float x) {
@@ -29,32 +45,142 @@ __device__ __forceinline__ float lanes8(float x) {
 // of a s alone would be off the same way at every row too (2e-4 of the state after 20000 rows of a = 1 - 1e-6).
 __device__ __forceinline__ float decayed(float a, float rest, float s, float x) { return fmaf(a, s, fmaf(rest, s, x)); }
 
-template <typename IO, int JD, bool REV>
-__global__ void __launch_bounds__(kRowThreads) k_delta_rows(DeltaArgs a) {
-    constexpr int DP = 32 * JD, PER = kTile * DP / kRowThreads;  // padded width; values of k (and q) a thread loads
-    __shared__ float4 sk[kTile][DP / 4], sq[kTile][DP / 4];
-    __shared__ float sx[kTile][kRowCols], sy[kTile][kRowCols], sz[kTile][kRowCols];
-    __shared__ float sa[kTile], sr[kTile], sb[kTile];
-    const int tid = threadIdx.x, p = tid % 8, cl = tid / 8;
+template <int JD>
+struct RowTile {
+    float4 k[kTile][8 * JD + 1], q[kTile][8 * JD + 1];  // (the padding: rows start in different banks)
+    float x[kTile][kRowCols], y[kTile][kRowCols], z[kTile][kRowCols], g[kTile];
+    Four four[kTile / kFour];
+};
+
+template <int JD, bool REV>
+__global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(DeltaArgs a) {
+    constexpr int DP = 32 * JD, LOADERS = kRowThreads / 2, PER = kTile * DP / LOADERS;  // padded width; values of k (and q) a loader fetches
+    __shared__ RowTile<JD> tile_[2];
+    const int tid = threadIdx.x % LOADERS, p = tid % 8, cl = tid / 8;
+    const bool loads = threadIdx.x >= LOADERS;
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * kRowCols, col = col0 + cl;
     const int len = head_length(a.lengths, b, a.n), tiles = (len + kTile - 1) / kTile;
-    const int hk = h / (a.H / a.k.heads);
-    const IO *k = static_cast<const IO *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
-    const IO *q = static_cast<const IO *>(a.q.p) + b * a.q.sb + hk * a.q.sh;
-    const RowView &xv = REV ? a.go : a.v;
-    const IO *x = static_cast<const IO *>(xv.p) + b * xv.sb + h * xv.sh;
-    IO *o = a.o ? static_cast<IO *>(a.o) + b * a.ob + h * a.oh : nullptr;
-    float *U = REV ? a.X : a.U;
-    if (U) U += bh * a.n * a.dv;
     const int64_t E = (int64_t)a.d * a.dv;
+    const RowView &xv = REV ? a.go : a.v;
+    float *o = a.o ? static_cast<float *>(a.o) + b * a.ob + h * a.oh : nullptr;
+    if (!REV && bh == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status = 0;  // (the call's first kernel; none of this form sets it)
+    auto tile_of = [&](int step) { return REV ? tiles - 1 - step : step; };
+    auto at = [](int f, int i) { return f * kFour + (REV ? kFour - 1 - i : i); };  // rows of a four in the order they are taken
+
+    if (loads) {
+        const int hk = h / (a.H / a.k.heads);
+        const float *k = static_cast<const float *>(a.k.p) + b * a.k.sb + hk * a.k.sh;
+        const float *q = static_cast<const float *>(a.q.p) + b * a.q.sb + hk * a.q.sh;
+        const float *x = static_cast<const float *>(xv.p) + b * xv.sb + h * xv.sh;
+        float *U = REV ? a.X : a.U;
+        if (U) U += bh * a.n * a.dv;
+        float nk[PER], nq[PER], nx[2], ng = 0.0f, nb = 0.0f;
+        auto fetch = [&](int tile) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int w = tid + i * LOADERS, t = tile * kTile + w / DP, c = w % DP;
+                const bool in = t < len && c < a.d;
+                nk[i] = in ? k[t * a.k.st + c] : 0.0f;
+                nq[i] = in ? q[t * a.q.st + c] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int w = tid + i * LOADERS, t = tile * kTile + w / kRowCols, c = col0 + w % kRowCols;
+                nx[i] = t < len && c < a.dv ? x[t * xv.st + c] : 0.0f;
+            }
+            if (tid < kTile) {
+                const int t = tile * kTile + tid;
+                ng = t < len ? gate_at<float>(a.g, b, h, t) : 0.0f;  // (behind the end: k = q = b = g = 0, which changes nothing)
+                nb = t < len ? gate_at<float>(a.b, b, h, t) : 0.0f;
+            }
+        };
+        // the fetched rows into a tile, and what its fours need
+        auto prepare = [&](RowTile<JD> &sm) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int w = tid + i * LOADERS;
+                reinterpret_cast<float *>(sm.k[w / DP])[w % DP] = nk[i];
+                reinterpret_cast<float *>(sm.q[w / DP])[w % DP] = nq[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) (&sm.x[0][0])[tid + i * LOADERS] = nx[i];
+            if (tid < kTile) {
+                sm.g[tid] = ng;
+                sm.four[tid / kFour].b[REV ? kFour - 1 - tid % kFour : tid % kFour] = nb;
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(LOADERS) : "memory");
+            // two threads a dot product: of the 16 of a four those with j <= i, k_i . k_j (j < i) and N's
+            const int f = tid / 32, lane = tid % 32, i = lane / 8, j = lane / 2 % 4, part = lane % 2;
+            Four &four = sm.four[f];
+            float kk = 0.0f, nn = 0.0f;
+            if (j <= i) {
+                const float4 *ki = sm.k[at(f, i)], *kj = sm.k[at(f, j)], *qi = sm.q[at(f, REV ? j : i)];
+#pragma unroll 4
+                for (int c = part; c < DP / 4; c += 2) {
+                    const float4 x4 = ki[c], y4 = kj[c], z4 = qi[c], w4 = REV ? x4 : y4;
+                    kk = fmaf(x4.x, y4.x, fmaf(x4.y, y4.y, fmaf(x4.z, y4.z, fmaf(x4.w, y4.w, kk))));
+                    nn = fmaf(w4.x, z4.x, fmaf(w4.y, z4.y, fmaf(w4.z, z4.z, fmaf(w4.w, z4.w, nn))));
+                }
+            }
+            kk += __shfl_xor_sync(0xffffffffu, kk, 1);
+            nn += __shfl_xor_sync(0xffffffffu, nn, 1);
+            // gates between: forward those of j + 1 .. i, in reverse of j .. i - 1
+            auto between = [&](int from, int to) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < kFour; ++r)
+                    if (r >= from && r < to) sum += sm.g[at(f, r)];
+                return sum;
+            };
+            if (part == 0 && j <= i) {
+                const float c = expf(REV ? between(j, i) : between(j + 1, i + 1));
+                four.M[i][j] = c * kk;
+                four.N[i][j] = REV ? a.scale * c * nn : c * nn;
+            }
+            if (lane < kFour) {
+                four.A[lane] = expf(REV ? between(0, lane) : between(0, lane + 1));
+                four.L[lane] = expf(REV ? between(lane, kFour) : between(lane + 1, kFour));
+            }
+            if (lane == kFour) gate_terms(between(0, kFour), four.all, four.rest);
+        };
+        auto write = [&](const RowTile<JD> &sm, int tile) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int w = tid + i * LOADERS, t = w / kRowCols, c = w % kRowCols;
+                const int64_t r = tile * kTile + t;
+                if (r < len && col0 + c < a.dv) {
+                    if (o) o[r * a.ot + col0 + c] = sm.y[t][c];
+                    if (U) U[r * a.dv + col0 + c] = sm.z[t][c];
+                }
+            }
+        };
+        if (tiles > 0) {
+            fetch(tile_of(0));
+            prepare(tile_[0]);
+        }
+        if (tiles > 1) fetch(tile_of(1));
+        __syncthreads();
+        for (int step = 0; step < tiles; ++step) {
+            if (step > 0) write(tile_[(step - 1) & 1], tile_of(step - 1));
+            if (step + 1 < tiles) prepare(tile_[(step + 1) & 1]);  // (which leaves y and z alone)
+            if (step + 2 < tiles) fetch(tile_of(step + 2));
+            __syncthreads();
+        }
+        if (tiles > 0) write(tile_[(tiles - 1) & 1], tile_of(tiles - 1));
+        if (o)
+            for (int64_t i = tid; i < (int64_t)(a.n - len) * kRowCols; i += LOADERS) {
+                const int c = col0 + (int)(i % kRowCols);
+                if (c < a.dv) o[(len + i / kRowCols) * a.ot + c] = 0.0f;
+            }
+        return;
+    }
+
     float *ends = REV ? a.after : a.before;
     if (ends) ends += bh * (a.m + 1) * E;
     const float *init = REV ? a.dS1 : a.S0;
     float *last = REV ? a.dS0 : a.S1;
-
-    if (!REV && bh == 0 && blockIdx.y == 0 && tid == 0) *a.status = 0;  // (the call's first kernel; none of this form sets it)
-    float s[JD][4], fade = 1.0f, fade2 = 0.0f;  // (reverse) the decay of the row before is still to be applied
+    float s[JD][4];
     auto row = [&](int j, int e) { return j * 32 + p * 4 + e; };
     auto keep = [&](float *to) {
         if (col < a.dv)
@@ -62,116 +188,98 @@ __global__ void __launch_bounds__(kRowThreads) k_delta_rows(DeltaArgs a) {
             for (int j = 0; j < JD; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (row(j, e) < a.d) to[(int64_t)row(j, e) * a.dv + col] = decayed(fade, fade2, s[j][e], 0.0f);
+                    if (row(j, e) < a.d) to[(int64_t)row(j, e) * a.dv + col] = s[j][e];
     };
 #pragma unroll
     for (int j = 0; j < JD; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             s[j][e] = init && col < a.dv && row(j, e) < a.d ? init[bh * E + (int64_t)row(j, e) * a.dv + col] : 0.0f;
+    constexpr int kTiles = kDeltaRows / kTile;  // of a chunk
     if (REV && ends) keep(ends + (int64_t)((len + kDeltaRows - 1) / kDeltaRows) * E);
-
-    float nk[PER], nq[PER], nx[2], ng = 0.0f, nb = 0.0f;
-    auto fetch = [&](int tile) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = tid + i * kRowThreads, t = tile * kTile + at / DP, c = at % DP;
-            const bool in = t < len && c < a.d;
-            nk[i] = in ? io_load(k + t * a.k.st + c) : 0.0f;
-            nq[i] = in ? io_load(q + t * a.q.st + c) : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = tid + i * kRowThreads, t = tile * kTile + at / kRowCols, c = col0 + at % kRowCols;
-            nx[i] = t < len && c < a.dv ? io_load(x + t * xv.st + c) : 0.0f;
-        }
-        if (tid < kTile && tile * kTile + tid < len) {
-            ng = gate_at<IO>(a.g, b, h, tile * kTile + tid);
-            nb = gate_at<IO>(a.b, b, h, tile * kTile + tid);
-        }
-    };
-    if (tiles > 0) fetch(REV ? tiles - 1 : 0);
+    __syncthreads();
     for (int step = 0; step < tiles; ++step) {
-        const int tile = REV ? tiles - 1 - step : step, rows = min(kTile, len - tile * kTile);
+        RowTile<JD> &sm = tile_[step & 1];
+        const int tile = tile_of(step);
+        if (!REV && ends && tile % kTiles == 0) keep(ends + (int64_t)(tile / kTiles) * E);
+#pragma unroll 1
+        for (int r = 0; r < kTile / kFour; ++r) {
+            const int f = REV ? kTile / kFour - 1 - r : r;
+            const Four &c = sm.four[f];
+            float dk[kFour], dq[kFour], u[kFour];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = tid + i * kRowThreads;
-            reinterpret_cast<float *>(sk)[at] = nk[i];
-            reinterpret_cast<float *>(sq)[at] = nq[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) (&sx[0][0])[tid + i * kRowThreads] = nx[i];
-        if (tid < kTile) {
-            gate_terms(ng, sa[tid], sr[tid]);
-            sb[tid] = nb;
-        }
-        __syncthreads();
-        if (step + 1 < tiles) fetch(REV ? tile - 1 : tile + 1);
-        if (!REV && ends && tile % (kDeltaRows / kTile) == 0) keep(ends + (int64_t)(tile / (kDeltaRows / kTile)) * E);
-        for (int r = 0; r < rows; ++r) {
-            const int t = REV ? rows - 1 - r : r;
-            const float lam = sa[t], rest = sr[t], beta = sb[t], xc = sx[t][cl];
-            float4 kk[JD], qq[JD];
-#pragma unroll
-            for (int j = 0; j < JD; ++j) { kk[j] = sk[t][j * 8 + p]; qq[j] = sq[t][j * 8 + p]; }
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            if (!REV) {
+            for (int i = 0; i < kFour; ++i) {
+                float x0 = 0.0f, x1 = 0.0f, y0 = 0.0f, y1 = 0.0f;
 #pragma unroll
                 for (int j = 0; j < JD; ++j) {
-                    acc[0] = fmaf(kk[j].x, s[j][0], acc[0]); acc[1] = fmaf(kk[j].y, s[j][1], acc[1]);
-                    acc[2] = fmaf(kk[j].z, s[j][2], acc[2]); acc[3] = fmaf(kk[j].w, s[j][3], acc[3]);
+                    const float4 kk = sm.k[at(f, i)][j * 8 + p];
+                    x0 = fmaf(kk.x, s[j][0], fmaf(kk.y, s[j][1], x0));
+                    x1 = fmaf(kk.z, s[j][2], fmaf(kk.w, s[j][3], x1));
+                    if (!REV) {
+                        const float4 qq = sm.q[at(f, i)][j * 8 + p];
+                        y0 = fmaf(qq.x, s[j][0], fmaf(qq.y, s[j][1], y0));
+                        y1 = fmaf(qq.z, s[j][2], fmaf(qq.w, s[j][3], y1));
+                    }
                 }
-                const float dot = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3]));
-                const float u = beta * (xc - fmaf(lam, dot, rest * dot));
-                acc[0] = acc[1] = acc[2] = acc[3] = 0.0f;
+                dk[i] = x0 + x1;
+                dq[i] = y0 + y1;
+            }
 #pragma unroll
-                for (int j = 0; j < JD; ++j) {
-                    s[j][0] = decayed(lam, rest, s[j][0], kk[j].x * u); s[j][1] = decayed(lam, rest, s[j][1], kk[j].y * u);
-                    s[j][2] = decayed(lam, rest, s[j][2], kk[j].z * u); s[j][3] = decayed(lam, rest, s[j][3], kk[j].w * u);
-                    acc[0] = fmaf(qq[j].x, s[j][0], acc[0]); acc[1] = fmaf(qq[j].y, s[j][1], acc[1]);
-                    acc[2] = fmaf(qq[j].z, s[j][2], acc[2]); acc[3] = fmaf(qq[j].w, s[j][3], acc[3]);
-                }
-                const float y = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3]));
-                if (p == 0) { sy[t][cl] = a.scale * y; sz[t][cl] = u; }
-            } else {
-                const float g = a.scale * xc;
+            for (int i = 0; i < kFour; ++i) {
+                dk[i] = lanes8(dk[i]);
+                if (!REV) dq[i] = lanes8(dq[i]);
+            }
 #pragma unroll
-                for (int j = 0; j < JD; ++j) {
-                    s[j][0] = decayed(fade, fade2, s[j][0], qq[j].x * g); s[j][1] = decayed(fade, fade2, s[j][1], qq[j].y * g);
-                    s[j][2] = decayed(fade, fade2, s[j][2], qq[j].z * g); s[j][3] = decayed(fade, fade2, s[j][3], qq[j].w * g);
-                    acc[0] = fmaf(kk[j].x, s[j][0], acc[0]); acc[1] = fmaf(kk[j].y, s[j][1], acc[1]);
-                    acc[2] = fmaf(kk[j].z, s[j][2], acc[2]); acc[3] = fmaf(kk[j].w, s[j][3], acc[3]);
-                }
-                const float du = lanes8((acc[0] + acc[1]) + (acc[2] + acc[3])), w = -beta * du;
+            for (int i = 0; i < kFour; ++i) {
+                const float xc = sm.x[at(f, i)][cl];
+                if (!REV) {
+                    float w = fmaf(-c.A[i], dk[i], xc);
 #pragma unroll
-                for (int j = 0; j < JD; ++j) {
-                    s[j][0] = fmaf(kk[j].x, w, s[j][0]); s[j][1] = fmaf(kk[j].y, w, s[j][1]);
-                    s[j][2] = fmaf(kk[j].z, w, s[j][2]); s[j][3] = fmaf(kk[j].w, w, s[j][3]);
+                    for (int j = 0; j < i; ++j) w = fmaf(-c.M[i][j], u[j], w);
+                    u[i] = c.b[i] * w;
+                    float y = c.A[i] * dq[i];
+#pragma unroll
+                    for (int j = 0; j <= i; ++j) y = fmaf(c.N[i][j], u[j], y);
+                    if (p == 0) { sm.y[at(f, i)][cl] = a.scale * y; sm.z[at(f, i)][cl] = u[i]; }
+                } else {
+                    dq[i] = xc;  // (dO_i)
+                    float w = c.A[i] * dk[i];
+#pragma unroll
+                    for (int j = 0; j <= i; ++j) w = fmaf(c.N[i][j], dq[j], w);
+#pragma unroll
+                    for (int j = 0; j < i; ++j) w = fmaf(-c.M[i][j], u[j], w);
+                    u[i] = c.b[i] * w;
+                    if (p == 0) { sm.y[at(f, i)][cl] = u[i]; sm.z[at(f, i)][cl] = w; }
                 }
-                fade = lam;
-                fade2 = rest;
-                if (p == 0) { sy[t][cl] = -w; sz[t][cl] = du; }
+            }
+#pragma unroll
+            for (int i = 0; i < kFour; ++i) {
+                dq[i] *= a.scale * c.L[i];
+                u[i] *= REV ? -c.L[i] : c.L[i];
+            }
+#pragma unroll
+            for (int j = 0; j < JD; ++j) {
+                float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < kFour; ++i) {
+                    const float4 kk = sm.k[at(f, i)][j * 8 + p];
+                    t[0] = fmaf(kk.x, u[i], t[0]); t[1] = fmaf(kk.y, u[i], t[1]);
+                    t[2] = fmaf(kk.z, u[i], t[2]); t[3] = fmaf(kk.w, u[i], t[3]);
+                    if (REV) {
+                        const float4 qq = sm.q[at(f, i)][j * 8 + p];
+                        t[0] = fmaf(qq.x, dq[i], t[0]); t[1] = fmaf(qq.y, dq[i], t[1]);
+                        t[2] = fmaf(qq.z, dq[i], t[2]); t[3] = fmaf(qq.w, dq[i], t[3]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[j][e] = decayed(c.all, c.rest, s[j][e], t[e]);
             }
         }
-        if (REV && ends && tile % (kDeltaRows / kTile) == 0) keep(ends + (int64_t)(tile / (kDeltaRows / kTile)) * E);
+        if (REV && ends && tile % kTiles == 0) keep(ends + (int64_t)(tile / kTiles) * E);
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = tid + i * kRowThreads, t = at / kRowCols, c = at % kRowCols;
-            if (t < rows && col0 + c < a.dv) {
-                const int64_t r = tile * kTile + t;
-                if (o) io_store(o + r * a.ot + col0 + c, sy[t][c]);
-                if (U) U[r * a.dv + col0 + c] = sz[t][c];
-            }
-        }
     }
     if (!REV && ends) keep(ends + (int64_t)((len + kDeltaRows - 1) / kDeltaRows) * E);
     if (last) keep(last + bh * E);
-    if (o)
-        for (int64_t i = tid; i < (int64_t)(a.n - len) * kRowCols; i += kRowThreads) {
-            const int c = col0 + (int)(i % kRowCols);
-            if (c < a.dv) io_store(o + (len + i / kRowCols) * a.ot + c, 0.0f);
-        }
 }
 
 // ---------------------------------------------------------------------------
@@ -221,7 +329,6 @@ __device__ __forceinline__ void grad_product(GradShared &sm, float (&acc)[4][NC]
     }
 }
 
-template <typename IO, typename OUT>
 __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     extern __shared__ char raw[];
     GradShared &sm = *reinterpret_cast<GradShared *>(raw);
@@ -231,14 +338,14 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     const int chunk = (int)(blockIdx.x % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
     const int len = head_length(a.lengths, b, a.n), rows = max(0, min(C, len - t0));
     const int hk = h / (a.H / a.k.heads);
-    const IO *q = static_cast<const IO *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st;
-    const IO *k = static_cast<const IO *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st;
-    const IO *v = static_cast<const IO *>(a.v.p) + b * a.v.sb + h * a.v.sh + t0 * a.v.st;
-    const IO *go = static_cast<const IO *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st;
-    OUT *dq = static_cast<OUT *>(a.dq) + b * a.dqb + h * a.dqh + t0 * a.dqt;
-    OUT *dk = static_cast<OUT *>(a.dk) + b * a.dkb + h * a.dkh + t0 * a.dkt;
-    IO *dg = static_cast<IO *>(a.dg.p) + b * a.dg.sb + h * a.dg.sh + t0 * a.dg.st;
-    IO *db = static_cast<IO *>(a.db.p) + b * a.db.sb + h * a.db.sh + t0 * a.db.st;
+    const float *q = static_cast<const float *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st;
+    const float *k = static_cast<const float *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st;
+    const float *v = static_cast<const float *>(a.v.p) + b * a.v.sb + h * a.v.sh + t0 * a.v.st;
+    const float *go = static_cast<const float *>(a.go.p) + b * a.go.sb + h * a.go.sh + t0 * a.go.st;
+    float *dq = static_cast<float *>(a.dq) + b * a.dqb + h * a.dqh + t0 * a.dqt;
+    float *dk = static_cast<float *>(a.dk) + b * a.dkb + h * a.dkh + t0 * a.dkt;
+    float *dg = static_cast<float *>(a.dg.p) + b * a.dg.sb + h * a.dg.sh + t0 * a.dg.st;
+    float *db = static_cast<float *>(a.db.p) + b * a.db.sb + h * a.db.sh + t0 * a.db.st;
     const int out_rows = min(C, a.n - t0);
     for (int i = tid; i < (out_rows - rows) * a.d; i += kGradThreads) {
         const int t = rows + i / a.d, c = i % a.d;
@@ -257,13 +364,13 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     const int d = a.d, dv = a.dv;
 
     if (tid < 32)
-        delta_gate_sums(tid, [&](int t) { return t < rows ? gate_at<IO>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
+        delta_gate_sums(tid, [&](int t) { return t < rows ? gate_at<float>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
                         sm.past, sm.left);
     else if (tid < 32 + C)
-        sm.b[tid - 32] = tid - 32 < rows ? gate_at<IO>(a.b, b, h, t0 + tid - 32) : 0.0f;
+        sm.b[tid - 32] = tid - 32 < rows ? gate_at<float>(a.b, b, h, t0 + tid - 32) : 0.0f;
     __syncthreads();
     auto gap = [&](int i, int j) { return expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])); };
-    auto at = [&](const IO *x, int64_t st, int t, int c, int w) { return t < rows && c < w ? io_load(x + t * st + c) : 0.0f; };
+    auto at = [&](const float *x, int64_t st, int t, int c, int w) { return t < rows && c < w ? io_load(x + t * st + c) : 0.0f; };
     auto in = [&](const float *x, int t, int c) { return t < rows && c < dv ? x[(int64_t)t * dv + c] : 0.0f; };
     auto fK = [&](int kk, int c) { return at(k, a.k.st, kk, c, d); };
     auto fQ = [&](int kk, int c) { return at(q, a.q.st, kk, c, d); };
@@ -389,7 +496,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         float all = 0.0f;
         for (int w = 0; w < kGradThreads / 32; ++w) all += sm.total[w];
         delta_gate_grads(all, sm.read, sm.wrote, rows, tid, [&](int t, float x) {
-            io_store(dg + t * a.dg.st, expf(gate_at<IO>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
+            io_store(dg + t * a.dg.st, expf(gate_at<float>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
         });
     }
 }
@@ -509,36 +616,29 @@ __global__ void __launch_bounds__(kStepThreads) k_delta_step(DeltaStep a) {
 
 unsigned cdiv(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
 
-template <typename IO, bool REV>
+template <bool REV>
 cudaError_t rows(const DeltaArgs &a, cudaStream_t s) {
     const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, kRowCols));
     if (a.d <= 32)
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 1, REV>), grid, kRowThreads, 0, s, a);
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<1, REV>), grid, kRowThreads, 0, s, a);
     else if (a.d <= 64)
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 2, REV>), grid, kRowThreads, 0, s, a);
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<2, REV>), grid, kRowThreads, 0, s, a);
     else
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<IO, 4, REV>), grid, kRowThreads, 0, s, a);
-    return cudaGetLastError();
-}
-
-template <typename IO, typename OUT>
-cudaError_t grad(const DeltaArgs &a, cudaStream_t s) {
-    cudaError_t e = cudaFuncSetAttribute(k_delta_grad<IO, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GradShared));
-    if (e != cudaSuccess) return e;
-    LUNA_LAUNCH("delta_grad", (k_delta_grad<IO, OUT>), (unsigned)((int64_t)a.B * a.H * a.m), kGradThreads, sizeof(GradShared), s, a);
+        LUNA_LAUNCH("delta_rows", (k_delta_rows<4, REV>), grid, kRowThreads, 0, s, a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s) {
-    if (io == LUNA_F32) return reverse ? rows<float, true>(a, s) : rows<float, false>(a, s);
-    return reverse ? rows<__nv_bfloat16, true>(a, s) : rows<__nv_bfloat16, false>(a, s);
+cudaError_t launch_delta_rows(const DeltaArgs &a, bool reverse, cudaStream_t s) {
+    return reverse ? rows<true>(a, s) : rows<false>(a, s);
 }
 
-cudaError_t launch_delta_grad(const DeltaArgs &a, luna_dtype io, luna_dtype out, cudaStream_t s) {
-    if (io == LUNA_F32) return grad<float, float>(a, s);
-    return out == LUNA_F32 ? grad<__nv_bfloat16, float>(a, s) : grad<__nv_bfloat16, __nv_bfloat16>(a, s);
+cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s) {
+    cudaError_t e = cudaFuncSetAttribute(k_delta_grad, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(GradShared));
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("delta_grad", k_delta_grad, (unsigned)((int64_t)a.B * a.H * a.m), kGradThreads, sizeof(GradShared), s, a);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_delta_step(const DeltaStep &a, luna_dtype io, cudaStream_t s) {

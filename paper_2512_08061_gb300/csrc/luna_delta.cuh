@@ -63,6 +63,7 @@ struct DeltaArgs {
     __half *Kp, *Qp, *Tp, *Pp, *Up, *Xp, *Gp, *Sp, *Rp;
     float *rows, *scales;
     int planes, dvp;
+    bool vec;               // every row of every tensor starts on a 16-byte boundary and has whole vectors
     int *status;            // the call's status word
 };
 
@@ -149,8 +150,9 @@ __device__ __forceinline__ void delta_gate_grads(float base, const float *read, 
     if (2 * lane + 1 < rows) store(2 * lane + 1, base - x[0]);
 }
 
-cudaError_t launch_delta_rows(const DeltaArgs &a, luna_dtype io, bool reverse, cudaStream_t s);
-cudaError_t launch_delta_grad(const DeltaArgs &a, luna_dtype io, luna_dtype out, cudaStream_t s);
+cudaError_t launch_delta_rows(const DeltaArgs &a, bool reverse, cudaStream_t s);  // fp32
+cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s);
+// bf16, on tensor cores
 cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s);
 cudaError_t launch_delta_chain(const DeltaArgs &a, bool reverse, cudaStream_t s);
 cudaError_t launch_delta_grad_tc(const DeltaArgs &a, luna_dtype out, cudaStream_t s);

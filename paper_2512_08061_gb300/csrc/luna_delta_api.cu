@@ -52,8 +52,7 @@ luna_status check(const luna_delta_desc *dd) {
 
 bool empty(const luna_delta_desc *dd) { return (int64_t)dd->B * dd->H == 0; }
 
-// Offsets of the parts of a workspace.  Which form runs is known at the call alone (by the tensors' alignment): both
-// lie in the same bytes.
+// Offsets of the parts of a workspace.
 struct Plan {
     int m, dvp, dp;
     size_t dq = 0, dk = 0;                          // gradients of shared queries and keys, one for each head
@@ -63,8 +62,9 @@ struct Plan {
     size_t fwd = 256, bwd = 256;
 };
 
-// Widths that the tensor-core form takes.
-bool tc_widths(const luna_delta_desc *dd) { return dd->io == LUNA_BF16 && dd->d % 8 == 0 && dd->dv % 8 == 0; }
+// fp32 runs on CUDA cores, bf16 on tensor cores.
+bool on_tc(const luna_delta_desc *dd) { return dd->io == LUNA_BF16; }
+bool whole_vectors(const luna_delta_desc *dd) { return dd->d % 8 == 0 && dd->dv % 8 == 0; }
 
 Plan make_plan(const luna_delta_desc *dd) {
     Plan p;
@@ -75,8 +75,7 @@ Plan make_plan(const luna_delta_desc *dd) {
     size_t at = 256;
     auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)align256(bytes); return o; };
     const int64_t tile = (int64_t)kDeltaRows * kDeltaRows * 2, chunks = BH * p.m;
-    const bool tc = tc_widths(dd);
-    if (tc) {
+    if (on_tc(dd)) {
         p.rows = take(chunks * kDeltaFactors * 4);
         p.K = take((int64_t)dd->B * dd->Hk * p.m * kDeltaRows * p.dp * 2);
         p.Q = take((int64_t)dd->B * dd->Hk * p.m * kDeltaRows * p.dp * 2);
@@ -91,14 +90,12 @@ Plan make_plan(const luna_delta_desc *dd) {
         p.Sp = take(chunks * p.dvp * p.dp * 2);
         p.Rp = take((chunks + BH) * p.dvp * p.dp * 2);
         p.scales = take((chunks + BH) * (p.dvp / 16) * kDeltaScales * 4);
+    } else {
+        p.U = take(BH * dd->n * dd->dv * 4);
+        p.X = take(BH * dd->n * dd->dv * 4);
+        p.before = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
+        p.after = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
     }
-    const size_t end_tc = at;
-    at = 256;
-    p.U = take(BH * dd->n * dd->dv * 4);
-    p.X = take(BH * dd->n * dd->dv * 4);
-    p.before = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
-    p.after = take(BH * (p.m + 1) * dd->d * dd->dv * 4);
-    at = std::max(at, end_tc);
     if (dd->H != dd->Hk) {
         p.dq = take(BH * dd->n * dd->d * 4);
         p.dk = take(BH * dd->n * dd->d * 4);
@@ -178,8 +175,8 @@ luna_status luna_delta_fwd(const luna_delta_desc *dd, const void *log_decay, con
     a.o = O; a.ob = so.b; a.oh = so.h; a.ot = so.t;
     a.S0 = S0;
     a.S1 = S1;
-    if (!tc_widths(dd) || !rows16(a.q) || !rows16(a.k) || !rows16(a.v) || !rows16(O, so))
-        return cuda_status(launch_delta_rows(a, dd->io, false, s));
+    if (!on_tc(dd)) return cuda_status(launch_delta_rows(a, false, s));
+    a.vec = whole_vectors(dd) && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(O, so);
     tc_parts(a, p, static_cast<char *>(workspace), false);
     if (launch_delta_prepare(a, s) != cudaSuccess) return LUNA_ERR_CUDA;
     return cuda_status(launch_delta_chain(a, false, s));
@@ -231,24 +228,25 @@ luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, con
     a.dg = GateOut{dlog_decay, gg.b, gg.h, gg.t};
     a.db = GateOut{dbeta, gb.b, gb.h, gb.t};
 
-    const bool tc = tc_widths(dd) && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(a.go) && rows16(dV, gv) &&
-                    (shared || (rows16(dQ, gq) && rows16(dK, gk)));
+    const bool tc = on_tc(dd);
+    a.vec = whole_vectors(dd) && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(a.go) && rows16(dV, gv) &&
+            (shared || (rows16(dQ, gq) && rows16(dK, gk)));
     cudaError_t e = cudaSuccess;
     if (tc) {
         tc_parts(a, p, ws, true);
         e = launch_delta_prepare(a, s);
         if (e == cudaSuccess) e = launch_delta_chain(a, false, s);
     } else {
-        e = launch_delta_rows(a, dd->io, false, s);
+        e = launch_delta_rows(a, false, s);
     }
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
     DeltaArgs r = a;
     r.o = dV; r.ob = gv.b; r.oh = gv.h; r.ot = gv.t;
     r.dS0 = dS0;
-    e = tc ? launch_delta_chain(r, true, s) : launch_delta_rows(r, dd->io, true, s);
+    e = tc ? launch_delta_chain(r, true, s) : launch_delta_rows(r, true, s);
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
     const luna_dtype out = shared ? LUNA_F32 : dd->io;
-    e = tc ? launch_delta_grad_tc(a, out, s) : launch_delta_grad(a, dd->io, out, s);
+    e = tc ? launch_delta_grad_tc(a, out, s) : launch_delta_grad(a, s);
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
     if (!shared) return LUNA_OK;
     e = launch_decay_group_sum(part_q, B, H, H / Hk, n, d, dQ, gq.b, gq.h, gq.t, dd->io, s);

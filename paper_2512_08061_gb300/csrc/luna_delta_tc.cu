@@ -54,15 +54,37 @@ __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_gro
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Eight values of a row into shared memory, zeros behind `n` of them: by an asynchronous copy, or one by one where rows do
+// not start on 16-byte boundaries (or end inside one)
+__device__ __forceinline__ void load_piece(uint32_t dst, const __nv_bfloat16 *src, const void *any, int n, bool vec) {
+    if (vec) {
+        copy16(dst, n > 0 ? src : any, n > 0);
+        return;
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+    const unsigned short *u = reinterpret_cast<const unsigned short *>(src);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) w[i / 2] |= (uint32_t)u[i] << (i % 2 * 16);
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
 // a tile of `rows` rows (64 of them, DP columns) of a tensor of d columns; zeros behind both
 template <int DP>
-__device__ __forceinline__ void load_rows(uint32_t dst, const __nv_bfloat16 *src, int64_t st, int rows, int d, int tid, int threads) {
+__device__ __forceinline__ void load_rows(uint32_t dst, const __nv_bfloat16 *src, int64_t st, int rows, int d, bool vec, int tid, int threads) {
     for (int i = tid; i < C * DP / 8; i += threads) {
         const int r = i / (DP / 8), p = i % (DP / 8);
-        const bool in = r < rows && p * 8 < d;
-        copy16(tile_at(dst, C, r, p), in ? src + r * st + p * 8 : src, in);
+        load_piece(tile_at(dst, C, r, p), src + r * st + p * 8, src, r < rows ? d - p * 8 : 0, vec);
     }
 }
+// two neighbouring values of a row of which n are left
+__device__ __forceinline__ float2 load_pair(const __nv_bfloat16 *p, int n, bool vec) {
+    if (vec && n > 0) {
+        const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
+        return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+    }
+    return make_float2(n > 0 ? io_load(p) : 0.0f, n > 1 ? io_load(p + 1) : 0.0f);
+}
+
 // What this file's kernels leave for each other lies in global memory as its tile does in shared memory: one copy a tile.
 __device__ __forceinline__ void load_tile(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
@@ -248,8 +270,8 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
     if (rows <= 0) return;
     const int hk = h / (a.H / a.k.heads);
     const uint32_t sk = smem_u32(sm.k), sq = smem_u32(sm.q), sA = smem_u32(sm.A);
-    load_rows<DP>(sk, static_cast<const __nv_bfloat16 *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st, a.k.st, rows, a.d, tid, kPrepThreads);
-    load_rows<DP>(sq, static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st, a.q.st, rows, a.d, tid, kPrepThreads);
+    load_rows<DP>(sk, static_cast<const __nv_bfloat16 *>(a.k.p) + b * a.k.sb + hk * a.k.sh + t0 * a.k.st, a.k.st, rows, a.d, a.vec, tid, kPrepThreads);
+    load_rows<DP>(sq, static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st, a.q.st, rows, a.d, a.vec, tid, kPrepThreads);
     copies_end();
     if (warp == 0)
         delta_gate_sums(lane, [&](int t) { return t < rows ? gate_at<__nv_bfloat16>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
@@ -482,8 +504,7 @@ __device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, MODE
 #pragma unroll
     for (int i = tid; i < C * NG * 2; i += Sh::kWarps * 32) {
         const int r = i / (NG * 2), p = i % (NG * 2);
-        const bool in = r < rows && col0 + p * 8 < a.dv;
-        copy16(sx + r * Sh::kPitch + p * 16, in ? x + r * xv.st + p * 8 : static_cast<const __nv_bfloat16 *>(xv.p), in);
+        load_piece(sx + r * Sh::kPitch + p * 16, x + r * xv.st + p * 8, xv.p, r < rows ? a.dv - col0 - p * 8 : 0, a.vec);
     }
     copies_end();
 }
@@ -491,7 +512,7 @@ __device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, MODE
 // Rows first, first + 1, .. (n of them) of a warp's 16 columns, given column by column, to the output: transposed through
 // shared memory
 __device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first, int n, char *mem, __nv_bfloat16 *out, int64_t st, int rows,
-                                            int col, int dv, int lane) {
+                                            int col, int dv, bool vec, int lane) {
     const uint32_t base = smem_u32(mem);
 #pragma unroll
     for (int nt = 0; nt < 8; nt += 2) {
@@ -503,8 +524,14 @@ __device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first,
     __syncwarp();
     for (int i = 0; i < n / 16; ++i) {
         const int r = first + i * 16 + lane / 2, half = lane % 2;
-        if (r < rows && col + half * 8 < dv)
-            *reinterpret_cast<uint4 *>(out + r * st + col + half * 8) = *reinterpret_cast<const uint4 *>(mem + r * 48 + half * 16);
+        if (r < rows && col + half * 8 < dv) {
+            const __nv_bfloat16 *from = reinterpret_cast<const __nv_bfloat16 *>(mem + r * 48 + half * 16);
+            __nv_bfloat16 *to = out + r * st + col + half * 8;
+            if (vec)
+                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+            else
+                for (int e = 0; e < min(8, dv - col - half * 8); ++e) to[e] = from[e];
+        }
     }
     __syncwarp();
 }
@@ -801,7 +828,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[nt][e] = fmaf(back_s * (e & 1 ? past.y : past.x), y[nt][e], back * x[nt][e]);
                     }
-                    chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+                    chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, a.vec, lane);
                 }
             }
 #pragma unroll
@@ -918,7 +945,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) split_left(x[2 * kt], x[2 * kt + 1], ws.by, fh[kt], fl[kt]);
             update(fh, fl, ws.back, sk, false);
-            chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, lane);
+            chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, a.vec, lane);
         }
     }
     if (REV && mine && chunks > 0) {  // R before the first chunk
@@ -947,7 +974,11 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     if (MODE != kKeep)  // rows behind the end, eight columns at a time
         for (int64_t i = tid; i < (int64_t)(a.n - len) * NG * 2; i += Sh::kWarps * 32) {
             const int c = col0 + (int)(i % (NG * 2)) * 8;
-            if (c < a.dv) *reinterpret_cast<uint4 *>(o + (len + i / (NG * 2)) * a.ot + c) = make_uint4(0, 0, 0, 0);
+            __nv_bfloat16 *to = o + (len + i / (NG * 2)) * a.ot + c;
+            if (a.vec && c < a.dv)
+                *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+            else
+                for (int e = 0; e < min(8, a.dv - c); ++e) io_store(to + e, 0.0f);
         }
 }
 
@@ -1062,9 +1093,18 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         const int i = tid % C;
         const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
         if (i < rows)
-            for (int c8 = tid / C; c8 < a.dv / 8; c8 += kParts) {
-                const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
-                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            for (int c8 = tid / C; c8 * 8 < a.dv; c8 += kParts) {
+                uint32_t w[4];
+                if (a.vec) {
+                    const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
+                    w[0] = w4.x; w[1] = w4.y; w[2] = w4.z; w[3] = w4.w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = load_pair(v + c8 * 8 + 2 * e, a.dv - c8 * 8 - 2 * e, false);
+                        w[e] = pack_bf16(f.x, f.y);
+                    }
+                }
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -1201,11 +1241,16 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                 OUT *to = out + r * st + c0 + q2;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    if (c0 + nt * 8 >= a.d) continue;
-                    if (sizeof(OUT) == 2)
+                    const int left = a.d - (c0 + nt * 8 + q2);  // (an odd width ends inside a pair)
+                    if (left <= 0) continue;
+                    if (!a.vec) {
+                        io_store(to + nt * 8, acc[mt][nt][2 * i]);
+                        if (left > 1) io_store(to + nt * 8 + 1, acc[mt][nt][2 * i + 1]);
+                    } else if (sizeof(OUT) == 2) {
                         *reinterpret_cast<uint32_t *>(to + nt * 8) = pack_bf16(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
-                    else
+                    } else {
                         *reinterpret_cast<float2 *>(to + nt * 8) = make_float2(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
+                    }
                 }
             }
     };
@@ -1335,8 +1380,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                 const int r = r0 + mt * 16 + lane / 4 + i * 8;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint32_t u = r < rows && c0 + nt * 8 < a.d ? *reinterpret_cast<const uint32_t *>(q + r * a.q.st + nt * 8) : 0u;
-                    dot[i] = fmaf(low(u), z[mt][nt][2 * i], fmaf(high(u), z[mt][nt][2 * i + 1], dot[i]));
+                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, a.vec);
+                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
                 }
             }
             row_sums(dot[0], dot[1], mt, 0);

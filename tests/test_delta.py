@@ -161,6 +161,11 @@ CASES = [  # B, H, Hk, n, d, dv, io, layout, lengths, state
     (1, 2, 1, 200, 33, 50, BF, "tokens", [199], True),     # widths that no 16-byte access covers
     (1, 2, 2, 520, 8, 120, BF, "wide", None, False),
     (4, 2, 2, 66, 64, 128, BF, "heads", [63, 64, 65, 66], True),
+    (2, 4, 2, 150, 61, 61, BF, "wide", [150, 77], True),
+    (1, 2, 2, 90, 5, 128, BF, "heads", None, True),
+    (1, 2, 1, 200, 127, 7, BF, "tokens", None, False),
+    (3, 5, 5, 70, 72, 88, BF, "tokens", [70, 3, 64], True),
+    (2, 2, 2, 400, 96, 17, F, "tokens", [400, 190], True),
 ]
 
 
