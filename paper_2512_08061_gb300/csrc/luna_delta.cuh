@@ -29,7 +29,7 @@ namespace luna {
 
 constexpr int kDeltaRows = 64;      // rows of a chunk
 // tensor-core form: fp32 values of a chunk's factors, and of the scales of 16 columns of it
-constexpr int kDeltaFactors = 4 * kDeltaRows + 8, kDeltaScales = 8;
+constexpr int kDeltaFactors = 4 * kDeltaRows + 12, kDeltaScales = 8;
 
 struct GateView {  // a (B, H, n) tensor
     const void *p;
@@ -154,7 +154,8 @@ cudaError_t launch_delta_rows(const DeltaArgs &a, bool reverse, cudaStream_t s);
 cudaError_t launch_delta_grad(const DeltaArgs &a, cudaStream_t s);
 // bf16, on tensor cores
 cudaError_t launch_delta_prepare(const DeltaArgs &a, cudaStream_t s);
-cudaError_t launch_delta_chain(const DeltaArgs &a, bool reverse, cudaStream_t s);
+cudaError_t launch_delta_chain64(const DeltaArgs &a, bool reverse, cudaStream_t s);   // d <= 64
+cudaError_t launch_delta_chain128(const DeltaArgs &a, bool reverse, cudaStream_t s);
 cudaError_t launch_delta_grad_tc(const DeltaArgs &a, luna_dtype out, cudaStream_t s);
 cudaError_t launch_delta_step(const DeltaStep &a, luna_dtype io, cudaStream_t s);
 

@@ -141,6 +141,10 @@ void tc_parts(DeltaArgs &a, const Plan &p, char *ws, bool backward) {
     a.scales = reinterpret_cast<float *>(ws + p.scales);
 }
 
+cudaError_t run_chain(const DeltaArgs &a, bool reverse, cudaStream_t s) {
+    return a.d <= 64 ? launch_delta_chain64(a, reverse, s) : launch_delta_chain128(a, reverse, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -179,7 +183,7 @@ luna_status luna_delta_fwd(const luna_delta_desc *dd, const void *log_decay, con
     a.vec = whole_vectors(dd) && rows16(a.q) && rows16(a.k) && rows16(a.v) && rows16(O, so);
     tc_parts(a, p, static_cast<char *>(workspace), false);
     if (launch_delta_prepare(a, s) != cudaSuccess) return LUNA_ERR_CUDA;
-    return cuda_status(launch_delta_chain(a, false, s));
+    return cuda_status(run_chain(a, false, s));
 }
 
 luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, const void *beta, const void *Q, const void *K,
@@ -235,7 +239,7 @@ luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, con
     if (tc) {
         tc_parts(a, p, ws, true);
         e = launch_delta_prepare(a, s);
-        if (e == cudaSuccess) e = launch_delta_chain(a, false, s);
+        if (e == cudaSuccess) e = run_chain(a, false, s);
     } else {
         e = launch_delta_rows(a, false, s);
     }
@@ -243,7 +247,7 @@ luna_status luna_delta_bwd(const luna_delta_desc *dd, const void *log_decay, con
     DeltaArgs r = a;
     r.o = dV; r.ob = gv.b; r.oh = gv.h; r.ot = gv.t;
     r.dS0 = dS0;
-    e = tc ? launch_delta_chain(r, true, s) : launch_delta_rows(r, true, s);
+    e = tc ? run_chain(r, true, s) : launch_delta_rows(r, true, s);
     if (e != cudaSuccess) return LUNA_ERR_CUDA;
     const luna_dtype out = shared ? LUNA_F32 : dd->io;
     e = tc ? launch_delta_grad_tc(a, out, s) : launch_delta_grad(a, s);

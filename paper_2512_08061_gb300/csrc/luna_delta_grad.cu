@@ -1,0 +1,521 @@
+// The gated delta rule on tensor cores: gradients by chunk.
+#include "luna_delta_tc.cuh"
+
+namespace luna {
+namespace {
+
+using namespace delta;
+
+// ---------------------------------------------------------------------------
+// Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X, dO and states.  A block of eight warps a chunk:
+// two groups of 32 rows by four quarters of the columns.  102 KB of shared memory, so that two blocks are on an SM and
+// the one's products cover the other's loads: R, then S, then Q lie in the same place, P and W in that of U.
+
+constexpr int kGradThreads = 256, kParts = 4;
+
+template <int DP, int DVT>
+struct GradShared {
+    alignas(128) char k[DP / 64][kTileB], go[DVT * 128], x[DVT * 128], u[DVT * 128 > 2 * kTileB ? DVT * 128 : 2 * kTileB];
+    alignas(128) char s[DVT * DP * 2 > DP / 64 * kTileB ? DVT * DP * 2 : DP / 64 * kTileB];
+    uint64_t bar[4];
+    float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales], behind[DVT / 16][2];  // (behind: of R)
+    __half2 steps[8][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
+    float all[8], total[kGradThreads / 32];
+    float sums[6][kParts][C];  // of a row's quarters: q . dQ, k . Z without the rows' part, k . (dK), W . K K^T, x . v, b k . Z
+    float most[2][kGradThreads / 32], read[C], wrote[C];
+};
+
+template <int DP, int DVT, typename OUT, bool VEC>
+__global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) {
+    using Sh = GradShared<DP, DVT>;
+    using Acc = float[2][DP / 32][4];
+    extern __shared__ __align__(128) char raw[];
+    Sh &sm = *reinterpret_cast<Sh *>(raw);
+    constexpr int NT = DP / 32;  // n-tiles of a warp's quarter of the columns of dQ, dK
+    const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, r0 = warp % 2 * 32, quarter = warp / 2, q2 = lane % 4 * 2;
+    const int of_half = 2 + quarter / 2 * 3;  // the products with S and R of the warp's half of the columns
+    const int64_t at = blockIdx.x, bh = at / a.m;
+    const int chunk = (int)(at % a.m), b = (int)(bh / a.H), h = (int)(bh % a.H), t0 = chunk * C;
+    const int rows = max(0, min(C, head_length(a.lengths, b, a.n) - t0)), out_rows = min(C, a.n - t0);
+    const int hk = h / (a.H / a.k.heads);
+    OUT *dq = static_cast<OUT *>(a.dq) + b * a.dqb + h * a.dqh + t0 * a.dqt;
+    OUT *dk = static_cast<OUT *>(a.dk) + b * a.dkb + h * a.dkh + t0 * a.dkt;
+    __nv_bfloat16 *dg = static_cast<__nv_bfloat16 *>(a.dg.p) + b * a.dg.sb + h * a.dg.sh + t0 * a.dg.st;
+    __nv_bfloat16 *db = static_cast<__nv_bfloat16 *>(a.db.p) + b * a.db.sb + h * a.db.sh + t0 * a.db.st;
+    for (int i = tid; i < (out_rows - rows) * a.d; i += kGradThreads) {
+        const int t = rows + i / a.d, c = i % a.d;
+        io_store(dq + t * a.dqt + c, 0.0f);
+        io_store(dk + t * a.dkt + c, 0.0f);
+    }
+    if (tid >= rows && tid < out_rows) {
+        io_store(dg + tid * a.dg.st, 0.0f);
+        io_store(db + tid * a.db.st, 0.0f);
+    }
+    if (rows == 0) return;
+
+    const uint32_t sk = smem_u32(sm.k), sgo = smem_u32(sm.go), su = smem_u32(sm.u), sx = smem_u32(sm.x), ss = smem_u32(sm.s);
+    const uint32_t sP = su, sW = su + kTileB;
+    const int dvp = a.dvp, groups = dvp / 16;
+    const int64_t kat = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
+    const int64_t slot = bh * (a.m + 1) + chunk;
+    const uint32_t of_rows = dvp * C * 2, of_state = dvp * DP * 2;
+    if (tid < 4) mbar_init(&sm.bar[tid], 1);
+    fence_mbar_init();
+    __syncthreads();
+    auto load_state = [&](const void *src, uint32_t bytes, int which) {  // (one thread)
+        mbar_arrive_expect_tx(&sm.bar[which], bytes);
+        load_tile(sm.s, src, bytes, &sm.bar[which]);
+    };
+    if (tid == 0) {
+        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 3 * of_rows);
+        load_tile(sm.u, a.Up + at * dvp * C, of_rows, &sm.bar[0]);
+        load_tile(sm.x, a.Xp + at * dvp * C, of_rows, &sm.bar[0]);
+        load_tile(sm.go, a.Gp + at * dvp * C, of_rows, &sm.bar[0]);
+        load_tile(sm.k, a.Kp + kat * C * DP, sizeof(sm.k), &sm.bar[0]);
+        load_state(a.Rp + (slot + 1) * dvp * DP, of_state, 1);
+        // what comes later, as far as L2
+        auto ask = [](const void *p, uint32_t bytes) {
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+        };
+        ask(a.Sp + at * dvp * DP, of_state);
+        ask(a.Rp + slot * dvp * DP, of_state);
+        ask(a.Qp + kat * C * DP, sizeof(sm.k));
+    }
+    const float *rowf = a.rows + at * kRowsF;
+    const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
+    if (warp == 0)
+        delta_gate_sums(lane, [&](int t) { return t < rows ? gate_at<__nv_bfloat16>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
+                        sm.past, sm.left);
+    else if (warp < 3)
+        sm.b[tid - 32] = rowf[2 * C + tid - 32];
+    for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[slot * groups * kDeltaScales + i];
+    if (tid < groups * 2) sm.behind[tid / 2][tid % 2] = a.scales[((slot + 1) * groups + tid / 2) * kDeltaScales + 2 + tid % 2];
+    __syncthreads();
+    // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
+    // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U; of either half of the
+    // other columns dO S, X S, U R.
+    if (tid < 8) {
+        const int side = tid < 2 ? 0 : (tid - 2) / 3, which = tid < 2 ? tid : (tid - 2) % 3;
+        auto scale = [&](int kt) {
+            const float *f = sm.scales[kt];
+            return tid < 2 ? f[6 - which] * f[4] : which < 2 ? f[6 - which] * f[side] : f[4] * sm.behind[kt][side];
+        };
+        float most = 0.0f;
+        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, scale(kt));
+        sm.all[tid] = most;
+        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = __float2half2_rn(most > 0.0f ? scale(kt) / most : 0.0f);
+    }
+    // x . v: a thread a row and a quarter of the columns, while the tiles come
+    float xv = 0.0f;
+    bool here = mbar_wait_long(&sm.bar[0], 0);
+    __syncthreads();
+    {
+        const int i = tid % C;
+        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
+        if (i < rows)
+            for (int c8 = tid / C; c8 * 8 < a.dv; c8 += kParts) {
+                uint32_t w[4];
+                if (VEC) {
+                    const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
+                    w[0] = w4.x; w[1] = w4.y; w[2] = w4.z; w[3] = w4.w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = load_pair(v + c8 * 8 + 2 * e, a.dv - c8 * 8 - 2 * e, false);
+                        w[e] = pack_bf16(f.x, f.y);
+                    }
+                }
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    unsigned short u;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
+                    sum = fmaf(e & 1 ? high(w[e / 2]) : low(w[e / 2]), __half2float(__ushort_as_half(u)), sum);
+                }
+                xv = fmaf(sm.scales[c8 / 2][5], sum, xv);
+            }
+        sm.sums[4][tid / C][i] = xv;
+    }
+
+    // 16 rows (m0) of a left operand from a plane, for the product's 16 columns kt
+    auto left_plane = [&](Frag &f, uint32_t tile, int m0, int kt, int product) {
+        left_k(f, tile, dvp, kt * 16, m0, lane);
+        const __half2 by = sm.steps[product][kt];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __half2 x;
+            memcpy(&x, &f[i], 4);
+            x = __hmul2(x, by);
+            memcpy(&f[i], &x, 4);
+        }
+    };
+    // sums over the four lanes of a row, for this quarter of the columns: rows r0 + 16 mt + lane / 4 and 8 more
+    auto row_sums = [&](float x, float y, int mt, int which) {
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        y += __shfl_xor_sync(0xffffffffu, y, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        y += __shfl_xor_sync(0xffffffffu, y, 2);
+        if (lane % 4 == 0) {
+            sm.sums[which][quarter][r0 + mt * 16 + lane / 4] = x;
+            sm.sums[which][quarter][r0 + mt * 16 + lane / 4 + 8] = y;
+        }
+    };
+    const int c0 = quarter * (DP / 4), n0 = quarter * 16;  // first column of the warp's, of P and W
+    // acc += F M over the columns of the state: F a plane, M the tile of the state
+    auto over_columns = [&](Acc &acc, uint32_t plane, int product) {
+#pragma unroll 2
+        for (int kt = 0; kt < groups; ++kt) {
+            Frag fl[2];
+            left_plane(fl[0], plane, r0, kt, product);
+            left_plane(fl[1], plane, r0 + 16, kt, product);
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                right_k(f, ss, dvp, kt * 16, c0 + np * 16, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    mma(acc[mt][2 * np], fl[mt], f[0], f[1]);
+                    mma(acc[mt][2 * np + 1], fl[mt], f[2], f[3]);
+                }
+            }
+        }
+    };
+    // acc += F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q
+    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, uint32_t sign) {
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            if (trans ? kt * 16 < r0 : kt * 16 > r0 + 16) continue;
+            Frag fl[2];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+                if (trans)
+                    left_k(fl[mt], from, C, kt * 16, r0 + mt * 16, lane);
+                else
+                    left_m(fl[mt], from, C, r0 + mt * 16, kt * 16, lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fl[mt][i] ^= sign;
+            }
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                right_k(f, tile, C, kt * 16, c0 + np * 16, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    mma(acc[mt][2 * np], fl[mt], f[0], f[1]);
+                    mma(acc[mt][2 * np + 1], fl[mt], f[2], f[3]);
+                }
+            }
+        }
+    };
+    // acc *= by row_factor (of every row)
+    auto times_rows = [&](Acc &acc, const float *row_factor, const float *more, float by) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            const int ra = r0 + mt * 16 + lane / 4;
+            float fa = by * row_factor[ra], fb = by * row_factor[ra + 8];
+            if (more) {
+                fa *= more[ra];
+                fb *= more[ra + 8];
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= e & 2 ? fb : fa;
+        }
+    };
+    auto times = [&](Acc &acc, float by) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= by;
+    };
+    // sums of the rows times those of K (whose left operands lie as the accumulators do)
+    auto dot_k = [&](const Acc &acc, int which) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float x = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+                Frag f;
+                left_m(f, sk, C, r0 + mt * 16, c0 + np * 16, lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 k2 = half_pair(f[i]);
+                    const float *c = acc[mt][2 * np + i / 2] + (i & 1) * 2;
+                    float &to = i & 1 ? y : x;
+                    to = fmaf(k2.x, c[0], fmaf(k2.y, c[1], to));
+                }
+            }
+            row_sums(back_k * x, back_k * y, mt, which);
+        }
+    };
+    auto store_rows = [&](const Acc &acc, OUT *out, int64_t st) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+                if (r >= rows) continue;
+                OUT *to = out + r * st + c0 + q2;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int left = a.d - (c0 + nt * 8 + q2);  // (an odd width ends inside a pair)
+                    if (left <= 0) continue;
+                    if (!VEC) {
+                        io_store(to + nt * 8, acc[mt][nt][2 * i]);
+                        if (left > 1) io_store(to + nt * 8 + 1, acc[mt][nt][2 * i + 1]);
+                    } else if (sizeof(OUT) == 2) {
+                        *reinterpret_cast<uint32_t *>(to + nt * 8) = pack_bf16(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
+                    } else {
+                        *reinterpret_cast<float2 *>(to + nt * 8) = make_float2(acc[mt][nt][2 * i], acc[mt][nt][2 * i + 1]);
+                    }
+                }
+            }
+    };
+    auto clear = [&](Acc &acc) {
+        zero(acc[0]);
+        zero(acc[1]);
+    };
+
+    // P_ij = scale c(i, j) dO_i . u_j,  W_ij = b_i c(i, j) x_i . u_j, 16 columns a warp; W . K K^T for db
+    float p[2][2][4], w[2][2][4];
+    float mp = 0.0f, mw = 0.0f;
+    {
+        float kk[2][2][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            zero(p[mt]);
+            zero(w[mt]);
+            zero(kk[mt]);
+        }
+        if (n0 <= r0 + 16) {
+#pragma unroll 2
+            for (int kt = 0; kt < groups; ++kt) {
+                Frag f;
+                right_k(f, su, dvp, kt * 16, n0, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    Frag fg, fx;
+                    left_plane(fg, sgo, r0 + mt * 16, kt, 0);
+                    left_plane(fx, sx, r0 + mt * 16, kt, 1);
+                    mma(p[mt][0], fg, f[0], f[1]);
+                    mma(p[mt][1], fg, f[2], f[3]);
+                    mma(w[mt][0], fx, f[0], f[1]);
+                    mma(w[mt][1], fx, f[2], f[3]);
+                }
+            }
+#pragma unroll
+            for (int k0 = 0; k0 < DP; k0 += 16) {
+                Frag f;
+                right_n(f, sk, C, n0, k0, lane);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    Frag fk;
+                    left_m(fk, sk, C, r0 + mt * 16, k0, lane);
+                    mma(kk[mt][0], fk, f[0], f[1]);
+                    mma(kk[mt][1], fk, f[2], f[3]);
+                }
+            }
+        }
+        const float by_p = a.scale * sm.all[0], by_w = sm.all[1];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = r0 + mt * 16 + lane / 4 + (e >> 1) * 8, j = n0 + nt * 8 + q2 + (e & 1);
+                    const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
+                    float &pp = p[mt][nt][e], &ww = w[mt][nt][e];
+                    pp = j <= i ? by_p * c * pp : 0.0f;
+                    ww = j < i ? by_w * c * ww : 0.0f;
+                    if (j < i) dot[e >> 1] = fmaf(ww, kk[mt][nt][e], dot[e >> 1]);
+                    ww *= sm.b[i];
+                    mp = fmaxf(mp, fabsf(pp));
+                    mw = fmaxf(mw, fabsf(ww));
+                }
+            row_sums(dot[0], dot[1], mt, 3);
+        }
+        mp = warp_max(mp);
+        mw = warp_max(mw);
+        if (lane == 0) {
+            sm.most[0][warp] = mp;
+            sm.most[1][warp] = mw;
+        }
+    }
+    // what dK takes from R
+    Acc acc, z;
+    clear(acc);
+    here = mbar_wait_long(&sm.bar[1], 0) && here;
+    if (here) over_columns(acc, su, of_half + 2);
+    if (__syncthreads_or(!here)) {  // a copy that did not arrive within a second: give up
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            for (int i = 0; i < 2; ++i) mbar_wait(&sm.bar[i], 0, kDrainNs);
+        }
+        return;
+    }
+    if (tid == 0) load_state(a.Sp + at * dvp * DP, of_state, 2);
+    mp = mw = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kGradThreads / 32; ++i) {
+        mp = fmaxf(mp, sm.most[0][i]);
+        mw = fmaxf(mw, sm.most[1][i]);
+    }
+    // P Q and W K are scaled down alike, so that they add up in dK
+    const float by = fmaxf(fmaxf(scale_of(mp).back * back_q, scale_of(mw).back * back_k), 0x1p-100f), inv = inverse2(by);
+    const float to_p = back_q * inv, to_w = back_k * inv, by_pk = by * back_k * inverse2(back_q);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const uint32_t to = tile_at(0, C, r0 + mt * 16 + lane / 4 + e * 4, quarter * 2 + nt) + q2 * 2;
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(to_p * p[mt][nt][e], to_p * p[mt][nt][e + 1])) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(to_w * w[mt][nt][e], to_w * w[mt][nt][e + 1])) : "memory");
+            }
+    times_rows(acc, sm.left, nullptr, sm.all[of_half + 2] * inv);
+    __syncthreads();
+    over_rows(acc, sW, true, sk, 0x80008000u);
+
+    // dQ and Z from S
+    here = mbar_wait_long(&sm.bar[2], 0);
+    clear(z);
+    if (here) over_columns(z, sgo, of_half);
+    times_rows(z, sm.past, nullptr, a.scale * sm.all[of_half] * inverse2(by_pk));
+    over_rows(z, sP, false, sk, 0);
+    times(z, by_pk);
+    store_rows(z, dq, a.dqt);
+    {  // q . dQ, with Q as it came
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, VEC);
+                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
+                }
+            }
+            row_sums(dot[0], dot[1], mt, 0);
+        }
+    }
+    {  // <S, R> before the chunk: of every 16 columns the diagonal of S^T R, R as it lies in memory (in both the summed
+       // values lie in the same, permuted order: a lane's 16 bytes of a row are those of two products)
+        float sum = 0.0f;
+        if (here && warp < groups) {
+            const char *r = reinterpret_cast<const char *>(a.Rp + slot * dvp * DP);
+            const int ra = warp * 16 + lane / 4;
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                float c[2][4];
+                zero(c);
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) {
+                    const int piece = (side * (DP / 64) + i) * 4 + lane % 4;
+                    const uint32_t at0 = tile_at(0, dvp, ra, piece), at1 = tile_at(0, dvp, ra + 8, piece);
+                    const uint4 s0 = *reinterpret_cast<const uint4 *>(sm.s + at0), s1 = *reinterpret_cast<const uint4 *>(sm.s + at1);
+                    const uint4 r0_ = *reinterpret_cast<const uint4 *>(r + at0), r1 = *reinterpret_cast<const uint4 *>(r + at1);
+                    const Frag f = {s0.x, s1.x, s0.y, s1.y}, g = {s0.z, s1.z, s0.w, s1.w};
+                    mma(c[0], f, r0_.x, r0_.y);
+                    mma(c[0], g, r0_.z, r0_.w);
+                    mma(c[1], f, r1.x, r1.y);
+                    mma(c[1], g, r1.z, r1.w);
+                }
+                const float *scale = sm.scales[warp];
+                float diag = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (lane / 4 == q2 + e) diag += c[0][e] + c[1][2 + e];
+                sum = fmaf(scale[side] * scale[2 + side], diag, sum);
+            }
+        }
+        sum = sum + __shfl_xor_sync(0xffffffffu, sum, 16);
+#pragma unroll
+        for (int w = 8; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        if (lane == 0) sm.total[warp] = sum;
+    }
+    clear(z);
+    if (here) over_columns(z, sx, of_half + 1);
+    if (__syncthreads_or(!here)) {
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            mbar_wait(&sm.bar[2], 0, kDrainNs);
+        }
+        return;
+    }
+    if (tid == 0) load_state(a.Qp + kat * C * DP, sizeof(sm.k), 3);
+    times_rows(z, sm.past, nullptr, sm.all[of_half + 1]);
+    dot_k(z, 1);
+    times_rows(z, sm.b, nullptr, inv);
+    over_rows(z, sW, false, sk, 0);
+    times(z, by);
+    dot_k(z, 5);
+
+    // dK
+    here = mbar_wait_long(&sm.bar[3], 0);
+    if (here) over_rows(acc, sP, true, ss, 0);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[mt][nt][e] = fmaf(by, acc[mt][nt][e], -z[mt][nt][e]);
+    dot_k(acc, 2);
+    store_rows(acc, dk, a.dkt);
+    if (__syncthreads_or(!here)) {
+        if (tid == 0) {
+            atomicOr(a.status, 1);
+            mbar_wait(&sm.bar[3], 0, kDrainNs);
+        }
+        return;
+    }
+    if (tid < rows) {
+        auto sum = [&](int which) {
+            return (sm.sums[which][0][tid] + sm.sums[which][1][tid]) + (sm.sums[which][2][tid] + sm.sums[which][3][tid]);
+        };
+        const float bz = sum(5);
+        io_store(db + tid * a.db.st, sum(4) - sum(1) - back_k * back_k * sum(3));
+        sm.read[tid] = sum(0) - bz;
+        sm.wrote[tid] = sum(2) + bz;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        float base = 0.0f;
+        for (int w = 0; w < kGradThreads / 32; ++w) base += sm.total[w];
+        delta_gate_grads(base, sm.read, sm.wrote, rows, lane, [&](int t, float x) {
+            io_store(dg + t * a.dg.st, expf(gate_at<__nv_bfloat16>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
+        });
+    }
+}
+
+template <int DP, int DVT, typename OUT, bool VEC>
+cudaError_t grad_launch(const DeltaArgs &a, cudaStream_t s) {
+    using Sh = GradShared<DP, DVT>;
+    cudaError_t e = cudaFuncSetAttribute(k_delta_grad_tc<DP, DVT, OUT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
+    if (e != cudaSuccess) return e;
+    LUNA_LAUNCH("delta_grad_tc", (k_delta_grad_tc<DP, DVT, OUT, VEC>), (unsigned)((int64_t)a.B * a.H * a.m), kGradThreads, sizeof(Sh), s, a);
+    return cudaGetLastError();
+}
+
+template <typename OUT, bool VEC>
+cudaError_t grad(const DeltaArgs &a, cudaStream_t s) {
+    if (a.d <= 64) return a.dv <= 64 ? grad_launch<64, 64, OUT, VEC>(a, s) : grad_launch<64, 128, OUT, VEC>(a, s);
+    return a.dv <= 64 ? grad_launch<128, 64, OUT, VEC>(a, s) : grad_launch<128, 128, OUT, VEC>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_grad_tc(const DeltaArgs &a, luna_dtype out, cudaStream_t s) {
+    if (out == LUNA_F32) return a.vec ? grad<float, true>(a, s) : grad<float, false>(a, s);
+    return a.vec ? grad<__nv_bfloat16, true>(a, s) : grad<__nv_bfloat16, false>(a, s);
+}
+
+}  // namespace luna
