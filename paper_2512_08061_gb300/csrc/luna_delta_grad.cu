@@ -389,24 +389,6 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     times_rows(z, sm.past, nullptr, a.scale * sm.all[of_half] * inverse2(by_pk));
     over_rows(z, sP, false, sk, 0);
     times(z, by_pk);
-    store_rows(z, dq, a.dqt);
-    {  // q . dQ, with Q as it came
-        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            float dot[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = r0 + mt * 16 + lane / 4 + i * 8;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, VEC);
-                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
-                }
-            }
-            row_sums(dot[0], dot[1], mt, 0);
-        }
-    }
     {  // <S, R> before the chunk: of every 16 columns the diagonal of S^T R, R as it lies in memory (in both the summed
        // values lie in the same, permuted order: a lane's 16 bytes of a row are those of two products)
         float sum = 0.0f;
@@ -422,7 +404,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                     const int piece = (side * (DP / 64) + i) * 4 + lane % 4;
                     const uint32_t at0 = tile_at(0, dvp, ra, piece), at1 = tile_at(0, dvp, ra + 8, piece);
                     const uint4 s0 = *reinterpret_cast<const uint4 *>(sm.s + at0), s1 = *reinterpret_cast<const uint4 *>(sm.s + at1);
-                    const uint4 r0_ = *reinterpret_cast<const uint4 *>(r + at0), r1 = *reinterpret_cast<const uint4 *>(r + at1);
+                    const uint4 r0_ = __ldg(reinterpret_cast<const uint4 *>(r + at0)), r1 = __ldg(reinterpret_cast<const uint4 *>(r + at1));
                     const Frag f = {s0.x, s1.x, s0.y, s1.y}, g = {s0.z, s1.z, s0.w, s1.w};
                     mma(c[0], f, r0_.x, r0_.y);
                     mma(c[0], g, r0_.z, r0_.w);
@@ -441,6 +423,24 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
 #pragma unroll
         for (int w = 8; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         if (lane == 0) sm.total[warp] = sum;
+    }
+    store_rows(z, dq, a.dqt);
+    {  // q . dQ, with Q as it came
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, VEC);
+                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
+                }
+            }
+            row_sums(dot[0], dot[1], mt, 0);
+        }
     }
     clear(z);
     if (here) over_columns(z, sx, of_half + 1);

@@ -775,9 +775,10 @@ class Delta(_Checked):
 
     def forward(self, Q, K, V, log_decay, beta, lengths=None, S0=None, want_state=False, O=None, S1=None, stream=None):
         """O, or (O, S1) with want_state."""
+        given = O  # (a new output lies as V does: not to be looked at again)
         if O is None:
             O = _new(stream, torch.empty_like)(V)
-        if not self._looked_at("forward", Q, K, V, log_decay, beta, lengths, S0, O, S1):
+        if not self._looked_at("forward", Q, K, V, log_decay, beta, lengths, S0, given, S1):
             for field, name, t in (("q", "Q", Q), ("k", "K", K), ("v", "V", V), ("g", "log_decay", log_decay),
                                    ("beta", "beta", beta), ("o", "O", O)):
                 self._view("forward", field, name, t)
@@ -793,13 +794,15 @@ class Delta(_Checked):
 
     def backward(self, Q, K, V, dO, log_decay, beta, lengths=None, S0=None, dS1=None, out=None, stream=None):
         """dQ, dK, dV, dlog_decay, dbeta, and dS0 where S0 is given (or `out` holds it), of forward on the same inputs."""
-        if out is None:
+        new = out is None  # (new gradients lie as what they are gradients of)
+        if new:
             out = {"d" + k: _new(stream, torch.empty_like)(t)
                    for k, t in (("Q", Q), ("K", K), ("V", V), ("log_decay", log_decay), ("beta", beta))}
             if S0 is not None:
                 out["dS0"] = _new(stream)(self.state_shape, dtype=torch.float32, device=self.device)
         dQ, dK, dV, dg, db, dS0 = (out.get("d" + k) for k in ("Q", "K", "V", "log_decay", "beta", "S0"))
-        if not self._looked_at("backward", Q, K, V, dO, log_decay, beta, lengths, S0, dS1, dQ, dK, dV, dg, db, dS0):
+        given = (None,) * 6 if new else (dQ, dK, dV, dg, db, dS0)
+        if not self._looked_at("backward", Q, K, V, dO, log_decay, beta, lengths, S0, dS1, *given):
             for field, name, t in (("q", "Q", Q), ("k", "K", K), ("v", "V", V), ("g", "log_decay", log_decay),
                                    ("beta", "beta", beta), ("go", "dO", dO), ("gq", "dQ", dQ), ("gk", "dK", dK),
                                    ("gv", "dV", dV), ("gg", "dlog_decay", dg), ("gbeta", "dbeta", db)):
@@ -815,9 +818,10 @@ class Delta(_Checked):
 
     def step(self, q, k, v, log_decay, beta, S, slots=None, o=None, stream=None):
         """One token: q, k (B, Hk, d), v (B, H, dv), log_decay, beta (B, H); S (nslots, H, d, dv) is advanced in place."""
+        given = o  # (a new output is contiguous)
         if o is None:
             o = _new(stream)(self.state_shape[:2] + self.state_shape[3:], dtype=self.io, device=self.device)
-        if not self._looked_at("step", q, k, v, log_decay, beta, S, slots, o):
+        if not self._looked_at("step", q, k, v, log_decay, beta, S, slots, given):
             for field, name, t in (("q", "q", q), ("k", "k", k), ("v", "v", v), ("g", "log_decay", log_decay),
                                    ("beta", "beta", beta), ("o", "o", o)):
                 self._view("step", field, name, t)
@@ -850,14 +854,17 @@ class Beam(_Checked):
         """The best continuations of every sequence from logits (B * beams, vocab), running log-probabilities scores
         (B, beams) fp32 and, with an end token, done (B, beams) bool: {"scores", "tokens", "parents"} and with an end
         token "done", each (B, beams), best first.  `out` may hold scores and done themselves."""
+        given = (None,) * 4  # (new outputs are as they have to be)
         if out is None:
-            new, at = _new(stream), dict(device=self.device)
-            out = {"scores": new(self.shape, dtype=torch.float32, **at), "tokens": new(self.shape, dtype=torch.int32, **at),
-                   "parents": new(self.shape, dtype=torch.int32, **at)}
+            new, at, shape = _new(stream), self.device, self.shape
+            out = {"scores": new(shape, dtype=torch.float32, device=at), "tokens": new(shape, dtype=torch.int32, device=at),
+                   "parents": new(shape, dtype=torch.int32, device=at)}
             if self.bd.end >= 0:
-                out["done"] = new(self.shape, dtype=torch.bool, **at)
-        to = [out.get(k) for k in ("scores", "tokens", "parents", "done")]
-        if not self._looked_at("select", logits, scores, done, *to):
+                out["done"] = new(shape, dtype=torch.bool, device=at)
+            to = [out["scores"], out["tokens"], out["parents"], out.get("done")]
+        else:
+            given = to = [out.get(k) for k in ("scores", "tokens", "parents", "done")]
+        if not self._looked_at("select", logits, scores, done, *given):
             _set_rows(self._desc["forward"], "ld", "logits", logits, (self.shape[0] * self.shape[1], self.bd.V), self.io,
                       self.device)
             if any(t is None for t in to[:3]):
@@ -873,9 +880,10 @@ class Beam(_Checked):
     def reorder(self, parents, slots, *pools, out=None, stream=None):
         """The states in `pools` (each (nslots, ...), contiguous) follow their beams in place; returns the new beams'
         slots (B, beams), for slots (B, beams) int32 of the old ones."""
+        given = out
         if out is None:
             out = _new(stream)(self.shape, dtype=torch.int32, device=self.device)
-        if not self._looked_at("reorder", parents, slots, out, *pools):
+        if not self._looked_at("reorder", parents, slots, given, *pools):
             self._beams(torch.int32, parents=parents, slots=slots, out=out)
             for i, t in enumerate(pools):
                 _want(f"pools[{i}]", t, t.shape, t.dtype, self.device)
@@ -884,7 +892,7 @@ class Beam(_Checked):
                 _dense(f"pools[{i}]", t)
             self._accept()
         handle = self._on(stream)
-        for at, n, size in [(t.data_ptr(), t.shape[0], t[0].numel() * t.element_size() if t.shape[0] else 0) for t in pools] or [(None, 0, 0)]:
+        for at, n, size in [(t.data_ptr(), t.shape[0], t.nbytes // t.shape[0] if t.shape[0] else 0) for t in pools] or [(None, 0, 0)]:
             _check(_lib.luna_beam_reorder(self._ref["forward"], parents.data_ptr(), slots.data_ptr(), n, at, size,
                                           out.data_ptr(), handle), "luna_beam_reorder")
         return out
