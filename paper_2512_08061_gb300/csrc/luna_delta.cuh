@@ -29,7 +29,7 @@ namespace luna {
 
 constexpr int kDeltaRows = 64;      // rows of a chunk
 // tensor-core form: fp32 values of a chunk's factors, and of the scales of 16 columns of it
-constexpr int kDeltaFactors = 4 * kDeltaRows + 12, kDeltaScales = 8;
+constexpr int kDeltaFactors = 6 * kDeltaRows + 12, kDeltaScales = 8;
 
 struct GateView {  // a (B, H, n) tensor
     const void *p;

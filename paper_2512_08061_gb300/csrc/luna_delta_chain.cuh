@@ -29,7 +29,7 @@ struct ChainShared {
     struct Stage {
         alignas(128) char k[DP / 64][kTileB], q[kQ ? DP / 64 : 1][kQ ? kTileB : 16], T[2][kTileB];
         alignas(128) char P[kPlanes][kQ ? kTileB : 16], x[C * kPitch];
-        alignas(16) float rows[kRowsF];
+        alignas(16) float rows[4 * C + 12];  // (the gates' sums behind them are not needed)
     } stage[2];
     uint64_t bar[2];
     alignas(16) char out[kQ ? kWarps : 1][C * 48];  // 16 columns of the outputs, rows of 32 bytes 48 apart
@@ -95,20 +95,11 @@ __device__ __forceinline__ void plane_room(int lane) {  // the copies before hav
     if (lane == 0) bulk_wait_read();
     __syncwarp();
 }
-__device__ __forceinline__ void plane_put(char *mem, int k0, const Frag &f, int lane) {
-    const int r = (lane >> 3 & 1) * 8 + (lane & 7);
-    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(smem_u32(mem) + tile_at(0, 16, r, (k0 >> 3) + (lane >> 4))),
-                 "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3])
-                 : "memory");
-}
 __device__ __forceinline__ void plane_send(const char *mem, __half *tile, int rows, int r0, int panels, int lane) {
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
-        for (int p = 0; p < panels; ++p)
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 2048;" ::"l"(reinterpret_cast<char *>(tile) + (p * rows + r0) * 128),
-                         "r"(smem_u32(mem) + p * 2048)
-                         : "memory");
+        for (int p = 0; p < panels; ++p) store_tile(reinterpret_cast<char *>(tile) + (p * rows + r0) * 128, smem_u32(mem) + p * 2048, 2048);
         bulk_commit();
     }
 }
@@ -139,7 +130,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     char *const mem = sm.planes[SP == 1 ? warp : 0];
     auto put = [&](__half *tile, int k0, const Frag &f) {
         if (SP == 1)
-            plane_put(mem, k0, f, lane);
+            tile_put(smem_u32(mem), 16, 0, k0, f, lane);
         else
             plane_store(tile, a.dvp, col, k0, f, lane);
     };

@@ -18,7 +18,9 @@ struct GradShared {
     alignas(128) char k[DP / 64][kTileB], go[DVT * 128], x[DVT * 128], u[DVT * 128 > 2 * kTileB ? DVT * 128 : 2 * kTileB];
     alignas(128) char s[DVT * DP * 2 > DP / 64 * kTileB ? DVT * DP * 2 : DP / 64 * kTileB];
     uint64_t bar[4];
-    float hi[C], lo[C], past[C], left[C], b[C], scales[DVT / 16][kDeltaScales], behind[DVT / 16][2];  // (behind: of R)
+    alignas(16) float rows[kRowsF];
+    alignas(16) float scales[2 * DVT / 16][kDeltaScales];  // of this chunk and, behind it, of the next place
+    float past[C], left[C];
     __half2 steps[8][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
     float all[8], total[kGradThreads / 32];
     float sums[6][kParts][C];  // of a row's quarters: q . dQ, k . Z without the rows' part, k . (dK), W . K K^T, x . v, b k . Z
@@ -67,7 +69,10 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         load_tile(sm.s, src, bytes, &sm.bar[which]);
     };
     if (tid == 0) {
-        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 3 * of_rows);
+        const uint32_t of_scales = 2 * groups * kDeltaScales * 4;
+        mbar_arrive_expect_tx(&sm.bar[0], sizeof(sm.k) + 3 * of_rows + sizeof(sm.rows) + of_scales);
+        load_tile(sm.rows, a.rows + at * kRowsF, sizeof(sm.rows), &sm.bar[0]);
+        load_tile(sm.scales, a.scales + slot * groups * kDeltaScales, of_scales, &sm.bar[0]);
         load_tile(sm.u, a.Up + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.x, a.Xp + at * dvp * C, of_rows, &sm.bar[0]);
         load_tile(sm.go, a.Gp + at * dvp * C, of_rows, &sm.bar[0]);
@@ -81,61 +86,67 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         ask(a.Rp + slot * dvp * DP, of_state);
         ask(a.Qp + kat * C * DP, sizeof(sm.k));
     }
-    const float *rowf = a.rows + at * kRowsF;
-    const float back_k = rowf[4 * C + 4], back_q = rowf[4 * C + 5];
-    if (warp == 0)
-        delta_gate_sums(lane, [&](int t) { return t < rows ? gate_at<__nv_bfloat16>(a.g, b, h, t0 + t) : 0.0f; }, sm.hi, sm.lo,
-                        sm.past, sm.left);
-    else if (warp < 3)
-        sm.b[tid - 32] = rowf[2 * C + tid - 32];
-    for (int i = tid; i < groups * kDeltaScales; i += kGradThreads) (&sm.scales[0][0])[i] = a.scales[slot * groups * kDeltaScales + i];
-    if (tid < groups * 2) sm.behind[tid / 2][tid % 2] = a.scales[((slot + 1) * groups + tid / 2) * kDeltaScales + 2 + tid % 2];
-    __syncthreads();
+    // x . v: a thread a row and a quarter of the columns, while the tiles come
+    uint32_t v[DVT / 8 / kParts][4];
+    {
+        const int i = tid % C;
+        const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
+#pragma unroll
+        for (int j = 0; j < DVT / 8 / kParts; ++j) {
+            const int c = (tid / C + j * kParts) * 8;
+            if (VEC) {
+                const uint4 w4 = i < rows && c < a.dv ? *reinterpret_cast<const uint4 *>(from + c) : make_uint4(0, 0, 0, 0);
+                v[j][0] = w4.x; v[j][1] = w4.y; v[j][2] = w4.z; v[j][3] = w4.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = load_pair(from + c + 2 * e, i < rows ? a.dv - c - 2 * e : 0, false);
+                    v[j][e] = pack_bf16(f.x, f.y);
+                }
+            }
+        }
+    }
+    bool here = mbar_wait_long(&sm.bar[0], 0);
+    const float back_k = sm.rows[4 * C + 4], back_q = sm.rows[4 * C + 5];
+    const float *gate_b = sm.rows + 2 * C, *hi = sm.rows + 4 * C + 12, *lo = hi + C;
     // What is summed over the columns has a scale of its own every 16 of them: the left operand takes the ratio to the
     // largest of them (at most 1, and what it loses is small beside that).  Products: dO U, X U; of either half of the
     // other columns dO S, X S, U R.
-    if (tid < 8) {
-        const int side = tid < 2 ? 0 : (tid - 2) / 3, which = tid < 2 ? tid : (tid - 2) % 3;
-        auto scale = [&](int kt) {
-            const float *f = sm.scales[kt];
-            return tid < 2 ? f[6 - which] * f[4] : which < 2 ? f[6 - which] * f[side] : f[4] * sm.behind[kt][side];
-        };
-        float most = 0.0f;
-        for (int kt = 0; kt < groups; ++kt) most = fmaxf(most, scale(kt));
-        sm.all[tid] = most;
-        for (int kt = 0; kt < groups; ++kt) sm.steps[tid][kt] = __float2half2_rn(most > 0.0f ? scale(kt) / most : 0.0f);
+    if (tid < 64) {
+        const int product = tid / 8, kt = tid % 8, side = product < 2 ? 0 : (product - 2) / 3, which = product < 2 ? product : (product - 2) % 3;
+        float scale = 0.0f;
+        if (kt < groups) {
+            const float *f = sm.scales[kt], *g = sm.scales[groups + kt];  // (behind the chunk: R)
+            scale = product < 2 ? f[6 - which] * f[4] : which < 2 ? f[6 - which] * f[side] : f[4] * g[2 + side];
+        }
+        float most = scale;
+#pragma unroll
+        for (int w = 4; w > 0; w /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+        if (kt == 0) sm.all[product] = most;
+        if (kt < groups) sm.steps[product][kt] = __float2half2_rn(most > 0.0f ? scale * inverse2(most) : 0.0f);
+    } else if (tid < 64 + C) {
+        sm.past[tid - 64] = sm.rows[tid - 64] * inverse2(back_k);
+        sm.left[tid - 64] = sm.rows[C + tid - 64] * inverse2(back_k);
     }
-    // x . v: a thread a row and a quarter of the columns, while the tiles come
-    float xv = 0.0f;
-    bool here = mbar_wait_long(&sm.bar[0], 0);
-    __syncthreads();
     {
         const int i = tid % C;
-        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v.p) + b * a.v.sb + h * a.v.sh + (t0 + i) * a.v.st;
-        if (i < rows)
-            for (int c8 = tid / C; c8 * 8 < a.dv; c8 += kParts) {
-                uint32_t w[4];
-                if (VEC) {
-                    const uint4 w4 = *reinterpret_cast<const uint4 *>(v + c8 * 8);
-                    w[0] = w4.x; w[1] = w4.y; w[2] = w4.z; w[3] = w4.w;
-                } else {
+        float xv = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 f = load_pair(v + c8 * 8 + 2 * e, a.dv - c8 * 8 - 2 * e, false);
-                        w[e] = pack_bf16(f.x, f.y);
-                    }
-                }
-                float sum = 0.0f;
+        for (int j = 0; j < DVT / 8 / kParts; ++j) {
+            const int c8 = tid / C + j * kParts;
+            if (c8 * 8 >= dvp) continue;
+            float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    unsigned short u;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
-                    sum = fmaf(e & 1 ? high(w[e / 2]) : low(w[e / 2]), __half2float(__ushort_as_half(u)), sum);
-                }
-                xv = fmaf(sm.scales[c8 / 2][5], sum, xv);
+            for (int e = 0; e < 8; ++e) {
+                unsigned short u;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(tile_at(sx, dvp, c8 * 8 + e, i >> 3) + (i & 7) * 2));
+                sum = fmaf(e & 1 ? high(v[j][e / 2]) : low(v[j][e / 2]), __half2float(__ushort_as_half(u)), sum);
             }
+            xv = fmaf(sm.scales[c8 / 2][5], sum, xv);
+        }
         sm.sums[4][tid / C][i] = xv;
     }
+    __syncthreads();
 
     // 16 rows (m0) of a left operand from a plane, for the product's 16 columns kt
     auto left_plane = [&](Frag &f, uint32_t tile, int m0, int kt, int product) {
@@ -328,12 +339,12 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = r0 + mt * 16 + lane / 4 + (e >> 1) * 8, j = n0 + nt * 8 + q2 + (e & 1);
-                    const float c = j <= i ? expf((sm.hi[i] - sm.hi[j]) + (sm.lo[i] - sm.lo[j])) : 0.0f;
+                    const float c = j <= i ? expf((hi[i] - hi[j]) + (lo[i] - lo[j])) : 0.0f;
                     float &pp = p[mt][nt][e], &ww = w[mt][nt][e];
                     pp = j <= i ? by_p * c * pp : 0.0f;
                     ww = j < i ? by_w * c * ww : 0.0f;
                     if (j < i) dot[e >> 1] = fmaf(ww, kk[mt][nt][e], dot[e >> 1]);
-                    ww *= sm.b[i];
+                    ww *= gate_b[i];
                     mp = fmaxf(mp, fabsf(pp));
                     mw = fmaxf(mw, fabsf(ww));
                 }
@@ -454,7 +465,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     if (tid == 0) load_state(a.Qp + kat * C * DP, sizeof(sm.k), 3);
     times_rows(z, sm.past, nullptr, sm.all[of_half + 1]);
     dot_k(z, 1);
-    times_rows(z, sm.b, nullptr, inv);
+    times_rows(z, gate_b, nullptr, inv);
     over_rows(z, sW, false, sk, 0);
     times(z, by);
     dot_k(z, 5);
@@ -491,7 +502,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         float base = 0.0f;
         for (int w = 0; w < kGradThreads / 32; ++w) base += sm.total[w];
         delta_gate_grads(base, sm.read, sm.wrote, rows, lane, [&](int t, float x) {
-            io_store(dg + t * a.dg.st, expf(gate_at<__nv_bfloat16>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
+            const float g = t > 0 ? (hi[t] - hi[t - 1]) + (lo[t] - lo[t - 1]) : hi[0];
+            io_store(dg + t * a.dg.st, expf(g) == 0.0f ? 0.0f : x);
         });
     }
 }

@@ -15,7 +15,8 @@ using namespace delta;
 //
 // with both operands in two terms.  It leaves T^T, P and in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b,
 // scale c(i, 0) 2^eq of its rows, then c(C, 0) in two terms and what T, P, K and Q were scaled down by (the last two
-// are 2^ek and 2^eq), and the largest of c(C, i) 2^ek, of c(i, 0) 2^ek b, of scale c(i, 0) 2^eq.  (With the inverse in fp32 by all threads, 13 barriers and 68 KB of shared memory: 248 us for 8192
+// are 2^ek and 2^eq), the largest of c(C, i) 2^ek, of c(i, 0) 2^ek b, of scale c(i, 0) 2^eq, and the sums of the gates
+// in two terms.  (With the inverse in fp32 by all threads, 13 barriers and 68 KB of shared memory: 248 us for 8192
 // chunks.)
 
 constexpr int kPrepThreads = 128;
@@ -23,40 +24,31 @@ constexpr int kPrepThreads = 128;
 template <int DP>
 struct PrepShared {
     alignas(128) char k[DP / 64][kTileB], q[DP / 64][kTileB], A[2][kTileB];  // A: two planes; T_II in its diagonal blocks
-    float diag[4][16][17];
+    alignas(16) float diag[4][16][20];
     float hi[C], lo[C], past[C], left[C], b[C], tail[C], most[5][kPrepThreads / 32], back_T[4];  // tail: c(last of its 16, j)
 };
 
-// the half row of a bf16 tile that a thread scales: its largest value; in fp16 to `out`
+// A thread's 16-byte pieces of a bf16 tile, as they lie in memory: their largest value; in fp16 to `out`
 template <int DP>
-__device__ __forceinline__ uint4 prep_piece(uint32_t tile, int tid, int p) {
-    uint4 w;
-    const uint32_t at = tile_at(tile, C, tid / 2, tid % 2 * (DP / 16) + p);
-    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at));
-    return w;
-}
-template <int DP>
-__device__ __forceinline__ float prep_most(uint32_t tile, int tid) {
+__device__ __forceinline__ float prep_most(const char *tile, int tid) {
     uint32_t most = 0;
 #pragma unroll
-    for (int p = 0; p < DP / 16; ++p) {
-        const uint4 w = prep_piece<DP>(tile, tid, p);
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) most = __vmaxu2(most, u[i] & 0x7fff7fffu);
+    for (int i = 0; i < C * DP / 8 / kPrepThreads; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(tile + (tid + i * kPrepThreads) * 16);
+        most = __vmaxu2(most, __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu)));
     }
     return __uint_as_float(max(most << 16, most & 0x7fff0000u));
 }
 template <int DP>
-__device__ __forceinline__ void prep_write(uint32_t tile, float by, __half *out, int tid) {
+__device__ __forceinline__ void prep_write(const char *tile, float by, __half *out, int tid) {
 #pragma unroll
-    for (int p = 0; p < DP / 16; ++p) {
-        const uint4 w = prep_piece<DP>(tile, tid, p);
+    for (int i = 0; i < C * DP / 8 / kPrepThreads; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(tile + (tid + i * kPrepThreads) * 16);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
         uint32_t f[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = pack(by * low(u[i]), by * high(u[i]));
-        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(out) + tile_at(0, C, tid / 2, tid % 2 * (DP / 16) + p)) = make_uint4(f[0], f[1], f[2], f[3]);
+        for (int e = 0; e < 4; ++e) f[e] = pack(by * low(u[e]), by * high(u[e]));
+        reinterpret_cast<uint4 *>(out)[tid + i * kPrepThreads] = make_uint4(f[0], f[1], f[2], f[3]);
     }
 }
 // acc += F M^T in two terms each, for F of 16 rows and 16 summed indices, M the 16 x 16 block (n0, k0) of two planes
@@ -102,8 +94,8 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
         const float *m = sm.most[which];
         return scale_of(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
     };
-    most_of(2, prep_most<DP>(sk, tid));
-    most_of(3, prep_most<DP>(sq, tid));
+    most_of(2, prep_most<DP>(sm.k[0], tid));
+    most_of(3, prep_most<DP>(sm.q[0], tid));
     if (tid < C) sm.tail[tid] = expf((sm.hi[tid | 15] - sm.hi[tid]) + (sm.lo[tid | 15] - sm.lo[tid]));
     __syncthreads();
 
@@ -160,8 +152,8 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
     const Scale ps = block_scale(0), as = block_scale(1), ks = block_scale(2), qs = block_scale(3);
     if (h % (a.H / a.k.heads) == 0) {  // one head of those that share queries and keys
         const int64_t to = ((int64_t)b * a.k.heads + hk) * a.m + chunk;
-        prep_write<DP>(sk, ks.by, a.Kp + to * C * DP, tid);
-        prep_write<DP>(sq, qs.by, a.Qp + to * C * DP, tid);
+        prep_write<DP>(sm.k[0], ks.by, a.Kp + to * C * DP, tid);
+        prep_write<DP>(sm.q[0], qs.by, a.Qp + to * C * DP, tid);
     }
     float *rowf = a.rows + at * kRowsF;
     if (tid < C) {
@@ -169,6 +161,8 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
         rowf[C + tid] = sm.left[tid] * ks.back;
         rowf[2 * C + tid] = sm.b[tid];
         rowf[3 * C + tid] = a.scale * sm.past[tid] * qs.back;
+        rowf[4 * C + 12 + tid] = sm.hi[tid];
+        rowf[5 * C + 12 + tid] = sm.lo[tid];
     }
     if (tid == 0) {
         gate_terms(sm.hi[C - 1], rowf[4 * C], rowf[4 * C + 1]);
@@ -176,21 +170,19 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
         rowf[4 * C + 4] = ks.back;
         rowf[4 * C + 5] = qs.back;
     }
-    char *P = reinterpret_cast<char *>(a.Pp + at * (TERMS ? 2 : 1) * C * C);
+    Frag ph[4], pl[4];  // P of the warp's rows
 #pragma unroll
-    for (int nt = 0; nt < 8; ++nt)
+    for (int np = 0; np < 4; ++np) {
 #pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-            const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, nt) + q2 * 2;
-            uint32_t hi = 0, lo = 0;
-            if (nt / 2 <= warp) split(ps.by * qk[nt][e], ps.by * qk[nt][e + 1], hi, lo);
-            *reinterpret_cast<uint32_t *>(P + to) = hi;
-            if (TERMS) *reinterpret_cast<uint32_t *>(P + kTileB + to) = lo;
-            if (nt / 2 >= warp) continue;  // (its diagonal block waits for T_II)
-            split(as.by * kk[nt][e], as.by * kk[nt][e + 1], hi, lo);
-            *reinterpret_cast<uint32_t *>(sm.A[0] + to) = hi;
-            *reinterpret_cast<uint32_t *>(sm.A[1] + to) = lo;
-        }
+        for (int i = 0; i < 4; ++i) ph[np][i] = pl[np][i] = 0;
+        if (np > warp) continue;
+        split_left(qk[2 * np], qk[2 * np + 1], ps.by, ph[np], pl[np]);
+        if (np == warp) continue;  // (its diagonal block waits for T_II)
+        Frag hi, lo;
+        split_left(kk[2 * np], kk[2 * np + 1], as.by, hi, lo);
+        tile_put(sA, C, r0, np * 16, hi, lane);
+        tile_put(sA + kTileB, C, r0, np * 16, lo, lane);
+    }
     // T_II, a lane a column
     {
         float x[16], m = 0.0f;
@@ -198,7 +190,13 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
         for (int i = 0; i < 16; ++i) {
             x[i] = i == lane ? 1.0f : 0.0f;
 #pragma unroll
-            for (int l = 0; l < i; ++l) x[i] = fmaf(-sm.diag[warp][i][l], x[l], x[i]);
+            for (int l4 = 0; l4 < i; l4 += 4) {
+                const float4 w4 = *reinterpret_cast<const float4 *>(&sm.diag[warp][i][l4]);
+                const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                for (int l = 0; l < 4; ++l)
+                    if (l4 + l < i) x[i] = fmaf(-w[l], x[l4 + l], x[i]);
+            }
             m = fmaxf(m, fabsf(x[i]));
         }
         const Scale s = scale_of(warp_max(m));  // (the lanes without a column hold zeros)
@@ -215,6 +213,13 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
             }
     }
     __syncthreads();
+    // (all have read K and Q, in whose place P goes)
+    const uint32_t sP = sk;
+#pragma unroll
+    for (int np = 0; np < 4; ++np) {
+        tile_put(sP, C, r0, np * 16, ph[np], lane);
+        if (TERMS) tile_put(sP + kTileB, C, r0, np * 16, pl[np], lane);
+    }
     if (warp == 3) {  // (whose block column is the diagonal block alone) the largest of what the chains multiply by
         float m[3];
         for (int i = 0; i < 2; ++i) {
@@ -286,19 +291,21 @@ __global__ void __launch_bounds__(kPrepThreads, 4) k_delta_prepare(DeltaArgs a) 
     __syncthreads();
     const Scale ts = block_scale(4);
     if (tid == 0) rowf[4 * C + 2] = ts.back;
-    char *planes = reinterpret_cast<char *>(a.Tp + at * 2 * C * C);
 #pragma unroll
-    for (int s = 0; s < 4; ++s)  // (block row J + s, or the empty ones before J)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                uint32_t th = 0, tl = 0;
-                if (warp + s < 4) split(ts.by * T[s][i][e], ts.by * T[s][i][e + 1], th, tl);
-                const uint32_t to = tile_at(0, C, r0 + lane / 4 + e * 4, (warp + s) % 4 * 2 + i) + q2 * 2;
-                *reinterpret_cast<uint32_t *>(planes + to) = th;
-                *reinterpret_cast<uint32_t *>(planes + kTileB + to) = tl;
-            }
+    for (int s = 0; s < 4; ++s) {  // (block row J + s, or the empty ones before J), in the place of A
+        Frag th = {0, 0, 0, 0}, tl = {0, 0, 0, 0};
+        if (warp + s < 4) split_left(T[s][0], T[s][1], ts.by, th, tl);
+        tile_put(sA, C, r0, (warp + s) % 4 * 16, th, lane);
+        tile_put(sA + kTileB, C, r0, (warp + s) % 4 * 16, tl, lane);
+    }
+    fence_proxy_async_smem();
+    __syncthreads();
+    if (tid == 0) {
+        store_tile(a.Tp + at * 2 * C * C, sA, 2 * kTileB);
+        store_tile(a.Pp + at * (TERMS ? 2 : 1) * C * C, sP, (TERMS ? 2 : 1) * kTileB);
+        bulk_commit();
+        bulk_wait();  // (shared memory is read to the end)
+    }
 }
 
 template <int DP, bool TERMS>

@@ -190,6 +190,16 @@ __device__ __forceinline__ void split_left(const float (&c0)[4], const float (&c
     split(by * c1[2], by * c1[3], hi[3], lo[3]);
 }
 
+// 16 x 16 values of a left operand (or of two neighbouring n-tiles) into a tile
+__device__ __forceinline__ void tile_put(uint32_t base, int rows, int r0, int k0, const Frag &f, int lane) {
+    const uint32_t at = tile_at(base, rows, r0 + (lane >> 3 & 1) * 8 + (lane & 7), (k0 >> 3) + (lane >> 4));
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+}
+// shared memory to global memory, by one thread (committed, not waited for)
+__device__ __forceinline__ void store_tile(void *dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void zero(float (&c)[N][4]) {
 #pragma unroll
