@@ -32,8 +32,9 @@ struct ChainShared {
         alignas(16) float rows[4 * C + 12];  // (the gates' sums behind them are not needed)
     } stage[2];
     uint64_t bar[2];
-    alignas(16) char out[kQ ? kWarps : 1][C * 48];  // 16 columns of the outputs, rows of 32 bytes 48 apart
-    alignas(128) char planes[MODE != kOutputs && SP == 1 ? kWarps : 1][DP * 32];  // 16 rows of a tile that is kept
+    // 16 columns of the outputs (one warp a group: they take the place of its columns of V or dO)
+    alignas(16) char out[kQ && SP == 2 ? kWarps : 1][kQ && SP == 2 ? C * 48 : 16];
+    alignas(128) char planes[MODE != kOutputs && SP == 1 ? kWarps : 1][MODE != kOutputs && SP == 1 ? DP * 32 : 16];  // 16 rows of a tile that is kept
     float4 shares[SP == 1 ? 1 : kWarps][SP == 1 ? 1 : 12][32];
 };
 
@@ -63,8 +64,8 @@ __device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, MODE
 }
 
 // Rows first, first + 1, .. (n of them) of a warp's 16 columns, given column by column, to the output: transposed through
-// shared memory
-__device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first, int n, char *mem, __nv_bfloat16 *out, int64_t st, int rows,
+// shared memory, in rows of 32 bytes `pitch` apart (a multiple of 16 whose eight first multiples fall into eight banks)
+__device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first, int n, char *mem, int pitch, __nv_bfloat16 *out, int64_t st, int rows,
                                             int col, int dv, bool vec, int lane) {
     const uint32_t base = smem_u32(mem);
 #pragma unroll
@@ -72,13 +73,13 @@ __device__ __forceinline__ void chain_store(const float (&acc)[8][4], int first,
         if (nt * 8 < first || nt * 8 >= first + n) continue;
         const Frag f = {pack_bf16(acc[nt][0], acc[nt][1]), pack_bf16(acc[nt][2], acc[nt][3]),
                         pack_bf16(acc[nt + 1][0], acc[nt + 1][1]), pack_bf16(acc[nt + 1][2], acc[nt + 1][3])};
-        stm_t(base + (nt * 8 + (lane >> 4) * 8 + (lane & 7)) * 48 + ((lane >> 3) & 1) * 16, f);
+        stm_t(base + (nt * 8 + (lane >> 4) * 8 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16, f);
     }
     __syncwarp();
     for (int i = 0; i < n / 16; ++i) {
         const int r = first + i * 16 + lane / 2, half = lane % 2;
         if (r < rows && col + half * 8 < dv) {
-            const __nv_bfloat16 *from = reinterpret_cast<const __nv_bfloat16 *>(mem + r * 48 + half * 16);
+            const __nv_bfloat16 *from = reinterpret_cast<const __nv_bfloat16 *>(mem + r * pitch + half * 16);
             __nv_bfloat16 *to = out + r * st + col + half * 8;
             if (vec)
                 *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
@@ -191,6 +192,8 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
         const float whole = st.rows[4 * C], rest = st.rows[4 * C + 1], back_T = st.rows[4 * C + 2], back_P = st.rows[4 * C + 3];
         auto factor = [&](int which, int t) { return *reinterpret_cast<const float2 *>(st.rows + which * C + t); };
         const int64_t at = bh * a.m + chunk;
+        char *const out = SP == 2 ? sm.out[warp] : st.x + group * 32;
+        constexpr int out_pitch = SP == 2 ? 48 : Sh::kPitch;
         // S <- c(C, 0) S (first) + F M for a left operand F of 64 summed rows and the tile M (a row for each)
         auto update = [&](const Frag (&fh)[4], const Frag (&fl)[4], float back, uint32_t tile, bool decay) {
 #pragma unroll
@@ -368,7 +371,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[nt][e] = fmaf(back_s * (e & 1 ? past.y : past.x), y[nt][e], back * x[nt][e]);
                     }
-                    chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, VEC, lane);
+                    chain_store(y, first, some, out, out_pitch, o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, VEC, lane);
                 }
             }
 #pragma unroll
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) split_left(x[2 * kt], x[2 * kt + 1], ws.by, fh[kt], fl[kt]);
             update(fh, fl, ws.back, sk, false);
-            chain_store(y, first, some, sm.out[warp], o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, VEC, lane);
+            chain_store(y, first, some, out, out_pitch, o + t0 * a.ot, a.ot, min(C, len - t0), col, a.dv, VEC, lane);
         }
     }
     if (REV && mine && chunks > 0) {  // R before the first chunk
