@@ -102,7 +102,8 @@ constexpr float kGateLeast = -120.0f;
 // rows stay exact, and the factors from the chunk's start (past) and to its end (left).  gate(t) is 0 behind the end.
 template <typename F>
 __device__ __forceinline__ void delta_gate_sums(int lane, F gate, float *hi, float *lo, float *past, float *left) {
-    const double g0 = (double)fmaxf(gate(2 * lane), kGateLeast), g1 = (double)fmaxf(gate(2 * lane + 1), kGateLeast);
+    auto least = [](float g) { return (double)(g < kGateLeast ? kGateLeast : g); };  // (a NaN stays one)
+    const double g0 = least(gate(2 * lane)), g1 = least(gate(2 * lane + 1));
     double sum = g0 + g1;
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) {

@@ -157,13 +157,14 @@ __device__ __forceinline__ void split(float x0, float x1, uint32_t &hi, uint32_t
     const float2 f = half_pair(hi);
     lo = pack(x0 - f.x, x1 - f.y);
 }
-// The power of two that takes a largest value of 2^E (to 2^(E+1)) to 2^12, and its inverse.  (Below 2^-113 all is 0.)
+// The power of two that takes a largest value of 2^E (to 2^(E+1)) to 2^12, and its inverse.  (Below 2^-113 all is 0; an
+// infinity would leave everything else 0, so that all becomes NaN with it.)
 struct Scale {
     float by, back;
 };
 __device__ __forceinline__ Scale scale_of(float most) {
     const uint32_t e = max((__float_as_uint(most) >> 23) & 255u, 14u);
-    return Scale{__uint_as_float((254u + 12u - e) << 23), __uint_as_float((e - 12u) << 23)};
+    return Scale{__uint_as_float(e == 255u ? 0x7fffffffu : (254u + 12u - e) << 23), __uint_as_float((e - 12u) << 23)};
 }
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll

@@ -249,6 +249,52 @@ def test_padding_may_hold_anything(L, io):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("io", [F, BF])
+@pytest.mark.parametrize("which", ["Q", "K", "V", "dO"])
+def test_rows_of_different_size(L, io, which):
+    """Rows of one tensor 2^-12 to 1 times as large as their neighbours.  What is proportional to a row (O to Q's, dQ to
+    dO's) is within the tolerance with that factor divided out, and everything within it as a whole.  (A row's error over
+    its own value has no bound: q_i . k_j may be as near to 0 as it likes, and the rounding of its terms is not.)"""
+    B, H, n, d = 1, 2, 200, 64
+    Q, K, V, dO, lg, bt, S0, dS1 = inputs(B, H, H, n, d, d, io, "tokens", 17, which != "V")
+    x = {"Q": Q, "K": K, "V": V, "dO": dO}
+    g = torch.Generator("cuda").manual_seed(3)
+    size = 2.0 ** -torch.randint(0, 13, (B, H, n, 1), generator=g, device="cuda")
+    x[which].mul_(size)
+    ref = recurrence(*(f64(t) for t in (Q, K, V, lg, bt)), d ** -0.5, None, None if S0 is None else f64(S0), f64(dO),
+                     None if dS1 is None else f64(dS1))
+    p = L.Delta(B, H, n, d, d, io=io, backward=True)
+    got = {"O": p.forward(Q, K, V, lg, bt, None, S0), **p.backward(Q, K, V, dO, lg, bt, None, S0, dS1)}
+    for name, t in got.items():
+        assert rel(t, ref[name]) < tol(name, t.dtype), name
+    own = {"Q": "O", "dO": "dQ"}.get(which)
+    if own:
+        assert rel(got[own].float() / size, ref[own] / f64(size)) < TOL[io]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 4, 5])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_not_finite(L, which, value):
+    """A value that is not finite shows in its row's outputs or gradients, and stays in its sequence and head."""
+    B, H, n, d = 2, 2, 150, 64
+    x = list(inputs(B, H, H, n, d, d, BF, "tokens", 6, False)[:6])  # Q, K, V, dO, gates, betas
+    p = L.Delta(B, H, n, d, d, io=BF, backward=True)
+
+    def run():
+        return {"O": p.forward(x[0], x[1], x[2], x[4], x[5]), **p.backward(x[0], x[1], x[2], x[3], x[4], x[5])}
+
+    want = run()
+    x[which][1, 0, 70].view(-1)[0] = value
+    got = run()
+    for name in got:
+        for b, h in ((0, 0), (0, 1), (1, 1)):
+            assert torch.equal(got[name][b, h], want[name][b, h]), name
+    assert any(not torch.isfinite(got[name][1, 0, 70].float()).all() for name in got)
+    assert L.luna_device_status(p.ws) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
 @pytest.mark.parametrize("case", ["none", "reset", "far", "all"])
 def test_extreme_gates(L, io, case):
     """No forgetting; a state that starts anew at some tokens (a gate of -inf, its gradient 0) between slow ones;
@@ -396,6 +442,55 @@ def test_other_stream_and_graph(L):
     assert torch.equal(O, want)
     for name in grads:
         assert torch.equal(out[name], grads[name]), name
+
+
+@pytest.mark.gpu
+def test_memory_of_a_call_on_another_stream(L):
+    """What a call on a stream allocates is that stream's: not handed out on the current one while the call may run."""
+    B, H, n, d = 2, 32, 1024, 128
+    io = dict(device="cuda", dtype=BF)
+    x, gate = torch.randn((B, H, n, d), **io), torch.full((B, H, n), -0.1, **io)
+    k = torch.nn.functional.normalize(x, dim=-1)
+    s = torch.cuda.Stream()
+    p = L.Delta(B, H, n, d, d, backward=True)
+    want = p.forward(k, k, x, gate, -gate)
+    torch.cuda.synchronize()
+    for call in (lambda: (p.forward(k, k, x, gate, -gate, stream=s),), lambda: tuple(p.backward(k, k, x, x, gate, -gate, stream=s).values())[:3]):
+        out = call()
+        there = {t.data_ptr(): (t.shape, t.dtype) for t in out}
+        del out
+        mine = [torch.empty(shape, dtype=dtype, device="cuda") for shape, dtype in there.values()]
+        assert not any(t.data_ptr() in there for t in mine)
+        del mine
+    torch.cuda.synchronize()
+    assert torch.equal(p.forward(k, k, x, gate, -gate), want)
+
+
+@pytest.mark.gpu
+def test_two_plans_at_once(L):
+    """Two plans on two streams, and a captured call replayed beside them, keep out of each other's memory."""
+    a = inputs(2, 4, 4, 900, 64, 64, BF, "tokens", 2, True)
+    b = inputs(2, 4, 2, 700, 128, 64, BF, "tokens", 3, True)
+    plans = [L.Delta(2, 4, 900, 64, 64, backward=True), L.Delta(2, 4, 700, 128, 64, Hk=2, backward=True), L.Delta(2, 4, 900, 64, 64)]
+    call = lambda p, x: p.backward(x[0], x[1], x[2], x[3], x[4], x[5], None, x[6], x[7])  # noqa: E731
+    want = [call(plans[0], a), call(plans[1], b), plans[2].forward(a[0], a[1], a[2], a[4], a[5], None, a[6])]
+    O = torch.empty_like(want[2])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        plans[2].forward(a[0], a[1], a[2], a[4], a[5], None, a[6], O=O)
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        O.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            x = call(plans[0], a)
+        with torch.cuda.stream(t):
+            y = call(plans[1], b)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x[k], want[0][k]) for k in x) and all(torch.equal(y[k], want[1][k]) for k in y)
+        assert torch.equal(O, want[2])
 
 
 @pytest.mark.gpu
