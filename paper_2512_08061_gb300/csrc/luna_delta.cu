@@ -6,13 +6,14 @@
 #include "luna_prof.cuh"
 
 namespace luna {
+int tc_sm_count();
+
 namespace {
 
 // ---------------------------------------------------------------------------
 // The recurrence, forward (S, from which u and o) and in reverse (R, from which x and dV).
 //
-// A column of the state takes part in no other: eight lanes hold one column, 16 values each at d = 128, and a block of
-// 128 threads 16 columns.  Four rows go at a time: their dot products with the state before them are summed over the
+// A column of the state takes part in no other: eight lanes hold one column, 16 values each at d = 128.  Four rows go at a time: their dot products with the state before them are summed over the
 // eight lanes together, and what they do to each other is known from the dot products of the rows themselves:
 //
 //     u_i = b_i (v_i - A_i k_i . S - sum_{j < i} M_ij u_j),   o_i = scale (A_i q_i . S + sum_{j <= i} N_ij u_j)
@@ -23,12 +24,12 @@ namespace {
 //
 //     x_i = A_i k_i . R + sum_{j <= i} N_ij G_j - sum_{j < i} M_ij b_j x_j,   R <- A R + sum_j L_j (q_j G_j - b_j k_j x_j)
 //
-// Rows come in tiles of 16 through shared memory.  Four warps carry the columns; four more fetch the tile after the next,
+// Rows come in tiles of 16 through shared memory.  A warp carries four columns; four more warps of a block fetch the tile after the next,
 // work out the rows' own products of the next and write the outputs of the one before, so that the columns' warps, whose
 // chain bounds the pass, do nothing else: 199 ns a row at d = 128 (with all of that in the same warps 430 ns, whether four
 // rows go at a time or one).
 
-constexpr int kRowCols = 16, kRowThreads = 256, kTile = 16, kFour = 4;
+constexpr int kLoaders = 128, kTile = 16, kFour = 4;
 
 struct Four {  // of four rows
     float b[kFour], A[kFour], L[kFour], M[kFour][kFour], N[kFour][kFour], all, rest;
@@ -45,21 +46,23 @@ __device__ __forceinline__ float lanes8(float x) {
 // of a s alone would be off the same way at every row too (2e-4 of the state after 20000 rows of a = 1 - 1e-6).
 __device__ __forceinline__ float decayed(float a, float rest, float s, float x) { return fmaf(a, s, fmaf(rest, s, x)); }
 
-template <int JD>
+template <int JD, int COLS>
 struct RowTile {
     float4 k[kTile][8 * JD + 1], q[kTile][8 * JD + 1];  // (the padding: rows start in different banks)
-    float x[kTile][kRowCols], y[kTile][kRowCols], z[kTile][kRowCols], g[kTile];
+    float x[kTile][COLS], y[kTile][COLS], z[kTile][COLS], g[kTile];
     Four four[kTile / kFour];
 };
 
-template <int JD, bool REV>
-__global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(DeltaArgs a) {
-    constexpr int DP = 32 * JD, LOADERS = kRowThreads / 2, PER = kTile * DP / LOADERS;  // padded width; values of k (and q) a loader fetches
-    __shared__ RowTile<JD> tile_[2];
-    const int tid = threadIdx.x % LOADERS, p = tid % 8, cl = tid / 8;
-    const bool loads = threadIdx.x >= LOADERS;
+template <int JD, bool REV, int COLS, int CPL>  // CPL: columns of a lane
+__global__ void __launch_bounds__(COLS / CPL * 8 + kLoaders, JD == 4 ? 2 : 3) k_delta_rows(DeltaArgs a) {
+    constexpr int DP = 32 * JD, PER = kTile * DP / kLoaders;  // padded width; values of k (and q) a loader fetches
+    constexpr int XPER = kTile * COLS / kLoaders;             // of v or dO
+    __shared__ RowTile<JD, COLS> tile_[2];
+    constexpr int CARRY = COLS / CPL * 8;                     // threads that carry the columns
+    const bool loads = threadIdx.x >= CARRY;
+    const int tid = loads ? threadIdx.x - CARRY : threadIdx.x, p = tid % 8, cl = tid / 8;
     const int64_t bh = blockIdx.x;
-    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * kRowCols, col = col0 + cl;
+    const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * COLS;
     const int len = head_length(a.lengths, b, a.n), tiles = (len + kTile - 1) / kTile;
     const int64_t E = (int64_t)a.d * a.dv;
     const RowView &xv = REV ? a.go : a.v;
@@ -75,18 +78,18 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
         const float *x = static_cast<const float *>(xv.p) + b * xv.sb + h * xv.sh;
         float *U = REV ? a.X : a.U;
         if (U) U += bh * a.n * a.dv;
-        float nk[PER], nq[PER], nx[2], ng = 0.0f, nb = 0.0f;
+        float nk[PER], nq[PER], nx[XPER], ng = 0.0f, nb = 0.0f;
         auto fetch = [&](int tile) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int w = tid + i * LOADERS, t = tile * kTile + w / DP, c = w % DP;
+                const int w = tid + i * kLoaders, t = tile * kTile + w / DP, c = w % DP;
                 const bool in = t < len && c < a.d;
                 nk[i] = in ? k[t * a.k.st + c] : 0.0f;
                 nq[i] = in ? q[t * a.q.st + c] : 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int w = tid + i * LOADERS, t = tile * kTile + w / kRowCols, c = col0 + w % kRowCols;
+            for (int i = 0; i < XPER; ++i) {
+                const int w = tid + i * kLoaders, t = tile * kTile + w / COLS, c = col0 + w % COLS;
                 nx[i] = t < len && c < a.dv ? x[t * xv.st + c] : 0.0f;
             }
             if (tid < kTile) {
@@ -96,20 +99,20 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
             }
         };
         // the fetched rows into a tile, and what its fours need
-        auto prepare = [&](RowTile<JD> &sm) {
+        auto prepare = [&](RowTile<JD, COLS> &sm) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int w = tid + i * LOADERS;
+                const int w = tid + i * kLoaders;
                 reinterpret_cast<float *>(sm.k[w / DP])[w % DP] = nk[i];
                 reinterpret_cast<float *>(sm.q[w / DP])[w % DP] = nq[i];
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) (&sm.x[0][0])[tid + i * LOADERS] = nx[i];
+            for (int i = 0; i < XPER; ++i) (&sm.x[0][0])[tid + i * kLoaders] = nx[i];
             if (tid < kTile) {
                 sm.g[tid] = ng;
                 sm.four[tid / kFour].b[REV ? kFour - 1 - tid % kFour : tid % kFour] = nb;
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(LOADERS) : "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(kLoaders) : "memory");
             // two threads a dot product: of the 16 of a four those with j <= i, k_i . k_j (j < i) and N's
             const int f = tid / 32, lane = tid % 32, i = lane / 8, j = lane / 2 % 4, part = lane % 2;
             Four &four = sm.four[f];
@@ -144,10 +147,10 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
             }
             if (lane == kFour) gate_terms(between(0, kFour), four.all, four.rest);
         };
-        auto write = [&](const RowTile<JD> &sm, int tile) {
+        auto write = [&](const RowTile<JD, COLS> &sm, int tile) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int w = tid + i * LOADERS, t = w / kRowCols, c = w % kRowCols;
+            for (int i = 0; i < XPER; ++i) {
+                const int w = tid + i * kLoaders, t = w / COLS, c = w % COLS;
                 const int64_t r = tile * kTile + t;
                 if (r < len && col0 + c < a.dv) {
                     if (o) o[r * a.ot + col0 + c] = sm.y[t][c];
@@ -169,9 +172,9 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
         }
         if (tiles > 0) write(tile_[(tiles - 1) & 1], tile_of(tiles - 1));
         if (o)
-            for (int64_t i = tid; i < (int64_t)(a.n - len) * kRowCols; i += LOADERS) {
-                const int c = col0 + (int)(i % kRowCols);
-                if (c < a.dv) o[(len + i / kRowCols) * a.ot + c] = 0.0f;
+            for (int64_t i = tid; i < (int64_t)(a.n - len) * COLS; i += kLoaders) {
+                const int c = col0 + (int)(i % COLS);
+                if (c < a.dv) o[(len + i / COLS) * a.ot + c] = 0.0f;
             }
         return;
     }
@@ -180,99 +183,134 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
     if (ends) ends += bh * (a.m + 1) * E;
     const float *init = REV ? a.dS1 : a.S0;
     float *last = REV ? a.dS0 : a.S1;
-    float s[JD][4];
+    float s[CPL][JD][4];  // of columns cl, cl + COLS / CPL, ..
     auto row = [&](int j, int e) { return j * 32 + p * 4 + e; };
+    auto column = [&](int c) { return cl + c * (COLS / CPL); };
     auto keep = [&](float *to) {
-        if (col < a.dv)
 #pragma unroll
-            for (int j = 0; j < JD; ++j)
+        for (int c = 0; c < CPL; ++c)
+            if (col0 + column(c) < a.dv)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (row(j, e) < a.d) to[(int64_t)row(j, e) * a.dv + col] = s[j][e];
+                for (int j = 0; j < JD; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (row(j, e) < a.d) to[(int64_t)row(j, e) * a.dv + col0 + column(c)] = s[c][j][e];
     };
 #pragma unroll
-    for (int j = 0; j < JD; ++j)
+    for (int c = 0; c < CPL; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            s[j][e] = init && col < a.dv && row(j, e) < a.d ? init[bh * E + (int64_t)row(j, e) * a.dv + col] : 0.0f;
+        for (int j = 0; j < JD; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = row(j, e), to = col0 + column(c);
+                s[c][j][e] = init && to < a.dv && r < a.d ? init[bh * E + (int64_t)r * a.dv + to] : 0.0f;
+            }
     constexpr int kTiles = kDeltaRows / kTile;  // of a chunk
     if (REV && ends) keep(ends + (int64_t)((len + kDeltaRows - 1) / kDeltaRows) * E);
     __syncthreads();
     for (int step = 0; step < tiles; ++step) {
-        RowTile<JD> &sm = tile_[step & 1];
+        RowTile<JD, COLS> &sm = tile_[step & 1];
         const int tile = tile_of(step);
         if (!REV && ends && tile % kTiles == 0) keep(ends + (int64_t)(tile / kTiles) * E);
 #pragma unroll 1
         for (int r = 0; r < kTile / kFour; ++r) {
             const int f = REV ? kTile / kFour - 1 - r : r;
-            const Four &c = sm.four[f];
-            float dk[kFour], dq[kFour], u[kFour];
+            const Four &four = sm.four[f];
+            float dk[CPL][kFour], dq[CPL][kFour], u[CPL][kFour];
 #pragma unroll
             for (int i = 0; i < kFour; ++i) {
-                float x0 = 0.0f, x1 = 0.0f, y0 = 0.0f, y1 = 0.0f;
+                float x0[CPL], x1[CPL], y0[CPL], y1[CPL];
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) x0[c] = x1[c] = y0[c] = y1[c] = 0.0f;
 #pragma unroll
                 for (int j = 0; j < JD; ++j) {
                     const float4 kk = sm.k[at(f, i)][j * 8 + p];
-                    x0 = fmaf(kk.x, s[j][0], fmaf(kk.y, s[j][1], x0));
-                    x1 = fmaf(kk.z, s[j][2], fmaf(kk.w, s[j][3], x1));
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c) {
+                        x0[c] = fmaf(kk.x, s[c][j][0], fmaf(kk.y, s[c][j][1], x0[c]));
+                        x1[c] = fmaf(kk.z, s[c][j][2], fmaf(kk.w, s[c][j][3], x1[c]));
+                    }
                     if (!REV) {
                         const float4 qq = sm.q[at(f, i)][j * 8 + p];
-                        y0 = fmaf(qq.x, s[j][0], fmaf(qq.y, s[j][1], y0));
-                        y1 = fmaf(qq.z, s[j][2], fmaf(qq.w, s[j][3], y1));
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c) {
+                            y0[c] = fmaf(qq.x, s[c][j][0], fmaf(qq.y, s[c][j][1], y0[c]));
+                            y1[c] = fmaf(qq.z, s[c][j][2], fmaf(qq.w, s[c][j][3], y1[c]));
+                        }
                     }
                 }
-                dk[i] = x0 + x1;
-                dq[i] = y0 + y1;
-            }
 #pragma unroll
-            for (int i = 0; i < kFour; ++i) {
-                dk[i] = lanes8(dk[i]);
-                if (!REV) dq[i] = lanes8(dq[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < kFour; ++i) {
-                const float xc = sm.x[at(f, i)][cl];
-                if (!REV) {
-                    float w = fmaf(-c.A[i], dk[i], xc);
-#pragma unroll
-                    for (int j = 0; j < i; ++j) w = fmaf(-c.M[i][j], u[j], w);
-                    u[i] = c.b[i] * w;
-                    float y = c.A[i] * dq[i];
-#pragma unroll
-                    for (int j = 0; j <= i; ++j) y = fmaf(c.N[i][j], u[j], y);
-                    if (p == 0) { sm.y[at(f, i)][cl] = a.scale * y; sm.z[at(f, i)][cl] = u[i]; }
-                } else {
-                    dq[i] = xc;  // (dO_i)
-                    float w = c.A[i] * dk[i];
-#pragma unroll
-                    for (int j = 0; j <= i; ++j) w = fmaf(c.N[i][j], dq[j], w);
-#pragma unroll
-                    for (int j = 0; j < i; ++j) w = fmaf(-c.M[i][j], u[j], w);
-                    u[i] = c.b[i] * w;
-                    if (p == 0) { sm.y[at(f, i)][cl] = u[i]; sm.z[at(f, i)][cl] = w; }
+                for (int c = 0; c < CPL; ++c) {
+                    dk[c][i] = x0[c] + x1[c];
+                    dq[c][i] = y0[c] + y1[c];
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kFour; ++i) {
-                dq[i] *= a.scale * c.L[i];
-                u[i] *= REV ? -c.L[i] : c.L[i];
-            }
+            for (int c = 0; c < CPL; ++c)
+#pragma unroll
+                for (int i = 0; i < kFour; ++i) {
+                    dk[c][i] = lanes8(dk[c][i]);
+                    if (!REV) dq[c][i] = lanes8(dq[c][i]);
+                }
+#pragma unroll
+            for (int c = 0; c < CPL; ++c)
+#pragma unroll
+                for (int i = 0; i < kFour; ++i) {
+                    const float xc = sm.x[at(f, i)][column(c)];
+                    float &y = sm.y[at(f, i)][column(c)], &z = sm.z[at(f, i)][column(c)];
+                    if (!REV) {
+                        float w = fmaf(-four.A[i], dk[c][i], xc);
+#pragma unroll
+                        for (int j = 0; j < i; ++j) w = fmaf(-four.M[i][j], u[c][j], w);
+                        u[c][i] = four.b[i] * w;
+                        float out = four.A[i] * dq[c][i];
+#pragma unroll
+                        for (int j = 0; j <= i; ++j) out = fmaf(four.N[i][j], u[c][j], out);
+                        if (p == 0) { y = a.scale * out; z = u[c][i]; }
+                    } else {
+                        dq[c][i] = xc;  // (dO_i)
+                        float w = four.A[i] * dk[c][i];
+#pragma unroll
+                        for (int j = 0; j <= i; ++j) w = fmaf(four.N[i][j], dq[c][j], w);
+#pragma unroll
+                        for (int j = 0; j < i; ++j) w = fmaf(-four.M[i][j], u[c][j], w);
+                        u[c][i] = four.b[i] * w;
+                        if (p == 0) { y = u[c][i]; z = w; }
+                    }
+                }
+#pragma unroll
+            for (int c = 0; c < CPL; ++c)
+#pragma unroll
+                for (int i = 0; i < kFour; ++i) {
+                    dq[c][i] *= a.scale * four.L[i];
+                    u[c][i] *= REV ? -four.L[i] : four.L[i];
+                }
 #pragma unroll
             for (int j = 0; j < JD; ++j) {
-                float t[4] = {0.f, 0.f, 0.f, 0.f};
+                float t[CPL][4];
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) t[c][0] = t[c][1] = t[c][2] = t[c][3] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kFour; ++i) {
                     const float4 kk = sm.k[at(f, i)][j * 8 + p];
-                    t[0] = fmaf(kk.x, u[i], t[0]); t[1] = fmaf(kk.y, u[i], t[1]);
-                    t[2] = fmaf(kk.z, u[i], t[2]); t[3] = fmaf(kk.w, u[i], t[3]);
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c) {
+                        t[c][0] = fmaf(kk.x, u[c][i], t[c][0]); t[c][1] = fmaf(kk.y, u[c][i], t[c][1]);
+                        t[c][2] = fmaf(kk.z, u[c][i], t[c][2]); t[c][3] = fmaf(kk.w, u[c][i], t[c][3]);
+                    }
                     if (REV) {
                         const float4 qq = sm.q[at(f, i)][j * 8 + p];
-                        t[0] = fmaf(qq.x, dq[i], t[0]); t[1] = fmaf(qq.y, dq[i], t[1]);
-                        t[2] = fmaf(qq.z, dq[i], t[2]); t[3] = fmaf(qq.w, dq[i], t[3]);
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c) {
+                            t[c][0] = fmaf(qq.x, dq[c][i], t[c][0]); t[c][1] = fmaf(qq.y, dq[c][i], t[c][1]);
+                            t[c][2] = fmaf(qq.z, dq[c][i], t[c][2]); t[c][3] = fmaf(qq.w, dq[c][i], t[c][3]);
+                        }
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[j][e] = decayed(c.all, c.rest, s[j][e], t[e]);
+                for (int c = 0; c < CPL; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[c][j][e] = decayed(four.all, four.rest, s[c][j][e], t[c][e]);
             }
         }
         if (REV && ends && tile % kTiles == 0) keep(ends + (int64_t)(tile / kTiles) * E);
@@ -284,28 +322,37 @@ __global__ void __launch_bounds__(kRowThreads, JD == 4 ? 2 : 3) k_delta_rows(Del
 
 // ---------------------------------------------------------------------------
 // Gradients of q, k and the gates from the states at the two ends of a chunk: seven products of 64 rows, each
-// thread with 4 rows and every 16th column of them.  The operands come from L2 in steps of 16 of the summed index;
-// bound by the shared-memory loads of the products (12 values for 32 multiply-adds): 107 us for 300 chunks of 40 x 72.
+// thread with 4 rows and two times 4 columns of them, two multiply-adds an instruction.  The operands come from L2 in
+// steps of 16 of the summed index; bound by that and its barriers: 872 us for 2048 chunks of 128 x 128 (every 16th column
+// a thread's, one multiply-add an instruction: 1140 us), 91 us for 300 of 40 x 72.
 
 constexpr int kGradThreads = 256, kGradK = 16;
 
 struct GradShared {
-    float A[kDeltaRows][kGradK + 1], B[kGradK][kMaxD + 1];
+    alignas(16) float A[kGradK][kDeltaRows + 4], B[kGradK][kMaxD + 4];
     float P[kDeltaRows][kDeltaRows + 1], W[kDeltaRows][kDeltaRows + 1];
     float hi[kDeltaRows], lo[kDeltaRows], b[kDeltaRows], past[kDeltaRows], left[kDeltaRows];
     float read[kDeltaRows], wrote[kDeltaRows], total[kGradThreads / 32];
 };
 
-// acc[r][c] += sum_k A(ty * 4 + r, k) B(k, tx + 16 c); BT: B is stored with k contiguous
+// A thread's c-th column
+__device__ __forceinline__ int grad_column(int tx, int c) { return tx * 4 + c % 4 + c / 4 * 64; }
+
+// acc[r][c] += sum_k A(ty * 4 + r, k) B(k, grad_column(tx, c)); BT: B is stored with k contiguous
 template <bool BT, int NC, typename FA, typename FB>
 __device__ __forceinline__ void grad_product(GradShared &sm, float (&acc)[4][NC], int K, FA fa, FB fb) {
     const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+    uint64_t two[4][NC / 2];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < NC / 2; ++c) two[r][c] = f2(acc[r][2 * c], acc[r][2 * c + 1]);
     for (int k0 = 0; k0 < K; k0 += kGradK) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = k0 + tid % kGradK, r = tid / kGradK + 16 * i;
-            sm.A[r][k - k0] = k < K ? fa(r, k) : 0.0f;
+            sm.A[k - k0][r] = k < K ? fa(r, k) : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -316,17 +363,24 @@ __device__ __forceinline__ void grad_product(GradShared &sm, float (&acc)[4][NC]
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kGradK; ++k) {
-            float x[4], y[NC];
+            const float4 x = *reinterpret_cast<const float4 *>(&sm.A[k][ty * 4]);
+            const uint64_t xx[4] = {f2(x.x, x.x), f2(x.y, x.y), f2(x.z, x.z), f2(x.w, x.w)};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = sm.A[ty * 4 + r][k];
+            for (int c = 0; c < NC / 4; ++c) {
+                const float4 y = *reinterpret_cast<const float4 *>(&sm.B[k][tx * 4 + c * 64]);
+                const uint64_t lo = f2(y.x, y.y), hi = f2(y.z, y.w);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) y[c] = sm.B[k][tx + 16 * c];
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int c = 0; c < NC; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+                for (int r = 0; r < 4; ++r) {
+                    two[r][2 * c] = fma2(xx[r], lo, two[r][2 * c]);
+                    two[r][2 * c + 1] = fma2(xx[r], hi, two[r][2 * c + 1]);
+                }
+            }
         }
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < NC / 2; ++c) unpack2(two[r][c], acc[r][2 * c], acc[r][2 * c + 1]);
 }
 
 __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
@@ -395,7 +449,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int i = ty * 4 + r, j = tx + 16 * c;
+                const int i = ty * 4 + r, j = grad_column(tx, c);
                 sm.P[i][j] = j <= i ? a.scale * gap(i, j) * acc[r][c] : 0.0f;
             }
         zero(acc);
@@ -404,7 +458,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int i = ty * 4 + r, j = tx + 16 * c;
+                const int i = ty * 4 + r, j = grad_column(tx, c);
                 sm.W[i][j] = j < i ? gap(i, j) * acc[r][c] : 0.0f;
             }
     }
@@ -425,7 +479,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         float dot = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int cc = tx + 16 * c;
+            const int cc = grad_column(tx, c);
             if (i < rows && cc < d) {
                 dot = fmaf(io_load(q + i * a.q.st + cc), acc[r][c], dot);
                 io_store(dq + i * a.dqt + cc, acc[r][c]);
@@ -448,7 +502,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         float dot = 0.0f, xv = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int cc = tx + 16 * c;
+            const int cc = grad_column(tx, c);
             if (i < rows && cc < d) dot = fmaf(io_load(k + i * a.k.st + cc), z[r][c], dot);
             if (i < rows && cc < dv) xv = fmaf(io_load(v + i * a.v.st + cc), X[(int64_t)i * dv + cc], xv);
         }
@@ -474,7 +528,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         float dot = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
-            if (i < rows && tx + 16 * c < d) dot = fmaf(io_load(k + i * a.k.st + tx + 16 * c), acc[r][c], dot);
+            if (i < rows && grad_column(tx, c) < d) dot = fmaf(io_load(k + i * a.k.st + grad_column(tx, c)), acc[r][c], dot);
         dot = rowsum(dot);
         if (tx == 0) sm.wrote[i] = dot;
     }
@@ -483,7 +537,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
         const int i = ty * 4 + r;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
-            if (i < rows && tx + 16 * c < d) io_store(dk + i * a.dkt + tx + 16 * c, fmaf(-sm.b[i], z[r][c], acc[r][c]));
+            if (i < rows && grad_column(tx, c) < d) io_store(dk + i * a.dkt + grad_column(tx, c), fmaf(-sm.b[i], z[r][c], acc[r][c]));
     }
     // dg
     float pass = 0.0f;
@@ -616,15 +670,24 @@ __global__ void __launch_bounds__(kStepThreads) k_delta_step(DeltaStep a) {
 
 unsigned cdiv(int64_t a, int64_t b) { return (unsigned)((a + b - 1) / b); }
 
+template <int JD, bool REV, int COLS, int CPL>
+void rows_launch(const DeltaArgs &a, cudaStream_t s) {
+    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, COLS));
+    LUNA_LAUNCH("delta_rows", (k_delta_rows<JD, REV, COLS, CPL>), grid, COLS / CPL * 8 + kLoaders, 0, s, a);
+}
+
+// Two columns a lane where blocks of 16 columns would be more than the SMs hold at a time: the rows are read from shared
+// memory, which then bounds the pass, half as often.  (64 heads of 2048 x 128 x 128: 852 us forward, with one column
+// a lane 1190.)
 template <bool REV>
 cudaError_t rows(const DeltaArgs &a, cudaStream_t s) {
-    const dim3 grid((unsigned)(a.B * a.H), cdiv(a.dv, kRowCols));
+    const bool wide = (int64_t)a.B * a.H * cdiv(a.dv, 16) > (int64_t)(a.d > 64 ? 2 : 3) * tc_sm_count();
     if (a.d <= 32)
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<1, REV>), grid, kRowThreads, 0, s, a);
+        wide ? rows_launch<1, REV, 32, 2>(a, s) : rows_launch<1, REV, 16, 1>(a, s);
     else if (a.d <= 64)
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<2, REV>), grid, kRowThreads, 0, s, a);
+        wide ? rows_launch<2, REV, 32, 2>(a, s) : rows_launch<2, REV, 16, 1>(a, s);
     else
-        LUNA_LAUNCH("delta_rows", (k_delta_rows<4, REV>), grid, kRowThreads, 0, s, a);
+        wide ? rows_launch<4, REV, 32, 2>(a, s) : rows_launch<4, REV, 16, 1>(a, s);
     return cudaGetLastError();
 }
 

@@ -166,6 +166,9 @@ CASES = [  # B, H, Hk, n, d, dv, io, layout, lengths, state
     (1, 2, 1, 200, 127, 7, BF, "tokens", None, False),
     (3, 5, 5, 70, 72, 88, BF, "tokens", [70, 3, 64], True),
     (2, 2, 2, 400, 96, 17, F, "tokens", [400, 190], True),
+    (8, 24, 24, 70, 72, 40, F, "tokens", [70, 1, 64, 65, 0, 17, 16, 33], True),  # (more columns than the SMs hold in small blocks)
+    (10, 16, 8, 40, 20, 50, F, "heads", None, False),
+    (10, 16, 16, 37, 64, 64, F, "wide", [37, 36, 32, 31, 17, 16, 15, 2, 1, 0], True),
 ]
 
 
