@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
 constexpr int kStepThreads = 256, kStepCols = 32;
 
 template <typename IO, bool VEC>
-__global__ void __launch_bounds__(kStepThreads) k_delta_step(DeltaStep a) {
+__global__ void __launch_bounds__(kStepThreads, 6) k_delta_step(DeltaStep a) {
     __shared__ float sq[kMaxD], sk[kMaxD], sgate[3];
     __shared__ float so[2][kStepThreads / 32][kStepCols];
     const int tid = threadIdx.x;
