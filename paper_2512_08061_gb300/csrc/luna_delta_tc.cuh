@@ -166,10 +166,9 @@ __device__ __forceinline__ Scale scale_of(float most) {
     const uint32_t e = max((__float_as_uint(most) >> 23) & 255u, 14u);
     return Scale{__uint_as_float(e == 255u ? 0x7fffffffu : (254u + 12u - e) << 23), __uint_as_float((e - 12u) << 23)};
 }
+// of values that are not negative, whose bits are in their order
 __device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-    for (int w = 16; w > 0; w /= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
-    return x;
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
 }
 // the largest of all that a warp holds
 template <int N>
