@@ -25,6 +25,8 @@ enum ChainMode {
 template <int DP, int NG, int SP, ChainMode MODE>
 struct ChainShared {
     static constexpr int kWarps = NG * SP;
+    static constexpr int kLoaders = SP == 2 ? 32 : kWarps * 32;         // threads that fetch tiles: with two warps a group, one more
+    static constexpr int kThreads = kWarps * 32 + (SP == 2 ? 32 : 0);
     static constexpr int kPitch = NG * 32 + 16;  // bytes of a row of V or dO: eight rows start in eight banks
     static constexpr bool kQ = MODE != kKeep;    // Q and P are needed
     static constexpr int kPlanes = MODE == kReverse ? 2 : 1;  // of P
@@ -58,7 +60,7 @@ __device__ __forceinline__ void chain_load(typename ChainShared<DP, NG, SP, MODE
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(xv.p) + b * xv.sb + h * xv.sh + t0 * xv.st + col0;
     const uint32_t sx = smem_u32(st.x);
 #pragma unroll
-    for (int i = tid; i < C * NG * 2; i += Sh::kWarps * 32) {
+    for (int i = tid; i < C * NG * 2; i += Sh::kLoaders) {
         const int r = i / (NG * 2), p = i % (NG * 2);
         load_piece(sx + r * Sh::kPitch + p * 16, x + r * xv.st + p * 8, xv.p, r < rows ? a.dv - col0 - p * 8 : 0, VEC);
     }
@@ -117,7 +119,7 @@ __device__ __forceinline__ void plane_store(__half *tile, int rows, int r0, int 
 }
 
 template <int DP, int NG, int SP, ChainMode MODE, bool VEC>
-__global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
+__global__ void __launch_bounds__(ChainShared<DP, NG, SP, MODE>::kThreads) k_delta_chain(DeltaArgs a) {
     using Sh = ChainShared<DP, NG, SP, MODE>;
     extern __shared__ __align__(128) char raw[];
     Sh &sm = *reinterpret_cast<Sh *>(raw);
@@ -127,7 +129,8 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / a.H), h = (int)(bh % a.H), col0 = blockIdx.y * NG * 16, col = col0 + group * 16;
     const int len = head_length(a.lengths, b, a.n), chunks = (len + C - 1) / C, q2 = lane % 4 * 2;
-    const bool mine = col < a.dv;  // the warp has columns
+    const bool mine = warp < Sh::kWarps && col < a.dv;  // the warp has columns
+    const int loader = SP == 2 ? tid - Sh::kWarps * 32 : tid;  // (not negative: fetches tiles)
     __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(a.o) + b * a.ob + h * a.oh;  // (not with kKeep)
     // what is kept: by copies where a warp has whole rows of 128 bytes
     char *const mem = sm.planes[SP == 1 ? warp : 0];
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     auto place = [&](int nt, int e, int64_t &at) {
         const int c = col + lane / 4 + (e >> 1) * 8, r = d0 + nt * 8 + q2 + (e & 1);
         at = (bh * a.d + r) * a.dv + c;
-        return r < a.d && c < a.dv;
+        return mine && r < a.d && c < a.dv;
     };
 #pragma unroll
     for (int nt = 0; nt < ND; ++nt)
@@ -173,7 +176,8 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
     if (tid < 2) mbar_init(&sm.bar[tid], 1);
     fence_mbar_init();
     __syncthreads();
-    if (chunks > 0) chain_load<DP, NG, SP, MODE, VEC>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, tid);
+    if (chunks > 0 && loader >= 0)
+        chain_load<DP, NG, SP, MODE, VEC>(sm.stage[0], &sm.bar[0], a, bh, b, h, REV ? chunks - 1 : 0, len, col0, loader);
     for (int step = 0; step < chunks; ++step) {
         const int chunk = REV ? chunks - 1 - step : step, t0 = chunk * C;
         typename Sh::Stage &st = sm.stage[step & 1];
@@ -186,8 +190,8 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
             }
             break;
         }
-        if (step + 1 < chunks)
-            chain_load<DP, NG, SP, MODE, VEC>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, tid);
+        if (step + 1 < chunks && loader >= 0)
+            chain_load<DP, NG, SP, MODE, VEC>(sm.stage[(step + 1) & 1], &sm.bar[(step + 1) & 1], a, bh, b, h, REV ? chunk - 1 : chunk + 1, len, col0, loader);
         if (!mine) continue;
         const uint32_t sk = smem_u32(st.k), sq = smem_u32(st.q), sT = smem_u32(st.T), sP = smem_u32(st.P);
         const uint32_t sx = smem_u32(st.x) + ((lane >> 4) * 8 + (lane & 7)) * Sh::kPitch + group * 32 + ((lane >> 3) & 1) * 16;
@@ -509,7 +513,7 @@ __global__ void __launch_bounds__(NG * SP * 32) k_delta_chain(DeltaArgs a) {
                 if (place(nt, e, at)) last[at] = S[nt][e];
             }
     if (MODE != kKeep)  // rows behind the end, eight columns at a time
-        for (int64_t i = tid; i < (int64_t)(a.n - len) * NG * 2; i += Sh::kWarps * 32) {
+        for (int64_t i = tid; i < (int64_t)(a.n - len) * NG * 2; i += Sh::kThreads) {
             const int c = col0 + (int)(i % (NG * 2)) * 8;
             __nv_bfloat16 *to = o + (len + i / (NG * 2)) * a.ot + c;
             if (VEC && c < a.dv)
@@ -525,7 +529,7 @@ cudaError_t chain_launch(const DeltaArgs &a, cudaStream_t s) {
     cudaError_t e = cudaFuncSetAttribute(k_delta_chain<DP, NG, SP, MODE, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sh));
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)(a.B * a.H), blocks_of(a.dv, NG * 16));
-    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NG, SP, MODE, VEC>), grid, NG * SP * 32, sizeof(Sh), s, a);
+    LUNA_LAUNCH("delta_chain", (k_delta_chain<DP, NG, SP, MODE, VEC>), grid, Sh::kThreads, sizeof(Sh), s, a);
     return cudaGetLastError();
 }
 
