@@ -12,9 +12,10 @@ using namespace delta;
 // The chains.  A block has NG groups of 16 columns of one head's state, a group SP warps: with few heads two, which hold
 // half of each column and exchange their shares of K S (and Q S) once a chunk; each then has 230 products a chunk where
 // one warp has 420.  The tiles of a chunk come by asynchronous copies while the chunk before is worked on; one barrier a
-// chunk.  Bound by the chain: a chunk of 128 x 128 takes two warps 2.8 us where heads are few (32 heads of 32768 rows
-// 1.43 ms, with one warp a group 2.1 ms), eight warps 5.1 us (128 heads of 4096 rows 0.33 ms, 0.47 in reverse), of which
-// the products alone would take 3.5.
+// chunk.  With two warps a group a further warp issues those copies (the chain waits less: 1.31 to 1.18 ms below); with one,
+// all warps do: eight of them and a ninth would not have 255 registers each (0.32 to 0.36 ms).  Bound by the chain: a chunk
+// of 128 x 128 takes two warps 2.3 us where heads are few (32 heads of 32768 rows 1.18 ms, with one warp a group 2.1 ms),
+// eight warps 4.9 us (128 heads of 4096 rows 0.32 ms, 0.47 in reverse), of which the products alone would take 3.5.
 
 enum ChainMode {
     kOutputs,   // O (and the last state)

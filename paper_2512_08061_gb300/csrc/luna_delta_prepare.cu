@@ -16,7 +16,7 @@ using namespace delta;
 // with both operands in two terms.  It leaves T^T, P and in a chunk's factors: c(i, 0) 2^ek, c(C, i) 2^ek, b,
 // scale c(i, 0) 2^eq of its rows, then c(C, 0) in two terms and what T, P, K and Q were scaled down by (the last two
 // are 2^ek and 2^eq), the largest of c(C, i) 2^ek, of c(i, 0) 2^ek b, of scale c(i, 0) 2^eq, and the sums of the gates
-// in two terms.  164 us for 8192 chunks of 128 columns, 89 KB in and out each (3.9 TB/s); bound by
+// in two terms.  157 us for 8192 chunks of 128 columns, 89 KB in and out each (4.6 TB/s); bound by
 // its stages between barriers, four blocks an SM.  (With the inverse in fp32 by all threads, 13 barriers, 68 KB of shared
 // memory and tiles stored from the registers: 248 us.)
 
