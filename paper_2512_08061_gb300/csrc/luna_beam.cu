@@ -221,11 +221,12 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
             if (tid == 0) count = 0;
             bar = threshold();  // (none where fewer than K threads have a value)
         } else {
+            const int had = count;  // (before the barrier: behind it faster warps add to it)
             const int hits = __syncthreads_count(m >= floor_of(bar));
             if (hits == 0) continue;
-            if (count + hits * PER > POOL) {
+            if (had + hits * PER > POOL) {
                 RowKey k;
-                best_of(count, [&](int i) { return pool[i]; }, k, list);
+                best_of(had, [&](int i) { return pool[i]; }, k, list);
                 const RowKey kth = list[a.K - 1];
                 if (tid < a.K) pool[tid] = k;
                 __syncthreads();

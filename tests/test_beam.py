@@ -112,6 +112,23 @@ def test_select_ordered_rows(L, order, K):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("io", [F, BF])
+def test_select_full_pools_repeat(L, io):
+    """Blocks whose room for candidates runs full again and again, at different pieces, give the same every time: whether
+    it is full has to be decided alike by all warps of a block."""
+    B, K, V = 32, 8, 60000
+    steps = torch.linspace(0.2, 4.0, B * K, device="cuda")[:, None] * torch.arange(V, device="cuda", dtype=F) * 1e-3
+    logits = (steps + torch.rand(B * K, V, device="cuda", generator=torch.Generator("cuda").manual_seed(1))).to(io)
+    scores = -torch.arange(B * K, device="cuda", dtype=F).view(B, K) * 0.1
+    p = L.Beam(B, K, V, io=io)
+    first = p.select(logits, scores)
+    for _ in range(40):
+        again = p.select(logits, scores)
+        assert all(torch.equal(first[name], again[name]) for name in first)
+    check(L, logits, scores, None, -1, K)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
 def test_select_equal_values(L, io):
     """Equal scores go by the lower beam, then the lower token; 0 and -0 are equal."""
     logits = torch.zeros((6, 500), device="cuda", dtype=io)
