@@ -455,7 +455,7 @@ luna_status luna_delta_step(const luna_delta_desc *dd, const void *log_decay, co
  *
  * luna_beam_reorder lets the states in a pool follow their beams.  The pool has
  * nslots slots of slot_bytes each; slots (int32, B x K) says where each old
- * beam's state is, and new_slots (another array) receives where the new beams'
+ * beam's state is, and new_slots (another array than these) receives where the new beams'
  * states are: the first child of a beam keeps its slot, further children get
  * copies in the slots of beams without a child, in order.  No two beams may share
  * a slot.  Slots outside [0, nslots) are neither read nor written; a parent

@@ -482,7 +482,7 @@ luna_status luna_beam_reorder(const luna_beam_desc *bd, const int32_t *parents, 
     if (st != LUNA_OK) return st;
     if (nslots < 0 || slot_bytes > (size_t(1) << 40)) return LUNA_ERR_INVALID_ARG;
     if (bd->B == 0) return LUNA_OK;
-    if (!parents || !slots || !new_slots || new_slots == slots || (slot_bytes > 0 && nslots > 0 && !pool)) return LUNA_ERR_INVALID_ARG;
+    if (!parents || !slots || !new_slots || new_slots == slots || new_slots == parents || (slot_bytes > 0 && nslots > 0 && !pool)) return LUNA_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const uintptr_t at = reinterpret_cast<uintptr_t>(pool) | slot_bytes;
     const int vec = at % 16 == 0 ? 16 : at % 4 == 0 ? 4 : 1;

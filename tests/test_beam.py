@@ -296,7 +296,7 @@ def test_refusals(L):
     bd = L.beam_desc(**dict(ok, end=-1))
     assert sel(bd, done=256) == 1 and sel(bd, ended=256) == 1
     bd = L.beam_desc(2, 4)
-    assert order(bd, parents=0) == 1 and order(bd, slots=0) == 1 and order(bd, new=0) == 1 and order(bd, new=512) == 1
+    assert order(bd, parents=0) == 1 and order(bd, slots=0) == 1 and order(bd, new=0) == 1 and order(bd, new=512) == 1 and order(bd, new=256) == 1
     assert order(bd, pool=0) == 1 and order(bd, nslots=-1) == 1 and order(bd, nbytes=(1 << 40) + 1) == 1
     none = L.beam_desc(0, 4, 100)
     assert sel(none, logits=0, scores=0, out=0, ws=0, nbytes=0) == 0 and order(none, parents=0, slots=0, new=0) == 0
