@@ -455,10 +455,10 @@ luna_status luna_delta_step(const luna_delta_desc *dd, const void *log_decay, co
  *
  * luna_beam_reorder lets the states in a pool follow their beams.  The pool has
  * nslots slots of slot_bytes each; slots (int32, B x K) says where each old
- * beam's state is, and new_slots (another array than these) receives where the new beams'
- * states are: the first child of a beam keeps its slot, further children get
- * copies in the slots of beams without a child, in order.  No two beams may share
- * a slot.  Slots outside [0, nslots) are neither read nor written; a parent
+ * beam's state is, and new_slots (another array than these) receives where the
+ * new beams' states are: the first child of a beam keeps its slot, further
+ * children get copies in the slots of beams without a child, in order.  No two
+ * beams may share a slot.  Slots outside [0, nslots) are neither read nor written; a parent
  * outside [0, K) stands for none (the beam takes a free slot as it is).  Several
  * pools are reordered by one call each with the same slots; pool may be NULL with
  * slot_bytes = 0 (new_slots alone).
