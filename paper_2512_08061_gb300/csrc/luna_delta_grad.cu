@@ -193,56 +193,50 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
             }
         }
     };
-    // acc += F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q
-    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, uint32_t sign) {
+    // acc += by F M over the 64 rows of the chunk: F from P or W (trans: its transpose), M a tile of K or Q.  Summed by itself
+    // and scaled as it is added, in fp32: `by` may be any power of two (of a tile of nothing or of very little), and
+    // its inverse is never taken.
+    auto over_rows = [&](Acc &acc, uint32_t from, bool trans, uint32_t tile, float by) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-            if (trans ? kt * 16 < r0 : kt * 16 > r0 + 16) continue;
-            Frag fl[2];
+        for (int np = 0; np < NT / 2; ++np) {
+            float sum[2][2][4];
+            zero(sum[0]);
+            zero(sum[1]);
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
-                if (trans)
-                    left_k(fl[mt], from, C, kt * 16, r0 + mt * 16, lane);
-                else
-                    left_m(fl[mt], from, C, r0 + mt * 16, kt * 16, lane);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) fl[mt][i] ^= sign;
-            }
-#pragma unroll
-            for (int np = 0; np < NT / 2; ++np) {
+            for (int kt = 0; kt < 4; ++kt) {
+                if (trans ? kt * 16 < r0 : kt * 16 > r0 + 16) continue;
                 Frag f;
                 right_k(f, tile, C, kt * 16, c0 + np * 16, lane);
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
-                    mma(acc[mt][2 * np], fl[mt], f[0], f[1]);
-                    mma(acc[mt][2 * np + 1], fl[mt], f[2], f[3]);
+                    Frag fl;
+                    if (trans)
+                        left_k(fl, from, C, kt * 16, r0 + mt * 16, lane);
+                    else
+                        left_m(fl, from, C, r0 + mt * 16, kt * 16, lane);
+                    mma(sum[mt][0], fl, f[0], f[1]);
+                    mma(sum[mt][1], fl, f[2], f[3]);
                 }
             }
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[mt][2 * np + i][e] = fmaf(by, sum[mt][i][e], acc[mt][2 * np + i][e]);
         }
     };
     // acc *= by row_factor (of every row)
-    auto times_rows = [&](Acc &acc, const float *row_factor, const float *more, float by) {
+    auto times_rows = [&](Acc &acc, const float *row_factor, float by) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             const int ra = r0 + mt * 16 + lane / 4;
-            float fa = by * row_factor[ra], fb = by * row_factor[ra + 8];
-            if (more) {
-                fa *= more[ra];
-                fb *= more[ra + 8];
-            }
+            const float fa = by * row_factor[ra], fb = by * row_factor[ra + 8];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= e & 2 ? fb : fa;
         }
-    };
-    auto times = [&](Acc &acc, float by) {
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[mt][nt][e] *= by;
     };
     // sums of the rows times those of K (whose left operands lie as the accumulators do)
     auto dot_k = [&](const Acc &acc, int which) {
@@ -378,9 +372,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         mp = fmaxf(mp, sm.most[0][i]);
         mw = fmaxf(mw, sm.most[1][i]);
     }
-    // P Q and W K are scaled down alike, so that they add up in dK
-    const float by = fmaxf(fmaxf(scale_of(mp).back * back_q, scale_of(mw).back * back_k), 0x1p-100f), inv = inverse2(by);
-    const float to_p = back_q * inv, to_w = back_k * inv, by_pk = by * back_k * inverse2(back_q);
+    // P and W each by its own largest value, whatever Q, K and each other are
+    const Scale ps = scale_of(mp), ws = scale_of(mw);
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -388,20 +381,19 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
                 const uint32_t to = tile_at(0, C, r0 + mt * 16 + lane / 4 + e * 4, quarter * 2 + nt) + q2 * 2;
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(to_p * p[mt][nt][e], to_p * p[mt][nt][e + 1])) : "memory");
-                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(to_w * w[mt][nt][e], to_w * w[mt][nt][e + 1])) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sP + to), "r"(pack(ps.by * p[mt][nt][e], ps.by * p[mt][nt][e + 1])) : "memory");
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(ws.by * w[mt][nt][e], ws.by * w[mt][nt][e + 1])) : "memory");
             }
-    times_rows(acc, sm.left, nullptr, sm.all[of_half + 2] * inv);
+    times_rows(acc, sm.left, sm.all[of_half + 2]);
     __syncthreads();
-    over_rows(acc, sW, true, sk, 0x80008000u);
+    over_rows(acc, sW, true, sk, -ws.back * back_k);
 
     // dQ and Z from S
     here = mbar_wait_long(&sm.bar[2], 0);
     clear(z);
     if (here) over_columns(z, sgo, of_half);
-    times_rows(z, sm.past, nullptr, a.scale * sm.all[of_half] * inverse2(by_pk));
-    over_rows(z, sP, false, sk, 0);
-    times(z, by_pk);
+    times_rows(z, sm.past, a.scale * sm.all[of_half]);
+    over_rows(z, sP, false, sk, ps.back * back_k);
     {  // <S, R> before the chunk: of every 16 columns the diagonal of S^T R, R as it lies in memory (in both the summed
        // values lie in the same, permuted order: a lane's 16 bytes of a row are those of two products)
         float sum = 0.0f;
@@ -465,22 +457,21 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         return;
     }
     if (tid == 0) load_state(a.Qp + kat * C * DP, sizeof(sm.k), 3);
-    times_rows(z, sm.past, nullptr, sm.all[of_half + 1]);
+    times_rows(z, sm.past, sm.all[of_half + 1]);
     dot_k(z, 1);
-    times_rows(z, gate_b, nullptr, inv);
-    over_rows(z, sW, false, sk, 0);
-    times(z, by);
+    times_rows(z, gate_b, 1.0f);
+    over_rows(z, sW, false, sk, ws.back * back_k);
     dot_k(z, 5);
 
     // dK
     here = mbar_wait_long(&sm.bar[3], 0);
-    if (here) over_rows(acc, sP, true, ss, 0);
+    if (here) over_rows(acc, sP, true, ss, ps.back * back_q);
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[mt][nt][e] = fmaf(by, acc[mt][nt][e], -z[mt][nt][e]);
+            for (int e = 0; e < 4; ++e) acc[mt][nt][e] -= z[mt][nt][e];
     dot_k(acc, 2);
     store_rows(acc, dk, a.dkt);
     if (__syncthreads_or(!here)) {
