@@ -127,8 +127,14 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         if (kt == 0) sm.all[product] = most;
         if (kt < groups) sm.steps[product][kt] = __float2half2_rn(most > 0.0f ? scale * inverse2(most) : 0.0f);
     } else if (tid < 64 + C) {
-        sm.past[tid - 64] = sm.rows[tid - 64] * inverse2(back_k);
-        sm.left[tid - 64] = sm.rows[C + tid - 64] * inverse2(back_k);
+        // from the sums of the gates: the chains' factors have K's scale in them, and none of their bits where K is 0
+        const int t = tid - 64;
+        auto factor = [](float h, float l) {
+            const float e = expf(h);
+            return fmaf(e, l, e);
+        };
+        sm.past[t] = factor(hi[t], lo[t]);
+        sm.left[t] = expf((hi[C - 1] - hi[t]) + (lo[C - 1] - lo[t]));
     }
     {
         const int i = tid % C;

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_delta import BF, F, L, f64, inputs, recurrence, tol  # noqa: F401  (L: the fixture)
+from test_delta import BF, F, L, TOL, f64, inputs, recurrence, tol  # noqa: F401  (L: the fixture)
 
 
 def by(parts, got, want):
@@ -60,3 +60,19 @@ def test_chunks_of_nothing_or_little(L, io, d, which, size, where, state):
     for name, t in got.items():
         parts = [np.s_[:]] if name in ("S1", "dS0") else chunks(n)
         assert by(parts, t, ref[name]) < tol(name, t.dtype), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
+def test_zero_keys_under_gates(L, io):
+    """Where a chunk's keys are zero and it has no output gradients, a key's gradient is that of the state behind the chunk
+    times what the gates leave of the row: row by row, down to exp(-16)."""
+    H, n, d = 2, 192, 64
+    x = list(inputs(1, H, H, n, d, d, io, "tokens", 37, True))
+    for t in (x[1], x[3]):
+        t[:, :, 64:128] = 0
+    x[4][:, :, 64:128] = -0.25
+    got, ref = gradients(L, x, H)
+    rows = [np.s_[:, h, t:t + 1] for h in range(H) for t in range(64, 128)]
+    assert by(rows, got["dK"], ref["dK"]) < TOL[io]
+    assert by(rows, got["dQ"], 0 * ref["dQ"]) == 0.0
