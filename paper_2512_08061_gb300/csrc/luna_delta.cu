@@ -331,8 +331,9 @@ constexpr int kGradThreads = 256, kGradK = 16;
 struct GradShared {
     alignas(16) float A[kGradK][kDeltaRows + 4], B[kGradK][kMaxD + 4];
     float P[kDeltaRows][kDeltaRows + 1], W[kDeltaRows][kDeltaRows + 1];
+    float reads[kDeltaRows][kDeltaRows + 1];  // what row i reads of row j < i; then from row i to the chunk's end
     float hi[kDeltaRows], lo[kDeltaRows], b[kDeltaRows], past[kDeltaRows], left[kDeltaRows];
-    float read[kDeltaRows], wrote[kDeltaRows], total[kGradThreads / 32];
+    float read[kDeltaRows], wrote[kDeltaRows], crossed[kDeltaRows], total[kGradThreads / 32];
 };
 
 // A thread's c-th column
@@ -413,7 +414,6 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     if (rows == 0) return;
     const int64_t E = (int64_t)a.d * a.dv;
     const float *S = a.before + (bh * (a.m + 1) + chunk) * E, *R = a.after + (bh * (a.m + 1) + chunk + 1) * E;
-    const float *R0 = a.after + (bh * (a.m + 1) + chunk) * E;  // before the chunk
     const float *U = a.U + (bh * a.n + t0) * a.dv, *X = a.X + (bh * a.n + t0) * a.dv;
     const int d = a.d, dv = a.dv;
 
@@ -461,6 +461,25 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
                 const int i = ty * 4 + r, j = grad_column(tx, c);
                 sm.W[i][j] = j < i ? gap(i, j) * acc[r][c] : 0.0f;
             }
+        // P_ij q_i . k_j - b_i W_ij k_i . k_j  (a thread's values of P, W and these are its own)
+        zero(acc);
+        grad_product<true>(sm, acc, d, [&](int r, int kk) { return at(q, a.q.st, r, kk, d); }, [&](int kk, int c) { return at(k, a.k.st, c, kk, d); });
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = ty * 4 + r, j = grad_column(tx, c);
+                sm.reads[i][j] = j < i ? sm.P[i][j] * acc[r][c] : 0.0f;
+            }
+        zero(acc);
+        grad_product<true>(sm, acc, d, [&](int r, int kk) { return at(k, a.k.st, r, kk, d); }, [&](int kk, int c) { return at(k, a.k.st, c, kk, d); });
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = ty * 4 + r, j = grad_column(tx, c);
+                if (j < i) sm.reads[i][j] = fmaf(-sm.b[i] * sm.W[i][j], acc[r][c], sm.reads[i][j]);
+            }
     }
     float acc[4][NC], z[4][NC];
     auto fS = [&](int kk, int c) { return c < d && kk < dv ? S[(int64_t)c * dv + kk] : 0.0f; };
@@ -472,22 +491,28 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[r][c] *= a.scale * sm.past[ty * 4 + r];
-    grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[r][kk]; }, fK);
+    auto dot = [&](const float *x, int64_t st, const float (&with)[4][NC], int r) {  // of row i = ty * 4 + r
+        const int i = ty * 4 + r;
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            if (i < rows && grad_column(tx, c) < d) sum = fmaf(io_load(x + i * st + grad_column(tx, c)), with[r][c], sum);
+        return rowsum(sum);
+    };
+    auto store = [&](float *to, int64_t st, const float (&from)[4][NC]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (ty * 4 + r < rows && grad_column(tx, c) < d) io_store(to + (ty * 4 + r) * st + grad_column(tx, c), from[r][c]);
+    };
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int i = ty * 4 + r;
-        float dot = 0.0f;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int cc = grad_column(tx, c);
-            if (i < rows && cc < d) {
-                dot = fmaf(io_load(q + i * a.q.st + cc), acc[r][c], dot);
-                io_store(dq + i * a.dqt + cc, acc[r][c]);
-            }
-        }
-        dot = rowsum(dot);
-        if (tx == 0) sm.read[i] = dot;
+        const float of_s = dot(q, a.q.st, acc, r);
+        if (tx == 0) sm.read[ty * 4 + r] = of_s;
     }
+    grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[r][kk]; }, fK);
+    store(dq, a.dqt, acc);
     // Z, and with it db
     zero(z);
     grad_product<true>(sm, z, dv, [&](int r, int kk) { return in(X, r, kk); }, fS);
@@ -495,23 +520,24 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < NC; ++c) z[r][c] *= sm.past[ty * 4 + r];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float of_s = dot(k, a.k.st, z, r);
+        if (tx == 0) sm.read[ty * 4 + r] -= sm.b[ty * 4 + r] * of_s;
+    }
     grad_product<false>(sm, z, C, [&](int r, int kk) { return sm.W[r][kk]; }, fK);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int i = ty * 4 + r;
-        float dot = 0.0f, xv = 0.0f;
+        float xv = 0.0f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int cc = grad_column(tx, c);
-            if (i < rows && cc < d) dot = fmaf(io_load(k + i * a.k.st + cc), z[r][c], dot);
             if (i < rows && cc < dv) xv = fmaf(io_load(v + i * a.v.st + cc), X[(int64_t)i * dv + cc], xv);
         }
-        dot = rowsum(dot);
         xv = rowsum(xv);
-        if (tx == 0 && i < rows) {
-            io_store(db + i * a.db.st, xv - dot);
-            sm.read[i] -= sm.b[i] * dot;
-        }
+        const float kz = dot(k, a.k.st, z, r);
+        if (tx == 0 && i < rows) io_store(db + i * a.db.st, xv - kz);
     }
     // dK
     zero(acc);
@@ -520,36 +546,39 @@ __global__ void __launch_bounds__(kGradThreads) k_delta_grad(DeltaArgs a) {
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[r][c] *= sm.left[ty * 4 + r];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float by_r = dot(k, a.k.st, acc, r);
+        if (tx == 0) sm.wrote[ty * 4 + r] = by_r;
+    }
     grad_product<false>(sm, acc, C, [&](int r, int kk) { return sm.P[kk][r]; }, fQ);
     grad_product<false>(sm, acc, C, [&](int r, int kk) { return -sm.b[kk] * sm.W[kk][r]; }, fK);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = ty * 4 + r;
-        float dot = 0.0f;
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
-            if (i < rows && grad_column(tx, c) < d) dot = fmaf(io_load(k + i * a.k.st + grad_column(tx, c)), acc[r][c], dot);
-        dot = rowsum(dot);
-        if (tx == 0) sm.wrote[i] = dot;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = ty * 4 + r;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-            if (i < rows && grad_column(tx, c) < d) io_store(dk + i * a.dkt + grad_column(tx, c), fmaf(-sm.b[i], z[r][c], acc[r][c]));
-    }
+        for (int c = 0; c < NC; ++c) acc[r][c] = fmaf(-sm.b[ty * 4 + r], z[r][c], acc[r][c]);
+    store(dk, a.dkt, acc);
     // dg
+    if (tid < C) {
+        float sum = 0.0f;
+        for (int i = C - 1; i > tid; --i) sm.reads[i][tid] = sum += sm.reads[i][tid];
+    }
     float pass = 0.0f;
-    for (int64_t i = tid; i < E; i += kGradThreads) pass = fmaf(S[i], R0[i], pass);
+    for (int64_t i = tid; i < E; i += kGradThreads) pass = fmaf(S[i], R[i], pass);
 #pragma unroll
     for (int w = 1; w < 32; w *= 2) pass += __shfl_xor_sync(0xffffffffu, pass, w);
     if (tid % 32 == 0) sm.total[tid / 32] = pass;
     __syncthreads();
+    if (tid < C) {
+        float sum = 0.0f;
+        for (int j = 0; j < tid; ++j) sum += sm.reads[tid][j];
+        sm.crossed[tid] = sum;
+    }
+    __syncthreads();
     if (tid < 32) {
         float all = 0.0f;
         for (int w = 0; w < kGradThreads / 32; ++w) all += sm.total[w];
-        delta_gate_grads(all, sm.read, sm.wrote, rows, tid, [&](int t, float x) {
+        delta_gate_grads(sm.past[C - 1] * all, sm.read, sm.wrote, sm.crossed, rows, tid, [&](int t, float x) {
             io_store(dg + t * a.dg.st, expf(gate_at<float>(a.g, b, h, t0 + t)) == 0.0f ? 0.0f : x);
         });
     }

@@ -17,8 +17,10 @@
 //     dQ_i = scale c(i, 0) S dO_i + sum_j P_ij k_j
 //     dK_j = c(C, j) R u_j + sum_i P_ij q_i - sum_i W_ij k_i  -  b_j c(j, 0) S x_j - sum_{l < j} W_jl k_l
 //
-// and dg is a sum over all pairs of a row at or behind t that reads and a row before t (or S) that was written:
-// each of the parts q_i . dQ_i, k_j . dK_j adds to the rows up to i, or takes from those up to j.
+// and dg is a sum over all pairs of a row at or behind t (or R) that reads and a row before t (or S) that was written:
+//
+//     dg_t = c(C, 0) <S, R> + sum_{i >= t} (scale c(i, 0) q_i . S dO_i - b_i c(i, 0) k_i . S x_i) + sum_{j < t} c(C, j) k_j . R u_j
+//            + sum_{j < t <= i} (P_ij q_i . k_j - W_ij k_i . k_j)
 #pragma once
 
 #include <cuda_fp16.h>
@@ -128,27 +130,34 @@ __device__ __forceinline__ void delta_gate_sums(int lane, F gate, float *hi, flo
     }
 }
 
-// dg of a chunk's rows, by one warp: `base` = <S, R> of the states before the chunk is that of its first row (and more:
-// what R takes from all rows behind), read_i what row i's reads give to the gates up to i, wrote_j what the reads of row
-// j give, which do not cross the gates up to j; each row's dg is the one's before it less read - wrote of that row.
+// dg of a chunk's rows, by one warp.  A gate takes part in all that is read at or behind it of what was written before it:
+// by R of S (`ends` = c(C, 0) <S, R>), by rows at or behind it of S (read), by R of rows before it (wrote), by the former of the
+// latter (crossed).  Each of these has the gate in its factor, so that a strong gate's gradient is a sum of small terms; as
+// the difference of what is read up to a row and up to the next it was off by 1e-7 of the large ones (9 % at a gate of -12).
 template <typename F>
-__device__ __forceinline__ void delta_gate_grads(float base, const float *read, const float *wrote, int rows, int lane, F store) {
-    float x[2], head = 0.0f;
+__device__ __forceinline__ void delta_gate_grads(float ends, const float *read, const float *wrote, const float *crossed,
+                                                 int rows, int lane, F store) {
+    float r[2], w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int t = 2 * lane + i;
-        x[i] = t < rows ? read[t] - wrote[t] : 0.0f;
-        head += x[i];
+        r[i] = t < rows ? read[t] : 0.0f;
+        w[i] = t < rows ? wrote[t] : 0.0f;
     }
+    float behind = r[0] + r[1], before = w[0] + w[1];
 #pragma unroll
-    for (int w = 1; w < 32; w *= 2) {
-        const float up = __shfl_up_sync(0xffffffffu, head, w);
-        if (lane >= w) head += up;
+    for (int m = 1; m < 32; m *= 2) {
+        const float x = __shfl_down_sync(0xffffffffu, behind, m), y = __shfl_up_sync(0xffffffffu, before, m);
+        if (lane + m < 32) behind += x;
+        if (lane >= m) before += y;
     }
-    head = __shfl_up_sync(0xffffffffu, head, 1);  // the rows before this lane's
-    base -= lane > 0 ? head : 0.0f;
-    if (2 * lane < rows) store(2 * lane, base);
-    if (2 * lane + 1 < rows) store(2 * lane + 1, base - x[0]);
+    behind = __shfl_down_sync(0xffffffffu, behind, 1);  // of the other lanes' rows
+    before = __shfl_up_sync(0xffffffffu, before, 1);
+    if (lane == 31) behind = 0.0f;
+    if (lane == 0) before = 0.0f;
+    behind += r[1];
+    if (2 * lane < rows) store(2 * lane, (ends + crossed[2 * lane]) + ((behind + r[0]) + before));
+    if (2 * lane + 1 < rows) store(2 * lane + 1, (ends + crossed[2 * lane + 1]) + (behind + (before + w[0])));
 }
 
 cudaError_t launch_delta_rows(const DeltaArgs &a, bool reverse, cudaStream_t s);  // fp32

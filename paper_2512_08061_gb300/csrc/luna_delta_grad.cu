@@ -25,8 +25,10 @@ struct GradShared {
     float past[C], left[C];
     __half2 steps[8][DVT / 16];  // of the products over columns: 16 columns' scale over the largest, that
     float all[8], total[kGradThreads / 32];
-    float sums[6][kParts][C];  // of a row's quarters: q . dQ, k . Z without the rows' part, k . (dK), W . K K^T, x . v, b k . Z
-    float most[2][kGradThreads / 32], read[C], wrote[C];
+    // of a row's quarters: q . dQ, k . Z and k . dK, all of the states' parts alone, W . K K^T, x . v; and what its reads of the rows of an
+    // earlier 16 (the quarter) add up to, of its own 16 what crosses its gate; of a row as written, what each later 16 reads
+    float sums[6][kParts][C], written[kParts][C];
+    float most[2][kGradThreads / 32], read[C], wrote[C], crossed[C];
 };
 
 template <int DP, int DVT, typename OUT, bool VEC>
@@ -85,7 +87,6 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
         };
         ask(a.Sp + at * dvp * DP, of_state);
-        ask(a.Rp + slot * dvp * DP, of_state);
         ask(a.Qp + kat * C * DP, sizeof(sm.k));
     }
     // x . v: a thread a row and a quarter of the columns, while the tiles come
@@ -296,12 +297,13 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     float p[2][2][4], w[2][2][4];
     float mp = 0.0f, mw = 0.0f;
     {
-        float kk[2][2][4];
+        float kk[2][2][4], qk[2][2][4];
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             zero(p[mt]);
             zero(w[mt]);
             zero(kk[mt]);
+            zero(qk[mt]);
         }
         if (n0 <= r0 + 16) {
 #pragma unroll 2
@@ -331,6 +333,26 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                     mma(kk[mt][1], fk, f[2], f[3]);
                 }
             }
+            // Q as it lies in memory (in both the summed values lie in the same, permuted order: a lane's 16 bytes of a row
+            // are those of two products)
+            const char *q = reinterpret_cast<const char *>(a.Qp + kat * C * DP);
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                const int piece = i * 4 + lane % 4, rk = n0 + lane / 4;
+                const uint4 k_0 = *reinterpret_cast<const uint4 *>(sm.k[0] + tile_at(0, C, rk, piece));
+                const uint4 k_1 = *reinterpret_cast<const uint4 *>(sm.k[0] + tile_at(0, C, rk + 8, piece));
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    const int rq = r0 + mt * 16 + lane / 4;
+                    const uint4 q0 = __ldg(reinterpret_cast<const uint4 *>(q + tile_at(0, C, rq, piece)));
+                    const uint4 q1 = __ldg(reinterpret_cast<const uint4 *>(q + tile_at(0, C, rq + 8, piece)));
+                    const Frag f = {q0.x, q1.x, q0.y, q1.y}, g = {q0.z, q1.z, q0.w, q1.w};
+                    mma(qk[mt][0], f, k_0.x, k_0.y);
+                    mma(qk[mt][0], g, k_0.z, k_0.w);
+                    mma(qk[mt][1], f, k_1.x, k_1.y);
+                    mma(qk[mt][1], g, k_1.z, k_1.w);
+                }
+            }
         }
         const float by_p = a.scale * sm.all[0], by_w = sm.all[1];
 #pragma unroll
@@ -349,8 +371,44 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                     ww *= gate_b[i];
                     mp = fmaxf(mp, fabsf(pp));
                     mw = fmaxf(mw, fabsf(ww));
+                    // what row i reads of row j, which crosses the gates between them
+                    float &read = qk[mt][nt][e];
+                    read = j < i ? pp * (read * back_q * back_k) - ww * (kk[mt][nt][e] * back_k * back_k) : 0.0f;
                 }
             row_sums(dot[0], dot[1], mt, 3);
+            const int I = r0 / 16 + mt;  // (of the 16 rows; those of the columns are `quarter`)
+            if (I > quarter) {
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = qk[mt][nt][e] + qk[mt][nt][2 + e];
+#pragma unroll
+                        for (int m = 4; m < 32; m *= 2) x += __shfl_xor_sync(0xffffffffu, x, m);
+                        if (lane < 4) sm.written[I][n0 + nt * 8 + q2 + e] = x;
+                    }
+            } else if (I == quarter) {  // columns' sums from their end to each row; of them those before the row cross its gate
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float &x = qk[mt][nt][e], &y = qk[mt][nt][2 + e];  // rows lane / 4 and 8 more
+#pragma unroll
+                        for (int m = 4; m < 32; m *= 2) {
+                            const float x_ = __shfl_down_sync(0xffffffffu, x, m), y_ = __shfl_down_sync(0xffffffffu, y, m);
+                            if (lane + m < 32) {
+                                x += x_;
+                                y += y_;
+                            }
+                        }
+                        x += __shfl_sync(0xffffffffu, y, lane % 4);
+                        const int j = nt * 8 + q2 + e, i = lane / 4;
+                        x = j < i ? x : 0.0f;
+                        y = j < i + 8 ? y : 0.0f;
+                    }
+            }
+            row_sums((qk[mt][0][0] + qk[mt][0][1]) + (qk[mt][1][0] + qk[mt][1][1]),
+                     (qk[mt][0][2] + qk[mt][0][3]) + (qk[mt][1][2] + qk[mt][1][3]), mt, 5);
         }
         mp = warp_max(mp);
         mw = warp_max(mw);
@@ -391,6 +449,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                 asm volatile("st.shared.b32 [%0], %1;" ::"r"(sW + to), "r"(pack(ws.by * w[mt][nt][e], ws.by * w[mt][nt][e + 1])) : "memory");
             }
     times_rows(acc, sm.left, sm.all[of_half + 2]);
+    dot_k(acc, 2);
     __syncthreads();
     over_rows(acc, sW, true, sk, -ws.back * back_k);
 
@@ -399,12 +458,29 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     clear(z);
     if (here) over_columns(z, sgo, of_half);
     times_rows(z, sm.past, a.scale * sm.all[of_half]);
+    {  // q . dQ of the state's part, with Q as it came
+        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            float dot[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + mt * 16 + lane / 4 + i * 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, VEC);
+                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
+                }
+            }
+            row_sums(dot[0], dot[1], mt, 0);
+        }
+    }
     over_rows(z, sP, false, sk, ps.back * back_k);
-    {  // <S, R> before the chunk: of every 16 columns the diagonal of S^T R, R as it lies in memory (in both the summed
-       // values lie in the same, permuted order: a lane's 16 bytes of a row are those of two products)
+    store_rows(z, dq, a.dqt);
+    {  // <S, R> of the states at the chunk's two ends: of every 16 columns the diagonal of S^T R, R as Q above
         float sum = 0.0f;
         if (here && warp < groups) {
-            const char *r = reinterpret_cast<const char *>(a.Rp + slot * dvp * DP);
+            const char *r = reinterpret_cast<const char *>(a.Rp + (slot + 1) * dvp * DP);
             const int ra = warp * 16 + lane / 4;
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
@@ -422,36 +498,18 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
                     mma(c[1], f, r1.x, r1.y);
                     mma(c[1], g, r1.z, r1.w);
                 }
-                const float *scale = sm.scales[warp];
+                const float *scale = sm.scales[warp], *scale_r = sm.scales[groups + warp];
                 float diag = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     if (lane / 4 == q2 + e) diag += c[0][e] + c[1][2 + e];
-                sum = fmaf(scale[side] * scale[2 + side], diag, sum);
+                sum = fmaf(scale[side] * scale_r[2 + side], diag, sum);
             }
         }
         sum = sum + __shfl_xor_sync(0xffffffffu, sum, 16);
 #pragma unroll
         for (int w = 8; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
         if (lane == 0) sm.total[warp] = sum;
-    }
-    store_rows(z, dq, a.dqt);
-    {  // q . dQ, with Q as it came
-        const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q.p) + b * a.q.sb + hk * a.q.sh + t0 * a.q.st + c0 + q2;
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            float dot[2] = {0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = r0 + mt * 16 + lane / 4 + i * 8;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float2 f = load_pair(q + r * a.q.st + nt * 8, r < rows ? a.d - (c0 + nt * 8 + q2) : 0, VEC);
-                    dot[i] = fmaf(f.x, z[mt][nt][2 * i], fmaf(f.y, z[mt][nt][2 * i + 1], dot[i]));
-                }
-            }
-            row_sums(dot[0], dot[1], mt, 0);
-        }
     }
     clear(z);
     if (here) over_columns(z, sx, of_half + 1);
@@ -467,7 +525,6 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
     dot_k(z, 1);
     times_rows(z, gate_b, 1.0f);
     over_rows(z, sW, false, sk, ws.back * back_k);
-    dot_k(z, 5);
 
     // dK
     here = mbar_wait_long(&sm.bar[3], 0);
@@ -478,7 +535,6 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[mt][nt][e] -= z[mt][nt][e];
-    dot_k(acc, 2);
     store_rows(acc, dk, a.dkt);
     if (__syncthreads_or(!here)) {
         if (tid == 0) {
@@ -491,16 +547,32 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_delta_grad_tc(DeltaArgs a) 
         auto sum = [&](int which) {
             return (sm.sums[which][0][tid] + sm.sums[which][1][tid]) + (sm.sums[which][2][tid] + sm.sums[which][3][tid]);
         };
-        const float bz = sum(5);
         io_store(db + tid * a.db.st, sum(4) - sum(1) - back_k * back_k * sum(3));
-        sm.read[tid] = sum(0) - bz;
-        sm.wrote[tid] = sum(2) + bz;
+        sm.read[tid] = sum(0) - gate_b[tid] * sum(1);
+        sm.wrote[tid] = sum(2);
+    }
+    if (tid >= C && tid < 2 * C) {  // what crosses gate t of its 16: reads of rows at or behind it of rows before it
+        const int t = tid - C, T = t / 16, c = t % 16;
+        const float(*of)[C] = sm.sums[5];
+        float read = 0.0f, wrote = 0.0f;  // in its own 16, of and by the others
+        for (int J = 0; J < T; ++J) read += of[J][t];
+        for (int I = T + 1; I < 4; ++I) wrote += sm.written[I][t];
+        float around = T == 1 ? of[0][32 + c] + of[0][48 + c] : T == 2 ? of[0][48 + c] + of[1][48 + c] : 0.0f;
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) {
+            const float r = __shfl_down_sync(0xffffffffu, read, m, 16), w = __shfl_up_sync(0xffffffffu, wrote, m, 16);
+            if (c + m < 16) read += r;
+            if (c >= m) wrote += w;
+            around += __shfl_xor_sync(0xffffffffu, around, m, 16);
+        }
+        wrote = __shfl_up_sync(0xffffffffu, wrote, 1, 16);
+        sm.crossed[t] = (of[T][t] + read) + (around + (c > 0 ? wrote : 0.0f));
     }
     __syncthreads();
     if (warp == 0) {
         float base = 0.0f;
         for (int w = 0; w < kGradThreads / 32; ++w) base += sm.total[w];
-        delta_gate_grads(base, sm.read, sm.wrote, rows, lane, [&](int t, float x) {
+        delta_gate_grads(sm.rows[4 * C] * base, sm.read, sm.wrote, sm.crossed, rows, lane, [&](int t, float x) {
             const float g = t > 0 ? (hi[t] - hi[t - 1]) + (lo[t] - lo[t - 1]) : hi[0];
             io_store(dg + t * a.dg.st, expf(g) == 0.0f ? 0.0f : x);
         });

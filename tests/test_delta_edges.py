@@ -1,13 +1,13 @@
-"""The gated delta rule where its parts are of very different size: chunks without queries, keys or gradients.
+"""The gated delta rule where its parts are of very different size: chunks without queries, keys or gradients, strong gates.
 
-Tolerances are those of test_delta.py, taken chunk by chunk instead of over whole tensors: they come
+Tolerances are those of test_delta.py, taken chunk by chunk or head by head instead of over whole tensors: they come
 from the rounding of single values and of the operands of a product, which is the same for any 64 rows.
 """
 import numpy as np
 import pytest
 import torch
 
-from test_delta import BF, F, L, TOL, f64, inputs, recurrence, tol  # noqa: F401  (L: the fixture)
+from test_delta import BF, F, GATE_TOL, L, TOL, f64, inputs, recurrence, tol  # noqa: F401  (L: the fixture)
 
 
 def by(parts, got, want):
@@ -23,6 +23,10 @@ def by(parts, got, want):
 
 def chunks(n):
     return [np.s_[:, :, t:t + 64] for t in range(0, n, 64)]
+
+
+def heads(H):
+    return [np.s_[:, h] for h in range(H)]
 
 
 def gradients(L, x, Hk, lens=None):
@@ -60,6 +64,35 @@ def test_chunks_of_nothing_or_little(L, io, d, which, size, where, state):
     for name, t in got.items():
         parts = [np.s_[:]] if name in ("S1", "dS0") else chunks(n)
         assert by(parts, t, ref[name]) < tol(name, t.dtype), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
+@pytest.mark.parametrize("d,dv,lens", [(64, 64, None), (128, 128, [200, 77]), (40, 24, None)])
+def test_strong_gates(L, io, d, dv, lens):
+    """Gates that forget nearly everything at every token: their gradients are as small as exp(gate), and as exact."""
+    rates = [-3.0, -5.0, -8.0, -12.0, -30.0]
+    H, n, B = len(rates), 200, 2
+    x = list(inputs(B, H, H, n, d, dv, io, "heads", 13, True))
+    x[4] = torch.tensor(rates, device="cuda").view(1, H, 1).expand(B, H, n).to(io).contiguous()
+    got, ref = gradients(L, x, H, lens and np.array(lens))
+    for name, t in got.items():
+        if name != "dS0" and name != "S1":  # (a state behind 200 such tokens is 0 but for the last of them)
+            assert by(heads(H), t, ref[name]) < tol(name, t.dtype), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
+def test_gates_strong_and_weak(L, io):
+    """A strong gate at every fifth token among weak ones, and gates that grow from 0 to -20 along the sequence: the
+    gradients of the strong ones on their own."""
+    H, n, d = 2, 250, 64
+    x = list(inputs(1, H, H, n, d, d, io, "heads", 19, True))
+    x[4][:, 0, ::5] = -9.0
+    x[4][:, 1] = -torch.linspace(0, 20, n, device="cuda").to(io)
+    got, ref = gradients(L, x, H)
+    parts = [np.s_[:, 0, ::5], np.s_[:, 0, 1::5], *(np.s_[:, 1, t:t + 50] for t in range(0, n, 50))]
+    assert by(parts, got["dlog_decay"], ref["dlog_decay"]) < GATE_TOL[io]
 
 
 @pytest.mark.gpu
