@@ -1,4 +1,5 @@
-"""The gated delta rule where its parts are of very different size: chunks without queries, keys or gradients, strong gates.
+"""The gated delta rule where its parts are of very different size: chunks without queries, keys or gradients, strong
+gates; and forms of the chain that only many heads reach.
 
 Tolerances are those of test_delta.py, taken chunk by chunk or head by head instead of over whole tensors: they come
 from the rounding of single values and of the operands of a product, which is the same for any 64 rows.
@@ -109,3 +110,80 @@ def test_zero_keys_under_gates(L, io):
     rows = [np.s_[:, h, t:t + 1] for h in range(H) for t in range(64, 128)]
     assert by(rows, got["dK"], ref["dK"]) < TOL[io]
     assert by(rows, got["dQ"], 0 * ref["dQ"]) == 0.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,Hk,n,d,dv", [(8, 8, 330, 61, 61), (8, 4, 330, 127, 127), (8, 8, 330, 64, 128), (8, 8, 200, 127, 20), (8, 2, 200, 64, 32)])
+def test_many_heads_of_any_width(L, H, Hk, n, d, dv):
+    """Rows that do not start on 16-byte boundaries, and 128 columns of a state of 64, with every SM at work: against the
+    fp32 form of the same call on the same values, head by head."""
+    B = 24
+    Q, K, V, dO, lg, bt, S0, dS1 = inputs(B, H, Hk, n, d, dv, BF, "tokens", 23, True)
+    lens = torch.randint(n // 2, n + 1, (B,), device="cuda", dtype=torch.int32, generator=torch.Generator("cuda").manual_seed(1))
+    p, f = (L.Delta(B, H, n, d, dv, Hk=Hk, io=io, backward=True) for io in (BF, F))
+    wide = [x.float() for x in (Q, K, V, dO, lg, bt)]
+    want, S = f.forward(*wide[:3], *wide[4:], lens, S0, want_state=True)
+    grads = f.backward(*wide, lens, S0, dS1)
+    got, S1 = p.forward(Q, K, V, lg, bt, lens, S0, want_state=True)
+    pairs = {"O": (got, want), "S1": (S1, S)}
+    pairs.update({k: (v, grads[k]) for k, v in p.backward(Q, K, V, dO, lg, bt, lens, S0, dS1).items()})
+    assert L.luna_device_status(p.ws) == 0
+    for name, (a, b) in pairs.items():
+        by_head = (a.double() - b).flatten(2).norm(dim=2) / b.double().flatten(2).norm(dim=2)
+        assert by_head.max() < tol(name, a.dtype), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,n,d,dv", [(1, 2, 200, 64, 64), (24, 8, 150, 64, 128)])
+def test_unaligned_views_to_the_bit(L, B, H, n, d, dv):
+    """bf16 tensors one element off a 16-byte boundary give the same bits: rows are read and written in other pieces, the
+    sums are the same."""
+    Q, K, V, dO, lg, bt, S0, dS1 = inputs(B, H, H, n, d, dv, BF, "heads", 3, True)
+    odd = [torch.empty(x.numel() + 1, dtype=BF, device="cuda")[1:].view(x.shape).copy_(x) for x in (Q, K, V, dO)]
+    p = L.Delta(B, H, n, d, dv, io=BF, backward=True)
+    assert torch.equal(p.forward(Q, K, V, lg, bt, None, S0), p.forward(*odd[:3], lg, bt, None, S0))
+    a, b = p.backward(Q, K, V, dO, lg, bt, None, S0, dS1), p.backward(*odd, lg, bt, None, S0, dS1)
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [16, 128])
+def test_slow_gates_over_many_bf16_tokens(L, d):
+    """As test_slow_gates_over_many_tokens, on bf16 tensors: the final state of 20000 tokens under slow gates."""
+    H, n = 5, 20000
+    g = torch.Generator("cuda").manual_seed(8)
+    rates = torch.tensor([-1e-6, -1e-5, -1e-4, -1e-3, -0.49], device="cuda")
+    q, v = (torch.rand((1, H, n, 16), generator=g, device="cuda").to(BF) for _ in range(2))
+    k = torch.rand((1, H, n, d), generator=g, device="cuda")
+    k = (k / k.norm(dim=-1, keepdim=True)).to(BF)
+    q = q if d == 16 else k
+    lg, bt = rates.view(1, H, 1).expand(1, H, n).to(BF).contiguous(), torch.full((1, H, n), 1e-3, device="cuda").to(BF)
+    want = recurrence(*(f64(x) for x in (q, k, v, lg, bt)), d ** -0.5)
+    _, prompt = L.Delta(1, H, n, d, 16, io=BF).forward(q, k, v, lg, bt, want_state=True)
+    p, state, o = L.Delta(1, H, 1, d, 16, io=BF), torch.zeros((1, H, d, 16), device="cuda"), None
+    for t in range(n):
+        o = p.step(q[:, :, t], k[:, :, t], v[:, :, t], lg[:, :, t], bt[:, :, t], state, o=o)
+    for got in (prompt, state):
+        assert by(heads(H), got, want["S1"]) < TOL[F]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 4, 5])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_not_finite_fp32(L, which, value):
+    """A value that is not finite shows in its row's outputs or gradients, and stays in its sequence and head."""
+    B, H, n, d = 2, 2, 150, 64
+    x = list(inputs(B, H, H, n, d, d, F, "tokens", 6, False)[:6])  # Q, K, V, dO, gates, betas
+    p = L.Delta(B, H, n, d, d, io=F, backward=True)
+
+    def run():
+        return {"O": p.forward(x[0], x[1], x[2], x[4], x[5]), **p.backward(x[0], x[1], x[2], x[3], x[4], x[5])}
+
+    want = run()
+    x[which][1, 0, 70].view(-1)[0] = value
+    got = run()
+    for name in got:
+        for b, h in ((0, 0), (0, 1), (1, 1)):
+            assert torch.equal(got[name][b, h], want[name][b, h]), name
+    assert any(not torch.isfinite(got[name][1, 0, 70].float()).all() for name in got)
