@@ -132,7 +132,9 @@ struct BeamArgs {
 // (there are K as good, and at most K threads have some), of the others too; a few dozen values are sorted at the end,
 // or before, where the kept ones run out of room (values that rise along a row).
 // Few rows come in pieces of 2048 values, so that more SMs share them.  The next piece is on its way to shared memory
-// meanwhile, each thread's own part of it.  36 us for 256 rows of 128256 bf16 values (1.8 TB/s), where the exponentials and
+// meanwhile, each thread's own part of it.  Which thread takes which tokens does not hang on where the row starts, so that rows of
+// equal values have equal sums and their beams are ordered by their place: where a row does not start on a 16-byte
+// boundary, a thread's values lie in two vectors, the second of which its neighbour has.  36 us for 256 rows of 128256 bf16 values (1.8 TB/s), where the exponentials and
 // comparisons take the time; 8 us for 4 rows of 50257, the chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
@@ -144,23 +146,25 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     const int tid = threadIdx.x, row = blockIdx.y, part = blockIdx.x;
     if (a.done && a.done[row]) return;
     const T *x = static_cast<const T *>(a.logits) + row * a.ld;
-    // vectors that start on 16-byte boundaries: the first may begin before the row
-    const int off = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));
-    const int vectors = (a.V + off + VEC - 1) / VEC, pieces = (vectors + PIECE / VEC - 1) / (PIECE / VEC);
+    const int off = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));  // of the row from the 16-byte boundary before it
+    const int pieces = (a.V + PIECE - 1) / PIECE;
     const int first = (int)((int64_t)pieces * part / a.S), last = (int)((int64_t)pieces * (part + 1) / a.S);
     float top = -INFINITY, sum = 0.0f;
     RowKey bar;  // K candidates are at least as good (none: v = 0)
     auto floor_of = [](const RowKey &k) { return k.v ? unordered((uint32_t)(k.v >> 32)) : -INFINITY; };
-    extern __shared__ uint4 ahead[];  // [2][NV][kThreads]
-    auto first_of = [&](int piece, int j) { return (piece * (PIECE / VEC) + j * kThreads + tid) * VEC - off; };  // every 256th vector
+    extern __shared__ uint4 ahead[];  // [2][NV][kThreads], behind them [2][NV][kThreads / 32]
+    uint4 *const beside = ahead + 2 * NV * kThreads;  // what comes behind a warp's vectors
+    auto first_of = [&](int piece, int j) { return (piece * (PIECE / VEC) + j * kThreads + tid) * VEC; };  // every 256 VEC tokens
+    auto fetch_one = [&](uint4 *to, int t) {  // from a 16-byte boundary, where all of it is the row's
+        if (t >= 0 && t + VEC <= a.V)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(x + t) : "memory");
+    };
     auto fetch = [&](int piece) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int t = first_of(piece, j);
-            if (t >= 0 && t + VEC <= a.V) {
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(&ahead[(((piece - first) & 1) * NV + j) * kThreads + tid]);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(x + t) : "memory");
-            }
+            const int t = first_of(piece, j) - off, at = ((piece - first) & 1) * NV + j;
+            fetch_one(&ahead[at * kThreads + tid], t);
+            if (off && tid % 32 == 31) fetch_one(&beside[at * (kThreads / 32) + tid / 32], t + VEC);
         }
     };
     if (first < last) fetch(first);
@@ -172,9 +176,26 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
         auto token = [&](int i) { return first_of(piece, i / VEC) + i % VEC; };
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int t = token(j * VEC);
-            if (t >= 0 && t + VEC <= a.V) {
-                const uint4 w = ahead[(((piece - first) & 1) * NV + j) * kThreads + tid];
+            const int t = token(j * VEC), at = ((piece - first) & 1) * NV + j;
+            uint4 w = ahead[at * kThreads + tid];
+            if (off) {  // (the same for the whole block) the values from `off` on, of two vectors
+                uint32_t u[8] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[4 + i] = __shfl_down_sync(0xffffffffu, u[i], 1);
+                if (tid % 32 == 31) {
+                    const uint4 next = beside[at * (kThreads / 32) + tid / 32];
+                    u[4] = next.x; u[5] = next.y; u[6] = next.z; u[7] = next.w;
+                }
+                const int bytes = off * (int)sizeof(T);
+#pragma unroll
+                for (int i = 0; i < 6; ++i) u[i] = bytes & 8 ? u[i + 2] : u[i];
+#pragma unroll
+                for (int i = 0; i < 5; ++i) u[i] = bytes & 4 ? u[i + 1] : u[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = __funnelshift_r(u[i], u[i + 1], bytes % 4 * 8);
+                w = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+            if (off ? t >= off && t - off + 2 * VEC <= a.V : t + VEC <= a.V) {
                 T e[VEC];
                 memcpy(e, &w, 16);
 #pragma unroll
@@ -182,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i)
-                    val[j * VEC + i] = t + i >= 0 && t + i < a.V ? io_load(x + t + i) : -INFINITY;
+                    val[j * VEC + i] = t + i < a.V ? io_load(x + t + i) : -INFINITY;
             }
         }
         float m = -INFINITY;
@@ -198,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
         auto key = [&](int i, float v) {
             const int t = token(i);
             RowKey k;
-            if (t >= 0 && t < a.V && v == v) k.v = (uint64_t)ordered(v + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
+            if (t < a.V && v == v) k.v = (uint64_t)ordered(v + 0.0f) << 32 | (uint32_t)~t;  // (-0 is 0)
             return k;
         };
         auto best_of_thread = [&]() {  // the first of its largest (tokens rise with i) that is a token's
@@ -206,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
             int at = -1;
 #pragma unroll
             for (int i = PER - 1; i >= 0; --i)
-                if (val[i] == m && token(i) >= 0 && token(i) < a.V) at = i;
+                if (val[i] == m && token(i) < a.V) at = i;
             if (at >= 0) k = key(at, m);
             return k;
         };
@@ -244,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
         while (mask) {  // (few: their values are read again)
             const int i = __ffs(mask) - 1, t = token(i);
             mask &= mask - 1;
-            if (t < 0 || t >= a.V) continue;
+            if (t >= a.V) continue;
             const RowKey c = key(i, io_load(x + t));
             if (c.v && !bar.over(c)) pool[atomicAdd(&count, 1)] = c;
         }
@@ -413,7 +434,7 @@ struct Cut {
     int per, parts;
 };
 Cut cut(const luna_beam_desc *bd) {
-    const int64_t rows = std::max<int64_t>(1, (int64_t)bd->B * bd->K), sms = tc_sm_count(), V = (int64_t)bd->V + 8;
+    const int64_t rows = std::max<int64_t>(1, (int64_t)bd->B * bd->K), sms = tc_sm_count(), V = bd->V;
     const int large = bd->io == LUNA_F32 ? kPer<float> : kPer<__nv_bfloat16>;
     const int per = rows * cdiv(V, kThreads * large) < sms ? kFew : large;
     const int64_t most = std::max<int64_t>(1, 4 * sms / rows);
@@ -422,7 +443,7 @@ Cut cut(const luna_beam_desc *bd) {
 
 template <typename T, int PER>
 cudaError_t launch_rows(const BeamArgs &a, cudaStream_t s) {
-    const size_t ahead = 2 * sizeof(T) * PER * kThreads;
+    const size_t ahead = 2 * sizeof(T) * PER * (kThreads + kThreads / 32);
     cudaError_t e = cudaFuncSetAttribute(k_beam_rows<T, PER>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ahead);
     if (e != cudaSuccess) return e;
     LUNA_LAUNCH("beam_rows", (k_beam_rows<T, PER>), dim3((unsigned)a.S, (unsigned)(a.B * a.K)), kThreads, ahead, s, a);
