@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     const int off = (int)((reinterpret_cast<uintptr_t>(x) % 16) / sizeof(T));  // of the row from the 16-byte boundary before it
     const int pieces = (a.V + PIECE - 1) / PIECE;
     const int first = (int)((int64_t)pieces * part / a.S), last = (int)((int64_t)pieces * (part + 1) / a.S);
-    float top = -INFINITY, sum = 0.0f;
+    float top = -INFINITY, sum = 0.0f, rest = 0.0f;  // rest: what roundings of the sum left
     RowKey bar;  // K candidates are at least as good (none: v = 0)
     auto floor_of = [](const RowKey &k) { return k.v ? unordered((uint32_t)(k.v >> 32)) : -INFINITY; };
     extern __shared__ uint4 ahead[];  // [2][NV][kThreads], behind them [2][NV][kThreads / 32]
@@ -210,10 +210,14 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
 #pragma unroll
         for (int i = 0; i < PER; ++i) m = fmaxf(m, val[i]);
         const float now = fmaxf(top, m), shift = now == -INFINITY ? 0.0f : now;
-        float part_sum[4] = {sum * power2((top - shift) * kLog2e), 0.0f, 0.0f, 0.0f};
+        float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < PER; ++i) part_sum[i % 4] += power2((val[i] - shift) * kLog2e);
-        sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+        // one addition to the sum a piece, and its rounding kept: beside a large value thousands of small ones would be cut off
+        const float scale = power2((top - shift) * kLog2e), more = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+        const float was = sum * scale, total = was + more, added = total - was;
+        rest = fmaf(rest, scale, (was - (total - added)) + (more - added));
+        sum = total;
         top = now;
         // the key of a value, or none: behind the row's ends, or a NaN (k_beam_join sees by the sum that such a row has no scores)
         auto key = [&](int i, float v) {
@@ -278,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     float m = top;
 #pragma unroll
     for (int w = 16; w > 0; w /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
-    float s = sum * power2((top - (m == -INFINITY ? 0.0f : m)) * kLog2e);
+    float s = (sum + rest) * power2((top - (m == -INFINITY ? 0.0f : m)) * kLog2e);
 #pragma unroll
     for (int w = 16; w > 0; w /= 2) s += __shfl_xor_sync(0xffffffffu, s, w);
     if (tid % 32 == 0) { smax[tid / 32] = m; ssum[tid / 32] = s; }
