@@ -383,8 +383,10 @@ luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, c
  * multiple of Hk): head h reads head h / (H / Hk).  log_decay (g) and beta are
  * (B, H, n) tensors of type io with strides of their own (g, beta; all three 0:
  * contiguous); g = -inf (a = 0: the state starts anew) is valid and takes a
- * gradient of 0.  Keys are meant to have length one and beta to lie in [0, 2];
- * with beta |k|^2 above 2 the recurrence itself grows, and nothing checks that.
+ * gradient of 0; values above 0 grow without a check, and with bf16 tensors lose
+ * their bits where they add up to more than about 10 within 64 tokens.  Keys are
+ * meant to have length one and beta to lie in [0, 2]; with beta |k|^2 above 2 the
+ * recurrence itself grows, and nothing checks that.
  * Rows at or past a sequence's length neither enter the state nor are read; their
  * outputs and gradients are 0.  A value that is not finite in a valid row may
  * reach any valid row of the sequence.
@@ -392,8 +394,11 @@ luna_status luna_decay_step(const luna_decay_desc *dd, const float *log_decay, c
  * 64 rows in all; empty problems are no-ops (n = 0 copies the initial state).
  * bf16 runs on tensor cores, in chunks of 64 rows whose operands are scaled fp16
  * values: outputs and gradients are as near to their definition as their own
- * rounding lets them be (1.7e-3), states 3e-7; rows that start on 16-byte
- * boundaries, with d and dv multiples of 8, are read and written in vectors.
+ * rounding lets them be (1.7e-3; their sums hold operands of 11 bits, some 3e-4),
+ * states 3e-7 (one that all but vanishes within 64 tokens 2^-30 of what it and
+ * their rows were); what is less than 2^-26 of the largest value of its kind in 64
+ * tokens may lose bits.  Rows that start on 16-byte boundaries, with d and dv
+ * multiples of 8, are read and written in vectors.
  * fp32 runs on CUDA cores. */
 typedef struct {
     int B, H, Hk, n, d, dv;
@@ -405,7 +410,9 @@ typedef struct {
 
 /* Bytes of scratch memory of luna_delta_fwd (backward = 0) or luna_delta_bwd
  * (1); the workspace must be 256-byte aligned.  The size does not depend on the
- * strides. */
+ * strides.  At d = dv = 128 with bf16 tensors it is 58 KB for each 64 tokens of a
+ * head (3.6 times one of the tensors), with gradients 178 KB (11 times; up to 48 KB
+ * more where heads share queries and keys); with fp32 tensors nothing, and 194 KB. */
 luna_status luna_delta_workspace_size(const luna_delta_desc *dd, int backward, size_t *bytes);
 
 /* Whole prompts.  S0: NULL (zero) or the initial states, fp32 [B][H][d][dv];
@@ -444,7 +451,10 @@ luna_status luna_delta_step(const luna_delta_desc *dd, const void *log_decay, co
  *
  * over all k and t, best first: their scores (fp32), tokens and parent beams
  * (int32, B x K).  Scores are compared in 64 bits; equal ones go by the lower
- * beam, then the lower token.  A beam of score -inf (one that is not in use yet),
+ * beam, then the lower token.  Within a beam that is the order of its logits as
+ * they came.  A row's sum of exponentials is taken in fp32 (off by 1e-6 at most,
+ * and the same for rows of equal values), so that candidates of different beams
+ * nearer to each other than that may come in either order.  A beam of score -inf (one that is not in use yet),
  * with a score or a logit that is NaN or +inf, or whose logits are all -inf, has
  * candidates of score -inf alone, which come behind all others.
  * end: the token that ends a sequence, or -1 (none; done and done_out are then

@@ -134,8 +134,9 @@ struct BeamArgs {
 // Few rows come in pieces of 2048 values, so that more SMs share them.  The next piece is on its way to shared memory
 // meanwhile, each thread's own part of it.  Which thread takes which tokens does not hang on where the row starts, so that rows of
 // equal values have equal sums and their beams are ordered by their place: where a row does not start on a 16-byte
-// boundary, a thread's values lie in two vectors, the second of which its neighbour has.  36 us for 256 rows of 128256 bf16 values (1.8 TB/s), where the exponentials and
-// comparisons take the time; 8 us for 4 rows of 50257, the chain of one piece.
+// boundary, a thread's values lie in two vectors, the second of which its neighbour has.  34 us for 256 rows of 128256 bf16 values (1.8 TB/s), 38 % of the
+// issue slots used: a piece's instructions are some 15 us of it, the rest waits at the sorts of a block's first piece and
+// of its end, at barriers, and for blocks (512 where the SMs hold 608); 8 us for 4 rows of 50257, the chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
     constexpr int VEC = 16 / sizeof(T), NV = PER / VEC, PIECE = kThreads * PER;
@@ -297,10 +298,11 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
     }
 }
 
-// The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that which of two near ones is better
-// does not hang on a rounding: 64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once
-// and a candidate costs two sums (exponentials and logarithms by a warp a row took 16 to 37 us, so 8 to 16).  One block a sequence:
-// K S K candidates, which its warps sort 32 at a time.
+// The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that two of one beam come in the order of
+// their logits; the logarithm is that of a sum in fp32, so that two of different beams may come in either order where they
+// are nearer than 1e-6.  64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once and a
+// candidate costs two sums (exponentials and logarithms by a warp a row took 16 to 37 us, so 9 to 17).  One block a
+// sequence: K S K candidates, which its warps sort 32 at a time.
 __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
     __shared__ SeqKey list[kThreads];
     __shared__ double base[kMaxBeams];  // score - log sum exp(logit - most)

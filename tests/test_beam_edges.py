@@ -9,6 +9,7 @@ import math
 import pytest
 import torch
 
+import test_beam
 from test_beam import BF, F, L, check, inputs  # noqa: F401  (L: the fixture)
 
 
@@ -41,3 +42,38 @@ def test_peaked_rows(L, io, B, K, V, low):
     others = (V - 1) * math.exp(low)
     bound = 25 * 2.0 ** -24 + 2.0 ** -19 * others / (1 + others) + 2.0 ** -24 * math.log1p(others)
     assert (got["scores"][:, 0].double() + math.log1p(others)).abs().max() < bound
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [F, BF])
+@pytest.mark.parametrize("K,V", [(2, 128256), (8, 50257), (32, 5001)])
+def test_near_beams(L, io, K, V):
+    """Beams with the same words in other orders, whose scores lie four times as far apart as their sums may be off, are told
+    apart."""
+    g = torch.Generator("cuda").manual_seed(K)
+    row = (torch.randn(V, generator=g, device="cuda") * 2).to(io)
+    row[5] = 20.0  # (ahead of the others by more than all the beams' scores are apart)
+    logits = torch.stack([row[torch.randperm(V, generator=g, device="cuda")] for _ in range(K)])
+    order = torch.randperm(K, generator=g, device="cuda")
+    scores = torch.empty((1, K), device="cuda")
+    scores[0, order] = -3.0 - 12e-6 * torch.arange(K, device="cuda", dtype=F)
+    got = L.Beam(1, K, V, io=io).select(logits, scores)
+    assert torch.equal(got["parents"][0].long(), order)
+    assert torch.equal(got["tokens"][0].long(), logits.argmax(1)[order])
+
+
+@pytest.mark.gpu
+def test_select_has_no_near_beams(L):
+    """The cases of test_beam.py's test_select, whose order is compared as it is: no two candidates of different beams that
+    are among the best lie within ten times the bound."""
+    (cases,) = (m.args[1] for m in test_beam.test_select.pytestmark if m.name == "parametrize")
+    for B, K, V, io, off in cases:
+        logits, scores, done = inputs(B, K, V, io, V + K, off=off)
+        each = torch.log_softmax(logits.double().view(B, K, V), -1) + scores.double()[..., None]
+        stay = torch.full_like(each, -math.inf)
+        stay[:, :, min(2, V - 1)] = scores.double()
+        for c in (each, torch.where(done[..., None], stay, each)):
+            best, at = c.view(B, -1).topk(min(K + 1, K * V))
+            apart = (best[:, :-1] - best[:, 1:]) / best[:, :-1].abs().clamp(min=1)
+            other = (at[:, :-1] // V != at[:, 1:] // V) & torch.isfinite(apart)
+            assert (apart[other] > 1e-5).all(), (B, K, V)
