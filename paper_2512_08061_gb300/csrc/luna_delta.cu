@@ -321,10 +321,11 @@ __global__ void __launch_bounds__(COLS / CPL * 8 + kLoaders, JD == 4 ? 2 : 3) k_
 }
 
 // ---------------------------------------------------------------------------
-// Gradients of q, k and the gates from the states at the two ends of a chunk: seven products of 64 rows, each
-// thread with 4 rows and two times 4 columns of them, two multiply-adds an instruction.  The operands come from L2 in
-// steps of 16 of the summed index; bound by that and its barriers: 872 us for 2048 chunks of 128 x 128 (every 16th column
-// a thread's, one multiply-add an instruction: 1140 us), 91 us for 300 of 40 x 72.
+// Gradients of q, k and the gates from the states at the two ends of a chunk: four products of 64 x 64 and seven of 64 rows by
+// d columns, each thread with 4 rows and one or two times 4 columns of them, two multiply-adds an instruction.  The
+// operands come from L2 in steps of 16 of the summed index; bound by that and its barriers: 102 us for 300 chunks of
+// 40 x 72.  (91 us with a gate's gradient as a difference of sums over the rows, without the products q_i . k_j and
+// k_i . k_j; of that form every 16th column a thread's and one multiply-add an instruction took 1.3 times as long.)
 
 constexpr int kGradThreads = 256, kGradK = 16;
 

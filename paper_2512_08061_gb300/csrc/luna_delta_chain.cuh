@@ -534,8 +534,10 @@ cudaError_t chain_launch(const DeltaArgs &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-// With few heads, few columns a block and two warps for 16 of them, so that the chains spread over the SMs.  (Rows that
-// do not start on 16-byte boundaries: no blocks of all 128 columns.)
+// With few heads, few columns a block and two warps for 16 of them, so that the chains spread over the SMs; states of at most
+// 32 columns always that way, however many heads (not measured against others).  (Rows that do not start on 16-byte
+// boundaries: no blocks of all 128 columns.)  On 152 SMs at 128 columns the forms change at 39 and 77 heads in all; times
+// were taken at 32 and 128 (above), none in between, where half of the SMs' quarters have no warp.
 template <int DP, ChainMode MODE>
 cudaError_t chain(const DeltaArgs &a, cudaStream_t s) {
     const int64_t bh = (int64_t)a.B * a.H, sms = tc_sm_count();

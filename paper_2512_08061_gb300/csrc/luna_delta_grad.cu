@@ -8,10 +8,11 @@ using namespace delta;
 
 // ---------------------------------------------------------------------------
 // Gradients of q, k and the gates (luna_delta.cuh) from the chunk's U, X, dO and states.  A block of eight warps a chunk:
-// two groups of 32 rows by four quarters of the columns.  102 KB of shared memory, so that two blocks are on an SM and
-// the one's products cover the other's loads: R, then S, then Q lie in the same place, P and W in that of U.  466 us for
-// 8192 chunks of 128 x 128 (with everything in place at once, 16 warps and one block an SM 804 us); bound by the waits
-// between those.
+// two groups of 32 rows by four quarters of the columns.  107 KB of shared memory, so that two blocks are on an SM and
+// the one's products cover the other's loads: R, then S, then Q lie in the same place, P and W in that of U.  546 us for
+// 8192 chunks of 128 x 128; bound by the waits between those.  (466 us with P and W in one unit, which loses dQ where a chunk's
+// queries or keys are 0, and with a gate's gradient as a difference, which loses it where the gate is strong; of that form, with
+// everything in place at once, 16 warps and one block an SM 804 us.)
 
 constexpr int kGradThreads = 256, kParts = 4;
 

@@ -29,7 +29,8 @@ struct PrepShared {
     float hi[C], lo[C], past[C], left[C], b[C], tail[C], most[5][kPrepThreads / 32], back_T[4];  // tail: c(last of its 16, j)
 };
 
-// A thread's 16-byte pieces of a bf16 tile, as they lie in memory: their largest value; in fp16 to `out`
+// A thread's 16-byte pieces of a bf16 tile, as they lie in memory: their largest value (prep_most), and they themselves in
+// fp16 to `out` (prep_write)
 template <int DP>
 __device__ __forceinline__ float prep_most(const char *tile, int tid) {
     uint32_t most = 0;

@@ -22,7 +22,8 @@
 // enter products in two terms, T and (in reverse) P too, so that states and U are off by a few 1e-7; the outputs take
 // one term of S, U and P (1.4e-4, under their own rounding).  K, Q, T and P are scaled by chunk, to a largest value of
 // 2^12 to 2^13, what a warp holds by its own largest value, so that whatever is 2^-15 of its neighbours still has
-// its 22 bits; K, Q and dO are exact down to 2^-26 of their tile's largest value.  What a chunk adds to the
+// its 22 bits, and a state that all but vanishes within a chunk is off by 2^-35 of what was in its place; K, Q and dO are
+// exact down to 2^-26 of their tile's largest value.  What a chunk adds to the
 // state is summed by itself and added in fp32, because the tensor cores cut sums off.
 #pragma once
 
