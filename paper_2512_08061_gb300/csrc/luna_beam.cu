@@ -135,7 +135,7 @@ struct BeamArgs {
 // meanwhile, each thread's own part of it.  Which thread takes which tokens does not hang on where the row starts, so that rows of
 // equal values have equal sums and their beams are ordered by their place: where a row does not start on a 16-byte
 // boundary, a thread's values lie in two vectors, the second of which its neighbour has.  34 us for 256 rows of 128256 bf16 values (1.8 TB/s), 38 % of the
-// issue slots used: a piece's instructions are some 15 us of it, the rest waits at the sorts of a block's first piece and
+// issue slots used: a piece's instructions are some 13 us of it, the rest waits at the sorts of a block's first piece and
 // of its end, at barriers, and for blocks (512 where the SMs hold 608); 8 us for 4 rows of 50257, the chain of one piece.
 template <typename T, int PER>
 __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(BeamArgs a) {
