@@ -452,11 +452,12 @@ luna_status luna_delta_step(const luna_delta_desc *dd, const void *log_decay, co
  * over all k and t, best first: their scores (fp32), tokens and parent beams
  * (int32, B x K).  Scores are compared in 64 bits; equal ones go by the lower
  * beam, then the lower token.  Within a beam that is the order of its logits as
- * they came.  A row's sum of exponentials is taken in fp32 (off by 1e-6 at most,
- * and the same for rows of equal values), so that candidates of different beams
- * nearer to each other than that may come in either order.  A beam of score -inf (one that is not in use yet),
- * with a score or a logit that is NaN or +inf, or whose logits are all -inf, has
- * candidates of score -inf alone, which come behind all others.
+ * they came.  A row's sum of exponentials is taken in fp32 (off by some 1e-6 in the
+ * worst rows, and the same for rows of equal values), so that candidates of
+ * different beams nearer to each other than that may come in either order.  A beam
+ * of score -inf (one that is not in use yet), with a score or a logit that is NaN
+ * or +inf, or whose logits are all -inf, has candidates of score -inf alone, which
+ * come behind all others.
  * end: the token that ends a sequence, or -1 (none; done and done_out are then
  * NULL).  done: NULL (none) or B x K bytes, not 0 where a beam has ended: its
  * logits are not read, and its one candidate is itself with the token `end` and

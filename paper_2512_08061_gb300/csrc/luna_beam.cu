@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, PER == kFew ? 1 : 4) k_beam_rows(Bea
 
 // The K best of a sequence from its rows' candidates.  Scores are in 64 bits, so that two of one beam come in the order of
 // their logits; the logarithm is that of a sum in fp32, so that two of different beams may come in either order where they
-// are nearer than 1e-6.  64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once and a
+// are nearer than some 1e-6.  64-bit arithmetic is scarce here, so one warp takes the logarithms of all rows at once and a
 // candidate costs two sums (exponentials and logarithms by a warp a row took 16 to 37 us, so 9 to 17).  One block a
 // sequence: K S K candidates, which its warps sort 32 at a time.
 __global__ void __launch_bounds__(kThreads) k_beam_join(BeamArgs a) {
